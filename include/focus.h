@@ -10,6 +10,9 @@
  *   focus_compact_kv                   append summary K/V rows to the cache
  *   focus_window_attn                  window attention over [cache ; window]
  *   focus_decode_step                  one-token decode over [cache ; window]
+ *   focus_rope                         rotary positions, rows stored in a paged cache
+ *   focus_paged_decode                 one-token attention over a paged cache
+ *   focus_paged_evict                  a paged cache cut down to a budget
  *
  * Conventions shared by every call
  * --------------------------------
@@ -91,7 +94,8 @@ int32_t focus_abi_version(void);
 const char* focus_status_str(focus_status s);
 /* sizeof of the descriptor structs below, in declaration order
  * (0 totals, 1 layout, 2 compact, 3 attn, 4 decode, 5 fidelity, 6 gemm,
- * 7 adapter, 8 adapter layer, 9 qkv projection, 10 decode schedule); -1
+ * 7 adapter, 8 adapter layer, 9 qkv projection, 10 decode schedule,
+ * 11 rope scaling, 12 paged cache, 13 rope, 14 paged decode, 15 paged evict); -1
  * otherwise.
  * Lets a binding check its mirror of the structs. */
 int64_t focus_struct_size(int32_t which);
@@ -664,6 +668,198 @@ typedef struct {
 } focus_qkv_desc;
 
 focus_status focus_qkv_project(const focus_qkv_desc* d, focus_stream_t stream);
+
+/* ------------------------------------------------------------------------ */
+/* Rotary positions                                                          */
+/* ------------------------------------------------------------------------ */
+
+/* Frequencies of the rotary pairs of a head, in turns (revolutions) per
+ * position: turns[i] = theta^(-2i/R) / (2 pi), 0 <= i < R/2 for R = rot_dim
+ * turned elements, then scaled for contexts longer than the trained one:
+ *   FOCUS_ROPE_NONE    as they are
+ *   FOCUS_ROPE_LINEAR  turns[i] / factor (positions interpolated)
+ *   FOCUS_ROPE_BASE    theta replaced by theta * factor^(R / (R - 2)), which
+ *                      leaves the fastest pair as it is and divides the slowest by
+ *                      factor (R >= 4)
+ *   FOCUS_ROPE_BANDS   by how often a pair turns over the trained context, r =
+ *                      context * turns[i]: with g = (r - low) / (high - low) clipped
+ *                      to [0, 1], turns[i] ((1 - g) / factor + g): slow pairs are
+ *                      interpolated, fast ones left (YaRN, arXiv 2309.00071; its
+ *                      attention temperature is focus_rope_desc.amplitude) */
+enum { FOCUS_ROPE_NONE = 0, FOCUS_ROPE_LINEAR = 1, FOCUS_ROPE_BASE = 2, FOCUS_ROPE_BANDS = 3 };
+
+typedef struct {
+  int32_t kind;                 /* FOCUS_ROPE_NONE .. FOCUS_ROPE_BANDS       */
+  int32_t rot_dim;              /* R, even, 2 .. 256                         */
+  double theta;                 /* > 1                                       */
+  double factor;                /* >= 1 (any kind but NONE)                  */
+  double context;               /* trained positions, > 0 (BANDS)            */
+  double low, high;             /* 0 <= low < high (BANDS)                   */
+} focus_rope_scaling;
+
+/* Fill turns [host][rot_dim / 2].  Errors: E_NULL, E_ARG. */
+focus_status focus_rope_turns(const focus_rope_scaling* s, double* turns);
+
+/* A paged K/V cache.  Row r of sequence b is row r % page_rows of page
+ * table[b * max_pages + r / page_rows]; element e of head g of row x of page p lies
+ * at p * page_stride + x * row_stride + g * head_stride + e, so that pages may hold
+ * [page_rows, H_kv, D] or [H_kv, page_rows, D], alone or beside other data.  Pages may
+ * be shared between sequences where they are only read.  Table entries past a
+ * sequence's last page are not read.  weight, where given, holds one accumulated
+ * attention weight per row of a sequence and KV head.  All arrays [device]. */
+typedef struct {
+  int32_t dtype;
+  int32_t n_kv_heads;
+  int32_t head_dim;             /* at most 256, whole 16-byte pieces         */
+  int32_t page_rows;            /* a power of two, 8 .. 1024                 */
+  int64_t n_pages;
+  void* k;
+  void* v;
+  int64_t page_stride;          /* elements, >= head_dim, whole 16-byte      */
+  int64_t row_stride;           /*   pieces; no two rows may overlap         */
+  int64_t head_stride;
+  int32_t batch;
+  int32_t max_pages;            /* entries of a sequence in table            */
+  const int32_t* table;         /* [batch, max_pages]                        */
+  int32_t* length;              /* [batch] rows cached                       */
+  float* weight;                /* [batch, n_kv_heads, weight_rows] or NULL  */
+  int64_t weight_rows;          /* >= max_pages * page_rows                  */
+} focus_paged_kv;
+
+/* Which elements of a head's first R form pair i: (2i, 2i + 1), or (i, i + R/2). */
+enum { FOCUS_ROPE_INTERLEAVED = 0, FOCUS_ROPE_HALF = 1 };
+
+/* Rotary positions of n_rows rows of queries and / or keys:
+ *     a        = 2 pi pos[t] turns[i]   (product and fraction in float64)
+ *     (x', y') = amplitude (x cos a - y sin a, x sin a + y cos a)   for every pair i
+ * and the elements from rot_dim on as they are.  inverse: a replaced by -a, which is
+ * the transpose of the map and so its backward pass (gradients of q' and k' in,
+ * gradients of q and k out).  Arithmetic is float32, rounded once.
+ *
+ * Into a paged cache (cache != NULL, inverse == 0): the turned k row t and the row t
+ * of v are stored at row row_slot[t] of sequence row_seq[t] (a negative slot stores
+ * nothing), cache->length raised (never lowered) past it, and its weights, where the
+ * cache has them, set to 0.  No two rows may have one slot, nor lie in a page that
+ * two sequences share.  rot_dim 0 stores k as it is (rows that
+ * focus_qkv_project has turned already).
+ *
+ * q, k, v are optional one by one (NULL): k_out needs k, v needs cache, cache needs k
+ * and v.  Rows may lie anywhere: row t of head h at t * row_stride + h * head_stride,
+ * so that q, k, v may be views of one projection.  Rows of an output may not overlap;
+ * an output may be its own input (same strides). */
+typedef struct {
+  int32_t dtype;
+  int32_t n_heads;              /* of q (ignored if NULL)                    */
+  int32_t n_kv_heads;           /* of k and v (ignored if both NULL)         */
+  int32_t head_dim;             /* at most 256, whole 16-byte pieces         */
+  int32_t rot_dim;              /* R, even, 0 .. head_dim                    */
+  int32_t pairs;                /* FOCUS_ROPE_INTERLEAVED or FOCUS_ROPE_HALF */
+  int32_t inverse;
+  float amplitude;              /* finite                                    */
+  int64_t n_rows;
+  const int32_t* pos;           /* [device][n_rows], any sign                */
+  const double* turns;          /* [device][rot_dim / 2]                     */
+  const void* q;                /* [device], strides in elements, whole      */
+  int64_t q_row, q_head;        /*   16-byte pieces                          */
+  void* q_out;
+  int64_t qo_row, qo_head;
+  const void* k;
+  int64_t k_row, k_head;
+  void* k_out;                  /* or NULL where the cache takes the rows    */
+  int64_t ko_row, ko_head;
+  const void* v;
+  int64_t v_row, v_head;
+  const focus_paged_kv* cache;  /* [host] or NULL                            */
+  const int32_t* row_seq;       /* [device][n_rows] with cache               */
+  const int32_t* row_slot;
+  int32_t* err;                 /* optional error word                       */
+} focus_rope_desc;
+
+/* Errors: E_NULL, E_ARG, E_DTYPE, E_SHAPE (cache of another head_dim, head count or
+ * dtype), E_UNSUPPORTED, E_HIP.  A row whose sequence is outside the batch or whose
+ * page is outside the pool is not stored (FOCUS_ERR_BOUNDS), nor one whose slot is
+ * past max_pages * page_rows (FOCUS_ERR_CAPACITY); its q_out and k_out are written. */
+focus_status focus_rope(const focus_rope_desc* d, focus_stream_t stream);
+
+/* ------------------------------------------------------------------------ */
+/* Paged decode                                                              */
+/* ------------------------------------------------------------------------ */
+
+/* Attention of one new token of every sequence over its cached rows (the row of the
+ * token itself, stored by focus_rope before, is the last of them):
+ *     o[b, h]   = softmax(scale * q[b, h] . k[b, 0:length[b], g]^T) . v,  g = h / (H / H_kv)
+ *     lse[b, h] = log sum exp(scale * q[b, h] . k)
+ *     weight[b, g, r] = weight_decay * weight[b, g, r] + sum of the softmax weights of
+ *                       row r over the heads of g        (accumulate; rows < length[b])
+ * With weight_decay 0 the old weight is not read.  A sequence of length 0 has o = 0
+ * and lse = -inf.  Rows past the length are never read, so whatever their page holds
+ * has no effect.
+ * The rows of a sequence are split over several workgroups, joined by log-sum-exp;
+ * with split_keys = 0 the split follows the lengths of the whole batch, so that a
+ * sequence's bits may differ by float32 rounding with what else is in the batch; a
+ * given split_keys fixes them.  Results are deterministic. */
+typedef struct {
+  focus_paged_kv cache;         /* bf16 or f32, head_dim 64 or 128           */
+  int32_t n_heads;
+  int32_t split_keys;           /* rows per workgroup, multiple of 128; 0: auto */
+  float softmax_scale;          /* <= 0: 1/sqrt(head_dim)                    */
+  int32_t accumulate;           /* nonzero: add to cache.weight              */
+  float weight_decay;           /* finite                                    */
+  int32_t reserved;
+  const void* q;                /* [batch, n_heads, head_dim], strides in    */
+  int64_t q_row, q_head;        /*   elements, whole 16-byte pieces          */
+  void* o;                      /* [batch, n_heads, head_dim] contiguous     */
+  float* lse;                   /* [batch, n_heads] or NULL                  */
+  void* workspace;
+  size_t workspace_bytes;
+  int32_t* err;
+} focus_paged_decode_desc;
+
+/* Workspace bytes of this descriptor on the current device (0 for one that the call
+ * refuses).  The workspace is in use until the call's kernels end; calls that share
+ * one on overlapping streams race. */
+size_t focus_paged_decode_workspace(const focus_paged_decode_desc* d);
+/* Errors: E_NULL, E_ARG, E_DTYPE, E_SHAPE, E_UNSUPPORTED, E_WORKSPACE, E_HIP.  Rows of
+ * a page outside the pool are left out of the softmax (FOCUS_ERR_BOUNDS; weight of the
+ * step 0); a length outside [0, max_pages * page_rows] is clipped to it
+ * (FOCUS_ERR_CAPACITY). */
+focus_status focus_paged_decode(const focus_paged_decode_desc* d, focus_stream_t stream);
+
+/* ------------------------------------------------------------------------ */
+/* Paged eviction                                                            */
+/* ------------------------------------------------------------------------ */
+
+/* Cut every sequence of a paged cache down to a budget, for each KV head by itself:
+ * of the n = cache.length[b] rows, m = min(n, budget) are kept, the last min(recent, m)
+ * of them and, of the others, those with the greatest cache.weight[b, g] (among equals
+ * the lowest row first; a NaN counts as greater than +inf).  The kept rows, in ascending
+ * order, are copied to rows 0 .. m - 1 of sequence b of `out`, with their weights (where
+ * out has them); out.length[b] = m; keep[b, g, 0:m] = the kept rows, -1 past them.
+ * The copy goes to other pages: a page that another sequence shares stays as it is, and
+ * the old pages are free as a whole afterwards.  `out` may lie in the same pool; a page
+ * in both tables, or twice in out's, is a race.  out.length may be cache.length;
+ * out.weight may not be cache.weight.  Rows of out past m are left as they were. */
+typedef struct {
+  focus_paged_kv cache;         /* with weight                               */
+  focus_paged_kv out;           /* same dtype, heads, head_dim, batch        */
+  int32_t budget;               /* rows kept, >= 0 (ignored with budgets)    */
+  int32_t recent;               /* latest rows always kept, >= 0             */
+  const int32_t* budgets;       /* [device][batch] or NULL                   */
+  int32_t* keep;                /* [device][batch, n_kv_heads, keep_rows]    */
+  int64_t keep_rows;
+  void* workspace;
+  size_t workspace_bytes;
+  int32_t* err;
+} focus_paged_evict_desc;
+
+/* Workspace bytes of this descriptor on the current device (may be 0). */
+size_t focus_paged_evict_workspace(const focus_paged_evict_desc* d);
+/* Errors: E_NULL, E_ARG, E_DTYPE, E_SHAPE, E_UNSUPPORTED, E_WORKSPACE, E_HIP.  Where
+ * keep_rows or out's table hold fewer rows than m, m is what they hold, and a length
+ * outside its table is clipped to it (FOCUS_ERR_CAPACITY for both); a negative budget
+ * counts as 0 and a row from or to a page outside the pool is not copied
+ * (FOCUS_ERR_BOUNDS for both). */
+focus_status focus_paged_evict(const focus_paged_evict_desc* d, focus_stream_t stream);
 
 #ifdef __cplusplus
 }

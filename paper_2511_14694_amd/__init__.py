@@ -12,6 +12,13 @@ the first call raises.
     focus_compact_kv(lay, k, v, cache_k, cache_v, cache_len)     # summary K/V -> cache
     o, lse = focus_window_attn(lay, q, k, v, cache_k, cache_v)   # [cache ; window] attention
     o, lse = focus_decode_step(q, k_new, v_new, kind, ...)       # one decode step
+
+Serving over a paged cache:
+
+    turns  = focus_rope_turns(head_dim)                          # rotary frequencies
+    q, _   = focus_rope(pos, turns, q, k, v, cache=cache, ...)   # turn q and k, store k and v
+    o, lse = focus_paged_decode(q, cache, weight_decay=1.0)      # one token, weights kept
+    keep   = focus_paged_evict(cache, out, budget, recent)       # cut down to a budget
 """
 
 from __future__ import annotations
@@ -23,11 +30,14 @@ from typing import Dict, Optional
 import numpy as np
 import torch
 
-from ._abi import (AdapterDesc, AdapterLayerDesc, AttnDesc, CompactDesc, DecodeDesc, DecodeSched, FidelityDesc, FocusError, GemmDesc, LayoutDesc, LayoutTotals, QkvDesc,
+from ._abi import (AdapterDesc, AdapterLayerDesc, AttnDesc, CompactDesc, DecodeDesc, DecodeSched, FidelityDesc, FocusError, GemmDesc, LayoutDesc, LayoutTotals,
+                   PagedDecodeDesc, PagedEvictDesc, PagedKv, QkvDesc, RopeDesc, RopeScaling,
                    FOCUS_BF16, FOCUS_F32, FOCUS_MASK_CT, FOCUS_MASK_KMER_LOCAL,
                    FOCUS_TOK_BASE, FOCUS_TOK_SUMMARY, FOCUS_STEP_SUMMARY, FOCUS_STEP_WINDOW_END,
                    FOCUS_ERR_CAPACITY, FOCUS_ERR_BOUNDS, FOCUS_ERR_PLAN,
-                   FOCUS_FID_LOGITS, FOCUS_FID_PROBS, FOCUS_FID_N, check, lib)
+                   FOCUS_FID_LOGITS, FOCUS_FID_PROBS, FOCUS_FID_N,
+                   FOCUS_ROPE_NONE, FOCUS_ROPE_LINEAR, FOCUS_ROPE_BASE, FOCUS_ROPE_BANDS,
+                   FOCUS_ROPE_INTERLEAVED, FOCUS_ROPE_HALF, check, lib)
 
 __all__ = ["focus_layout_plan", "focus_layout", "focus_compact_kv", "focus_window_attn",
            "focus_window_attn_workspace", "focus_decode_step", "focus_decode_workspace",
@@ -37,7 +47,11 @@ __all__ = ["focus_layout_plan", "focus_layout", "focus_compact_kv", "focus_windo
            "FOCUS_FID_LOGITS", "FOCUS_FID_PROBS", "FOCUS_FID_N",
            "FOCUS_BF16", "FOCUS_F32", "FOCUS_MASK_CT", "FOCUS_MASK_KMER_LOCAL",
            "FOCUS_TOK_BASE", "FOCUS_TOK_SUMMARY", "FOCUS_STEP_SUMMARY", "FOCUS_STEP_WINDOW_END",
-           "FOCUS_ERR_CAPACITY", "FOCUS_ERR_BOUNDS", "FOCUS_ERR_PLAN"]
+           "FOCUS_ERR_CAPACITY", "FOCUS_ERR_BOUNDS", "FOCUS_ERR_PLAN",
+           "PagedCache", "focus_rope_turns", "focus_rope", "focus_paged_decode", "focus_paged_decode_workspace",
+           "focus_paged_evict", "focus_paged_evict_workspace",
+           "FOCUS_ROPE_NONE", "FOCUS_ROPE_LINEAR", "FOCUS_ROPE_BASE", "FOCUS_ROPE_BANDS",
+           "FOCUS_ROPE_INTERLEAVED", "FOCUS_ROPE_HALF"]
 
 _DTYPES = {torch.bfloat16: FOCUS_BF16, torch.float32: FOCUS_F32}
 
@@ -530,3 +544,225 @@ def focus_qkv_project(lay: Layout, hidden, w_qkv, n_heads: int, n_kv_heads: int,
     d.cache_len, d.err = _ptr(cache_len), _ptr(err)
     check("focus_qkv_project", lib().focus_qkv_project(C.byref(d), _stream(stream, hidden.device)))
     return q, k, v
+
+
+# ------------------------------------------------------------------ paged caches
+
+def _need(t, dtype, shape, dev, what):
+    """t as a contiguous tensor of this dtype, shape (None: any) and device."""
+    if t.dtype != dtype or t.device != dev or not t.is_contiguous() or (shape is not None and t.shape != shape):
+        raise ValueError(f"{what} must be a contiguous {dtype} tensor"
+                         + ("" if shape is None else f" {list(shape)}") + f" on {dev}")
+    return t.data_ptr()
+
+
+def _err_ptr(err, dev):
+    if err is None:
+        return None
+    if err.numel() < 1:
+        raise ValueError("err needs one element")
+    return _need(err, torch.int32, None, dev, "err")
+
+
+def _launch(call: str, d, dev, stream):
+    """Enqueue a call on dev, whichever device is current."""
+    if dev.type != "cuda":
+        raise ValueError(f"{call} needs tensors on a GPU")
+    fn = getattr(lib(), call)
+    if dev.index == torch.cuda.current_device():
+        check(call, fn(C.byref(d), _stream(stream, dev)))
+    else:
+        with torch.cuda.device(dev):
+            check(call, fn(C.byref(d), _stream(stream, dev)))
+
+
+@dataclass
+class PagedCache:
+    """A paged K/V cache (focus_paged_kv): row r of sequence b is row r % page_rows of
+    page table[b, r // page_rows].
+
+    k, v    [n_pages, page_rows, H_kv, D], unit stride in D, any other strides (a
+            transposed [n_pages, H_kv, page_rows, D] too), the same for both;
+            page_rows a power of two, 8 to 1024
+    table   int32 [batch, max_pages]; entries past a sequence's last page are not read
+    length  int32 [batch]: rows cached
+    weight  float32 [batch, H_kv, >= max_pages * page_rows] or None: accumulated
+            attention weight of every row
+    """
+    k: torch.Tensor
+    v: torch.Tensor
+    table: torch.Tensor
+    length: torch.Tensor
+    weight: Optional[torch.Tensor] = None
+
+    def desc(self) -> PagedKv:
+        k, v, dev = self.k, self.v, self.k.device
+        if (k.dim() != 4 or v.shape != k.shape or v.dtype != k.dtype or v.device != dev or v.stride() != k.stride()
+                or k.stride(3) != 1):
+            raise ValueError("k and v must be [n_pages, page_rows, H_kv, D] of one dtype, device and strides, "
+                             "with unit stride in D")
+        n_pages, rows, heads, dim = k.shape
+        if self.table.dim() != 2:
+            raise ValueError("table must be [batch, max_pages]")
+        batch, max_pages = self.table.shape
+        # the stride of a dimension of one element says nothing: replaced by one that passes
+        page, row, head, _ = (dim if n == 1 else st for n, st in zip(k.shape, k.stride()))
+        w, w_rows = None, 0
+        if self.weight is not None:
+            w_rows = self.weight.shape[-1]
+            w = _need(self.weight, torch.float32, (batch, heads, w_rows), dev, "weight")
+        return PagedKv(_dtype(k), heads, dim, rows, n_pages, k.data_ptr(), v.data_ptr(), page, row, head, batch,
+                       max_pages, _need(self.table, torch.int32, None, dev, "table"),
+                       _need(self.length, torch.int32, (batch,), dev, "length"), w, w_rows)
+
+
+def focus_rope_turns(rot_dim: int, theta: float = 10000.0, scaling: int = FOCUS_ROPE_NONE, factor: float = 1.0,
+                     context: float = 0.0, low: float = 1.0, high: float = 32.0, device="cuda"):
+    """Rotary frequencies of a head's rot_dim turned elements, in turns per position:
+    float64 [rot_dim / 2] on device, to be kept by the caller.  scaling
+    (FOCUS_ROPE_*), factor, context, low, high: see focus_rope_scaling in focus.h."""
+    out = np.empty(max(int(rot_dim) // 2, 0), np.float64)
+    s = RopeScaling(int(scaling), int(rot_dim), float(theta), float(factor), float(context), float(low), float(high))
+    check("focus_rope_turns", lib().focus_rope_turns(C.byref(s), out.ctypes.data_as(C.POINTER(C.c_double))))
+    return torch.from_numpy(out).to(device)
+
+
+def _rows(t, n, heads, dim, like, what):
+    """(address, row stride, head stride) of [n, heads, dim] rows of like's dtype and device."""
+    if t is None:
+        return None, 0, 0
+    if t.shape != (n, heads, dim) or t.dtype != like.dtype or t.device != like.device or (dim > 1 and t.stride(2) != 1):
+        raise ValueError(f"{what} must be [{n}, {heads}, {dim}] {like.dtype} on {like.device} with unit stride in the "
+                         "last dimension")
+    # the stride of a dimension of one element is never used
+    return t.data_ptr(), t.stride(0) if n > 1 else 0, t.stride(1) if heads > 1 else 0
+
+
+def focus_rope(pos, turns, q=None, k=None, v=None, layout: int = FOCUS_ROPE_INTERLEAVED, inverse: bool = False,
+               amplitude: float = 1.0, q_out=None, k_out=None, cache: Optional[PagedCache] = None, row_seq=None,
+               row_slot=None, err=None, stream=None):
+    """Rotary positions of q [rows, H, D] and k [rows, H_kv, D] (either may be None; any
+    row and head strides): pair i of a head's first 2 * len(turns) elements turns by
+    pos * turns[i] revolutions (turns: focus_rope_turns; None or empty: nothing turns).
+    inverse: the backward pass, from gradients of the outputs to gradients of q and k.
+    cache: the turned k and v also go to rows row_slot [rows] (int32, negative: not
+    stored) of sequences row_seq [rows] (int32) of the paged cache.  Returns (q_out,
+    k_out); k_out is only allocated without a cache.  Outputs may be the inputs."""
+    like = q if q is not None else k
+    if like is None or like.dim() != 3:
+        raise ValueError("q or k [rows, heads, D] is needed")
+    n, dim, dev = like.shape[0], like.shape[2], like.device
+    heads = q.shape[1] if q is not None else 0
+    kv = k.shape[1] if k is not None else 0
+    if q is not None and q_out is None:
+        q_out = torch.empty(n, heads, dim, dtype=q.dtype, device=dev)
+    if k is not None and k_out is None and cache is None:
+        k_out = torch.empty(n, kv, dim, dtype=k.dtype, device=dev)
+    rot = 0 if turns is None else 2 * turns.numel()
+    if (q_out is not None and q is None) or (k_out is not None and k is None):
+        raise ValueError("an output without its input")
+    if cache is not None and (k is None or v is None or row_seq is None or row_slot is None):
+        raise ValueError("a cache needs k, v, row_seq and row_slot")
+    if cache is None and v is not None:
+        raise ValueError("v without a cache to store it in")
+    c = seq = slot = None
+    if cache is not None:
+        c = cache.desc()
+        if cache.k.device != dev:
+            raise ValueError("the cache is on another device")
+        seq, slot = (_need(x, torch.int32, (n,), dev, w) for x, w in ((row_seq, "row_seq"), (row_slot, "row_slot")))
+    d = RopeDesc(_dtype(like), heads, kv, dim, rot, int(layout), int(bool(inverse)), float(amplitude), n,
+                 _need(pos, torch.int32, (n,), dev, "pos"),
+                 None if rot == 0 else _need(turns, torch.float64, None, dev, "turns"),
+                 *_rows(q, n, heads, dim, like, "q"), *_rows(q_out, n, heads, dim, like, "q_out"),
+                 *_rows(k, n, kv, dim, like, "k"), *_rows(k_out, n, kv, dim, like, "k_out"),
+                 *_rows(v, n, kv, dim, like, "v"), None if c is None else C.pointer(c), seq, slot, _err_ptr(err, dev))
+    _launch("focus_rope", d, dev, stream)
+    return q_out, k_out
+
+
+def _paged_decode_desc(q, cache, o, lse, weight_decay, workspace, split_keys, softmax_scale, err):
+    c = cache.desc()
+    if q.dim() != 3 or q.device != cache.k.device or q.dtype != cache.k.dtype:
+        raise ValueError("q must be [batch, heads, D] of the cache's dtype and device")
+    batch, heads, dim = q.shape
+    if batch != c.batch or dim != c.head_dim:
+        raise ValueError("q does not match the cache's batch or head_dim")
+    if weight_decay is not None and cache.weight is None:
+        raise ValueError("weight_decay needs a cache with weight")
+    return PagedDecodeDesc(c, heads, int(split_keys), float(softmax_scale), 0 if weight_decay is None else 1,
+                           0.0 if weight_decay is None else float(weight_decay), 0,
+                           *_rows(q, batch, heads, dim, q, "q"),
+                           None if o is None else _need(o, q.dtype, (batch, heads, dim), q.device, "o"),
+                           None if lse is None else _need(lse, torch.float32, (batch, heads), q.device, "lse"),
+                           _ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(),
+                           _err_ptr(err, q.device))
+
+
+def focus_paged_decode_workspace(q, cache: PagedCache, weight_decay=None, split_keys: int = 0) -> int:
+    d = _paged_decode_desc(q, cache, None, None, weight_decay, None, split_keys, 0.0, None)
+    return lib().focus_paged_decode_workspace(C.byref(d))
+
+
+def focus_paged_decode(q, cache: PagedCache, o=None, lse=None, weight_decay: Optional[float] = None, workspace=None,
+                       split_keys: int = 0, softmax_scale: float = 0.0, want_lse: bool = True, err=None, stream=None):
+    """Attention of one new token of every sequence, q [batch, H, D] (turned), over the
+    rows of a paged cache (the token's own row among them); returns (o, lse).
+    weight_decay: also cache.weight = weight_decay * cache.weight + the step's softmax
+    weights, summed over the heads of each KV head."""
+    if o is None:
+        o = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    if lse is None and want_lse:
+        lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device)
+    d = _paged_decode_desc(q, cache, o, lse, weight_decay, workspace, split_keys, softmax_scale, err)
+    if workspace is None:
+        n = lib().focus_paged_decode_workspace(C.byref(d))
+        if n > 0:
+            workspace = _scratch(n, q.device, stream)
+            d.workspace, d.workspace_bytes = workspace.data_ptr(), n
+    _launch("focus_paged_decode", d, q.device, stream)
+    return o, lse
+
+
+def _paged_evict_desc(cache, out, budget, recent, keep, workspace, err):
+    c, to, dev = cache.desc(), out.desc(), cache.k.device
+    if out.k.device != dev:
+        raise ValueError("out is on another device")
+    budgets = None
+    if torch.is_tensor(budget):
+        budgets, budget = _need(budget, torch.int32, (c.batch,), dev, "budget"), 0
+    rows = 0
+    if keep is not None:
+        rows = keep.shape[-1]
+        keep = _need(keep, torch.int32, (c.batch, c.n_kv_heads, rows), dev, "keep")
+    return PagedEvictDesc(c, to, int(budget), int(recent), budgets, keep, rows, _ptr(workspace),
+                          0 if workspace is None else workspace.numel() * workspace.element_size(),
+                          _err_ptr(err, dev))
+
+
+def focus_paged_evict_workspace(cache: PagedCache, out: PagedCache, budget, recent: int = 0, keep=None) -> int:
+    d = _paged_evict_desc(cache, out, budget, recent, keep, None, None)
+    return lib().focus_paged_evict_workspace(C.byref(d))
+
+
+def focus_paged_evict(cache: PagedCache, out: PagedCache, budget, recent: int = 0, keep=None, workspace=None, err=None,
+                      stream=None):
+    """Cut every sequence of cache down to budget rows (an int, or int32 [batch]) for
+    each KV head: the latest `recent` rows and those with the greatest cache.weight,
+    copied in ascending order to the pages of out (other pages, of the same pool or of
+    another), out.length and out.weight set.  Returns keep [batch, H_kv, rows], the rows
+    kept and -1 past them; allocated, it holds as many rows as out's table or the
+    budget, whichever is less."""
+    if keep is None:
+        rows = out.table.shape[-1] * out.k.shape[1]
+        if not torch.is_tensor(budget):
+            rows = min(rows, max(int(budget), 0))
+        keep = torch.empty(cache.table.shape[0], cache.k.shape[2], rows, dtype=torch.int32, device=cache.k.device)
+    d = _paged_evict_desc(cache, out, budget, recent, keep, workspace, err)
+    if workspace is None:
+        n = lib().focus_paged_evict_workspace(C.byref(d))
+        if n > 0:
+            workspace = _scratch(n, cache.k.device, stream)
+            d.workspace, d.workspace_bytes = workspace.data_ptr(), n
+    _launch("focus_paged_evict", d, cache.k.device, stream)
+    return keep

@@ -18,9 +18,11 @@ FOCUS_STEP_SUMMARY, FOCUS_STEP_WINDOW_END = 1, 2
 FOCUS_ERR_CAPACITY, FOCUS_ERR_BOUNDS, FOCUS_ERR_PLAN = 1, 2, 4
 FOCUS_FID_LOGITS, FOCUS_FID_PROBS = 0, 1
 FOCUS_FID_N = 5
+FOCUS_ROPE_NONE, FOCUS_ROPE_LINEAR, FOCUS_ROPE_BASE, FOCUS_ROPE_BANDS = 0, 1, 2, 3
+FOCUS_ROPE_INTERLEAVED, FOCUS_ROPE_HALF = 0, 1
 
 p = C.c_void_p
-i32, i64, f32, sz = C.c_int32, C.c_int64, C.c_float, C.c_size_t
+i32, i64, f32, f64, sz = C.c_int32, C.c_int64, C.c_float, C.c_double, C.c_size_t
 
 
 class LayoutTotals(C.Structure):
@@ -119,8 +121,40 @@ class QkvDesc(C.Structure):
                 ("cache_len", p), ("err", p)]
 
 
+class RopeScaling(C.Structure):
+    _fields_ = [("kind", i32), ("rot_dim", i32), ("theta", f64), ("factor", f64), ("context", f64),
+                ("low", f64), ("high", f64)]
+
+
+class PagedKv(C.Structure):
+    _fields_ = [("dtype", i32), ("n_kv_heads", i32), ("head_dim", i32), ("page_rows", i32), ("n_pages", i64),
+                ("k", p), ("v", p), ("page_stride", i64), ("row_stride", i64), ("head_stride", i64),
+                ("batch", i32), ("max_pages", i32), ("table", p), ("length", p), ("weight", p),
+                ("weight_rows", i64)]
+
+
+class RopeDesc(C.Structure):
+    _fields_ = [("dtype", i32), ("n_heads", i32), ("n_kv_heads", i32), ("head_dim", i32), ("rot_dim", i32),
+                ("pairs", i32), ("inverse", i32), ("amplitude", f32), ("n_rows", i64), ("pos", p), ("turns", p),
+                ("q", p), ("q_row", i64), ("q_head", i64), ("q_out", p), ("qo_row", i64), ("qo_head", i64),
+                ("k", p), ("k_row", i64), ("k_head", i64), ("k_out", p), ("ko_row", i64), ("ko_head", i64),
+                ("v", p), ("v_row", i64), ("v_head", i64), ("cache", C.POINTER(PagedKv)), ("row_seq", p),
+                ("row_slot", p), ("err", p)]
+
+
+class PagedDecodeDesc(C.Structure):
+    _fields_ = [("cache", PagedKv), ("n_heads", i32), ("split_keys", i32), ("softmax_scale", f32),
+                ("accumulate", i32), ("weight_decay", f32), ("reserved", i32), ("q", p), ("q_row", i64),
+                ("q_head", i64), ("o", p), ("lse", p), ("workspace", p), ("workspace_bytes", sz), ("err", p)]
+
+
+class PagedEvictDesc(C.Structure):
+    _fields_ = [("cache", PagedKv), ("out", PagedKv), ("budget", i32), ("recent", i32), ("budgets", p), ("keep", p),
+                ("keep_rows", i64), ("workspace", p), ("workspace_bytes", sz), ("err", p)]
+
+
 STRUCTS = [LayoutTotals, LayoutDesc, CompactDesc, AttnDesc, DecodeDesc, FidelityDesc, GemmDesc, AdapterDesc,
-           AdapterLayerDesc, QkvDesc, DecodeSched]
+           AdapterLayerDesc, QkvDesc, DecodeSched, RopeScaling, PagedKv, RopeDesc, PagedDecodeDesc, PagedEvictDesc]
 
 # name -> (restype, argtypes): every symbol include/focus.h declares
 SYMBOLS = {
@@ -145,6 +179,12 @@ SYMBOLS = {
     "focus_adapter_layer_workspace": (sz, [C.POINTER(AdapterLayerDesc)]),
     "focus_adapter_layer": (i32, [C.POINTER(AdapterLayerDesc), p]),
     "focus_qkv_project": (i32, [C.POINTER(QkvDesc), p]),
+    "focus_rope_turns": (i32, [C.POINTER(RopeScaling), C.POINTER(f64)]),
+    "focus_rope": (i32, [C.POINTER(RopeDesc), p]),
+    "focus_paged_decode_workspace": (sz, [C.POINTER(PagedDecodeDesc)]),
+    "focus_paged_decode": (i32, [C.POINTER(PagedDecodeDesc), p]),
+    "focus_paged_evict_workspace": (sz, [C.POINTER(PagedEvictDesc)]),
+    "focus_paged_evict": (i32, [C.POINTER(PagedEvictDesc), p]),
 }
 
 

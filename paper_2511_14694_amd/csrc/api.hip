@@ -32,6 +32,11 @@ extern "C" int64_t focus_struct_size(int32_t which) {
     case 8: return sizeof(focus_adapter_layer_desc);
     case 9: return sizeof(focus_qkv_desc);
     case 10: return sizeof(focus_decode_sched);
+    case 11: return sizeof(focus_rope_scaling);
+    case 12: return sizeof(focus_paged_kv);
+    case 13: return sizeof(focus_rope_desc);
+    case 14: return sizeof(focus_paged_decode_desc);
+    case 15: return sizeof(focus_paged_evict_desc);
     default: return -1;
   }
 }

@@ -1,0 +1,247 @@
+"""focus_paged_decode on the GPU against the float64 oracle (tolerances:
+paged_util.decode_tolerances)."""
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2511_14694_amd as F
+from gpu_util import DEV, announce, to64
+from oracle import paged as P
+from paged_util import Cache, decode_tolerances, values, within
+
+pytestmark = pytest.mark.gpu
+
+
+def _check(c, q64, got, dtype, scale=None, visible=None, weight=None, decay=None):
+    """got (o, lse) and the cache's weights against the oracle, sequence by sequence."""
+    o, lse = to64(got[0]), to64(got[1])
+    w = None if weight is None else c.dev.weight.cpu().numpy().astype(np.float64)
+    H, D = q64.shape[1:]
+    K = c.dev.k.shape[2]
+    sc = D ** -0.5 if scale is None else scale
+    for b, n in enumerate(c.lens):
+        seen = np.ones(n, bool) if visible is None else visible[b]
+        ro, rl, rw = P.decode(q64[b], c.k[b], c.v[b], sc, seen)
+        to, tl, rel = decode_tolerances(q64[b], c.k[b][seen], sc, dtype, c.v[b][seen], ro)
+        within(o[b], ro, to, f"o[{b}]")
+        within(lse[b], rl, tl, f"lse[{b}]")
+        if w is not None:
+            old = decay * weight[b].astype(np.float64) if decay else np.zeros_like(weight[b], np.float64)
+            ref = old.copy()
+            ref[:, :n] += rw
+            ref[:, n:] = weight[b][:, n:]
+            tol = np.zeros_like(ref)
+            grow = rel.reshape(K, H // K).max(1)[:, None] + 2.0 ** -21 + (H // K) * 2.0 ** -24
+            tol[:, :n] = rw * grow + np.abs(ref[:, :n]) * 2.0 ** -23 + 1e-30
+            within(w[b], ref, tol, f"weight[{b}]")
+
+
+@pytest.mark.parametrize("lens,H,K,D,page,dtype,by_head", [
+    ([1], 1, 1, 64, 8, "f32", False),
+    ([1], 32, 8, 128, 64, "bf16", False),
+    ([137], 32, 8, 128, 64, "bf16", False),
+    ([0, 5, 0], 4, 2, 64, 16, "bf16", False),
+    ([31, 32, 33, 7, 8, 9], 6, 2, 128, 8, "bf16", False),
+    ([15, 16, 17, 63, 65], 6, 6, 64, 16, "f32", True),
+    ([300, 1, 2021], 6, 2, 64, 32, "f32", True),
+    ([1000, 129, 127, 128], 8, 8, 128, 128, "bf16", True),
+    ([513, 90], 16, 1, 128, 16, "bf16", False),      # a group of 16
+    ([257], 40, 2, 64, 16, "bf16", False),           # groups of 20: more than one tile
+    ([257, 70], 34, 2, 128, 16, "f32", False),       # groups of 17
+    ([3000], 3, 3, 128, 1024, "bf16", False),
+    ([5000, 10, 2500], 8, 2, 128, 64, "bf16", False),
+    ([5000, 10, 2500], 4, 4, 128, 16, "f32", False),
+])
+@pytest.mark.parametrize("split", [0, 128, 640])
+def test_decode_matches_oracle(lens, H, K, D, page, dtype, by_head, split):
+    announce(f"paged decode {lens} {H}/{K} x {D} page {page} {dtype} by_head {by_head} split {split}")
+    rng = np.random.default_rng(sum(lens) + H + D)
+    c = Cache(rng, lens, K, D, page, dtype, by_head=by_head, padded=not by_head and D == 64, weight=True)
+    q, q64 = values(rng, (len(lens), H, D), dtype, 1.5)
+    got = F.focus_paged_decode(q, c.dev, split_keys=split)
+    _check(c, q64, got, dtype)
+    assert np.array_equal(c.dev.weight.cpu().numpy(), c.weight), "weights without weight_decay"
+    again = F.focus_paged_decode(q, c.dev, split_keys=split, weight_decay=0.875)
+    assert torch.equal(again[0], got[0]) and torch.equal(again[1], got[1]), "not deterministic"
+    _check(c, q64, again, dtype, weight=c.weight, decay=0.875)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_decode_table_far_larger_than_the_lengths(dtype):
+    """Capacity of 65 536 rows a sequence, lengths from none to a few hundred."""
+    rng = np.random.default_rng(31)
+    lens = [0, 1, 700, 33]
+    c = Cache(rng, lens, 2, 128, 64, dtype, max_pages=1024, weight=True)
+    q, q64 = values(rng, (4, 8, 128), dtype)
+    announce(f"paged decode wide table {dtype}")
+    got = F.focus_paged_decode(q, c.dev, weight_decay=0.0)
+    _check(c, q64, got, dtype, weight=c.weight, decay=0.0)
+
+
+def test_decode_many_sequences():
+    rng = np.random.default_rng(32)
+    lens = [int(x) for x in rng.integers(0, 90, 300)]
+    c = Cache(rng, lens, 1, 64, 16, "bf16", weight=True)
+    q, q64 = values(rng, (300, 2, 64), "bf16")
+    announce("paged decode 300 sequences")
+    _check(c, q64, F.focus_paged_decode(q, c.dev, weight_decay=1.0), "bf16", weight=c.weight, decay=1.0)
+
+
+def test_decode_sharp_scores_scale_and_views():
+    """Scores of several hundred, a given scale, q as a view of a projection, outputs
+    given; old weights that are not numbers count only where they are read."""
+    rng = np.random.default_rng(33)
+    c = Cache(rng, [400, 77], 2, 128, 32, "bf16", weight=True)
+    qkv, x = values(rng, (2, 12, 128), "bf16", 6.0)
+    q, q64 = qkv[:, 2:10], x[:, 2:10]
+    c.dev.weight.fill_(float("nan"))
+    o, lse = torch.empty(2, 8, 128, dtype=torch.bfloat16, device=DEV), torch.empty(2, 8, device=DEV)
+    got = F.focus_paged_decode(q, c.dev, o=o, lse=lse, softmax_scale=0.5, weight_decay=0.0)
+    assert got[0] is o and got[1] is lse
+    nan = np.full_like(c.weight, np.nan)
+    _check(c, q64, got, "bf16", scale=0.5, weight=nan, decay=0.0)
+    o2, none = F.focus_paged_decode(q, c.dev, softmax_scale=0.5, want_lse=False)
+    assert none is None and torch.equal(o2, o)
+
+
+def test_decode_infinities_stay_in_their_column():
+    """V of visible rows: an infinity or NaN reaches its column only; rows past the
+    length and masked rows nothing (they hold NaN throughout these tests)."""
+    rng = np.random.default_rng(34)
+    for dtype in ("bf16", "f32"):
+        c = Cache(rng, [45], 1, 64, 16, dtype)
+        q, q64 = values(rng, (1, 4, 64), dtype)
+        clean = F.focus_paged_decode(q, c.dev)[0]
+        page, row = int(c.table[0, 2]), 7
+        c.dev.v[page, row, 0, 5] = float("inf")
+        c.dev.v[page, row, 0, 9] = float("nan")
+        got = F.focus_paged_decode(q, c.dev)[0]
+        assert torch.isposinf(got[..., 5]).all() and torch.isnan(got[..., 9]).all()
+        got[..., 5], got[..., 9] = clean[..., 5], clean[..., 9]
+        assert torch.equal(got, clean)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("accumulate", [False, True])
+def test_decode_bad_pages_and_lengths(dtype, accumulate):
+    """Rows of pages outside the pool are left out; a length past the table is clipped."""
+    announce(f"paged decode bad pages {dtype} accumulate {accumulate}")
+    rng = np.random.default_rng(35)
+    page = 16
+    lens = [100, 64, 20, 48]
+    c = Cache(rng, lens, 2, 64, page, dtype, weight=True, max_pages=7)
+    c.dev.table[0, 1] = -5
+    c.dev.table[0, 6] = c.dev.k.shape[0]
+    c.dev.table[2, 0] = 2 ** 31 - 1
+    c.dev.table[2, 1] = -1
+    seen = [np.ones(n, bool) for n in lens]
+    seen[0][16:32] = seen[0][96:] = False
+    seen[2][:] = False
+    q, q64 = values(rng, (4, 4, 64), dtype)
+    err = torch.zeros(1, dtype=torch.int32, device=DEV)
+    got = F.focus_paged_decode(q, c.dev, weight_decay=0.5 if accumulate else None, err=err)
+    assert int(err.item()) == 2
+    _check(c, q64, got, dtype, visible=seen, weight=c.weight if accumulate else None, decay=0.5)
+    err.zero_()
+    c.dev.length[3] = -3
+    c.dev.length[1] = 64
+    got = F.focus_paged_decode(q, c.dev, err=err)
+    assert int(err.item()) == 3
+    assert not got[0][3].any() and torch.isneginf(got[1][3]).all()
+    # a length past the table: its rows, here of bad pages past the fourth
+    err.zero_()
+    c.dev.length[3] = 10_000
+    got = F.focus_paged_decode(q, c.dev, err=err)
+    assert int(err.item()) == 3
+    ro, rl, _ = P.decode(q64[3], c.k[3], c.v[3])
+    to, tl, _ = decode_tolerances(q64[3], c.k[3], 64 ** -0.5, dtype, c.v[3], ro)
+    within(to64(got[0])[3], ro, to, "clipped o")
+    within(to64(got[1])[3], rl, tl, "clipped lse")
+
+
+def test_decode_shared_pages():
+    """Two sequences that share their first pages (a common prefix), with weights."""
+    rng = np.random.default_rng(36)
+    page = 16
+    c = Cache(rng, [64, 40], 2, 128, page, "bf16", weight=True)
+    c.table[1, :2] = c.table[0, :2]
+    c.dev.table.copy_(torch.as_tensor(c.table))
+    for x in (c.k, c.v):
+        x[1] = np.concatenate([x[0][:32], x[1][32:]])
+    q, q64 = values(rng, (2, 4, 128), "bf16")
+    _check(c, q64, F.focus_paged_decode(q, c.dev, weight_decay=1.0), "bf16", weight=c.weight, decay=1.0)
+
+
+def test_decode_offsets_past_32_bits():
+    """A pool of more than 2^32 bytes (2^31 elements), the sequence's rows at its end."""
+    page, K, D = 64, 8, 128
+    n_pages = (1 << 31) // (page * K * D) + 3
+    announce(f"paged decode pool of {n_pages} pages")
+    k = torch.empty(n_pages, page, K, D, dtype=torch.bfloat16, device=DEV)
+    v = torch.empty_like(k)
+    rng = np.random.default_rng(37)
+    rows = {w: values(rng, (2 * page, K, D), "bf16") for w in "kv"}
+    last = [n_pages - 1, n_pages - 2]
+    for t, w in ((k, "k"), (v, "v")):
+        for i, p in enumerate(last):
+            t[p] = rows[w][0][i * page:(i + 1) * page]
+    n = 2 * page - 5
+    cache = F.PagedCache(k, v, torch.tensor([last], dtype=torch.int32, device=DEV),
+                         torch.tensor([n], dtype=torch.int32, device=DEV))
+    q, q64 = values(rng, (1, 16, D), "bf16")
+    o, lse = F.focus_paged_decode(q, cache)
+    ro, rl, _ = P.decode(q64[0], rows["k"][1][:n], rows["v"][1][:n])
+    to, tl, _ = decode_tolerances(q64[0], rows["k"][1][:n], D ** -0.5, "bf16", rows["v"][1][:n], ro)
+    within(to64(o)[0], ro, to, "o")
+    within(to64(lse)[0], rl, tl, "lse")
+
+
+def test_decode_other_stream_and_workspace():
+    rng = np.random.default_rng(38)
+    c = Cache(rng, [900, 4000], 2, 128, 64, "bf16", weight=True)
+    q, q64 = values(rng, (2, 8, 128), "bf16")
+    ref = F.focus_paged_decode(q, c.dev, weight_decay=0.0)
+    w = c.dev.weight.clone()
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    n = F.focus_paged_decode_workspace(q, c.dev, weight_decay=0.0)
+    ws = torch.empty(n, dtype=torch.uint8, device=DEV)
+    outs = []
+    for workspace in (None, ws):
+        c.dev.weight.fill_(3.0)
+        torch.cuda.synchronize()
+        outs.append(F.focus_paged_decode(q, c.dev, weight_decay=0.0, workspace=workspace, stream=s))
+        s.synchronize()
+        live = torch.as_tensor(np.arange(c.weight.shape[2])[None] < np.array(c.lens)[:, None]).to(DEV)[:, None]
+        assert torch.equal(torch.where(live, c.dev.weight, w), w)
+    for o, lse in outs:
+        assert torch.equal(o, ref[0]) and torch.equal(lse, ref[1])
+
+
+def test_decode_captured_and_replayed():
+    """Lengths that grow between replays, eager work in between."""
+    rng = np.random.default_rng(39)
+    c = Cache(rng, [300, 20], 2, 128, 16, "bf16", weight=True)
+    q, _ = values(rng, (2, 8, 128), "bf16")
+    full = c.dev.length.clone()
+    o, lse = torch.empty_like(q), torch.empty(2, 8, device=DEV)
+    ws = torch.empty(max(16, F.focus_paged_decode_workspace(q, c.dev, weight_decay=1.0)), dtype=torch.uint8, device=DEV)
+    call = lambda: F.focus_paged_decode(q, c.dev, o=o, lse=lse, weight_decay=1.0, workspace=ws)  # noqa: E731
+    call()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        call()
+    for n0, n1 in ((1, 20), (130, 0), (300, 7)):
+        c.dev.length.copy_(torch.tensor([n0, n1], dtype=torch.int32))
+        q.copy_(values(rng, (2, 8, 128), "bf16")[0])
+        w0 = c.dev.weight.clone()
+        g.replay()
+        torch.cuda.synchronize()
+        got = o.clone(), lse.clone(), c.dev.weight.clone()
+        c.dev.weight.copy_(w0)
+        call()
+        torch.cuda.synchronize()
+        assert torch.equal(got[0], o) and torch.equal(got[1], lse) and torch.equal(got[2], c.dev.weight)
+    c.dev.length.copy_(full)

@@ -1,0 +1,187 @@
+"""focus_paged_evict on the GPU: the rows kept equal the oracle's, and rows, weights and
+lengths are copied bit for bit."""
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2511_14694_amd as F
+from gpu_util import DEV, announce
+from oracle import paged as P
+from paged_util import Cache, paged_rows
+
+pytestmark = pytest.mark.gpu
+
+
+def _weights(rng, shape, kind):
+    if kind == "ties":
+        return rng.integers(0, 3, shape).astype(np.float32)
+    if kind == "equal":
+        return np.full(shape, 0.25, np.float32)
+    if kind == "signs":
+        return (rng.standard_normal(shape) * np.exp2(rng.integers(-40, 40, shape))).astype(np.float32)
+    if kind == "special":
+        return rng.choice(np.array([0.0, -0.0, np.nan, -np.nan, np.inf, -np.inf, 1e-45, -1e-45, 1.0], np.float32), shape)
+    return (rng.random(shape) ** 8).astype(np.float32)
+
+
+def _check(c, out, budgets, recent, keep, old):
+    """out and keep after an eviction of the Cache c (its pools before: old)."""
+    K = c.dev.k.shape[2]
+    got, w, ow = keep.cpu().numpy(), c.dev.weight.cpu().numpy(), None if out.weight is None else out.weight.cpu().numpy()
+    touched = [old[0].clone(), old[1].clone()]
+    lens = []
+    for b, n in enumerate(c.lens):
+        m = min(n, max(budgets[b], 0), got.shape[2], out.table.shape[1] * out.k.shape[1])
+        lens.append(m)
+        for g in range(K):
+            ref = P.keep(w[b, g, :n], m, recent)
+            assert got[b, g, :m].tolist() == ref, (b, g)
+            assert (got[b, g, m:] == -1).all()
+            if ow is not None:
+                assert np.array_equal(ow[b, g, :m], w[b, g, ref], equal_nan=True)
+                assert (ow[b, g, m:] == -1.0).all(), "weights past the rows kept"
+            for which, rows in (("k", c.k[b]), ("v", c.v[b])):
+                assert np.array_equal(paged_rows(out, b, m, which)[:, g], rows[ref, g]), (b, g, which)
+        if m:
+            r = np.arange(m)
+            pid = out.table[b][torch.as_tensor(r // out.k.shape[1]).to(DEV)].long()
+            for t, now in zip(touched, (out.k, out.v)):
+                t[pid, torch.as_tensor(r % out.k.shape[1]).to(DEV)] = now[pid, torch.as_tensor(r % out.k.shape[1]).to(DEV)]
+    assert out.length.tolist() == lens
+    for t, now in zip(touched, (out.k, out.v)):
+        assert torch.equal(t.nan_to_num(7.0), now.nan_to_num(7.0)), "rows that are not kept were written"
+
+
+@pytest.mark.parametrize("lens,K,D,page,dtype,budget,recent", [
+    ([1], 1, 64, 8, "f32", 1, 0),
+    ([5, 0, 9], 2, 64, 8, "bf16", 4, 2),
+    ([40, 41, 8, 200], 3, 128, 16, "bf16", 40, 7),
+    ([1210], 1, 64, 16, "f32", 200, 37),
+    ([3000, 129], 2, 128, 64, "bf16", 1500, 0),
+    ([3000, 129], 2, 96, 128, "bf16", 1, 1),
+    ([700, 64], 8, 8, 32, "bf16", 300, 300),         # the latest rows only
+    ([700, 64], 4, 256, 32, "f32", 0, 10),           # nothing
+    ([9000], 2, 64, 16, "bf16", 8999, 100),
+])
+@pytest.mark.parametrize("kind", ["skewed", "ties", "equal", "signs", "special"])
+def test_evict_matches_oracle(lens, K, D, page, dtype, budget, recent, kind):
+    announce(f"evict {lens} x {K} x {D} page {page} {dtype} budget {budget} recent {recent} {kind}")
+    rng = np.random.default_rng(sum(lens) + budget)
+    rows = -(-budget // page) * page or page
+    c = Cache(rng, lens, K, D, page, dtype, weight=True, spare=len(lens) * (rows // page), by_head=kind == "ties")
+    c.dev.weight.copy_(torch.as_tensor(_weights(rng, c.weight.shape, kind)))
+    out = c.other(rng, budget)
+    old = c.dev.k.clone(), c.dev.v.clone()
+    err = torch.zeros(1, dtype=torch.int32, device=DEV)
+    keep = F.focus_paged_evict(c.dev, out, budget, recent=recent, err=err)
+    assert keep.shape == (len(lens), K, budget) and int(err.item()) == 0
+    _check(c, out, [budget] * len(lens), recent, keep, old)
+
+
+@pytest.mark.parametrize("n,budget", [(70_001, 20_000), (131_072, 131_000)])
+def test_evict_long(n, budget):
+    """Rows beyond what one pass of a workgroup holds; most of the weights equal."""
+    announce(f"evict long {n} -> {budget}")
+    rng = np.random.default_rng(n)
+    c = Cache(rng, [n, 300], 1, 64, 128, "bf16", weight=True, spare=2 * (budget // 128 + 1))
+    w = np.where(rng.random(c.weight.shape) < 0.5, 0.0, c.weight).astype(np.float32)
+    c.dev.weight.copy_(torch.as_tensor(w))
+    out = c.other(rng, budget)
+    old = c.dev.k.clone(), c.dev.v.clone()
+    keep = F.focus_paged_evict(c.dev, out, budget, recent=1000)
+    _check(c, out, [budget] * 2, 1000, keep, old)
+
+
+def test_evict_budgets_other_pool_and_errors():
+    """Budgets of their own (a negative one counts as 0), rows of another pool with other
+    pages, too little room, pages outside the pool, lengths outside the table."""
+    rng = np.random.default_rng(51)
+    lens = [100, 50, 20]
+    c = Cache(rng, lens, 2, 64, 16, "bf16", weight=True, max_pages=7)
+    budgets = [30, 60, -4]
+    k = torch.full((12, 2, 8, 64), 9.0, dtype=torch.bfloat16, device=DEV).transpose(1, 2)
+    out = F.PagedCache(k, k.clone(memory_format=torch.preserve_format),
+                       torch.tensor([[7, 0, 11, 3], [2, 9, 4, 5], [1, 6, 8, 10]], dtype=torch.int32, device=DEV),
+                       torch.full((3,), -1, dtype=torch.int32, device=DEV))
+    old = out.k.clone(), out.v.clone()
+    err = torch.zeros(1, dtype=torch.int32, device=DEV)
+    announce("evict budgets")
+    keep = F.focus_paged_evict(c.dev, out, torch.tensor(budgets, dtype=torch.int32, device=DEV), recent=5, err=err)
+    assert int(err.item()) == 3 and keep.shape == (3, 2, 32)      # 50 rows do not fit in four pages of 8
+    _check(c, out, budgets, 5, keep, old)
+    # a caller's keep of fewer rows than the budget
+    err.zero_()
+    out.k.fill_(9.0)
+    out.v.fill_(9.0)
+    keep = torch.full((3, 2, 17), 5, dtype=torch.int32, device=DEV)
+    assert F.focus_paged_evict(c.dev, out, 20, recent=5, keep=keep, err=err) is keep
+    assert int(err.item()) == 1
+    _check(c, out, [20] * 3, 5, keep, old)
+    # a source page and a destination page outside the pool: those rows stay as they were
+    announce("evict bad pages")
+    err.zero_()
+    out.k.fill_(9.0)
+    c.dev.table[0, 0] = -1
+    out.table[1, 1] = 12
+    keep = F.focus_paged_evict(c.dev, out, 20, recent=20, err=err)
+    assert int(err.item()) == 2
+    assert keep[0, 0].tolist() == list(range(80, 100))
+    keep = F.focus_paged_evict(c.dev, out, 100, recent=0, err=err)
+    assert out.length.tolist() == [32, 32, 20]
+    # lengths outside the table are clipped
+    err.zero_()
+    c.dev.length[1] = -1
+    F.focus_paged_evict(c.dev, out, 20, err=err)
+    assert int(err.item()) & 1 and out.length.tolist() == [20, 0, 20]
+
+
+def test_evict_length_in_place_and_empty():
+    rng = np.random.default_rng(52)
+    c = Cache(rng, [33, 12], 2, 64, 8, "f32", weight=True, spare=8)
+    out = c.other(rng, 16)
+    out.length = c.dev.length
+    old = c.dev.k.clone(), c.dev.v.clone()
+    keep = F.focus_paged_evict(c.dev, out, 16, recent=3)
+    _check(c, out, [16, 16], 3, keep, old)
+    none = F.PagedCache(c.dev.k, c.dev.v, c.dev.table[:0], c.dev.length[:0], c.dev.weight[:0])
+    assert F.focus_paged_evict(none, none, 4).shape == (0, 2, 4)
+
+
+def test_evict_shared_pages_stay():
+    """Two sequences that share a prefix's pages: each is cut on its own, the shared
+    pages keep their rows."""
+    rng = np.random.default_rng(53)
+    c = Cache(rng, [64, 40], 2, 64, 16, "bf16", weight=True, spare=4)
+    c.table[1, :2] = c.table[0, :2]
+    c.dev.table.copy_(torch.as_tensor(c.table))
+    for x in (c.k, c.v):
+        x[1] = np.concatenate([x[0][:32], x[1][32:]])
+    out = c.other(rng, 24)
+    old = c.dev.k.clone(), c.dev.v.clone()
+    keep = F.focus_paged_evict(c.dev, out, 24, recent=4)
+    _check(c, out, [24, 24], 4, keep, old)
+
+
+def test_evict_captured_and_replayed():
+    rng = np.random.default_rng(54)
+    c = Cache(rng, [600, 90], 2, 64, 16, "bf16", weight=True, spare=20)
+    out = c.other(rng, 64)
+    old = c.dev.k.clone(), c.dev.v.clone()
+    keep = torch.empty(2, 2, 64, dtype=torch.int32, device=DEV)
+    n = F.focus_paged_evict_workspace(c.dev, out, 64, 8, keep)
+    ws = torch.empty(max(n, 16), dtype=torch.uint8, device=DEV)
+    call = lambda: F.focus_paged_evict(c.dev, out, 64, recent=8, keep=keep, workspace=ws)  # noqa: E731
+    call()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        call()
+    for i in range(3):
+        c.dev.weight.copy_(torch.as_tensor(_weights(rng, c.weight.shape, ("ties", "skewed", "special")[i])))
+        out.k.copy_(old[0])
+        out.v.copy_(old[1])
+        out.weight.fill_(-1.0)
+        g.replay()
+        torch.cuda.synchronize()
+        _check(c, out, [64, 64], 8, keep, old)

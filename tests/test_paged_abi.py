@@ -1,0 +1,306 @@
+"""CPU checks of the paged-cache and rotary calls: host validation refuses bad
+descriptors before any launch (no GPU is touched), the binding refuses tensors that do
+not fit, and fills every field of its descriptors."""
+
+import ctypes as C
+import math
+
+import pytest
+import torch
+
+import paper_2511_14694_amd as F
+from paper_2511_14694_amd import _abi
+
+FAKE = 1 << 20   # aligned, never dereferenced: every case below is refused first
+E_NULL, E_ARG, E_SHAPE, E_DTYPE, E_UNSUPPORTED, E_WORKSPACE = 1, 2, 3, 4, 5, 6
+
+
+def _call(fn, d):
+    return getattr(_abi.lib(), fn)(C.byref(d), None)
+
+
+def _set(path, value):
+    def mutate(d):
+        *at, name = path.split(".")
+        for a in at:
+            d = getattr(d, a)
+        setattr(d, name, value)
+    return mutate
+
+
+def _paged(dim=128, heads=4, batch=2):
+    return _abi.PagedKv(0, heads, dim, 16, 10, FAKE, FAKE, 16 * heads * dim, heads * dim, dim, batch, 5, FAKE, FAKE, FAKE,
+                        80)
+
+
+PAGED_BAD = [
+    ("dtype", 2, E_DTYPE), ("dtype", -1, E_DTYPE), ("n_kv_heads", 0, E_ARG), ("head_dim", 0, E_ARG),
+    ("n_pages", -1, E_ARG), ("batch", -1, E_ARG), ("max_pages", -1, E_ARG),
+    ("head_dim", 264, E_UNSUPPORTED), ("head_dim", 100, E_UNSUPPORTED),
+    ("page_rows", 0, E_UNSUPPORTED), ("page_rows", 4, E_UNSUPPORTED), ("page_rows", 24, E_UNSUPPORTED),
+    ("page_rows", 2048, E_UNSUPPORTED), ("page_rows", -16, E_UNSUPPORTED),
+    ("max_pages", 1 << 27, E_SHAPE), ("n_pages", 1 << 33, E_SHAPE),
+    ("page_stride", 64, E_ARG), ("row_stride", 0, E_ARG), ("head_stride", -128, E_ARG),
+    ("head_stride", 132, E_ARG), ("row_stride", 516, E_ARG),
+    ("page_stride", 16 * 4 * 128 - 128, E_ARG),          # pages overlap
+    ("row_stride", 3 * 128, E_ARG),                      # rows overlap
+    ("weight_rows", 79, E_SHAPE),
+    ("length", None, E_NULL), ("table", None, E_NULL), ("k", None, E_NULL), ("v", None, E_NULL),
+    ("k", FAKE + 8, E_ARG), ("v", FAKE + 2, E_ARG), ("table", FAKE + 2, E_ARG), ("length", FAKE + 1, E_ARG),
+    ("weight", FAKE + 2, E_ARG),
+]
+
+
+def _rope_ok(with_cache=True):
+    d = _abi.RopeDesc()
+    d.dtype, d.n_heads, d.n_kv_heads, d.head_dim, d.rot_dim, d.n_rows = 0, 8, 4, 128, 128, 3
+    d.amplitude = 1.0
+    for f in ("pos", "turns", "q", "q_out", "k", "k_out"):
+        setattr(d, f, FAKE)
+    d.q_row = d.qo_row = 8 * 128
+    d.k_row = d.ko_row = d.v_row = 4 * 128
+    d.q_head = d.qo_head = d.k_head = d.ko_head = d.v_head = 128
+    if with_cache:
+        d.v = d.row_seq = d.row_slot = FAKE
+        d.kept = _paged()
+        d.cache = C.pointer(d.kept)
+    return d
+
+
+@pytest.mark.parametrize("field,value,status", [
+    ("dtype", 5, E_DTYPE), ("n_rows", -1, E_ARG), ("head_dim", 0, E_ARG), ("rot_dim", 3, E_ARG),
+    ("rot_dim", 130, E_ARG), ("rot_dim", -2, E_ARG), ("pairs", 2, E_ARG), ("pairs", -1, E_ARG),
+    ("amplitude", math.nan, E_ARG), ("amplitude", math.inf, E_ARG), ("n_heads", 0, E_ARG),
+    ("n_kv_heads", 0, E_ARG), ("pos", None, E_NULL), ("turns", None, E_NULL), ("q_out", None, E_NULL),
+    ("row_seq", None, E_NULL), ("row_slot", None, E_NULL), ("k", None, E_NULL), ("v", None, E_NULL),
+    ("inverse", 1, E_ARG), ("q", FAKE + 8, E_ARG), ("k_out", FAKE + 4, E_ARG), ("v", FAKE + 2, E_ARG),
+    ("turns", FAKE + 4, E_ARG), ("pos", FAKE + 2, E_ARG), ("q_row", 1028, E_ARG), ("k_head", 132, E_ARG),
+    ("q_row", -1024, E_ARG), ("qo_row", 0, E_ARG), ("qo_head", 0, E_ARG), ("qo_row", 512, E_ARG),
+    ("ko_row", 384, E_ARG), ("ko_head", 64, E_ARG), ("n_rows", 1 << 40, E_SHAPE),
+])
+def test_rope_refusals(field, value, status):
+    d = _rope_ok()
+    _set(field, value)(d)
+    assert _call("focus_rope", d) == status
+
+
+@pytest.mark.parametrize("field,value,status", PAGED_BAD)
+def test_rope_refuses_bad_caches(field, value, status):
+    d = _rope_ok()
+    d.head_dim = d.kept.head_dim
+    _set(field, value)(d.kept)
+    assert _call("focus_rope", d) == status
+
+
+def test_rope_cache_of_other_shape_and_missing_parts():
+    for field, value in (("n_kv_heads", 2), ("dtype", 1), ("head_dim", 64)):
+        d = _rope_ok()
+        setattr(d.kept, field, value)
+        assert _call("focus_rope", d) == E_SHAPE, field
+    d = _rope_ok(with_cache=False)
+    d.v = FAKE
+    assert _call("focus_rope", d) == E_NULL             # v without a cache
+    d = _rope_ok(with_cache=False)
+    d.k_out = None
+    assert _call("focus_rope", d) == E_NULL             # k goes nowhere
+    d = _rope_ok(with_cache=False)
+    d.k = None
+    assert _call("focus_rope", d) == E_NULL             # k_out without k
+    d = _rope_ok(with_cache=False)
+    d.head_dim, d.rot_dim = 264, 8
+    assert _call("focus_rope", d) == E_UNSUPPORTED
+    d = _rope_ok(with_cache=False)
+    d.n_rows = 0
+    assert _call("focus_rope", d) == 0                  # nothing to do
+    d = _rope_ok(with_cache=False)
+    d.q = d.k = d.k_out = None
+    assert _call("focus_rope", d) == 0
+    assert _abi.lib().focus_rope(None, None) == E_NULL
+    assert _abi.lib().focus_rope_turns(None, None) == E_NULL
+
+
+def _decode_ok():
+    d = _abi.PagedDecodeDesc()
+    d.cache = _paged()
+    d.n_heads, d.q_row, d.q_head = 8, 8 * 128, 128
+    d.q = d.o = d.lse = d.workspace = FAKE
+    d.workspace_bytes = 1 << 40
+    d.accumulate, d.weight_decay = 1, 0.5
+    return d
+
+
+@pytest.mark.parametrize("field,value,status", [
+    ("n_heads", 0, E_ARG), ("n_heads", 6, E_SHAPE), ("split_keys", -128, E_ARG), ("split_keys", 64, E_ARG),
+    ("softmax_scale", math.nan, E_ARG), ("weight_decay", math.nan, E_ARG), ("weight_decay", -math.inf, E_ARG),
+    ("cache.head_dim", 96, E_UNSUPPORTED), ("q_row", 1028, E_ARG), ("q_head", -128, E_ARG),
+    ("q", None, E_NULL), ("o", None, E_NULL), ("cache.weight", None, E_NULL), ("q", FAKE + 8, E_ARG),
+    ("o", FAKE + 8, E_ARG), ("lse", FAKE + 2, E_ARG), ("workspace", None, E_WORKSPACE),
+    ("workspace_bytes", 0, E_WORKSPACE), ("workspace", FAKE + 8, E_ARG), ("n_heads", 1 << 30, E_SHAPE),
+] + [("cache." + f, v, s) for f, v, s in PAGED_BAD])
+def test_paged_decode_refusals(field, value, status):
+    d = _decode_ok()
+    _set(field, value)(d)
+    assert _call("focus_paged_decode", d) == status
+
+
+def test_paged_decode_empty_batch_and_workspace():
+    d = _decode_ok()
+    n = _abi.lib().focus_paged_decode_workspace(C.byref(d))
+    assert n >= 2 * 8 * 80 * 4                  # the scores of every head and row
+    d.workspace_bytes = n - 1
+    assert _call("focus_paged_decode", d) == E_WORKSPACE
+    d.cache.batch = 0
+    d.q = d.o = None
+    assert _call("focus_paged_decode", d) == 0
+    d = _decode_ok()
+    d.cache.head_dim = 80
+    assert _abi.lib().focus_paged_decode_workspace(C.byref(d)) == 0
+    assert _abi.lib().focus_paged_decode_workspace(None) == 0
+    assert _abi.lib().focus_paged_decode(None, None) == E_NULL
+
+
+def _evict_ok():
+    d = _abi.PagedEvictDesc()
+    d.cache, d.out = _paged(), _paged()
+    d.out.weight = 2 * FAKE
+    d.budget, d.recent, d.keep, d.keep_rows = 20, 4, FAKE, 20
+    d.workspace, d.workspace_bytes = FAKE, 1 << 40
+    return d
+
+
+@pytest.mark.parametrize("field,value,status", [
+    ("budget", -1, E_ARG), ("recent", -1, E_ARG), ("keep_rows", -1, E_ARG), ("keep_rows", 1 << 40, E_SHAPE),
+    ("keep", None, E_NULL), ("keep", FAKE + 2, E_ARG), ("budgets", FAKE + 2, E_ARG), ("cache.weight", None, E_NULL),
+    ("out.weight", FAKE, E_ARG),                # the cache's own
+    ("out.dtype", 1, E_SHAPE), ("out.n_kv_heads", 2, E_SHAPE), ("out.batch", 3, E_SHAPE), ("out.head_dim", 64, E_SHAPE),
+] + [("cache." + f, v, s) for f, v, s in PAGED_BAD] + [("out." + f, v, s) for f, v, s in PAGED_BAD])
+def test_paged_evict_refusals(field, value, status):
+    d = _evict_ok()
+    _set(field, value)(d)
+    assert _call("focus_paged_evict", d) == status
+
+
+def test_paged_evict_empty_batch():
+    d = _evict_ok()
+    d.cache.batch = d.out.batch = 0
+    assert _call("focus_paged_evict", d) == 0
+    assert _abi.lib().focus_paged_evict(None, None) == E_NULL
+    assert _abi.lib().focus_paged_evict_workspace(None) == 0
+
+
+# ---- the binding ----
+
+def _cache(batch=2, pages=6, page=16, heads=2, dim=64, dt=torch.bfloat16, rows=48):
+    k = torch.zeros(pages, page, heads, dim, dtype=dt)
+    return F.PagedCache(k, torch.zeros_like(k), torch.zeros(batch, 3, dtype=torch.int32),
+                        torch.zeros(batch, dtype=torch.int32), torch.zeros(batch, heads, rows))
+
+
+def test_binding_refuses_tensors_that_do_not_fit():
+    t = torch.zeros
+    i32 = torch.int32
+    q, k, pos, turns = t(3, 4, 64), t(3, 2, 64), t(3, dtype=i32), t(32, dtype=torch.float64)
+    slot = t(3, dtype=i32)
+    c = _cache(dt=torch.float32)
+    bad = [
+        lambda: F.focus_rope(pos, turns),
+        lambda: F.focus_rope(pos.long(), turns, q),
+        lambda: F.focus_rope(pos[:2], turns, q),
+        lambda: F.focus_rope(pos, turns.float(), q),
+        lambda: F.focus_rope(pos, turns, q.half()),
+        lambda: F.focus_rope(pos, turns, q, k.bfloat16()),
+        lambda: F.focus_rope(pos, turns, q, k[:2]),
+        lambda: F.focus_rope(pos, turns, q, k, k),
+        lambda: F.focus_rope(pos, turns, q, q_out=t(3, 4, 32)),
+        lambda: F.focus_rope(pos, turns, q, k_out=k),
+        lambda: F.focus_rope(pos, turns, q.transpose(1, 2)),
+        lambda: F.focus_rope(pos, turns, q, k, cache=c, row_seq=slot, row_slot=slot),
+        lambda: F.focus_rope(pos, turns, q, k, k, cache=c, row_seq=slot),
+        lambda: F.focus_rope(pos, turns, q, k, k, cache=c, row_seq=slot[:2], row_slot=slot),
+        lambda: F.focus_rope(pos, turns, q, err=t(1)),
+        lambda: F.focus_paged_decode(t(2, 4, 64), _cache()),                    # another dtype
+        lambda: F.focus_paged_decode(t(3, 4, 64), c),
+        lambda: F.focus_paged_decode(t(2, 4, 32), c),
+        lambda: F.focus_paged_decode(t(2, 4, 64), c, o=t(2, 4, 32)),
+        lambda: F.focus_paged_decode(t(2, 4, 64), c, lse=t(2, 4, dtype=torch.float64)),
+        lambda: F.focus_paged_decode(t(2, 4, 64), F.PagedCache(c.k, c.v, c.table, c.length), weight_decay=1.0),
+        lambda: F.focus_paged_evict(c, c, torch.tensor([3, 4])),
+        lambda: F.focus_paged_evict(c, c, 3, keep=t(2, 2, 3)),
+        lambda: F.PagedCache(c.k, c.v[:, :8], c.table, c.length).desc(),
+        lambda: F.PagedCache(c.k, c.v.transpose(1, 2).contiguous().transpose(1, 2), c.table, c.length).desc(),
+        lambda: F.PagedCache(c.k, c.v, c.table[0], c.length).desc(),
+        lambda: F.PagedCache(c.k, c.v, c.table.long(), c.length).desc(),
+        lambda: F.PagedCache(c.k, c.v, c.table, c.length[:1]).desc(),
+        lambda: F.PagedCache(c.k, c.v, c.table, c.length, c.weight[:, :1]).desc(),
+        lambda: F.focus_rope(pos, turns, q),                                    # on no GPU
+    ]
+    for i, call in enumerate(bad):
+        with pytest.raises(ValueError):
+            call()
+            pytest.fail(f"case {i} was taken")
+
+
+def test_descriptors_hold_what_their_fields_say(monkeypatch):
+    calls = {}
+    monkeypatch.setattr(F, "_launch", lambda name, d, dev, stream: calls.__setitem__(name, d))
+
+    class Lib:
+        def __getattr__(self, name):
+            return lambda d: 0
+    monkeypatch.setattr(F, "lib", Lib)
+
+    def fields(d, want):
+        assert set(want) == {n for n, *_ in d._fields_}
+        for name, x in want.items():
+            got = getattr(d, name)
+            if isinstance(x, dict):
+                fields(got, x)
+            else:
+                assert got == (x.data_ptr() if torch.is_tensor(x) else x), name
+
+    t, i32 = torch.zeros, torch.int32
+    H, K, D, n = 6, 3, 64, 5
+    pool = t(4, K, 16, D, dtype=torch.bfloat16)
+    c = F.PagedCache(pool.transpose(1, 2), t(4, K, 16, D, dtype=torch.bfloat16).transpose(1, 2), t(2, 7, dtype=i32),
+                     t(2, dtype=i32), t(2, K, 120))
+    paged = dict(dtype=0, n_kv_heads=K, head_dim=D, page_rows=16, n_pages=4, k=c.k, v=c.v, page_stride=K * 16 * D,
+                 row_stride=D, head_stride=16 * D, batch=2, max_pages=7, table=c.table, length=c.length,
+                 weight=c.weight, weight_rows=120)
+    fields(c.desc(), paged)
+    qkv = t(n, H + 2 * K, D, dtype=torch.bfloat16)
+    q, k, v = qkv[:, :H], qkv[:, H:H + K], qkv[:, H + K:]
+    qo, ko = t(H, n, D, dtype=torch.bfloat16).transpose(0, 1), t(n, K, D, dtype=torch.bfloat16)
+    pos, seq, slot, err, turns = t(n, dtype=i32), t(n, dtype=i32), t(n, dtype=i32), t(1, dtype=i32), \
+        t(20, dtype=torch.float64)
+    F.focus_rope(pos, turns, q, k, v, layout=1, inverse=True, amplitude=0.75, q_out=qo, k_out=ko, cache=c, row_seq=seq,
+                 row_slot=slot, err=err)
+    d = calls["focus_rope"]
+    fields(d.cache.contents, paged)
+    d.cache = None
+    row = (H + 2 * K) * D
+    want = dict(dtype=0, n_heads=H, n_kv_heads=K, head_dim=D, rot_dim=40, pairs=1, inverse=1, amplitude=0.75, n_rows=n,
+                pos=pos, turns=turns, q=q, q_row=row, q_head=D, q_out=qo, qo_row=D, qo_head=n * D, k=k, k_row=row,
+                k_head=D, k_out=ko, ko_row=K * D, ko_head=D, v=v, v_row=row, v_head=D, row_seq=seq, row_slot=slot,
+                err=err)
+    for name, x in want.items():
+        assert getattr(d, name) == (x.data_ptr() if torch.is_tensor(x) else x), name
+    assert set(want) | {"cache"} == {f for f, *_ in d._fields_}
+
+    q2, o, lse, ws = t(2, 3 * H, D, dtype=torch.bfloat16)[:, :H], t(2, H, D, dtype=torch.bfloat16), t(2, H), t(8)
+    F.focus_paged_decode(q2, c, o=o, lse=lse, weight_decay=0.25, workspace=ws, split_keys=128, softmax_scale=0.5, err=err)
+    fields(calls["focus_paged_decode"], dict(
+        cache=paged, n_heads=H, split_keys=128, softmax_scale=0.5, accumulate=1, weight_decay=0.25, reserved=0, q=q2,
+        q_row=3 * H * D, q_head=D, o=o, lse=lse, workspace=ws, workspace_bytes=32, err=err))
+    F.focus_paged_decode(q2, c, want_lse=False)
+    d = calls["focus_paged_decode"]
+    assert (d.accumulate, d.weight_decay, d.lse) == (0, 0.0, None) and d.o
+
+    out = F.PagedCache(c.k, c.v, t(2, 5, dtype=i32), t(2, dtype=i32))
+    keep, budgets = t(2, K, 33, dtype=i32), t(2, dtype=i32)
+    F.focus_paged_evict(c, out, budgets, recent=9, keep=keep, workspace=ws, err=err)
+    to = dict(paged, max_pages=5, table=out.table, length=out.length, weight=None, weight_rows=0)
+    fields(calls["focus_paged_evict"], dict(cache=paged, out=to, budget=0, recent=9, budgets=budgets, keep=keep,
+                                            keep_rows=33, workspace=ws, workspace_bytes=32, err=err))
+    got = F.focus_paged_evict(c, out, 12)
+    assert got.shape == (2, K, 12) and calls["focus_paged_evict"].budget == 12
+    assert F.focus_paged_evict(c, out, 999).shape == (2, K, 80)
