@@ -1,106 +1,454 @@
 // Attention of one new token over a paged K/V cache (focus_paged_decode).
 //
-//   paged_attend   one workgroup per (sequence, head): four waves take the rows in
-//                  turn, each with a running maximum and sum, joined through LDS
-//   paged_weights  where weights are accumulated: per cached row and KV head, the
-//                  softmax weights of the group's heads from the stored scores
+//   paged_attend   one workgroup per (chunk of a sequence's rows, KV head, up to 16 of
+//                  its query heads); writes o and lse where the chunk is the whole
+//                  sequence, else an unnormalised partial (running max, sum, output)
+//   paged_join     merges the partials of a sequence's chunks by log-sum-exp; where
+//                  weights are accumulated, further workgroups turn the scores that
+//                  paged_attend stored into weights of every row
+//
+// Every cached byte is read once, for all query heads of its KV head, so the kernel is
+// HBM bound as long as the products keep up: they run on the matrix cores at every
+// group size (a group of one wastes 15 of 16 columns and still needs a tenth of the
+// time its bytes take).  No operand goes through LDS: the products are arranged so that
+// each lane's loads are operands as they arrive.  For bf16, a wave takes 32 rows:
+//     S^T = K Q^T     row m of product t is cached row 8 (m / 4) + 4 t + m % 4, so lane
+//                     (column q = lane % 16, group x = lane / 16) gets the scores of
+//                     rows 8 x .. 8 x + 7 of query q
+//     O^T += V^T P^T  contraction index 8 x + j is row 8 x + j: the lane's own weights;
+//                     lane i of group x loaded elements D/16 i .. of rows 8 x .. 8 x + 7
+//                     (whole rows, 16 lanes each), of which product t takes element
+//                     D/16 i + t, one byte permutation per register
+// so maximum, sum and rescaling of a query stay in the lanes of its column.  float32
+// takes 16 rows a tile on the 16x16x4 products, which need no permutation at all.
 #include "paged.h"
 
 #include <math.h>
 
+#include <algorithm>
+
 namespace {
+
+using focus::bf16x8;
+using focus::f32x4;
+using focus::u32x4;
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
 constexpr float kLn2 = 0.69314718055994531f;
 constexpr float kLog2e = 1.44269504088896341f;
 constexpr float kMinit = -1.0e30f;
 constexpr int kThreads = 256, kWaves = 4;
+constexpr int kCols = 16;       // query heads of a workgroup: columns of a product
+constexpr int kPages = 1024;    // page numbers held in LDS at a time
+constexpr int kUnit = 128;      // chunks are multiples of this many rows
 
+// What a lane reads in the place of a row that is past its sequence's end or in a page
+// outside the pool (such a row may hold anything, and zero times a NaN is a NaN).
+__device__ __align__(16) const uint32_t kZeros[256] = {};
+
+// Workspace: int4 info[batch] {first slot, chunks, rows, 0}, then the partials of
+// `slots` chunks: float2 ml[slots][H], float o[slots][H][D], then, where weights are
+// accumulated, float score[batch][H][cap] (log2 units).
 struct Plan {
-  int64_t scores, cap;  // float offset and rows of the stored scores
+  int64_t slots;        // upper bound of the chunks of all sequences
+  int64_t target;       // chunks wanted from the whole batch (split_keys 0)
+  int64_t cap;          // rows of a sequence's table
+  int64_t ml, o, score; // byte offsets
   size_t bytes;
+  int tiles;            // workgroups a KV head's query heads take
 };
 
 Plan make_plan(const focus_paged_decode_desc* d) {
+  const focus_paged_kv& c = d->cache;
   Plan p = {};
-  p.cap = (int64_t)d->cache.max_pages * d->cache.page_rows;
-  if (d->accumulate) {
-    const int64_t heads = (int64_t)d->cache.batch * d->n_heads;
-    p.scores = heads;  // the log-sum-exps (log2) come first
-    p.bytes = (size_t)(heads + heads * p.cap) * sizeof(float);
+  p.cap = (int64_t)c.max_pages * c.page_rows;
+  p.tiles = (int)focus::ceil_div(d->n_heads / c.n_kv_heads, kCols);
+  if (d->split_keys > 0) {
+    p.slots = c.batch * std::max<int64_t>(1, focus::ceil_div(p.cap, d->split_keys));
+  } else {
+    // two workgroups fit on a compute unit: one round of them over the whole batch
+    p.target = std::max<int64_t>(1, 2 * focus::device_cus() / ((int64_t)c.n_kv_heads * p.tiles));
+    // a sequence has at least one chunk and at most rows / chunk rounded up
+    p.slots = std::min(c.batch + p.target, c.batch * std::max<int64_t>(1, focus::ceil_div(p.cap, kUnit)));
   }
+  const int64_t heads = p.slots * d->n_heads;
+  p.ml = 16 * (int64_t)c.batch;
+  p.o = p.ml + focus::ceil_div(8 * heads, 16) * 16;
+  p.score = p.o + 4 * heads * c.head_dim;
+  p.bytes = (size_t)(p.score + (d->accumulate ? 4 * (int64_t)c.batch * d->n_heads * p.cap : 0));
   return p;
 }
 
-template <typename T, int D>
-__global__ __launch_bounds__(kThreads) void paged_attend(focus_paged_decode_desc d, float sc, int shift, float* ws,
-                                                         int64_t scores, int64_t cap) {
-  constexpr int E = D / 64;
-  __shared__ float red_m[kWaves], red_l[kWaves], red_o[kWaves][D];
-  const focus_paged_kv& c = d.cache;
-  const int H = d.n_heads, b = blockIdx.x / H, h = blockIdx.x % H, g = h / (H / c.n_kv_heads);
-  const int wave = threadIdx.x / 64, lane = threadIdx.x % 64;
-  const int n = focus::paged_length(c, b);
-  if (threadIdx.x == 0 && h == 0 && n != c.length[b]) focus::raise_err(d.err, FOCUS_ERR_CAPACITY);
-  const T* q = reinterpret_cast<const T*>(d.q) + b * d.q_row + h * d.q_head + lane * E;
-  float x[E], o[E];
+struct Args {
+  focus_paged_decode_desc d;
+  float sc;             // softmax scale in log2 units
+  int shift;            // log2 page_rows
+  int tiles;
+  int64_t target, cap;
+  int4* info;
+  float2* ml;
+  float* o;
+  float* score;
+};
+
+// Chunk of the split with index i: every wave finds it by itself from the lengths, 64
+// sequences at a time.  A chunk is split_keys rows, or what spreads the rows of the
+// whole batch over `target` of them.
+struct Chunk {
+  int b, c, n, slot0, chunks, rows;
+};
+__device__ bool find_chunk(const Args& a, int i, Chunk& out) {
+  const focus_paged_kv& c = a.d.cache;
+  const int lane = threadIdx.x % 64;
+  int rows = a.d.split_keys;
+  if (rows == 0) {
+    int64_t total = 0;
+    for (int b0 = 0; b0 < c.batch; b0 += 64) {
+      int64_t x = b0 + lane < c.batch ? focus::paged_length(c, b0 + lane) : 0;
 #pragma unroll
-  for (int e = 0; e < E; ++e) x[e] = (float)q[e] * sc, o[e] = 0.f;
-  float m = kMinit, l = 0.f;
-  for (int r = wave; r < n; r += kWaves) {
-    const int64_t p = focus::page_of(c, b, r, shift);
-    float s = 0.f;
-    if (p < 0) {
-      if (lane == 0) focus::raise_err(d.err, FOCUS_ERR_BOUNDS);
-      s = -INFINITY;
-    } else {
-      const int64_t at = focus::row_at(c, p, r, g) + lane * E;
-#pragma unroll
-      for (int e = 0; e < E; ++e) s = fmaf(x[e], (float)reinterpret_cast<const T*>(c.k)[at + e], s);
-#pragma unroll
-      for (int i = 32; i >= 1; i >>= 1) s += __shfl_xor(s, i);
-      const float m_new = fmaxf(m, s), alpha = exp2f(m - m_new), w = exp2f(s - m_new);
-      l = fmaf(l, alpha, w);
-#pragma unroll
-      for (int e = 0; e < E; ++e) o[e] = fmaf(w, (float)reinterpret_cast<const T*>(c.v)[at + e], o[e] * alpha);
-      m = m_new;
+      for (int k = 32; k >= 1; k >>= 1) x += __shfl_xor(x, k);
+      total += x;
     }
-    if (d.accumulate && lane == 0) ws[scores + ((int64_t)b * H + h) * cap + r] = s;
+    const int64_t per = (total + a.target - 1) / a.target;
+    rows = (int)min((per + kUnit - 1) / kUnit * kUnit, (int64_t)1 << 30);
+    rows = max(rows, kUnit);
   }
-  if (lane == 0) red_m[wave] = m, red_l[wave] = l;
+  int before = 0;
+  for (int b0 = 0; b0 < c.batch; b0 += 64) {
+    const int n = b0 + lane < c.batch ? focus::paged_length(c, b0 + lane) : 0;
+    const int own = b0 + lane < c.batch ? max(1, (n - 1) / rows + 1) : 0;
+    int upto = own;
 #pragma unroll
-  for (int e = 0; e < E; ++e) red_o[wave][lane * E + e] = o[e];
+    for (int k = 1; k < 64; k <<= 1) {
+      const int y = __shfl_up(upto, k);
+      if (lane >= k) upto += y;
+    }
+    const int all = __shfl(upto, 63);
+    if (i < before + all) {
+      const uint64_t past = __ballot(i < before + upto);
+      const int at = __ffsll((unsigned long long)past) - 1;
+      out.b = b0 + at;
+      out.n = __shfl(n, at);
+      out.chunks = __shfl(own, at);
+      out.slot0 = before + __shfl(upto, at) - out.chunks;
+      out.c = i - out.slot0;
+      out.rows = rows;
+      return true;
+    }
+    before += all;
+  }
+  return false;
+}
+
+template <typename T, int D> struct Tile {
+  static constexpr bool kBf16 = sizeof(T) == 2;
+  static constexpr int kRows = kBf16 ? 32 : 16;     // rows a wave takes at a time
+  static constexpr int kScores = kRows / 4;         // scores of a lane: rows kScores x ..
+  static constexpr int kPer = D / 16;               // elements of a V row a lane holds
+  static constexpr int kWords = kPer * sizeof(T) / 4;
+  static constexpr int kPiece = 16 / sizeof(T);     // elements of a 16-byte load
+  static constexpr int kSteps = D / (4 * kPiece);   // 16-byte pieces of a K row a lane holds
+  static constexpr int kProducts = kBf16 ? 2 : 1;   // K rows a lane holds
+  u32x4 k[kProducts][kSteps];
+  uint32_t v[kScores][kWords];
+};
+
+template <typename T, int D>
+__global__ __launch_bounds__(kThreads, 2) void paged_attend(Args a) {
+  using L = Tile<T, D>;
+  constexpr int kPitch = D + 4;
+  __shared__ int s_page[kPages + 1];  // (a chunk may begin inside a page)
+  __shared__ float s_o[kWaves][kCols][kPitch];
+  __shared__ float2 s_ml[kWaves][kCols];
+  const focus_paged_kv& c = a.d.cache;
+  const int K = c.n_kv_heads, H = a.d.n_heads, G = H / K;
+  const int tid = threadIdx.x, wave = tid / 64, lane = tid % 64, col = lane % 16, x = lane / 16;
+  const int tile_id = blockIdx.x % a.tiles, g = blockIdx.x / a.tiles % K;
+  Chunk ch;
+  if (!find_chunk(a, blockIdx.x / (a.tiles * K), ch)) return;
+  const int b = ch.b, r0 = ch.c * ch.rows, r1 = min(ch.n, r0 + ch.rows);
+  const bool first = g == 0 && tile_id == 0;
+  if (first && ch.c == 0 && tid == 0) {
+    a.info[b] = make_int4(ch.slot0, ch.chunks, ch.n, 0);
+    if (ch.n != c.length[b]) focus::raise_err(a.d.err, FOCUS_ERR_CAPACITY);
+  }
+  const int h0 = g * G + tile_id * kCols, heads = min(kCols, G - tile_id * kCols);
+
+  // Q: column col, elements as the K rows' pieces
+  u32x4 q[L::kSteps];
+  {
+    const T* src = reinterpret_cast<const T*>(a.d.q) + (int64_t)b * a.d.q_row + (int64_t)(h0 + col) * a.d.q_head;
+#pragma unroll
+    for (int i = 0; i < L::kSteps; ++i)
+      q[i] = col < heads ? *reinterpret_cast<const u32x4*>(src + (i * 4 + x) * L::kPiece) : u32x4{0, 0, 0, 0};
+  }
+
+  const T* kbase = reinterpret_cast<const T*>(c.k) + (int64_t)g * c.head_stride;
+  const T* vbase = reinterpret_cast<const T*>(c.v) + (int64_t)g * c.head_stride;
+  const T* zeros = reinterpret_cast<const T*>(kZeros);
+  const int mask = c.page_rows - 1;
+  // rows of eight from which this lane reads K and V; the offsets of its rows in them
+  const int k8 = L::kBf16 ? col / 4 * 8 : col / 8 * 8, k_in = L::kBf16 ? col % 4 : col % 8;
+  const int v8 = L::kBf16 ? x * 8 : x / 2 * 8, v_in = L::kBf16 ? 0 : x % 2 * 4;
+  float* score = a.d.accumulate && col < heads ? a.score + ((int64_t)b * H + h0 + col) * a.cap : nullptr;
+
+  float m, l;
+  f32x4 o[L::kPer];
+  // The low part of the weights (below) turns an infinity in V into a NaN: sums that are
+  // NaN are taken again without it (the others keep what they are).
+  for (bool low = true;; low = false) {
+    m = kMinit;
+    l = 0.f;
+#pragma unroll
+    for (int t = 0; t < L::kPer; ++t) o[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int seg = r0; seg < r1; seg += kPages << a.shift) {
+      const int seg_end = min(r1, seg + (kPages << a.shift)), page0 = seg >> a.shift;
+      __syncthreads();
+      for (int i = tid; i + page0 <= (seg_end - 1) >> a.shift; i += kThreads) {
+        const int64_t p = focus::page_of(c, b, (i + page0) << a.shift, a.shift);
+        if (p < 0 && first) focus::raise_err(a.d.err, FOCUS_ERR_BOUNDS);
+        s_page[i] = (int)p;
+      }
+      __syncthreads();
+      // page of the eight rows at r (-1: none)
+      auto page = [&](int r) { return r < seg_end ? s_page[(r >> a.shift) - page0] : -1; };
+      auto load = [&](L& w, int r) {
+        const int pk = page(r + k8), pv = page(r + v8);
+        const T* kp = kbase + pk * c.page_stride + (int64_t)((r + k8) & mask) * c.row_stride;
+        const T* vp = vbase + pv * c.page_stride + (int64_t)((r + v8) & mask) * c.row_stride;
+#pragma unroll
+        for (int t = 0; t < L::kProducts; ++t) {
+          const int in = k_in + 4 * t;
+          const T* p = pk >= 0 && r + k8 + in < seg_end ? kp + in * c.row_stride : zeros;
+#pragma unroll
+          for (int i = 0; i < L::kSteps; ++i) w.k[t][i] = *reinterpret_cast<const u32x4*>(p + (i * 4 + x) * L::kPiece);
+        }
+#pragma unroll
+        for (int j = 0; j < L::kScores; ++j) {
+          const int in = v_in + j;
+          const T* p = (pv >= 0 && r + v8 + in < seg_end ? vp + in * c.row_stride : zeros) + col * L::kPer;
+          if constexpr (L::kWords == 2) {
+            const u32x2 y = *reinterpret_cast<const u32x2*>(p);
+            w.v[j][0] = y[0], w.v[j][1] = y[1];
+          } else {
+#pragma unroll
+            for (int i = 0; i < L::kWords / 4; ++i) {
+              const u32x4 y = reinterpret_cast<const u32x4*>(p)[i];
+#pragma unroll
+              for (int e = 0; e < 4; ++e) w.v[j][4 * i + e] = y[e];
+            }
+          }
+        }
+      };
+      auto compute = [&](const L& w, int r) {
+        f32x4 s[L::kProducts];
+#pragma unroll
+        for (int t = 0; t < L::kProducts; ++t) {
+          s[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int i = 0; i < L::kSteps; ++i) {
+            if constexpr (L::kBf16) {
+              s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w.k[t][i]),
+                                                             __builtin_bit_cast(bf16x8, q[i]), s[t], 0, 0, 0);
+            } else {
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+                s[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(w.k[t][i][e]), __uint_as_float(q[i][e]), s[t],
+                                                            0, 0, 0);
+            }
+          }
+        }
+        const int row = r + v8 + v_in;  // of the lane's first score
+        const int live = page(r + v8) >= 0 ? seg_end - row : 0;
+        float y[L::kScores], mx = m;
+#pragma unroll
+        for (int j = 0; j < L::kScores; ++j) {
+          y[j] = j < live ? s[j / 4][j % 4] * a.sc : -INFINITY;
+          mx = fmaxf(mx, y[j]);
+        }
+        if (score && row < seg_end) {
+#pragma unroll
+          for (int j = 0; j < L::kScores; j += 4)
+            *reinterpret_cast<float4*>(score + row + j) = make_float4(y[j], y[j + 1], y[j + 2], y[j + 3]);
+        }
+        mx = fmaxf(mx, __shfl_xor(mx, 16));
+        mx = fmaxf(mx, __shfl_xor(mx, 32));
+        const float alpha = __builtin_amdgcn_exp2f(m - mx);
+        m = mx;
+        l *= alpha;
+#pragma unroll
+        for (int j = 0; j < L::kScores; ++j) {
+          y[j] = __builtin_amdgcn_exp2f(y[j] - m);
+          l += y[j];
+        }
+#pragma unroll
+        for (int t = 0; t < L::kPer; ++t) o[t] *= alpha;
+        if constexpr (L::kBf16) {
+          // the weights in two bf16 parts, off by 2^-17 of them together (one part
+          // alone adds as much to o as its own rounding); the matrix cores have the time
+          bf16x8 hi, lo;
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            hi[j] = (__bf16)y[j];
+            lo[j] = (__bf16)(y[j] - (float)hi[j]);
+          }
+#pragma unroll
+          for (int t = 0; t < L::kPer; ++t) {
+            u32x4 z;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              z[e] = __builtin_amdgcn_perm(w.v[2 * e + 1][t / 2], w.v[2 * e][t / 2], t % 2 ? 0x07060302 : 0x05040100);
+            o[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, z), hi, o[t], 0, 0, 0);
+            if (low) o[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, z), lo, o[t], 0, 0, 0);
+          }
+        } else {
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int t = 0; t < L::kPer; ++t)
+              o[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(w.v[j][t]), y[j], o[t], 0, 0, 0);
+        }
+      };
+      // a wave's tiles, the next one's loads in flight while one is computed
+      constexpr int kStep = kWaves * L::kRows;
+      int r = seg + wave * L::kRows;
+      if (r < seg_end) {
+        L w0, w1;
+        load(w0, r);
+        while (true) {
+          if (r + kStep < seg_end) load(w1, r + kStep);
+          compute(w0, r);
+          if ((r += kStep) >= seg_end) break;
+          if (r + kStep < seg_end) load(w0, r + kStep);
+          compute(w1, r);
+          if ((r += kStep) >= seg_end) break;
+        }
+      }
+    }
+    bool nan = false;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+#pragma unroll
+      for (int t = 0; t < L::kPer; t += 4) {
+        float4* to = reinterpret_cast<float4*>(&s_o[wave][col][(x * 4 + e) * L::kPer + t]);
+        float4 y = make_float4(o[t][e], o[t + 1][e], o[t + 2][e], o[t + 3][e]);
+        if (!low) {
+          const float4 was = *to;
+          y = make_float4(was.x == was.x ? was.x : y.x, was.y == was.y ? was.y : y.y, was.z == was.z ? was.z : y.z,
+                          was.w == was.w ? was.w : y.w);
+        }
+        *to = y;
+        nan |= y.x != y.x || y.y != y.y || y.z != y.z || y.w != y.w;
+      }
+    if (!L::kBf16 || !low || !__syncthreads_or(nan)) break;
+  }
+
+  // the waves' parts, joined
+  l += __shfl_xor(l, 16);
+  l += __shfl_xor(l, 32);
+  if (x == 0) s_ml[wave][col] = make_float2(m, l);
   __syncthreads();
-  float M = kMinit, L = 0.f;
+  for (int i = tid; i < heads * D; i += kThreads) {
+    const int h = i / D, e = i % D;
+    float M = kMinit, Lsum = 0.f, y = 0.f;
 #pragma unroll
-  for (int w = 0; w < kWaves; ++w) M = fmaxf(M, red_m[w]);
+    for (int w = 0; w < kWaves; ++w) M = fmaxf(M, s_ml[w][h].x);
 #pragma unroll
-  for (int w = 0; w < kWaves; ++w) L += red_l[w] * exp2f(red_m[w] - M);
-  if (threadIdx.x < D) {
-    float y = 0.f;
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) y = fmaf(red_o[w][threadIdx.x], exp2f(red_m[w] - M), y);
-    reinterpret_cast<T*>(d.o)[((int64_t)b * H + h) * D + threadIdx.x] = (T)(L == 0.f ? 0.f : y / L);
-  }
-  if (threadIdx.x == 0) {
-    const float e = L == 0.f ? -INFINITY : M + log2f(L);
-    if (d.lse) d.lse[(int64_t)b * H + h] = e * kLn2;
-    if (d.accumulate) ws[(int64_t)b * H + h] = e;
+    for (int w = 0; w < kWaves; ++w) {
+      const float f = __builtin_amdgcn_exp2f(s_ml[w][h].x - M);
+      Lsum = fmaf(s_ml[w][h].y, f, Lsum);
+      y = fmaf(s_o[w][h][e], f, y);
+    }
+    const int64_t at = (int64_t)b * H + h0 + h, slot = (int64_t)(ch.slot0 + ch.c) * H + h0 + h;
+    if (ch.chunks == 1) {
+      reinterpret_cast<T*>(a.d.o)[at * D + e] = (T)(Lsum == 0.f ? 0.f : y / Lsum);
+      if (e == 0 && a.d.lse) a.d.lse[at] = Lsum == 0.f ? -INFINITY : (M + log2f(Lsum)) * kLn2;
+    } else {
+      a.o[slot * D + e] = y;
+    }
+    if (e == 0) a.ml[slot] = make_float2(M, Lsum);
   }
 }
 
-__global__ __launch_bounds__(kThreads) void paged_weights(focus_paged_decode_desc d, const float* ws, int64_t scores,
-                                                          int64_t cap) {
-  const focus_paged_kv& c = d.cache;
-  const int H = d.n_heads, K = c.n_kv_heads, G = H / K;
-  const int b = blockIdx.x / K, g = blockIdx.x % K, n = focus::paged_length(c, b);
-  float* w = c.weight + ((int64_t)b * K + g) * c.weight_rows;
-  for (int r = blockIdx.y * kThreads + threadIdx.x; r < n; r += gridDim.y * kThreads) {
-    float x = 0.f;
-    for (int h = g * G; h < (g + 1) * G; ++h) {
-      const float s = ws[scores + ((int64_t)b * H + h) * cap + r];
-      if (s != -INFINITY) x += exp2f(s - ws[(int64_t)b * H + h]);
+// Maximum and sum over a sequence's chunks of head h, by one wave.
+__device__ float2 joined(const Args& a, const int4& info, int h) {
+  const int H = a.d.n_heads, lane = threadIdx.x % 64;
+  float M = kMinit, L = 0.f;
+  for (int i = lane; i < info.y; i += 64) {
+    const float2 y = a.ml[(int64_t)(info.x + i) * H + h];
+    const float m = fmaxf(M, y.x);
+    L = L * __builtin_amdgcn_exp2f(M - m) + y.y * __builtin_amdgcn_exp2f(y.x - m);
+    M = m;
+  }
+#pragma unroll
+  for (int k = 32; k >= 1; k >>= 1) {
+    const float m2 = __shfl_xor(M, k), l2 = __shfl_xor(L, k), m = fmaxf(M, m2);
+    L = L * __builtin_amdgcn_exp2f(M - m) + l2 * __builtin_amdgcn_exp2f(m2 - m);
+    M = m;
+  }
+  return make_float2(M, L);
+}
+
+constexpr int kWeightRows = 1024;   // rows of a workgroup that writes weights
+
+template <typename T, int D>
+__global__ __launch_bounds__(kThreads) void paged_join(Args a, int joins, int row_blocks) {
+  const focus_paged_kv& c = a.d.cache;
+  const int K = c.n_kv_heads, H = a.d.n_heads, G = H / K, tid = threadIdx.x;
+  if ((int)blockIdx.x < joins) {
+    __shared__ float s_o[kThreads / D][D];
+    const int b = blockIdx.x / H, h = blockIdx.x % H;
+    const int4 info = a.info[b];
+    if (info.y == 1) return;
+    const float2 ml = joined(a, info, h);
+    constexpr int kGroups = kThreads / D;
+    const int e = tid % D, grp = tid / D;
+    float y = 0.f;
+    for (int i = grp; i < info.y; i += kGroups) {
+      const int64_t slot = (int64_t)(info.x + i) * H + h;
+      y = fmaf(a.o[slot * D + e], __builtin_amdgcn_exp2f(a.ml[slot].x - ml.x), y);
     }
-    w[r] = d.weight_decay == 0.f ? x : fmaf(d.weight_decay, w[r], x);
+    s_o[grp][e] = y;
+    __syncthreads();
+    if (tid < D) {
+#pragma unroll
+      for (int k = 1; k < kGroups; ++k) y += s_o[k][e];
+      const int64_t at = (int64_t)b * H + h;
+      reinterpret_cast<T*>(a.d.o)[at * D + e] = (T)(ml.y == 0.f ? 0.f : y / ml.y);
+      if (e == 0 && a.d.lse) a.d.lse[at] = ml.y == 0.f ? -INFINITY : (ml.x + log2f(ml.y)) * kLn2;
+    }
+    return;
+  }
+  // weights of the rows of one (sequence, KV head)
+  const int item = blockIdx.x - joins, part = item % row_blocks, g = item / row_blocks % K, b = item / row_blocks / K;
+  const int4 info = a.info[b];
+  const int n = info.z;
+  float* w = c.weight + ((int64_t)b * K + g) * c.weight_rows;
+  __shared__ float s_lse[kThreads];
+  for (int r0 = part * kWeightRows; r0 < n; r0 += row_blocks * kWeightRows) {
+    float x[kWeightRows / kThreads] = {};
+    for (int hb = 0; hb < G; hb += kThreads) {
+      const int some = min(kThreads, G - hb);
+      __syncthreads();
+      for (int h = tid / 64; h < some; h += kWaves) {
+        const float2 ml = joined(a, info, g * G + hb + h);
+        if (tid % 64 == 0) s_lse[h] = ml.y == 0.f ? INFINITY : ml.x + log2f(ml.y);
+      }
+      __syncthreads();
+      for (int h = 0; h < some; ++h) {
+        const float* s = a.score + ((int64_t)b * H + g * G + hb + h) * a.cap;
+#pragma unroll
+        for (int i = 0; i < kWeightRows / kThreads; ++i) {
+          const int r = r0 + i * kThreads + tid;
+          if (r < n) x[i] += __builtin_amdgcn_exp2f(s[r] - s_lse[h]);
+        }
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < kWeightRows / kThreads; ++i) {
+      const int r = r0 + i * kThreads + tid;
+      if (r < n) w[r] = a.d.weight_decay == 0.f ? x[i] : fmaf(a.d.weight_decay, w[r], x[i]);
+    }
   }
 }
 
@@ -109,7 +457,7 @@ focus_status validate(const focus_paged_decode_desc* d) {
   const focus_status st = focus::check_paged(c);
   if (st != FOCUS_OK) return st;
   if (c.head_dim != 64 && c.head_dim != 128) return FOCUS_E_UNSUPPORTED;
-  if (d->n_heads <= 0 || d->split_keys < 0 || d->split_keys % 128 || !(d->softmax_scale == d->softmax_scale) ||
+  if (d->n_heads <= 0 || d->split_keys < 0 || d->split_keys % kUnit || !(d->softmax_scale == d->softmax_scale) ||
       !isfinite(d->weight_decay))
     return FOCUS_E_ARG;
   if (d->n_heads % c.n_kv_heads) return FOCUS_E_SHAPE;
@@ -118,6 +466,23 @@ focus_status validate(const focus_paged_decode_desc* d) {
   if (d->q_row < 0 || d->q_head < 0 || !focus::pieces16(d->q_row, es) || !focus::pieces16(d->q_head, es))
     return FOCUS_E_ARG;
   return FOCUS_OK;
+}
+
+template <typename T, int D>
+focus_status launch(const Args& a, const Plan& p, hipStream_t s) {
+  const focus_paged_kv& c = a.d.cache;
+  const int64_t blocks = p.slots * c.n_kv_heads * p.tiles;
+  const int joins = c.batch * a.d.n_heads;
+  // enough workgroups to write the weights at the memory's rate, not one per row of the table
+  const int64_t per = focus::ceil_div(p.cap > 0 ? p.cap : 1, kWeightRows), heads = (int64_t)c.batch * c.n_kv_heads;
+  const int64_t row_blocks = std::min(per, std::max<int64_t>(1, focus::ceil_div(8 * focus::device_cus(), heads)));
+  const int64_t second = joins + (a.d.accumulate ? heads * row_blocks : 0);
+  if (blocks > INT32_MAX / kThreads || second > INT32_MAX / kThreads) return FOCUS_E_SHAPE;
+  hipLaunchKernelGGL((paged_attend<T, D>), dim3((uint32_t)blocks), dim3(kThreads), 0, s, a);
+  const focus_status st = focus::launch_status();
+  if (st != FOCUS_OK) return st;
+  hipLaunchKernelGGL((paged_join<T, D>), dim3((uint32_t)second), dim3(kThreads), 0, s, a, joins, (int)row_blocks);
+  return focus::launch_status();
 }
 
 }  // namespace
@@ -129,31 +494,22 @@ extern "C" size_t focus_paged_decode_workspace(const focus_paged_decode_desc* d)
 
 extern "C" focus_status focus_paged_decode(const focus_paged_decode_desc* d, focus_stream_t stream) {
   if (!d) return FOCUS_E_NULL;
-  focus_status st = validate(d);
+  const focus_status st = validate(d);
   if (st != FOCUS_OK) return st;
   const focus_paged_kv& c = d->cache;
   if (c.batch == 0) return FOCUS_OK;
   if (!d->q || !d->o || (d->accumulate && !c.weight)) return FOCUS_E_NULL;
   if (!focus::aligned16(d->q) || !focus::aligned16(d->o) || (reinterpret_cast<uintptr_t>(d->lse) & 3u)) return FOCUS_E_ARG;
   const Plan p = make_plan(d);
-  if (p.bytes && (!d->workspace || d->workspace_bytes < p.bytes)) return FOCUS_E_WORKSPACE;
+  if (!d->workspace || d->workspace_bytes < p.bytes) return FOCUS_E_WORKSPACE;
   if (!focus::aligned16(d->workspace)) return FOCUS_E_ARG;
+  char* ws = reinterpret_cast<char*>(d->workspace);
+  Args a = {*d, 0.f, focus::page_shift(c), p.tiles, p.target, p.cap, reinterpret_cast<int4*>(ws),
+            reinterpret_cast<float2*>(ws + p.ml), reinterpret_cast<float*>(ws + p.o),
+            reinterpret_cast<float*>(ws + p.score)};
   const float scale = d->softmax_scale > 0.f ? d->softmax_scale : 1.0f / sqrtf((float)c.head_dim);
-  const float sc = scale * kLog2e;
-  const int shift = focus::page_shift(c);
-  float* ws = reinterpret_cast<float*>(d->workspace);
+  a.sc = scale * kLog2e;
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
-  const dim3 grid((uint32_t)(c.batch * d->n_heads)), block(kThreads);
-#define FOCUS_LAUNCH(T, D) hipLaunchKernelGGL((paged_attend<T, D>), grid, block, 0, s, *d, sc, shift, ws, p.scores, p.cap)
-  if (c.dtype == FOCUS_BF16) {
-    if (c.head_dim == 128) FOCUS_LAUNCH(__bf16, 128); else FOCUS_LAUNCH(__bf16, 64);
-  } else {
-    if (c.head_dim == 128) FOCUS_LAUNCH(float, 128); else FOCUS_LAUNCH(float, 64);
-  }
-#undef FOCUS_LAUNCH
-  if ((st = focus::launch_status()) != FOCUS_OK || !d->accumulate) return st;
-  const int64_t y = focus::ceil_div(p.cap > 0 ? p.cap : 1, kThreads * 4);
-  hipLaunchKernelGGL(paged_weights, dim3((uint32_t)(c.batch * c.n_kv_heads), (uint32_t)(y > 64 ? 64 : y)), block, 0, s, *d,
-                     ws, p.scores, p.cap);
-  return focus::launch_status();
+  if (c.dtype == FOCUS_BF16) return c.head_dim == 128 ? launch<__bf16, 128>(a, p, s) : launch<__bf16, 64>(a, p, s);
+  return c.head_dim == 128 ? launch<float, 128>(a, p, s) : launch<float, 64>(a, p, s);
 }
