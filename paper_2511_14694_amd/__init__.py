@@ -548,15 +548,22 @@ def focus_qkv_project(lay: Layout, hidden, w_qkv, n_heads: int, n_kv_heads: int,
 
 # ------------------------------------------------------------------ paged caches
 
-def _need(t, dtype, shape, dev, what):
-    """t as a contiguous tensor of this dtype, shape (None: any) and device."""
-    if t.dtype != dtype or t.device != dev or not t.is_contiguous() or (shape is not None and t.shape != shape):
-        raise ValueError(f"{what} must be a contiguous {dtype} tensor"
-                         + ("" if shape is None else f" {list(shape)}") + f" on {dev}")
-    return t.data_ptr()
+# A decode step makes one call of each kind a layer, and its kernels run for a few
+# microseconds: the checks below cost as little as they can (a tensor's attributes are
+# each read once; dtypes are singletons, devices compared by number, -1 for the host).
+
+_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
 
-def _err_ptr(err, dev):
+def _need(t, dtype, shape, dev: int, what):
+    """Address of t, contiguous and of this dtype, shape (None: any) and device."""
+    if t.dtype is dtype and t.get_device() == dev and t.is_contiguous() and (shape is None or t.shape == shape):
+        return t.data_ptr()
+    raise ValueError(f"{what} must be a contiguous {dtype} tensor" + ("" if shape is None else f" {list(shape)}")
+                     + " on the other tensors' device")
+
+
+def _err_ptr(err, dev: int):
     if err is None:
         return None
     if err.numel() < 1:
@@ -564,16 +571,22 @@ def _err_ptr(err, dev):
     return _need(err, torch.int32, None, dev, "err")
 
 
-def _launch(call: str, d, dev, stream):
-    """Enqueue a call on dev, whichever device is current."""
-    if dev.type != "cuda":
+def _launch(call: str, d, dev: int, stream):
+    """Enqueue a call on device dev, whichever one is current."""
+    if dev < 0:
         raise ValueError(f"{call} needs tensors on a GPU")
     fn = getattr(lib(), call)
-    if dev.index == torch.cuda.current_device():
-        check(call, fn(C.byref(d), _stream(stream, dev)))
+    if stream is None and _raw_stream is not None:
+        handle = _raw_stream(dev)
+    else:
+        handle = _stream(stream, torch.device("cuda", dev))
+    if dev == _device():
+        st = fn(C.byref(d), handle)
     else:
         with torch.cuda.device(dev):
-            check(call, fn(C.byref(d), _stream(stream, dev)))
+            st = fn(C.byref(d), handle)
+    if st:
+        check(call, st)
 
 
 @dataclass
@@ -596,23 +609,28 @@ class PagedCache:
     weight: Optional[torch.Tensor] = None
 
     def desc(self) -> PagedKv:
-        k, v, dev = self.k, self.v, self.k.device
-        if (k.dim() != 4 or v.shape != k.shape or v.dtype != k.dtype or v.device != dev or v.stride() != k.stride()
-                or k.stride(3) != 1):
+        k, v, table, weight = self.k, self.v, self.table, self.weight
+        shape, strides, dev, dtype = k.shape, k.stride(), k.get_device(), k.dtype
+        if (len(shape) != 4 or v.shape != shape or v.dtype is not dtype or v.get_device() != dev
+                or v.stride() != strides or strides[3] != 1):
             raise ValueError("k and v must be [n_pages, page_rows, H_kv, D] of one dtype, device and strides, "
                              "with unit stride in D")
-        n_pages, rows, heads, dim = k.shape
-        if self.table.dim() != 2:
+        n_pages, rows, heads, dim = shape
+        if dtype not in _DTYPES:
+            raise ValueError(f"unsupported dtype {dtype}")
+        batch_pages = table.shape
+        if len(batch_pages) != 2:
             raise ValueError("table must be [batch, max_pages]")
-        batch, max_pages = self.table.shape
-        # the stride of a dimension of one element says nothing: replaced by one that passes
-        page, row, head, _ = (dim if n == 1 else st for n, st in zip(k.shape, k.stride()))
+        batch, max_pages = batch_pages
+        if n_pages <= 1 or heads <= 1:
+            # the stride of a dimension of one element says nothing: replaced by one that passes
+            strides = [dim if n <= 1 else st for n, st in zip(shape, strides)]
         w, w_rows = None, 0
-        if self.weight is not None:
-            w_rows = self.weight.shape[-1]
-            w = _need(self.weight, torch.float32, (batch, heads, w_rows), dev, "weight")
-        return PagedKv(_dtype(k), heads, dim, rows, n_pages, k.data_ptr(), v.data_ptr(), page, row, head, batch,
-                       max_pages, _need(self.table, torch.int32, None, dev, "table"),
+        if weight is not None:
+            w_rows = weight.shape[-1]
+            w = _need(weight, torch.float32, (batch, heads, w_rows), dev, "weight")
+        return PagedKv(_DTYPES[dtype], heads, dim, rows, n_pages, k.data_ptr(), v.data_ptr(), strides[0], strides[1],
+                       strides[2], batch, max_pages, _need(table, torch.int32, None, dev, "table"),
                        _need(self.length, torch.int32, (batch,), dev, "length"), w, w_rows)
 
 
@@ -627,15 +645,17 @@ def focus_rope_turns(rot_dim: int, theta: float = 10000.0, scaling: int = FOCUS_
     return torch.from_numpy(out).to(device)
 
 
-def _rows(t, n, heads, dim, like, what):
-    """(address, row stride, head stride) of [n, heads, dim] rows of like's dtype and device."""
-    if t is None:
-        return None, 0, 0
-    if t.shape != (n, heads, dim) or t.dtype != like.dtype or t.device != like.device or (dim > 1 and t.stride(2) != 1):
-        raise ValueError(f"{what} must be [{n}, {heads}, {dim}] {like.dtype} on {like.device} with unit stride in the "
-                         "last dimension")
+def _rows(t, shape, dtype, dev: int, what):
+    """(address, row stride, head stride) of rows [rows, heads, D]."""
+    strides = t.stride()
+    if t.shape != shape or t.dtype is not dtype or t.get_device() != dev or strides[2] != 1:
+        raise ValueError(f"{what} must be {list(shape)} {dtype}, with unit stride in the last dimension, on the other "
+                         "tensors' device")
     # the stride of a dimension of one element is never used
-    return t.data_ptr(), t.stride(0) if n > 1 else 0, t.stride(1) if heads > 1 else 0
+    return t.data_ptr(), strides[0] if shape[0] > 1 else 0, strides[1] if shape[1] > 1 else 0
+
+
+_NO_ROWS = (None, 0, 0)
 
 
 def focus_rope(pos, turns, q=None, k=None, v=None, layout: int = FOCUS_ROPE_INTERLEAVED, inverse: bool = False,
@@ -649,54 +669,67 @@ def focus_rope(pos, turns, q=None, k=None, v=None, layout: int = FOCUS_ROPE_INTE
     stored) of sequences row_seq [rows] (int32) of the paged cache.  Returns (q_out,
     k_out); k_out is only allocated without a cache.  Outputs may be the inputs."""
     like = q if q is not None else k
-    if like is None or like.dim() != 3:
-        raise ValueError("q or k [rows, heads, D] is needed")
-    n, dim, dev = like.shape[0], like.shape[2], like.device
-    heads = q.shape[1] if q is not None else 0
-    kv = k.shape[1] if k is not None else 0
-    if q is not None and q_out is None:
-        q_out = torch.empty(n, heads, dim, dtype=q.dtype, device=dev)
-    if k is not None and k_out is None and cache is None:
-        k_out = torch.empty(n, kv, dim, dtype=k.dtype, device=dev)
-    rot = 0 if turns is None else 2 * turns.numel()
-    if (q_out is not None and q is None) or (k_out is not None and k is None):
-        raise ValueError("an output without its input")
-    if cache is not None and (k is None or v is None or row_seq is None or row_slot is None):
-        raise ValueError("a cache needs k, v, row_seq and row_slot")
-    if cache is None and v is not None:
-        raise ValueError("v without a cache to store it in")
+    if like is None or like.dim() != 3 or like.dtype not in _DTYPES:
+        raise ValueError("q or k [rows, heads, D], bfloat16 or float32, is needed")
+    dtype, dev = like.dtype, like.get_device()
+    n, _, dim = like.shape
+    qs = ks = None
+    q_rows = qo_rows = k_rows = ko_rows = v_rows = _NO_ROWS
+    heads = kv = 0
+    if q is not None:
+        heads = q.shape[1]
+        qs = (n, heads, dim)
+        if q_out is None:
+            q_out = torch.empty(qs, dtype=dtype, device=q.device)
+        q_rows, qo_rows = _rows(q, qs, dtype, dev, "q"), _rows(q_out, qs, dtype, dev, "q_out")
+    elif q_out is not None:
+        raise ValueError("q_out without q")
+    if k is not None:
+        kv = k.shape[1]
+        ks = (n, kv, dim)
+        k_rows = _rows(k, ks, dtype, dev, "k")
+        if k_out is None and cache is None:
+            k_out = torch.empty(ks, dtype=dtype, device=k.device)
+        if k_out is not None:
+            ko_rows = _rows(k_out, ks, dtype, dev, "k_out")
+    elif k_out is not None:
+        raise ValueError("k_out without k")
     c = seq = slot = None
     if cache is not None:
-        c = cache.desc()
-        if cache.k.device != dev:
+        if k is None or v is None or row_seq is None or row_slot is None:
+            raise ValueError("a cache needs k, v, row_seq and row_slot")
+        if cache.k.get_device() != dev:
             raise ValueError("the cache is on another device")
-        seq, slot = (_need(x, torch.int32, (n,), dev, w) for x, w in ((row_seq, "row_seq"), (row_slot, "row_slot")))
-    d = RopeDesc(_dtype(like), heads, kv, dim, rot, int(layout), int(bool(inverse)), float(amplitude), n,
+        v_rows = _rows(v, ks, dtype, dev, "v")
+        c = C.pointer(cache.desc())
+        seq = _need(row_seq, torch.int32, (n,), dev, "row_seq")
+        slot = _need(row_slot, torch.int32, (n,), dev, "row_slot")
+    elif v is not None:
+        raise ValueError("v without a cache to store it in")
+    rot = 0 if turns is None else 2 * turns.numel()
+    d = RopeDesc(_DTYPES[dtype], heads, kv, dim, rot, layout, 1 if inverse else 0, amplitude, n,
                  _need(pos, torch.int32, (n,), dev, "pos"),
-                 None if rot == 0 else _need(turns, torch.float64, None, dev, "turns"),
-                 *_rows(q, n, heads, dim, like, "q"), *_rows(q_out, n, heads, dim, like, "q_out"),
-                 *_rows(k, n, kv, dim, like, "k"), *_rows(k_out, n, kv, dim, like, "k_out"),
-                 *_rows(v, n, kv, dim, like, "v"), None if c is None else C.pointer(c), seq, slot, _err_ptr(err, dev))
+                 _need(turns, torch.float64, None, dev, "turns") if rot else None,
+                 *q_rows, *qo_rows, *k_rows, *ko_rows, *v_rows, c, seq, slot,
+                 None if err is None else _err_ptr(err, dev))
     _launch("focus_rope", d, dev, stream)
     return q_out, k_out
 
 
 def _paged_decode_desc(q, cache, o, lse, weight_decay, workspace, split_keys, softmax_scale, err):
     c = cache.desc()
-    if q.dim() != 3 or q.device != cache.k.device or q.dtype != cache.k.dtype:
-        raise ValueError("q must be [batch, heads, D] of the cache's dtype and device")
-    batch, heads, dim = q.shape
-    if batch != c.batch or dim != c.head_dim:
-        raise ValueError("q does not match the cache's batch or head_dim")
+    dev, dtype = q.get_device(), cache.k.dtype
+    shape = q.shape
+    if len(shape) != 3 or shape[0] != c.batch or shape[2] != c.head_dim or dev != cache.k.get_device():
+        raise ValueError("q must be [batch, heads, D] of the cache's batch, head_dim and device")
     if weight_decay is not None and cache.weight is None:
         raise ValueError("weight_decay needs a cache with weight")
-    return PagedDecodeDesc(c, heads, int(split_keys), float(softmax_scale), 0 if weight_decay is None else 1,
-                           0.0 if weight_decay is None else float(weight_decay), 0,
-                           *_rows(q, batch, heads, dim, q, "q"),
-                           None if o is None else _need(o, q.dtype, (batch, heads, dim), q.device, "o"),
-                           None if lse is None else _need(lse, torch.float32, (batch, heads), q.device, "lse"),
+    return PagedDecodeDesc(c, shape[1], split_keys, softmax_scale, 0 if weight_decay is None else 1,
+                           0.0 if weight_decay is None else weight_decay, 0, *_rows(q, shape, dtype, dev, "q"),
+                           None if o is None else _need(o, dtype, shape, dev, "o"),
+                           None if lse is None else _need(lse, torch.float32, shape[:2], dev, "lse"),
                            _ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(),
-                           _err_ptr(err, q.device))
+                           None if err is None else _err_ptr(err, dev))
 
 
 def focus_paged_decode_workspace(q, cache: PagedCache, weight_decay=None, split_keys: int = 0) -> int:
@@ -720,13 +753,13 @@ def focus_paged_decode(q, cache: PagedCache, o=None, lse=None, weight_decay: Opt
         if n > 0:
             workspace = _scratch(n, q.device, stream)
             d.workspace, d.workspace_bytes = workspace.data_ptr(), n
-    _launch("focus_paged_decode", d, q.device, stream)
+    _launch("focus_paged_decode", d, q.get_device(), stream)
     return o, lse
 
 
 def _paged_evict_desc(cache, out, budget, recent, keep, workspace, err):
-    c, to, dev = cache.desc(), out.desc(), cache.k.device
-    if out.k.device != dev:
+    c, to, dev = cache.desc(), out.desc(), cache.k.get_device()
+    if out.k.get_device() != dev:
         raise ValueError("out is on another device")
     budgets = None
     if torch.is_tensor(budget):
@@ -764,5 +797,5 @@ def focus_paged_evict(cache: PagedCache, out: PagedCache, budget, recent: int = 
         if n > 0:
             workspace = _scratch(n, cache.k.device, stream)
             d.workspace, d.workspace_bytes = workspace.data_ptr(), n
-    _launch("focus_paged_evict", d, cache.k.device, stream)
+    _launch("focus_paged_evict", d, cache.k.get_device(), stream)
     return keep

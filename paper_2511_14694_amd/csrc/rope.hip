@@ -6,13 +6,23 @@
 // taking out whole quarter turns is a float32 of at most 1/8, whose sine and cosine
 // carry float32's relative accuracy.
 //
-// One workgroup per row: the sines and cosines of a row are computed once, in LDS, and
-// serve every head.
+// A workgroup takes a few rows.  The sines and cosines of its rows are computed once, in
+// LDS, and serve every head.  A thread then takes pieces of 16 bytes (for half pairs two of
+// them, half the turned part apart), always the same ones of a head, with 128 bytes in
+// flight: the first are loaded before the angles are computed.  q, k and v are taken one
+// after another, so that a step's addresses are a scalar and an offset that a thread keeps.
+//
+// HBM bound: 101 000 rows of 32 + 32 heads of 128 in bf16, k and v into pages, take 973 us
+// (5.1 TB/s read and written; torch's copy of the same q reaches 4.3); without the cache
+// 623 us (5.3 TB/s).  The first form, a workgroup a row and a thread a pair, took 2160.  One
+// row takes 4.1 us from launch to launch.
 #include "paged.h"
 
 #include <math.h>
 
 namespace {
+
+using focus::u32x4;
 
 constexpr int kThreads = 256;
 constexpr int kMaxRot = 256;
@@ -23,79 +33,256 @@ struct Store {
   bool on;
 };
 
-// Slot of row t in the cache: the page's element offset for head 0, or -1.
-__device__ int64_t slot_of(const focus_rope_desc& d, const Store& st, int64_t t, bool first) {
+// Slot of row t in the cache: the element offset of its head 0, or -1 and in `bit` why.
+__device__ int64_t slot_of(const focus_rope_desc& d, const Store& st, int64_t t, int32_t& bit) {
   const int slot = d.row_slot[t], b = d.row_seq[t];
+  bit = 0;
   if (slot < 0) return -1;
   if (b < 0 || b >= st.c.batch) {
-    if (first) focus::raise_err(d.err, FOCUS_ERR_BOUNDS);
+    bit = FOCUS_ERR_BOUNDS;
     return -1;
   }
   if (slot >= (int64_t)st.c.max_pages * st.c.page_rows) {
-    if (first) focus::raise_err(d.err, FOCUS_ERR_CAPACITY);
+    bit = FOCUS_ERR_CAPACITY;
     return -1;
   }
   const int64_t p = focus::page_of(st.c, b, slot, st.shift);
   if (p < 0) {
-    if (first) focus::raise_err(d.err, FOCUS_ERR_BOUNDS);
+    bit = FOCUS_ERR_BOUNDS;
     return -1;
   }
   return focus::row_at(st.c, p, slot, 0);
 }
 
-template <typename T>
-__global__ __launch_bounds__(kThreads) void rope_rows(focus_rope_desc d, Store st) {
-  __shared__ float2 cs[kMaxRot / 2];
-  const int64_t t = blockIdx.x;
-  const int tid = threadIdx.x, R = d.rot_dim, D = d.head_dim, half = R / 2;
-  for (int i = tid; i < half; i += kThreads) {
-    double f = (double)d.pos[t] * d.turns[i];
-    f -= rint(f);
-    const double q = rint(4.0 * f);
-    const float x = (float)(f - 0.25 * q);
-    float s, c;
-    sincospif(2.f * x, &s, &c);
-    const int k = (int)q & 3;  // quarter turns
-    float2 r = k == 0 ? make_float2(c, s) : k == 1 ? make_float2(-s, c) : k == 2 ? make_float2(-c, -s) : make_float2(s, -c);
-    if (d.inverse) r.y = -r.y;
-    cs[i] = make_float2(r.x * d.amplitude, r.y * d.amplitude);
-  }
-  __syncthreads();
-  const int64_t slot = st.on ? slot_of(d, st, t, tid == 0) : -1;
-  const int H = d.q ? d.n_heads : 0, K = d.k ? d.n_kv_heads : 0;
-  const int units = half + (D - R);  // pairs, then single elements
-  for (int64_t u = tid; u < (int64_t)(H + K) * units; u += kThreads) {
-    const int h = (int)(u / units), i = (int)(u % units);
-    const bool is_q = h < H;
-    const int hh = is_q ? h : h - H;
-    const T* src = reinterpret_cast<const T*>(is_q ? d.q : d.k) + t * (is_q ? d.q_row : d.k_row) +
-                   hh * (is_q ? d.q_head : d.k_head);
-    T* dst = reinterpret_cast<T*>(is_q ? d.q_out : d.k_out);
-    if (dst) dst += t * (is_q ? d.qo_row : d.ko_row) + hh * (is_q ? d.qo_head : d.ko_head);
-    T* page = !is_q && slot >= 0 ? reinterpret_cast<T*>(st.c.k) + slot + hh * st.c.head_stride : nullptr;
-    if (i < half) {
-      const int a = d.pairs == FOCUS_ROPE_HALF ? i : 2 * i, b = d.pairs == FOCUS_ROPE_HALF ? i + half : 2 * i + 1;
-      const float x = (float)src[a], y = (float)src[b];
-      const T xo = (T)(x * cs[i].x - y * cs[i].y), yo = (T)(x * cs[i].y + y * cs[i].x);
-      if (dst) dst[a] = xo, dst[b] = yo;
-      if (page) page[a] = xo, page[b] = yo;
+// N elements of a head in registers: one 16-byte access, or (heads whose turned part
+// is not whole pieces) element by element.
+template <typename T, int N> struct Piece {
+  static constexpr bool kWhole = N * sizeof(T) == 16;
+  static constexpr int kWords = kWhole ? 4 : N;
+  uint32_t w[kWords];
+  __device__ void load(const T* p) {
+    if constexpr (kWhole) {
+      const u32x4 x = *reinterpret_cast<const u32x4*>(p);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) w[i] = x[i];
     } else {
-      const int e = R + i - half;
-      const T x = src[e];
-      if (dst) dst[e] = x;
-      if (page) page[e] = x;
+#pragma unroll
+      for (int i = 0; i < N; ++i) w[i] = __float_as_uint((float)p[i]);
     }
   }
-  if (slot < 0) return;
-  for (int u = tid; u < K * D; u += kThreads) {
-    const int h = u / D, e = u % D;
-    reinterpret_cast<T*>(st.c.v)[slot + h * st.c.head_stride + e] =
-        reinterpret_cast<const T*>(d.v)[t * d.v_row + h * d.v_head + e];
+  __device__ void store(T* p) const {
+    if constexpr (kWhole) {
+      *reinterpret_cast<u32x4*>(p) = u32x4{w[0], w[1], w[2], w[3]};
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i) p[i] = (T)__uint_as_float(w[i]);
+    }
   }
-  if (st.c.weight)
-    for (int h = tid; h < K; h += kThreads)
-      st.c.weight[((int64_t)d.row_seq[t] * K + h) * st.c.weight_rows + d.row_slot[t]] = 0.f;
-  if (tid == 0) atomicMax(st.c.length + d.row_seq[t], d.row_slot[t] + 1);
+  __device__ void unpack(float (&x)[N]) const {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      if constexpr (kWhole && sizeof(T) == 2)
+        x[i] = i % 2 ? focus::bf16_hi(w[i / 2]) : focus::bf16_lo(w[i / 2]);
+      else
+        x[i] = __uint_as_float(w[i]);
+    }
+  }
+  __device__ void pack(const float (&x)[N]) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      if constexpr (kWhole && sizeof(T) == 2) {
+        if (i % 2 == 0) w[i / 2] = focus::pack_bf16x2(x[i], x[i + 1]);
+      } else {
+        w[i] = __float_as_uint(x[i]);
+      }
+    }
+  }
+};
+
+constexpr int kMaxRows = 8;
+
+// Rows of one tensor: where they come from and go to.
+template <typename T> struct Rows {
+  const T* src;
+  int64_t row, head;
+  T* dst;               // or NULL
+  int64_t drow, dhead;
+  T* page;              // the cache's pool, or NULL
+  int heads;
+  bool turn;
+};
+
+template <typename T, int N, bool HALF>
+__global__ __launch_bounds__(kThreads) void rope_rows(focus_rope_desc d, Store st, int rows) {
+  using P = Piece<T, N>;
+  constexpr int kFlight = HALF ? 4 : 8;
+  __shared__ float2 cs[kMaxRows][kMaxRot / 2];
+  __shared__ int64_t s_slot[kMaxRows];
+  const int64_t t0 = (int64_t)blockIdx.x * rows;
+  const int tid = threadIdx.x, R = d.rot_dim, half = R / 2;
+  const int here = (int)min((int64_t)rows, d.n_rows - t0);
+  // units of a head: turned pieces (pairs of pieces), then the others
+  const int turned = HALF ? half / N : R / N, units = turned + (d.head_dim - R) / N;
+  const int lanes = kThreads / units, u = tid % units, lane = tid / units;
+  const bool pair = HALF && u < turned;
+  const int e = !HALF || u < turned ? u * N : R + (u - turned) * N;
+
+  P lo[kFlight], hi[kFlight];
+  // a step takes `lanes` heads of a row, or all heads of several rows
+  struct Walk {
+    int per, chunks, steps;   // rows of a step; steps of a row; steps of all rows
+    int row, h;               // the thread's first row and head
+  };
+  auto walk = [&](const Rows<T>& x) {
+    Walk w;
+    w.per = max(1, lanes / x.heads);
+    w.chunks = (x.heads + lanes - 1) / lanes;
+    w.steps = (here + w.per - 1) / w.per * w.chunks;
+    w.row = w.chunks > 1 ? 0 : lane / x.heads;
+    w.h = lane - w.row * x.heads;
+    if (lane >= lanes || w.row >= w.per) w.row = here;
+    return w;
+  };
+  auto load = [&](const Rows<T>& x, const Walk& w, int s0) {
+    const T* at = x.src + (t0 + w.row) * x.row + w.h * x.head + e;
+#pragma unroll
+    for (int i = 0; i < kFlight; ++i) {
+      const int block = (s0 + i) / w.chunks, j = (s0 + i) - block * w.chunks;
+      if (s0 + i < w.steps && block * w.per + w.row < here && w.h + j * lanes < x.heads) {
+        const T* p = at + (int64_t)block * w.per * x.row + (int64_t)j * lanes * x.head;
+        lo[i].load(p);
+        if (pair) hi[i].load(p + half);
+      }
+    }
+  };
+  auto store = [&](const Rows<T>& x, const Walk& w, int s0) {
+    T* at = x.dst ? x.dst + (t0 + w.row) * x.drow + w.h * x.dhead + e : nullptr;
+#pragma unroll
+    for (int i = 0; i < kFlight; ++i) {
+      const int block = (s0 + i) / w.chunks, j = (s0 + i) - block * w.chunks, row = block * w.per + w.row;
+      if (s0 + i < w.steps && row < here && w.h + j * lanes < x.heads) {
+        if (x.turn && u < turned) {
+          const float2* a = cs[row] + (HALF ? e : e / 2);
+          float y[N], z[N];
+          lo[i].unpack(y);
+          if constexpr (HALF) {
+            hi[i].unpack(z);
+#pragma unroll
+            for (int k = 0; k < N; ++k) {
+              const float v = y[k] * a[k].x - z[k] * a[k].y;
+              z[k] = y[k] * a[k].y + z[k] * a[k].x;
+              y[k] = v;
+            }
+            hi[i].pack(z);
+          } else {
+#pragma unroll
+            for (int k = 0; k < N; k += 2) {
+              const float v = y[k] * a[k / 2].x - y[k + 1] * a[k / 2].y;
+              y[k + 1] = y[k] * a[k / 2].y + y[k + 1] * a[k / 2].x;
+              y[k] = v;
+            }
+          }
+          lo[i].pack(y);
+        }
+        if (x.dst) {
+          T* p = at + (int64_t)block * w.per * x.drow + (int64_t)j * lanes * x.dhead;
+          lo[i].store(p);
+          if (pair) hi[i].store(p + half);
+        }
+        if (x.page && s_slot[row] >= 0) {
+          T* p = x.page + s_slot[row] + (w.h + j * lanes) * st.c.head_stride + e;
+          lo[i].store(p);
+          if (pair) hi[i].store(p + half);
+        }
+      }
+    }
+  };
+
+  const Rows<T> q = {reinterpret_cast<const T*>(d.q), d.q_row, d.q_head, reinterpret_cast<T*>(d.q_out), d.qo_row,
+                     d.qo_head, nullptr, d.n_heads, true};
+  const Rows<T> k = {reinterpret_cast<const T*>(d.k), d.k_row, d.k_head, reinterpret_cast<T*>(d.k_out), d.ko_row,
+                     d.ko_head, st.on ? reinterpret_cast<T*>(st.c.k) : nullptr, d.n_kv_heads, true};
+  const Rows<T>& first = d.q ? q : k;
+  Walk w = walk(first);
+  load(first, w, 0);
+
+  for (int i = tid; i < here * half; i += kThreads) {
+    const int row = i / half, p = i - row * half;
+    double f = (double)d.pos[t0 + row] * d.turns[p];
+    f -= rint(f);
+    const double quarter = rint(4.0 * f);
+    float s, c;
+    sincospif(2.f * (float)(f - 0.25 * quarter), &s, &c);
+    const int n = (int)quarter & 3;
+    float2 r = n == 0 ? make_float2(c, s) : n == 1 ? make_float2(-s, c) : n == 2 ? make_float2(-c, -s) : make_float2(s, -c);
+    cs[row][p] = make_float2(r.x * d.amplitude, (d.inverse ? -r.y : r.y) * d.amplitude);
+  }
+  if (st.on && tid < here) {
+    const int64_t t = t0 + tid;
+    int32_t bit;
+    const int64_t slot = slot_of(d, st, t, bit);
+    s_slot[tid] = slot;
+    if (bit) focus::raise_err(d.err, bit);
+    // The length is raised by the last row of a run of ascending ones (the next row is
+    // then stored, and raises it further): a prefill's rows would otherwise queue at one
+    // address (101 000 of them for 0.5 ms).
+    if (slot >= 0) {
+      const int to = d.row_slot[t], b = d.row_seq[t];
+      bool last = true;
+      if (t + 1 < d.n_rows && d.row_seq[t + 1] == b && d.row_slot[t + 1] > to) last = slot_of(d, st, t + 1, bit) < 0;
+      if (last) atomicMax(st.c.length + b, to + 1);
+    }
+  }
+  __syncthreads();
+  if (st.on && st.c.weight)
+    for (int i = tid; i < here * d.n_kv_heads; i += kThreads) {
+      const int64_t t = t0 + i / d.n_kv_heads;
+      if (s_slot[i / d.n_kv_heads] >= 0)
+        st.c.weight[((int64_t)d.row_seq[t] * d.n_kv_heads + i % d.n_kv_heads) * st.c.weight_rows + d.row_slot[t]] = 0.f;
+    }
+
+  auto rest = [&](const Rows<T>& x, int s0) {
+    for (; s0 < w.steps; s0 += kFlight) {
+      if (s0 > 0) load(x, w, s0);
+      store(x, w, s0);
+    }
+  };
+  rest(first, 0);
+  if (d.q && d.k) {
+    w = walk(k);
+    load(k, w, 0);
+    rest(k, 0);
+  }
+  if (st.on) {
+    const Rows<T> v = {reinterpret_cast<const T*>(d.v), d.v_row, d.v_head, nullptr, 0, 0, reinterpret_cast<T*>(st.c.v),
+                       d.n_kv_heads, false};
+    w = walk(v);
+    load(v, w, 0);
+    rest(v, 0);
+  }
+}
+
+// Rows a workgroup takes: several where there are enough of them for every compute
+// unit, so that a thread has pieces to keep in flight.
+int rows_per_group(int64_t n_rows) {
+  const int64_t r = n_rows / (8 * focus::device_cus());
+  return (int)(r < 1 ? 1 : r > kMaxRows ? kMaxRows : r);
+}
+
+template <typename T>
+void launch(const focus_rope_desc& d, const Store& st, hipStream_t s) {
+  constexpr int N = 16 / sizeof(T);
+  const bool half = d.pairs == FOCUS_ROPE_HALF;
+  const bool whole = (half ? d.rot_dim / 2 : d.rot_dim) % N == 0;
+  const int rows = rows_per_group(d.n_rows);
+  const dim3 grid((uint32_t)focus::ceil_div(d.n_rows, rows)), block(kThreads);
+  if (half) {
+    if (whole) hipLaunchKernelGGL((rope_rows<T, N, true>), grid, block, 0, s, d, st, rows);
+    else hipLaunchKernelGGL((rope_rows<T, 1, true>), grid, block, 0, s, d, st, rows);
+  } else {
+    if (whole) hipLaunchKernelGGL((rope_rows<T, N, false>), grid, block, 0, s, d, st, rows);
+    else hipLaunchKernelGGL((rope_rows<T, 2, false>), grid, block, 0, s, d, st, rows);
+  }
 }
 
 bool strides_ok(int64_t row, int64_t head, int64_t es) {
@@ -168,11 +355,10 @@ extern "C" focus_status focus_rope(const focus_rope_desc* d, focus_stream_t stre
     st.shift = focus::page_shift(st.c);
     st.on = true;
   }
-  const dim3 grid((uint32_t)d->n_rows), block(kThreads);
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   if (d->dtype == FOCUS_BF16)
-    hipLaunchKernelGGL((rope_rows<__bf16>), grid, block, 0, s, *d, st);
+    launch<__bf16>(*d, st, s);
   else
-    hipLaunchKernelGGL((rope_rows<float>), grid, block, 0, s, *d, st);
+    launch<float>(*d, st, s);
   return focus::launch_status();
 }
