@@ -716,8 +716,8 @@ typedef struct {
   void* k;
   void* v;
   int64_t page_stride;          /* elements, >= head_dim, whole 16-byte      */
-  int64_t row_stride;           /*   pieces; no two rows may overlap         */
-  int64_t head_stride;
+  int64_t row_stride;           /*   pieces; no two rows may overlap; row    */
+  int64_t head_stride;          /*   stride below 2^31                       */
   int32_t batch;
   int32_t max_pages;            /* entries of a sequence in table            */
   const int32_t* table;         /* [batch, max_pages]                        */
@@ -792,8 +792,7 @@ focus_status focus_rope(const focus_rope_desc* d, focus_stream_t stream);
  *     weight[b, g, r] = weight_decay * weight[b, g, r] + sum of the softmax weights of
  *                       row r over the heads of g        (accumulate; rows < length[b])
  * With weight_decay 0 the old weight is not read.  A sequence of length 0 has o = 0
- * and lse = -inf.  Rows past the length are never read, so whatever their page holds
- * has no effect.
+ * and lse = -inf.  Whatever the pages hold past a sequence's length has no effect.
  * The rows of a sequence are split over several workgroups, joined by log-sum-exp;
  * with split_keys = 0 the split follows the lengths of the whole batch, so that a
  * sequence's bits may differ by float32 rounding with what else is in the batch; a

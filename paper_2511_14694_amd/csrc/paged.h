@@ -39,6 +39,7 @@ inline focus_status check_paged(const focus_paged_kv& c) {
       !pieces16(c.page_stride, es) || !pieces16(c.row_stride, es) || !pieces16(c.head_stride, es) ||
       !disjoint_rows<3>(c.head_dim, {c.page_stride, c.row_stride, c.head_stride}, {c.n_pages, c.page_rows, c.n_kv_heads}))
     return FOCUS_E_ARG;
+  if (c.row_stride > INT32_MAX) return FOCUS_E_SHAPE;
   if (c.weight && c.weight_rows < (int64_t)c.max_pages * c.page_rows) return FOCUS_E_SHAPE;
   if (c.batch == 0) return FOCUS_OK;
   if (!c.length || (c.max_pages > 0 && !c.table) || (c.n_pages > 0 && (!c.k || !c.v))) return FOCUS_E_NULL;

@@ -26,6 +26,7 @@
 #include <math.h>
 
 #include <algorithm>
+#include <type_traits>
 
 namespace {
 
@@ -39,11 +40,11 @@ constexpr float kLog2e = 1.44269504088896341f;
 constexpr float kMinit = -1.0e30f;
 constexpr int kThreads = 256, kWaves = 4;
 constexpr int kCols = 16;       // query heads of a workgroup: columns of a product
-constexpr int kPages = 1024;    // page numbers held in LDS at a time
+constexpr int kPages = 1024;    // page offsets held in LDS at a time
 constexpr int kUnit = 128;      // chunks are multiples of this many rows
 
-// What a lane reads in the place of a row that is past its sequence's end or in a page
-// outside the pool (such a row may hold anything, and zero times a NaN is a NaN).
+// What a lane reads in the place of eight rows that begin past their sequence's end or
+// lie in a page outside the pool.
 __device__ __align__(16) const uint32_t kZeros[256] = {};
 
 // Workspace: int4 info[batch] {first slot, chunks, rows, 0}, then the partials of
@@ -111,7 +112,7 @@ __device__ bool find_chunk(const Args& a, int i, Chunk& out) {
     }
     const int64_t per = (total + a.target - 1) / a.target;
     rows = (int)min((per + kUnit - 1) / kUnit * kUnit, (int64_t)1 << 30);
-    rows = max(rows, kUnit);
+    rows = __builtin_amdgcn_readfirstlane(max(rows, kUnit));
   }
   int before = 0;
   for (int b0 = 0; b0 < c.batch; b0 += 64) {
@@ -123,14 +124,14 @@ __device__ bool find_chunk(const Args& a, int i, Chunk& out) {
       const int y = __shfl_up(upto, k);
       if (lane >= k) upto += y;
     }
-    const int all = __shfl(upto, 63);
+    const int all = __builtin_amdgcn_readlane(upto, 63);
     if (i < before + all) {
       const uint64_t past = __ballot(i < before + upto);
       const int at = __ffsll((unsigned long long)past) - 1;
       out.b = b0 + at;
-      out.n = __shfl(n, at);
-      out.chunks = __shfl(own, at);
-      out.slot0 = before + __shfl(upto, at) - out.chunks;
+      out.n = __builtin_amdgcn_readlane(n, at);
+      out.chunks = __builtin_amdgcn_readlane(own, at);
+      out.slot0 = before + __builtin_amdgcn_readlane(upto, at) - out.chunks;
       out.c = i - out.slot0;
       out.rows = rows;
       return true;
@@ -149,20 +150,35 @@ template <typename T, int D> struct Tile {
   static constexpr int kPiece = 16 / sizeof(T);     // elements of a 16-byte load
   static constexpr int kSteps = D / (4 * kPiece);   // 16-byte pieces of a K row a lane holds
   static constexpr int kProducts = kBf16 ? 2 : 1;   // K rows a lane holds
+  // pieces of 16 bytes (8 where a lane's share of a V row is that): whole vectors, which
+  // stay where their load puts them
+  using V = typename std::conditional<kWords == 2, u32x2, u32x4>::type;
+  static constexpr int kVSize = sizeof(V) / 4, kVs = kWords / kVSize;
   u32x4 k[kProducts][kSteps];
-  uint32_t v[kScores][kWords];
+  V v[kScores][kVs];
+  __device__ uint32_t word(int j, int i) const { return v[j][i / kVSize][i % kVSize]; }
 };
+
+// Load once, from global memory: the compiler takes a choice between a page and kZeros
+// for an address of any kind, whose loads it can only wait for all together.
+template <typename V>
+__device__ __forceinline__ V load_once(const void* p) {
+  return __builtin_nontemporal_load(reinterpret_cast<const __attribute__((address_space(1))) V*>(
+      reinterpret_cast<uintptr_t>(p)));
+}
 
 template <typename T, int D>
 __global__ __launch_bounds__(kThreads, 2) void paged_attend(Args a) {
   using L = Tile<T, D>;
   constexpr int kPitch = D + 4;
-  __shared__ int s_page[kPages + 1];  // (a chunk may begin inside a page)
+  __shared__ int64_t s_page[kPages + 1];  // (a chunk may begin inside a page)
   __shared__ float s_o[kWaves][kCols][kPitch];
   __shared__ float2 s_ml[kWaves][kCols];
   const focus_paged_kv& c = a.d.cache;
   const int K = c.n_kv_heads, H = a.d.n_heads, G = H / K;
-  const int tid = threadIdx.x, wave = tid / 64, lane = tid % 64, col = lane % 16, x = lane / 16;
+  // (a wave's number in a scalar register: its loops are branches then, not masks)
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / 64);
+  const int lane = tid % 64, col = lane % 16, x = lane / 16;
   const int tile_id = blockIdx.x % a.tiles, g = blockIdx.x / a.tiles % K;
   Chunk ch;
   if (!find_chunk(a, blockIdx.x / (a.tiles * K), ch)) return;
@@ -196,7 +212,8 @@ __global__ __launch_bounds__(kThreads, 2) void paged_attend(Args a) {
   f32x4 o[L::kPer];
   // The low part of the weights (below) turns an infinity in V into a NaN: sums that are
   // NaN are taken again without it (the others keep what they are).
-  for (bool low = true;; low = false) {
+  auto pass = [&](auto with_low) {
+    constexpr bool low = decltype(with_low)::value;
     m = kMinit;
     l = 0.f;
 #pragma unroll
@@ -207,40 +224,30 @@ __global__ __launch_bounds__(kThreads, 2) void paged_attend(Args a) {
       for (int i = tid; i + page0 <= (seg_end - 1) >> a.shift; i += kThreads) {
         const int64_t p = focus::page_of(c, b, (i + page0) << a.shift, a.shift);
         if (p < 0 && first) focus::raise_err(a.d.err, FOCUS_ERR_BOUNDS);
-        s_page[i] = (int)p;
+        s_page[i] = p < 0 ? -1 : p * c.page_stride;
       }
       __syncthreads();
-      // page of the eight rows at r (-1: none)
-      auto page = [&](int r) { return r < seg_end ? s_page[(r >> a.shift) - page0] : -1; };
-      auto load = [&](L& w, int r) {
-        const int pk = page(r + k8), pv = page(r + v8);
-        const T* kp = kbase + pk * c.page_stride + (int64_t)((r + k8) & mask) * c.row_stride;
-        const T* vp = vbase + pv * c.page_stride + (int64_t)((r + v8) & mask) * c.row_stride;
+      // whole tiles end here
+      const int full_end = seg_end - (seg_end - seg) % L::kRows;
+      // offset of the page that holds the eight rows at r (negative: none, or past end)
+      auto page = [&](int r, int end) { return r < end ? s_page[(r >> a.shift) - page0] : -1; };
+      // Rows of eight lie in one page, so all of them can be read where the first is cached.
+      auto load = [&](L& w, int r, int end) {
+        const int64_t pk = page(r + k8, end), pv = page(r + v8, end);
+        const uint32_t step = (uint32_t)c.row_stride;
+        const uint64_t ks = pk >= 0 ? step : 0, vs = pv >= 0 ? step : 0;
+        const T* kp = (pk >= 0 ? kbase + pk + (uint64_t)(uint32_t)((r + k8) & mask) * step : zeros) + k_in * ks + x * L::kPiece;
+        const T* vp = (pv >= 0 ? vbase + pv + (uint64_t)(uint32_t)((r + v8) & mask) * step : zeros) + v_in * vs + col * L::kPer;
 #pragma unroll
-        for (int t = 0; t < L::kProducts; ++t) {
-          const int in = k_in + 4 * t;
-          const T* p = pk >= 0 && r + k8 + in < seg_end ? kp + in * c.row_stride : zeros;
+        for (int t = 0; t < L::kProducts; ++t)
 #pragma unroll
-          for (int i = 0; i < L::kSteps; ++i) w.k[t][i] = *reinterpret_cast<const u32x4*>(p + (i * 4 + x) * L::kPiece);
-        }
+          for (int i = 0; i < L::kSteps; ++i) w.k[t][i] = load_once<u32x4>(kp + 4 * t * ks + i * 4 * L::kPiece);
 #pragma unroll
-        for (int j = 0; j < L::kScores; ++j) {
-          const int in = v_in + j;
-          const T* p = (pv >= 0 && r + v8 + in < seg_end ? vp + in * c.row_stride : zeros) + col * L::kPer;
-          if constexpr (L::kWords == 2) {
-            const u32x2 y = *reinterpret_cast<const u32x2*>(p);
-            w.v[j][0] = y[0], w.v[j][1] = y[1];
-          } else {
+        for (int j = 0; j < L::kScores; ++j)
 #pragma unroll
-            for (int i = 0; i < L::kWords / 4; ++i) {
-              const u32x4 y = reinterpret_cast<const u32x4*>(p)[i];
-#pragma unroll
-              for (int e = 0; e < 4; ++e) w.v[j][4 * i + e] = y[e];
-            }
-          }
-        }
+          for (int i = 0; i < L::kVs; ++i) w.v[j][i] = load_once<typename L::V>(vp + j * vs + i * L::kPiece);
       };
-      auto compute = [&](const L& w, int r) {
+      auto compute = [&](L& w, int r, auto whole) {
         f32x4 s[L::kProducts];
 #pragma unroll
         for (int t = 0; t < L::kProducts; ++t) {
@@ -259,14 +266,24 @@ __global__ __launch_bounds__(kThreads, 2) void paged_attend(Args a) {
           }
         }
         const int row = r + v8 + v_in;  // of the lane's first score
-        const int live = page(r + v8) >= 0 ? seg_end - row : 0;
+        // of the lane's rows, those that count: the first `live`
+        int live = page(r + v8, seg_end) >= 0 ? L::kScores : 0;
+        if constexpr (!decltype(whole)::value) {
+          live = min(live, seg_end - row);
+          // rows past the end may hold anything, and zero times a NaN is a NaN
+#pragma unroll
+          for (int j = 0; j < L::kScores; ++j)
+#pragma unroll
+            for (int i = 0; i < L::kVs; ++i)
+              if (j >= live) w.v[j][i] = typename L::V{};
+        }
         float y[L::kScores], mx = m;
 #pragma unroll
         for (int j = 0; j < L::kScores; ++j) {
           y[j] = j < live ? s[j / 4][j % 4] * a.sc : -INFINITY;
           mx = fmaxf(mx, y[j]);
         }
-        if (score && row < seg_end) {
+        if (score && (decltype(whole)::value || row < seg_end)) {
 #pragma unroll
           for (int j = 0; j < L::kScores; j += 4)
             *reinterpret_cast<float4*>(score + row + j) = make_float4(y[j], y[j + 1], y[j + 2], y[j + 3]);
@@ -297,32 +314,44 @@ __global__ __launch_bounds__(kThreads, 2) void paged_attend(Args a) {
             u32x4 z;
 #pragma unroll
             for (int e = 0; e < 4; ++e)
-              z[e] = __builtin_amdgcn_perm(w.v[2 * e + 1][t / 2], w.v[2 * e][t / 2], t % 2 ? 0x07060302 : 0x05040100);
+              z[e] = __builtin_amdgcn_perm(w.word(2 * e + 1, t / 2), w.word(2 * e, t / 2), t % 2 ? 0x07060302 : 0x05040100);
             o[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, z), hi, o[t], 0, 0, 0);
-            if (low) o[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, z), lo, o[t], 0, 0, 0);
+            if constexpr (low) o[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, z), lo, o[t], 0, 0, 0);
           }
         } else {
 #pragma unroll
           for (int j = 0; j < 4; ++j)
 #pragma unroll
             for (int t = 0; t < L::kPer; ++t)
-              o[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(w.v[j][t]), y[j], o[t], 0, 0, 0);
+              o[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(w.word(j, t)), y[j], o[t], 0, 0, 0);
         }
       };
-      // a wave's tiles, the next one's loads in flight while one is computed
+      // A wave's whole tiles, two a round, the next one's loads in flight while one is
+      // computed; then, for one wave, the tile that the chunk ends in.  One way out of the
+      // loop, loads past the end taken from kZeros and the last of them waited for behind
+      // it: otherwise the compiler cannot tell which loads are in flight at a round's start
+      // and waits for half of them.
       constexpr int kStep = kWaves * L::kRows;
       int r = seg + wave * L::kRows;
-      if (r < seg_end) {
+      if (r < full_end) {
         L w0, w1;
-        load(w0, r);
-        while (true) {
-          if (r + kStep < seg_end) load(w1, r + kStep);
-          compute(w0, r);
-          if ((r += kStep) >= seg_end) break;
-          if (r + kStep < seg_end) load(w0, r + kStep);
-          compute(w1, r);
-          if ((r += kStep) >= seg_end) break;
+        load(w0, r, full_end);
+        for (; r + kStep < full_end; r += 2 * kStep) {
+          load(w1, r + kStep, full_end);
+          compute(w0, r, std::true_type{});
+          load(w0, r + 2 * kStep, full_end);
+          compute(w1, r + kStep, std::true_type{});
         }
+        if (r < full_end) {
+          compute(w0, r, std::true_type{});
+          r += kStep;
+        }
+        __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0)
+      }
+      if (r < seg_end && r == full_end) {
+        L w;
+        load(w, r, seg_end);
+        compute(w, r, std::false_type{});
       }
     }
     bool nan = false;
@@ -332,7 +361,7 @@ __global__ __launch_bounds__(kThreads, 2) void paged_attend(Args a) {
       for (int t = 0; t < L::kPer; t += 4) {
         float4* to = reinterpret_cast<float4*>(&s_o[wave][col][(x * 4 + e) * L::kPer + t]);
         float4 y = make_float4(o[t][e], o[t + 1][e], o[t + 2][e], o[t + 3][e]);
-        if (!low) {
+        if (L::kBf16 && !low) {
           const float4 was = *to;
           y = make_float4(was.x == was.x ? was.x : y.x, was.y == was.y ? was.y : y.y, was.z == was.z ? was.z : y.z,
                           was.w == was.w ? was.w : y.w);
@@ -340,7 +369,11 @@ __global__ __launch_bounds__(kThreads, 2) void paged_attend(Args a) {
         *to = y;
         nan |= y.x != y.x || y.y != y.y || y.z != y.z || y.w != y.w;
       }
-    if (!L::kBf16 || !low || !__syncthreads_or(nan)) break;
+    return nan;
+  };
+  const bool nan = pass(std::integral_constant<bool, L::kBf16>{});
+  if constexpr (L::kBf16) {
+    if (__syncthreads_or(nan)) pass(std::false_type{});
   }
 
   // the waves' parts, joined
@@ -389,44 +422,65 @@ __device__ float2 joined(const Args& a, const int4& info, int h) {
   return make_float2(M, L);
 }
 
-constexpr int kWeightRows = 1024;   // rows of a workgroup that writes weights
+constexpr int kWeightRows = 4 * kThreads;   // rows of a workgroup that writes weights
 
+// The first `joins` workgroups merge the partials of a (sequence, head) each: D / 4
+// threads over the output, the other groups of them over the chunks, eight loads in
+// flight each, the first of them before the maximum is known.  The others write weights.
 template <typename T, int D>
 __global__ __launch_bounds__(kThreads) void paged_join(Args a, int joins, int row_blocks) {
   const focus_paged_kv& c = a.d.cache;
   const int K = c.n_kv_heads, H = a.d.n_heads, G = H / K, tid = threadIdx.x;
   if ((int)blockIdx.x < joins) {
-    __shared__ float s_o[kThreads / D][D];
+    constexpr int kLanes = D / 4, kGroups = kThreads / kLanes, kFlight = 8;
+    __shared__ float4 s_o[kGroups][kLanes];
     const int b = blockIdx.x / H, h = blockIdx.x % H;
     const int4 info = a.info[b];
     if (info.y == 1) return;
-    const float2 ml = joined(a, info, h);
-    constexpr int kGroups = kThreads / D;
-    const int e = tid % D, grp = tid / D;
-    float y = 0.f;
-    for (int i = grp; i < info.y; i += kGroups) {
-      const int64_t slot = (int64_t)(info.x + i) * H + h;
-      y = fmaf(a.o[slot * D + e], __builtin_amdgcn_exp2f(a.ml[slot].x - ml.x), y);
+    const int e = tid % kLanes, grp = tid / kLanes;
+    const float4* o = reinterpret_cast<const float4*>(a.o);
+    float2 ml = {};
+    float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int i0 = grp; i0 == grp || i0 < info.y; i0 += kGroups * kFlight) {
+      float4 y[kFlight];
+      float m[kFlight];
+#pragma unroll
+      for (int k = 0; k < kFlight; ++k) {
+        const int64_t slot = (int64_t)(info.x + min(i0 + k * kGroups, info.y - 1)) * H + h;
+        y[k] = o[slot * kLanes + e];
+        m[k] = a.ml[slot].x;
+      }
+      if (i0 == grp) ml = joined(a, info, h);
+#pragma unroll
+      for (int k = 0; k < kFlight; ++k) {
+        if (i0 + k * kGroups < info.y) {
+          const float f = __builtin_amdgcn_exp2f(m[k] - ml.x);
+          sum.x = fmaf(y[k].x, f, sum.x), sum.y = fmaf(y[k].y, f, sum.y);
+          sum.z = fmaf(y[k].z, f, sum.z), sum.w = fmaf(y[k].w, f, sum.w);
+        }
+      }
     }
-    s_o[grp][e] = y;
+    s_o[grp][e] = sum;
     __syncthreads();
     if (tid < D) {
+      float y = 0.f;
 #pragma unroll
-      for (int k = 1; k < kGroups; ++k) y += s_o[k][e];
+      for (int k = 0; k < kGroups; ++k) y += reinterpret_cast<const float*>(s_o[k])[tid];
       const int64_t at = (int64_t)b * H + h;
-      reinterpret_cast<T*>(a.d.o)[at * D + e] = (T)(ml.y == 0.f ? 0.f : y / ml.y);
-      if (e == 0 && a.d.lse) a.d.lse[at] = ml.y == 0.f ? -INFINITY : (ml.x + log2f(ml.y)) * kLn2;
+      reinterpret_cast<T*>(a.d.o)[at * D + tid] = (T)(ml.y == 0.f ? 0.f : y / ml.y);
+      if (tid == 0 && a.d.lse) a.d.lse[at] = ml.y == 0.f ? -INFINITY : (ml.x + log2f(ml.y)) * kLn2;
     }
     return;
   }
-  // weights of the rows of one (sequence, KV head)
+  // weights of rows of one (sequence, KV head), four a thread
   const int item = blockIdx.x - joins, part = item % row_blocks, g = item / row_blocks % K, b = item / row_blocks / K;
   const int4 info = a.info[b];
   const int n = info.z;
   float* w = c.weight + ((int64_t)b * K + g) * c.weight_rows;
   __shared__ float s_lse[kThreads];
   for (int r0 = part * kWeightRows; r0 < n; r0 += row_blocks * kWeightRows) {
-    float x[kWeightRows / kThreads] = {};
+    const int r = r0 + 4 * tid;
+    float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
     for (int hb = 0; hb < G; hb += kThreads) {
       const int some = min(kThreads, G - hb);
       __syncthreads();
@@ -435,20 +489,21 @@ __global__ __launch_bounds__(kThreads) void paged_join(Args a, int joins, int ro
         if (tid % 64 == 0) s_lse[h] = ml.y == 0.f ? INFINITY : ml.x + log2f(ml.y);
       }
       __syncthreads();
-      for (int h = 0; h < some; ++h) {
-        const float* s = a.score + ((int64_t)b * H + g * G + hb + h) * a.cap;
-#pragma unroll
-        for (int i = 0; i < kWeightRows / kThreads; ++i) {
-          const int r = r0 + i * kThreads + tid;
-          if (r < n) x[i] += __builtin_amdgcn_exp2f(s[r] - s_lse[h]);
+      const float* score = a.score + ((int64_t)b * H + g * G + hb) * a.cap + r;
+      if (r < n) {
+#pragma unroll 4
+        for (int h = 0; h < some; ++h) {
+          const float4 s = *reinterpret_cast<const float4*>(score + h * a.cap);
+          x.x += __builtin_amdgcn_exp2f(s.x - s_lse[h]), x.y += __builtin_amdgcn_exp2f(s.y - s_lse[h]);
+          x.z += __builtin_amdgcn_exp2f(s.z - s_lse[h]), x.w += __builtin_amdgcn_exp2f(s.w - s_lse[h]);
         }
       }
     }
+    // (scores are stored up to the next multiple of four rows; weights end at n)
+    const float y[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
-    for (int i = 0; i < kWeightRows / kThreads; ++i) {
-      const int r = r0 + i * kThreads + tid;
-      if (r < n) w[r] = a.d.weight_decay == 0.f ? x[i] : fmaf(a.d.weight_decay, w[r], x[i]);
-    }
+    for (int i = 0; i < 4; ++i)
+      if (r + i < n) w[r + i] = a.d.weight_decay == 0.f ? y[i] : fmaf(a.d.weight_decay, w[r + i], y[i]);
   }
 }
 
@@ -475,7 +530,7 @@ focus_status launch(const Args& a, const Plan& p, hipStream_t s) {
   const int joins = c.batch * a.d.n_heads;
   // enough workgroups to write the weights at the memory's rate, not one per row of the table
   const int64_t per = focus::ceil_div(p.cap > 0 ? p.cap : 1, kWeightRows), heads = (int64_t)c.batch * c.n_kv_heads;
-  const int64_t row_blocks = std::min(per, std::max<int64_t>(1, focus::ceil_div(8 * focus::device_cus(), heads)));
+  const int64_t row_blocks = std::min(per, std::max<int64_t>(1, focus::ceil_div(16 * focus::device_cus(), heads)));
   const int64_t second = joins + (a.d.accumulate ? heads * row_blocks : 0);
   if (blocks > INT32_MAX / kThreads || second > INT32_MAX / kThreads) return FOCUS_E_SHAPE;
   hipLaunchKernelGGL((paged_attend<T, D>), dim3((uint32_t)blocks), dim3(kThreads), 0, s, a);
