@@ -1,11 +1,25 @@
 // A paged K/V cache cut down to a budget by accumulated weight (focus_paged_evict).
 //
-//   evict_select  one workgroup per (sequence, KV head): the weight of the last row
-//                 kept by a radix selection, eight bits a pass over an order-preserving
-//                 integer of the weights, then one ordered pass that writes the kept
-//                 rows (prefix counts settle which of the equal weights stay)
+// The weight of the last row kept is found by a radix selection over an order-preserving
+// integer of the weights, in digits of 11, 11 and 10 bits: a histogram of a digit among
+// the rows that share the digits above says in which bucket the row lies and how many of
+// it are still wanted.  Then the rows above that weight and the first of those that equal
+// it are written in order; a wave holds consecutive rows, so one prefix sum over the
+// waves places them.
+//
+//   evict_select  tables of up to 32 768 rows: one workgroup per (sequence, KV head), the
+//                 weights in registers throughout; where a head's rows are few, or heads
+//                 enough to fill the device, it copies them as well
+//   evict_count   longer tables: a workgroup per 8 192 rows, one launch a digit, each
+//                 adding up the histograms of the digit before
+//   evict_keep    and the rows kept; what a workgroup's rows add to the ones before it
+//                 follows from the same histograms
 //   evict_copy    the kept rows and their weights to the pages of `out`
+//
+// The copy is HBM bound; the selection by the latency of its passes.
 #include "paged.h"
+
+#include <algorithm>
 
 namespace {
 
@@ -51,81 +65,324 @@ __device__ inline int scan(int x, int* waves, int* total) {
   return before + y - x;
 }
 
-__global__ __launch_bounds__(kThreads) void evict_select(focus_paged_evict_desc d) {
-  __shared__ int hist[256], waves[kWaves];
-  __shared__ int s_bucket, s_rest;
-  const int K = d.cache.n_kv_heads, b = blockIdx.x / K, g = blockIdx.x % K, tid = threadIdx.x;
-  const int n = focus::paged_length(d.cache, b);
-  int32_t bits = n != d.cache.length[b] ? FOCUS_ERR_CAPACITY : 0;
-  const int m = kept_rows(d, b, n, &bits);
-  if (bits && tid == 0 && g == 0) focus::raise_err(d.err, bits);
-  const int recent = min(d.recent, m), old = n - recent, take = m - recent;
-  const float* w = d.cache.weight + ((int64_t)b * K + g) * d.cache.weight_rows;
-  int32_t* keep = d.keep + ((int64_t)b * K + g) * d.keep_rows;
-  for (int64_t j = m + tid; j < d.keep_rows; j += kThreads) keep[j] = -1;
-  for (int j = tid; j < recent; j += kThreads) keep[take + j] = old + j;
-  if (take == 0) return;
-  // threshold: the take-th greatest of the old rows; `equal` of the rows that equal it stay
-  uint32_t prefix = 0;
-  int equal = take;
-  for (int shift = 24; shift >= 0; shift -= 8) {
-    if (tid < 256) hist[tid] = 0;
-    __syncthreads();
-    const uint32_t mask = shift == 24 ? 0u : 0xffffffffu << (shift + 8);
-    for (int r = tid; r < old; r += kThreads) {
-      const uint32_t u = order_of(w[r]);
-      if ((u & mask) == prefix) atomicAdd(&hist[(u >> shift) & 255], 1);
-    }
-    __syncthreads();
-    // rows in the buckets above this thread's
-    const int x = tid < 256 ? hist[255 - tid] : 0;
-    int total;
-    const int above = scan(x, waves, &total);
-    if (tid < 256 && above < equal && above + x >= equal) s_bucket = 255 - tid, s_rest = equal - above;
-    __syncthreads();
-    prefix |= (uint32_t)s_bucket << shift;
-    equal = s_rest;
-  }
-  int at = 0, ties = 0;
-  for (int r0 = 0; r0 < old; r0 += kThreads) {
-    const int r = r0 + tid;
-    const uint32_t u = r < old ? order_of(w[r]) : 0u;
-    const bool tie = r < old && u == prefix;
-    int total;
-    const int before = scan(tie ? 1 : 0, waves, &total);
-    const bool in = r < old && (u > prefix || (tie && ties + before < equal));
-    ties += total;
-    const int j = at + scan(in ? 1 : 0, waves, &total);
-    if (in) keep[j] = r;
-    at += total;
+constexpr int kDigits = 3, kBins = 2048;
+__device__ constexpr int digit_shift(int i) { return i == 0 ? 21 : i == 1 ? 10 : 0; }
+__device__ constexpr uint32_t digit_mask(int i) { return i == 2 ? 1023u : 2047u; }
+// the digits above digit i
+__device__ constexpr uint32_t above_mask(int i) { return i == 0 ? 0u : 0xffffffffu << digit_shift(i - 1); }
+
+// What a workgroup knows of one (sequence, KV head).
+struct Head {
+  int b, g, n;
+  int old, recent, take;  // rows before the recent ones; recent ones; how many old ones stay
+  const float* w;
+  int32_t* keep;
+};
+__device__ Head head_of(const focus_paged_evict_desc& d, int bg, bool report) {
+  const int K = d.cache.n_kv_heads;
+  Head h;
+  h.b = bg / K, h.g = bg % K;
+  h.n = focus::paged_length(d.cache, h.b);
+  int32_t bits = h.n != d.cache.length[h.b] ? FOCUS_ERR_CAPACITY : 0;
+  const int m = kept_rows(d, h.b, h.n, &bits);
+  if (report && bits && h.g == 0 && threadIdx.x == 0) focus::raise_err(d.err, bits);
+  h.recent = min(d.recent, m), h.old = h.n - h.recent, h.take = m - h.recent;
+  h.w = d.cache.weight + (int64_t)bg * d.cache.weight_rows;
+  h.keep = d.keep + (int64_t)bg * d.keep_rows;
+  return h;
+}
+
+// The rows of a workgroup in registers, as integers of their weights' order: NR a thread,
+// wave w the rows from first + 64 NR w, a register's 64 rows consecutive.
+template <int NR>
+__device__ void load_keys(const Head& h, int first, uint32_t (&key)[NR], int& row0) {
+  row0 = first + (int)(threadIdx.x / 64) * 64 * NR + (int)(threadIdx.x % 64);
+  float w[NR];
+#pragma unroll
+  for (int i = 0; i < NR; ++i) w[i] = row0 + 64 * i < h.old ? h.w[row0 + 64 * i] : 0.f;
+#pragma unroll
+  for (int i = 0; i < NR; ++i) key[i] = order_of(w[i]);
+}
+
+// Histogram of a digit among the rows that share the digits above it, added to hist
+// (cleared by the caller).  Lanes that share the first one's bucket are counted at once:
+// atomics on one address go one after another, and equal weights are common.
+template <int NR>
+__device__ void count_digit(const Head& h, const uint32_t (&key)[NR], int row0, int digit, uint32_t prefix, int* hist) {
+  const uint32_t mask = above_mask(digit), dm = digit_mask(digit);
+  const int shift = digit_shift(digit);
+#pragma unroll
+  for (int i = 0; i < NR; ++i) {
+    const bool in = row0 + 64 * i < h.old && (key[i] & mask) == prefix;
+    const uint64_t any = __ballot(in);
+    if (any == 0) continue;
+    const int bin = (key[i] >> shift) & dm;
+    const int lead = __ffsll((unsigned long long)any) - 1;
+    const int one = __builtin_amdgcn_readlane(bin, lead);
+    const uint64_t same = __ballot(in && bin == one);
+    if ((int)(threadIdx.x % 64) == lead) atomicAdd(&hist[one], (int)__popcll(same));
+    else if (in && bin != one) atomicAdd(&hist[bin], 1);
   }
 }
 
-__global__ __launch_bounds__(kCopy) void evict_copy(focus_paged_evict_desc d, int in_shift, int out_shift, int pieces,
-                                                    int es) {
-  const int K = d.cache.n_kv_heads, b = blockIdx.x / K, g = blockIdx.x % K;
-  if (blockIdx.y == 0 && g == 0 && threadIdx.x == 0) {
-    int32_t bits = 0;
-    d.out.length[b] = kept_rows(d, b, focus::paged_length(d.cache, b), &bits);
+// How far the selection has come: the rows above `level` stay and `equal` of those that
+// share the digits found so far; done: none of those are left over (equal 0).
+struct Level {
+  uint32_t level;
+  int equal, done;
+};
+
+// The bucket that holds the last of the `equal` greatest rows of a digit's histogram (of
+// kBins, with at least so many rows), in every thread: the level with that digit.  Where
+// the whole bucket stays, no further digit is needed: its rows are the ones above a level.
+__device__ int next_level(const int* hist, int digit, int* waves, int* found, Level& x) {
+  constexpr int kPer = kBins / kThreads;
+  const int tid = threadIdx.x;
+  int c[kPer], sum = 0;
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) {
+    c[i] = hist[kBins - 1 - (tid * kPer + i)];
+    sum += c[i];
   }
-  const int32_t* keep = d.keep + ((int64_t)b * K + g) * d.keep_rows;
-  const int per = kCopy / pieces, sub = threadIdx.x % pieces;
-  if ((int)threadIdx.x >= per * pieces) return;
-  for (int64_t j = (int64_t)blockIdx.y * per + threadIdx.x / pieces; j < d.keep_rows; j += (int64_t)gridDim.y * per) {
-    const int r = keep[j];
-    if (r < 0) break;
-    const int64_t sp = focus::page_of(d.cache, b, r, in_shift), dp = focus::page_of(d.out, b, (int)j, out_shift);
-    if (sub == 0 && d.out.weight)
-      d.out.weight[((int64_t)b * K + g) * d.out.weight_rows + j] =
-          d.cache.weight[((int64_t)b * K + g) * d.cache.weight_rows + r];
-    if (sp < 0 || dp < 0) {
-      if (sub == 0) focus::raise_err(d.err, FOCUS_ERR_BOUNDS);
-      continue;
+  int total, above = scan(sum, waves, &total);
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) {
+    if (above < x.equal && above + c[i] >= x.equal)
+      found[0] = kBins - 1 - (tid * kPer + i), found[1] = x.equal - above, found[2] = c[i];
+    above += c[i];
+  }
+  __syncthreads();
+  const int bucket = found[0];
+  x.level |= (uint32_t)bucket << digit_shift(digit);
+  x.equal = found[1];
+  if (digit < kDigits - 1 && x.equal == found[2]) {
+    x.level -= 1;  // (no weight's integer is 0)
+    x.equal = 0, x.done = 1;
+  }
+  __syncthreads();
+  return bucket;
+}
+
+// Write the rows above `level` and, of those equal to it, the ones that number less than
+// `equal`: rows above that come before this workgroup's: before_above, equal ones: before_equal.
+template <int NR>
+__device__ void write_rows(const Head& h, const uint32_t (&key)[NR], int row0, uint32_t level, int equal, int before_above,
+                           int before_equal, int (*waves)[2]) {
+  const int wave = threadIdx.x / 64;
+  int above = 0, ties = 0;  // of this wave
+#pragma unroll
+  for (int i = 0; i < NR; ++i) {
+    const bool in = row0 + 64 * i < h.old;
+    above += __popcll(__ballot(in && key[i] > level));
+    ties += __popcll(__ballot(in && key[i] == level));
+  }
+  if (threadIdx.x % 64 == 0) waves[wave][0] = above, waves[wave][1] = ties;
+  __syncthreads();
+  above = before_above, ties = before_equal;
+  for (int w = 0; w < wave; ++w) above += waves[w][0], ties += waves[w][1];
+#pragma unroll
+  for (int i = 0; i < NR; ++i) {
+    const bool in = row0 + 64 * i < h.old;
+    const uint64_t up = __ballot(in && key[i] > level), tie = __ballot(in && key[i] == level);
+    const uint64_t lower = (1ull << (threadIdx.x % 64)) - 1;
+    const int t = ties + __popcll(tie & lower), a = above + __popcll(up & lower);
+    if (in && (key[i] > level || (key[i] == level && t < equal))) h.keep[a + min(t, equal)] = row0 + 64 * i;
+    above += __popcll(up), ties += __popcll(tie);
+  }
+}
+
+// The recent rows, and -1 past the rows kept; by `groups` workgroups of which this is `at`.
+__device__ void write_rest(const focus_paged_evict_desc& d, const Head& h, int at, int groups) {
+  const int step = groups * kThreads;
+  for (int j = at * kThreads + threadIdx.x; j < h.recent; j += step) h.keep[h.take + j] = h.old + j;
+  for (int64_t j = h.take + h.recent + at * kThreads + threadIdx.x; j < d.keep_rows; j += step) h.keep[j] = -1;
+}
+
+struct Copy {
+  int in_shift, out_shift, pieces, es;  // log2 page rows; 16-byte pieces of a row; element bytes
+  bool lengths;                         // whether evict_select sets them (no length is read and written)
+};
+
+// Copies the kept rows j0, j0 + step, ... of one head, a piece a thread and `per` rows at a
+// time, with four of them in flight.
+__device__ void copy_rows(const focus_paged_evict_desc& d, const Copy& y, int b, int g, int64_t j0, int64_t step,
+                          int64_t end, int sub) {
+  constexpr int kFlight = 4;
+  const int K = d.cache.n_kv_heads;
+  const int64_t bg = (int64_t)b * K + g;
+  const int32_t* keep = d.keep + bg * d.keep_rows;
+  for (; j0 < end; j0 += step * kFlight) {
+    int r[kFlight];
+    int64_t src[kFlight], dst[kFlight];
+#pragma unroll
+    for (int i = 0; i < kFlight; ++i) r[i] = j0 + i * step < end ? keep[j0 + i * step] : -1;
+#pragma unroll
+    for (int i = 0; i < kFlight; ++i) {
+      src[i] = dst[i] = -1;
+      if (r[i] < 0) continue;
+      const int j = (int)(j0 + i * step);
+      const int64_t sp = focus::page_of(d.cache, b, r[i], y.in_shift), dp = focus::page_of(d.out, b, j, y.out_shift);
+      if (sp < 0 || dp < 0) {
+        if (sub == 0) focus::raise_err(d.err, FOCUS_ERR_BOUNDS);
+        continue;
+      }
+      src[i] = focus::row_at(d.cache, sp, r[i], g) * y.es / 16 + sub;
+      dst[i] = focus::row_at(d.out, dp, j, g) * y.es / 16 + sub;
     }
-    const int64_t src = focus::row_at(d.cache, sp, r, g) * es / 16 + sub, dst = focus::row_at(d.out, dp, (int)j, g) * es / 16 + sub;
-    reinterpret_cast<uint4*>(d.out.k)[dst] = reinterpret_cast<const uint4*>(d.cache.k)[src];
-    reinterpret_cast<uint4*>(d.out.v)[dst] = reinterpret_cast<const uint4*>(d.cache.v)[src];
+    focus::u32x4 k[kFlight], v[kFlight];
+    float w[kFlight];
+#pragma unroll
+    for (int i = 0; i < kFlight; ++i) {
+      if (src[i] >= 0) {
+        k[i] = __builtin_nontemporal_load(reinterpret_cast<const focus::u32x4*>(d.cache.k) + src[i]);
+        v[i] = __builtin_nontemporal_load(reinterpret_cast<const focus::u32x4*>(d.cache.v) + src[i]);
+      }
+      if (sub == 0 && r[i] >= 0 && d.out.weight) w[i] = d.cache.weight[bg * d.cache.weight_rows + r[i]];
+    }
+#pragma unroll
+    for (int i = 0; i < kFlight; ++i) {
+      if (src[i] >= 0) {
+        __builtin_nontemporal_store(k[i], reinterpret_cast<focus::u32x4*>(d.out.k) + dst[i]);
+        __builtin_nontemporal_store(v[i], reinterpret_cast<focus::u32x4*>(d.out.v) + dst[i]);
+      }
+      if (sub == 0 && r[i] >= 0 && d.out.weight) d.out.weight[bg * d.out.weight_rows + j0 + i * step] = w[i];
+    }
   }
+}
+
+// out.length of sequence b, by one thread.
+__device__ void set_length(const focus_paged_evict_desc& d, int b) {
+  int32_t bits = 0;
+  d.out.length[b] = kept_rows(d, b, focus::paged_length(d.cache, b), &bits);
+}
+
+template <int NR, bool COPY>
+__global__ __launch_bounds__(kThreads) void evict_select(focus_paged_evict_desc d, Copy y) {
+  __shared__ int hist[kBins];
+  __shared__ int waves[kWaves], found[3], parts[kWaves][2];
+  const Head h = head_of(d, blockIdx.x, true);
+  if (h.take > 0) {
+    uint32_t key[NR];
+    int row0;
+    load_keys<NR>(h, 0, key, row0);
+    Level x = {0, h.take, 0};
+    for (int digit = 0; digit < kDigits && !x.done; ++digit) {
+      for (int i = threadIdx.x; i < kBins; i += kThreads) hist[i] = 0;
+      __syncthreads();
+      count_digit<NR>(h, key, row0, digit, x.level, hist);
+      __syncthreads();
+      next_level(hist, digit, waves, found, x);
+    }
+    write_rows<NR>(h, key, row0, x.level, x.equal, 0, 0, parts);
+  }
+  write_rest(d, h, 0, 1);
+  if constexpr (COPY) {
+    if (y.lengths && h.g == 0 && threadIdx.x == 0) d.out.length[h.b] = h.take + h.recent;
+    __syncthreads();  // the kept rows are this workgroup's own
+    const int per = kThreads / y.pieces;
+    if ((int)threadIdx.x < per * y.pieces)
+      copy_rows(d, y, h.b, h.g, threadIdx.x / y.pieces, per, h.take + h.recent, threadIdx.x % y.pieces);
+  }
+}
+
+constexpr int kLongRows = 8;                   // registers of rows of the long form
+constexpr int kPart = kThreads * kLongRows;    // rows of a workgroup there
+
+// The long form's workspace: per head the level so far, per part the rows above it in the
+// parts before, and the histograms [head][part][digit] (counts up to kPart).
+struct Long {
+  Level* level;
+  int* before;
+  uint16_t* hist;
+  int parts;
+};
+
+// Launch STEP adds up the histograms of digit STEP - 1 and counts digit STEP, or, the last,
+// writes the rows kept.
+template <int STEP>
+__global__ __launch_bounds__(kThreads) void evict_part(focus_paged_evict_desc d, Long y) {
+  __shared__ int hist[kBins];
+  __shared__ int waves[kWaves], found[3], pair[kWaves][2];
+  const int bg = blockIdx.x / y.parts, part = blockIdx.x % y.parts, tid = threadIdx.x;
+  const Head h = head_of(d, bg, STEP == 0 && part == 0);
+  if (STEP == kDigits) write_rest(d, h, part, y.parts);
+  const int live = (h.old + kPart - 1) / kPart;  // parts that hold rows
+  if (h.take == 0 || part >= live) return;
+  // a digit's histogram of a part, two bins a thread
+  auto bins = [&](int p, int digit) {
+    return reinterpret_cast<uint32_t*>(y.hist + (((int64_t)bg * y.parts + p) * kDigits + digit) * kBins) + tid;
+  };
+  Level x = {0, h.take, 0};
+  int before = 0, before_equal = 0;
+  if constexpr (STEP >= 2) {
+    x = y.level[2 * bg + STEP % 2];
+    before = y.before[(int64_t)bg * y.parts + part];
+    if (x.done && STEP < kDigits) {
+      if (part == 0 && tid == 0) y.level[2 * bg + (STEP + 1) % 2] = x;
+      return;
+    }
+  }
+  uint32_t key[kLongRows];
+  int row0;
+  load_keys<kLongRows>(h, part * kPart, key, row0);
+  if constexpr (STEP >= 1) {
+    if (!x.done) {
+      constexpr int kFlight = 8;
+      // of all parts, and of those before this one
+      int lo = 0, hi = 0, lo_b = 0, hi_b = 0;
+      for (int p0 = 0; p0 < live; p0 += kFlight) {
+        uint32_t c[kFlight];
+#pragma unroll
+        for (int i = 0; i < kFlight; ++i) c[i] = p0 + i < live ? *bins(p0 + i, STEP - 1) : 0;
+#pragma unroll
+        for (int i = 0; i < kFlight; ++i) {
+          lo += c[i] & 0xffff, hi += c[i] >> 16;
+          if (p0 + i < part) lo_b += c[i] & 0xffff, hi_b += c[i] >> 16;
+        }
+      }
+      hist[2 * tid] = lo, hist[2 * tid + 1] = hi;
+      __syncthreads();
+      const int bucket = next_level(hist, STEP - 1, waves, found, x);
+      const int own = 2 * tid == bucket ? lo_b : 2 * tid + 1 == bucket ? hi_b : 0;
+      const int up = (2 * tid > bucket ? lo_b : 0) + (2 * tid + 1 > bucket ? hi_b : 0);
+      int total;
+      scan(up + (x.done ? own : 0), waves, &total);
+      before += total;
+      if constexpr (STEP == kDigits) {
+        scan(own, waves, &total);
+        before_equal = total;
+      } else if (tid == 0) {
+        y.before[(int64_t)bg * y.parts + part] = before;
+        if (part == 0) y.level[2 * bg + (STEP + 1) % 2] = x;
+      }
+    }
+  }
+  if constexpr (STEP == kDigits) {
+    write_rows<kLongRows>(h, key, row0, x.level, x.equal, before, before_equal, pair);
+  } else {
+    if (x.done) return;
+    __syncthreads();
+    for (int i = tid; i < kBins; i += kThreads) hist[i] = 0;
+    __syncthreads();
+    count_digit<kLongRows>(h, key, row0, STEP, x.level, hist);
+    __syncthreads();
+    *bins(part, STEP) = (uint32_t)hist[2 * tid] | (uint32_t)hist[2 * tid + 1] << 16;
+  }
+}
+static_assert(kBins == 2 * kThreads, "two bins a thread");
+
+__global__ __launch_bounds__(kCopy) void evict_copy(focus_paged_evict_desc d, Copy y) {
+  const int K = d.cache.n_kv_heads, b = blockIdx.x / K, g = blockIdx.x % K;
+  const int per = kCopy / y.pieces;
+  if ((int)threadIdx.x < per * y.pieces)
+    copy_rows(d, y, b, g, (int64_t)blockIdx.y * per + threadIdx.x / y.pieces, (int64_t)gridDim.y * per, d.keep_rows,
+              threadIdx.x % y.pieces);
+  if (blockIdx.y == 0 && g == 0 && threadIdx.x == 0) set_length(d, b);
+}
+
+__global__ __launch_bounds__(kCopy) void evict_lengths(focus_paged_evict_desc d) {
+  const int b = blockIdx.x * kCopy + threadIdx.x;
+  if (b < d.cache.batch) set_length(d, b);
 }
 
 focus_status validate(const focus_paged_evict_desc* d) {
@@ -141,9 +398,35 @@ focus_status validate(const focus_paged_evict_desc* d) {
   return FOCUS_OK;
 }
 
+// Rows of a table that one workgroup selects from by itself.
+constexpr int64_t kShortRows = 32 * kThreads;
+
+int64_t parts_of(const focus_paged_evict_desc& d) {
+  const int64_t cap = (int64_t)d.cache.max_pages * d.cache.page_rows;
+  return cap > kShortRows ? focus::ceil_div(cap, kPart) : 0;
+}
+
+// The long form's arrays in the workspace (out may be NULL); returns their bytes.  Two
+// levels a head: a launch reads one that its first part's workgroup does not write.
+size_t long_form(const focus_paged_evict_desc& d, void* workspace, Long* out) {
+  const int64_t parts = parts_of(d), heads = (int64_t)d.cache.batch * d.cache.n_kv_heads;
+  if (parts == 0) return 0;
+  const int64_t level = focus::ceil_div(2 * heads * (int64_t)sizeof(Level), 16) * 16;
+  const int64_t before = focus::ceil_div(heads * parts * 4, 16) * 16;
+  if (out) {
+    char* ws = reinterpret_cast<char*>(workspace);
+    *out = {reinterpret_cast<Level*>(ws), reinterpret_cast<int*>(ws + level),
+            reinterpret_cast<uint16_t*>(ws + level + before), (int)parts};
+  }
+  return (size_t)(level + before + heads * parts * kDigits * kBins * 2);
+}
+
 }  // namespace
 
-extern "C" size_t focus_paged_evict_workspace(const focus_paged_evict_desc*) { return 0; }
+extern "C" size_t focus_paged_evict_workspace(const focus_paged_evict_desc* d) {
+  if (!d || validate(d) != FOCUS_OK) return 0;
+  return long_form(*d, nullptr, nullptr);
+}
 
 extern "C" focus_status focus_paged_evict(const focus_paged_evict_desc* d, focus_stream_t stream) {
   if (!d) return FOCUS_E_NULL;
@@ -154,13 +437,46 @@ extern "C" focus_status focus_paged_evict(const focus_paged_evict_desc* d, focus
   if (d->out.weight == d->cache.weight || (reinterpret_cast<uintptr_t>(d->keep) & 3u) ||
       (reinterpret_cast<uintptr_t>(d->budgets) & 3u))
     return FOCUS_E_ARG;
+  const int64_t parts = parts_of(*d), heads = (int64_t)d->cache.batch * d->cache.n_kv_heads;
+  const size_t need = focus_paged_evict_workspace(d);
+  if (need > 0 && (!d->workspace || d->workspace_bytes < need)) return FOCUS_E_WORKSPACE;
+  if (!focus::aligned16(d->workspace)) return FOCUS_E_ARG;
+  if (heads * std::max<int64_t>(parts, 1) > INT32_MAX / kThreads) return FOCUS_E_SHAPE;
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
-  const uint32_t heads = (uint32_t)(d->cache.batch * d->cache.n_kv_heads);
-  hipLaunchKernelGGL(evict_select, dim3(heads), dim3(kThreads), 0, s, *d);
-  if ((st = focus::launch_status()) != FOCUS_OK) return st;
   const int es = (int)focus::elt_bytes(d->cache.dtype), pieces = d->cache.head_dim * es / 16;
-  const int64_t y = focus::ceil_div(d->keep_rows > 0 ? d->keep_rows : 1, (kCopy / pieces) * 8);
-  hipLaunchKernelGGL(evict_copy, dim3(heads, (uint32_t)(y > 1024 ? 1024 : y)), dim3(kCopy), 0, s, *d,
-                     focus::page_shift(d->cache), focus::page_shift(d->out), pieces, es);
+  // (out.length may be cache.length, which every head's workgroup reads: it is set by a
+  // later launch then)
+  const int64_t apart = d->out.length - d->cache.length;
+  const Copy y = {focus::page_shift(d->cache), focus::page_shift(d->out), pieces, es,
+                  apart >= d->cache.batch || -apart >= d->cache.batch};
+  const dim3 block(kThreads);
+  if (parts > 0) {
+    const dim3 grid((uint32_t)(heads * parts));
+    Long scratch;
+    long_form(*d, d->workspace, &scratch);
+    hipLaunchKernelGGL((evict_part<0>), grid, block, 0, s, *d, scratch);
+    hipLaunchKernelGGL((evict_part<1>), grid, block, 0, s, *d, scratch);
+    hipLaunchKernelGGL((evict_part<2>), grid, block, 0, s, *d, scratch);
+    hipLaunchKernelGGL((evict_part<3>), grid, block, 0, s, *d, scratch);
+  } else {
+    // A workgroup copies its own head's rows where that is little work, or where there
+    // are heads for every compute unit: a launch less.
+    const bool copies = d->keep_rows * pieces * 64 <= (256 << 10) || heads >= 2 * focus::device_cus();
+    const dim3 grid((uint32_t)heads);
+    const int64_t cap = (int64_t)d->cache.max_pages * d->cache.page_rows;
+#define FOCUS_SELECT(NR)                                                              \
+  if (copies) hipLaunchKernelGGL((evict_select<NR, true>), grid, block, 0, s, *d, y); \
+  else hipLaunchKernelGGL((evict_select<NR, false>), grid, block, 0, s, *d, y);
+    if (cap <= 4 * kThreads) { FOCUS_SELECT(4) } else if (cap <= 16 * kThreads) { FOCUS_SELECT(16) } else { FOCUS_SELECT(32) }
+#undef FOCUS_SELECT
+    if (copies) {
+      if ((st = focus::launch_status()) != FOCUS_OK || y.lengths) return st;
+      hipLaunchKernelGGL(evict_lengths, dim3((uint32_t)focus::ceil_div(d->cache.batch, kCopy)), dim3(kCopy), 0, s, *d);
+      return focus::launch_status();
+    }
+  }
+  if ((st = focus::launch_status()) != FOCUS_OK) return st;
+  const int64_t blocks = focus::ceil_div(d->keep_rows > 0 ? d->keep_rows : 1, (kCopy / pieces) * 8);
+  hipLaunchKernelGGL(evict_copy, dim3((uint32_t)heads, (uint32_t)std::min<int64_t>(blocks, 1024)), dim3(kCopy), 0, s, *d, y);
   return focus::launch_status();
 }
