@@ -92,42 +92,54 @@ struct Args {
   float* score;
 };
 
+// Inclusive prefix sum over the wave (DPP: rows of 16, then their last lanes' sums).
+__device__ inline int wave_scan(int x) {
+#define FOCUS_SCAN_STEP(ctrl, rows) x += __builtin_amdgcn_update_dpp(0, x, ctrl, rows, 0xf, true)
+  FOCUS_SCAN_STEP(0x111, 0xf);
+  FOCUS_SCAN_STEP(0x112, 0xf);
+  FOCUS_SCAN_STEP(0x114, 0xf);
+  FOCUS_SCAN_STEP(0x118, 0xf);
+  FOCUS_SCAN_STEP(0x142, 0xa);
+  FOCUS_SCAN_STEP(0x143, 0xc);
+#undef FOCUS_SCAN_STEP
+  return x;
+}
+
+// Maximum over the lanes 16 and 32 apart.
+__device__ inline float max_column(float x) {
+  const uint32_t u = __float_as_uint(x);
+  auto y = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+  const uint32_t v = __float_as_uint(fmaxf(__uint_as_float(y[0]), __uint_as_float(y[1])));
+  y = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+  return fmaxf(__uint_as_float(y[0]), __uint_as_float(y[1]));
+}
+
 // Chunk of the split with index i: every wave finds it by itself from the lengths, 64
 // sequences at a time.  A chunk is split_keys rows, or what spreads the rows of the
-// whole batch over `target` of them.
+// whole batch, in units, over `target` of them.
 struct Chunk {
   int b, c, n, slot0, chunks, rows;
 };
 __device__ bool find_chunk(const Args& a, int i, Chunk& out) {
   const focus_paged_kv& c = a.d.cache;
   const int lane = threadIdx.x % 64;
-  int rows = a.d.split_keys;
+  int rows = a.d.split_keys, n = 0;
   if (rows == 0) {
     int64_t total = 0;
     for (int b0 = 0; b0 < c.batch; b0 += 64) {
-      int64_t x = b0 + lane < c.batch ? focus::paged_length(c, b0 + lane) : 0;
-#pragma unroll
-      for (int k = 32; k >= 1; k >>= 1) x += __shfl_xor(x, k);
-      total += x;
+      n = b0 + lane < c.batch ? focus::paged_length(c, b0 + lane) : 0;
+      total += __builtin_amdgcn_readlane(wave_scan((n + kUnit - 1) / kUnit), 63);
     }
-    const int64_t per = (total + a.target - 1) / a.target;
-    rows = (int)min((per + kUnit - 1) / kUnit * kUnit, (int64_t)1 << 30);
-    rows = __builtin_amdgcn_readfirstlane(max(rows, kUnit));
+    rows = (int)min((total + a.target - 1) / a.target * kUnit, (int64_t)1 << 30);
+    rows = max(rows, kUnit);
   }
   int before = 0;
   for (int b0 = 0; b0 < c.batch; b0 += 64) {
-    const int n = b0 + lane < c.batch ? focus::paged_length(c, b0 + lane) : 0;
+    if (c.batch > 64 || a.d.split_keys) n = b0 + lane < c.batch ? focus::paged_length(c, b0 + lane) : 0;
     const int own = b0 + lane < c.batch ? max(1, (n - 1) / rows + 1) : 0;
-    int upto = own;
-#pragma unroll
-    for (int k = 1; k < 64; k <<= 1) {
-      const int y = __shfl_up(upto, k);
-      if (lane >= k) upto += y;
-    }
-    const int all = __builtin_amdgcn_readlane(upto, 63);
+    const int upto = wave_scan(own), all = __builtin_amdgcn_readlane(upto, 63);
     if (i < before + all) {
-      const uint64_t past = __ballot(i < before + upto);
-      const int at = __ffsll((unsigned long long)past) - 1;
+      const int at = __ffsll((unsigned long long)__ballot(i < before + upto)) - 1;
       out.b = b0 + at;
       out.n = __builtin_amdgcn_readlane(n, at);
       out.chunks = __builtin_amdgcn_readlane(own, at);
@@ -288,8 +300,7 @@ __global__ __launch_bounds__(kThreads, 2) void paged_attend(Args a) {
           for (int j = 0; j < L::kScores; j += 4)
             *reinterpret_cast<float4*>(score + row + j) = make_float4(y[j], y[j + 1], y[j + 2], y[j + 3]);
         }
-        mx = fmaxf(mx, __shfl_xor(mx, 16));
-        mx = fmaxf(mx, __shfl_xor(mx, 32));
+        mx = max_column(mx);
         const float alpha = __builtin_amdgcn_exp2f(m - mx);
         m = mx;
         l *= alpha;
@@ -422,73 +433,78 @@ __device__ float2 joined(const Args& a, const int4& info, int h) {
   return make_float2(M, L);
 }
 
-constexpr int kWeightRows = 4 * kThreads;   // rows of a workgroup that writes weights
+constexpr int kWeightRows = 4 * kThreads;   // rows whose weights a workgroup writes at a time
 
-// The first `joins` workgroups merge the partials of a (sequence, head) each: D / 4
-// threads over the output, the other groups of them over the chunks, eight loads in
-// flight each, the first of them before the maximum is known.  The others write weights.
+// One of `parts` workgroups of a (sequence, KV head): merges the partials of every
+// parts-th of its query heads (D / 4 threads over the output, the other groups of them
+// over the chunks, eight loads in flight each, the first of them before the maximum is
+// known) and, where weights are accumulated, writes those of every parts-th block of rows.
 template <typename T, int D>
-__global__ __launch_bounds__(kThreads) void paged_join(Args a, int joins, int row_blocks) {
+__global__ __launch_bounds__(kThreads) void paged_join(Args a, int parts) {
+  constexpr int kLanes = D / 4, kGroups = kThreads / kLanes, kFlight = 8;
+  __shared__ float4 s_o[kGroups][kLanes];
+  __shared__ float s_lse[kThreads];
   const focus_paged_kv& c = a.d.cache;
   const int K = c.n_kv_heads, H = a.d.n_heads, G = H / K, tid = threadIdx.x;
-  if ((int)blockIdx.x < joins) {
-    constexpr int kLanes = D / 4, kGroups = kThreads / kLanes, kFlight = 8;
-    __shared__ float4 s_o[kGroups][kLanes];
-    const int b = blockIdx.x / H, h = blockIdx.x % H;
-    const int4 info = a.info[b];
-    if (info.y == 1) return;
+  // (part 0 of all first: the later ones have nothing to do where sequences are short, and
+  // with parts side by side those that do would all lie on a few of the XCDs)
+  const int item = blockIdx.x % (c.batch * K), part = blockIdx.x / (c.batch * K), g = item % K, b = item / K;
+  const int4 info = a.info[b];
+  if (info.y > 1) {
     const int e = tid % kLanes, grp = tid / kLanes;
     const float4* o = reinterpret_cast<const float4*>(a.o);
-    float2 ml = {};
-    float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int i0 = grp; i0 == grp || i0 < info.y; i0 += kGroups * kFlight) {
-      float4 y[kFlight];
-      float m[kFlight];
+    for (int h = g * G + part; h < (g + 1) * G; h += parts) {
+      float2 ml = {};
+      float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+      for (int i0 = grp; i0 == grp || i0 < info.y; i0 += kGroups * kFlight) {
+        float4 y[kFlight];
+        float m[kFlight];
 #pragma unroll
-      for (int k = 0; k < kFlight; ++k) {
-        const int64_t slot = (int64_t)(info.x + min(i0 + k * kGroups, info.y - 1)) * H + h;
-        y[k] = o[slot * kLanes + e];
-        m[k] = a.ml[slot].x;
-      }
-      if (i0 == grp) ml = joined(a, info, h);
+        for (int k = 0; k < kFlight; ++k) {
+          const int64_t slot = (int64_t)(info.x + min(i0 + k * kGroups, info.y - 1)) * H + h;
+          y[k] = o[slot * kLanes + e];
+          m[k] = a.ml[slot].x;
+        }
+        if (i0 == grp) ml = joined(a, info, h);
 #pragma unroll
-      for (int k = 0; k < kFlight; ++k) {
-        if (i0 + k * kGroups < info.y) {
-          const float f = __builtin_amdgcn_exp2f(m[k] - ml.x);
-          sum.x = fmaf(y[k].x, f, sum.x), sum.y = fmaf(y[k].y, f, sum.y);
-          sum.z = fmaf(y[k].z, f, sum.z), sum.w = fmaf(y[k].w, f, sum.w);
+        for (int k = 0; k < kFlight; ++k) {
+          if (i0 + k * kGroups < info.y) {
+            const float f = __builtin_amdgcn_exp2f(m[k] - ml.x);
+            sum.x = fmaf(y[k].x, f, sum.x), sum.y = fmaf(y[k].y, f, sum.y);
+            sum.z = fmaf(y[k].z, f, sum.z), sum.w = fmaf(y[k].w, f, sum.w);
+          }
         }
       }
-    }
-    s_o[grp][e] = sum;
-    __syncthreads();
-    if (tid < D) {
-      float y = 0.f;
+      __syncthreads();
+      s_o[grp][e] = sum;
+      __syncthreads();
+      if (tid < D) {
+        float y = 0.f;
 #pragma unroll
-      for (int k = 0; k < kGroups; ++k) y += reinterpret_cast<const float*>(s_o[k])[tid];
-      const int64_t at = (int64_t)b * H + h;
-      reinterpret_cast<T*>(a.d.o)[at * D + tid] = (T)(ml.y == 0.f ? 0.f : y / ml.y);
-      if (tid == 0 && a.d.lse) a.d.lse[at] = ml.y == 0.f ? -INFINITY : (ml.x + log2f(ml.y)) * kLn2;
+        for (int k = 0; k < kGroups; ++k) y += reinterpret_cast<const float*>(s_o[k])[tid];
+        const int64_t at = (int64_t)b * H + h;
+        reinterpret_cast<T*>(a.d.o)[at * D + tid] = (T)(ml.y == 0.f ? 0.f : y / ml.y);
+        if (tid == 0 && a.d.lse) a.d.lse[at] = ml.y == 0.f ? -INFINITY : (ml.x + log2f(ml.y)) * kLn2;
+      }
     }
-    return;
   }
-  // weights of rows of one (sequence, KV head), four a thread
-  const int item = blockIdx.x - joins, part = item % row_blocks, g = item / row_blocks % K, b = item / row_blocks / K;
-  const int4 info = a.info[b];
+  if (!a.d.accumulate) return;
+  // weights, four rows a thread
   const int n = info.z;
   float* w = c.weight + ((int64_t)b * K + g) * c.weight_rows;
-  __shared__ float s_lse[kThreads];
-  for (int r0 = part * kWeightRows; r0 < n; r0 += row_blocks * kWeightRows) {
+  for (int r0 = part * kWeightRows; r0 < n; r0 += parts * kWeightRows) {
     const int r = r0 + 4 * tid;
     float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
     for (int hb = 0; hb < G; hb += kThreads) {
       const int some = min(kThreads, G - hb);
-      __syncthreads();
-      for (int h = tid / 64; h < some; h += kWaves) {
-        const float2 ml = joined(a, info, g * G + hb + h);
-        if (tid % 64 == 0) s_lse[h] = ml.y == 0.f ? INFINITY : ml.x + log2f(ml.y);
+      if (r0 == part * kWeightRows || G > kThreads) {
+        __syncthreads();
+        for (int h = tid / 64; h < some; h += kWaves) {
+          const float2 ml = joined(a, info, g * G + hb + h);
+          if (tid % 64 == 0) s_lse[h] = ml.y == 0.f ? INFINITY : ml.x + log2f(ml.y);
+        }
+        __syncthreads();
       }
-      __syncthreads();
       const float* score = a.score + ((int64_t)b * H + g * G + hb) * a.cap + r;
       if (r < n) {
 #pragma unroll 4
@@ -527,16 +543,17 @@ template <typename T, int D>
 focus_status launch(const Args& a, const Plan& p, hipStream_t s) {
   const focus_paged_kv& c = a.d.cache;
   const int64_t blocks = p.slots * c.n_kv_heads * p.tiles;
-  const int joins = c.batch * a.d.n_heads;
-  // enough workgroups to write the weights at the memory's rate, not one per row of the table
-  const int64_t per = focus::ceil_div(p.cap > 0 ? p.cap : 1, kWeightRows), heads = (int64_t)c.batch * c.n_kv_heads;
-  const int64_t row_blocks = std::min(per, std::max<int64_t>(1, focus::ceil_div(16 * focus::device_cus(), heads)));
-  const int64_t second = joins + (a.d.accumulate ? heads * row_blocks : 0);
-  if (blocks > INT32_MAX / kThreads || second > INT32_MAX / kThreads) return FOCUS_E_SHAPE;
+  // workgroups of a (sequence, KV head) in the second launch: one per query head, or, for
+  // weights, per block of the table's rows, but not many more than the device holds
+  const int64_t per = focus::ceil_div(std::max<int64_t>(p.cap, 1), kWeightRows), heads = (int64_t)c.batch * c.n_kv_heads;
+  const int64_t group = a.d.n_heads / c.n_kv_heads;
+  const int64_t parts = a.d.accumulate
+      ? std::max(std::min(per, focus::ceil_div(8 * focus::device_cus(), heads)), std::min<int64_t>(group, 4)) : group;
+  if (blocks > INT32_MAX / kThreads || heads * parts > INT32_MAX / kThreads) return FOCUS_E_SHAPE;
   hipLaunchKernelGGL((paged_attend<T, D>), dim3((uint32_t)blocks), dim3(kThreads), 0, s, a);
   const focus_status st = focus::launch_status();
   if (st != FOCUS_OK) return st;
-  hipLaunchKernelGGL((paged_join<T, D>), dim3((uint32_t)second), dim3(kThreads), 0, s, a, joins, (int)row_blocks);
+  hipLaunchKernelGGL((paged_join<T, D>), dim3((uint32_t)(heads * parts)), dim3(kThreads), 0, s, a, (int)parts);
   return focus::launch_status();
 }
 
