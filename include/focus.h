@@ -818,7 +818,8 @@ typedef struct {
  * refuses).  The workspace is in use until the call's kernels end; calls that share
  * one on overlapping streams race. */
 size_t focus_paged_decode_workspace(const focus_paged_decode_desc* d);
-/* Errors: E_NULL, E_ARG, E_DTYPE, E_SHAPE, E_UNSUPPORTED, E_WORKSPACE, E_HIP.  Rows of
+/* Errors: E_NULL, E_ARG, E_DTYPE, E_SHAPE (batch * max_pages * page_rows of 2^36 or more
+ * among others), E_UNSUPPORTED, E_WORKSPACE, E_HIP.  Rows of
  * a page outside the pool are left out of the softmax (FOCUS_ERR_BOUNDS; weight of the
  * step 0); a length outside [0, max_pages * page_rows] is clipped to it
  * (FOCUS_ERR_CAPACITY). */

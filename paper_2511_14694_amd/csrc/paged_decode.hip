@@ -1,7 +1,7 @@
 // Attention of one new token over a paged K/V cache (focus_paged_decode).
 //
-//   paged_attend   one workgroup per (chunk of a sequence's rows, KV head, up to 16 of
-//                  its query heads); writes o and lse where the chunk is the whole
+//   paged_attend   one workgroup per (chunk of a sequence's rows, one to four KV heads, up
+//                  to 16 query heads of each); writes o and lse where the chunk is the whole
 //                  sequence, else an unnormalised partial (running max, sum, output)
 //   paged_join     merges the partials of a sequence's chunks by log-sum-exp; where
 //                  weights are accumulated, further workgroups turn the scores that
@@ -39,9 +39,10 @@ constexpr float kLn2 = 0.69314718055994531f;
 constexpr float kLog2e = 1.44269504088896341f;
 constexpr float kMinit = -1.0e30f;
 constexpr int kThreads = 256, kWaves = 4;
+constexpr int kMaxGrid = 32768; // workgroups in a grid's second and third dimension
 constexpr int kCols = 16;       // query heads of a workgroup: columns of a product
 constexpr int kPages = 1024;    // page offsets held in LDS at a time
-constexpr int kUnit = 128;      // chunks are multiples of this many rows
+constexpr int kUnit = 128;      // rows of a chunk times KV heads of a workgroup: a multiple of this
 
 // What a lane reads in the place of eight rows that begin past their sequence's end or
 // lie in a page outside the pool.
@@ -52,25 +53,36 @@ __device__ __align__(16) const uint32_t kZeros[256] = {};
 // accumulated, float score[batch][H][cap] (log2 units).
 struct Plan {
   int64_t slots;        // upper bound of the chunks of all sequences
-  int64_t target;       // chunks wanted from the whole batch (split_keys 0)
+  int64_t target;       // chunks resident at a time (split_keys 0)
   int64_t cap;          // rows of a sequence's table
   int64_t ml, o, score; // byte offsets
   size_t bytes;
   int tiles;            // workgroups a KV head's query heads take
+  int wide, unit;       // KV heads of a workgroup; chunks are multiples of `unit` rows
+  int64_t groups;       // workgroups of a chunk: n_kv_heads / wide * tiles
 };
+
+// Workgroups of paged_attend that a compute unit holds (by their registers).
+constexpr int resident(int head_dim) { return head_dim == 64 ? 4 : 2; }
 
 Plan make_plan(const focus_paged_decode_desc* d) {
   const focus_paged_kv& c = d->cache;
   Plan p = {};
   p.cap = (int64_t)c.max_pages * c.page_rows;
   p.tiles = (int)focus::ceil_div(d->n_heads / c.n_kv_heads, kCols);
+  // Where the heads of a row lie side by side, the waves of a workgroup take one KV head
+  // each (or two waves each of two): read together, four neighbouring 128-byte rows come at
+  // FIXME TB/s, by workgroups on their own at 4.5 (D 64, bf16, 8 KV heads; 256-byte rows at
+  // FIXME and 5.3).
+  p.wide = c.head_stride > c.row_stride ? 1 : c.n_kv_heads % 4 == 0 ? 4 : c.n_kv_heads % 2 == 0 ? 2 : 1;
+  p.unit = kUnit / p.wide;
+  p.groups = (int64_t)c.n_kv_heads / p.wide * p.tiles;
   if (d->split_keys > 0) {
     p.slots = c.batch * std::max<int64_t>(1, focus::ceil_div(p.cap, d->split_keys));
   } else {
-    // two workgroups fit on a compute unit: one round of them over the whole batch
-    p.target = std::max<int64_t>(1, 2 * focus::device_cus() / ((int64_t)c.n_kv_heads * p.tiles));
-    // a sequence has at least one chunk and at most rows / chunk rounded up
-    p.slots = std::min(c.batch + p.target, c.batch * std::max<int64_t>(1, focus::ceil_div(p.cap, kUnit)));
+    p.target = std::max<int64_t>(1, resident(c.head_dim) * focus::device_cus() / p.groups);
+    // a chunk has at least the rows of the batch over the target; a sequence at least one
+    p.slots = std::min(c.batch + p.target, c.batch * std::max<int64_t>(1, focus::ceil_div(p.cap, p.unit)));
   }
   const int64_t heads = p.slots * d->n_heads;
   p.ml = 16 * (int64_t)c.batch;
@@ -84,25 +96,34 @@ struct Args {
   focus_paged_decode_desc d;
   float sc;             // softmax scale in log2 units
   int shift;            // log2 page_rows
-  int tiles;
-  int64_t target, cap;
+  int tiles, wide_shift, unit_shift, target;   // wide and unit are powers of two
+  int group, parts;     // query heads of a KV head; workgroups of one in the second launch
+  int64_t cap;
   int4* info;
   float2* ml;
   float* o;
   float* score;
 };
 
-// Inclusive prefix sum over the wave (DPP: rows of 16, then their last lanes' sums).
-__device__ inline int wave_scan(int x) {
-#define FOCUS_SCAN_STEP(ctrl, rows) x += __builtin_amdgcn_update_dpp(0, x, ctrl, rows, 0xf, true)
-  FOCUS_SCAN_STEP(0x111, 0xf);
-  FOCUS_SCAN_STEP(0x112, 0xf);
-  FOCUS_SCAN_STEP(0x114, 0xf);
-  FOCUS_SCAN_STEP(0x118, 0xf);
-  FOCUS_SCAN_STEP(0x142, 0xa);
-  FOCUS_SCAN_STEP(0x143, 0xc);
-#undef FOCUS_SCAN_STEP
+// Inclusive prefix over the wave of a sum or, for values from 0 up, a maximum (DPP: rows of
+// 16 lanes, then their last lanes' values).
+template <typename Op>
+__device__ inline int wave_prefix(int x, Op op) {
+#define FOCUS_STEP(ctrl, rows) x = op(x, __builtin_amdgcn_update_dpp(0, x, ctrl, rows, 0xf, true))
+  FOCUS_STEP(0x111, 0xf);
+  FOCUS_STEP(0x112, 0xf);
+  FOCUS_STEP(0x114, 0xf);
+  FOCUS_STEP(0x118, 0xf);
+  FOCUS_STEP(0x142, 0xa);
+  FOCUS_STEP(0x143, 0xc);
+#undef FOCUS_STEP
   return x;
+}
+__device__ inline int wave_scan(int x) {
+  return wave_prefix(x, [](int a, int b) { return a + b; });
+}
+__device__ inline int wave_max(int x) {
+  return __builtin_amdgcn_readlane(wave_prefix(x, [](int a, int b) { return max(a, b); }), 63);
 }
 
 // Maximum over the lanes 16 and 32 apart.
@@ -114,28 +135,89 @@ __device__ inline float max_column(float x) {
   return fmaxf(__uint_as_float(y[0]), __uint_as_float(y[1]));
 }
 
+// Rows of a chunk when they are to be chosen, for `target` chunks resident at a time: the
+// least estimate of the time among
+//   the rows of the whole batch spread over `target` chunks, rounded up to units, or over
+//   half as many;
+//   the least size at which the chunks of all sequences are resident at once (up to 64
+//   sequences; it needs 16 steps of a search);
+//   no split at all.
+// The estimate, in rows a resident workgroup streams while all of them do: what there is
+// to read, and for each chunk kStart rows' worth of beginning and end and its partials
+// written and read, over the target; where not all are resident at once a last one begins
+// late and runs, with the memory to itself, at kAlone times the rate; so does the longest
+// one if it is longer than that.
+// 14 sequences of 209 921 rows, one KV head: 518 chunks of 5 760 rows on 512 places took
+// 304 us, 504 chunks of 5 888 237; 4 of 12 694 rows, 32 KV heads, with weights: no split
+// (128 workgroups) 289, FIXME.
+constexpr int kStart = 100;
+constexpr float kAlone = 1.25f;
+
+__device__ inline float estimate(const Args& a, uint32_t units, int chunks, int rows, int longest) {
+  const float each = (float)(kStart >> a.wide_shift) + (a.d.cache.dtype == FOCUS_BF16 ? 2.f : 1.f) * a.group;
+  const float even = ((float)units * (1 << a.unit_shift) + each * (float)chunks) / (float)a.target;
+  const float alone = (float)min(rows, longest) / kAlone;
+  return chunks > a.target ? even + alone : fmaxf(even, alone);
+}
+
+// (Counted in units: the host has checked that all tables together hold fewer than 2^31.)
+__device__ int chunk_rows(const Args& a) {
+  const focus_paged_kv& c = a.d.cache;
+  const int lane = threadIdx.x % 64, shift = a.unit_shift, unit = 1 << shift;
+  const uint32_t target = (uint32_t)a.target;
+  auto length = [&](int b) { return b < c.batch ? focus::paged_length(c, b) : -1; };
+  // units of a sequence; its chunks of so many units
+  auto units_of = [&](int n) { return (uint32_t)(max(n, 0) + unit - 1) >> shift; };
+  auto chunks_of = [&](int n, uint32_t units) { return n < 0 ? 0u : max(1u, (units_of(n) + units - 1) / units); };
+  auto sum = [](uint32_t x) { return (uint32_t)__builtin_amdgcn_readlane(wave_scan((int)x), 63); };
+  uint32_t total = 0;
+  int n = -1;
+  for (int b0 = 0; b0 < c.batch; b0 += 64) {
+    n = length(b0 + lane);
+    total += sum(units_of(n));
+  }
+  if (total + c.batch <= target) return unit;
+  const uint32_t one = (total + target - 1) / target, two = min(2 * one, 1u << 30 >> shift);
+  uint32_t count1 = 0, count2 = 0, whole = 1;
+  for (int b0 = 0; b0 < c.batch; b0 += 64) {
+    if (c.batch > 64) n = length(b0 + lane);
+    count1 += sum(chunks_of(n, one));
+    count2 += sum(chunks_of(n, two));
+    whole = max(whole, (uint32_t)wave_max((int)units_of(n)));
+  }
+  if (one >= whole) return (int)(whole << shift);
+  const int longest = (int)(whole << shift);
+  uint32_t units = one;
+  float best = estimate(a, total, count1, one << shift, longest);
+  auto better = [&](uint32_t count, uint32_t with) {
+    const float e = estimate(a, total, count, with << shift, longest);
+    if (e < best) best = e, units = with;
+  };
+  better(count2, two);
+  if (count1 > target && c.batch <= 64 && (uint32_t)c.batch <= target) {
+    uint32_t lo = one, hi = whole;  // too many chunks at lo, few enough at hi
+    for (int k = 0; k < 16 && hi - lo > 1; ++k) {
+      const uint32_t mid = (lo + hi) / 2;
+      if (sum(chunks_of(n, mid)) > target) lo = mid; else hi = mid;
+    }
+    better(sum(chunks_of(n, hi)), hi);
+  }
+  better(c.batch, whole);
+  return (int)(units << shift);
+}
+
 // Chunk of the split with index i: every wave finds it by itself from the lengths, 64
-// sequences at a time.  A chunk is split_keys rows, or what spreads the rows of the
-// whole batch, in units, over `target` of them.
+// sequences at a time.
 struct Chunk {
   int b, c, n, slot0, chunks, rows;
 };
 __device__ bool find_chunk(const Args& a, int i, Chunk& out) {
   const focus_paged_kv& c = a.d.cache;
   const int lane = threadIdx.x % 64;
-  int rows = a.d.split_keys, n = 0;
-  if (rows == 0) {
-    int64_t total = 0;
-    for (int b0 = 0; b0 < c.batch; b0 += 64) {
-      n = b0 + lane < c.batch ? focus::paged_length(c, b0 + lane) : 0;
-      total += __builtin_amdgcn_readlane(wave_scan((n + kUnit - 1) / kUnit), 63);
-    }
-    rows = (int)min((total + a.target - 1) / a.target * kUnit, (int64_t)1 << 30);
-    rows = max(rows, kUnit);
-  }
+  const int rows = __builtin_amdgcn_readfirstlane(a.d.split_keys ? a.d.split_keys : chunk_rows(a));
   int before = 0;
   for (int b0 = 0; b0 < c.batch; b0 += 64) {
-    if (c.batch > 64 || a.d.split_keys) n = b0 + lane < c.batch ? focus::paged_length(c, b0 + lane) : 0;
+    const int n = b0 + lane < c.batch ? focus::paged_length(c, b0 + lane) : 0;
     const int own = b0 + lane < c.batch ? max(1, (n - 1) / rows + 1) : 0;
     const int upto = wave_scan(own), all = __builtin_amdgcn_readlane(upto, 63);
     if (i < before + all) {
@@ -160,13 +242,13 @@ template <typename T, int D> struct Tile {
   static constexpr int kPer = D / 16;               // elements of a V row a lane holds
   static constexpr int kWords = kPer * sizeof(T) / 4;
   static constexpr int kPiece = 16 / sizeof(T);     // elements of a 16-byte load
-  static constexpr int kSteps = D / (4 * kPiece);   // 16-byte pieces of a K row a lane holds
+  static constexpr int strides = D / (4 * kPiece);   // 16-byte pieces of a K row a lane holds
   static constexpr int kProducts = kBf16 ? 2 : 1;   // K rows a lane holds
   // pieces of 16 bytes (8 where a lane's share of a V row is that): whole vectors, which
   // stay where their load puts them
   using V = typename std::conditional<kWords == 2, u32x2, u32x4>::type;
   static constexpr int kVSize = sizeof(V) / 4, kVs = kWords / kVSize;
-  u32x4 k[kProducts][kSteps];
+  u32x4 k[kProducts][strides];
   V v[kScores][kVs];
   __device__ uint32_t word(int j, int i) const { return v[j][i / kVSize][i % kVSize]; }
 };
@@ -180,22 +262,25 @@ __device__ __forceinline__ V load_once(const void* p) {
 }
 
 template <typename T, int D>
-__global__ __launch_bounds__(kThreads, 2) void paged_attend(Args a) {
+__global__ __launch_bounds__(kThreads, resident(D)) void paged_attend(Args a) {
   using L = Tile<T, D>;
   constexpr int kPitch = D + 4;
   __shared__ int64_t s_page[kPages + 1];  // (a chunk may begin inside a page)
   __shared__ float s_o[kWaves][kCols][kPitch];
   __shared__ float2 s_ml[kWaves][kCols];
   const focus_paged_kv& c = a.d.cache;
-  const int K = c.n_kv_heads, H = a.d.n_heads, G = H / K;
+  const int H = a.d.n_heads, G = a.group;
   // (a wave's number in a scalar register: its loops are branches then, not masks)
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / 64);
   const int lane = tid % 64, col = lane % 16, x = lane / 16;
-  const int tile_id = blockIdx.x % a.tiles, g = blockIdx.x / a.tiles % K;
+  const int tile_id = a.tiles == 1 ? 0 : blockIdx.x % a.tiles;
+  const int g0 = (a.tiles == 1 ? blockIdx.x : blockIdx.x / a.tiles) << a.wide_shift;
+  // waves of a KV head; this wave's head, and which of its waves it is
+  const int by = kWaves >> a.wide_shift, at_head = wave >> (2 - a.wide_shift), g = g0 + at_head, among = wave & (by - 1);
   Chunk ch;
-  if (!find_chunk(a, blockIdx.x / (a.tiles * K), ch)) return;
+  if (!find_chunk(a, blockIdx.z * kMaxGrid + blockIdx.y, ch)) return;
   const int b = ch.b, r0 = ch.c * ch.rows, r1 = min(ch.n, r0 + ch.rows);
-  const bool first = g == 0 && tile_id == 0;
+  const bool first = g0 == 0 && tile_id == 0;
   if (first && ch.c == 0 && tid == 0) {
     a.info[b] = make_int4(ch.slot0, ch.chunks, ch.n, 0);
     if (ch.n != c.length[b]) focus::raise_err(a.d.err, FOCUS_ERR_CAPACITY);
@@ -203,11 +288,11 @@ __global__ __launch_bounds__(kThreads, 2) void paged_attend(Args a) {
   const int h0 = g * G + tile_id * kCols, heads = min(kCols, G - tile_id * kCols);
 
   // Q: column col, elements as the K rows' pieces
-  u32x4 q[L::kSteps];
+  u32x4 q[L::strides];
   {
     const T* src = reinterpret_cast<const T*>(a.d.q) + (int64_t)b * a.d.q_row + (int64_t)(h0 + col) * a.d.q_head;
 #pragma unroll
-    for (int i = 0; i < L::kSteps; ++i)
+    for (int i = 0; i < L::strides; ++i)
       q[i] = col < heads ? *reinterpret_cast<const u32x4*>(src + (i * 4 + x) * L::kPiece) : u32x4{0, 0, 0, 0};
   }
 
@@ -253,7 +338,7 @@ __global__ __launch_bounds__(kThreads, 2) void paged_attend(Args a) {
 #pragma unroll
         for (int t = 0; t < L::kProducts; ++t)
 #pragma unroll
-          for (int i = 0; i < L::kSteps; ++i) w.k[t][i] = load_once<u32x4>(kp + 4 * t * ks + i * 4 * L::kPiece);
+          for (int i = 0; i < L::strides; ++i) w.k[t][i] = load_once<u32x4>(kp + 4 * t * ks + i * 4 * L::kPiece);
 #pragma unroll
         for (int j = 0; j < L::kScores; ++j)
 #pragma unroll
@@ -265,7 +350,7 @@ __global__ __launch_bounds__(kThreads, 2) void paged_attend(Args a) {
         for (int t = 0; t < L::kProducts; ++t) {
           s[t] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-          for (int i = 0; i < L::kSteps; ++i) {
+          for (int i = 0; i < L::strides; ++i) {
             if constexpr (L::kBf16) {
               s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w.k[t][i]),
                                                              __builtin_bit_cast(bf16x8, q[i]), s[t], 0, 0, 0);
@@ -342,20 +427,20 @@ __global__ __launch_bounds__(kThreads, 2) void paged_attend(Args a) {
       // loop, loads past the end taken from kZeros and the last of them waited for behind
       // it: otherwise the compiler cannot tell which loads are in flight at a round's start
       // and waits for half of them.
-      constexpr int kStep = kWaves * L::kRows;
-      int r = seg + wave * L::kRows;
+      const int stride = by * L::kRows;
+      int r = seg + among * L::kRows;
       if (r < full_end) {
         L w0, w1;
         load(w0, r, full_end);
-        for (; r + kStep < full_end; r += 2 * kStep) {
-          load(w1, r + kStep, full_end);
+        for (; r + stride < full_end; r += 2 * stride) {
+          load(w1, r + stride, full_end);
           compute(w0, r, std::true_type{});
-          load(w0, r + 2 * kStep, full_end);
-          compute(w1, r + kStep, std::true_type{});
+          load(w0, r + 2 * stride, full_end);
+          compute(w1, r + stride, std::true_type{});
         }
         if (r < full_end) {
           compute(w0, r, std::true_type{});
-          r += kStep;
+          r += stride;
         }
         __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0)
       }
@@ -387,30 +472,37 @@ __global__ __launch_bounds__(kThreads, 2) void paged_attend(Args a) {
     if (__syncthreads_or(nan)) pass(std::false_type{});
   }
 
-  // the waves' parts, joined
+  // the waves' parts of each query head, joined
   l += __shfl_xor(l, 16);
   l += __shfl_xor(l, 32);
   if (x == 0) s_ml[wave][col] = make_float2(m, l);
   __syncthreads();
-  for (int i = tid; i < heads * D; i += kThreads) {
-    const int h = i / D, e = i % D;
-    float M = kMinit, Lsum = 0.f, y = 0.f;
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) M = fmaxf(M, s_ml[w][h].x);
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
-      const float f = __builtin_amdgcn_exp2f(s_ml[w][h].x - M);
-      Lsum = fmaf(s_ml[w][h].y, f, Lsum);
-      y = fmaf(s_o[w][h][e], f, y);
+  constexpr int kLanes = D / 4;  // threads of a head, four elements each
+  const int e = tid % kLanes * 4;
+  for (int h = tid / kLanes, w0 = 0; w0 < kWaves; h += kThreads / kLanes) {
+    while (h >= heads && w0 < kWaves) h -= heads, w0 += by;
+    if (w0 >= kWaves) break;
+    float2 ml = s_ml[w0][h];
+    f32x4 y = *reinterpret_cast<const f32x4*>(&s_o[w0][h][e]);
+    for (int w = w0 + 1; w < w0 + by; ++w) {
+      const float2 other = s_ml[w][h];
+      const float M = fmaxf(ml.x, other.x);
+      const float f = __builtin_amdgcn_exp2f(ml.x - M), f2 = __builtin_amdgcn_exp2f(other.x - M);
+      ml = make_float2(M, fmaf(ml.y, f, other.y * f2));
+      y = y * f + *reinterpret_cast<const f32x4*>(&s_o[w][h][e]) * f2;
     }
-    const int64_t at = (int64_t)b * H + h0 + h, slot = (int64_t)(ch.slot0 + ch.c) * H + h0 + h;
+    const int head = (g0 + (w0 >> (2 - a.wide_shift))) * G + tile_id * kCols + h;
+    const int64_t at = (int64_t)b * H + head, slot = (int64_t)(ch.slot0 + ch.c) * H + head;
     if (ch.chunks == 1) {
-      reinterpret_cast<T*>(a.d.o)[at * D + e] = (T)(Lsum == 0.f ? 0.f : y / Lsum);
-      if (e == 0 && a.d.lse) a.d.lse[at] = Lsum == 0.f ? -INFINITY : (M + log2f(Lsum)) * kLn2;
+      y = ml.y == 0.f ? f32x4{0.f, 0.f, 0.f, 0.f} : y * (1.f / ml.y);
+      T* o_at = reinterpret_cast<T*>(a.d.o) + at * D + e;
+      if constexpr (L::kBf16) *reinterpret_cast<u32x2*>(o_at) = u32x2{focus::pack_bf16x2(y[0], y[1]), focus::pack_bf16x2(y[2], y[3])};
+      else *reinterpret_cast<f32x4*>(o_at) = y;
+      if (e == 0 && a.d.lse) a.d.lse[at] = ml.y == 0.f ? -INFINITY : (ml.x + log2f(ml.y)) * kLn2;
     } else {
-      a.o[slot * D + e] = y;
+      *reinterpret_cast<f32x4*>(a.o + slot * D + e) = y;
     }
-    if (e == 0) a.ml[slot] = make_float2(M, Lsum);
+    if (e == 0) a.ml[slot] = ml;
   }
 }
 
@@ -440,15 +532,17 @@ constexpr int kWeightRows = 4 * kThreads;   // rows whose weights a workgroup wr
 // over the chunks, eight loads in flight each, the first of them before the maximum is
 // known) and, where weights are accumulated, writes those of every parts-th block of rows.
 template <typename T, int D>
-__global__ __launch_bounds__(kThreads) void paged_join(Args a, int parts) {
+__global__ __launch_bounds__(kThreads) void paged_join(Args a) {
   constexpr int kLanes = D / 4, kGroups = kThreads / kLanes, kFlight = 8;
   __shared__ float4 s_o[kGroups][kLanes];
   __shared__ float s_lse[kThreads];
   const focus_paged_kv& c = a.d.cache;
-  const int K = c.n_kv_heads, H = a.d.n_heads, G = H / K, tid = threadIdx.x;
+  const int K = c.n_kv_heads, H = a.d.n_heads, G = a.group, tid = threadIdx.x, parts = a.parts;
   // (part 0 of all first: the later ones have nothing to do where sequences are short, and
   // with parts side by side those that do would all lie on a few of the XCDs)
-  const int item = blockIdx.x % (c.batch * K), part = blockIdx.x / (c.batch * K), g = item % K, b = item / K;
+  const int part = c.batch <= kMaxGrid ? blockIdx.z : blockIdx.z % parts, g = blockIdx.x;
+  const int b = blockIdx.y + (c.batch <= kMaxGrid ? 0 : blockIdx.z / parts * kMaxGrid);
+  if (b >= c.batch) return;
   const int4 info = a.info[b];
   if (info.y > 1) {
     const int e = tid % kLanes, grp = tid / kLanes;
@@ -533,6 +627,8 @@ focus_status validate(const focus_paged_decode_desc* d) {
     return FOCUS_E_ARG;
   if (d->n_heads % c.n_kv_heads) return FOCUS_E_SHAPE;
   if ((int64_t)c.batch * d->n_heads > INT32_MAX / kThreads) return FOCUS_E_SHAPE;
+  // (chunks are counted in 32 bits, in units of 32 rows at least)
+  if ((int64_t)c.batch * focus::ceil_div((int64_t)c.max_pages * c.page_rows, 32) > INT32_MAX) return FOCUS_E_SHAPE;
   const int64_t es = focus::elt_bytes(c.dtype);
   if (d->q_row < 0 || d->q_head < 0 || !focus::pieces16(d->q_row, es) || !focus::pieces16(d->q_head, es))
     return FOCUS_E_ARG;
@@ -540,20 +636,25 @@ focus_status validate(const focus_paged_decode_desc* d) {
 }
 
 template <typename T, int D>
-focus_status launch(const Args& a, const Plan& p, hipStream_t s) {
+focus_status launch(Args a, const Plan& p, hipStream_t s) {
   const focus_paged_kv& c = a.d.cache;
-  const int64_t blocks = p.slots * c.n_kv_heads * p.tiles;
   // workgroups of a (sequence, KV head) in the second launch: one per query head, or, for
   // weights, per block of the table's rows, but not many more than the device holds
   const int64_t per = focus::ceil_div(std::max<int64_t>(p.cap, 1), kWeightRows), heads = (int64_t)c.batch * c.n_kv_heads;
-  const int64_t group = a.d.n_heads / c.n_kv_heads;
-  const int64_t parts = a.d.accumulate
-      ? std::max(std::min(per, focus::ceil_div(8 * focus::device_cus(), heads)), std::min<int64_t>(group, 4)) : group;
-  if (blocks > INT32_MAX / kThreads || heads * parts > INT32_MAX / kThreads) return FOCUS_E_SHAPE;
-  hipLaunchKernelGGL((paged_attend<T, D>), dim3((uint32_t)blocks), dim3(kThreads), 0, s, a);
+  if (a.d.accumulate)
+    a.parts = (int)std::max(std::min(per, focus::ceil_div(8 * focus::device_cus(), heads)), std::min<int64_t>(a.group, 4));
+  const int64_t slots = focus::ceil_div(p.slots, kMaxGrid), batches = focus::ceil_div(c.batch, kMaxGrid);
+  if (p.groups * p.slots > INT32_MAX / kThreads || heads * a.parts > INT32_MAX / kThreads || slots > kMaxGrid ||
+      batches * a.parts > kMaxGrid)
+    return FOCUS_E_SHAPE;
+  hipLaunchKernelGGL((paged_attend<T, D>),
+                     dim3((uint32_t)p.groups, (uint32_t)std::min<int64_t>(p.slots, kMaxGrid), (uint32_t)slots),
+                     dim3(kThreads), 0, s, a);
   const focus_status st = focus::launch_status();
   if (st != FOCUS_OK) return st;
-  hipLaunchKernelGGL((paged_join<T, D>), dim3((uint32_t)(heads * parts)), dim3(kThreads), 0, s, a, (int)parts);
+  hipLaunchKernelGGL((paged_join<T, D>),
+                     dim3((uint32_t)c.n_kv_heads, (uint32_t)std::min(c.batch, kMaxGrid), (uint32_t)(batches * a.parts)),
+                     dim3(kThreads), 0, s, a);
   return focus::launch_status();
 }
 
@@ -576,7 +677,8 @@ extern "C" focus_status focus_paged_decode(const focus_paged_decode_desc* d, foc
   if (!d->workspace || d->workspace_bytes < p.bytes) return FOCUS_E_WORKSPACE;
   if (!focus::aligned16(d->workspace)) return FOCUS_E_ARG;
   char* ws = reinterpret_cast<char*>(d->workspace);
-  Args a = {*d, 0.f, focus::page_shift(c), p.tiles, p.target, p.cap, reinterpret_cast<int4*>(ws),
+  Args a = {*d, 0.f, focus::page_shift(c), p.tiles, __builtin_ctz((unsigned)p.wide),
+            __builtin_ctz((unsigned)p.unit), (int)p.target, d->n_heads / c.n_kv_heads, d->n_heads / c.n_kv_heads, p.cap, reinterpret_cast<int4*>(ws),
             reinterpret_cast<float2*>(ws + p.ml), reinterpret_cast<float*>(ws + p.o),
             reinterpret_cast<float*>(ws + p.score)};
   const float scale = d->softmax_scale > 0.f ? d->softmax_scale : 1.0f / sqrtf((float)c.head_dim);
