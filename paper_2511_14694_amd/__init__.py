@@ -571,6 +571,15 @@ def _err_ptr(err, dev: int):
     return _need(err, torch.int32, None, dev, "err")
 
 
+def _workspace(t, dev: int):
+    """(address, bytes) of a caller's workspace, or none."""
+    if t is None:
+        return None, 0
+    if t.get_device() != dev or not t.is_contiguous():
+        raise ValueError("workspace must be contiguous, on the other tensors' device")
+    return t.data_ptr(), t.numel() * t.element_size()
+
+
 def _launch(call: str, d, dev: int, stream):
     """Enqueue a call on device dev, whichever one is current."""
     if dev < 0:
@@ -680,7 +689,7 @@ def focus_rope(pos, turns, q=None, k=None, v=None, layout: int = FOCUS_ROPE_INTE
         heads = q.shape[1]
         qs = (n, heads, dim)
         if q_out is None:
-            q_out = torch.empty(qs, dtype=dtype, device=q.device)
+            q_out = torch.empty_like(q, memory_format=torch.contiguous_format)
         q_rows, qo_rows = _rows(q, qs, dtype, dev, "q"), _rows(q_out, qs, dtype, dev, "q_out")
     elif q_out is not None:
         raise ValueError("q_out without q")
@@ -689,7 +698,7 @@ def focus_rope(pos, turns, q=None, k=None, v=None, layout: int = FOCUS_ROPE_INTE
         ks = (n, kv, dim)
         k_rows = _rows(k, ks, dtype, dev, "k")
         if k_out is None and cache is None:
-            k_out = torch.empty(ks, dtype=dtype, device=k.device)
+            k_out = torch.empty_like(k, memory_format=torch.contiguous_format)
         if k_out is not None:
             ko_rows = _rows(k_out, ks, dtype, dev, "k_out")
     elif k_out is not None:
@@ -728,8 +737,7 @@ def _paged_decode_desc(q, cache, o, lse, weight_decay, workspace, split_keys, so
                            0.0 if weight_decay is None else weight_decay, 0, *_rows(q, shape, dtype, dev, "q"),
                            None if o is None else _need(o, dtype, shape, dev, "o"),
                            None if lse is None else _need(lse, torch.float32, shape[:2], dev, "lse"),
-                           _ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(),
-                           None if err is None else _err_ptr(err, dev))
+                           *_workspace(workspace, dev), None if err is None else _err_ptr(err, dev))
 
 
 def focus_paged_decode_workspace(q, cache: PagedCache, weight_decay=None, split_keys: int = 0) -> int:
@@ -744,9 +752,9 @@ def focus_paged_decode(q, cache: PagedCache, o=None, lse=None, weight_decay: Opt
     weight_decay: also cache.weight = weight_decay * cache.weight + the step's softmax
     weights, summed over the heads of each KV head."""
     if o is None:
-        o = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        o = torch.empty_like(q, memory_format=torch.contiguous_format)
     if lse is None and want_lse:
-        lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device)
+        lse = q.new_empty(q.shape[:2], dtype=torch.float32)
     d = _paged_decode_desc(q, cache, o, lse, weight_decay, workspace, split_keys, softmax_scale, err)
     if workspace is None:
         n = lib().focus_paged_decode_workspace(C.byref(d))
@@ -768,9 +776,8 @@ def _paged_evict_desc(cache, out, budget, recent, keep, workspace, err):
     if keep is not None:
         rows = keep.shape[-1]
         keep = _need(keep, torch.int32, (c.batch, c.n_kv_heads, rows), dev, "keep")
-    return PagedEvictDesc(c, to, int(budget), int(recent), budgets, keep, rows, _ptr(workspace),
-                          0 if workspace is None else workspace.numel() * workspace.element_size(),
-                          _err_ptr(err, dev))
+    return PagedEvictDesc(c, to, int(budget), int(recent), budgets, keep, rows, *_workspace(workspace, dev),
+                          None if err is None else _err_ptr(err, dev))
 
 
 def focus_paged_evict_workspace(cache: PagedCache, out: PagedCache, budget, recent: int = 0, keep=None) -> int:
