@@ -69,4 +69,25 @@ __device__ inline int64_t row_at(const focus_paged_kv& c, int64_t p, int r, int 
   return p * c.page_stride + (int64_t)(r & (c.page_rows - 1)) * c.row_stride + (int64_t)g * c.head_stride;
 }
 
+// Inclusive prefix over the wave of a sum or, for values from 0 up, a maximum (DPP: rows of
+// 16 lanes, then their last lanes' values).
+template <typename Op>
+__device__ inline int wave_prefix(int x, Op op) {
+#define FOCUS_STEP(ctrl, rows) x = op(x, __builtin_amdgcn_update_dpp(0, x, ctrl, rows, 0xf, true))
+  FOCUS_STEP(0x111, 0xf);
+  FOCUS_STEP(0x112, 0xf);
+  FOCUS_STEP(0x114, 0xf);
+  FOCUS_STEP(0x118, 0xf);
+  FOCUS_STEP(0x142, 0xa);
+  FOCUS_STEP(0x143, 0xc);
+#undef FOCUS_STEP
+  return x;
+}
+__device__ inline int wave_scan(int x) {
+  return wave_prefix(x, [](int a, int b) { return a + b; });
+}
+__device__ inline int wave_max(int x) {
+  return __builtin_amdgcn_readlane(wave_prefix(x, [](int a, int b) { return max(a, b); }), 63);
+}
+
 }  // namespace focus

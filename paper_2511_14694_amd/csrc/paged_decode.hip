@@ -33,6 +33,8 @@ namespace {
 using focus::bf16x8;
 using focus::f32x4;
 using focus::u32x4;
+using focus::wave_max;
+using focus::wave_scan;
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
 constexpr float kLn2 = 0.69314718055994531f;
@@ -105,27 +107,6 @@ struct Args {
   float* o;
   float* score;
 };
-
-// Inclusive prefix over the wave of a sum or, for values from 0 up, a maximum (DPP: rows of
-// 16 lanes, then their last lanes' values).
-template <typename Op>
-__device__ inline int wave_prefix(int x, Op op) {
-#define FOCUS_STEP(ctrl, rows) x = op(x, __builtin_amdgcn_update_dpp(0, x, ctrl, rows, 0xf, true))
-  FOCUS_STEP(0x111, 0xf);
-  FOCUS_STEP(0x112, 0xf);
-  FOCUS_STEP(0x114, 0xf);
-  FOCUS_STEP(0x118, 0xf);
-  FOCUS_STEP(0x142, 0xa);
-  FOCUS_STEP(0x143, 0xc);
-#undef FOCUS_STEP
-  return x;
-}
-__device__ inline int wave_scan(int x) {
-  return wave_prefix(x, [](int a, int b) { return a + b; });
-}
-__device__ inline int wave_max(int x) {
-  return __builtin_amdgcn_readlane(wave_prefix(x, [](int a, int b) { return max(a, b); }), 63);
-}
 
 // Maximum over the lanes 16 and 32 apart.
 __device__ inline float max_column(float x) {

@@ -45,27 +45,23 @@ __device__ inline int kept_rows(const focus_paged_evict_desc& d, int b, int n, i
 
 // Exclusive prefix sum of x over the workgroup; *total: the sum.
 __device__ inline int scan(int x, int* waves, int* total) {
-  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-  int y = x;
-#pragma unroll
-  for (int i = 1; i < 64; i <<= 1) {
-    const int z = __shfl_up(y, i);
-    if (lane >= i) y += z;
-  }
+  const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  const int y = focus::wave_scan(x);
   __syncthreads();
   if (lane == 63) waves[wave] = y;
   __syncthreads();
-  int before = 0, sum = 0;
-#pragma unroll
-  for (int w = 0; w < kWaves; ++w) {
-    if (w < wave) before += waves[w];
-    sum += waves[w];
-  }
-  *total = sum;
-  return before + y - x;
+  const int sums = focus::wave_scan(lane < kWaves ? waves[lane] : 0);
+  *total = __builtin_amdgcn_readlane(sums, kWaves - 1);
+  return (wave ? __builtin_amdgcn_readlane(sums, wave - 1) : 0) + y - x;
+}
+
+// Lanes below this one whose bit of mask is set.
+__device__ inline int lanes_below(uint64_t mask) {
+  return __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0));
 }
 
 constexpr int kDigits = 3, kBins = 2048;
+constexpr int kCopies = 4;  // of a histogram in LDS, lane by lane: [bin][copy]
 __device__ constexpr int digit_shift(int i) { return i == 0 ? 21 : i == 1 ? 10 : 0; }
 __device__ constexpr uint32_t digit_mask(int i) { return i == 2 ? 1023u : 2047u; }
 // the digits above digit i
@@ -92,47 +88,54 @@ __device__ Head head_of(const focus_paged_evict_desc& d, int bg, bool report) {
   return h;
 }
 
-// The rows of a workgroup in registers, as integers of their weights' order: NR a thread,
-// wave w the rows from first + 64 NR w, a register's 64 rows consecutive.  0, which is no
-// weight's integer (that of -inf is 0x7fffff), past the rows that a choice is made of.
+// The rows of a workgroup in registers, as integers of their weights' order: `used` of NR
+// registers a thread, wave w the rows from first + 64 used w, a register's 64 rows
+// consecutive.  0, which is no weight's integer (that of -inf is 0x7fffff), past the rows
+// that a choice is made of.
 template <int NR>
-__device__ void load_keys(const float* w, int64_t rows, int first, float (&x)[NR], int& row0) {
-  row0 = first + (int)(threadIdx.x / 64) * 64 * NR + (int)(threadIdx.x % 64);
+__device__ void load_keys(const float* w, int64_t rows, int first, int used, float (&x)[NR], int& row0) {
+  row0 = first + (int)(threadIdx.x / 64) * 64 * used + (int)(threadIdx.x % 64);
 #pragma unroll
-  for (int i = 0; i < NR; ++i) x[i] = row0 + 64 * i < rows ? w[row0 + 64 * i] : 0.f;
+  for (int i = 0; i < NR; ++i) x[i] = i < used && row0 + 64 * i < rows ? w[row0 + 64 * i] : 0.f;
 }
 template <int NR>
-__device__ void order_keys(const Head& h, const float (&x)[NR], int row0, uint32_t (&key)[NR]) {
+__device__ void order_keys(const Head& h, const float (&x)[NR], int row0, int used, uint32_t (&key)[NR]) {
 #pragma unroll
-  for (int i = 0; i < NR; ++i) key[i] = row0 + 64 * i < h.old ? order_of(x[i]) : 0u;
+  for (int i = 0; i < NR; ++i) key[i] = i < used && row0 + 64 * i < h.old ? order_of(x[i]) : 0u;
 }
+// Registers a thread needs for this many rows.
+__device__ inline int used_for(int rows) { return (rows + kThreads - 1) / kThreads; }
 
 // Histogram of a digit among the rows that share the digits above it, added to hist
 // (cleared by the caller; of digit 0, bucket 0 holds rows that are none, which no choice
-// reaches).  Atomics on one address go one after another, and equal weights are common:
-// where many lanes share the first one's bucket they are counted at once.  16 heads-of-8 x
-// 10 000 rows, the whole call: weights all different 24.8 us (23.9 with atomics alone, 27.1
-// with the first lane's always counted at once), all equal 27.5 (46.9; 28.8).
+// reaches).  Atomics on one address go one after another, and the first digit, mostly the
+// exponent, has few buckets that are full: lanes add to four copies in turn.  16 x 8 heads
+// of 10 000 rows, 64 of them kept, the whole call, with weights all different / all equal:
+// one copy 23.9 / 46.9 us, four 21.3 / 26.2, eight 22.0 / 24.2; lanes that share a bucket
+// counted at once where they are many, one copy, 24.8 / 27.5.
 template <int NR>
-__device__ void count_digit(const uint32_t (&key)[NR], int digit, uint32_t prefix, int* hist) {
+__device__ void count_digit(const uint32_t (&key)[NR], int used, int digit, uint32_t prefix, int* hist) {
   const uint32_t mask = above_mask(digit), dm = digit_mask(digit);
   const int shift = digit_shift(digit);
 #pragma unroll
   for (int i = 0; i < NR; ++i) {
-    const bool in = (key[i] & mask) == prefix;
-    const uint64_t any = __ballot(in);
-    if (any == 0) continue;
-    const int bin = in ? (int)((key[i] >> shift) & dm) : -1;
-    const int lead = __ffsll((unsigned long long)any) - 1;
-    const int one = __builtin_amdgcn_readlane(bin, lead);
-    const uint64_t same = __ballot(bin == one);
-    if (__popcll(same) > 16) {
-      if ((int)(threadIdx.x % 64) == lead) atomicAdd(&hist[one], (int)__popcll(same));
-      else if (in && bin != one) atomicAdd(&hist[bin], 1);
-    } else if (in) {
-      atomicAdd(&hist[bin], 1);
-    }
+    if (i < used && (key[i] & mask) == prefix)
+      atomicAdd(&hist[(key[i] >> shift & dm) * kCopies + threadIdx.x % kCopies], 1);
   }
+}
+
+// Clears the copies of a histogram; sums those of a bin.
+__device__ inline void clear_hist(int* hist) {
+  for (int i = threadIdx.x; i < kBins * kCopies / 4; i += kThreads) reinterpret_cast<int4*>(hist)[i] = make_int4(0, 0, 0, 0);
+}
+__device__ inline int bin_sum(const int* hist, int bin) {
+  int sum = 0;
+#pragma unroll
+  for (int i = 0; i < kCopies / 4; ++i) {
+    const int4 x = reinterpret_cast<const int4*>(hist + bin * kCopies)[i];
+    sum += (x.x + x.y) + (x.z + x.w);
+  }
+  return sum;
 }
 
 // How far the selection has come: the rows above `level` stay and `equal` of those that
@@ -142,18 +145,17 @@ struct Level {
   int equal, done;
 };
 
-// The bucket that holds the last of the `equal` greatest rows of a digit's histogram (of
-// kBins, with at least so many rows), in every thread: the level with that digit.  Where
-// the whole bucket stays, no further digit is needed: its rows are the ones above a level.
-__device__ int next_level(const int* hist, int digit, int* waves, int* found, Level& x) {
-  constexpr int kPer = kBins / kThreads;
+// The bucket that holds the last of the `equal` greatest rows of a digit's histogram (with
+// at least so many rows; c: this thread's bins, kBins - 1 - kPer tid downwards), in every
+// thread: the level with that digit.  Where the whole bucket stays, no further digit is
+// needed: its rows are the ones above a level.
+constexpr int kPer = kBins / kThreads;
+static_assert(kPer == 2, "two bins a thread");
+__device__ int next_level(const int (&c)[kPer], int digit, int* waves, int* found, Level& x) {
   const int tid = threadIdx.x;
-  int c[kPer], sum = 0;
+  int sum = 0;
 #pragma unroll
-  for (int i = 0; i < kPer; ++i) {
-    c[i] = hist[kBins - 1 - (tid * kPer + i)];
-    sum += c[i];
-  }
+  for (int i = 0; i < kPer; ++i) sum += c[i];
   int total, above = scan(sum, waves, &total);
 #pragma unroll
   for (int i = 0; i < kPer; ++i) {
@@ -177,27 +179,36 @@ __device__ int next_level(const int* hist, int digit, int* waves, int* found, Le
 // than `equal`; before this workgroup's rows come before_above above it and before_equal
 // equal to it.
 template <int NR>
-__device__ void write_rows(const Head& h, const uint32_t (&key)[NR], int row0, uint32_t level, int equal, int before_above,
+__device__ void write_rows(const Head& h, const uint32_t (&key)[NR], int used, int row0, uint32_t level, int equal, int before_above,
                            int before_equal, int (*waves)[2]) {
-  const int wave = threadIdx.x / 64;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   int above = 0, ties = 0;  // of this wave
 #pragma unroll
   for (int i = 0; i < NR; ++i) {
-    above += __popcll(__ballot(key[i] > level));
-    ties += __popcll(__ballot(key[i] == level));
+    if (i < used) {
+      above += __popcll(__ballot(key[i] > level));
+      ties += __popcll(__ballot(key[i] == level));
+    }
   }
   if (threadIdx.x % 64 == 0) waves[wave][0] = above, waves[wave][1] = ties;
   __syncthreads();
   above = before_above, ties = before_equal;
-  for (int w = 0; w < wave; ++w) above += waves[w][0], ties += waves[w][1];
+  const int lane = threadIdx.x % 64;
+  const int sum_above = focus::wave_scan(lane < kWaves ? waves[lane][0] : 0);
+  const int sum_ties = focus::wave_scan(lane < kWaves ? waves[lane][1] : 0);
+  if (wave) above += __builtin_amdgcn_readlane(sum_above, wave - 1), ties += __builtin_amdgcn_readlane(sum_ties, wave - 1);
 #pragma unroll
   for (int i = 0; i < NR; ++i) {
+    if (i >= used) continue;
     const uint64_t up = __ballot(key[i] > level), tie = __ballot(key[i] == level);
-    if ((up | tie) == 0) continue;
-    const uint64_t lower = (1ull << (threadIdx.x % 64)) - 1;
-    const int t = ties + __popcll(tie & lower), a = above + __popcll(up & lower);
-    if (key[i] > level || (key[i] == level && t < equal)) h.keep[a + min(t, equal)] = row0 + 64 * i;
-    above += __popcll(up), ties += __popcll(tie);
+    if (tie) {
+      const int t = ties + lanes_below(tie);
+      if (key[i] > level || (key[i] == level && t < equal)) h.keep[above + lanes_below(up) + min(t, equal)] = row0 + 64 * i;
+      ties += __popcll(tie);
+    } else if (key[i] > level) {
+      h.keep[above + lanes_below(up) + min(ties, equal)] = row0 + 64 * i;
+    }
+    above += __popcll(up);
   }
 }
 
@@ -268,27 +279,34 @@ __device__ void set_length(const focus_paged_evict_desc& d, int b) {
 
 template <int NR, bool COPY>
 __global__ __launch_bounds__(kThreads) void evict_select(focus_paged_evict_desc d, Copy y) {
-  __shared__ int hist[kBins];
+  __shared__ __align__(16) int hist[kBins * kCopies];
   __shared__ int waves[kWaves], found[3], parts[kWaves][2];
   // few weights are read at once, up to the table's end, before the length is known
   const int64_t cap = (int64_t)d.cache.max_pages * d.cache.page_rows;
   float w[NR];
   int row0;
-  if constexpr (NR <= 4) load_keys<NR>(d.cache.weight + (int64_t)blockIdx.x * d.cache.weight_rows, cap, 0, w, row0);
+  int used = NR;
+  if constexpr (NR <= 4) load_keys<NR>(d.cache.weight + (int64_t)blockIdx.x * d.cache.weight_rows, cap, 0, used, w, row0);
   const Head h = head_of(d, blockIdx.x, true);
   if (h.take > 0) {
     uint32_t key[NR];
-    if constexpr (NR > 4) load_keys<NR>(h.w, h.old, 0, w, row0);
-    order_keys<NR>(h, w, row0, key);
+    if constexpr (NR > 4) {
+      used = used_for(h.old);  // all waves alike
+      load_keys<NR>(h.w, h.old, 0, used, w, row0);
+    }
+    order_keys<NR>(h, w, row0, used, key);
     Level x = {0, h.take, 0};
     for (int digit = 0; digit < kDigits && !x.done; ++digit) {
-      for (int i = threadIdx.x; i < kBins; i += kThreads) hist[i] = 0;
+      clear_hist(hist);
       __syncthreads();
-      count_digit<NR>(key, digit, x.level, hist);
+      count_digit<NR>(key, used, digit, x.level, hist);
       __syncthreads();
-      next_level(hist, digit, waves, found, x);
+      int c[kPer];
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) c[i] = bin_sum(hist, kBins - 1 - (kPer * (int)threadIdx.x + i));
+      next_level(c, digit, waves, found, x);
     }
-    write_rows<NR>(h, key, row0, x.level, x.equal, 0, 0, parts);
+    write_rows<NR>(h, key, used, row0, x.level, x.equal, 0, 0, parts);
   }
   write_rest(d, h, 0, 1);
   if constexpr (COPY) {
@@ -316,16 +334,17 @@ struct Long {
 // writes the rows kept.
 template <int STEP>
 __global__ __launch_bounds__(kThreads) void evict_part(focus_paged_evict_desc d, Long y) {
-  __shared__ int hist[kBins];
+  __shared__ __align__(16) int hist[kBins * kCopies];
   __shared__ int waves[kWaves], found[3], pair[kWaves][2];
   const int bg = blockIdx.x / y.parts, part = blockIdx.x % y.parts, tid = threadIdx.x;
   const Head h = head_of(d, bg, STEP == 0 && part == 0);
   if (STEP == kDigits) write_rest(d, h, part, y.parts);
   const int live = (h.old + kPart - 1) / kPart;  // parts that hold rows
   if (h.take == 0 || part >= live) return;
-  // a digit's histogram of a part, two bins a thread
+  // a digit's histogram of a part, two bins a thread, the first thread's the last ones
+  const int bin0 = kBins - kPer * (tid + 1);
   auto bins = [&](int p, int digit) {
-    return reinterpret_cast<uint32_t*>(y.hist + (((int64_t)bg * y.parts + p) * kDigits + digit) * kBins) + tid;
+    return reinterpret_cast<uint32_t*>(y.hist + (((int64_t)bg * y.parts + p) * kDigits + digit) * kBins + bin0);
   };
   Level x = {0, h.take, 0};
   int before = 0, before_equal = 0;
@@ -341,8 +360,8 @@ __global__ __launch_bounds__(kThreads) void evict_part(focus_paged_evict_desc d,
   int row0;
   {
     float w[kLongRows];
-    load_keys<kLongRows>(h.w, h.old, part * kPart, w, row0);
-    order_keys<kLongRows>(h, w, row0, key);
+    load_keys<kLongRows>(h.w, h.old, part * kPart, kLongRows, w, row0);
+    order_keys<kLongRows>(h, w, row0, kLongRows, key);
   }
   if constexpr (STEP >= 1) {
     if (!x.done) {
@@ -359,11 +378,10 @@ __global__ __launch_bounds__(kThreads) void evict_part(focus_paged_evict_desc d,
           if (p0 + i < part) lo_b += c[i] & 0xffff, hi_b += c[i] >> 16;
         }
       }
-      hist[2 * tid] = lo, hist[2 * tid + 1] = hi;
-      __syncthreads();
-      const int bucket = next_level(hist, STEP - 1, waves, found, x);
-      const int own = 2 * tid == bucket ? lo_b : 2 * tid + 1 == bucket ? hi_b : 0;
-      const int up = (2 * tid > bucket ? lo_b : 0) + (2 * tid + 1 > bucket ? hi_b : 0);
+      const int c[kPer] = {hi, lo};
+      const int bucket = next_level(c, STEP - 1, waves, found, x);
+      const int own = bin0 == bucket ? lo_b : bin0 + 1 == bucket ? hi_b : 0;
+      const int up = (bin0 > bucket ? lo_b : 0) + (bin0 + 1 > bucket ? hi_b : 0);
       int total;
       scan(up + (x.done ? own : 0), waves, &total);
       before += total;
@@ -377,19 +395,16 @@ __global__ __launch_bounds__(kThreads) void evict_part(focus_paged_evict_desc d,
     }
   }
   if constexpr (STEP == kDigits) {
-    write_rows<kLongRows>(h, key, row0, x.level, x.equal, before, before_equal, pair);
+    write_rows<kLongRows>(h, key, kLongRows, row0, x.level, x.equal, before, before_equal, pair);
   } else {
     if (x.done) return;
+    clear_hist(hist);
     __syncthreads();
-    for (int i = tid; i < kBins; i += kThreads) hist[i] = 0;
+    count_digit<kLongRows>(key, kLongRows, STEP, x.level, hist);
     __syncthreads();
-    count_digit<kLongRows>(key, STEP, x.level, hist);
-    __syncthreads();
-    *bins(part, STEP) = (uint32_t)hist[2 * tid] | (uint32_t)hist[2 * tid + 1] << 16;
+    *bins(part, STEP) = (uint32_t)bin_sum(hist, bin0) | (uint32_t)bin_sum(hist, bin0 + 1) << 16;
   }
 }
-static_assert(kBins == 2 * kThreads, "two bins a thread");
-
 __global__ __launch_bounds__(kCopy) void evict_copy(focus_paged_evict_desc d, Copy y) {
   const int K = d.cache.n_kv_heads, b = blockIdx.x / K, g = blockIdx.x % K;
   const int per = kCopy / y.pieces;
@@ -478,9 +493,13 @@ extern "C" focus_status focus_paged_evict(const focus_paged_evict_desc* d, focus
     hipLaunchKernelGGL((evict_part<2>), grid, block, 0, s, *d, scratch);
     hipLaunchKernelGGL((evict_part<3>), grid, block, 0, s, *d, scratch);
   } else {
-    // A workgroup copies its own head's rows where that is little work, or where there
-    // are heads for every compute unit: a launch less.
-    const bool copies = d->keep_rows * pieces * 64 <= (256 << 10) || heads >= 2 * focus::device_cus();
+    // A workgroup copies its own head's rows where that is little work, somewhat more where
+    // there are heads for every compute unit: a launch less, but a long sequence's rows
+    // are copied by one compute unit.  64 x 8 heads, 2 000 rows kept of 4 000 (2 MB a head
+    // read and written): 238 us by the heads' own workgroups, 244 by a launch of its own, of
+    // uneven lengths 86 and 69; 32 x 32 heads, 500 rows kept of 1 000 (0.5 MB): 131 and 146.
+    const int64_t bytes = d->keep_rows * pieces * 64;
+    const bool copies = bytes <= (256 << 10) || (bytes <= (512 << 10) && heads >= 2 * focus::device_cus());
     const dim3 grid((uint32_t)heads);
     const int64_t cap = (int64_t)d->cache.max_pages * d->cache.page_rows;
 #define FOCUS_SELECT(NR)                                                              \
