@@ -224,8 +224,19 @@ struct Copy {
   bool lengths;                         // whether evict_select sets them (no length is read and written)
 };
 
-// Copies the kept rows j0, j0 + step, ... of one head, a piece a thread and `per` rows at a
-// time, with four of them in flight.
+template <bool STREAM>
+__device__ inline focus::u32x4 load_row(const void* pool, int64_t piece) {
+  const focus::u32x4* p = reinterpret_cast<const focus::u32x4*>(pool) + piece;
+  if constexpr (STREAM) return __builtin_nontemporal_load(p);
+  return *p;
+}
+
+// Copies the kept rows j0, j0 + step, ... of one head, a 16-byte piece of each by one thread,
+// four of them in flight.  Rows that a decode step has just read may still be in the last-level
+// cache: they are loaded past it only where there are more than it may hold (16 x 8 heads,
+// 5 000 rows of 256 bytes: 151 us past it, 155 through it; 8 heads, 32 768 rows: 87, 82; uneven
+// lengths count as the longest: 4 of up to 70 806 rows, 4 heads, 29 570 kept: 85, 68).
+template <bool STREAM>
 __device__ void copy_rows(const focus_paged_evict_desc& d, const Copy& y, int b, int g, int64_t j0, int64_t step,
                           int64_t end, int sub) {
   constexpr int kFlight = 4;
@@ -255,8 +266,8 @@ __device__ void copy_rows(const focus_paged_evict_desc& d, const Copy& y, int b,
 #pragma unroll
     for (int i = 0; i < kFlight; ++i) {
       if (src[i] >= 0) {
-        k[i] = __builtin_nontemporal_load(reinterpret_cast<const focus::u32x4*>(d.cache.k) + src[i]);
-        v[i] = __builtin_nontemporal_load(reinterpret_cast<const focus::u32x4*>(d.cache.v) + src[i]);
+        k[i] = load_row<STREAM>(d.cache.k, src[i]);
+        v[i] = load_row<STREAM>(d.cache.v, src[i]);
       }
       if (sub == 0 && r[i] >= 0 && d.out.weight) w[i] = d.cache.weight[bg * d.cache.weight_rows + r[i]];
     }
@@ -314,7 +325,7 @@ __global__ __launch_bounds__(kThreads) void evict_select(focus_paged_evict_desc 
     __syncthreads();  // the kept rows are this workgroup's own
     const int per = kThreads / y.pieces;
     if ((int)threadIdx.x < per * y.pieces)
-      copy_rows(d, y, h.b, h.g, threadIdx.x / y.pieces, per, h.take + h.recent, threadIdx.x % y.pieces);
+      copy_rows<false>(d, y, h.b, h.g, threadIdx.x / y.pieces, per, h.take + h.recent, threadIdx.x % y.pieces);
   }
 }
 
@@ -405,13 +416,23 @@ __global__ __launch_bounds__(kThreads) void evict_part(focus_paged_evict_desc d,
     *bins(part, STEP) = (uint32_t)bin_sum(hist, bin0) | (uint32_t)bin_sum(hist, bin0 + 1) << 16;
   }
 }
+// Neighbouring KV heads that a workgroup of evict_copy takes: their rows lie side by side
+// where they go.
+inline __host__ __device__ int heads_together(int n_kv_heads) {
+  return n_kv_heads % 4 == 0 ? 4 : n_kv_heads % 2 == 0 ? 2 : 1;
+}
+
+template <bool STREAM>
 __global__ __launch_bounds__(kCopy) void evict_copy(focus_paged_evict_desc d, Copy y) {
-  const int K = d.cache.n_kv_heads, b = blockIdx.x / K, g = blockIdx.x % K;
-  const int per = kCopy / y.pieces;
-  if ((int)threadIdx.x < per * y.pieces)
-    copy_rows(d, y, b, g, (int64_t)blockIdx.y * per + threadIdx.x / y.pieces, (int64_t)gridDim.y * per, d.keep_rows,
+  // (the heads' order turns with the rows: those of one sequence would all lie on the same
+  // XCDs otherwise)
+  const int K = d.cache.n_kv_heads, wide = heads_together(K), item = (blockIdx.x + blockIdx.y) % gridDim.x;
+  const int b = item / (K / wide), g0 = item % (K / wide) * wide;
+  const int at = threadIdx.x / y.pieces, per = kCopy / (y.pieces * wide);
+  if (at < per * wide)
+    copy_rows<STREAM>(d, y, b, g0 + at % wide, (int64_t)blockIdx.y * per + at / wide, (int64_t)gridDim.y * per, d.keep_rows,
               threadIdx.x % y.pieces);
-  if (blockIdx.y == 0 && g == 0 && threadIdx.x == 0) set_length(d, b);
+  if (blockIdx.y == 0 && g0 == 0 && threadIdx.x == 0) set_length(d, b);
 }
 
 __global__ __launch_bounds__(kCopy) void evict_lengths(focus_paged_evict_desc d) {
@@ -514,7 +535,13 @@ extern "C" focus_status focus_paged_evict(const focus_paged_evict_desc* d, focus
     }
   }
   if ((st = focus::launch_status()) != FOCUS_OK) return st;
-  const int64_t blocks = focus::ceil_div(d->keep_rows > 0 ? d->keep_rows : 1, (kCopy / pieces) * 8);
-  hipLaunchKernelGGL(evict_copy, dim3((uint32_t)heads, (uint32_t)std::min<int64_t>(blocks, 1024)), dim3(kCopy), 0, s, *d, y);
+  // four rows of a head and thread in flight, one round of them where the grid allows
+  const int wide = heads_together(d->cache.n_kv_heads);
+  const int64_t blocks = focus::ceil_div(std::max<int64_t>(d->keep_rows, 1), kCopy / (pieces * wide) * 4);
+  const dim3 grid((uint32_t)(heads / wide), (uint32_t)std::min<int64_t>(blocks, 4096));
+  if (heads * d->keep_rows * pieces * 64 > (512ll << 20))
+    hipLaunchKernelGGL((evict_copy<true>), grid, dim3(kCopy), 0, s, *d, y);
+  else
+    hipLaunchKernelGGL((evict_copy<false>), grid, dim3(kCopy), 0, s, *d, y);
   return focus::launch_status();
 }
