@@ -44,6 +44,7 @@ constexpr int kThreads = 256, kWaves = 4;
 constexpr int kMaxGrid = 32768; // workgroups in a grid's second and third dimension
 constexpr int kCols = 16;       // query heads of a workgroup: columns of a product
 constexpr int kPages = 1024;    // page offsets held in LDS at a time
+constexpr int kWhole = 256;     // rows of a table that is not split
 constexpr int kUnit = 128;      // rows of a chunk times KV heads of a workgroup: a multiple of this
 
 // What a lane reads in the place of eight rows that begin past their sequence's end or
@@ -62,6 +63,7 @@ struct Plan {
   int tiles;            // workgroups a KV head's query heads take
   int wide, unit;       // KV heads of a workgroup; chunks are multiples of `unit` rows
   int64_t groups;       // workgroups of a chunk: n_kv_heads / wide * tiles
+  bool single;          // a sequence is one chunk
 };
 
 // Workgroups of paged_attend that a compute unit holds (by their registers).
@@ -78,19 +80,33 @@ Plan make_plan(const focus_paged_decode_desc* d) {
   // 4.5 apart; of 256 bytes 5.9, 5.3; 16 x 10 000 rows of 32 KV heads 6.5, 5.6.  Where a
   // head's rows follow one another (5.9) there is nothing to gain.
   p.wide = c.head_stride > c.row_stride ? 1 : c.n_kv_heads % 4 == 0 ? 4 : c.n_kv_heads % 2 == 0 ? 2 : 1;
+  // Short tables are not split, so that without weights nothing is left for a second launch;
+  // up to twice as long where their heads alone fill half of the device, and not where they
+  // fill it several times and neighbouring heads are better read together.  us, split / not:
+  //   sequences, KV heads, group     128 rows      256          500          1000
+  //     1,  8, 4 (D 128, bf16)      9.2 /  5.8   9.2 /  7.6   9.4 /  9.8  10.0 / 17.8
+  //    32,  8, 4                   11.4 /  6.9  15.3 / 10.1  22.4 / 15.5  31.8 / 27.5
+  //    32,  4, 16 (f32)            18.8 / 10.2  23.1 / 15.5  30.1 / 26.1  40.9 / 46.7
+  //   128, 32, 1                   54.0 / 73.3  93.1 / 118    170 / 197    329 / 374
+  const int64_t heads = (int64_t)c.batch * c.n_kv_heads * p.tiles;
+  p.single = d->split_keys == 0 && ((p.cap <= kWhole && (heads <= 1024 || p.wide == 1)) ||
+                                    (p.cap <= 2 * kWhole && heads >= 128 && heads <= 1024));
+  if (p.single) p.wide = 1;
   p.unit = kUnit / p.wide;
   p.groups = (int64_t)c.n_kv_heads / p.wide * p.tiles;
-  if (d->split_keys > 0) {
+  if (p.single) {
+    p.slots = c.batch;
+  } else if (d->split_keys > 0) {
     p.slots = c.batch * std::max<int64_t>(1, focus::ceil_div(p.cap, d->split_keys));
   } else {
     p.target = std::max<int64_t>(1, resident(c.head_dim) * focus::device_cus() / p.groups);
     // a chunk has at least the rows of the batch over the target; a sequence at least one
     p.slots = std::min(c.batch + p.target, c.batch * std::max<int64_t>(1, focus::ceil_div(p.cap, p.unit)));
   }
-  const int64_t heads = p.slots * d->n_heads;
+  const int64_t partials = p.slots * d->n_heads;
   p.ml = 16 * (int64_t)c.batch;
-  p.o = p.ml + focus::ceil_div(8 * heads, 16) * 16;
-  p.score = p.o + 4 * heads * c.head_dim;
+  p.o = p.ml + focus::ceil_div(8 * partials, 16) * 16;
+  p.score = p.o + 4 * partials * c.head_dim;
   p.bytes = (size_t)(p.score + (d->accumulate ? 4 * (int64_t)c.batch * d->n_heads * p.cap : 0));
   return p;
 }
@@ -633,7 +649,7 @@ focus_status launch(Args a, const Plan& p, hipStream_t s) {
                      dim3((uint32_t)p.groups, (uint32_t)std::min<int64_t>(p.slots, kMaxGrid), (uint32_t)slots),
                      dim3(kThreads), 0, s, a);
   const focus_status st = focus::launch_status();
-  if (st != FOCUS_OK) return st;
+  if (st != FOCUS_OK || (p.single && !a.d.accumulate)) return st;
   hipLaunchKernelGGL((paged_join<T, D>),
                      dim3((uint32_t)c.n_kv_heads, (uint32_t)std::min(c.batch, kMaxGrid), (uint32_t)(batches * a.parts)),
                      dim3(kThreads), 0, s, a);
@@ -665,6 +681,7 @@ extern "C" focus_status focus_paged_decode(const focus_paged_decode_desc* d, foc
             reinterpret_cast<float*>(ws + p.score)};
   const float scale = d->softmax_scale > 0.f ? d->softmax_scale : 1.0f / sqrtf((float)c.head_dim);
   a.sc = scale * kLog2e;
+  if (p.single) a.d.split_keys = (int)focus::ceil_div(std::max<int64_t>(p.cap, 1), kUnit) * kUnit;
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   if (c.dtype == FOCUS_BF16) return c.head_dim == 128 ? launch<__bf16, 128>(a, p, s) : launch<__bf16, 64>(a, p, s);
   return c.head_dim == 128 ? launch<float, 128>(a, p, s) : launch<float, 64>(a, p, s);
