@@ -793,7 +793,8 @@ focus_status focus_rope(const focus_rope_desc* d, focus_stream_t stream);
  *                       row r over the heads of g        (accumulate; rows < length[b])
  * With weight_decay 0 the old weight is not read.  A sequence of length 0 has o = 0
  * and lse = -inf.  Whatever the pages hold past a sequence's length has no effect.
- * The rows of a sequence are split over several workgroups, joined by log-sum-exp;
+ * The rows of a sequence are split over several workgroups, joined by log-sum-exp (not
+ * those of short tables);
  * with split_keys = 0 the split follows the lengths of the whole batch, so that a
  * sequence's bits may differ by float32 rounding with what else is in the batch; a
  * given split_keys fixes them.  Results are deterministic. */
@@ -814,8 +815,8 @@ typedef struct {
   int32_t* err;
 } focus_paged_decode_desc;
 
-/* Workspace bytes of this descriptor on the current device (0 for one that the call
- * refuses).  The workspace is in use until the call's kernels end; calls that share
+/* Workspace bytes of this descriptor on the current device (0 where none is needed, as
+ * for tables of a few rows without weights, or the call refuses it).  The workspace is in use until the call's kernels end; calls that share
  * one on overlapping streams race. */
 size_t focus_paged_decode_workspace(const focus_paged_decode_desc* d);
 /* Errors: E_NULL, E_ARG, E_DTYPE, E_SHAPE (batch * max_pages * page_rows of 2^36 or more

@@ -18,6 +18,9 @@ Modules
              textbook dense causal attention it must reduce to with no summaries
   decode     streaming one token at a time over the same state
              (Appendix A.2 "Streaming with controlled memory")
+  paged      rotary positions, one token's attention over a paged cache and the
+             cache's eviction by accumulated weight (operators of serving that the
+             paper does not define; their definitions are the module's own)
 
 Parity pins (each function is checked against facts the paper or mathematics
 fix, never against itself) live in tests/test_oracle_*.py.  No function here is

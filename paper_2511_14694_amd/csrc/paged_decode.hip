@@ -53,7 +53,7 @@ __device__ __align__(16) const uint32_t kZeros[256] = {};
 
 // Workspace: int4 info[batch] {first slot, chunks, rows, 0}, then the partials of
 // `slots` chunks: float2 ml[slots][H], float o[slots][H][D], then, where weights are
-// accumulated, float score[batch][H][cap] (log2 units).
+// accumulated, float score[batch][H][cap] (log2 units).  None where neither is needed.
 struct Plan {
   int64_t slots;        // upper bound of the chunks of all sequences
   int64_t target;       // chunks resident at a time (split_keys 0)
@@ -108,6 +108,7 @@ Plan make_plan(const focus_paged_decode_desc* d) {
   p.o = p.ml + focus::ceil_div(8 * partials, 16) * 16;
   p.score = p.o + 4 * partials * c.head_dim;
   p.bytes = (size_t)(p.score + (d->accumulate ? 4 * (int64_t)c.batch * d->n_heads * p.cap : 0));
+  if (p.single && !d->accumulate) p.bytes = 0;  // nothing is handed on
   return p;
 }
 
@@ -280,7 +281,7 @@ __global__ __launch_bounds__(kThreads, resident(D)) void paged_attend(Args a) {
   const int b = ch.b, r0 = ch.c * ch.rows, r1 = min(ch.n, r0 + ch.rows);
   const bool first = g0 == 0 && tile_id == 0;
   if (first && ch.c == 0 && tid == 0) {
-    a.info[b] = make_int4(ch.slot0, ch.chunks, ch.n, 0);
+    if (a.info) a.info[b] = make_int4(ch.slot0, ch.chunks, ch.n, 0);
     if (ch.n != c.length[b]) focus::raise_err(a.d.err, FOCUS_ERR_CAPACITY);
   }
   const int h0 = g * G + tile_id * kCols, heads = min(kCols, G - tile_id * kCols);
@@ -500,7 +501,7 @@ __global__ __launch_bounds__(kThreads, resident(D)) void paged_attend(Args a) {
     } else {
       *reinterpret_cast<f32x4*>(a.o + slot * D + e) = y;
     }
-    if (e == 0) a.ml[slot] = ml;
+    if (e == 0 && a.ml) a.ml[slot] = ml;
   }
 }
 
@@ -672,13 +673,14 @@ extern "C" focus_status focus_paged_decode(const focus_paged_decode_desc* d, foc
   if (!d->q || !d->o || (d->accumulate && !c.weight)) return FOCUS_E_NULL;
   if (!focus::aligned16(d->q) || !focus::aligned16(d->o) || (reinterpret_cast<uintptr_t>(d->lse) & 3u)) return FOCUS_E_ARG;
   const Plan p = make_plan(d);
-  if (!d->workspace || d->workspace_bytes < p.bytes) return FOCUS_E_WORKSPACE;
+  if (p.bytes > 0 && (!d->workspace || d->workspace_bytes < p.bytes)) return FOCUS_E_WORKSPACE;
   if (!focus::aligned16(d->workspace)) return FOCUS_E_ARG;
   char* ws = reinterpret_cast<char*>(d->workspace);
   Args a = {*d, 0.f, focus::page_shift(c), p.tiles, __builtin_ctz((unsigned)p.wide),
             __builtin_ctz((unsigned)p.unit), (int)p.target, d->n_heads / c.n_kv_heads, d->n_heads / c.n_kv_heads, p.cap, reinterpret_cast<int4*>(ws),
             reinterpret_cast<float2*>(ws + p.ml), reinterpret_cast<float*>(ws + p.o),
             reinterpret_cast<float*>(ws + p.score)};
+  if (p.bytes == 0) a.info = nullptr, a.ml = nullptr;
   const float scale = d->softmax_scale > 0.f ? d->softmax_scale : 1.0f / sqrtf((float)c.head_dim);
   a.sc = scale * kLog2e;
   if (p.single) a.d.split_keys = (int)focus::ceil_div(std::max<int64_t>(p.cap, 1), kUnit) * kUnit;

@@ -88,6 +88,41 @@ def test_decode_many_sequences():
     _check(c, q64, F.focus_paged_decode(q, c.dev, weight_decay=1.0), "bf16", weight=c.weight, decay=1.0)
 
 
+@pytest.mark.parametrize("batch,top,H,K,dim,dtype,by_head", [
+    (130, 700, 4, 4, 64, "bf16", False),     # more sequences than a wave has lanes
+    (70, 1500, 2, 1, 128, "f32", False),
+    (40, 1100, 8, 8, 128, "bf16", True),     # chunks that would not all be resident: larger ones
+    (5, 4000, 34, 2, 64, "bf16", False),     # groups of 17, two KV heads together
+    (3, 9000, 4, 4, 128, "bf16", False),
+])
+def test_decode_chunks_chosen(batch, top, H, K, dim, dtype, by_head):
+    """Lengths from 0 to top in tables long enough to be split: every way a chunk's size
+    is chosen, with weights and without."""
+    announce(f"paged decode {batch} x {top} {H}/{K} x {dim} {dtype} by_head {by_head}")
+    rng = np.random.default_rng(batch)
+    lens = [top, 0, 1] + [int(x) for x in (rng.integers(top * 9 // 10, top, batch - 3) if by_head else
+                                           np.exp(rng.uniform(0, np.log(top), batch - 3)))]
+    c = Cache(rng, lens, K, dim, 64, dtype, by_head=by_head, weight=True)
+    q, q64 = values(rng, (batch, H, dim), dtype)
+    got = F.focus_paged_decode(q, c.dev)
+    _check(c, q64, got, dtype)
+    again = F.focus_paged_decode(q, c.dev, weight_decay=1.0)
+    assert torch.equal(again[0], got[0]) and torch.equal(again[1], got[1])
+    _check(c, q64, again, dtype, weight=c.weight, decay=1.0)
+
+
+def test_decode_split_keys_fix_a_sequences_bits():
+    """With a given split a sequence's result does not depend on the rest of the batch."""
+    rng = np.random.default_rng(40)
+    c = Cache(rng, [3000, 900, 40], 2, 128, 32, "bf16")
+    q, _ = values(rng, (3, 8, 128), "bf16")
+    o, lse = F.focus_paged_decode(q, c.dev, split_keys=256)
+    for b in range(3):
+        one = F.PagedCache(c.dev.k, c.dev.v, c.dev.table[b:b + 1], c.dev.length[b:b + 1])
+        o1, l1 = F.focus_paged_decode(q[b:b + 1], one, split_keys=256)
+        assert torch.equal(o1[0], o[b]) and torch.equal(l1[0], lse[b])
+
+
 def test_decode_sharp_scores_scale_and_views():
     """Scores of several hundred, a given scale, q as a view of a projection, outputs
     given; old weights that are not numbers count only where they are read."""

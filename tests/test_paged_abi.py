@@ -136,6 +136,7 @@ def _decode_ok():
     ("q", None, E_NULL), ("o", None, E_NULL), ("cache.weight", None, E_NULL), ("q", FAKE + 8, E_ARG),
     ("o", FAKE + 8, E_ARG), ("lse", FAKE + 2, E_ARG), ("workspace", None, E_WORKSPACE),
     ("workspace_bytes", 0, E_WORKSPACE), ("workspace", FAKE + 8, E_ARG), ("n_heads", 1 << 30, E_SHAPE),
+    ("cache.row_stride", 1 << 33, E_SHAPE),     # pages inside the rows: apart, but too far
 ] + [("cache." + f, v, s) for f, v, s in PAGED_BAD])
 def test_paged_decode_refusals(field, value, status):
     d = _decode_ok()
@@ -147,6 +148,13 @@ def test_paged_decode_empty_batch_and_workspace():
     d = _decode_ok()
     n = _abi.lib().focus_paged_decode_workspace(C.byref(d))
     assert n >= 2 * 8 * 80 * 4                  # the scores of every head and row
+    d.workspace_bytes = n - 1
+    assert _call("focus_paged_decode", d) == E_WORKSPACE
+    d.accumulate = 0
+    assert _abi.lib().focus_paged_decode_workspace(C.byref(d)) == 0     # 80 rows are not split
+    d.cache.max_pages, d.cache.weight_rows = 1000, 16_000
+    n = _abi.lib().focus_paged_decode_workspace(C.byref(d))
+    assert n > 0
     d.workspace_bytes = n - 1
     assert _call("focus_paged_decode", d) == E_WORKSPACE
     d.cache.batch = 0
@@ -178,6 +186,22 @@ def test_paged_evict_refusals(field, value, status):
     d = _evict_ok()
     _set(field, value)(d)
     assert _call("focus_paged_evict", d) == status
+
+
+def test_paged_evict_long_tables_need_a_workspace():
+    d = _evict_ok()
+    assert _abi.lib().focus_paged_evict_workspace(C.byref(d)) == 0
+    for c in (d.cache, d.out):
+        c.max_pages, c.weight_rows = 4096, 1 << 16
+    n = _abi.lib().focus_paged_evict_workspace(C.byref(d))
+    assert n >= 2 * 4 * 8 * 3 * 2048 * 2            # three histograms for each 8 192 rows of a head
+    for field, value, status in (("workspace_bytes", n - 1, E_WORKSPACE), ("workspace", None, E_WORKSPACE),
+                                 ("workspace", FAKE + 8, E_ARG)):
+        d.workspace, d.workspace_bytes = FAKE, n
+        setattr(d, field, value)
+        assert _call("focus_paged_evict", d) == status
+    d.cache.head_dim = 100
+    assert _abi.lib().focus_paged_evict_workspace(C.byref(d)) == 0
 
 
 def test_paged_evict_empty_batch():
