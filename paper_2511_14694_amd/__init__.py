@@ -716,7 +716,7 @@ def focus_rope(pos, turns, q=None, k=None, v=None, layout: int = FOCUS_ROPE_INTE
     elif v is not None:
         raise ValueError("v without a cache to store it in")
     rot = 0 if turns is None else 2 * turns.numel()
-    d = RopeDesc(_DTYPES[dtype], heads, kv, dim, rot, layout, 1 if inverse else 0, amplitude, n,
+    d = RopeDesc(_DTYPES[dtype], heads, kv, dim, rot, layout, 1 if inverse else 0, float(amplitude), n,
                  _need(pos, torch.int32, (n,), dev, "pos"),
                  _need(turns, torch.float64, None, dev, "turns") if rot else None,
                  *q_rows, *qo_rows, *k_rows, *ko_rows, *v_rows, c, seq, slot,
@@ -733,8 +733,8 @@ def _paged_decode_desc(q, cache, o, lse, weight_decay, workspace, split_keys, so
         raise ValueError("q must be [batch, heads, D] of the cache's batch, head_dim and device")
     if weight_decay is not None and cache.weight is None:
         raise ValueError("weight_decay needs a cache with weight")
-    return PagedDecodeDesc(c, shape[1], split_keys, softmax_scale, 0 if weight_decay is None else 1,
-                           0.0 if weight_decay is None else weight_decay, 0, *_rows(q, shape, dtype, dev, "q"),
+    return PagedDecodeDesc(c, shape[1], split_keys, float(softmax_scale), 0 if weight_decay is None else 1,
+                           0.0 if weight_decay is None else float(weight_decay), 0, *_rows(q, shape, dtype, dev, "q"),
                            None if o is None else _need(o, dtype, shape, dev, "o"),
                            None if lse is None else _need(lse, torch.float32, shape[:2], dev, "lse"),
                            *_workspace(workspace, dev), None if err is None else _err_ptr(err, dev))

@@ -241,13 +241,13 @@ template <typename T, int D> struct Tile {
   static constexpr int kPer = D / 16;               // elements of a V row a lane holds
   static constexpr int kWords = kPer * sizeof(T) / 4;
   static constexpr int kPiece = 16 / sizeof(T);     // elements of a 16-byte load
-  static constexpr int strides = D / (4 * kPiece);   // 16-byte pieces of a K row a lane holds
+  static constexpr int kSteps = D / (4 * kPiece);   // 16-byte pieces of a K row a lane holds
   static constexpr int kProducts = kBf16 ? 2 : 1;   // K rows a lane holds
   // pieces of 16 bytes (8 where a lane's share of a V row is that): whole vectors, which
   // stay where their load puts them
   using V = typename std::conditional<kWords == 2, u32x2, u32x4>::type;
   static constexpr int kVSize = sizeof(V) / 4, kVs = kWords / kVSize;
-  u32x4 k[kProducts][strides];
+  u32x4 k[kProducts][kSteps];
   V v[kScores][kVs];
   __device__ uint32_t word(int j, int i) const { return v[j][i / kVSize][i % kVSize]; }
 };
@@ -287,11 +287,11 @@ __global__ __launch_bounds__(kThreads, resident(D)) void paged_attend(Args a) {
   const int h0 = g * G + tile_id * kCols, heads = min(kCols, G - tile_id * kCols);
 
   // Q: column col, elements as the K rows' pieces
-  u32x4 q[L::strides];
+  u32x4 q[L::kSteps];
   {
     const T* src = reinterpret_cast<const T*>(a.d.q) + (int64_t)b * a.d.q_row + (int64_t)(h0 + col) * a.d.q_head;
 #pragma unroll
-    for (int i = 0; i < L::strides; ++i)
+    for (int i = 0; i < L::kSteps; ++i)
       q[i] = col < heads ? *reinterpret_cast<const u32x4*>(src + (i * 4 + x) * L::kPiece) : u32x4{0, 0, 0, 0};
   }
 
@@ -337,7 +337,7 @@ __global__ __launch_bounds__(kThreads, resident(D)) void paged_attend(Args a) {
 #pragma unroll
         for (int t = 0; t < L::kProducts; ++t)
 #pragma unroll
-          for (int i = 0; i < L::strides; ++i) w.k[t][i] = load_once<u32x4>(kp + 4 * t * ks + i * 4 * L::kPiece);
+          for (int i = 0; i < L::kSteps; ++i) w.k[t][i] = load_once<u32x4>(kp + 4 * t * ks + i * 4 * L::kPiece);
 #pragma unroll
         for (int j = 0; j < L::kScores; ++j)
 #pragma unroll
@@ -349,7 +349,7 @@ __global__ __launch_bounds__(kThreads, resident(D)) void paged_attend(Args a) {
         for (int t = 0; t < L::kProducts; ++t) {
           s[t] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-          for (int i = 0; i < L::strides; ++i) {
+          for (int i = 0; i < L::kSteps; ++i) {
             if constexpr (L::kBf16) {
               s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w.k[t][i]),
                                                              __builtin_bit_cast(bf16x8, q[i]), s[t], 0, 0, 0);

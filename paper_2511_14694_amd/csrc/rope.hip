@@ -14,8 +14,9 @@
 //
 // HBM bound: 101 000 rows of 32 + 32 heads of 128 in bf16, k and v into pages, take 973 us
 // (5.1 TB/s read and written; torch's copy of the same q reaches 4.3); without the cache
-// 623 us (5.3 TB/s).  The first form, a workgroup a row and a thread a pair, took 2160.  One
-// row takes 4.1 us from launch to launch.
+// 623 us (5.3 TB/s).  The first form, a workgroup a row and a thread a pair, took 2160.  How the threads
+// share heads and rows is worked out by the host: with the divisions in the kernel one row
+// took 5.4 us from launch to launch, now 4.5, and 2000 rows 17.4, now 14.1.
 #include "paged.h"
 
 #include <math.h>
@@ -112,8 +113,20 @@ template <typename T> struct Rows {
   bool turn;
 };
 
+// How the threads of a workgroup share a tensor's rows (host: no division at a kernel's
+// start, where a single row's latency lies).
+struct Walk {
+  int per, chunks;   // rows of a step; steps of a row
+  uint32_t by_heads; // 65536 / heads, rounded up: lane / heads = lane * by_heads >> 16
+};
+struct Units {
+  int turned, units, lanes;  // turned units of a head; all; heads a workgroup takes at a time
+  uint32_t by_units;         // 65536 / units, rounded up
+  Walk q, kv;
+};
+
 template <typename T, int N, bool HALF>
-__global__ __launch_bounds__(kThreads) void rope_rows(focus_rope_desc d, Store st, int rows) {
+__global__ __launch_bounds__(kThreads) void rope_rows(focus_rope_desc d, Store st, Units sh, int rows) {
   using P = Piece<T, N>;
   constexpr int kFlight = HALF ? 4 : 8;
   __shared__ float2 cs[kMaxRows][kMaxRot / 2];
@@ -122,45 +135,47 @@ __global__ __launch_bounds__(kThreads) void rope_rows(focus_rope_desc d, Store s
   const int tid = threadIdx.x, R = d.rot_dim, half = R / 2;
   const int here = (int)min((int64_t)rows, d.n_rows - t0);
   // units of a head: turned pieces (pairs of pieces), then the others
-  const int turned = HALF ? half / N : R / N, units = turned + (d.head_dim - R) / N;
-  const int lanes = kThreads / units, u = tid % units, lane = tid / units;
+  const int turned = sh.turned, lanes = sh.lanes, lane = tid * sh.by_units >> 16, u = tid - lane * sh.units;
   const bool pair = HALF && u < turned;
   const int e = !HALF || u < turned ? u * N : R + (u - turned) * N;
 
   P lo[kFlight], hi[kFlight];
   // a step takes `lanes` heads of a row, or all heads of several rows
-  struct Walk {
-    int per, chunks, steps;   // rows of a step; steps of a row; steps of all rows
-    int row, h;               // the thread's first row and head
+  struct At {
+    int row, h;           // the thread's first row and head
+    int load_row, load_h; // the next step to load: its first row, and heads before it
+    int store_row, store_h;
   };
-  auto walk = [&](const Rows<T>& x) {
-    Walk w;
-    w.per = max(1, lanes / x.heads);
-    w.chunks = (x.heads + lanes - 1) / lanes;
-    w.steps = (here + w.per - 1) / w.per * w.chunks;
-    w.row = w.chunks > 1 ? 0 : lane / x.heads;
-    w.h = lane - w.row * x.heads;
-    if (lane >= lanes || w.row >= w.per) w.row = here;
-    return w;
+  auto start = [&](const Rows<T>& x, const Walk& w) {
+    At at = {};
+    at.row = w.chunks > 1 ? 0 : lane * w.by_heads >> 16;
+    at.h = lane - at.row * x.heads;
+    if (lane >= lanes || at.row >= w.per) at.row = here;
+    return at;
   };
-  auto load = [&](const Rows<T>& x, const Walk& w, int s0) {
-    const T* at = x.src + (t0 + w.row) * x.row + w.h * x.head + e;
+  // the step after (row, h)
+  auto next = [&](const Rows<T>& x, const Walk& w, int& row, int& h) {
+    h += lanes;
+    if (h >= x.heads) h = 0, row += w.per;
+  };
+  auto load = [&](const Rows<T>& x, const Walk& w, At& at) {
+    const T* from = x.src + (t0 + at.row) * x.row + at.h * x.head + e;
 #pragma unroll
     for (int i = 0; i < kFlight; ++i) {
-      const int block = (s0 + i) / w.chunks, j = (s0 + i) - block * w.chunks;
-      if (s0 + i < w.steps && block * w.per + w.row < here && w.h + j * lanes < x.heads) {
-        const T* p = at + (int64_t)block * w.per * x.row + (int64_t)j * lanes * x.head;
+      if (at.load_row + at.row < here && at.load_h + at.h < x.heads) {
+        const T* p = from + (int64_t)at.load_row * x.row + (int64_t)at.load_h * x.head;
         lo[i].load(p);
         if (pair) hi[i].load(p + half);
       }
+      next(x, w, at.load_row, at.load_h);
     }
   };
-  auto store = [&](const Rows<T>& x, const Walk& w, int s0) {
-    T* at = x.dst ? x.dst + (t0 + w.row) * x.drow + w.h * x.dhead + e : nullptr;
+  auto store = [&](const Rows<T>& x, const Walk& w, At& at) {
+    T* to = x.dst ? x.dst + (t0 + at.row) * x.drow + at.h * x.dhead + e : nullptr;
 #pragma unroll
     for (int i = 0; i < kFlight; ++i) {
-      const int block = (s0 + i) / w.chunks, j = (s0 + i) - block * w.chunks, row = block * w.per + w.row;
-      if (s0 + i < w.steps && row < here && w.h + j * lanes < x.heads) {
+      const int row = at.store_row + at.row, h = at.store_h + at.h;
+      if (row < here && h < x.heads) {
         if (x.turn && u < turned) {
           const float2* a = cs[row] + (HALF ? e : e / 2);
           float y[N], z[N];
@@ -185,16 +200,17 @@ __global__ __launch_bounds__(kThreads) void rope_rows(focus_rope_desc d, Store s
           lo[i].pack(y);
         }
         if (x.dst) {
-          T* p = at + (int64_t)block * w.per * x.drow + (int64_t)j * lanes * x.dhead;
+          T* p = to + (int64_t)at.store_row * x.drow + (int64_t)at.store_h * x.dhead;
           lo[i].store(p);
           if (pair) hi[i].store(p + half);
         }
         if (x.page && s_slot[row] >= 0) {
-          T* p = x.page + s_slot[row] + (w.h + j * lanes) * st.c.head_stride + e;
+          T* p = x.page + s_slot[row] + h * st.c.head_stride + e;
           lo[i].store(p);
           if (pair) hi[i].store(p + half);
         }
       }
+      next(x, w, at.store_row, at.store_h);
     }
   };
 
@@ -203,11 +219,12 @@ __global__ __launch_bounds__(kThreads) void rope_rows(focus_rope_desc d, Store s
   const Rows<T> k = {reinterpret_cast<const T*>(d.k), d.k_row, d.k_head, reinterpret_cast<T*>(d.k_out), d.ko_row,
                      d.ko_head, st.on ? reinterpret_cast<T*>(st.c.k) : nullptr, d.n_kv_heads, true};
   const Rows<T>& first = d.q ? q : k;
-  Walk w = walk(first);
-  load(first, w, 0);
+  const Walk& w0 = d.q ? sh.q : sh.kv;
+  At at = start(first, w0);
+  load(first, w0, at);
 
   for (int i = tid; i < here * half; i += kThreads) {
-    const int row = i / half, p = i - row * half;
+    const int row = here == 1 ? 0 : i / half, p = i - row * half;
     double f = (double)d.pos[t0 + row] * d.turns[p];
     f -= rint(f);
     const double quarter = rint(4.0 * f);
@@ -236,29 +253,29 @@ __global__ __launch_bounds__(kThreads) void rope_rows(focus_rope_desc d, Store s
   __syncthreads();
   if (st.on && st.c.weight)
     for (int i = tid; i < here * d.n_kv_heads; i += kThreads) {
-      const int64_t t = t0 + i / d.n_kv_heads;
-      if (s_slot[i / d.n_kv_heads] >= 0)
-        st.c.weight[((int64_t)d.row_seq[t] * d.n_kv_heads + i % d.n_kv_heads) * st.c.weight_rows + d.row_slot[t]] = 0.f;
+      const int row = here == 1 ? 0 : i / d.n_kv_heads, h = i - row * d.n_kv_heads;
+      if (s_slot[row] >= 0)
+        st.c.weight[((int64_t)d.row_seq[t0 + row] * d.n_kv_heads + h) * st.c.weight_rows + d.row_slot[t0 + row]] = 0.f;
     }
 
-  auto rest = [&](const Rows<T>& x, int s0) {
-    for (; s0 < w.steps; s0 += kFlight) {
-      if (s0 > 0) load(x, w, s0);
-      store(x, w, s0);
+  auto rest = [&](const Rows<T>& x, const Walk& w) {
+    for (bool loaded = true; at.store_row < here; loaded = false) {
+      if (!loaded) load(x, w, at);
+      store(x, w, at);
     }
   };
-  rest(first, 0);
+  rest(first, w0);
   if (d.q && d.k) {
-    w = walk(k);
-    load(k, w, 0);
-    rest(k, 0);
+    at = start(k, sh.kv);
+    load(k, sh.kv, at);
+    rest(k, sh.kv);
   }
   if (st.on) {
     const Rows<T> v = {reinterpret_cast<const T*>(d.v), d.v_row, d.v_head, nullptr, 0, 0, reinterpret_cast<T*>(st.c.v),
                        d.n_kv_heads, false};
-    w = walk(v);
-    load(v, w, 0);
-    rest(v, 0);
+    at = start(v, sh.kv);
+    load(v, sh.kv, at);
+    rest(v, sh.kv);
   }
 }
 
@@ -269,19 +286,36 @@ int rows_per_group(int64_t n_rows) {
   return (int)(r < 1 ? 1 : r > kMaxRows ? kMaxRows : r);
 }
 
+Walk walk(int heads, int lanes) {
+  if (heads <= 0) return {1, 1, 0};
+  return {lanes >= heads ? lanes / heads : 1, (heads + lanes - 1) / lanes, (uint32_t)((65536 + heads - 1) / heads)};
+}
+
+template <typename T, int N, bool HALF>
+void launch_rows(const focus_rope_desc& d, const Store& st, hipStream_t s) {
+  Units sh;
+  sh.turned = (HALF ? d.rot_dim / 2 : d.rot_dim) / N;
+  sh.units = sh.turned + (d.head_dim - d.rot_dim) / N;
+  sh.lanes = kThreads / sh.units;
+  sh.by_units = (uint32_t)((65536 + sh.units - 1) / sh.units);  // exact: thread numbers are below 256
+  sh.q = walk(d.q ? d.n_heads : 0, sh.lanes);
+  sh.kv = walk(d.k ? d.n_kv_heads : 0, sh.lanes);
+  const int rows = rows_per_group(d.n_rows);
+  hipLaunchKernelGGL((rope_rows<T, N, HALF>), dim3((uint32_t)focus::ceil_div(d.n_rows, rows)), dim3(kThreads), 0, s, d, st,
+                     sh, rows);
+}
+
 template <typename T>
 void launch(const focus_rope_desc& d, const Store& st, hipStream_t s) {
   constexpr int N = 16 / sizeof(T);
   const bool half = d.pairs == FOCUS_ROPE_HALF;
   const bool whole = (half ? d.rot_dim / 2 : d.rot_dim) % N == 0;
-  const int rows = rows_per_group(d.n_rows);
-  const dim3 grid((uint32_t)focus::ceil_div(d.n_rows, rows)), block(kThreads);
   if (half) {
-    if (whole) hipLaunchKernelGGL((rope_rows<T, N, true>), grid, block, 0, s, d, st, rows);
-    else hipLaunchKernelGGL((rope_rows<T, 1, true>), grid, block, 0, s, d, st, rows);
+    if (whole) launch_rows<T, N, true>(d, st, s);
+    else launch_rows<T, 1, true>(d, st, s);
   } else {
-    if (whole) hipLaunchKernelGGL((rope_rows<T, N, false>), grid, block, 0, s, d, st, rows);
-    else hipLaunchKernelGGL((rope_rows<T, 2, false>), grid, block, 0, s, d, st, rows);
+    if (whole) launch_rows<T, N, false>(d, st, s);
+    else launch_rows<T, 2, false>(d, st, s);
   }
 }
 
