@@ -3,9 +3,11 @@
 //   paged_attend   one workgroup per (chunk of a sequence's rows, one to four KV heads, up
 //                  to 16 query heads of each); writes o and lse where the chunk is the whole
 //                  sequence, else an unnormalised partial (running max, sum, output)
-//   paged_join     merges the partials of a sequence's chunks by log-sum-exp; where
-//                  weights are accumulated, further workgroups turn the scores that
-//                  paged_attend stored into weights of every row
+//   paged_join     merges the partials of a sequence's chunks by log-sum-exp and, where
+//                  weights are accumulated, turns the scores that paged_attend stored into
+//                  weights of every row
+//   paged_plan     before both for more than 128 sequences: the chunks' size and the sequence
+//                  of each; of up to 128, a wave of paged_attend finds its chunk by itself
 //
 // Every cached byte is read once, for all query heads of its KV head, so the kernel is
 // HBM bound as long as the products keep up: they run on the matrix cores at every
@@ -39,31 +41,34 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
 constexpr float kLn2 = 0.69314718055994531f;
 constexpr float kLog2e = 1.44269504088896341f;
-constexpr float kMinit = -1.0e30f;
+constexpr float kMinit = -3.40282347e38f; // the least finite score still counts
 constexpr int kThreads = 256, kWaves = 4;
 constexpr int kMaxGrid = 32768; // workgroups in a grid's second and third dimension
 constexpr int kCols = 16;       // query heads of a workgroup: columns of a product
 constexpr int kPages = 1024;    // page offsets held in LDS at a time
 constexpr int kWhole = 256;     // rows of a table that is not split
+constexpr int kWave = 128;      // sequences whose lengths a wave holds, two a lane
+constexpr int kPlan = 1024;     // threads of paged_plan
 constexpr int kUnit = 128;      // rows of a chunk times KV heads of a workgroup: a multiple of this
 
 // What a lane reads in the place of eight rows that begin past their sequence's end or
 // lie in a page outside the pool.
 __device__ __align__(16) const uint32_t kZeros[256] = {};
 
-// Workspace: int4 info[batch] {first slot, chunks, rows, 0}, then the partials of
-// `slots` chunks: float2 ml[slots][H], float o[slots][H][D], then, where weights are
+// Workspace: int4 info[batch] {first slot, chunks, rows, rows of a chunk}; for more than 64
+// sequences int owner[slots]; then the partials of `slots` chunks: float2 ml[slots][H], float o[slots][H][D], then, where weights are
 // accumulated, float score[batch][H][cap] (log2 units).  None where neither is needed.
 struct Plan {
   int64_t slots;        // upper bound of the chunks of all sequences
   int64_t target;       // chunks resident at a time (split_keys 0)
   int64_t cap;          // rows of a sequence's table
-  int64_t ml, o, score; // byte offsets
+  int64_t owner, ml, o, score; // byte offsets
   size_t bytes;
   int tiles;            // workgroups a KV head's query heads take
   int wide, unit;       // KV heads of a workgroup; chunks are multiples of `unit` rows
   int64_t groups;       // workgroups of a chunk: n_kv_heads / wide * tiles
   bool single;          // a sequence is one chunk
+  bool planned;         // by paged_plan
 };
 
 // Workgroups of paged_attend that a compute unit holds (by their registers).
@@ -81,17 +86,16 @@ Plan make_plan(const focus_paged_decode_desc* d) {
   // head's rows follow one another (5.9) there is nothing to gain.
   p.wide = c.head_stride > c.row_stride ? 1 : c.n_kv_heads % 4 == 0 ? 4 : c.n_kv_heads % 2 == 0 ? 2 : 1;
   // Short tables are not split, so that without weights nothing is left for a second launch;
-  // up to twice as long where their heads alone fill half of the device, and not where they
-  // fill it several times and neighbouring heads are better read together.  us, split / not:
+  // up to twice as long where their heads alone fill half of the device.  With few heads
+  // the waves then share each.  us, split / not:
   //   sequences, KV heads, group     128 rows      256          500          1000
   //     1,  8, 4 (D 128, bf16)      9.2 /  5.8   9.2 /  7.6   9.4 /  9.8  10.0 / 17.8
   //    32,  8, 4                   11.4 /  6.9  15.3 / 10.1  22.4 / 15.5  31.8 / 27.5
   //    32,  4, 16 (f32)            18.8 / 10.2  23.1 / 15.5  30.1 / 26.1  40.9 / 46.7
-  //   128, 32, 1                   54.0 / 73.3  93.1 / 118    170 / 197    329 / 374
   const int64_t heads = (int64_t)c.batch * c.n_kv_heads * p.tiles;
-  p.single = d->split_keys == 0 && ((p.cap <= kWhole && (heads <= 1024 || p.wide == 1)) ||
-                                    (p.cap <= 2 * kWhole && heads >= 128 && heads <= 1024));
-  if (p.single) p.wide = 1;
+  p.single = d->split_keys == 0 && (p.cap <= kWhole || (p.cap <= 2 * kWhole && heads >= 128));
+  if (p.single && heads <= 1024) p.wide = 1;
+  p.planned = !p.single && c.batch > kWave;
   p.unit = kUnit / p.wide;
   p.groups = (int64_t)c.n_kv_heads / p.wide * p.tiles;
   if (p.single) {
@@ -104,7 +108,8 @@ Plan make_plan(const focus_paged_decode_desc* d) {
     p.slots = std::min(c.batch + p.target, c.batch * std::max<int64_t>(1, focus::ceil_div(p.cap, p.unit)));
   }
   const int64_t partials = p.slots * d->n_heads;
-  p.ml = 16 * (int64_t)c.batch;
+  p.owner = 16 * (int64_t)c.batch;
+  p.ml = p.owner + (p.planned ? focus::ceil_div(4 * p.slots, 16) * 16 : 0);
   p.o = p.ml + focus::ceil_div(8 * partials, 16) * 16;
   p.score = p.o + 4 * partials * c.head_dim;
   p.bytes = (size_t)(p.score + (d->accumulate ? 4 * (int64_t)c.batch * d->n_heads * p.cap : 0));
@@ -119,7 +124,10 @@ struct Args {
   int tiles, wide_shift, unit_shift, target;   // wide and unit are powers of two
   int group, parts;     // query heads of a KV head; workgroups of one in the second launch
   int64_t cap;
+  bool single;
+  int64_t slots;
   int4* info;
+  int* owner;           // sequence of each slot (-1: none); null unless planned
   float2* ml;
   float* o;
   float* score;
@@ -138,7 +146,7 @@ __device__ inline float max_column(float x) {
 // least estimate of the time among
 //   the rows of the whole batch spread over `target` chunks, rounded up to units, or over
 //   half as many;
-//   the least size at which the chunks of all sequences are resident at once (up to 64
+//   the least size at which the chunks of all sequences are resident at once (up to kWave
 //   sequences; it needs 16 steps of a search);
 //   no split at all.
 // The estimate, in rows a resident workgroup streams while all of them do: what there is
@@ -159,33 +167,55 @@ __device__ inline float estimate(const Args& a, uint32_t units, int chunks, int 
   return chunks > a.target ? even + alone : fmaxf(even, alone);
 }
 
+// Sum and maximum of f(rows) over the sequences: of a wave, two sequences a lane, or of
+// paged_plan's workgroup.  The results are the same in all threads.
+struct OverWave {
+  int n0, n1;  // rows of the lane's sequences; -1 for none
+  template <typename F> __device__ uint32_t total(F f) const {
+    return (uint32_t)__builtin_amdgcn_readlane(wave_scan((int)(f(n0) + f(n1))), 63);
+  }
+  template <typename F> __device__ uint32_t most(F f) const { return (uint32_t)wave_max((int)max(f(n0), f(n1))); }
+};
+struct OverGroup {
+  const focus_paged_kv& c;
+  int* s_part;  // one per wave
+  template <typename F> __device__ uint32_t total(F f) const {
+    uint32_t x = 0;
+    for (int b = threadIdx.x; b < c.batch; b += kPlan) x += f(focus::paged_length(c, b));
+    return join(wave_scan((int)x), [](int x, int y) { return x + y; });
+  }
+  template <typename F> __device__ uint32_t most(F f) const {
+    uint32_t x = 0;
+    for (int b = threadIdx.x; b < c.batch; b += kPlan) x = max(x, f(focus::paged_length(c, b)));
+    return join(wave_max((int)x), [](int x, int y) { return max(x, y); });
+  }
+  template <typename Op> __device__ uint32_t join(int x, Op op) const {
+    __syncthreads();
+    if (threadIdx.x % 64 == 63) s_part[threadIdx.x / 64] = x;
+    __syncthreads();
+    x = 0;
+#pragma unroll
+    for (int w = 0; w < kPlan / 64; ++w) x = op(x, s_part[w]);
+    return (uint32_t)x;
+  }
+};
+
 // (Counted in units: the host has checked that all tables together hold fewer than 2^31.)
-__device__ int chunk_rows(const Args& a) {
-  const focus_paged_kv& c = a.d.cache;
-  const int lane = threadIdx.x % 64, shift = a.unit_shift, unit = 1 << shift;
+template <typename Over> __device__ int chunk_rows(const Args& a, const Over& over) {
+  const int batch = a.d.cache.batch, shift = a.unit_shift, unit = 1 << shift;
   const uint32_t target = (uint32_t)a.target;
-  auto length = [&](int b) { return b < c.batch ? focus::paged_length(c, b) : -1; };
   // units of a sequence; its chunks of so many units
   auto units_of = [&](int n) { return (uint32_t)(max(n, 0) + unit - 1) >> shift; };
-  auto chunks_of = [&](int n, uint32_t units) { return n < 0 ? 0u : max(1u, (units_of(n) + units - 1) / units); };
-  auto sum = [](uint32_t x) { return (uint32_t)__builtin_amdgcn_readlane(wave_scan((int)x), 63); };
-  uint32_t total = 0;
-  int n = -1;
-  for (int b0 = 0; b0 < c.batch; b0 += 64) {
-    n = length(b0 + lane);
-    total += sum(units_of(n));
-  }
-  if (total + c.batch <= target) return unit;
+  auto chunks = [&](uint32_t units) {
+    return over.total([&](int n) { return n < 0 ? 0u : max(1u, (units_of(n) + units - 1) / units); });
+  };
+  const uint32_t total = over.total(units_of);
+  if (total + batch <= target) return unit;
   const uint32_t one = (total + target - 1) / target, two = min(2 * one, 1u << 30 >> shift);
-  uint32_t count1 = 0, count2 = 0, whole = 1;
-  for (int b0 = 0; b0 < c.batch; b0 += 64) {
-    if (c.batch > 64) n = length(b0 + lane);
-    count1 += sum(chunks_of(n, one));
-    count2 += sum(chunks_of(n, two));
-    whole = max(whole, (uint32_t)wave_max((int)units_of(n)));
-  }
+  const uint32_t whole = max(1u, over.most(units_of));
   if (one >= whole) return (int)(whole << shift);
   const int longest = (int)(whole << shift);
+  const uint32_t count1 = chunks(one), count2 = chunks(two);
   uint32_t units = one;
   float best = estimate(a, total, count1, one << shift, longest);
   auto better = [&](uint32_t count, uint32_t with) {
@@ -193,45 +223,82 @@ __device__ int chunk_rows(const Args& a) {
     if (e < best) best = e, units = with;
   };
   better(count2, two);
-  if (count1 > target && c.batch <= 64 && (uint32_t)c.batch <= target) {
+  if (count1 > target && batch <= kWave && (uint32_t)batch <= target) {
     uint32_t lo = one, hi = whole;  // too many chunks at lo, few enough at hi
     for (int k = 0; k < 16 && hi - lo > 1; ++k) {
       const uint32_t mid = (lo + hi) / 2;
-      if (sum(chunks_of(n, mid)) > target) lo = mid; else hi = mid;
+      const bool many = chunks(mid) > target;
+      lo = many ? mid : lo, hi = many ? hi : mid;
     }
-    better(sum(chunks_of(n, hi)), hi);
+    better(chunks(hi), hi);
   }
-  better(c.batch, whole);
+  better(batch, whole);
   return (int)(units << shift);
 }
 
-// Chunk of the split with index i: every wave finds it by itself from the lengths, 64
-// sequences at a time.
+// The chunk of slot i (chunks 0: none), in scalar registers: all of a wave's lanes ask for
+// the same.
+__device__ inline int scalar(int x) { return __builtin_amdgcn_readfirstlane(x); }
 struct Chunk {
   int b, c, n, slot0, chunks, rows;
 };
-__device__ bool find_chunk(const Args& a, int i, Chunk& out) {
+__device__ __forceinline__ Chunk find_chunk(const Args& a, int i) {
   const focus_paged_kv& c = a.d.cache;
-  const int lane = threadIdx.x % 64;
-  const int rows = __builtin_amdgcn_readfirstlane(a.d.split_keys ? a.d.split_keys : chunk_rows(a));
-  int before = 0;
-  for (int b0 = 0; b0 < c.batch; b0 += 64) {
-    const int n = b0 + lane < c.batch ? focus::paged_length(c, b0 + lane) : 0;
-    const int own = b0 + lane < c.batch ? max(1, (n - 1) / rows + 1) : 0;
-    const int upto = wave_scan(own), all = __builtin_amdgcn_readlane(upto, 63);
-    if (i < before + all) {
-      const int at = __ffsll((unsigned long long)__ballot(i < before + upto)) - 1;
-      out.b = b0 + at;
-      out.n = __builtin_amdgcn_readlane(n, at);
-      out.chunks = __builtin_amdgcn_readlane(own, at);
-      out.slot0 = before + __builtin_amdgcn_readlane(upto, at) - out.chunks;
-      out.c = i - out.slot0;
-      out.rows = rows;
-      return true;
+  int b = 0, n = 0, slot0 = i, chunks = 0, rows = (int)a.cap;
+  if (a.single) {
+    if (i < c.batch) b = i, n = focus::paged_length(c, i), chunks = 1;
+  } else if (a.owner) {
+    const int own = i < a.slots ? scalar(a.owner[i]) : -1;
+    if (own >= 0) {
+      const int4 info = a.info[own];
+      b = own, slot0 = info.x, chunks = info.y, n = info.z, rows = info.w;
     }
-    before += all;
+  } else {
+    const int two = threadIdx.x % 64 * 2;
+    const int n0 = two < c.batch ? focus::paged_length(c, two) : -1;
+    const int n1 = two + 1 < c.batch ? focus::paged_length(c, two + 1) : -1;
+    rows = scalar(a.d.split_keys ? a.d.split_keys : chunk_rows(a, OverWave{n0, n1}));
+    auto chunks_of = [&](int n) { return n < 0 ? 0 : max(1, (n - 1) / rows + 1); };
+    const int own0 = chunks_of(n0), own1 = chunks_of(n1), upto = wave_scan(own0 + own1);
+    if (i < __builtin_amdgcn_readlane(upto, 63)) {
+      const int lane = __ffsll((unsigned long long)__ballot(i < upto)) - 1;
+      const int end = __builtin_amdgcn_readlane(upto, lane), last = __builtin_amdgcn_readlane(own1, lane);
+      const bool second = i >= end - last;
+      b = 2 * lane + second;
+      n = __builtin_amdgcn_readlane(second ? n1 : n0, lane);
+      chunks = __builtin_amdgcn_readlane(second ? own1 : own0, lane);
+      slot0 = end - last - (second ? 0 : chunks);
+    }
   }
-  return false;
+  slot0 = scalar(slot0);
+  return {scalar(b), i - slot0, scalar(n), slot0, scalar(chunks), scalar(rows)};
+}
+
+// The chunks of more than kWave sequences, by one workgroup.  (With every wave going through
+// all lengths by itself 4096 sequences of 200 to 400 rows, 8 KV heads of 128, took 1570 us,
+// now 900; of 128 sequences the launch would cost as much as it saves.)
+__global__ __launch_bounds__(kPlan) void paged_plan(Args a) {
+  __shared__ int s_part[kPlan / 64];
+  const focus_paged_kv& c = a.d.cache;
+  const int tid = threadIdx.x;
+  const int rows = a.d.split_keys ? a.d.split_keys : chunk_rows(a, OverGroup{c, s_part});
+  int before = 0;
+  for (int b0 = 0; b0 < c.batch; b0 += kPlan) {
+    const int b = b0 + tid, n = b < c.batch ? focus::paged_length(c, b) : 0;
+    const int own = b < c.batch ? max(1, (n - 1) / rows + 1) : 0, upto = wave_scan(own);
+    __syncthreads();
+    if (tid % 64 == 63) s_part[tid / 64] = upto;
+    __syncthreads();
+    int slot = before + upto - own;
+#pragma unroll
+    for (int w = 0; w < kPlan / 64; ++w) {
+      if (w < tid / 64) slot += s_part[w];
+      before += s_part[w];
+    }
+    if (b < c.batch) a.info[b] = make_int4(slot, own, n, rows);
+    for (int k = 0; k < own; ++k) a.owner[slot + k] = b;
+  }
+  for (int64_t i = before + tid; i < a.slots; i += kPlan) a.owner[i] = -1;
 }
 
 template <typename T, int D> struct Tile {
@@ -276,14 +343,10 @@ __global__ __launch_bounds__(kThreads, resident(D)) void paged_attend(Args a) {
   const int g0 = (a.tiles == 1 ? blockIdx.x : blockIdx.x / a.tiles) << a.wide_shift;
   // waves of a KV head; this wave's head, and which of its waves it is
   const int by = kWaves >> a.wide_shift, at_head = wave >> (2 - a.wide_shift), g = g0 + at_head, among = wave & (by - 1);
-  Chunk ch;
-  if (!find_chunk(a, blockIdx.z * kMaxGrid + blockIdx.y, ch)) return;
+  const Chunk ch = find_chunk(a, blockIdx.z * kMaxGrid + blockIdx.y);
+  if (ch.chunks == 0) return;
   const int b = ch.b, r0 = ch.c * ch.rows, r1 = min(ch.n, r0 + ch.rows);
   const bool first = g0 == 0 && tile_id == 0;
-  if (first && ch.c == 0 && tid == 0) {
-    if (a.info) a.info[b] = make_int4(ch.slot0, ch.chunks, ch.n, 0);
-    if (ch.n != c.length[b]) focus::raise_err(a.d.err, FOCUS_ERR_CAPACITY);
-  }
   const int h0 = g * G + tile_id * kCols, heads = min(kCols, G - tile_id * kCols);
 
   // Q: column col, elements as the K rows' pieces
@@ -471,6 +534,11 @@ __global__ __launch_bounds__(kThreads, resident(D)) void paged_attend(Args a) {
     if (__syncthreads_or(nan)) pass(std::false_type{});
   }
 
+  // (not at the start, where it would leave b in vector registers during the loops)
+  if (first && ch.c == 0 && tid == 0) {
+    if (a.info && !a.owner) a.info[b] = make_int4(ch.slot0, ch.chunks, ch.n, ch.rows);
+    if (ch.n != c.length[b]) focus::raise_err(a.d.err, FOCUS_ERR_CAPACITY);
+  }
   // the waves' parts of each query head, joined
   l += __shfl_xor(l, 16);
   l += __shfl_xor(l, 32);
@@ -640,12 +708,17 @@ focus_status launch(Args a, const Plan& p, hipStream_t s) {
   // workgroups of a (sequence, KV head) in the second launch: one per query head, or, for
   // weights, per block of the table's rows, but not many more than the device holds
   const int64_t per = focus::ceil_div(std::max<int64_t>(p.cap, 1), kWeightRows), heads = (int64_t)c.batch * c.n_kv_heads;
-  if (a.d.accumulate)
-    a.parts = (int)std::max(std::min(per, focus::ceil_div(8 * focus::device_cus(), heads)), std::min<int64_t>(a.group, 4));
+  const int64_t most = focus::ceil_div(8 * focus::device_cus(), heads);
+  a.parts = (int)std::min(most, a.d.accumulate ? std::max(per, std::min<int64_t>(a.group, 4)) : a.group);
   const int64_t slots = focus::ceil_div(p.slots, kMaxGrid), batches = focus::ceil_div(c.batch, kMaxGrid);
   if (p.groups * p.slots > INT32_MAX / kThreads || heads * a.parts > INT32_MAX / kThreads || slots > kMaxGrid ||
       batches * a.parts > kMaxGrid)
     return FOCUS_E_SHAPE;
+  if (p.planned) {
+    hipLaunchKernelGGL(paged_plan, dim3(1), dim3(kPlan), 0, s, a);
+    const focus_status st = focus::launch_status();
+    if (st != FOCUS_OK) return st;
+  }
   hipLaunchKernelGGL((paged_attend<T, D>),
                      dim3((uint32_t)p.groups, (uint32_t)std::min<int64_t>(p.slots, kMaxGrid), (uint32_t)slots),
                      dim3(kThreads), 0, s, a);
@@ -676,14 +749,20 @@ extern "C" focus_status focus_paged_decode(const focus_paged_decode_desc* d, foc
   if (p.bytes > 0 && (!d->workspace || d->workspace_bytes < p.bytes)) return FOCUS_E_WORKSPACE;
   if (!focus::aligned16(d->workspace)) return FOCUS_E_ARG;
   char* ws = reinterpret_cast<char*>(d->workspace);
-  Args a = {*d, 0.f, focus::page_shift(c), p.tiles, __builtin_ctz((unsigned)p.wide),
-            __builtin_ctz((unsigned)p.unit), (int)p.target, d->n_heads / c.n_kv_heads, d->n_heads / c.n_kv_heads, p.cap, reinterpret_cast<int4*>(ws),
-            reinterpret_cast<float2*>(ws + p.ml), reinterpret_cast<float*>(ws + p.o),
-            reinterpret_cast<float*>(ws + p.score)};
-  if (p.bytes == 0) a.info = nullptr, a.ml = nullptr;
+  Args a = {};
+  a.d = *d;
+  a.shift = focus::page_shift(c);
+  a.tiles = p.tiles, a.wide_shift = __builtin_ctz((unsigned)p.wide), a.unit_shift = __builtin_ctz((unsigned)p.unit);
+  a.target = (int)p.target;
+  a.group = d->n_heads / c.n_kv_heads;
+  a.cap = p.cap, a.single = p.single, a.slots = p.slots;
+  if (p.bytes > 0) {
+    a.info = reinterpret_cast<int4*>(ws), a.ml = reinterpret_cast<float2*>(ws + p.ml);
+    a.o = reinterpret_cast<float*>(ws + p.o), a.score = reinterpret_cast<float*>(ws + p.score);
+  }
+  if (p.planned) a.owner = reinterpret_cast<int*>(ws + p.owner);
   const float scale = d->softmax_scale > 0.f ? d->softmax_scale : 1.0f / sqrtf((float)c.head_dim);
   a.sc = scale * kLog2e;
-  if (p.single) a.d.split_keys = (int)focus::ceil_div(std::max<int64_t>(p.cap, 1), kUnit) * kUnit;
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   if (c.dtype == FOCUS_BF16) return c.head_dim == 128 ? launch<__bf16, 128>(a, p, s) : launch<__bf16, 64>(a, p, s);
   return c.head_dim == 128 ? launch<float, 128>(a, p, s) : launch<float, 64>(a, p, s);

@@ -111,6 +111,49 @@ def test_decode_chunks_chosen(batch, top, H, K, dim, dtype, by_head):
     _check(c, q64, again, dtype, weight=c.weight, decay=1.0)
 
 
+@pytest.mark.parametrize("batch,top,H,K,dim,dtype", [
+    (128, 600, 4, 2, 64, "f32"),         # as many as one wave counts
+    (129, 2000, 8, 1, 128, "bf16"),
+    (1300, 700, 2, 2, 64, "bf16"),       # more than one workgroup's threads
+])
+@pytest.mark.parametrize("split", [0, 256])
+def test_decode_chunks_of_many_sequences(batch, top, H, K, dim, dtype, split):
+    """A few long sequences among many short or empty ones, the longest first and last."""
+    announce(f"paged decode {batch} x {top} {H}/{K} x {dim} {dtype} split {split}")
+    rng = np.random.default_rng(batch + split)
+    lens = [int(x) for x in np.where(rng.random(batch) < 0.05, rng.integers(0, top, batch), rng.integers(0, 40, batch))]
+    lens[0] = lens[-1] = top
+    c = Cache(rng, lens, K, dim, 32, dtype, weight=True)
+    q, q64 = values(rng, (batch, H, dim), dtype)
+    got = F.focus_paged_decode(q, c.dev, split_keys=split)
+    _check(c, q64, got, dtype)
+    again = F.focus_paged_decode(q, c.dev, split_keys=split, weight_decay=0.5)
+    assert torch.equal(again[0], got[0]) and torch.equal(again[1], got[1])
+    _check(c, q64, again, dtype, weight=c.weight, decay=0.5)
+
+
+@pytest.mark.parametrize("rows", [50, 5000])
+def test_decode_scores_far_below_zero(rows):
+    """Scores of -1e31 and less are scores: the highest takes all the weight, alone in its
+    chunk or not (each differs from the next by more than 1e30)."""
+    rng = np.random.default_rng(41)
+    c = Cache(rng, [rows], 1, 64, 64, "f32", weight=True)
+    q = torch.full((1, 2, 64), 1e15, device=DEV)
+    best = rows * 2 // 3
+    order = np.arange(1, rows + 1) + np.where(np.arange(rows) == best, -rows, rows)
+    for r in range(rows):
+        c.k[0][r, 0] = -2e15 * max(int(order[r]), 1)
+    k = torch.as_tensor(c.k[0][:, 0, 0].astype(np.float32)).to(DEV)
+    where = torch.as_tensor(c.table[0][np.arange(rows) // 64].astype(np.int64)).to(DEV)
+    c.dev.k[where, torch.arange(rows, device=DEV) % 64, 0] = k[:, None].expand(rows, 64)
+    o, lse = F.focus_paged_decode(q, c.dev, weight_decay=0.0)
+    assert np.array_equal(to64(o)[0], np.broadcast_to(c.v[0][best], (2, 64)))
+    top = float(k[best]) * 1e15 * 8
+    within(to64(lse)[0], np.full(2, top), abs(top) * 80 * 2.0 ** -24, "lse")
+    w = c.dev.weight.cpu().numpy()[0, 0, :rows]
+    assert w[best] == 2 and np.count_nonzero(w) == 1
+
+
 def test_decode_split_keys_fix_a_sequences_bits():
     """With a given split a sequence's result does not depend on the rest of the batch."""
     rng = np.random.default_rng(40)
