@@ -286,7 +286,7 @@ __global__ __launch_bounds__(kPlan) void paged_plan(Args a) {
   for (int b0 = 0; b0 < c.batch; b0 += kPlan) {
     const int b = b0 + tid, n = b < c.batch ? focus::paged_length(c, b) : 0;
     const int own = b < c.batch ? max(1, (n - 1) / rows + 1) : 0, upto = wave_scan(own);
-    __syncthreads();
+    __syncthreads();  // the last round's sums are read
     if (tid % 64 == 63) s_part[tid / 64] = upto;
     __syncthreads();
     int slot = before + upto - own;
@@ -296,7 +296,7 @@ __global__ __launch_bounds__(kPlan) void paged_plan(Args a) {
       before += s_part[w];
     }
     if (b < c.batch) a.info[b] = make_int4(slot, own, n, rows);
-    for (int k = 0; k < own; ++k) a.owner[slot + k] = b;
+    for (int k = 0; k < own && slot + k < a.slots; ++k) a.owner[slot + k] = b;
   }
   for (int64_t i = before + tid; i < a.slots; i += kPlan) a.owner[i] = -1;
 }

@@ -416,6 +416,7 @@ __global__ __launch_bounds__(kThreads) void evict_part(focus_paged_evict_desc d,
     *bins(part, STEP) = (uint32_t)bin_sum(hist, bin0) | (uint32_t)bin_sum(hist, bin0 + 1) << 16;
   }
 }
+
 // Neighbouring KV heads that a workgroup of evict_copy takes: their rows lie side by side
 // where they go.
 inline __host__ __device__ int heads_together(int n_kv_heads) {
@@ -453,6 +454,13 @@ focus_status validate(const focus_paged_evict_desc* d) {
   return FOCUS_OK;
 }
 
+// Whether two arrays of 4-byte elements have any in common.
+bool overlap(const void* a, int64_t na, const void* b, int64_t nb) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return x < y ? y - x < (uint64_t)na * 4 : x - y < (uint64_t)nb * 4;
+}
+int64_t weights_of(const focus_paged_kv& c) { return (int64_t)c.batch * c.n_kv_heads * c.weight_rows; }
+
 // Rows of a table that one workgroup selects from by itself.
 constexpr int64_t kShortRows = 32 * kThreads;
 
@@ -489,21 +497,22 @@ extern "C" focus_status focus_paged_evict(const focus_paged_evict_desc* d, focus
   if (st != FOCUS_OK) return st;
   if (d->cache.batch == 0) return FOCUS_OK;
   if (!d->cache.weight || (d->keep_rows > 0 && !d->keep)) return FOCUS_E_NULL;
-  if (d->out.weight == d->cache.weight || (reinterpret_cast<uintptr_t>(d->keep) & 3u) ||
-      (reinterpret_cast<uintptr_t>(d->budgets) & 3u))
-    return FOCUS_E_ARG;
+  if ((reinterpret_cast<uintptr_t>(d->keep) & 3u) || (reinterpret_cast<uintptr_t>(d->budgets) & 3u)) return FOCUS_E_ARG;
   const int64_t parts = parts_of(*d), heads = (int64_t)d->cache.batch * d->cache.n_kv_heads;
   const size_t need = focus_paged_evict_workspace(d);
   if (need > 0 && (!d->workspace || d->workspace_bytes < need)) return FOCUS_E_WORKSPACE;
   if (!focus::aligned16(d->workspace)) return FOCUS_E_ARG;
+  // (out.length may be cache.length or budgets, which every head's workgroup reads: it is
+  // set by a later launch then, one entry by the thread that read it)
+  const bool over_length = overlap(d->out.length, d->cache.batch, d->cache.length, d->cache.batch);
+  const bool over_budgets = d->budgets && overlap(d->out.length, d->cache.batch, d->budgets, d->cache.batch);
+  if ((over_length && d->out.length != d->cache.length) || (over_budgets && d->out.length != d->budgets) ||
+      (d->out.weight && overlap(d->out.weight, weights_of(d->out), d->cache.weight, weights_of(d->cache))))
+    return FOCUS_E_ARG;
   if (heads * std::max<int64_t>(parts, 1) > INT32_MAX / kThreads) return FOCUS_E_SHAPE;
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   const int es = (int)focus::elt_bytes(d->cache.dtype), pieces = d->cache.head_dim * es / 16;
-  // (out.length may be cache.length, which every head's workgroup reads: it is set by a
-  // later launch then)
-  const int64_t apart = d->out.length - d->cache.length;
-  const Copy y = {focus::page_shift(d->cache), focus::page_shift(d->out), pieces, es,
-                  apart >= d->cache.batch || -apart >= d->cache.batch};
+  const Copy y = {focus::page_shift(d->cache), focus::page_shift(d->out), pieces, es, !over_length && !over_budgets};
   const dim3 block(kThreads);
   if (parts > 0) {
     const dim3 grid((uint32_t)(heads * parts));
@@ -539,7 +548,7 @@ extern "C" focus_status focus_paged_evict(const focus_paged_evict_desc* d, focus
   const int wide = heads_together(d->cache.n_kv_heads);
   const int64_t blocks = focus::ceil_div(std::max<int64_t>(d->keep_rows, 1), kCopy / (pieces * wide) * 4);
   const dim3 grid((uint32_t)(heads / wide), (uint32_t)std::min<int64_t>(blocks, 4096));
-  if (heads * d->keep_rows * pieces * 64 > (512ll << 20))
+  if ((double)heads * d->keep_rows * pieces * 64 > 512 << 20)
     hipLaunchKernelGGL((evict_copy<true>), grid, dim3(kCopy), 0, s, *d, y);
   else
     hipLaunchKernelGGL((evict_copy<false>), grid, dim3(kCopy), 0, s, *d, y);

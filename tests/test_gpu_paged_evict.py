@@ -185,3 +185,19 @@ def test_evict_captured_and_replayed():
         g.replay()
         torch.cuda.synchronize()
         _check(c, out, [64, 64], 8, keep, old)
+
+
+@pytest.mark.parametrize("n,budget", [(300, 40), (9000, 5000), (40_000, 700)])
+def test_evict_lengths_in_the_place_of_budgets(n, budget):
+    """out.length is the tensor that holds the budgets, of as many sequences as there are
+    heads to run beside each other."""
+    announce(f"evict lengths over budgets {n} -> {budget}")
+    rng = np.random.default_rng(n)
+    lens = [n, 0, n // 2, budget, 7, n]
+    c = Cache(rng, lens, 4, 64, 64, "bf16", weight=True, spare=len(lens) * (budget // 64 + 1))
+    out = c.other(rng, budget)
+    old = c.dev.k.clone(), c.dev.v.clone()
+    budgets = [budget, 3, budget // 2, budget, 0, 1]
+    out.length.copy_(torch.tensor(budgets, dtype=torch.int32))
+    keep = F.focus_paged_evict(c.dev, out, out.length, recent=9)
+    _check(c, out, budgets, 9, keep, old)

@@ -188,6 +188,16 @@ def test_paged_evict_refusals(field, value, status):
     assert _call("focus_paged_evict", d) == status
 
 
+def test_paged_evict_refuses_outputs_over_a_part_of_its_inputs():
+    for field, value in (("out.length", FAKE + 4), ("out.length", FAKE - 4), ("budgets", FAKE + 4), ("budgets", FAKE - 4),
+                         ("out.weight", FAKE + 4 * (2 * 4 * 80 - 1)), ("out.weight", FAKE - 4)):
+        d = _evict_ok()
+        _set(field, value)(d)
+        if field == "budgets":
+            d.cache.length = 2 * FAKE
+        assert _call("focus_paged_evict", d) == E_ARG, (field, value)
+
+
 def test_paged_evict_long_tables_need_a_workspace():
     d = _evict_ok()
     assert _abi.lib().focus_paged_evict_workspace(C.byref(d)) == 0
