@@ -21,9 +21,12 @@
 
 #include <math.h>
 
+#include <type_traits>
+
 namespace {
 
 using focus::u32x4;
+using u32x2 = uint32_t __attribute__((ext_vector_type(2)));
 
 constexpr int kThreads = 256;
 constexpr int kMaxRot = 256;
@@ -55,47 +58,41 @@ __device__ int64_t slot_of(const focus_rope_desc& d, const Store& st, int64_t t,
   return focus::row_at(st.c, p, slot, 0);
 }
 
-// N elements of a head in registers: one 16-byte access, or (heads whose turned part
-// is not whole pieces) element by element.
+// N elements of a head in registers: one access of 4, 8 or 16 bytes (as wide as a head's
+// turned part is whole pieces of), or a single bf16.
 template <typename T, int N> struct Piece {
-  static constexpr bool kWhole = N * sizeof(T) == 16;
-  static constexpr int kWords = kWhole ? 4 : N;
-  uint32_t w[kWords];
+  static constexpr bool kHalfWord = N * sizeof(T) == 2;
+  static constexpr int kWords = kHalfWord ? 1 : N * sizeof(T) / 4;
+  using V = typename std::conditional<kWords == 4, u32x4, typename std::conditional<kWords == 2, u32x2, uint32_t>::type>::type;
+  V w;
+  __device__ uint32_t word(int i) const {
+    if constexpr (kWords == 1) return w;
+    else return w[i];
+  }
+  __device__ void set(int i, uint32_t x) {
+    if constexpr (kWords == 1) w = x;
+    else w[i] = x;
+  }
   __device__ void load(const T* p) {
-    if constexpr (kWhole) {
-      const u32x4 x = *reinterpret_cast<const u32x4*>(p);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) w[i] = x[i];
-    } else {
-#pragma unroll
-      for (int i = 0; i < N; ++i) w[i] = __float_as_uint((float)p[i]);
-    }
+    if constexpr (kHalfWord) w = *reinterpret_cast<const uint16_t*>(p);
+    else w = *reinterpret_cast<const V*>(p);
   }
   __device__ void store(T* p) const {
-    if constexpr (kWhole) {
-      *reinterpret_cast<u32x4*>(p) = u32x4{w[0], w[1], w[2], w[3]};
-    } else {
-#pragma unroll
-      for (int i = 0; i < N; ++i) p[i] = (T)__uint_as_float(w[i]);
-    }
+    if constexpr (kHalfWord) *reinterpret_cast<uint16_t*>(p) = (uint16_t)w;
+    else *reinterpret_cast<V*>(p) = w;
   }
   __device__ void unpack(float (&x)[N]) const {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      if constexpr (kWhole && sizeof(T) == 2)
-        x[i] = i % 2 ? focus::bf16_hi(w[i / 2]) : focus::bf16_lo(w[i / 2]);
-      else
-        x[i] = __uint_as_float(w[i]);
+      if constexpr (sizeof(T) == 2) x[i] = i % 2 ? focus::bf16_hi(word(i / 2)) : focus::bf16_lo(word(i / 2));
+      else x[i] = __uint_as_float(word(i));
     }
   }
   __device__ void pack(const float (&x)[N]) {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      if constexpr (kWhole && sizeof(T) == 2) {
-        if (i % 2 == 0) w[i / 2] = focus::pack_bf16x2(x[i], x[i + 1]);
-      } else {
-        w[i] = __float_as_uint(x[i]);
-      }
+      if constexpr (sizeof(T) == 4) set(i, __float_as_uint(x[i]));
+      else if (i % 2 == 0) set(i / 2, focus::pack_bf16x2(x[i], i + 1 < N ? x[i + 1] : 0.f));
     }
   }
 };
@@ -128,7 +125,7 @@ struct Units {
 template <typename T, int N, bool HALF>
 __global__ __launch_bounds__(kThreads) void rope_rows(focus_rope_desc d, Store st, Units sh, int rows) {
   using P = Piece<T, N>;
-  constexpr int kFlight = HALF ? 4 : 8;
+  constexpr int kFlight = HALF && P::kWords == 4 ? 4 : 8;
   __shared__ float2 cs[kMaxRows][kMaxRot / 2];
   __shared__ int64_t s_slot[kMaxRows];
   const int64_t t0 = (int64_t)blockIdx.x * rows;
@@ -305,16 +302,19 @@ void launch_rows(const focus_rope_desc& d, const Store& st, hipStream_t s) {
                      sh, rows);
 }
 
+// The widest pieces that the turned part is whole ones of.  9000 rows of 64 + 8 heads of 80
+// elements in bf16, 40 of them turned in halves: pieces of 8 bytes 39 us, single elements
+// 92.  (float32 gains nothing by 8 bytes over 4: 20 000 rows of 24 heads of 128, 136 and 130.)
 template <typename T>
 void launch(const focus_rope_desc& d, const Store& st, hipStream_t s) {
   constexpr int N = 16 / sizeof(T);
-  const bool half = d.pairs == FOCUS_ROPE_HALF;
-  const bool whole = (half ? d.rot_dim / 2 : d.rot_dim) % N == 0;
-  if (half) {
-    if (whole) launch_rows<T, N, true>(d, st, s);
+  const int part = d.pairs == FOCUS_ROPE_HALF ? d.rot_dim / 2 : d.rot_dim;
+  if (d.pairs == FOCUS_ROPE_HALF) {
+    if (part % N == 0) launch_rows<T, N, true>(d, st, s);
+    else if (sizeof(T) == 2 && part % 4 == 0) launch_rows<T, 4, true>(d, st, s);
     else launch_rows<T, 1, true>(d, st, s);
   } else {
-    if (whole) launch_rows<T, N, false>(d, st, s);
+    if (part % N == 0) launch_rows<T, N, false>(d, st, s);
     else launch_rows<T, 2, false>(d, st, s);
   }
 }

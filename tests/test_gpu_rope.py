@@ -113,6 +113,23 @@ def test_rope_values_that_are_not_finite_stay_in_their_pair():
     assert torch.equal(got[~hit], clean[~hit]) and not torch.isfinite(got[hit]).any()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("pairs", ["half", "interleaved"])
+@pytest.mark.parametrize("rot", [0, 2, 12, 20, 24, 32, 40])
+def test_rope_elements_that_do_not_turn_keep_their_bits(rot, pairs, dtype):
+    """Any bits at all, NaN with payloads among them; every width of piece."""
+    announce(f"rope bits {rot} {pairs} {dtype}")
+    rng = np.random.default_rng(rot)
+    kind = np.uint16 if dtype == "bf16" else np.uint32
+    bits = rng.integers(0, 1 << 8 * np.dtype(kind).itemsize, (77, 3, 64)).astype(kind)
+    q = torch.as_tensor(bits.view(np.int16 if dtype == "bf16" else np.int32)).to(DEV).view(torch_dtype(dtype))
+    pos = torch.arange(77, dtype=torch.int32, device=DEV)
+    turns = F.focus_rope_turns(rot) if rot else None
+    got, _ = F.focus_rope(pos, turns, q, layout=PAIRS[pairs])
+    got = got.view(torch.int16 if dtype == "bf16" else torch.int32).cpu().numpy().view(kind)
+    assert np.array_equal(got[..., rot:], bits[..., rot:])
+
+
 def test_rope_gradient_against_differences():
     """The inverse call is the gradient of sum(g * rope(x)): against the formula's own
     differences in float64 (the map is linear, so a difference of any width is exact)."""
