@@ -1,7 +1,7 @@
 // A paged K/V cache cut down to a budget by accumulated weight (focus_paged_evict).
 //
 // The weight of the last row kept is found by a radix selection over an order-preserving
-// integer of the weights, in digits of 11, 11 and 10 bits: a histogram of a digit among
+// integer of the weights, in digits of 11, 11 and 10 bits (8 for short tables): a histogram of a digit among
 // the rows that share the digits above says in which bucket the row lies and how many of
 // it are still wanted.  Then the rows above that weight and the first of those that equal
 // it are written in order; a wave holds consecutive rows, so one prefix sum over the
@@ -10,21 +10,37 @@
 //   evict_select  tables of up to 32 768 rows: one workgroup per (sequence, KV head), the
 //                 weights in registers throughout; where a head's rows are few, or heads
 //                 enough to fill the device, it copies them as well
-//   evict_count   longer tables: a workgroup per 8 192 rows, one launch a digit, each
-//                 adding up the histograms of the digit before
-//   evict_keep    and the rows kept; what a workgroup's rows add to the ones before it
-//                 follows from the same histograms
+//   evict_part    longer tables: a workgroup per 8 192 rows, one launch a digit, each
+//                 adding up the histograms of the digit before, and a last one that writes
+//                 the rows kept; what a workgroup's rows add to the ones before it follows
+//                 from the same histograms
 //   evict_copy    the kept rows and their weights to the pages of `out`
 //
-// The copy is HBM bound; the selection by the latency of its passes.
+// The copy is HBM bound, the selection bound by the latency of its passes: 16 x 8 heads of
+// 10 000 rows cut to 5 000 take 145 us, 12 of them the selection; 8 heads of 131 072 rows
+// cut to 32 768 take 84 us, 25 of them the selection.  The first form (one workgroup a head,
+// four digits of eight bits, the weights read for each) took 180 and 394.
 #include "paged.h"
 
 #include <algorithm>
 
 namespace {
 
-constexpr int kThreads = 1024, kWaves = kThreads / 64;
 constexpr int kCopy = 256;
+constexpr int kCopies = 4;  // of a histogram in LDS, lane by lane: [bin][copy]
+
+// A workgroup's threads, and the digits (the uppermost first) it takes a weight's integer in.
+template <int THREADS, int BITS> struct Form {
+  static constexpr int kThreads = THREADS, kWaves = THREADS / 64, kBins = 1 << BITS, kDigits = (31 + BITS) / BITS;
+  static constexpr int kPer = kBins / THREADS;  // bins a thread sums
+  static_assert(kPer >= 1 && kPer <= 2, "one or two bins a thread");
+  static constexpr __device__ int shift(int i) { return i == kDigits - 1 ? 0 : 32 - BITS * (i + 1); }
+  static constexpr __device__ uint32_t mask(int i) { return i == kDigits - 1 ? (1u << (32 - BITS * i)) - 1 : kBins - 1u; }
+  // the digits above digit i
+  static constexpr __device__ uint32_t above(int i) { return i == 0 ? 0u : 0xffffffffu << shift(i - 1); }
+};
+using Wide = Form<1024, 11>;
+using Small = Form<256, 8>;
 
 // Weights as integers of the same order; -0 counts as +0, every NaN as the greatest.
 __device__ inline uint32_t order_of(float w) {
@@ -44,14 +60,14 @@ __device__ inline int kept_rows(const focus_paged_evict_desc& d, int b, int n, i
 }
 
 // Exclusive prefix sum of x over the workgroup; *total: the sum.
-__device__ inline int scan(int x, int* waves, int* total) {
+template <typename F> __device__ inline int scan(int x, int* waves, int* total) {
   const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   const int y = focus::wave_scan(x);
   __syncthreads();
   if (lane == 63) waves[wave] = y;
   __syncthreads();
-  const int sums = focus::wave_scan(lane < kWaves ? waves[lane] : 0);
-  *total = __builtin_amdgcn_readlane(sums, kWaves - 1);
+  const int sums = focus::wave_scan(lane < F::kWaves ? waves[lane] : 0);
+  *total = __builtin_amdgcn_readlane(sums, F::kWaves - 1);
   return (wave ? __builtin_amdgcn_readlane(sums, wave - 1) : 0) + y - x;
 }
 
@@ -59,13 +75,6 @@ __device__ inline int scan(int x, int* waves, int* total) {
 __device__ inline int lanes_below(uint64_t mask) {
   return __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0));
 }
-
-constexpr int kDigits = 3, kBins = 2048;
-constexpr int kCopies = 4;  // of a histogram in LDS, lane by lane: [bin][copy]
-__device__ constexpr int digit_shift(int i) { return i == 0 ? 21 : i == 1 ? 10 : 0; }
-__device__ constexpr uint32_t digit_mask(int i) { return i == 2 ? 1023u : 2047u; }
-// the digits above digit i
-__device__ constexpr uint32_t above_mask(int i) { return i == 0 ? 0u : 0xffffffffu << digit_shift(i - 1); }
 
 // What a workgroup knows of one (sequence, KV head).
 struct Head {
@@ -103,8 +112,6 @@ __device__ void order_keys(const Head& h, const float (&x)[NR], int row0, int us
 #pragma unroll
   for (int i = 0; i < NR; ++i) key[i] = i < used && row0 + 64 * i < h.old ? order_of(x[i]) : 0u;
 }
-// Registers a thread needs for this many rows.
-__device__ inline int used_for(int rows) { return (rows + kThreads - 1) / kThreads; }
 
 // Histogram of a digit among the rows that share the digits above it, added to hist
 // (cleared by the caller; of digit 0, bucket 0 holds rows that are none, which no choice
@@ -113,10 +120,10 @@ __device__ inline int used_for(int rows) { return (rows + kThreads - 1) / kThrea
 // of 10 000 rows, 64 of them kept, the whole call, with weights all different / all equal:
 // one copy 23.9 / 46.9 us, four 21.3 / 26.2, eight 22.0 / 24.2; lanes that share a bucket
 // counted at once where they are many, one copy, 24.8 / 27.5.
-template <int NR>
+template <typename F, int NR>
 __device__ void count_digit(const uint32_t (&key)[NR], int used, int digit, uint32_t prefix, int* hist) {
-  const uint32_t mask = above_mask(digit), dm = digit_mask(digit);
-  const int shift = digit_shift(digit);
+  const uint32_t mask = F::above(digit), dm = F::mask(digit);
+  const int shift = F::shift(digit);
 #pragma unroll
   for (int i = 0; i < NR; ++i) {
     if (i < used && (key[i] & mask) == prefix)
@@ -125,8 +132,8 @@ __device__ void count_digit(const uint32_t (&key)[NR], int used, int digit, uint
 }
 
 // Clears the copies of a histogram; sums those of a bin.
-__device__ inline void clear_hist(int* hist) {
-  for (int i = threadIdx.x; i < kBins * kCopies / 4; i += kThreads) reinterpret_cast<int4*>(hist)[i] = make_int4(0, 0, 0, 0);
+template <typename F> __device__ inline void clear_hist(int* hist) {
+  for (int i = threadIdx.x; i < F::kBins * kCopies / 4; i += F::kThreads) reinterpret_cast<int4*>(hist)[i] = make_int4(0, 0, 0, 0);
 }
 __device__ inline int bin_sum(const int* hist, int bin) {
   int sum = 0;
@@ -149,25 +156,24 @@ struct Level {
 // at least so many rows; c: this thread's bins, kBins - 1 - kPer tid downwards), in every
 // thread: the level with that digit.  Where the whole bucket stays, no further digit is
 // needed: its rows are the ones above a level.
-constexpr int kPer = kBins / kThreads;
-static_assert(kPer == 2, "two bins a thread");
-__device__ int next_level(const int (&c)[kPer], int digit, int* waves, int* found, Level& x) {
+template <typename F>
+__device__ int next_level(const int (&c)[F::kPer], int digit, int* waves, int* found, Level& x) {
   const int tid = threadIdx.x;
   int sum = 0;
 #pragma unroll
-  for (int i = 0; i < kPer; ++i) sum += c[i];
-  int total, above = scan(sum, waves, &total);
+  for (int i = 0; i < F::kPer; ++i) sum += c[i];
+  int total, above = scan<F>(sum, waves, &total);
 #pragma unroll
-  for (int i = 0; i < kPer; ++i) {
+  for (int i = 0; i < F::kPer; ++i) {
     if (above < x.equal && above + c[i] >= x.equal)
-      found[0] = kBins - 1 - (tid * kPer + i), found[1] = x.equal - above, found[2] = c[i];
+      found[0] = F::kBins - 1 - (tid * F::kPer + i), found[1] = x.equal - above, found[2] = c[i];
     above += c[i];
   }
   __syncthreads();
   const int bucket = found[0];
-  x.level |= (uint32_t)bucket << digit_shift(digit);
+  x.level |= (uint32_t)bucket << F::shift(digit);
   x.equal = found[1];
-  if (digit < kDigits - 1 && x.equal == found[2]) {
+  if (digit < F::kDigits - 1 && x.equal == found[2]) {
     x.level -= 1;  // (no weight's integer is 0)
     x.equal = 0, x.done = 1;
   }
@@ -178,7 +184,7 @@ __device__ int next_level(const int (&c)[kPer], int digit, int* waves, int* foun
 // Write the rows above `level` (> 0) and, of those equal to it, the ones that number less
 // than `equal`; before this workgroup's rows come before_above above it and before_equal
 // equal to it.
-template <int NR>
+template <typename F, int NR>
 __device__ void write_rows(const Head& h, const uint32_t (&key)[NR], int used, int row0, uint32_t level, int equal, int before_above,
                            int before_equal, int (*waves)[2]) {
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
@@ -194,8 +200,8 @@ __device__ void write_rows(const Head& h, const uint32_t (&key)[NR], int used, i
   __syncthreads();
   above = before_above, ties = before_equal;
   const int lane = threadIdx.x % 64;
-  const int sum_above = focus::wave_scan(lane < kWaves ? waves[lane][0] : 0);
-  const int sum_ties = focus::wave_scan(lane < kWaves ? waves[lane][1] : 0);
+  const int sum_above = focus::wave_scan(lane < F::kWaves ? waves[lane][0] : 0);
+  const int sum_ties = focus::wave_scan(lane < F::kWaves ? waves[lane][1] : 0);
   if (wave) above += __builtin_amdgcn_readlane(sum_above, wave - 1), ties += __builtin_amdgcn_readlane(sum_ties, wave - 1);
 #pragma unroll
   for (int i = 0; i < NR; ++i) {
@@ -213,10 +219,11 @@ __device__ void write_rows(const Head& h, const uint32_t (&key)[NR], int used, i
 }
 
 // The recent rows, and -1 past the rows kept; by `groups` workgroups of which this is `at`.
+template <typename F>
 __device__ void write_rest(const focus_paged_evict_desc& d, const Head& h, int at, int groups) {
-  const int step = groups * kThreads;
-  for (int j = at * kThreads + threadIdx.x; j < h.recent; j += step) h.keep[h.take + j] = h.old + j;
-  for (int64_t j = h.take + h.recent + at * kThreads + threadIdx.x; j < d.keep_rows; j += step) h.keep[j] = -1;
+  const int step = groups * F::kThreads;
+  for (int j = at * F::kThreads + threadIdx.x; j < h.recent; j += step) h.keep[h.take + j] = h.old + j;
+  for (int64_t j = h.take + h.recent + at * F::kThreads + threadIdx.x; j < d.keep_rows; j += step) h.keep[j] = -1;
 }
 
 struct Copy {
@@ -288,10 +295,10 @@ __device__ void set_length(const focus_paged_evict_desc& d, int b) {
   d.out.length[b] = kept_rows(d, b, focus::paged_length(d.cache, b), &bits);
 }
 
-template <int NR, bool COPY>
-__global__ __launch_bounds__(kThreads) void evict_select(focus_paged_evict_desc d, Copy y) {
-  __shared__ __align__(16) int hist[kBins * kCopies];
-  __shared__ int waves[kWaves], found[3], parts[kWaves][2];
+template <typename F, int NR, bool COPY>
+__global__ __launch_bounds__(F::kThreads) void evict_select(focus_paged_evict_desc d, Copy y) {
+  __shared__ __align__(16) int hist[F::kBins * kCopies];
+  __shared__ int waves[F::kWaves], found[3], parts[F::kWaves][2];
   // few weights are read at once, up to the table's end, before the length is known
   const int64_t cap = (int64_t)d.cache.max_pages * d.cache.page_rows;
   float w[NR];
@@ -302,34 +309,35 @@ __global__ __launch_bounds__(kThreads) void evict_select(focus_paged_evict_desc 
   if (h.take > 0) {
     uint32_t key[NR];
     if constexpr (NR > 4) {
-      used = used_for(h.old);  // all waves alike
+      used = (h.old + F::kThreads - 1) / F::kThreads;  // all waves alike
       load_keys<NR>(h.w, h.old, 0, used, w, row0);
     }
     order_keys<NR>(h, w, row0, used, key);
     Level x = {0, h.take, 0};
-    for (int digit = 0; digit < kDigits && !x.done; ++digit) {
-      clear_hist(hist);
+    for (int digit = 0; digit < F::kDigits && !x.done; ++digit) {
+      clear_hist<F>(hist);
       __syncthreads();
-      count_digit<NR>(key, used, digit, x.level, hist);
+      count_digit<F, NR>(key, used, digit, x.level, hist);
       __syncthreads();
-      int c[kPer];
+      int c[F::kPer];
 #pragma unroll
-      for (int i = 0; i < kPer; ++i) c[i] = bin_sum(hist, kBins - 1 - (kPer * (int)threadIdx.x + i));
-      next_level(c, digit, waves, found, x);
+      for (int i = 0; i < F::kPer; ++i) c[i] = bin_sum(hist, F::kBins - 1 - (F::kPer * (int)threadIdx.x + i));
+      next_level<F>(c, digit, waves, found, x);
     }
-    write_rows<NR>(h, key, used, row0, x.level, x.equal, 0, 0, parts);
+    write_rows<F, NR>(h, key, used, row0, x.level, x.equal, 0, 0, parts);
   }
-  write_rest(d, h, 0, 1);
+  write_rest<F>(d, h, 0, 1);
   if constexpr (COPY) {
     if (y.lengths && h.g == 0 && threadIdx.x == 0) d.out.length[h.b] = h.take + h.recent;
     __syncthreads();  // the kept rows are this workgroup's own
-    const int per = kThreads / y.pieces;
+    const int per = F::kThreads / y.pieces;
     if ((int)threadIdx.x < per * y.pieces)
       copy_rows<false>(d, y, h.b, h.g, threadIdx.x / y.pieces, per, h.take + h.recent, threadIdx.x % y.pieces);
   }
 }
 
 constexpr int kLongRows = 8;                   // registers of rows of the long form
+constexpr int kThreads = Wide::kThreads, kWaves = Wide::kWaves, kBins = Wide::kBins, kDigits = Wide::kDigits, kPer = Wide::kPer;
 constexpr int kPart = kThreads * kLongRows;    // rows of a workgroup there
 
 // The long form's workspace: per head the level so far, per part the rows above it in the
@@ -349,7 +357,7 @@ __global__ __launch_bounds__(kThreads) void evict_part(focus_paged_evict_desc d,
   __shared__ int waves[kWaves], found[3], pair[kWaves][2];
   const int bg = blockIdx.x / y.parts, part = blockIdx.x % y.parts, tid = threadIdx.x;
   const Head h = head_of(d, bg, STEP == 0 && part == 0);
-  if (STEP == kDigits) write_rest(d, h, part, y.parts);
+  if (STEP == kDigits) write_rest<Wide>(d, h, part, y.parts);
   const int live = (h.old + kPart - 1) / kPart;  // parts that hold rows
   if (h.take == 0 || part >= live) return;
   // a digit's histogram of a part, two bins a thread, the first thread's the last ones
@@ -390,14 +398,14 @@ __global__ __launch_bounds__(kThreads) void evict_part(focus_paged_evict_desc d,
         }
       }
       const int c[kPer] = {hi, lo};
-      const int bucket = next_level(c, STEP - 1, waves, found, x);
+      const int bucket = next_level<Wide>(c, STEP - 1, waves, found, x);
       const int own = bin0 == bucket ? lo_b : bin0 + 1 == bucket ? hi_b : 0;
       const int up = (bin0 > bucket ? lo_b : 0) + (bin0 + 1 > bucket ? hi_b : 0);
       int total;
-      scan(up + (x.done ? own : 0), waves, &total);
+      scan<Wide>(up + (x.done ? own : 0), waves, &total);
       before += total;
       if constexpr (STEP == kDigits) {
-        scan(own, waves, &total);
+        scan<Wide>(own, waves, &total);
         before_equal = total;
       } else if (tid == 0) {
         y.before[(int64_t)bg * y.parts + part] = before;
@@ -406,12 +414,12 @@ __global__ __launch_bounds__(kThreads) void evict_part(focus_paged_evict_desc d,
     }
   }
   if constexpr (STEP == kDigits) {
-    write_rows<kLongRows>(h, key, kLongRows, row0, x.level, x.equal, before, before_equal, pair);
+    write_rows<Wide, kLongRows>(h, key, kLongRows, row0, x.level, x.equal, before, before_equal, pair);
   } else {
     if (x.done) return;
-    clear_hist(hist);
+    clear_hist<Wide>(hist);
     __syncthreads();
-    count_digit<kLongRows>(key, kLongRows, STEP, x.level, hist);
+    count_digit<Wide, kLongRows>(key, kLongRows, STEP, x.level, hist);
     __syncthreads();
     *bins(part, STEP) = (uint32_t)bin_sum(hist, bin0) | (uint32_t)bin_sum(hist, bin0 + 1) << 16;
   }
@@ -532,10 +540,20 @@ extern "C" focus_status focus_paged_evict(const focus_paged_evict_desc* d, focus
     const bool copies = bytes <= (256 << 10) || (bytes <= (512 << 10) && heads >= 2 * focus::device_cus());
     const dim3 grid((uint32_t)heads);
     const int64_t cap = (int64_t)d->cache.max_pages * d->cache.page_rows;
-#define FOCUS_SELECT(NR)                                                              \
-  if (copies) hipLaunchKernelGGL((evict_select<NR, true>), grid, block, 0, s, *d, y); \
-  else hipLaunchKernelGGL((evict_select<NR, false>), grid, block, 0, s, *d, y);
-    if (cap <= 4 * kThreads) { FOCUS_SELECT(4) } else if (cap <= 16 * kThreads) { FOCUS_SELECT(16) } else { FOCUS_SELECT(32) }
+#define FOCUS_SELECT(F, NR)                                                                            \
+  if (copies) hipLaunchKernelGGL((evict_select<F, NR, true>), grid, dim3(F::kThreads), 0, s, *d, y);  \
+  else hipLaunchKernelGGL((evict_select<F, NR, false>), grid, dim3(F::kThreads), 0, s, *d, y);
+    // More heads than compute units go through several of them at a time, by workgroups of
+    // 256 threads, whose passes cost less: 1024 x 8 heads of 300 rows, 100 kept, 186 us,
+    // with 1024 threads 321; 64 x 8 of 1000, 250 kept, 27 and 34; 512 x 4 of 4000, 200 kept,
+    // 53 and 77.  Fewer heads have a compute unit each, and its threads copy as well: 16 x 8
+    // of 900, 256 kept, 16.9 and 14.5.
+    const bool small = heads > focus::device_cus();
+    if (small && cap <= 4 * Small::kThreads) { FOCUS_SELECT(Small, 4) }
+    else if (small && cap <= 16 * Small::kThreads) { FOCUS_SELECT(Small, 16) }
+    else if (cap <= 4 * Wide::kThreads) { FOCUS_SELECT(Wide, 4) }
+    else if (cap <= 16 * Wide::kThreads) { FOCUS_SELECT(Wide, 16) }
+    else { FOCUS_SELECT(Wide, 32) }
 #undef FOCUS_SELECT
     if (copies) {
       if ((st = focus::launch_status()) != FOCUS_OK || y.lengths) return st;

@@ -201,3 +201,19 @@ def test_evict_lengths_in_the_place_of_budgets(n, budget):
     out.length.copy_(torch.tensor(budgets, dtype=torch.int32))
     keep = F.focus_paged_evict(c.dev, out, out.length, recent=9)
     _check(c, out, budgets, 9, keep, old)
+
+
+@pytest.mark.parametrize("batch,top,K,D,budget", [(40, 1000, 8, 64, 100), (70, 130, 4, 128, 130), (300, 60, 1, 64, 7),
+                                                  (75, 4000, 4, 64, 600)])
+@pytest.mark.parametrize("kind", ["skewed", "ties", "equal", "special"])
+def test_evict_many_heads(batch, top, K, D, budget, kind):
+    """More heads than the device has compute units, of every length up to top."""
+    announce(f"evict {batch} x {top} x {K} x {D} budget {budget} {kind}")
+    rng = np.random.default_rng(batch)
+    lens = [top, 0, 1] + [int(x) for x in rng.integers(0, top + 1, batch - 3)]
+    c = Cache(rng, lens, K, D, 64, "bf16", weight=True, spare=batch * -(-budget // 64))
+    c.dev.weight.copy_(torch.as_tensor(_weights(rng, c.weight.shape, kind)))
+    out = c.other(rng, budget)
+    old = c.dev.k.clone(), c.dev.v.clone()
+    keep = F.focus_paged_evict(c.dev, out, budget, recent=5)
+    _check(c, out, [budget] * batch, 5, keep, old)
