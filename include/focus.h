@@ -820,8 +820,8 @@ typedef struct {
  * holds a float32 for every query head and row of the tables.  The workspace is in use
  * until the call's kernels end; calls that share one on overlapping streams race. */
 size_t focus_paged_decode_workspace(const focus_paged_decode_desc* d);
-/* Errors: E_NULL, E_ARG, E_DTYPE, E_SHAPE (batch * max_pages * page_rows of 2^36 or
- * batch * n_heads of 2^23 among others), E_UNSUPPORTED, E_WORKSPACE, E_HIP.  Rows of a
+/* Errors: E_NULL, E_ARG, E_DTYPE, E_SHAPE (batch * max_pages * page_rows of 2^36,
+ * batch * n_heads of 2^23, more than 512 query heads of a KV head, among others), E_UNSUPPORTED, E_WORKSPACE, E_HIP.  Rows of a
  * page outside the pool are left out of the softmax (FOCUS_ERR_BOUNDS; weight of the step
  * 0); a length outside [0, max_pages * page_rows] is clipped to it (FOCUS_ERR_CAPACITY). */
 focus_status focus_paged_decode(const focus_paged_decode_desc* d, focus_stream_t stream);

@@ -593,16 +593,19 @@ __device__ float2 joined(const Args& a, const int4& info, int h) {
 }
 
 constexpr int kWeightRows = 4 * kThreads;   // rows whose weights a workgroup writes at a time
+constexpr int kMaxGroup = 512;              // query heads of a KV head
 
 // One of `parts` workgroups of a (sequence, KV head): merges the partials of every
 // parts-th of its query heads (D / 4 threads over the output, the other groups of them
-// over the chunks, eight loads in flight each, the first of them before the maximum is
-// known) and, where weights are accumulated, writes those of every parts-th block of rows.
+// over the chunks, eight loads in flight each) and, where weights are accumulated, writes
+// those of every parts-th block of rows.  Maxima and sums come first, a wave a head; the
+// first partials, scores and old weights are in flight meanwhile.
 template <typename T, int D>
 __global__ __launch_bounds__(kThreads) void paged_join(Args a) {
-  constexpr int kLanes = D / 4, kGroups = kThreads / kLanes, kFlight = 8;
+  constexpr int kLanes = D / 4, kGroups = kThreads / kLanes, kFlight = 8, kHeads = 2;
   __shared__ float4 s_o[kGroups][kLanes];
-  __shared__ float s_lse[kThreads];
+  __shared__ float2 s_ml[kMaxGroup];  // a head's maximum and sum
+  __shared__ float s_lse[kMaxGroup];
   const focus_paged_kv& c = a.d.cache;
   const int K = c.n_kv_heads, H = a.d.n_heads, G = a.group, tid = threadIdx.x, parts = a.parts;
   // (part 0 of all first: the later ones have nothing to do where sequences are short, and
@@ -611,22 +614,48 @@ __global__ __launch_bounds__(kThreads) void paged_join(Args a) {
   const int b = blockIdx.y + (c.batch <= kMaxGrid ? 0 : blockIdx.z / parts * kMaxGrid);
   if (b >= c.batch) return;
   const int4 info = a.info[b];
-  if (info.y > 1) {
-    const int e = tid % kLanes, grp = tid / kLanes;
-    const float4* o = reinterpret_cast<const float4*>(a.o);
-    for (int h = g * G + part; h < (g + 1) * G; h += parts) {
-      float2 ml = {};
-      float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
-      for (int i0 = grp; i0 == grp || i0 < info.y; i0 += kGroups * kFlight) {
-        float4 y[kFlight];
-        float m[kFlight];
+  const int n = info.z;
+  const bool merges = info.y > 1 && part < G, weighs = a.d.accumulate && part * kWeightRows < n;
+  if (!merges && !weighs) return;
+  const int e = tid % kLanes, grp = tid / kLanes;
+  const float4* o = reinterpret_cast<const float4*>(a.o);
+  float4 y[kFlight];
+  float m[kFlight];
+  auto load_partials = [&](int h, int i0) {
 #pragma unroll
-        for (int k = 0; k < kFlight; ++k) {
-          const int64_t slot = (int64_t)(info.x + min(i0 + k * kGroups, info.y - 1)) * H + h;
-          y[k] = o[slot * kLanes + e];
-          m[k] = a.ml[slot].x;
-        }
-        if (i0 == grp) ml = joined(a, info, h);
+    for (int k = 0; k < kFlight; ++k) {
+      const int64_t slot = (int64_t)(info.x + min(i0 + k * kGroups, info.y - 1)) * H + g * G + h;
+      y[k] = o[slot * kLanes + e];
+      m[k] = a.ml[slot].x;
+    }
+  };
+  float* w = c.weight + ((int64_t)b * K + g) * c.weight_rows;
+  float4 sc[kHeads];
+  float old[4];
+  auto load_scores = [&](int r, int h0) {
+#pragma unroll
+    for (int k = 0; k < kHeads; ++k)
+      if (r < n && h0 + k < G) sc[k] = *reinterpret_cast<const float4*>(a.score + ((int64_t)b * H + g * G + h0 + k) * a.cap + r);
+  };
+  auto load_weights = [&](int r) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) old[i] = r + i < n && a.d.weight_decay != 0.f ? w[r + i] : 0.f;
+  };
+  if (merges) load_partials(part, grp);
+  if (weighs) load_scores(part * kWeightRows + 4 * tid, 0), load_weights(part * kWeightRows + 4 * tid);
+  // of all heads for the weights, else of those to be merged
+  const int first = weighs ? 0 : part, step = weighs ? 1 : parts;
+  for (int h = first + tid / 64 * step; h < G; h += kWaves * step) {
+    const float2 ml = joined(a, info, g * G + h);
+    if (tid % 64 == 0) s_ml[h] = ml, s_lse[h] = ml.y == 0.f ? INFINITY : ml.x + log2f(ml.y);
+  }
+  __syncthreads();
+  if (merges) {
+    for (int h = part; h < G; h += parts) {
+      const float2 ml = s_ml[h];
+      float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+      for (int i0 = grp; i0 < info.y; i0 += kGroups * kFlight) {
+        if (h > part || i0 > grp) load_partials(h, i0);
 #pragma unroll
         for (int k = 0; k < kFlight; ++k) {
           if (i0 + k * kGroups < info.y) {
@@ -636,51 +665,40 @@ __global__ __launch_bounds__(kThreads) void paged_join(Args a) {
           }
         }
       }
-      __syncthreads();
       s_o[grp][e] = sum;
       __syncthreads();
       if (tid < D) {
-        float y = 0.f;
+        float z = 0.f;
 #pragma unroll
-        for (int k = 0; k < kGroups; ++k) y += reinterpret_cast<const float*>(s_o[k])[tid];
-        const int64_t at = (int64_t)b * H + h;
-        reinterpret_cast<T*>(a.d.o)[at * D + tid] = (T)(ml.y == 0.f ? 0.f : y / ml.y);
+        for (int k = 0; k < kGroups; ++k) z += reinterpret_cast<const float*>(s_o[k])[tid];
+        const int64_t at = (int64_t)b * H + g * G + h;
+        reinterpret_cast<T*>(a.d.o)[at * D + tid] = (T)(ml.y == 0.f ? 0.f : z / ml.y);
         if (tid == 0 && a.d.lse) a.d.lse[at] = ml.y == 0.f ? -INFINITY : (ml.x + log2f(ml.y)) * kLn2;
       }
+      __syncthreads();
     }
   }
-  if (!a.d.accumulate) return;
+  if (!weighs) return;
   // weights, four rows a thread
-  const int n = info.z;
-  float* w = c.weight + ((int64_t)b * K + g) * c.weight_rows;
   for (int r0 = part * kWeightRows; r0 < n; r0 += parts * kWeightRows) {
     const int r = r0 + 4 * tid;
-    float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int hb = 0; hb < G; hb += kThreads) {
-      const int some = min(kThreads, G - hb);
-      if (r0 == part * kWeightRows || G > kThreads) {
-        __syncthreads();
-        for (int h = tid / 64; h < some; h += kWaves) {
-          const float2 ml = joined(a, info, g * G + hb + h);
-          if (tid % 64 == 0) s_lse[h] = ml.y == 0.f ? INFINITY : ml.x + log2f(ml.y);
-        }
-        __syncthreads();
-      }
-      const float* score = a.score + ((int64_t)b * H + g * G + hb) * a.cap + r;
-      if (r < n) {
-#pragma unroll 4
-        for (int h = 0; h < some; ++h) {
-          const float4 s = *reinterpret_cast<const float4*>(score + h * a.cap);
-          x.x += __builtin_amdgcn_exp2f(s.x - s_lse[h]), x.y += __builtin_amdgcn_exp2f(s.y - s_lse[h]);
-          x.z += __builtin_amdgcn_exp2f(s.z - s_lse[h]), x.w += __builtin_amdgcn_exp2f(s.w - s_lse[h]);
+    if (r0 > part * kWeightRows) load_weights(r);
+    float x[4] = {};
+    for (int h0 = 0; h0 < G; h0 += kHeads) {
+      if (r0 > part * kWeightRows || h0 > 0) load_scores(r, h0);
+#pragma unroll
+      for (int k = 0; k < kHeads; ++k) {
+        if (r < n && h0 + k < G) {
+          const float lse = s_lse[h0 + k];
+          x[0] += __builtin_amdgcn_exp2f(sc[k].x - lse), x[1] += __builtin_amdgcn_exp2f(sc[k].y - lse);
+          x[2] += __builtin_amdgcn_exp2f(sc[k].z - lse), x[3] += __builtin_amdgcn_exp2f(sc[k].w - lse);
         }
       }
     }
     // (scores are stored up to the next multiple of four rows; weights end at n)
-    const float y[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-      if (r + i < n) w[r + i] = a.d.weight_decay == 0.f ? y[i] : fmaf(a.d.weight_decay, w[r + i], y[i]);
+      if (r + i < n) w[r + i] = a.d.weight_decay == 0.f ? x[i] : fmaf(a.d.weight_decay, old[i], x[i]);
   }
 }
 
@@ -693,7 +711,7 @@ focus_status validate(const focus_paged_decode_desc* d) {
       !isfinite(d->weight_decay))
     return FOCUS_E_ARG;
   if (d->n_heads % c.n_kv_heads) return FOCUS_E_SHAPE;
-  if ((int64_t)c.batch * d->n_heads > INT32_MAX / kThreads) return FOCUS_E_SHAPE;
+  if ((int64_t)c.batch * d->n_heads > INT32_MAX / kThreads || d->n_heads / c.n_kv_heads > kMaxGroup) return FOCUS_E_SHAPE;
   // (chunks are counted in 32 bits, in units of 32 rows at least)
   if ((int64_t)c.batch * focus::ceil_div((int64_t)c.max_pages * c.page_rows, 32) > INT32_MAX) return FOCUS_E_SHAPE;
   const int64_t es = focus::elt_bytes(c.dtype);

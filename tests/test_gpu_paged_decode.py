@@ -132,6 +132,21 @@ def test_decode_chunks_of_many_sequences(batch, top, H, K, dim, dtype, split):
     _check(c, q64, again, dtype, weight=c.weight, decay=0.5)
 
 
+@pytest.mark.parametrize("H,K,lens", [(260, 1, [900, 3]), (512, 1, [130]), (27, 3, [2000, 300, 0])])
+def test_decode_large_groups(H, K, lens):
+    """More heads of a KV head than one workgroup or one wave of the second launch has
+    threads for, and groups that its steps do not divide; with weights."""
+    announce(f"paged decode {H}/{K} {lens}")
+    rng = np.random.default_rng(H)
+    c = Cache(rng, lens, K, 64, 16, "bf16", weight=True)
+    q, q64 = values(rng, (len(lens), H, 64), "bf16")
+    got = F.focus_paged_decode(q, c.dev, split_keys=128)
+    _check(c, q64, got, "bf16")
+    again = F.focus_paged_decode(q, c.dev, split_keys=128, weight_decay=0.75)
+    assert torch.equal(again[0], got[0]) and torch.equal(again[1], got[1])
+    _check(c, q64, again, "bf16", weight=c.weight, decay=0.75)
+
+
 @pytest.mark.parametrize("rows", [50, 5000])
 def test_decode_scores_far_below_zero(rows):
     """Scores of -1e31 and less are scores: the highest takes all the weight, alone in its

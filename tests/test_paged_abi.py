@@ -137,6 +137,7 @@ def _decode_ok():
     ("o", FAKE + 8, E_ARG), ("lse", FAKE + 2, E_ARG), ("workspace", None, E_WORKSPACE),
     ("workspace_bytes", 0, E_WORKSPACE), ("workspace", FAKE + 8, E_ARG), ("n_heads", 1 << 30, E_SHAPE),
     ("cache.row_stride", 1 << 33, E_SHAPE),     # pages inside the rows: apart, but too far
+    ("n_heads", 4 * 513, E_SHAPE),              # a group of more than 512
 ] + [("cache." + f, v, s) for f, v, s in PAGED_BAD])
 def test_paged_decode_refusals(field, value, status):
     d = _decode_ok()
