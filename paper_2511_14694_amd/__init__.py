@@ -754,7 +754,7 @@ def focus_paged_decode(q, cache: PagedCache, o=None, lse=None, weight_decay: Opt
     if o is None:
         o = torch.empty_like(q, memory_format=torch.contiguous_format)
     if lse is None and want_lse:
-        lse = q.new_empty(q.shape[:2], dtype=torch.float32)
+        lse = q.new_empty(*q.shape[:2], dtype=torch.float32)
     d = _paged_decode_desc(q, cache, o, lse, weight_decay, workspace, split_keys, softmax_scale, err)
     if workspace is None:
         n = lib().focus_paged_decode_workspace(C.byref(d))
