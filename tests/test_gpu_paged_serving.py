@@ -10,7 +10,7 @@ import torch
 import paper_2511_14694_amd as F
 from gpu_util import DEV, announce, to64
 from oracle import paged as P
-from paged_util import HALF_STEP, decode_tolerances, paged_rows, values, within
+from paged_util import HALF_STEP, Cache, decode_tolerances, paged_rows, values, within
 
 pytestmark = pytest.mark.gpu
 
@@ -144,3 +144,101 @@ def test_summary_rows_of_a_prefill_into_pages():
         to, tl, _ = decode_tolerances(q64, k64, D ** -0.5, "bf16", v64, to64(o1)[b])
         within(to64(o2)[b], to64(o1)[b], 2 * to, "o")
         within(to64(l2)[b], to64(l1)[b], 2 * tl, "lse")
+
+
+@pytest.mark.parametrize("batch,rows,K,G", [(3, 700, 2, 4), (140, 600, 1, 2)])
+def test_serving_steps_captured(batch, rows, K, G):
+    """Store, attend and weigh in one graph, cut in another (both with scratch of their
+    own), replayed in turn with eager work between, against the same calls eagerly."""
+    announce(f"captured serving of {batch} x {rows}")
+    rng = np.random.default_rng(batch)
+    D, page, steps, budget = 64, 16, 3, rows // 2
+    lens = [int(x) for x in rng.integers(1, rows, batch)]
+    lens[0] = rows
+    per = -(-(rows + steps) // page)
+    c = Cache(rng, lens, K, D, page, "bf16", max_pages=per, weight=True, spare=batch * (per + 2))
+    free = c.free
+    for b in range(batch):       # pages for the rows to come
+        for j in range(per):
+            if c.table[b, j] < 0:
+                c.table[b, j] = free.pop()
+    c.dev.table.copy_(torch.as_tensor(c.table))
+    c.dev.weight.zero_()
+    q, k, v = (values(rng, (batch, h, D), "bf16")[0] for h in (K * G, K, K))
+    seq = torch.arange(batch, dtype=torch.int32, device=DEV)
+    slot, pos = c.dev.length.clone(), c.dev.length.clone()
+    turns = F.focus_rope_turns(D)
+    opages = -(-budget // page)
+    pool = torch.zeros(batch * opages, page, K, D, dtype=torch.bfloat16, device=DEV)
+    out = F.PagedCache(pool, pool.clone(), torch.arange(batch * opages, dtype=torch.int32, device=DEV).view(batch, -1),
+                       torch.zeros_like(slot), torch.zeros(batch, K, opages * page, device=DEV))
+    keep = torch.empty(batch, K, budget, dtype=torch.int32, device=DEV)
+    o, lse, qt = torch.empty_like(q), torch.empty(batch, K * G, device=DEV), torch.empty_like(q)
+    src = c.dev
+
+    def step():
+        F.focus_rope(pos, turns, q, k, v, q_out=qt, cache=src, row_seq=seq, row_slot=slot)
+        F.focus_paged_decode(qt, src, o=o, lse=lse, weight_decay=0.9)
+
+    def cut():
+        F.focus_paged_evict(src, out, budget, recent=8, keep=keep)
+
+    state = [src.k, src.v, src.length, src.weight, o, lse, qt, out.k, out.v, out.length, out.weight, keep]
+    first = [t.clone() for t in state]
+    eager = []
+    for i in range(steps):
+        step(), cut()
+        eager.append([t.clone() for t in state])
+        slot += 1
+        pos += 1
+    torch.cuda.synchronize()
+    for t, x in zip(state, first):
+        t.copy_(x)
+    slot -= steps
+    pos -= steps
+    torch.cuda.synchronize()
+    graphs = []
+    for call in (step, cut):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            call()
+        graphs.append(g)
+    for i in range(steps):
+        for g in graphs:
+            g.replay()
+            F.focus_paged_decode(q, src)     # eager work in between
+        torch.cuda.synchronize()
+        for t, x in zip(state, eager[i]):
+            assert torch.equal(t.view(torch.uint8), x.view(torch.uint8))
+        slot += 1
+        pos += 1
+
+
+def test_calls_on_two_streams_at_once():
+    """Each call has scratch of its own: decoding and cutting on two streams gives what one
+    after another gives."""
+    announce("two streams")
+    rng = np.random.default_rng(63)
+    work = []
+    for n in (5000, 36_000):
+        c = Cache(rng, [n, 100], 2, 64, 64, "bf16", weight=True, spare=2 * 20)
+        q, _ = values(rng, (2, 8, 64), "bf16")
+        out = c.other(rng, 1000)
+        work.append((c, q, out))
+
+    def call(c, q, out, stream=None):
+        o, lse = F.focus_paged_decode(q, c.dev, weight_decay=0.5, stream=stream)
+        keep = F.focus_paged_evict(c.dev, out, 1000, recent=10, stream=stream)
+        return o, lse, keep, c.dev.weight.clone() if stream is None else None
+
+    w0 = [c.dev.weight.clone() for c, _, _ in work]
+    one = [call(*x) for x in work]
+    for (c, _, _), w in zip(work, w0):
+        c.dev.weight.copy_(w)
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    two = [call(*x, stream=s) for x, s in zip(work, streams)]
+    torch.cuda.synchronize()
+    for a, b, (c, _, _) in zip(one, two, work):
+        assert all(torch.equal(x, y) for x, y in zip(a[:3], b[:3]))
+        assert torch.equal(a[3], c.dev.weight)
