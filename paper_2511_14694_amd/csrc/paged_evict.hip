@@ -14,6 +14,7 @@
 //                 adding up the histograms of the digit before, and a last one that writes
 //                 the rows kept; what a workgroup's rows add to the ones before it follows
 //                 from the same histograms
+//   evict_stream  longer tables of heads enough for half of the device: one workgroup each
 //   evict_copy    the kept rows and their weights to the pages of `out`
 //
 // The copy is HBM bound, the selection bound by the latency of its passes: 16 x 8 heads of
@@ -182,11 +183,11 @@ __device__ int next_level(const int (&c)[F::kPer], int digit, int* waves, int* f
 }
 
 // Write the rows above `level` (> 0) and, of those equal to it, the ones that number less
-// than `equal`; before this workgroup's rows come before_above above it and before_equal
-// equal to it.
+// than `equal`; before these rows come before_above above it and before_equal equal to it,
+// both raised by what these rows, of all the waves, add.
 template <typename F, int NR>
-__device__ void write_rows(const Head& h, const uint32_t (&key)[NR], int used, int row0, uint32_t level, int equal, int before_above,
-                           int before_equal, int (*waves)[2]) {
+__device__ void write_rows(const Head& h, const uint32_t (&key)[NR], int used, int row0, uint32_t level, int equal, int& before_above,
+                           int& before_equal, int (*waves)[2]) {
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   int above = 0, ties = 0;  // of this wave
 #pragma unroll
@@ -198,11 +199,13 @@ __device__ void write_rows(const Head& h, const uint32_t (&key)[NR], int used, i
   }
   if (threadIdx.x % 64 == 0) waves[wave][0] = above, waves[wave][1] = ties;
   __syncthreads();
-  above = before_above, ties = before_equal;
   const int lane = threadIdx.x % 64;
   const int sum_above = focus::wave_scan(lane < F::kWaves ? waves[lane][0] : 0);
   const int sum_ties = focus::wave_scan(lane < F::kWaves ? waves[lane][1] : 0);
-  if (wave) above += __builtin_amdgcn_readlane(sum_above, wave - 1), ties += __builtin_amdgcn_readlane(sum_ties, wave - 1);
+  above = before_above + (wave ? __builtin_amdgcn_readlane(sum_above, wave - 1) : 0);
+  ties = before_equal + (wave ? __builtin_amdgcn_readlane(sum_ties, wave - 1) : 0);
+  before_above += __builtin_amdgcn_readlane(sum_above, F::kWaves - 1);
+  before_equal += __builtin_amdgcn_readlane(sum_ties, F::kWaves - 1);
 #pragma unroll
   for (int i = 0; i < NR; ++i) {
     if (i >= used) continue;
@@ -324,7 +327,8 @@ __global__ __launch_bounds__(F::kThreads) void evict_select(focus_paged_evict_de
       for (int i = 0; i < F::kPer; ++i) c[i] = bin_sum(hist, F::kBins - 1 - (F::kPer * (int)threadIdx.x + i));
       next_level<F>(c, digit, waves, found, x);
     }
-    write_rows<F, NR>(h, key, used, row0, x.level, x.equal, 0, 0, parts);
+    int above = 0, ties = 0;
+    write_rows<F, NR>(h, key, used, row0, x.level, x.equal, above, ties, parts);
   }
   write_rest<F>(d, h, 0, 1);
   if constexpr (COPY) {
@@ -333,6 +337,45 @@ __global__ __launch_bounds__(F::kThreads) void evict_select(focus_paged_evict_de
     const int per = F::kThreads / y.pieces;
     if ((int)threadIdx.x < per * y.pieces)
       copy_rows<false>(d, y, h.b, h.g, threadIdx.x / y.pieces, per, h.take + h.recent, threadIdx.x % y.pieces);
+  }
+}
+
+// Long tables of many heads: one workgroup per (sequence, KV head), which reads the weights
+// again for each digit and to write the rows.
+__global__ __launch_bounds__(Wide::kThreads) void evict_stream(focus_paged_evict_desc d) {
+  using F = Wide;
+  constexpr int NR = 16, kRows = NR * F::kThreads;
+  __shared__ __align__(16) int hist[F::kBins * kCopies];
+  __shared__ int waves[F::kWaves], found[3], parts[2][F::kWaves][2];
+  const Head h = head_of(d, blockIdx.x, true);
+  write_rest<F>(d, h, 0, 1);
+  if (h.take == 0) return;
+  uint32_t key[NR];
+  int row0;
+  auto load = [&](int first) {
+    float w[NR];
+    load_keys<NR>(h.w, h.old, first, NR, w, row0);
+    order_keys<NR>(h, w, row0, NR, key);
+  };
+  Level x = {0, h.take, 0};
+  for (int digit = 0; digit < F::kDigits && !x.done; ++digit) {
+    clear_hist<F>(hist);
+    __syncthreads();
+    for (int first = 0; first < h.old; first += kRows) {
+      load(first);
+      count_digit<F, NR>(key, NR, digit, x.level, hist);
+    }
+    __syncthreads();
+    int c[F::kPer];
+#pragma unroll
+    for (int i = 0; i < F::kPer; ++i) c[i] = bin_sum(hist, F::kBins - 1 - (F::kPer * (int)threadIdx.x + i));
+    next_level<F>(c, digit, waves, found, x);
+  }
+  int above = 0, ties = 0;
+  for (int first = 0, turn = 0; first < h.old; first += kRows, turn ^= 1) {
+    load(first);
+    // (a round's counts are read while the next one's are written)
+    write_rows<F, NR>(h, key, NR, row0, x.level, x.equal, above, ties, parts[turn]);
   }
 }
 
@@ -472,9 +515,14 @@ int64_t weights_of(const focus_paged_kv& c) { return (int64_t)c.batch * c.n_kv_h
 // Rows of a table that one workgroup selects from by itself.
 constexpr int64_t kShortRows = 32 * kThreads;
 
+// Workgroups a head of the long form; 0 where it is not taken: for short tables, and for
+// heads enough for half of the compute units, of which one workgroup each goes through the
+// weights (evict_stream) in less time than several pass histograms on.  us, the whole call,
+// by parts / by heads, 40 000 rows: 64 heads 46 / 50, 128 69 / 61, 512 226 / 178; 131 072
+// rows: 32 heads 51 / 92, 64 90 / 104, 256 234 / 120; 260 000 rows, 64 heads 135 / 158.
 int64_t parts_of(const focus_paged_evict_desc& d) {
-  const int64_t cap = (int64_t)d.cache.max_pages * d.cache.page_rows;
-  return cap > kShortRows ? focus::ceil_div(cap, kPart) : 0;
+  const int64_t cap = (int64_t)d.cache.max_pages * d.cache.page_rows, heads = (int64_t)d.cache.batch * d.cache.n_kv_heads;
+  return cap > kShortRows && heads < focus::device_cus() / 2 ? focus::ceil_div(cap, kPart) : 0;
 }
 
 // The long form's arrays in the workspace (out may be NULL); returns their bytes.  Two
@@ -522,6 +570,7 @@ extern "C" focus_status focus_paged_evict(const focus_paged_evict_desc* d, focus
   const int es = (int)focus::elt_bytes(d->cache.dtype), pieces = d->cache.head_dim * es / 16;
   const Copy y = {focus::page_shift(d->cache), focus::page_shift(d->out), pieces, es, !over_length && !over_budgets};
   const dim3 block(kThreads);
+  const int64_t cap = (int64_t)d->cache.max_pages * d->cache.page_rows;
   if (parts > 0) {
     const dim3 grid((uint32_t)(heads * parts));
     Long scratch;
@@ -530,6 +579,8 @@ extern "C" focus_status focus_paged_evict(const focus_paged_evict_desc* d, focus
     hipLaunchKernelGGL((evict_part<1>), grid, block, 0, s, *d, scratch);
     hipLaunchKernelGGL((evict_part<2>), grid, block, 0, s, *d, scratch);
     hipLaunchKernelGGL((evict_part<3>), grid, block, 0, s, *d, scratch);
+  } else if (cap > kShortRows) {
+    hipLaunchKernelGGL(evict_stream, dim3((uint32_t)heads), block, 0, s, *d);
   } else {
     // A workgroup copies its own head's rows where that is little work, somewhat more where
     // there are heads for every compute unit: a launch less, but a long sequence's rows
@@ -539,7 +590,6 @@ extern "C" focus_status focus_paged_evict(const focus_paged_evict_desc* d, focus
     const int64_t bytes = d->keep_rows * pieces * 64;
     const bool copies = bytes <= (256 << 10) || (bytes <= (512 << 10) && heads >= 2 * focus::device_cus());
     const dim3 grid((uint32_t)heads);
-    const int64_t cap = (int64_t)d->cache.max_pages * d->cache.page_rows;
 #define FOCUS_SELECT(F, NR)                                                                            \
   if (copies) hipLaunchKernelGGL((evict_select<F, NR, true>), grid, dim3(F::kThreads), 0, s, *d, y);  \
   else hipLaunchKernelGGL((evict_select<F, NR, false>), grid, dim3(F::kThreads), 0, s, *d, y);

@@ -217,3 +217,31 @@ def test_evict_many_heads(batch, top, K, D, budget, kind):
     old = c.dev.k.clone(), c.dev.v.clone()
     keep = F.focus_paged_evict(c.dev, out, budget, recent=5)
     _check(c, out, [budget] * batch, 5, keep, old)
+
+
+@pytest.mark.parametrize("kind", ["skewed", "ties", "special"])
+def test_evict_long_tables_of_many_heads(kind):
+    """Tables past what a workgroup holds, heads enough for half of the device: lengths of
+    none to all, on and beside the rounds of 16 384 rows."""
+    announce(f"evict long tables of many heads {kind}")
+    rng = np.random.default_rng(71)
+    lens = [0, 1, 33_000, 16_384, 16_385, 32_768, 20_000, 700] + [int(x) for x in rng.integers(0, 900, 24)]
+    c = Cache(rng, lens, 4, 64, 1024, "bf16", weight=True, spare=32)
+    c.dev.weight.copy_(torch.as_tensor(_weights(rng, c.weight.shape, kind)))
+    out = c.other(rng, 500)
+    old = c.dev.k.clone(), c.dev.v.clone()
+    keep = F.focus_paged_evict(c.dev, out, 500, recent=20)
+    _check(c, out, [500] * 32, 20, keep, old)
+
+
+@pytest.mark.parametrize("dtype,K", [("f32", 4), ("f32", 3), ("bf16", 6)])
+def test_evict_widest_rows(dtype, K):
+    """Heads of 256 elements, copied by a launch of their own and by the selecting workgroup."""
+    announce(f"evict widest rows {dtype} {K}")
+    rng = np.random.default_rng(72)
+    for budget in (9, 400):
+        c = Cache(rng, [900, 31], K, 256, 16, dtype, weight=True, spare=2 * 25)
+        out = c.other(rng, budget)
+        old = c.dev.k.clone(), c.dev.v.clone()
+        keep = F.focus_paged_evict(c.dev, out, budget, recent=4)
+        _check(c, out, [budget] * 2, 4, keep, old)
