@@ -10,7 +10,7 @@
 //   evict_select  tables of up to 32 768 rows: one workgroup per (sequence, KV head), the
 //                 weights in registers throughout; where a head's rows are few, or heads
 //                 enough to fill the device, it copies them as well
-//   evict_part    longer tables: a workgroup per 8 192 rows, one launch a digit, each
+//   evict_part    longer tables: a workgroup per 8 192 rows or more, one launch a digit, each
 //                 adding up the histograms of the digit before, and a last one that writes
 //                 the rows kept; what a workgroup's rows add to the ones before it follows
 //                 from the same histograms
@@ -379,12 +379,11 @@ __global__ __launch_bounds__(Wide::kThreads) void evict_stream(focus_paged_evict
   }
 }
 
-constexpr int kLongRows = 8;                   // registers of rows of the long form
+// The long form's workgroups.
 constexpr int kThreads = Wide::kThreads, kWaves = Wide::kWaves, kBins = Wide::kBins, kDigits = Wide::kDigits, kPer = Wide::kPer;
-constexpr int kPart = kThreads * kLongRows;    // rows of a workgroup there
 
 // The long form's workspace: per head the level so far, per part the rows above it in the
-// parts before, and the histograms [head][part][digit] (counts up to kPart).
+// parts before, and the histograms [head][part][digit] (counts of at most 32 768 rows).
 struct Long {
   Level* level;
   int* before;
@@ -393,14 +392,15 @@ struct Long {
 };
 
 // Launch STEP adds up the histograms of digit STEP - 1 and counts digit STEP, or, the last,
-// writes the rows kept.
-template <int STEP>
+// writes the rows kept.  A part is NR rows a thread.
+template <int STEP, int NR>
 __global__ __launch_bounds__(kThreads) void evict_part(focus_paged_evict_desc d, Long y) {
   __shared__ __align__(16) int hist[kBins * kCopies];
   __shared__ int waves[kWaves], found[3], pair[kWaves][2];
   const int bg = blockIdx.x / y.parts, part = blockIdx.x % y.parts, tid = threadIdx.x;
   const Head h = head_of(d, bg, STEP == 0 && part == 0);
   if (STEP == kDigits) write_rest<Wide>(d, h, part, y.parts);
+  constexpr int kPart = NR * kThreads;
   const int live = (h.old + kPart - 1) / kPart;  // parts that hold rows
   if (h.take == 0 || part >= live) return;
   // a digit's histogram of a part, two bins a thread, the first thread's the last ones
@@ -418,12 +418,12 @@ __global__ __launch_bounds__(kThreads) void evict_part(focus_paged_evict_desc d,
       return;
     }
   }
-  uint32_t key[kLongRows];
+  uint32_t key[NR];
   int row0;
   {
-    float w[kLongRows];
-    load_keys<kLongRows>(h.w, h.old, part * kPart, kLongRows, w, row0);
-    order_keys<kLongRows>(h, w, row0, kLongRows, key);
+    float w[NR];
+    load_keys<NR>(h.w, h.old, part * kPart, NR, w, row0);
+    order_keys<NR>(h, w, row0, NR, key);
   }
   if constexpr (STEP >= 1) {
     if (!x.done) {
@@ -457,12 +457,12 @@ __global__ __launch_bounds__(kThreads) void evict_part(focus_paged_evict_desc d,
     }
   }
   if constexpr (STEP == kDigits) {
-    write_rows<Wide, kLongRows>(h, key, kLongRows, row0, x.level, x.equal, before, before_equal, pair);
+    write_rows<Wide, NR>(h, key, NR, row0, x.level, x.equal, before, before_equal, pair);
   } else {
     if (x.done) return;
     clear_hist<Wide>(hist);
     __syncthreads();
-    count_digit<Wide, kLongRows>(key, kLongRows, STEP, x.level, hist);
+    count_digit<Wide, NR>(key, NR, STEP, x.level, hist);
     __syncthreads();
     *bins(part, STEP) = (uint32_t)bin_sum(hist, bin0) | (uint32_t)bin_sum(hist, bin0 + 1) << 16;
   }
@@ -518,17 +518,26 @@ constexpr int64_t kShortRows = 32 * kThreads;
 // Workgroups a head of the long form; 0 where it is not taken: for short tables, and for
 // heads enough for half of the compute units, of which one workgroup each goes through the
 // weights (evict_stream) in less time than several pass histograms on.  us, the whole call,
-// by parts / by heads, 40 000 rows: 64 heads 46 / 50, 128 69 / 61, 512 226 / 178; 131 072
-// rows: 32 heads 51 / 92, 64 90 / 104, 256 234 / 120; 260 000 rows, 64 heads 135 / 158.
-int64_t parts_of(const focus_paged_evict_desc& d) {
+// by parts / by heads, 40 000 rows: 64 heads 46 / 50, 128 69 / 62, 512 247 / 178; 131 072
+// rows: 32 heads 48 / 92, 64 71 / 104, 256 183 / 121.
+int64_t parts_of(const focus_paged_evict_desc& d, int* rows) {
   const int64_t cap = (int64_t)d.cache.max_pages * d.cache.page_rows, heads = (int64_t)d.cache.batch * d.cache.n_kv_heads;
-  return cap > kShortRows && heads < focus::device_cus() / 2 ? focus::ceil_div(cap, kPart) : 0;
+  if (cap <= kShortRows || heads >= focus::device_cus() / 2) return 0;
+  // Rows a thread holds: every workgroup adds up the histograms of all parts of its head, so
+  // that few large parts are better as soon as small ones would go around the device more
+  // than once, or are more than 32 a head.  8 / 16 / 32, us of the whole call: 8 heads of
+  // 131 072 rows 31.6 / 33.8 / 44.4, 32 of them 51 / 47 / 56, 64 of them 90 / 78 / 72; 8 heads
+  // of 400 000 rows 52 / 40 / 45, of a million 132 / 70 / 56, one of a million 51 / 43 / 47.
+  const int64_t parts = focus::ceil_div(cap, 8 * kThreads), groups = heads * parts, cus = focus::device_cus();
+  *rows = groups <= cus && parts <= 32 ? 8 : groups <= 3 * cus ? 16 : 32;
+  return focus::ceil_div(cap, *rows * kThreads);
 }
 
 // The long form's arrays in the workspace (out may be NULL); returns their bytes.  Two
 // levels a head: a launch reads one that its first part's workgroup does not write.
 size_t long_form(const focus_paged_evict_desc& d, void* workspace, Long* out) {
-  const int64_t parts = parts_of(d), heads = (int64_t)d.cache.batch * d.cache.n_kv_heads;
+  int rows;
+  const int64_t parts = parts_of(d, &rows), heads = (int64_t)d.cache.batch * d.cache.n_kv_heads;
   if (parts == 0) return 0;
   const int64_t level = focus::ceil_div(2 * heads * (int64_t)sizeof(Level), 16) * 16;
   const int64_t before = focus::ceil_div(heads * parts * 4, 16) * 16;
@@ -554,7 +563,8 @@ extern "C" focus_status focus_paged_evict(const focus_paged_evict_desc* d, focus
   if (d->cache.batch == 0) return FOCUS_OK;
   if (!d->cache.weight || (d->keep_rows > 0 && !d->keep)) return FOCUS_E_NULL;
   if ((reinterpret_cast<uintptr_t>(d->keep) & 3u) || (reinterpret_cast<uintptr_t>(d->budgets) & 3u)) return FOCUS_E_ARG;
-  const int64_t parts = parts_of(*d), heads = (int64_t)d->cache.batch * d->cache.n_kv_heads;
+  int rows = 0;
+  const int64_t parts = parts_of(*d, &rows), heads = (int64_t)d->cache.batch * d->cache.n_kv_heads;
   const size_t need = focus_paged_evict_workspace(d);
   if (need > 0 && (!d->workspace || d->workspace_bytes < need)) return FOCUS_E_WORKSPACE;
   if (!focus::aligned16(d->workspace)) return FOCUS_E_ARG;
@@ -575,10 +585,13 @@ extern "C" focus_status focus_paged_evict(const focus_paged_evict_desc* d, focus
     const dim3 grid((uint32_t)(heads * parts));
     Long scratch;
     long_form(*d, d->workspace, &scratch);
-    hipLaunchKernelGGL((evict_part<0>), grid, block, 0, s, *d, scratch);
-    hipLaunchKernelGGL((evict_part<1>), grid, block, 0, s, *d, scratch);
-    hipLaunchKernelGGL((evict_part<2>), grid, block, 0, s, *d, scratch);
-    hipLaunchKernelGGL((evict_part<3>), grid, block, 0, s, *d, scratch);
+#define FOCUS_PARTS(NR)                                                      \
+  hipLaunchKernelGGL((evict_part<0, NR>), grid, block, 0, s, *d, scratch);   \
+  hipLaunchKernelGGL((evict_part<1, NR>), grid, block, 0, s, *d, scratch);   \
+  hipLaunchKernelGGL((evict_part<2, NR>), grid, block, 0, s, *d, scratch);   \
+  hipLaunchKernelGGL((evict_part<3, NR>), grid, block, 0, s, *d, scratch);
+    if (rows == 8) { FOCUS_PARTS(8) } else if (rows == 16) { FOCUS_PARTS(16) } else { FOCUS_PARTS(32) }
+#undef FOCUS_PARTS
   } else if (cap > kShortRows) {
     hipLaunchKernelGGL(evict_stream, dim3((uint32_t)heads), block, 0, s, *d);
   } else {

@@ -245,3 +245,20 @@ def test_evict_widest_rows(dtype, K):
         old = c.dev.k.clone(), c.dev.v.clone()
         keep = F.focus_paged_evict(c.dev, out, budget, recent=4)
         _check(c, out, [budget] * 2, 4, keep, old)
+
+
+@pytest.mark.parametrize("batch,K,cap", [(30, 4, 40_960), (100, 1, 66_560), (3, 1, 1 << 20)])
+@pytest.mark.parametrize("kind", ["skewed", "ties"])
+def test_evict_long_tables_in_larger_parts(batch, K, cap, kind):
+    """Long tables of many rows in all, whose workgroups take more rows each; lengths on and
+    beside the parts' ends, most sequences short."""
+    announce(f"evict larger parts {batch} x {K} x {cap} {kind}")
+    rng = np.random.default_rng(cap + batch)
+    lens = [0, 32_769, 16_384] + [int(x) for x in rng.integers(0, 500, batch - 3)]
+    lens[-1] = min(cap, 40_000)
+    c = Cache(rng, lens, K, 64, 1024, "bf16", weight=True, max_pages=cap // 1024, spare=batch)
+    c.dev.weight.copy_(torch.as_tensor(_weights(rng, c.weight.shape, kind)))
+    out = c.other(rng, 700)
+    old = c.dev.k.clone(), c.dev.v.clone()
+    keep = F.focus_paged_evict(c.dev, out, 700, recent=33)
+    _check(c, out, [700] * batch, 33, keep, old)
