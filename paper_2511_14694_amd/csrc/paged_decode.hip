@@ -128,6 +128,7 @@ struct Args {
   float sc;             // softmax scale in log2 units
   int shift;            // log2 page_rows
   int tiles, wide_shift, unit_shift, target;   // wide and unit are powers of two
+  int units;            // workgroups of a chunk and 16 query heads each
   int group, parts;     // query heads of a KV head; workgroups of one in the second launch
   int64_t cap;
   bool single;
@@ -325,15 +326,20 @@ template <typename T, int D> struct Tile {
   __device__ uint32_t word(int j, int i) const { return v[j][i / kVSize][i % kVSize]; }
 };
 
-// Load once, from global memory: the compiler takes a choice between a page and kZeros
-// for an address of any kind, whose loads it can only wait for all together.
-template <typename V>
-__device__ __forceinline__ V load_once(const void* p) {
-  return __builtin_nontemporal_load(reinterpret_cast<const __attribute__((address_space(1))) V*>(
-      reinterpret_cast<uintptr_t>(p)));
+// Load from global memory: the compiler takes a choice between a page and kZeros for an
+// address of any kind, whose loads it can only wait for all together.  Past the caches,
+// unless other workgroups read the same rows: 64 sequences of 16 000 rows of one head of 128
+// (bf16) in 90 us, 97 through them (of tables that the last-level cache could hold between
+// calls, 102 MB: 35.7 and 33.6 if nothing comes between, 35.7 and 36.8 if something does).
+template <typename V, bool SHARED>
+__device__ __forceinline__ V load_row(const void* p) {
+  const auto* from = reinterpret_cast<const __attribute__((address_space(1))) V*>(reinterpret_cast<uintptr_t>(p));
+  if constexpr (SHARED) return *from;
+  else return __builtin_nontemporal_load(from);
 }
 
-template <typename T, int D>
+// SHARED: a KV head has more than 16 query heads, whose workgroups read the same rows.
+template <typename T, int D, bool SHARED>
 __global__ __launch_bounds__(kThreads, resident(D)) void paged_attend(Args a) {
   using L = Tile<T, D>;
   constexpr int kPitch = D + 4;
@@ -345,11 +351,22 @@ __global__ __launch_bounds__(kThreads, resident(D)) void paged_attend(Args a) {
   // (a wave's number in a scalar register: its loops are branches then, not masks)
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / 64);
   const int lane = tid % 64, col = lane % 16, x = lane / 16;
-  const int tile_id = a.tiles == 1 ? 0 : blockIdx.x % a.tiles;
-  const int g0 = (a.tiles == 1 ? blockIdx.x : blockIdx.x / a.tiles) << a.wide_shift;
+  int slot_id = blockIdx.z * kMaxGrid + blockIdx.y, tile_id = 0, g0 = blockIdx.x;
+  if constexpr (SHARED) {
+    // Workgroups are dealt over the XCDs in turn: those that read the same rows to one XCD,
+    // one after another, so that its L2 reads them once.  64 sequences of 16 000 rows of one
+    // head of 128 (bf16), 32 query heads: 117 us; loaded past the caches 146, in the order of
+    // the grid's indices as well 180.
+    const int id = blockIdx.x, among = id % (focus::kXcds * a.tiles);
+    const int unit = id / (focus::kXcds * a.tiles) * focus::kXcds + among % focus::kXcds;
+    tile_id = among / focus::kXcds;
+    slot_id = unit / a.units;
+    g0 = unit % a.units;
+  }
+  g0 <<= a.wide_shift;
   // waves of a KV head; this wave's head, and which of its waves it is
   const int by = kWaves >> a.wide_shift, at_head = wave >> (2 - a.wide_shift), g = g0 + at_head, among = wave & (by - 1);
-  const Chunk ch = find_chunk(a, blockIdx.z * kMaxGrid + blockIdx.y);
+  const Chunk ch = find_chunk(a, slot_id);
   if (ch.chunks == 0) return;
   const int b = ch.b, r0 = ch.c * ch.rows, r1 = min(ch.n, r0 + ch.rows);
   const bool first = g0 == 0 && tile_id == 0;
@@ -406,11 +423,11 @@ __global__ __launch_bounds__(kThreads, resident(D)) void paged_attend(Args a) {
 #pragma unroll
         for (int t = 0; t < L::kProducts; ++t)
 #pragma unroll
-          for (int i = 0; i < L::kSteps; ++i) w.k[t][i] = load_once<u32x4>(kp + 4 * t * ks + i * 4 * L::kPiece);
+          for (int i = 0; i < L::kSteps; ++i) w.k[t][i] = load_row<u32x4, SHARED>(kp + 4 * t * ks + i * 4 * L::kPiece);
 #pragma unroll
         for (int j = 0; j < L::kScores; ++j)
 #pragma unroll
-          for (int i = 0; i < L::kVs; ++i) w.v[j][i] = load_once<typename L::V>(vp + j * vs + i * L::kPiece);
+          for (int i = 0; i < L::kVs; ++i) w.v[j][i] = load_row<typename L::V, SHARED>(vp + j * vs + i * L::kPiece);
       };
       auto compute = [&](L& w, int r, auto whole) {
         f32x4 s[L::kProducts];
@@ -735,7 +752,7 @@ focus_status launch(Args a, const Plan& p, hipStream_t s) {
   const int64_t most = focus::ceil_div(8 * focus::device_cus(), heads);
   a.parts = (int)std::min(most, a.d.accumulate ? std::max(per, std::min<int64_t>(a.group, 4)) : a.group);
   const int64_t slots = focus::ceil_div(p.slots, kMaxGrid), batches = focus::ceil_div(c.batch, kMaxGrid);
-  if (p.groups * p.slots > INT32_MAX / kThreads || heads * a.parts > INT32_MAX / kThreads || slots > kMaxGrid ||
+  if (p.groups * p.slots > INT32_MAX / kThreads - focus::kXcds * kMaxGroup || heads * a.parts > INT32_MAX / kThreads || slots > kMaxGrid ||
       batches * a.parts > kMaxGrid)
     return FOCUS_E_SHAPE;
   if (p.planned) {
@@ -743,9 +760,10 @@ focus_status launch(Args a, const Plan& p, hipStream_t s) {
     const focus_status st = focus::launch_status();
     if (st != FOCUS_OK) return st;
   }
-  hipLaunchKernelGGL((paged_attend<T, D>),
-                     dim3((uint32_t)p.groups, (uint32_t)std::min<int64_t>(p.slots, kMaxGrid), (uint32_t)slots),
-                     dim3(kThreads), 0, s, a);
+  const dim3 grid = p.tiles > 1 ? dim3((uint32_t)(focus::ceil_div(a.units * p.slots, focus::kXcds) * focus::kXcds * p.tiles))
+                                : dim3((uint32_t)p.groups, (uint32_t)std::min<int64_t>(p.slots, kMaxGrid), (uint32_t)slots);
+  if (p.tiles > 1) hipLaunchKernelGGL((paged_attend<T, D, true>), grid, dim3(kThreads), 0, s, a);
+  else hipLaunchKernelGGL((paged_attend<T, D, false>), grid, dim3(kThreads), 0, s, a);
   const focus_status st = focus::launch_status();
   if (st != FOCUS_OK || (p.single && !a.d.accumulate)) return st;
   hipLaunchKernelGGL((paged_join<T, D>),
@@ -777,7 +795,7 @@ extern "C" focus_status focus_paged_decode(const focus_paged_decode_desc* d, foc
   a.d = *d;
   a.shift = focus::page_shift(c);
   a.tiles = p.tiles, a.wide_shift = __builtin_ctz((unsigned)p.wide), a.unit_shift = __builtin_ctz((unsigned)p.unit);
-  a.target = (int)p.target;
+  a.target = (int)p.target, a.units = (int)(p.groups / p.tiles);
   a.group = d->n_heads / c.n_kv_heads;
   a.cap = p.cap, a.single = p.single, a.slots = p.slots;
   if (p.bytes > 0) {

@@ -147,6 +147,22 @@ def test_decode_large_groups(H, K, lens):
     _check(c, q64, again, "bf16", weight=c.weight, decay=0.75)
 
 
+@pytest.mark.parametrize("batch,top,H,K,dtype", [(140, 900, 20, 1, "bf16"), (5, 200, 99, 3, "f32"), (9, 3000, 36, 2, "f32")])
+def test_decode_rows_shared_by_workgroups(batch, top, H, K, dtype):
+    """Groups of more than 16 heads in tables that are split, not split, and divided by a
+    launch of their own."""
+    announce(f"paged decode shared rows {batch} x {top} {H}/{K} {dtype}")
+    rng = np.random.default_rng(batch + H)
+    lens = [top, 0] + [int(x) for x in rng.integers(0, top + 1, batch - 2)]
+    c = Cache(rng, lens, K, 64, 32, dtype, weight=True)
+    q, q64 = values(rng, (batch, H, 64), dtype)
+    got = F.focus_paged_decode(q, c.dev)
+    _check(c, q64, got, dtype)
+    again = F.focus_paged_decode(q, c.dev, weight_decay=0.5)
+    assert torch.equal(again[0], got[0]) and torch.equal(again[1], got[1])
+    _check(c, q64, again, dtype, weight=c.weight, decay=0.5)
+
+
 @pytest.mark.parametrize("rows", [50, 5000])
 def test_decode_scores_far_below_zero(rows):
     """Scores of -1e31 and less are scores: the highest takes all the weight, alone in its
