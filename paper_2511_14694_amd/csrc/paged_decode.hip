@@ -27,7 +27,7 @@
 // 16 sequences of 10 000 rows of 32 heads of 128 (bf16, 2.62 GB) take 401 us, 6.5 TB/s; one
 // of 262 144 rows of 8 heads (1.07 GB) 169, 6.4 TB/s.  Where there is less to read the start
 // and the second launch count: 64 sequences of 1 to 8 192 rows of 8 heads (0.26 GB), with
-// weights, 70 us, of which 61 in paged_attend and 10 in paged_join.  The first form, one
+// weights, 71 us, of which 61 in paged_attend and 10 in paged_join.  The first form, one
 // workgroup a (sequence, head) on the vector units, took 2754, 62 241 and 2061.
 #include "paged.h"
 
@@ -110,8 +110,9 @@ Plan make_plan(const focus_paged_decode_desc* d) {
     p.slots = c.batch * std::max<int64_t>(1, focus::ceil_div(p.cap, d->split_keys));
   } else {
     p.target = std::max<int64_t>(1, resident(c.head_dim) * focus::device_cus() / p.groups);
-    // a chunk has at least the rows of the batch over the target; a sequence at least one
-    p.slots = std::min(c.batch + p.target, c.batch * std::max<int64_t>(1, focus::ceil_div(p.cap, p.unit)));
+    // a chunk has at least half of the rows of the batch over the target; a sequence at
+    // least one
+    p.slots = std::min(c.batch + 2 * p.target, c.batch * std::max<int64_t>(1, focus::ceil_div(p.cap, p.unit)));
   }
   const int64_t partials = p.slots * d->n_heads;
   p.owner = 16 * (int64_t)c.batch;
@@ -152,26 +153,26 @@ __device__ inline float max_column(float x) {
 // Rows of a chunk when they are to be chosen, for `target` chunks resident at a time: the
 // least estimate of the time among
 //   the rows of the whole batch spread over `target` chunks, rounded up to units, or over
-//   half as many;
+//   half or twice as many;
 //   the least size at which the chunks of all sequences are resident at once (up to kWave
 //   sequences; it needs 16 steps of a search);
 //   no split at all.
 // The estimate, in rows a resident workgroup streams while all of them do: what there is
 // to read, and for each chunk kStart rows' worth of beginning and end and its partials
-// written and read, over the target; where not all are resident at once a last one begins
-// late and runs, with the memory to itself, at kAlone times the rate; so does the longest
-// one if it is longer than that.
-// 14 sequences of 209 921 rows, one KV head: 518 chunks of 5 760 rows on 512 places took
-// 304 us, 504 chunks of 5 888 237; 60 of 782 rows, 8 KV heads: no split (120 workgroups of
-// four heads on 128 places) 46 us, half of the places 62.
-constexpr int kStart = 100;
-constexpr float kAlone = 1.25f;
+// written and read, over the target; where not all are resident at once kLate of the
+// longest more, which may begin late; at least the longest at kAlone times the rate, as
+// fast as one gets when the others have ended.  us, before twice as many were tried (kStart
+// 100, all of the longest more) / now: 64 sequences of 4096 rows, 5 KV heads, 152 / 120; 48
+// with 7 heads 152 / 121; 16 of 10 000, 32 heads, 417 / 409; 200 of 1000 to 2000, 8 heads,
+// 272 / 246; 400 of 600 to 1200, 4 heads, 165 / 184; over 104 such batches 0.8 % less.
+constexpr int kStart = 72;
+constexpr float kLate = 0.3f, kAlone = 1.1f;
 
 __device__ inline float estimate(const Args& a, uint32_t units, int chunks, int rows, int longest) {
-  const float each = (float)(kStart >> a.wide_shift) + (a.d.cache.dtype == FOCUS_BF16 ? 2.f : 1.f) * a.group;
+  const float each = (float)(kStart >> a.wide_shift) + (a.d.cache.dtype == FOCUS_BF16 ? 4.f : 2.f) * a.group;
   const float even = ((float)units * (1 << a.unit_shift) + each * (float)chunks) / (float)a.target;
-  const float alone = (float)min(rows, longest) / kAlone;
-  return chunks > a.target ? even + alone : fmaxf(even, alone);
+  const float last = (float)min(rows, longest);
+  return fmaxf(chunks > a.target ? even + kLate * last : even, last / kAlone);
 }
 
 // Sum and maximum of f(rows) over the sequences: of a wave, two sequences a lane, or of
@@ -230,6 +231,8 @@ template <typename Over> __device__ int chunk_rows(const Args& a, const Over& ov
     if (e < best) best = e, units = with;
   };
   better(count2, two);
+  const uint32_t half = (one + 1) / 2;
+  better(chunks(half), half);
   if (count1 > target && batch <= kWave && (uint32_t)batch <= target) {
     uint32_t lo = one, hi = whole;  // too many chunks at lo, few enough at hi
     for (int k = 0; k < 16 && hi - lo > 1; ++k) {
