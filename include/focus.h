@@ -776,9 +776,10 @@ typedef struct {
 } focus_rope_desc;
 
 /* Errors: E_NULL, E_ARG, E_DTYPE, E_SHAPE (cache of another head_dim, head count or
- * dtype; 2^23 rows or more), E_UNSUPPORTED, E_HIP.  A row whose sequence is outside the batch or whose
- * page is outside the pool is not stored (FOCUS_ERR_BOUNDS), nor one whose slot is
- * past max_pages * page_rows (FOCUS_ERR_CAPACITY); its q_out and k_out are written. */
+ * dtype; 2^23 rows or more), E_UNSUPPORTED, E_HIP.  A row whose sequence is outside the
+ * batch or whose page is outside the pool is not stored (FOCUS_ERR_BOUNDS), nor one whose
+ * slot is past max_pages * page_rows (FOCUS_ERR_CAPACITY); its q_out and k_out are
+ * written. */
 focus_status focus_rope(const focus_rope_desc* d, focus_stream_t stream);
 
 /* ------------------------------------------------------------------------ */
@@ -821,9 +822,10 @@ typedef struct {
  * until the call's kernels end; calls that share one on overlapping streams race. */
 size_t focus_paged_decode_workspace(const focus_paged_decode_desc* d);
 /* Errors: E_NULL, E_ARG, E_DTYPE, E_SHAPE (batch * max_pages * page_rows of 2^36,
- * batch * n_heads of 2^23, more than 512 query heads of a KV head, among others), E_UNSUPPORTED, E_WORKSPACE, E_HIP.  Rows of a
- * page outside the pool are left out of the softmax (FOCUS_ERR_BOUNDS; weight of the step
- * 0); a length outside [0, max_pages * page_rows] is clipped to it (FOCUS_ERR_CAPACITY). */
+ * batch * n_heads of 2^23, more than 512 query heads of a KV head, among others),
+ * E_UNSUPPORTED, E_WORKSPACE, E_HIP.  Rows of a page outside the pool are left out of the
+ * softmax (FOCUS_ERR_BOUNDS; weight of the step 0); a length outside [0, max_pages *
+ * page_rows] is clipped to it (FOCUS_ERR_CAPACITY). */
 focus_status focus_paged_decode(const focus_paged_decode_desc* d, focus_stream_t stream);
 
 /* ------------------------------------------------------------------------ */
@@ -839,7 +841,8 @@ focus_status focus_paged_decode(const focus_paged_decode_desc* d, focus_stream_t
  * The copy goes to other pages: a page that another sequence shares stays as it is, and
  * the old pages are free as a whole afterwards.  `out` may lie in the same pool; a page
  * in both tables, or twice in out's, is a race.  out.length may be cache.length or
- * budgets (not a part of either); out.weight and cache.weight may have nothing in common.  Rows of out past m are left as they were. */
+ * budgets (not a part of either); out.weight and cache.weight may have nothing in common.
+ * Rows of out past m are left as they were. */
 typedef struct {
   focus_paged_kv cache;         /* with weight                               */
   focus_paged_kv out;           /* same dtype, heads, head_dim, batch        */

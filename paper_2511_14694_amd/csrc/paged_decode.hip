@@ -61,9 +61,10 @@ constexpr int kUnit = 128;      // rows of a chunk times KV heads of a workgroup
 // lie in a page outside the pool.
 __device__ __align__(16) const uint32_t kZeros[256] = {};
 
-// Workspace: int4 info[batch] {first slot, chunks, rows, rows of a chunk}; for more than 64
-// sequences int owner[slots]; then the partials of `slots` chunks: float2 ml[slots][H], float o[slots][H][D], then, where weights are
-// accumulated, float score[batch][H][cap] (log2 units).  None where neither is needed.
+// Workspace: int4 info[batch] {first slot, chunks, rows, rows of a chunk}; for more than
+// kWave sequences int owner[slots]; then the partials of `slots` chunks: float2
+// ml[slots][H], float o[slots][H][D]; then, where weights are accumulated, float
+// score[batch][H][cap] (log2 units).  None where nothing is handed on.
 struct Plan {
   int64_t slots;        // upper bound of the chunks of all sequences
   int64_t target;       // chunks resident at a time (split_keys 0)
@@ -589,7 +590,8 @@ __global__ __launch_bounds__(kThreads, resident(D)) void paged_attend(Args a) {
     if (ch.chunks == 1) {
       y = ml.y == 0.f ? f32x4{0.f, 0.f, 0.f, 0.f} : y * (1.f / ml.y);
       T* o_at = reinterpret_cast<T*>(a.d.o) + at * D + e;
-      if constexpr (L::kBf16) *reinterpret_cast<u32x2*>(o_at) = u32x2{focus::pack_bf16x2(y[0], y[1]), focus::pack_bf16x2(y[2], y[3])};
+      if constexpr (L::kBf16)
+        *reinterpret_cast<u32x2*>(o_at) = u32x2{focus::pack_bf16x2(y[0], y[1]), focus::pack_bf16x2(y[2], y[3])};
       else *reinterpret_cast<f32x4*>(o_at) = y;
       if (e == 0 && a.d.lse) a.d.lse[at] = ml.y == 0.f ? -INFINITY : (ml.x + log2f(ml.y)) * kLn2;
     } else {
@@ -658,10 +660,11 @@ __global__ __launch_bounds__(kThreads) void paged_join(Args a) {
   float* w = c.weight + ((int64_t)b * K + g) * c.weight_rows;
   float4 sc[kHeads];
   float old[4];
+  const float* score = a.score + ((int64_t)b * H + g * G) * a.cap;
   auto load_scores = [&](int r, int h0) {
 #pragma unroll
     for (int k = 0; k < kHeads; ++k)
-      if (r < n && h0 + k < G) sc[k] = *reinterpret_cast<const float4*>(a.score + ((int64_t)b * H + g * G + h0 + k) * a.cap + r);
+      if (r < n && h0 + k < G) sc[k] = *reinterpret_cast<const float4*>(score + (h0 + k) * a.cap + r);
   };
   auto load_weights = [&](int r) {
 #pragma unroll
@@ -755,8 +758,8 @@ focus_status launch(Args a, const Plan& p, hipStream_t s) {
   const int64_t most = focus::ceil_div(8 * focus::device_cus(), heads);
   a.parts = (int)std::min(most, a.d.accumulate ? std::max(per, std::min<int64_t>(a.group, 4)) : a.group);
   const int64_t slots = focus::ceil_div(p.slots, kMaxGrid), batches = focus::ceil_div(c.batch, kMaxGrid);
-  if (p.groups * p.slots > INT32_MAX / kThreads - focus::kXcds * kMaxGroup || heads * a.parts > INT32_MAX / kThreads || slots > kMaxGrid ||
-      batches * a.parts > kMaxGrid)
+  if (p.groups * p.slots > INT32_MAX / kThreads - focus::kXcds * kMaxGroup ||
+      heads * a.parts > INT32_MAX / kThreads || slots > kMaxGrid || batches * a.parts > kMaxGrid)
     return FOCUS_E_SHAPE;
   if (p.planned) {
     hipLaunchKernelGGL(paged_plan, dim3(1), dim3(kPlan), 0, s, a);
