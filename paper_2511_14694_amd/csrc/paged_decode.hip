@@ -396,8 +396,8 @@ __global__ __launch_bounds__(kThreads, resident(D)) void paged_attend(Args a) {
 
   float m, l;
   f32x4 o[L::kPer];
-  // The low part of the weights (below) turns an infinity in V into a NaN: sums that are
-  // NaN are taken again without it (the others keep what they are).
+  // The lower parts of the weights (below) turn an infinity in V into a NaN: sums that are
+  // NaN are taken again without them (the others keep what they are).
   auto pass = [&](auto with_low) {
     constexpr bool low = decltype(with_low)::value;
     m = kMinit;
@@ -486,22 +486,29 @@ __global__ __launch_bounds__(kThreads, resident(D)) void paged_attend(Args a) {
 #pragma unroll
         for (int t = 0; t < L::kPer; ++t) o[t] *= alpha;
         if constexpr (L::kBf16) {
-          // the weights in two bf16 parts, off by 2^-17 of them together (one part
-          // alone adds as much to o as its own rounding); the matrix cores have the time
-          bf16x8 hi, lo;
+          // product t's rows of V^T, in the place of what was loaded
+          u32x4 z[L::kPer];
 #pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            hi[j] = (__bf16)y[j];
-            lo[j] = (__bf16)(y[j] - (float)hi[j]);
-          }
-#pragma unroll
-          for (int t = 0; t < L::kPer; ++t) {
-            u32x4 z;
+          for (int t = 0; t < L::kPer; ++t)
 #pragma unroll
             for (int e = 0; e < 4; ++e)
-              z[e] = __builtin_amdgcn_perm(w.word(2 * e + 1, t / 2), w.word(2 * e, t / 2), t % 2 ? 0x07060302 : 0x05040100);
-            o[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, z), hi, o[t], 0, 0, 0);
-            if constexpr (low) o[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, z), lo, o[t], 0, 0, 0);
+              z[t][e] = __builtin_amdgcn_perm(w.word(2 * e + 1, t / 2), w.word(2 * e, t / 2), t % 2 ? 0x07060302 : 0x05040100);
+          // The weights in three bf16 parts, which hold all 24 bits of a float32, one part
+          // after another: by products instead, all parts of each, D = 64 spills and takes 2 to
+          // 6 % longer.  (Two parts, 17 bits, round twice as many elements of o the other way
+          // and take as long within 2 %: 16 x 10 000 rows of 32 heads of 128 400 and 400 us, of
+          // 64 208 and 208, 64 x 16 000 rows of one head of 128 for 128 query heads 307 and 305.)
+#pragma unroll
+          for (int part = 0; part < (low ? 3 : 1); ++part) {
+            bf16x8 p;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+              p[j] = (__bf16)y[j];
+              y[j] -= (float)p[j];
+            }
+#pragma unroll
+            for (int t = 0; t < L::kPer; ++t)
+              o[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, z[t]), p, o[t], 0, 0, 0);
           }
         } else {
 #pragma unroll

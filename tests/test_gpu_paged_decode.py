@@ -8,7 +8,7 @@ import torch
 import paper_2511_14694_amd as F
 from gpu_util import DEV, announce, to64
 from oracle import paged as P
-from paged_util import Cache, decode_tolerances, values, within
+from paged_util import HALF_STEP, Cache, decode_tolerances, values, within
 
 pytestmark = pytest.mark.gpu
 
@@ -354,3 +354,40 @@ def test_decode_captured_and_replayed():
         torch.cuda.synchronize()
         assert torch.equal(got[0], o) and torch.equal(got[1], lse) and torch.equal(got[2], c.dev.weight)
     c.dev.length.copy_(full)
+
+
+@pytest.mark.parametrize("D,group", [(64, 1), (64, 20), (128, 1), (128, 5)])
+def test_decode_weights_hold_the_bits_of_a_float32(D, group):
+    """bf16 products with the softmax weights lose none of their 24 bits.  Three rows of
+    weights 1, y and 1 before the division, whose v are y's first two bf16 parts and -1:
+    what is left of the sum is the third part of y, up to 2^-18.
+
+    Off by: the score's scale and product, 2 2^-24 of at most 0.6 log2 e; the exponential,
+    one step, 2^-24; at most twelve additions in float32 of at most 1; together
+    (1.8 + 1 + 12) 2^-24, over a sum of weights of at least 2.5, and half a step of o.
+    The rows' y are chosen so that two parts alone would be off by twice that."""
+    announce(f"paged decode bits of the weights {D} group {group}")
+    K = 32
+    bf = lambda x: to64(torch.as_tensor(x).to(torch.bfloat16))  # noqa: E731
+    s = bf(np.linspace(0.07, 0.6, 20_000, dtype=np.float32))
+    s = np.unique(s)
+    y = np.exp(-s)
+    hi = bf(y)
+    mid = bf(y - hi)
+    rest = np.abs(y - hi - mid) / (2 + y)
+    best = np.argsort(-rest)[:K]
+    s, y, hi, mid = s[best], y[best], hi[best], mid[best]
+    ref = (hi + mid - y) / (2 + y)
+    tol = (1.8 + 1 + 12) * 2.0 ** -24 / 2.5 + HALF_STEP["bf16"] * np.abs(ref)
+    assert (np.abs(ref) > 2 * tol).all()
+    k, v = (np.zeros((1, 8, K, D), np.float32) for _ in range(2))
+    k[0, 1, :, 0] = -s
+    v[0, 0], v[0, 1], v[0, 2] = hi[:, None], -1.0, mid[:, None]
+    dev = lambda a: torch.as_tensor(a).to(torch.bfloat16).to(DEV)  # noqa: E731
+    cache = F.PagedCache(dev(k), dev(v), torch.zeros(1, 1, dtype=torch.int32, device=DEV),
+                         torch.tensor([3], dtype=torch.int32, device=DEV))
+    q = torch.zeros(1, K * group, D, dtype=torch.bfloat16, device=DEV)
+    q[..., 0] = 1.0
+    o, _ = F.focus_paged_decode(q, cache, softmax_scale=1.0)
+    within(to64(o)[0].reshape(K, group, D), np.broadcast_to(ref[:, None, None], (K, group, D)),
+           np.broadcast_to(tol[:, None, None], (K, group, D)), "o")
