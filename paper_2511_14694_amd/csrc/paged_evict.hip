@@ -35,7 +35,7 @@ template <int THREADS, int BITS> struct Form {
   static constexpr int kThreads = THREADS, kWaves = THREADS / 64, kBins = 1 << BITS, kDigits = (31 + BITS) / BITS;
   static constexpr int kPer = kBins / THREADS;  // bins a thread sums
   static_assert(kPer >= 1 && kPer <= 2, "one or two bins a thread");
-  static constexpr __device__ int shift(int i) { return i == kDigits - 1 ? 0 : 32 - BITS * (i + 1); }
+  static constexpr __host__ __device__ int shift(int i) { return i == kDigits - 1 ? 0 : 32 - BITS * (i + 1); }
   static constexpr __device__ uint32_t mask(int i) { return i == kDigits - 1 ? (1u << (32 - BITS * i)) - 1 : kBins - 1u; }
   // the digits above digit i
   static constexpr __device__ uint32_t above(int i) { return i == 0 ? 0u : 0xffffffffu << shift(i - 1); }
@@ -115,8 +115,9 @@ __device__ void order_keys(const Head& h, const float (&x)[NR], int row0, int us
 }
 
 // Histogram of a digit among the rows that share the digits above it, added to hist
-// (cleared by the caller; of digit 0, bucket 0 holds rows that are none, which no choice
-// reaches).  Atomics on one address go one after another, and the first digit, mostly the
+// (cleared by the caller).  Bucket 0 of digit 0 also counts what is no row, and so does bucket
+// 0 of each next digit where the digits above are 0: behind all rows, of which no choice
+// wants more than there are.  Atomics on one address go one after another, and the first digit, mostly the
 // exponent, has few buckets that are full: lanes add to four copies in turn.  16 x 8 heads
 // of 10 000 rows, 64 of them kept, the whole call, with weights all different / all equal:
 // one copy 23.9 / 46.9 us, four 21.3 / 26.2, eight 22.0 / 24.2; lanes that share a bucket
@@ -153,10 +154,27 @@ struct Level {
   int equal, done;
 };
 
+// The level with one more digit: the last of the rows wanted lies in `bucket`, of `count`
+// rows, of which `wanted` are.  Where the whole bucket stays, no further digit is needed: its
+// rows are the ones above a level, unless that would be one below 0: with digits of 8 bits
+// the integers of -2^127 and less, -inf among them, begin with a digit of 0.
+template <typename F> constexpr __host__ __device__ Level refined(Level x, int digit, int bucket, int wanted, int count) {
+  x.level |= (uint32_t)bucket << F::shift(digit);
+  x.equal = wanted;
+  if (digit < F::kDigits - 1 && wanted == count && x.level != 0) {
+    x.level -= 1;
+    x.equal = 0, x.done = 1;
+  }
+  return x;
+}
+constexpr Level kAllLow = refined<Small>({0, 256, 0}, 0, 0, 256, 256);
+static_assert(kAllLow.level == 0 && kAllLow.equal == 256 && !kAllLow.done, "no level is below 0");
+static_assert(refined<Small>(kAllLow, 1, 0x7f, 256, 256).level == 0x7effff, "the rows of -inf, 0x7fffff");
+static_assert(refined<Wide>({0, 9, 0}, 0, 3, 2, 2).level == 0x5fffff, "the rows of -2^127 and less");
+
 // The bucket that holds the last of the `equal` greatest rows of a digit's histogram (with
 // at least so many rows; c: this thread's bins, kBins - 1 - kPer tid downwards), in every
-// thread: the level with that digit.  Where the whole bucket stays, no further digit is
-// needed: its rows are the ones above a level.
+// thread: the level with that digit.
 template <typename F>
 __device__ int next_level(const int (&c)[F::kPer], int digit, int* waves, int* found, Level& x) {
   const int tid = threadIdx.x;
@@ -172,12 +190,7 @@ __device__ int next_level(const int (&c)[F::kPer], int digit, int* waves, int* f
   }
   __syncthreads();
   const int bucket = found[0];
-  x.level |= (uint32_t)bucket << F::shift(digit);
-  x.equal = found[1];
-  if (digit < F::kDigits - 1 && x.equal == found[2]) {
-    x.level -= 1;  // (no weight's integer is 0)
-    x.equal = 0, x.done = 1;
-  }
+  x = refined<F>(x, digit, bucket, found[1], found[2]);
   __syncthreads();
   return bucket;
 }

@@ -262,3 +262,30 @@ def test_evict_long_tables_in_larger_parts(batch, K, cap, kind):
     old = c.dev.k.clone(), c.dev.v.clone()
     keep = F.focus_paged_evict(c.dev, out, 700, recent=33)
     _check(c, out, [700] * batch, 33, keep, old)
+
+
+@pytest.mark.parametrize("lowest", [-np.inf, -3e38, -2.0 ** 127, -1.7e38])
+@pytest.mark.parametrize("cap,recent", [(1024, 0), (2048, 0), (2048, 37), (4096, 5)])
+def test_evict_keeps_all_rows_of_lowest_weights(cap, recent, lowest):
+    """More heads than the device has compute units, and sequences that stay whole: in one
+    head all weights are the lowest, in others one is, among sequences of every weight and
+    some that are cut.  Lengths that fill a workgroup's registers, and one less or more."""
+    announce(f"evict lowest weights {lowest} cap {cap} recent {recent}")
+    rng = np.random.default_rng(cap + recent)
+    lens = [cap, cap, 256 + recent, 1024, 512 + recent, 1024 - recent, 255, 257, cap - 1] + [3] * 58
+    K = 4
+    c = Cache(rng, lens, K, 8, 256, "bf16", weight=True, spare=len(lens) * (cap // 256))
+    w = c.weight.copy()
+    w[0, 0] = lowest
+    for b, n in enumerate(lens):
+        w[b, 1, n // 2] = lowest
+        w[b, 2, :n:3] = lowest
+    c.dev.weight.copy_(torch.as_tensor(w))
+    out = c.other(rng, cap)
+    budgets = [cap] * len(lens)
+    budgets[1], budgets[6] = cap - 1, 254
+    old = c.dev.k.clone(), c.dev.v.clone()
+    err = torch.zeros(1, dtype=torch.int32, device=DEV)
+    keep = F.focus_paged_evict(c.dev, out, torch.tensor(budgets, dtype=torch.int32, device=DEV), recent=recent, err=err)
+    assert int(err.item()) == 0
+    _check(c, out, budgets, recent, keep, old)
