@@ -115,6 +115,39 @@ def _scratch(nbytes: int, device, stream):
         return torch.empty(nbytes, dtype=torch.uint8, device=device)
 
 
+def _empty(shape, dtype, device, stream):
+    """An output that a call allocates itself: on the stream its kernels run on, as with
+    _scratch (a block freed on the caller's stream may still be in use there), and known
+    to the caller's stream, so that the block, once freed, waits for what reads it there."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    here = torch.cuda.current_stream(device)
+    with torch.cuda.stream(stream):
+        t = torch.empty(shape, dtype=dtype, device=device)
+    t.record_stream(here)
+    return t
+
+
+def _empty_like(t, stream):
+    """_empty of t's shape, dtype and device, contiguous."""
+    if stream is None:
+        return torch.empty_like(t, memory_format=torch.contiguous_format)
+    return _empty(t.shape, t.dtype, t.device, stream)
+
+
+def _input(x, dtype, device, stream):
+    """An array argument as a contiguous tensor of dtype on device: x itself if it is
+    one, else a copy made on the call's stream, as _empty."""
+    if stream is None or (torch.is_tensor(x) and x.dtype is dtype and x.device == device and x.is_contiguous()):
+        return torch.as_tensor(x, dtype=dtype).to(device).contiguous()
+    here = torch.cuda.current_stream(device)
+    with torch.cuda.stream(stream):
+        t = torch.as_tensor(x, dtype=dtype).to(device).contiguous()
+    if t is not x:
+        t.record_stream(here)
+    return t
+
+
 def _dtype(t) -> int:
     if t.dtype not in _DTYPES:
         raise ValueError(f"unsupported dtype {t.dtype}")
@@ -158,16 +191,13 @@ def focus_layout(totals: LayoutTotals, seq_nt, window_nt: int, kmer=None, kmer_u
     same totals whose arrays are written again instead of allocating new ones.
     next_base: also fill tok_next_base (the target map pi(t))."""
     dev = torch.device(device)
-    seq = torch.as_tensor(np.asarray(seq_nt, dtype=np.int64) if not torch.is_tensor(seq_nt) else seq_nt,
-                          dtype=torch.int64).to(dev).contiguous()
+    seq = _input(np.asarray(seq_nt, dtype=np.int64) if not torch.is_tensor(seq_nt) else seq_nt, torch.int64, dev, stream)
     km = None
     if kmer is not None:
-        km = torch.as_tensor(np.asarray(kmer, dtype=np.int32) if not torch.is_tensor(kmer) else kmer,
-                             dtype=torch.int32).to(dev).contiguous()
+        km = _input(np.asarray(kmer, dtype=np.int32) if not torch.is_tensor(kmer) else kmer, torch.int32, dev, stream)
     bs = None
     if bases is not None:
-        bs = torch.as_tensor(np.asarray(bases, dtype=np.uint8) if not torch.is_tensor(bases) else bases,
-                             dtype=torch.uint8).to(dev).contiguous()
+        bs = _input(np.asarray(bases, dtype=np.uint8) if not torch.is_tensor(bases) else bases, torch.uint8, dev, stream)
     B = seq.numel()
     sizes = {"cu_windows": B + 1, "cu_tokens": B + 1, "cu_summaries": B + 1,
              "sum_tok": totals.n_summaries}
@@ -182,7 +212,7 @@ def focus_layout(totals: LayoutTotals, seq_nt, window_nt: int, kmer=None, kmer_u
         if any(f not in arrays or arrays[f].numel() != max(int(n), 0) for f, n in sizes.items()):
             raise ValueError("`out` layout has different sizes")
     else:
-        arrays = {f: torch.empty(max(int(n), 0), dtype=_FIELD_DTYPE[f], device=dev) for f, n in sizes.items()}
+        arrays = {f: _empty(max(int(n), 0), _FIELD_DTYPE[f], dev, stream) for f, n in sizes.items()}
     d = LayoutDesc()
     d.totals = totals
     d.batch, d.window_nt, d.kmer_uniform, d.summary_token_id = B, int(window_nt), int(kmer_uniform), int(summary_token_id)
@@ -246,9 +276,9 @@ def focus_window_attn(lay: Layout, q, k, v, cache_k=None, cache_v=None, o=None, 
     workspace None allocates what focus_window_attn_workspace asks for; an
     empty tensor runs without the key split."""
     if o is None:
-        o = torch.empty_like(q)
+        o = _empty_like(q, stream)
     if lse is None and want_lse:
-        lse = torch.empty(q.shape[0], q.shape[1], dtype=torch.float32, device=q.device)
+        lse = _empty(q.shape[:2], torch.float32, q.device, stream)
     if o.shape != q.shape or o.dtype != q.dtype or (lse is not None and tuple(lse.shape) != tuple(q.shape[:2])):
         raise ValueError("o must match q; lse must be [rows, heads]")
     d = _attn_desc(lay, q, k, v, cache_k, cache_v, o, lse, win_ids, qkv_tok_base, softmax_scale,
@@ -288,9 +318,9 @@ def focus_decode_step(q, k_new, v_new, kind, cache_k, cache_v, cache_len, win_k,
                       softmax_scale: float = 0.0, want_lse: bool = True, err=None, stream=None):
     """One decode step for every sequence of the batch; returns (o, lse)."""
     if o is None:
-        o = torch.empty_like(q)
+        o = _empty_like(q, stream)
     if lse is None and want_lse:
-        lse = torch.empty(q.shape[0], q.shape[1], dtype=torch.float32, device=q.device)
+        lse = _empty(q.shape[:2], torch.float32, q.device, stream)
     B, H, D = q.shape
     Hkv = k_new.shape[1]
     if (k_new.shape != (B, Hkv, D) or v_new.shape != k_new.shape or kind.numel() < B
@@ -344,7 +374,7 @@ class DecodeSchedule:
     def start(self, tokens, stream=None):
         """Walk tokens[b] tokens into each sequence's current window; returns
         the device tensor of how many of them are summaries."""
-        t = torch.as_tensor(tokens, dtype=torch.int32).to(self.kind.device).contiguous()
+        t = _input(tokens, torch.int32, self.kind.device, stream)
         d = self._desc(t)
         check("focus_decode_sched_start", lib().focus_decode_sched_start(C.byref(d),
                                                                        _stream(stream, self.kind.device)))
@@ -386,15 +416,15 @@ def focus_fidelity(p, q, input_kind: int = FOCUS_FID_LOGITS, cu_pos=None, out=No
         raise ValueError("p and q must be contiguous [n_pos, vocab] tensors of one dtype")
     n_pos, vocab = p.shape
     if out is None:
-        out = torch.empty(n_pos, FOCUS_FID_N, dtype=torch.float32, device=p.device)
+        out = _empty((n_pos, FOCUS_FID_N), torch.float32, p.device, stream)
     if tuple(out.shape) != (n_pos, FOCUS_FID_N) or out.dtype != torch.float32:
         raise ValueError("out must be float32 [n_pos, 5]")
     n_seq = 0
     if cu_pos is not None:
-        cu_pos = torch.as_tensor(cu_pos, dtype=torch.int64).to(p.device).contiguous()
+        cu_pos = _input(cu_pos, torch.int64, p.device, stream)
         n_seq = cu_pos.numel() - 1
         if seq_mean is None:
-            seq_mean = torch.empty(n_seq, FOCUS_FID_N, dtype=torch.float32, device=p.device)
+            seq_mean = _empty((n_seq, FOCUS_FID_N), torch.float32, p.device, stream)
     d = FidelityDesc()
     d.dtype = _dtype(p)
     d.input_kind = int(input_kind)
@@ -418,11 +448,11 @@ def focus_gemm(a, b, out=None, a_rows=None, alpha: float = 1.0, out_dtype=torch.
     if a.stride(1) != 1 or b.stride(1) != 1 or a.shape[1] != b.shape[0]:
         raise ValueError("a [rows, k] and b [k, n] must be row-major with matching k")
     if a_rows is not None:
-        a_rows = torch.as_tensor(a_rows, dtype=torch.int64).to(a.device).contiguous()
+        a_rows = _input(a_rows, torch.int64, a.device, stream)
     m = a.shape[0] if a_rows is None else a_rows.numel()
     n = b.shape[1]
     if out is None:
-        out = torch.empty(m, n, dtype=out_dtype, device=a.device)
+        out = _empty((m, n), out_dtype, a.device, stream)
     if tuple(out.shape) != (m, n) or out.stride(1) != 1:
         raise ValueError("out must be [m, n] row-major")
     d = GemmDesc(m, n, a.shape[1], _ptr_rows(a), a.stride(0), _ptr(a_rows), a.shape[0], _ptr_rows(b), b.stride(0),
@@ -438,9 +468,9 @@ def focus_adapter_attn(lay: Layout, q_sum, k, v, cache_k=None, cache_v=None, o_s
     global summary index - sum_base), k / v [rows, H_kv, D] (row = token -
     kv_tok_base), cache [batch, cap, H_kv, D].  Returns (o_sum, lse_sum)."""
     if o_sum is None:
-        o_sum = torch.empty_like(q_sum)
+        o_sum = _empty_like(q_sum, stream)
     if lse_sum is None and want_lse:
-        lse_sum = torch.empty(q_sum.shape[0], q_sum.shape[1], dtype=torch.float32, device=q_sum.device)
+        lse_sum = _empty(q_sum.shape[:2], torch.float32, q_sum.device, stream)
     if (o_sum.shape != q_sum.shape or q_sum.dtype != k.dtype or k.shape != v.shape
             or q_sum.shape[2] != k.shape[2]):
         raise ValueError("adapter attention shapes disagree")
@@ -503,7 +533,7 @@ def focus_adapter_layer(lay: Layout, hidden, w_q, w_k, w_v, w_o, n_heads: int, n
     """FOCUS adapter update of the summary tokens (eq. focus-attn): returns
     out [n_summaries, d_model] in summary order."""
     if out is None:
-        out = torch.empty(lay.totals.n_summaries, hidden.shape[1], dtype=hidden.dtype, device=hidden.device)
+        out = _empty((lay.totals.n_summaries, hidden.shape[1]), hidden.dtype, hidden.device, stream)
     if workspace is None:
         n = focus_adapter_layer_workspace(lay, hidden, w_q, w_k, w_v, w_o, n_heads, n_kv_heads, mask)
         workspace = _scratch(max(n, 256), hidden.device, stream)
@@ -522,7 +552,7 @@ def focus_qkv_project(lay: Layout, hidden, w_qkv, n_heads: int, n_kv_heads: int,
     D = w_qkv.shape[1] // (n_heads + 2 * n_kv_heads)
     if w_qkv.shape != (d_model, (n_heads + 2 * n_kv_heads) * D) or hidden.dtype != w_qkv.dtype:
         raise ValueError("w_qkv must be [d_model, (H + 2 H_kv) D] of hidden's dtype")
-    mk = lambda h: torch.empty(rows, h, D, dtype=hidden.dtype, device=hidden.device)   # noqa: E731
+    mk = lambda h: _empty((rows, h, D), hidden.dtype, hidden.device, stream)   # noqa: E731
     q = mk(n_heads) if q is None else q
     k = mk(n_kv_heads) if k is None else k
     v = mk(n_kv_heads) if v is None else v
@@ -689,7 +719,7 @@ def focus_rope(pos, turns, q=None, k=None, v=None, layout: int = FOCUS_ROPE_INTE
         heads = q.shape[1]
         qs = (n, heads, dim)
         if q_out is None:
-            q_out = torch.empty_like(q, memory_format=torch.contiguous_format)
+            q_out = _empty_like(q, stream)
         q_rows, qo_rows = _rows(q, qs, dtype, dev, "q"), _rows(q_out, qs, dtype, dev, "q_out")
     elif q_out is not None:
         raise ValueError("q_out without q")
@@ -698,7 +728,7 @@ def focus_rope(pos, turns, q=None, k=None, v=None, layout: int = FOCUS_ROPE_INTE
         ks = (n, kv, dim)
         k_rows = _rows(k, ks, dtype, dev, "k")
         if k_out is None and cache is None:
-            k_out = torch.empty_like(k, memory_format=torch.contiguous_format)
+            k_out = _empty_like(k, stream)
         if k_out is not None:
             ko_rows = _rows(k_out, ks, dtype, dev, "k_out")
     elif k_out is not None:
@@ -752,9 +782,10 @@ def focus_paged_decode(q, cache: PagedCache, o=None, lse=None, weight_decay: Opt
     weight_decay: also cache.weight = weight_decay * cache.weight + the step's softmax
     weights, summed over the heads of each KV head."""
     if o is None:
-        o = torch.empty_like(q, memory_format=torch.contiguous_format)
+        o = _empty_like(q, stream)
     if lse is None and want_lse:
-        lse = q.new_empty(*q.shape[:2], dtype=torch.float32)
+        lse = q.new_empty(*q.shape[:2], dtype=torch.float32) if stream is None else \
+            _empty(q.shape[:2], torch.float32, q.device, stream)
     d = _paged_decode_desc(q, cache, o, lse, weight_decay, workspace, split_keys, softmax_scale, err)
     if workspace is None:
         n = lib().focus_paged_decode_workspace(C.byref(d))
@@ -797,7 +828,7 @@ def focus_paged_evict(cache: PagedCache, out: PagedCache, budget, recent: int = 
         rows = out.table.shape[-1] * out.k.shape[1]
         if not torch.is_tensor(budget):
             rows = min(rows, max(int(budget), 0))
-        keep = torch.empty(cache.table.shape[0], cache.k.shape[2], rows, dtype=torch.int32, device=cache.k.device)
+        keep = _empty((cache.table.shape[0], cache.k.shape[2], rows), torch.int32, cache.k.device, stream)
     d = _paged_evict_desc(cache, out, budget, recent, keep, workspace, err)
     if workspace is None:
         n = lib().focus_paged_evict_workspace(C.byref(d))

@@ -242,3 +242,75 @@ def test_calls_on_two_streams_at_once():
     for a, b, (c, _, _) in zip(one, two, work):
         assert all(torch.equal(x, y) for x, y in zip(a[:3], b[:3]))
         assert torch.equal(a[3], c.dev.weight)
+
+
+def test_outputs_do_not_take_blocks_that_the_callers_stream_still_writes():
+    """Blocks of the outputs' sizes, freed on the caller's stream with a write to them still
+    to come there: calls on another stream have outputs of their own."""
+    announce("outputs on another stream")
+    rng = np.random.default_rng(64)
+    c = Cache(rng, [5000, 100], 2, 64, 64, "bf16", weight=True, spare=2 * 20)
+    q, _ = values(rng, (2, 8, 64), "bf16")
+    out = c.other(rng, 1000)
+    pos = torch.tensor([7, 8], dtype=torch.int32, device=DEV)
+    turns = F.focus_rope_turns(64)
+
+    def call(stream=None):
+        qt, _ = F.focus_rope(pos, turns, q, stream=stream)
+        o, lse = F.focus_paged_decode(q, c.dev, stream=stream)
+        keep = F.focus_paged_evict(c.dev, out, 1000, recent=10, stream=stream)
+        return qt, o, lse, keep
+
+    want = [t.clone() for t in call()]
+    other = torch.cuda.Stream()
+    warm = call(other)
+    torch.cuda.synchronize()
+    del warm
+    a = torch.randn(4096, 4096, device=DEV)
+    torch.cuda.synchronize()
+    blocks = [torch.empty_like(t) for t in want]
+    for _ in range(20):
+        a = a @ a * 1e-3          # some milliseconds before the writes
+    for t in blocks:
+        t.fill_(77)
+    del blocks, t
+    got = call(other)
+    torch.cuda.synchronize()
+    for g, w in zip(got, want):
+        assert torch.equal(g, w)
+    # a result read on the caller's stream and freed there keeps its block until then
+    a = torch.randn(4096, 4096, device=DEV)
+    torch.cuda.synchronize()
+    o, _ = F.focus_paged_decode(q, c.dev, stream=other)
+    torch.cuda.current_stream().wait_stream(other)
+    for _ in range(20):
+        a = a @ a * 1e-3
+    read = o.clone()
+    del o
+    for _ in range(3):
+        F.focus_paged_decode(torch.zeros_like(q), c.dev, stream=other)
+    torch.cuda.synchronize()
+    assert torch.equal(read, want[1])
+
+
+def test_a_call_on_another_stream_inside_a_capture():
+    """A capture that forks to another stream for a call, outputs allocated in it, and joins."""
+    announce("captured on another stream")
+    rng = np.random.default_rng(65)
+    c = Cache(rng, [3000, 100], 2, 64, 64, "bf16", weight=True)
+    q, _ = values(rng, (2, 8, 64), "bf16")
+    F.focus_paged_decode(q, c.dev)
+    other = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        other.wait_stream(torch.cuda.current_stream())
+        o, lse = F.focus_paged_decode(q, c.dev, stream=other)
+        torch.cuda.current_stream().wait_stream(other)
+    for seed in range(3):
+        q.copy_(values(rng, (2, 8, 64), "bf16")[0])
+        g.replay()
+        torch.cuda.synchronize()
+        got = o.clone(), lse.clone()
+        want = F.focus_paged_decode(q, c.dev)
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
