@@ -593,6 +593,16 @@ def _need(t, dtype, shape, dev: int, what):
                      + " on the other tensors' device")
 
 
+_I32_MAX = 2 ** 31 - 1
+
+
+def _i32(x, what) -> int:
+    """x for a field of 32 bits, which would cut more of them off."""
+    if -_I32_MAX <= x <= _I32_MAX:
+        return int(x)
+    raise ValueError(f"{what} {x} does not fit in 32 bits")
+
+
 def _err_ptr(err, dev: int):
     if err is None:
         return None
@@ -678,8 +688,9 @@ def focus_rope_turns(rot_dim: int, theta: float = 10000.0, scaling: int = FOCUS_
     """Rotary frequencies of a head's rot_dim turned elements, in turns per position:
     float64 [rot_dim / 2] on device, to be kept by the caller.  scaling
     (FOCUS_ROPE_*), factor, context, low, high: see focus_rope_scaling in focus.h."""
-    out = np.empty(max(int(rot_dim) // 2, 0), np.float64)
-    s = RopeScaling(int(scaling), int(rot_dim), float(theta), float(factor), float(context), float(low), float(high))
+    rot_dim, scaling = _i32(rot_dim, "rot_dim"), _i32(scaling, "scaling")
+    out = np.empty(max(rot_dim // 2, 0), np.float64)
+    s = RopeScaling(scaling, rot_dim, float(theta), float(factor), float(context), float(low), float(high))
     check("focus_rope_turns", lib().focus_rope_turns(C.byref(s), out.ctypes.data_as(C.POINTER(C.c_double))))
     return torch.from_numpy(out).to(device)
 
@@ -746,7 +757,7 @@ def focus_rope(pos, turns, q=None, k=None, v=None, layout: int = FOCUS_ROPE_INTE
     elif v is not None:
         raise ValueError("v without a cache to store it in")
     rot = 0 if turns is None else 2 * turns.numel()
-    d = RopeDesc(_DTYPES[dtype], heads, kv, dim, rot, layout, 1 if inverse else 0, float(amplitude), n,
+    d = RopeDesc(_DTYPES[dtype], heads, kv, dim, rot, _i32(layout, "layout"), 1 if inverse else 0, float(amplitude), n,
                  _need(pos, torch.int32, (n,), dev, "pos"),
                  _need(turns, torch.float64, None, dev, "turns") if rot else None,
                  *q_rows, *qo_rows, *k_rows, *ko_rows, *v_rows, c, seq, slot,
@@ -763,7 +774,7 @@ def _paged_decode_desc(q, cache, o, lse, weight_decay, workspace, split_keys, so
         raise ValueError("q must be [batch, heads, D] of the cache's batch, head_dim and device")
     if weight_decay is not None and cache.weight is None:
         raise ValueError("weight_decay needs a cache with weight")
-    return PagedDecodeDesc(c, shape[1], split_keys, float(softmax_scale), 0 if weight_decay is None else 1,
+    return PagedDecodeDesc(c, shape[1], _i32(split_keys, "split_keys"), float(softmax_scale), 0 if weight_decay is None else 1,
                            0.0 if weight_decay is None else float(weight_decay), 0, *_rows(q, shape, dtype, dev, "q"),
                            None if o is None else _need(o, dtype, shape, dev, "o"),
                            None if lse is None else _need(lse, torch.float32, shape[:2], dev, "lse"),
@@ -807,7 +818,10 @@ def _paged_evict_desc(cache, out, budget, recent, keep, workspace, err):
     if keep is not None:
         rows = keep.shape[-1]
         keep = _need(keep, torch.int32, (c.batch, c.n_kv_heads, rows), dev, "keep")
-    return PagedEvictDesc(c, to, int(budget), int(recent), budgets, keep, rows, *_workspace(workspace, dev),
+    # 32 bits in the descriptor: no table has more rows than they count, and all below 0
+    # is refused
+    budget, recent = (max(-1, min(int(x), _I32_MAX)) for x in (budget, recent))
+    return PagedEvictDesc(c, to, budget, recent, budgets, keep, rows, *_workspace(workspace, dev),
                           None if err is None else _err_ptr(err, dev))
 
 

@@ -339,3 +339,31 @@ def test_descriptors_hold_what_their_fields_say(monkeypatch):
     got = F.focus_paged_evict(c, out, 12)
     assert got.shape == (2, K, 12) and calls["focus_paged_evict"].budget == 12
     assert F.focus_paged_evict(c, out, 999).shape == (2, K, 80)
+
+
+def test_whole_numbers_past_32_bits_are_not_cut_off(monkeypatch):
+    """The descriptors hold 32 bits: a budget beyond them keeps all rows, as the formula
+    has it, and what has no such meaning is refused."""
+    calls = {}
+    monkeypatch.setattr(F, "_launch", lambda name, d, dev, stream: calls.__setitem__(name, d))
+
+    class Lib:
+        def __getattr__(self, name):
+            return lambda d: 0
+    monkeypatch.setattr(F, "lib", Lib)
+    c = _cache()
+    for big in (1 << 31, 1 << 32, (1 << 40) + 5, (1 << 63) - 1, 1 << 64):
+        keep = F.focus_paged_evict(c, c, big, recent=big)
+        d = calls["focus_paged_evict"]
+        assert (d.budget, d.recent) == (2 ** 31 - 1, 2 ** 31 - 1) and keep.shape[2] == 48
+        F.focus_paged_evict(c, c, 1 - big, recent=-big)         # refused by the library: below 0
+        assert calls["focus_paged_evict"].budget < 0 and calls["focus_paged_evict"].recent < 0
+    q, pos, turns = torch.zeros(2, 4, 64, dtype=torch.bfloat16), torch.zeros(2, dtype=torch.int32), \
+        torch.zeros(32, dtype=torch.float64)
+    for call in (lambda: F.focus_paged_decode(q, c, split_keys=(1 << 32) + 128),
+                 lambda: F.focus_paged_decode_workspace(q, c, split_keys=1 << 31),
+                 lambda: F.focus_rope(pos, turns, q, layout=1 << 32),
+                 lambda: F.focus_rope_turns((1 << 32) + 64, device="cpu"),
+                 lambda: F.focus_rope_turns(64, scaling=1 << 32, device="cpu")):
+        with pytest.raises(ValueError):
+            call()
