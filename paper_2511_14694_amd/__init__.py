@@ -638,6 +638,15 @@ def _launch(call: str, d, dev: int, stream):
         check(call, st)
 
 
+def _query(call: str, d, dev: int) -> int:
+    """A workspace's bytes on device dev, as _launch will need them there."""
+    fn = getattr(lib(), call)
+    if dev < 0 or dev == _device():
+        return fn(C.byref(d))
+    with torch.cuda.device(dev):
+        return fn(C.byref(d))
+
+
 @dataclass
 class PagedCache:
     """A paged K/V cache (focus_paged_kv): row r of sequence b is row r % page_rows of
@@ -783,7 +792,7 @@ def _paged_decode_desc(q, cache, o, lse, weight_decay, workspace, split_keys, so
 
 def focus_paged_decode_workspace(q, cache: PagedCache, weight_decay=None, split_keys: int = 0) -> int:
     d = _paged_decode_desc(q, cache, None, None, weight_decay, None, split_keys, 0.0, None)
-    return lib().focus_paged_decode_workspace(C.byref(d))
+    return _query("focus_paged_decode_workspace", d, q.get_device())
 
 
 def focus_paged_decode(q, cache: PagedCache, o=None, lse=None, weight_decay: Optional[float] = None, workspace=None,
@@ -799,7 +808,7 @@ def focus_paged_decode(q, cache: PagedCache, o=None, lse=None, weight_decay: Opt
             _empty(q.shape[:2], torch.float32, q.device, stream)
     d = _paged_decode_desc(q, cache, o, lse, weight_decay, workspace, split_keys, softmax_scale, err)
     if workspace is None:
-        n = lib().focus_paged_decode_workspace(C.byref(d))
+        n = _query("focus_paged_decode_workspace", d, q.get_device())
         if n > 0:
             workspace = _scratch(n, q.device, stream)
             d.workspace, d.workspace_bytes = workspace.data_ptr(), n
@@ -827,7 +836,7 @@ def _paged_evict_desc(cache, out, budget, recent, keep, workspace, err):
 
 def focus_paged_evict_workspace(cache: PagedCache, out: PagedCache, budget, recent: int = 0, keep=None) -> int:
     d = _paged_evict_desc(cache, out, budget, recent, keep, None, None)
-    return lib().focus_paged_evict_workspace(C.byref(d))
+    return _query("focus_paged_evict_workspace", d, cache.k.get_device())
 
 
 def focus_paged_evict(cache: PagedCache, out: PagedCache, budget, recent: int = 0, keep=None, workspace=None, err=None,
@@ -845,7 +854,7 @@ def focus_paged_evict(cache: PagedCache, out: PagedCache, budget, recent: int = 
         keep = _empty((cache.table.shape[0], cache.k.shape[2], rows), torch.int32, cache.k.device, stream)
     d = _paged_evict_desc(cache, out, budget, recent, keep, workspace, err)
     if workspace is None:
-        n = lib().focus_paged_evict_workspace(C.byref(d))
+        n = _query("focus_paged_evict_workspace", d, cache.k.get_device())
         if n > 0:
             workspace = _scratch(n, cache.k.device, stream)
             d.workspace, d.workspace_bytes = workspace.data_ptr(), n

@@ -367,3 +367,34 @@ def test_whole_numbers_past_32_bits_are_not_cut_off(monkeypatch):
                  lambda: F.focus_rope_turns(64, scaling=1 << 32, device="cpu")):
         with pytest.raises(ValueError):
             call()
+
+
+def test_workspaces_are_asked_of_the_tensors_device(monkeypatch):
+    """A workspace's size depends on the device that will use it (its compute units), not
+    on the current one: tensors on device 1, current device 0."""
+    asked, at = [], [0]
+
+    class Lib:
+        def __getattr__(self, name):
+            return lambda *a: asked.append((name, at[-1])) or 16
+
+    class Device:
+        def __init__(self, n):
+            self.n = n
+
+        def __enter__(self):
+            at.append(self.n)
+
+        def __exit__(self, *a):
+            at.pop()
+    monkeypatch.setattr(F, "lib", Lib)
+    monkeypatch.setattr(F, "_device", lambda: at[-1])
+    monkeypatch.setattr(F, "_launch", lambda *a: None)
+    monkeypatch.setattr(torch.cuda, "device", Device)
+    monkeypatch.setattr(torch.Tensor, "get_device", lambda t: 1)
+    c, q = _cache(), torch.zeros(2, 4, 64, dtype=torch.bfloat16)
+    F.focus_paged_decode_workspace(q, c)
+    F.focus_paged_decode(q, c)
+    F.focus_paged_evict_workspace(c, c, 3)
+    F.focus_paged_evict(c, c, 3)
+    assert [d for _, d in asked] == [1] * 4 and at == [0], asked
