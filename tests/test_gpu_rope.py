@@ -265,3 +265,100 @@ def test_rope_captured_and_replayed():
         call()
         torch.cuda.synchronize()
         assert torch.equal(got, qo)
+
+
+@pytest.mark.parametrize("rows,heads,kv,dim,rot,pairs,dtype", [
+    (4_097, 1, 1, 64, 64, "half", "bf16"),             # two rows a workgroup, one in the last
+    (17_003, 2, 1, 64, 32, "interleaved", "bf16"),     # eight, many of them in one step
+    (17_001, 20, 3, 64, 64, "interleaved", "f32"),     # 16 heads a step: two steps a row
+    (16_385, 37, 5, 64, 48, "half", "bf16"),           # 32 heads a step
+    (9_001, 5, 2, 80, 40, "half", "bf16"),             # pieces of 8 bytes
+    (8_195, 9, 1, 64, 20, "half", "bf16"),             # single elements, 4 heads a step
+    (6_200, 3, 2, 64, 20, "half", "f32"),
+    (12_300, 7, 7, 32, 6, "interleaved", "bf16"),      # pieces of two elements
+    (6_147, 2, 2, 256, 256, "half", "f32"),
+])
+def test_rope_several_rows_a_workgroup(rows, heads, kv, dim, rot, pairs, dtype):
+    """More rows than eight for each of 256 compute units: a workgroup takes several, the
+    last one fewer."""
+    announce(f"rope {rows} x {heads}/{kv} x {dim} rot {rot} {pairs} {dtype}")
+    rng = np.random.default_rng(rows + dim + rot)
+    q, q64 = values(rng, (rows, heads, dim), dtype)
+    k, k64 = values(rng, (rows, kv, dim), dtype)
+    pos = rng.integers(-50, 3_000_000, rows).astype(np.int32)
+    turns = F.focus_rope_turns(rot)
+    t64 = turns.cpu().numpy()
+    p = torch.as_tensor(pos).to(DEV)
+    qo, ko = F.focus_rope(p, turns, q, k, layout=PAIRS[pairs], amplitude=0.75)
+    _check(qo, q64, pos, t64, pairs, False, 0.75, dtype, "q")
+    _check(ko, k64, pos, t64, pairs, False, 0.75, dtype, "k")
+    back, _ = F.focus_rope(p, turns, q, None, layout=PAIRS[pairs], inverse=True)
+    _check(back, q64, pos, t64, pairs, True, 1.0, dtype, "inverse")
+    F.focus_rope(p, turns, q, k, layout=PAIRS[pairs], amplitude=0.75, q_out=q, k_out=k)
+    assert torch.equal(q, qo) and torch.equal(k, ko)
+
+
+@pytest.mark.parametrize("page,K,dtype,by_head", [(16, 3, "bf16", False), (64, 1, "f32", True), (8, 8, "bf16", True)])
+def test_rope_stores_many_ragged_rows(page, K, dtype, by_head):
+    """A ragged batch of some thousand rows, several rows a workgroup: runs that cross
+    workgroups and sequences, rows not stored and rows that cannot be among them, single
+    rows out of order, one sequence of them alone."""
+    announce(f"rope ragged store page {page} K {K} {dtype} by_head {by_head}")
+    rng = np.random.default_rng(page + K)
+    H, dim, rot = 4, 64, 32
+    lens = [0, 5, 3000, 1, 4100, 17, 0, 1900]
+    cap = 4200
+    c = Cache(rng, [0] * len(lens), K, dim, page, dtype, weight=True, by_head=by_head, max_pages=-(-cap // page),
+              spare=sum(-(-n // page) for n in lens) + 2)
+    table = c.table.copy()
+    for b, n in enumerate(lens):
+        for j in range(-(-n // page)):
+            table[b, j] = c.free.pop()
+    table[2, 20] = -1                                  # pages outside the pool
+    table[7, 3] = c.dev.k.shape[0]
+    c.dev.table.copy_(torch.as_tensor(table))
+    seq = np.concatenate([np.full(n, b) for b, n in enumerate(lens)])
+    slot = np.concatenate([np.arange(n) for n in lens])
+    n = len(seq)
+    assert n > 8192
+    tail = rng.permutation(np.flatnonzero(seq == 7))   # the last sequence out of order
+    slot[seq == 7] = slot[tail]
+    skip = rng.random(n) < 0.02
+    skip[np.flatnonzero(seq == 4)[-3:]] = True         # a length that ends before the run does
+    slot = np.where(skip, -1 - rng.integers(0, 5, n), slot)
+    bad_seq = (rng.random(n) < 0.01) & ~skip
+    seq = np.where(bad_seq, rng.choice([-1, len(lens), 2 ** 31 - 1], n), seq)
+    past = (rng.random(n) < 0.01) & ~skip & ~bad_seq
+    slot = np.where(past, table.shape[1] * page + rng.integers(0, 9, n), slot)
+    seq, slot = seq.astype(np.int32), slot.astype(np.int32)
+    ok = ~skip & ~bad_seq & ~past
+    pid = np.full(n, -1)
+    pid[ok] = table[seq[ok], slot[ok] // page]
+    stored = ok & (pid >= 0) & (pid < c.dev.k.shape[0])
+    assert (ok & ~stored).any()
+    q, q64 = values(rng, (n, H, dim), dtype)
+    k, k64 = values(rng, (n, K, dim), dtype)
+    v, v64 = values(rng, (n, K, dim), dtype)
+    pos = rng.integers(0, 1_000_000, n).astype(np.int32)
+    turns = F.focus_rope_turns(rot)
+    t64 = turns.cpu().numpy()
+    err = torch.zeros(1, dtype=torch.int32, device=DEV)
+    before = c.dev.k.clone(), c.dev.v.clone()
+    d = lambda a: torch.as_tensor(a).to(DEV)  # noqa: E731
+    qo, ko = F.focus_rope(d(pos), turns, q, k, v, k_out=torch.empty_like(k), cache=c.dev, row_seq=d(seq),
+                          row_slot=d(slot), err=err)
+    assert int(err.item()) == 3
+    _check(qo, q64, pos, t64, "interleaved", False, 1.0, dtype, "q")
+    _check(ko, k64, pos, t64, "interleaved", False, 1.0, dtype, "k")
+    at = d(pid[stored].astype(np.int64)), d((slot[stored] % page).astype(np.int64))
+    assert torch.equal(c.dev.k[at], ko[d(stored)])
+    assert np.array_equal(to64(c.dev.v[at]), v64[stored])
+    for now, was in zip((c.dev.k, c.dev.v), before):
+        now = now.clone()
+        now[at] = was[at]
+        assert torch.equal(now.nan_to_num(7.0), was.nan_to_num(7.0)), "other rows were written"
+    ends = [int(slot[stored & (seq == b)].max(initial=-1)) + 1 for b in range(len(lens))]
+    assert c.dev.length.tolist() == ends
+    w = c.weight.copy()
+    w[seq[stored], :, slot[stored]] = 0.0
+    assert np.array_equal(c.dev.weight.cpu().numpy(), w)
