@@ -391,3 +391,50 @@ def test_decode_weights_hold_the_bits_of_a_float32(D, group):
     o, _ = F.focus_paged_decode(q, cache, softmax_scale=1.0)
     within(to64(o)[0].reshape(K, group, D), np.broadcast_to(ref[:, None, None], (K, group, D)),
            np.broadcast_to(tol[:, None, None], (K, group, D)), "o")
+
+
+@pytest.mark.parametrize("rows,page,split,H,K,dtype", [
+    (20_011, 8, 16_384, 6, 3, "bf16"),         # chunks of two rounds of 1024 pages, and one
+    (20_011, 8, 16_384, 3, 3, "f32"),
+    (50_000, 8, 24_960, 17, 1, "bf16"),        # three and more, more than one tile of heads
+    (532_813, 256, 266_368, 2, 1, "bf16"),     # the second chunk and its rounds begin inside a page
+    (532_813, 256, 266_368, 1, 1, "f32"),
+])
+def test_decode_chunks_of_more_pages_than_are_held_at_a_time(rows, page, split, H, K, dtype):
+    announce(f"paged decode {rows} rows on pages of {page} split {split} {H}/{K} {dtype}")
+    rng = np.random.default_rng(rows + H)
+    c = Cache(rng, [rows, 70], K, 64, page, dtype, weight=True)
+    q, q64 = values(rng, (2, H, 64), dtype)
+    got = F.focus_paged_decode(q, c.dev, split_keys=split)
+    _check(c, q64, got, dtype)
+    again = F.focus_paged_decode(q, c.dev, split_keys=split, weight_decay=0.5)
+    assert torch.equal(again[0], got[0]) and torch.equal(again[1], got[1])
+    _check(c, q64, again, dtype, weight=c.weight, decay=0.5)
+    # an infinity and a NaN in V, in the second round and in the last rows: the sums are
+    # taken again, page by page
+    clean = got[0]
+    for r, col, x in ((1024 * page + 3, 5, float("inf")), (rows - 1, 9, float("nan"))):
+        c.dev.v[int(c.table[0, r // page]), r % page, 0, col] = x
+    o = F.focus_paged_decode(q, c.dev, split_keys=split)[0]
+    G = H // K
+    assert not torch.isfinite(o[0, :G, 5]).any() and torch.isnan(o[0, :G, 9]).all()
+    o[0, :G, 5], o[0, :G, 9] = clean[0, :G, 5], clean[0, :G, 9]
+    assert torch.equal(o, clean)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_decode_bad_pages_past_the_first_round(dtype):
+    """Pages outside the pool in the second round of a chunk's pages, reported and left out."""
+    announce(f"paged decode bad pages past the first round {dtype}")
+    rng = np.random.default_rng(73)
+    rows, page = 12_000, 8
+    c = Cache(rng, [rows], 1, 64, page, dtype, weight=True)
+    seen = np.ones(rows, bool)
+    for j in (1023, 1024, 1300, rows // page - 1):
+        c.dev.table[0, j] = -1 if j % 2 else c.dev.k.shape[0]
+        seen[j * page:(j + 1) * page] = False
+    q, q64 = values(rng, (1, 2, 64), dtype)
+    err = torch.zeros(1, dtype=torch.int32, device=DEV)
+    got = F.focus_paged_decode(q, c.dev, split_keys=16_384, weight_decay=0.25, err=err)
+    assert int(err.item()) == 2
+    _check(c, q64, got, dtype, visible=[seen], weight=c.weight, decay=0.25)
