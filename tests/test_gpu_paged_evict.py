@@ -289,3 +289,44 @@ def test_evict_keeps_all_rows_of_lowest_weights(cap, recent, lowest):
     keep = F.focus_paged_evict(c.dev, out, torch.tensor(budgets, dtype=torch.int32, device=DEV), recent=recent, err=err)
     assert int(err.item()) == 0
     _check(c, out, budgets, recent, keep, old)
+
+
+@pytest.mark.parametrize("budget", [12, 100])
+@pytest.mark.parametrize("side", ["source", "destination"])
+def test_evict_rows_of_bad_pages_are_not_copied(side, budget):
+    """Kept rows whose own page, or the page they go to, lies outside the pool: reported,
+    that place of out as it was, everything else copied."""
+    announce(f"evict bad {side} page, budget {budget}")
+    rng = np.random.default_rng(74)
+    page, K = 8, 2
+    c = Cache(rng, [120, 40], K, 64, page, "bf16", weight=True, max_pages=15)
+    k = torch.full((30, page, K, 64), 9.0, dtype=torch.bfloat16, device=DEV)
+    ids = rng.permutation(30)[:26].reshape(2, 13).astype(np.int32)
+    out = F.PagedCache(k, k.clone(), torch.as_tensor(ids).to(DEV), torch.full((2,), -1, dtype=torch.int32, device=DEV),
+                       torch.full((2, K, 104), -1.0, device=DEV))
+    # rows 40 .. 47 of the first sequence stay, whatever else does
+    c.weight[0, :, 40:48] = 5.0
+    c.dev.weight.copy_(torch.as_tensor(c.weight))
+    if side == "source":
+        c.dev.table[0, 5] = 2 ** 31 - 1
+    else:
+        out.table[0, 0] = 30
+    err = torch.zeros(1, dtype=torch.int32, device=DEV)
+    keep = F.focus_paged_evict(c.dev, out, budget, recent=2, err=err).cpu().numpy()
+    assert int(err.item()) == 2
+    want = [np.full((30, page, K, 64), 9.0) for _ in range(2)]
+    for b, n in enumerate(c.lens):
+        for g in range(K):
+            ref = P.keep(c.weight[b, g, :n], budget, 2)
+            assert keep[b, g, :len(ref)].tolist() == ref
+            missed = 0
+            for j, r in enumerate(ref):
+                if b == 0 and (40 <= r < 48 if side == "source" else j < page):
+                    missed += 1
+                    continue
+                for w, rows in zip(want, (c.k[b], c.v[b])):
+                    w[ids[b, j // page], j % page, g] = rows[r, g]
+            assert b or missed == 8
+    for w, now in zip(want, (out.k, out.v)):
+        assert np.array_equal(now.double().cpu().numpy(), w)
+    assert out.length.tolist() == [min(n, budget) for n in c.lens]
