@@ -64,7 +64,7 @@ __device__ __align__(16) const uint32_t kZeros[256] = {};
 // Workspace: int4 info[batch] {first slot, chunks, rows, rows of a chunk}; for more than
 // kWave sequences int owner[slots]; then the partials of `slots` chunks: float2
 // ml[slots][H], float o[slots][H][D]; then, where weights are accumulated, float
-// score[batch][H][cap] (log2 units).  None where nothing is handed on.
+// score[batch][H][cap] (unscaled).  None where nothing is handed on.
 struct Plan {
   int64_t slots;        // upper bound of the chunks of all sequences
   int64_t target;       // chunks resident at a time (split_keys 0)
@@ -342,6 +342,10 @@ __device__ __forceinline__ V load_row(const void* p) {
   else return __builtin_nontemporal_load(from);
 }
 
+__device__ inline float lse_of(const Args& a, float2 ml) {
+  return ml.y == 0.f ? -INFINITY : fmaf(ml.x, a.sc, log2f(ml.y)) * kLn2;
+}
+
 // SHARED: a KV head has more than 16 query heads, whose workgroups read the same rows.
 template <typename T, int D, bool SHARED>
 __global__ __launch_bounds__(kThreads, resident(D)) void paged_attend(Args a) {
@@ -466,7 +470,7 @@ __global__ __launch_bounds__(kThreads, resident(D)) void paged_attend(Args a) {
         float y[L::kScores], mx = m;
 #pragma unroll
         for (int j = 0; j < L::kScores; ++j) {
-          y[j] = j < live ? s[j / 4][j % 4] * a.sc : -INFINITY;
+          y[j] = j < live ? s[j / 4][j % 4] : -INFINITY;
           mx = fmaxf(mx, y[j]);
         }
         if (score && (decltype(whole)::value || row < seg_end)) {
@@ -475,12 +479,14 @@ __global__ __launch_bounds__(kThreads, resident(D)) void paged_attend(Args a) {
             *reinterpret_cast<float4*>(score + row + j) = make_float4(y[j], y[j + 1], y[j + 2], y[j + 3]);
         }
         mx = max_column(mx);
-        const float alpha = __builtin_amdgcn_exp2f(m - mx);
+        // (scaled after the difference: scaled before, a score of 4096 would be rounded to
+        // 2^-12, and so would the weight)
+        const float alpha = __builtin_amdgcn_exp2f((m - mx) * a.sc);
         m = mx;
         l *= alpha;
 #pragma unroll
         for (int j = 0; j < L::kScores; ++j) {
-          y[j] = __builtin_amdgcn_exp2f(y[j] - m);
+          y[j] = __builtin_amdgcn_exp2f((y[j] - m) * a.sc);
           l += y[j];
         }
 #pragma unroll
@@ -588,7 +594,7 @@ __global__ __launch_bounds__(kThreads, resident(D)) void paged_attend(Args a) {
     for (int w = w0 + 1; w < w0 + by; ++w) {
       const float2 other = s_ml[w][h];
       const float M = fmaxf(ml.x, other.x);
-      const float f = __builtin_amdgcn_exp2f(ml.x - M), f2 = __builtin_amdgcn_exp2f(other.x - M);
+      const float f = __builtin_amdgcn_exp2f((ml.x - M) * a.sc), f2 = __builtin_amdgcn_exp2f((other.x - M) * a.sc);
       ml = make_float2(M, fmaf(ml.y, f, other.y * f2));
       y = y * f + *reinterpret_cast<const f32x4*>(&s_o[w][h][e]) * f2;
     }
@@ -600,7 +606,7 @@ __global__ __launch_bounds__(kThreads, resident(D)) void paged_attend(Args a) {
       if constexpr (L::kBf16)
         *reinterpret_cast<u32x2*>(o_at) = u32x2{focus::pack_bf16x2(y[0], y[1]), focus::pack_bf16x2(y[2], y[3])};
       else *reinterpret_cast<f32x4*>(o_at) = y;
-      if (e == 0 && a.d.lse) a.d.lse[at] = ml.y == 0.f ? -INFINITY : (ml.x + log2f(ml.y)) * kLn2;
+      if (e == 0 && a.d.lse) a.d.lse[at] = lse_of(a, ml);
     } else {
       *reinterpret_cast<f32x4*>(a.o + slot * D + e) = y;
     }
@@ -615,13 +621,13 @@ __device__ float2 joined(const Args& a, const int4& info, int h) {
   for (int i = lane; i < info.y; i += 64) {
     const float2 y = a.ml[(int64_t)(info.x + i) * H + h];
     const float m = fmaxf(M, y.x);
-    L = L * __builtin_amdgcn_exp2f(M - m) + y.y * __builtin_amdgcn_exp2f(y.x - m);
+    L = L * __builtin_amdgcn_exp2f((M - m) * a.sc) + y.y * __builtin_amdgcn_exp2f((y.x - m) * a.sc);
     M = m;
   }
 #pragma unroll
   for (int k = 32; k >= 1; k >>= 1) {
     const float m2 = __shfl_xor(M, k), l2 = __shfl_xor(L, k), m = fmaxf(M, m2);
-    L = L * __builtin_amdgcn_exp2f(M - m) + l2 * __builtin_amdgcn_exp2f(m2 - m);
+    L = L * __builtin_amdgcn_exp2f((M - m) * a.sc) + l2 * __builtin_amdgcn_exp2f((m2 - m) * a.sc);
     M = m;
   }
   return make_float2(M, L);
@@ -640,7 +646,7 @@ __global__ __launch_bounds__(kThreads) void paged_join(Args a) {
   constexpr int kLanes = D / 4, kGroups = kThreads / kLanes, kFlight = 8, kHeads = 2;
   __shared__ float4 s_o[kGroups][kLanes];
   __shared__ float2 s_ml[kMaxGroup];  // a head's maximum and sum
-  __shared__ float s_lse[kMaxGroup];
+  __shared__ float s_inv[kMaxGroup];  // 1 / the sum
   const focus_paged_kv& c = a.d.cache;
   const int K = c.n_kv_heads, H = a.d.n_heads, G = a.group, tid = threadIdx.x, parts = a.parts;
   // (part 0 of all first: the later ones have nothing to do where sequences are short, and
@@ -683,7 +689,7 @@ __global__ __launch_bounds__(kThreads) void paged_join(Args a) {
   const int first = weighs ? 0 : part, step = weighs ? 1 : parts;
   for (int h = first + tid / 64 * step; h < G; h += kWaves * step) {
     const float2 ml = joined(a, info, g * G + h);
-    if (tid % 64 == 0) s_ml[h] = ml, s_lse[h] = ml.y == 0.f ? INFINITY : ml.x + log2f(ml.y);
+    if (tid % 64 == 0) s_ml[h] = ml, s_inv[h] = ml.y == 0.f ? 0.f : 1.f / ml.y;
   }
   __syncthreads();
   if (merges) {
@@ -695,7 +701,7 @@ __global__ __launch_bounds__(kThreads) void paged_join(Args a) {
 #pragma unroll
         for (int k = 0; k < kFlight; ++k) {
           if (i0 + k * kGroups < info.y) {
-            const float f = __builtin_amdgcn_exp2f(m[k] - ml.x);
+            const float f = __builtin_amdgcn_exp2f((m[k] - ml.x) * a.sc);
             sum.x = fmaf(y[k].x, f, sum.x), sum.y = fmaf(y[k].y, f, sum.y);
             sum.z = fmaf(y[k].z, f, sum.z), sum.w = fmaf(y[k].w, f, sum.w);
           }
@@ -709,7 +715,7 @@ __global__ __launch_bounds__(kThreads) void paged_join(Args a) {
         for (int k = 0; k < kGroups; ++k) z += reinterpret_cast<const float*>(s_o[k])[tid];
         const int64_t at = (int64_t)b * H + g * G + h;
         reinterpret_cast<T*>(a.d.o)[at * D + tid] = (T)(ml.y == 0.f ? 0.f : z / ml.y);
-        if (tid == 0 && a.d.lse) a.d.lse[at] = ml.y == 0.f ? -INFINITY : (ml.x + log2f(ml.y)) * kLn2;
+        if (tid == 0 && a.d.lse) a.d.lse[at] = lse_of(a, ml);
       }
       __syncthreads();
     }
@@ -725,9 +731,9 @@ __global__ __launch_bounds__(kThreads) void paged_join(Args a) {
 #pragma unroll
       for (int k = 0; k < kHeads; ++k) {
         if (r < n && h0 + k < G) {
-          const float lse = s_lse[h0 + k];
-          x[0] += __builtin_amdgcn_exp2f(sc[k].x - lse), x[1] += __builtin_amdgcn_exp2f(sc[k].y - lse);
-          x[2] += __builtin_amdgcn_exp2f(sc[k].z - lse), x[3] += __builtin_amdgcn_exp2f(sc[k].w - lse);
+          const float top = s_ml[h0 + k].x, inv = s_inv[h0 + k];
+          auto add = [&](float& to, float s) { to = fmaf(__builtin_amdgcn_exp2f((s - top) * a.sc), inv, to); };
+          add(x[0], sc[k].x), add(x[1], sc[k].y), add(x[2], sc[k].z), add(x[3], sc[k].w);
         }
       }
     }

@@ -438,3 +438,34 @@ def test_decode_bad_pages_past_the_first_round(dtype):
     got = F.focus_paged_decode(q, c.dev, split_keys=16_384, weight_decay=0.25, err=err)
     assert int(err.item()) == 2
     _check(c, q64, got, dtype, visible=[seen], weight=c.weight, decay=0.25)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,top", [(60, 4096), (60, -4096), (3000, 4096), (3000, 512)])
+def test_decode_large_scores_keep_their_differences(rows, top, dtype):
+    """Scores of thousands, exact in float32, that differ by up to 4: the weights follow from
+    the differences.  Off by: the scale's roundings, 2^-24 + 2^-25 of at most 4 log2 e; the
+    exponential, 2^-23; the sums, each of at most rows / 16 + 16 additions in float32; the
+    division, 2^-23.  Together below rel; o by that and its own sums, lse by its logarithm's
+    and product's roundings.  (Scores scaled and rounded first would be off by 2^-12.)"""
+    announce(f"paged decode large scores {rows} around {top} {dtype}")
+    rng = np.random.default_rng(abs(rows + top))
+    c = Cache(rng, [rows], 1, 64, 64, dtype, weight=True)
+    t = rng.integers(0, 64, rows) / 16.0
+    k = np.zeros((rows, 64))
+    k[:, 0], k[:, 1] = top / 64.0, t
+    at = torch.as_tensor(c.table[0][np.arange(rows) // 64].astype(np.int64)).to(DEV), torch.arange(rows, device=DEV) % 64
+    c.dev.k[at] = torch.as_tensor(k).to(c.dev.k.dtype).to(DEV)[:, None]
+    assert np.array_equal(to64(c.dev.k[at])[:, 0], k)
+    q64 = np.zeros((2, 64))
+    q64[:, 0], q64[0, 1], q64[1, 1] = 64.0, 1.0, -1.0
+    q = torch.as_tensor(q64).to(c.dev.k.dtype).to(DEV)[None]
+    o, lse = F.focus_paged_decode(q, c.dev, softmax_scale=1.0, weight_decay=0.0)
+    ro, rl, rw = P.decode(q64, k[:, None], c.v[0], 1.0)
+    sums = (rows / 16 + 16) * 2.0 ** -24
+    rel = 4 * 1.4427 * (2.0 ** -24 + 2.0 ** -25) + 2 * 2.0 ** -23 + sums
+    vmax = np.abs(c.v[0]).max()
+    within(to64(o)[0], ro, (2 * rel + sums) * vmax + HALF_STEP[dtype] * np.abs(ro), "o")
+    within(to64(lse)[0], rl, rel + np.abs(rl) * 2.0 ** -22, "lse")
+    w = c.dev.weight.cpu().numpy()[0, :, :rows].astype(np.float64)
+    within(w, rw, rw * (2 * rel + 2.0 ** -22), "weight")
