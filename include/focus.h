@@ -746,7 +746,8 @@ enum { FOCUS_ROPE_INTERLEAVED = 0, FOCUS_ROPE_HALF = 1 };
  * q, k, v are optional one by one (NULL): k_out needs k, v needs cache, cache needs k
  * and v.  Rows may lie anywhere: row t of head h at t * row_stride + h * head_stride,
  * so that q, k, v may be views of one projection.  Rows of an output may not overlap;
- * an output may be its own input (same strides). */
+ * an output may be its own input (same strides) and otherwise
+ * have no element in common with an input, the cache or the other output. */
 typedef struct {
   int32_t dtype;
   int32_t n_heads;              /* of q (ignored if NULL)                    */
@@ -856,7 +857,8 @@ typedef struct {
   int32_t* err;
 } focus_paged_evict_desc;
 
-/* Workspace bytes of this descriptor on the current device (may be 0). */
+/* Workspace bytes of this descriptor on the current device (may be 0).  The workspace is
+ * in use until the call's kernels end; calls that share one on overlapping streams race. */
 size_t focus_paged_evict_workspace(const focus_paged_evict_desc* d);
 /* Errors: E_NULL, E_ARG, E_DTYPE, E_SHAPE, E_UNSUPPORTED, E_WORKSPACE, E_HIP.  Where
  * keep_rows or out's table hold fewer rows than m, m is what they hold, and a length

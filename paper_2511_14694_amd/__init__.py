@@ -723,7 +723,8 @@ def focus_rope(pos, turns, q=None, k=None, v=None, layout: int = FOCUS_ROPE_INTE
     """Rotary positions of q [rows, H, D] and k [rows, H_kv, D] (either may be None; any
     row and head strides): pair i of a head's first 2 * len(turns) elements turns by
     pos * turns[i] revolutions (turns: focus_rope_turns; None or empty: nothing turns).
-    inverse: the backward pass, from gradients of the outputs to gradients of q and k.
+    inverse: the backward pass, from gradients of the outputs to gradients of q and k (the
+    call itself records nothing for autograd, like the others here).
     cache: the turned k and v also go to rows row_slot [rows] (int32, negative: not
     stored) of sequences row_seq [rows] (int32) of the paged cache.  Returns (q_out,
     k_out); k_out is only allocated without a cache.  Outputs may be the inputs."""
@@ -797,8 +798,8 @@ def focus_paged_decode_workspace(q, cache: PagedCache, weight_decay=None, split_
 
 def focus_paged_decode(q, cache: PagedCache, o=None, lse=None, weight_decay: Optional[float] = None, workspace=None,
                        split_keys: int = 0, softmax_scale: float = 0.0, want_lse: bool = True, err=None, stream=None):
-    """Attention of one new token of every sequence, q [batch, H, D] (turned), over the
-    rows of a paged cache (the token's own row among them); returns (o, lse).
+    """Attention of one new token of every sequence, q [batch, H, D] (turned; D 64 or
+    128), over the rows of a paged cache (the token's own row among them); returns (o, lse).
     weight_decay: also cache.weight = weight_decay * cache.weight + the step's softmax
     weights, summed over the heads of each KV head."""
     if o is None:

@@ -24,8 +24,9 @@
 // so maximum, sum and rescaling of a query stay in the lanes of its column.  float32
 // takes 16 rows a tile on the 16x16x4 products, which need no permutation at all.
 //
-// 16 sequences of 10 000 rows of 32 heads of 128 (bf16, 2.62 GB) take 401 us, 6.5 TB/s; one
-// of 262 144 rows of 8 heads (1.07 GB) 169, 6.4 TB/s.  Where there is less to read the start
+// 16 sequences of 10 000 rows of 32 heads of 128 (bf16, 2.62 GB) take 403 us, 6.5 TB/s; one
+// of 262 144 rows of 8 heads (1.07 GB) 170, 6.3 TB/s; 16 of 5 000 rows of 32 heads of 128 in
+// float32 (2.62 GB) 458, 5.7 TB/s.  Where there is less to read the start
 // and the second launch count: 64 sequences of 1 to 8 192 rows of 8 heads (0.26 GB), with
 // weights, 71 us, of which 61 in paged_attend and 10 in paged_join.  The first form, one
 // workgroup a (sequence, head) on the vector units, took 2754, 62 241 and 2061.
