@@ -841,9 +841,9 @@ focus_status focus_paged_decode(const focus_paged_decode_desc* d, focus_stream_t
  * out has them); out.length[b] = m; keep[b, g, 0:m] = the kept rows, -1 past them.
  * The copy goes to other pages: a page that another sequence shares stays as it is, and
  * the old pages are free as a whole afterwards.  `out` may lie in the same pool; a page
- * in both tables, or twice in out's, is a race.  out.length may be cache.length or
- * budgets (not a part of either); out.weight and cache.weight may have nothing in common.
- * Rows of out past m are left as they were. */
+ * in both tables, or twice in out's, is a race (one table for both is refused there).
+ * out.length may be cache.length or budgets (not a part of either); out.weight and
+ * cache.weight may have nothing in common.  Rows of out past m are left as they were. */
 typedef struct {
   focus_paged_kv cache;         /* with weight                               */
   focus_paged_kv out;           /* same dtype, heads, head_dim, batch        */

@@ -588,6 +588,9 @@ extern "C" focus_status focus_paged_evict(const focus_paged_evict_desc* d, focus
   if ((over_length && d->out.length != d->cache.length) || (over_budgets && d->out.length != d->budgets) ||
       (d->out.weight && overlap(d->out.weight, weights_of(d->out), d->cache.weight, weights_of(d->cache))))
     return FOCUS_E_ARG;
+  // one table of one pool: rows would be copied over others that are still to be copied
+  if (d->out.table == d->cache.table && d->out.max_pages > 0 && (d->out.k == d->cache.k || d->out.v == d->cache.v))
+    return FOCUS_E_ARG;
   if (heads * std::max<int64_t>(parts, 1) > INT32_MAX / kThreads) return FOCUS_E_SHAPE;
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   const int es = (int)focus::elt_bytes(d->cache.dtype), pieces = d->cache.head_dim * es / 16;

@@ -469,3 +469,49 @@ def test_decode_large_scores_keep_their_differences(rows, top, dtype):
     within(to64(lse)[0], rl, rel + np.abs(rl) * 2.0 ** -22, "lse")
     w = c.dev.weight.cpu().numpy()[0, :, :rows].astype(np.float64)
     within(w, rw, rw * (2 * rel + 2.0 ** -22), "weight")
+
+
+@pytest.mark.parametrize("pages,split", [(4, 0), (80, 0), (80, 128)])
+def test_decode_batch_past_the_grids_second_dimension(pages, split):
+    """33 000 sequences, of short tables and of longer ones whose chunks a launch of its own
+    divides: parts of the batch as by themselves (a given split, or none, fixes the bits), and
+    single sequences against the oracle."""
+    batch, page, D = 33_000, 8, 64
+    announce(f"paged decode {batch} sequences of {pages} pages split {split}")
+    g = torch.Generator(device=DEV).manual_seed(pages)
+    k = torch.randn(4000, page, 1, D, generator=g, device=DEV).to(torch.bfloat16)
+    v = torch.randn(4000, page, 1, D, generator=g, device=DEV).to(torch.bfloat16)
+    table = torch.randint(0, 4000, (batch, pages), generator=g, device=DEV, dtype=torch.int32)
+    n = torch.randint(0, 40, (batch,), generator=g, device=DEV, dtype=torch.int32).clamp(max=pages * page)
+    n[::5000] = pages * page
+    w = torch.rand(batch, 1, pages * page, generator=g, device=DEV)
+    q = torch.randn(batch, 2, D, generator=g, device=DEV).to(torch.bfloat16)
+    for decay in (None, 0.5):
+        old = w.clone()
+        o, lse = F.focus_paged_decode(q, F.PagedCache(k, v, table, n, w), split_keys=split, weight_decay=decay)
+        if decay is None:
+            assert torch.equal(w, old)
+        if split or pages * page <= 256:
+            for b in (0, 4950, 16_300, 32_700, batch - 100):
+                at = slice(b, b + 100)
+                ow = old[at].clone()
+                o1, l1 = F.focus_paged_decode(q[at], F.PagedCache(k, v, table[at], n[at].contiguous(), ow),
+                                              split_keys=split, weight_decay=decay)
+                assert torch.equal(o1, o[at]) and torch.equal(l1, lse[at]) and torch.equal(ow, w[at])
+        for b in (0, 1, 5000, 20_000, 32_767, 32_768, 32_769, batch - 1):
+            m = int(n[b])
+            rows = table[b].long().cpu()[torch.arange(m) // page], torch.arange(m) % page
+            kk, vv = to64(k[rows[0].to(DEV), rows[1].to(DEV)]), to64(v[rows[0].to(DEV), rows[1].to(DEV)])
+            ro, rl, _ = P.decode(to64(q[b]), kk, vv)
+            to, tl, _ = decode_tolerances(to64(q[b]), kk, D ** -0.5, "bf16", vv, ro)
+            within(to64(o[b]), ro, to, f"o[{b}]")
+            within(to64(lse[b]), rl, tl, f"lse[{b}]")
+
+
+def test_decode_q_shared_by_the_batch():
+    """One query for all sequences and heads (strides of 0)."""
+    rng = np.random.default_rng(77)
+    c = Cache(rng, [300, 41], 2, 64, 16, "bf16", weight=True)
+    q, _ = values(rng, (1, 1, 64), "bf16")
+    q = q.expand(2, 4, 64)
+    _check(c, to64(q), F.focus_paged_decode(q, c.dev, weight_decay=1.0), "bf16", weight=c.weight, decay=1.0)

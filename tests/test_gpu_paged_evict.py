@@ -330,3 +330,93 @@ def test_evict_rows_of_bad_pages_are_not_copied(side, budget):
     for w, now in zip(want, (out.k, out.v)):
         assert np.array_equal(now.double().cpu().numpy(), w)
     assert out.length.tolist() == [min(n, budget) for n in c.lens]
+
+
+def test_evict_to_the_same_pages_of_another_pool():
+    """One table for two pools: every page goes to the page of its number."""
+    announce("evict one table, two pools")
+    rng = np.random.default_rng(75)
+    c = Cache(rng, [300, 77], 2, 64, 16, "bf16", weight=True)
+    out = F.PagedCache(torch.full_like(c.dev.k, 9.0), torch.full_like(c.dev.v, 9.0), c.dev.table,
+                       torch.full((2,), -1, dtype=torch.int32, device=DEV))
+    old = out.k.clone(), out.v.clone()
+    keep = F.focus_paged_evict(c.dev, out, 100, recent=7)
+    _check(c, out, [100, 100], 7, keep, old)
+
+
+@pytest.mark.parametrize("batch,K,cap", [(2, 1, 40_960), (33, 4, 36_864)])
+@pytest.mark.parametrize("lowest", [-np.inf, -3e38])
+def test_evict_long_tables_kept_whole(batch, K, cap, lowest):
+    """Tables of more rows than a workgroup holds, whose sequences stay whole, the lowest
+    weights among them; one of each is cut by a row."""
+    announce(f"evict long tables kept whole {batch} x {K} x {cap} {lowest}")
+    rng = np.random.default_rng(cap + batch)
+    lens = [cap, cap - 1] + [int(x) for x in rng.choice([0, 1, 1024, 8192], batch - 2, p=[.3, .3, .39, .01])]
+    c = Cache(rng, lens, K, 8, 1024, "bf16", weight=True, spare=batch * (cap // 1024))
+    w = c.weight.copy()
+    w[:, :, ::3] = lowest
+    w[1, 0] = lowest
+    c.dev.weight.copy_(torch.as_tensor(w))
+    out = c.other(rng, cap)
+    for recent, last in ((0, cap), (100, cap - 2)):
+        budgets = [cap] * batch
+        budgets[1] = last
+        out.k.copy_(c.dev.k)
+        out.weight.fill_(-1.0)
+        old = c.dev.k.clone(), c.dev.v.clone()
+        keep = F.focus_paged_evict(c.dev, out, torch.tensor(budgets, dtype=torch.int32, device=DEV), recent=recent)
+        _check(c, out, budgets, recent, keep, old)
+
+
+def test_evict_and_stored_rows_past_32_bits():
+    """A pool of more than 2^32 bytes (2^31 elements): rows stored in its last pages, and cut
+    to others of its last."""
+    page, K, D = 64, 8, 128
+    n_pages = (1 << 31) // (page * K * D) + 5
+    announce(f"store and evict in a pool of {n_pages} pages")
+    rng = np.random.default_rng(76)
+    k = torch.empty(n_pages, page, K, D, dtype=torch.bfloat16, device=DEV)
+    v = torch.empty_like(k)
+    n = 2 * page - 3
+    table = torch.tensor([[n_pages - 1, n_pages - 4]], dtype=torch.int32, device=DEV)
+    cache = F.PagedCache(k, v, table, torch.zeros(1, dtype=torch.int32, device=DEV), torch.zeros(1, K, 2 * page, device=DEV))
+    kn, vn = (torch.as_tensor(rng.standard_normal((n, K, D)).astype(np.float32)).to(torch.bfloat16).to(DEV) for _ in range(2))
+    rows = torch.arange(n, dtype=torch.int32, device=DEV)
+    F.focus_rope(rows, None, None, kn, vn, cache=cache, row_seq=torch.zeros_like(rows), row_slot=rows)
+    assert cache.length.tolist() == [n]
+    at = table[0].long()[rows.long() // page], rows.long() % page
+    assert torch.equal(k[at], kn) and torch.equal(v[at], vn)
+    w = rng.random((K, 2 * page)).astype(np.float32)
+    cache.weight.copy_(torch.as_tensor(w)[None])
+    out = F.PagedCache(k, v, torch.tensor([[n_pages - 2]], dtype=torch.int32, device=DEV), torch.zeros(1, dtype=torch.int32, device=DEV))
+    keep = F.focus_paged_evict(cache, out, 50, recent=5)
+    for g in range(K):
+        ref = P.keep(w[g, :n], 50, 5)
+        assert keep[0, g].tolist() == ref
+        for pool, new in ((k, kn), (v, vn)):
+            assert torch.equal(pool[n_pages - 2, :50, g], new[torch.as_tensor(ref).to(DEV), g])
+
+
+def test_evict_batch_past_the_grids_second_dimension():
+    """33 000 short sequences."""
+    announce("evict 33 000 sequences")
+    batch, page = 33_000, 8
+    g = torch.Generator(device=DEV).manual_seed(7)
+    k = torch.randn(2 * batch, page, 1, 8, generator=g, device=DEV)
+    ids = torch.randperm(2 * batch, generator=g, device=DEV).to(torch.int32).view(2, batch, 1)
+    n = torch.randint(0, page + 1, (batch,), generator=g, device=DEV, dtype=torch.int32)
+    w = torch.rand(batch, 1, page, generator=g, device=DEV)
+    cache = F.PagedCache(k, k.clone(), ids[0].contiguous(), n, w)
+    out = F.PagedCache(k, cache.v, ids[1].contiguous(), torch.zeros_like(n), torch.zeros_like(w))
+    before = k.clone()
+    keep = F.focus_paged_evict(cache, out, 5, recent=1).cpu().numpy()
+    assert torch.equal(out.length, n.clamp(max=5))
+    for b in range(0, batch, 97):
+        ref = P.keep(w[b, 0, :int(n[b])].cpu().numpy(), 5, 1)
+        assert keep[b, 0, :len(ref)].tolist() == ref and (keep[b, 0, len(ref):] == -1).all()
+    rows = torch.as_tensor(keep[:, 0]).to(DEV).long()
+    live = rows >= 0
+    src, dst = before[ids[0, :, 0].long()], k[ids[1, :, 0].long()]
+    got, want = dst[:, :5, 0], src[:, :, 0].gather(1, rows.clamp(min=0)[..., None].expand(-1, -1, 8))
+    assert torch.equal(got[live], want[live])
+    assert torch.equal(k[ids[0, :, 0].long()], src)

@@ -362,3 +362,21 @@ def test_rope_stores_many_ragged_rows(page, K, dtype, by_head):
     w = c.weight.copy()
     w[seq[stored], :, slot[stored]] = 0.0
     assert np.array_equal(c.dev.weight.cpu().numpy(), w)
+
+
+def test_rope_offsets_past_32_bits():
+    """q of more than 2^31 elements, in place: its last rows as by themselves."""
+    n, H, D = 66_000, 256, 128
+    announce(f"rope {n} x {H} x {D} in place")
+    q = torch.empty(n, H, D, dtype=torch.bfloat16, device=DEV)
+    assert q.numel() > 1 << 31
+    g = torch.Generator(device=DEV).manual_seed(5)
+    ends = [slice(0, 9), slice(65_530, 65_540), slice(n - 9, n)]
+    for at in ends:
+        q[at] = torch.randn(q[at].shape, generator=g, device=DEV).to(torch.bfloat16)
+    pos = torch.arange(n, dtype=torch.int32, device=DEV)
+    turns = F.focus_rope_turns(D)
+    want = [F.focus_rope(pos[at], turns, q[at].clone())[0] for at in ends]
+    F.focus_rope(pos, turns, q, q_out=q)
+    for at, x in zip(ends, want):
+        assert torch.equal(q[at], x)

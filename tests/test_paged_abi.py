@@ -398,3 +398,14 @@ def test_workspaces_are_asked_of_the_tensors_device(monkeypatch):
     F.focus_paged_evict_workspace(c, c, 3)
     F.focus_paged_evict(c, c, 3)
     assert [d for _, d in asked] == [1] * 4 and at == [0], asked
+
+
+def test_paged_evict_refuses_a_cut_in_place():
+    """One table for both sides, in one pool of k or of v."""
+    for k, v in ((FAKE, FAKE), (FAKE, 2 * FAKE), (2 * FAKE, FAKE)):
+        d = _evict_ok()
+        d.out.weight, d.out.k, d.out.v = None, k, v
+        assert d.out.table == d.cache.table
+        assert _call("focus_paged_evict", d) == E_ARG
+        d.out.length = d.cache.length
+        assert _call("focus_paged_evict", d) == E_ARG
