@@ -104,6 +104,14 @@ def _stream(stream, device) -> int:
 # one attribute assignment each took 3).
 
 
+def _on(stream, device):
+    """The context in which a call given stream= allocates: that stream's, torch's own or
+    any object that holds a handle in cuda_stream."""
+    if not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(stream.cuda_stream, device=device)
+    return torch.cuda.stream(stream)
+
+
 def _scratch(nbytes: int, device, stream):
     """Scratch for the duration of one call: allocated on the stream the call's
     kernels run on, so the caching allocator hands the block to other work only
@@ -111,7 +119,7 @@ def _scratch(nbytes: int, device, stream):
     None)."""
     if stream is None:
         return torch.empty(nbytes, dtype=torch.uint8, device=device)
-    with torch.cuda.stream(stream):
+    with _on(stream, device):
         return torch.empty(nbytes, dtype=torch.uint8, device=device)
 
 
@@ -122,7 +130,7 @@ def _empty(shape, dtype, device, stream):
     if stream is None:
         return torch.empty(shape, dtype=dtype, device=device)
     here = torch.cuda.current_stream(device)
-    with torch.cuda.stream(stream):
+    with _on(stream, device):
         t = torch.empty(shape, dtype=dtype, device=device)
     t.record_stream(here)
     return t
@@ -141,7 +149,7 @@ def _input(x, dtype, device, stream):
     if stream is None or (torch.is_tensor(x) and x.dtype is dtype and x.device == device and x.is_contiguous()):
         return torch.as_tensor(x, dtype=dtype).to(device).contiguous()
     here = torch.cuda.current_stream(device)
-    with torch.cuda.stream(stream):
+    with _on(stream, device):
         t = torch.as_tensor(x, dtype=dtype).to(device).contiguous()
     if t is not x:
         t.record_stream(here)

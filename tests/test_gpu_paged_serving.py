@@ -3,6 +3,8 @@ attended with weights accumulated, the cache cut to a budget on the way, decodin
 continued over what is left -- against the float64 oracle, which follows the same loop
 on its own rows.  And FOCUS's own retention over pages: the summary rows of a prefill."""
 
+from types import SimpleNamespace
+
 import numpy as np
 import pytest
 import torch
@@ -314,3 +316,17 @@ def test_a_call_on_another_stream_inside_a_capture():
         got = o.clone(), lse.clone()
         want = F.focus_paged_decode(q, c.dev)
         assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+def test_a_stream_given_by_its_handle():
+    """stream= takes any object with a handle in cuda_stream, also where a call allocates."""
+    announce("a stream by its handle")
+    rng = np.random.default_rng(66)
+    c = Cache(rng, [3000, 100], 2, 64, 64, "bf16", weight=True)
+    q, _ = values(rng, (2, 8, 64), "bf16")
+    want = F.focus_paged_decode(q, c.dev)
+    torch.cuda.synchronize()
+    other = torch.cuda.Stream()
+    got = F.focus_paged_decode(q, c.dev, stream=SimpleNamespace(cuda_stream=other.cuda_stream))
+    other.synchronize()
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])

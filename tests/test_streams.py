@@ -3,6 +3,7 @@ made on that stream, and the caller's own stream is told of it (no GPU is touche
 streams are stand-ins, the library answers every call with success)."""
 
 import contextlib
+from types import SimpleNamespace
 
 import numpy as np
 import pytest
@@ -75,15 +76,15 @@ def test_what_a_call_makes_belongs_to_its_stream(name, monkeypatch):
     monkeypatch.setattr(F, "_launch", lambda *a: None)
     monkeypatch.setattr(F, "_stream", lambda *a: 0)
     monkeypatch.setattr(torch.cuda, "stream", stream)
+    monkeypatch.setattr(torch.cuda, "ExternalStream", lambda handle, device=None: f"stream {handle}")
     monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: current[-1])
     monkeypatch.setattr(torch.Tensor, "record_stream", lambda t, s: told.append(s), raising=False)
     call, count = _calls()[name]
-    for s in ("another", None):
+    for s, name in ((SimpleNamespace(cuda_stream=5), "stream 5"), (None, "the caller's")):
         with Watch(current) as w:
             call(s)
-        made = [x for x in w.made]
-        assert len(made) == count, made
-        assert {x for _, x in made} == {s or "the caller's"}, made
+        assert len(w.made) == count, w.made
+        assert {x for _, x in w.made} == {name}, w.made
         # all but the scratch, which nobody but the kernels reads
         if s:
             assert set(told) == {"the caller's"} and count - 1 <= len(told) <= count
