@@ -13,6 +13,9 @@
  *   focus_rope                         rotary positions, rows stored in a paged cache
  *   focus_paged_decode                 one-token attention over a paged cache
  *   focus_paged_evict                  a paged cache cut down to a budget
+ *   focus_paged_extend                 page tables and slot maps from the rows to come
+ *   focus_paged_append8                rows stored in a paged cache of 8 bits
+ *   focus_paged_attend8                attention of the newest tokens over one
  *
  * Conventions shared by every call
  * --------------------------------
@@ -67,7 +70,9 @@ enum {
   FOCUS_E_HIP = 8          /* the HIP runtime refused a launch                  */
 };
 
-typedef enum { FOCUS_BF16 = 0, FOCUS_F32 = 1 } focus_dtype;
+/* FOCUS_E4M3: 8 bits, 1 sign, 4 exponent (bias 7), 3 mantissa; largest number 448, no
+ * infinity, 0x7f and 0xff NaN.  Only of focus_paged_kv8. */
+typedef enum { FOCUS_BF16 = 0, FOCUS_F32 = 1, FOCUS_E4M3 = 2 } focus_dtype;
 
 /* Visibility rule of focus_window_attn.
  * FOCUS_MASK_CT: the set C(t) of Appendix A.1 ("Objective and visibility"):
@@ -95,7 +100,8 @@ const char* focus_status_str(focus_status s);
 /* sizeof of the descriptor structs below, in declaration order
  * (0 totals, 1 layout, 2 compact, 3 attn, 4 decode, 5 fidelity, 6 gemm,
  * 7 adapter, 8 adapter layer, 9 qkv projection, 10 decode schedule,
- * 11 rope scaling, 12 paged cache, 13 rope, 14 paged decode, 15 paged evict); -1
+ * 11 rope scaling, 12 paged cache, 13 rope, 14 paged decode, 15 paged evict,
+ * 16 paged extend, 17 paged 8-bit cache, 18 paged append, 19 paged attend); -1
  * otherwise.
  * Lets a binding check its mirror of the structs. */
 int64_t focus_struct_size(int32_t which);
@@ -866,6 +872,154 @@ size_t focus_paged_evict_workspace(const focus_paged_evict_desc* d);
  * counts as 0 and a row from or to a page outside the pool is not copied
  * (FOCUS_ERR_BOUNDS for both). */
 focus_status focus_paged_evict(const focus_paged_evict_desc* d, focus_stream_t stream);
+
+/* ------------------------------------------------------------------------ */
+/* Slots of a paged cache                                                    */
+/* ------------------------------------------------------------------------ */
+
+/* Slots for the rows to come and back from the rows that go, for every sequence of a
+ * paged cache (of any type), without the host: page tables, lengths and the maps that
+ * focus_rope, focus_paged_append8 and focus_paged_attend8 take.  With n = length[b],
+ * a = add[b] and P = page_rows:
+ *   a < 0   the last -a rows go (all of them if there are fewer): length[b] = n' =
+ *           max(n + a, 0), table entries ceil(n' / P) .. ceil(n / P) - 1 are pushed on the
+ *           stack free_pages[0 : free_count] in that order and set to -1;
+ *   a > 0   a rows come: table entries ceil(n / P) .. ceil((n + a) / P) - 1 are popped off
+ *           the end of the stack in that order, length[b] = n + a.
+ * All pages are given back before any are taken; in both, sequences come in ascending
+ * order.  A sequence whose table is too short for its rows (or whose rows end past n_rows)
+ * is not served; where pages run out, neither is the first sequence that cannot have all
+ * of its pages nor any after it that needs one.  A sequence that is not served keeps its length
+ * and gets start[b] = -1 (FOCUS_ERR_CAPACITY).
+ *   start[b]            rows before the new ones (a <= 0: the length afterwards)
+ *   cu_rows[b]          sum of max(add, 0) over the sequences before b, served or not (at
+ *                       most 2^31 - 1); b = 0 .. batch
+ *   row_seq[t] = b, row_slot[t] = start[b] + i, row_pos[t] = first_pos[b] + i (first_pos
+ *                       NULL: row_slot[t]) of t = cu_rows[b] + i, 0 <= i < add[b]; row_slot
+ *                       is -1 for the rows of a sequence that is not served (row_pos too
+ *                       without first_pos); all three are -1 past the last row.
+ * Pages that several sequences share must not be given back this way.  No array may have
+ * anything in common with another. */
+typedef struct {
+  int32_t page_rows;            /* a power of two, 8 .. 1024                 */
+  int32_t batch;
+  int32_t max_pages;            /* entries of a sequence in table            */
+  int32_t free_cap;             /* entries of free_pages                     */
+  int32_t* table;               /* [device][batch, max_pages]                */
+  int32_t* length;              /* [device][batch]                           */
+  const int32_t* add;           /* [device][batch]                           */
+  int32_t* free_pages;          /* [device][free_cap]                        */
+  int32_t* free_count;          /* [device][1]                               */
+  const int32_t* first_pos;     /* [device][batch] or NULL                   */
+  int32_t* start;               /* [device][batch]                           */
+  int32_t* cu_rows;             /* [device][batch + 1]                       */
+  int64_t n_rows;               /* of the three maps, below 2^31             */
+  int32_t* row_seq;             /* [device][n_rows], each or NULL            */
+  int32_t* row_slot;
+  int32_t* row_pos;
+  int32_t* err;                 /* optional error word                       */
+} focus_paged_extend_desc;
+
+/* Errors: E_NULL, E_ARG, E_SHAPE, E_UNSUPPORTED (page_rows), E_HIP.  A length outside [0,
+ * max_pages * page_rows] or a free_count outside [0, free_cap] is clipped to it
+ * (FOCUS_ERR_BOUNDS); pages given back past free_cap are lost (FOCUS_ERR_CAPACITY).  With
+ * batch 0 only cu_rows[0] and the maps are written. */
+focus_status focus_paged_extend(const focus_paged_extend_desc* d, focus_stream_t stream);
+
+/* ------------------------------------------------------------------------ */
+/* Paged caches of 8 bits                                                    */
+/* ------------------------------------------------------------------------ */
+
+/* A paged K/V cache in FOCUS_E4M3, with a scale for each block of scale_rows rows and KV
+ * head: row r of sequence b in page p stands for its 8-bit elements times
+ * k_scale[(p * n_kv_heads + g) * (page_rows / scale_rows) + r % page_rows / scale_rows].
+ * Scales may be any float32 (focus_paged_append8 makes powers of two). */
+typedef struct {
+  focus_paged_kv kv;            /* dtype FOCUS_E4M3; strides in elements, whole
+                                   16-byte pieces; weight NULL               */
+  int32_t scale_rows;           /* a power of two, 8 .. page_rows            */
+  int32_t reserved;
+  float* k_scale;               /* [device][n_pages, n_kv_heads,             */
+  float* v_scale;               /*           page_rows / scale_rows]         */
+} focus_paged_kv8;
+
+/* New rows of k and v stored: row cu_rows[b] + i at row start[b] + i of sequence b, for
+ * cu_rows[b] <= cu_rows[b] + i < cu_rows[b + 1] (ascending, within n_rows; rows past the
+ * last are not read).  cu_rows NULL: row b of sequence b alone (n_rows = batch).  start[b] < 0
+ * stores nothing.  Rows that a sequence has from start[b] on are overwritten, or of no
+ * more meaning where the new ones end before them in the same block.  For each block that gets
+ * rows, KV head, and k and v by themselves,
+ *     scale' = max(2^e, its scale if it holds rows before start[b], else 0),
+ *     e      = the least integer >= -126 with |x| <= 448 * 2^e for all finite new x,
+ *     row    = e4m3(x / scale')          (to nearest, ties to even)
+ * and, where the scale has grown, the rows before start[b] become e4m3(row * scale / scale'):
+ * exact for powers of two, but for what falls below the smallest normal number.  An infinity
+ * or NaN is stored as a NaN.  cache.length is raised (never lowered) past the rows; start
+ * may have nothing in common with it.  Pages that several sequences share must not get
+ * rows. */
+typedef struct {
+  focus_paged_kv8 cache;        /* head_dim at most 256, a multiple of 16    */
+  int32_t dtype;                /* of k and v: FOCUS_BF16 or FOCUS_F32       */
+  int32_t reserved;
+  int64_t n_rows;
+  const int32_t* cu_rows;       /* [device][batch + 1] or NULL               */
+  const int32_t* start;         /* [device][batch]                           */
+  const void* k;                /* [device], strides in elements, whole      */
+  int64_t k_row, k_head;        /*   16-byte pieces                          */
+  const void* v;
+  int64_t v_row, v_head;
+  int32_t* err;                 /* optional error word                       */
+} focus_paged_append8_desc;
+
+/* Errors: E_NULL, E_ARG, E_DTYPE, E_SHAPE (n_rows of 2^31, or not batch without cu_rows,
+ * among others), E_UNSUPPORTED, E_HIP.  A block in a page outside the pool
+ * (FOCUS_ERR_BOUNDS) and rows past max_pages * page_rows (FOCUS_ERR_CAPACITY) are not
+ * stored; offsets outside [0, n_rows] are clipped to it (FOCUS_ERR_BOUNDS). */
+focus_status focus_paged_append8(const focus_paged_append8_desc* d, focus_stream_t stream);
+
+/* Attention of the newest tokens of every sequence over its cached rows: of sequence b the
+ * rows cu_rows[b] .. cu_rows[b + 1] - 1 of q, m of them, are its last m tokens (whose own
+ * rows are in the cache), so that token i sees the first n_i = length[b] - (m - 1 - i):
+ *     o[t, h]   = softmax(scale * q[t, h] . k[b, 0:n_i, g]^T) . v,  g = h / (H / H_kv)
+ *     lse[t, h] = log sum exp(scale * q[t, h] . k)
+ * A token with n_i <= 0 has o = 0 and lse = -inf; what it does not see has no effect.
+ * cu_rows NULL: one token of every sequence, row b (n_rows = batch).  max_rows bounds m; rows of
+ * o and lse past the last sequence's are left as they were.  Scores, weights and sums are
+ * float32; each element of k and v enters exactly.
+ * The rows of a sequence are split over several workgroups, joined by log-sum-exp;
+ * with split_keys = 0 the split follows the lengths of the whole batch, so that a
+ * sequence's bits may differ by float32 rounding with what else is in the batch; a
+ * given split_keys fixes them.  Results are deterministic. */
+typedef struct {
+  focus_paged_kv8 cache;        /* head_dim 64 or 128                        */
+  int32_t dtype;                /* of q and o: FOCUS_BF16 or FOCUS_F32       */
+  int32_t n_heads;
+  int32_t max_rows;             /* >= 1; times n_heads / n_kv_heads <= 512   */
+  int32_t split_keys;           /* rows per workgroup, multiple of 128; 0: auto */
+  float softmax_scale;          /* <= 0: 1/sqrt(head_dim)                    */
+  int32_t reserved;
+  int64_t n_rows;
+  const int32_t* cu_rows;       /* [device][batch + 1] or NULL               */
+  const void* q;                /* [n_rows, n_heads, head_dim], strides in   */
+  int64_t q_row, q_head;        /*   elements, whole 16-byte pieces          */
+  void* o;                      /* [n_rows, n_heads, head_dim] contiguous    */
+  float* lse;                   /* [n_rows, n_heads] or NULL                 */
+  void* workspace;
+  size_t workspace_bytes;
+  int32_t* err;
+} focus_paged_attend8_desc;
+
+/* Workspace bytes of this descriptor on the current device (0 where none is needed, or the
+ * call refuses it).  The workspace is in use until the call's kernels end; calls that share
+ * one on overlapping streams race. */
+size_t focus_paged_attend8_workspace(const focus_paged_attend8_desc* d);
+/* Errors: E_NULL, E_ARG, E_DTYPE, E_SHAPE (as focus_paged_decode; n_rows not batch without
+ * cu_rows), E_UNSUPPORTED, E_WORKSPACE, E_HIP.  Rows of a page outside the pool are left
+ * out of the softmax (FOCUS_ERR_BOUNDS); a length outside [0, max_pages * page_rows] is
+ * clipped to it (FOCUS_ERR_CAPACITY); the rows of a sequence that has more than max_rows
+ * (FOCUS_ERR_CAPACITY) or whose offsets do not ascend within [0, n_rows]
+ * (FOCUS_ERR_BOUNDS) are left as they were. */
+focus_status focus_paged_attend8(const focus_paged_attend8_desc* d, focus_stream_t stream);
 
 #ifdef __cplusplus
 }

@@ -19,6 +19,12 @@ Serving over a paged cache:
     q, _   = focus_rope(pos, turns, q, k, v, cache=cache, ...)   # turn q and k, store k and v
     o, lse = focus_paged_decode(q, cache, weight_decay=1.0)      # one token, weights kept
     keep   = focus_paged_evict(cache, out, budget, recent)       # cut down to a budget
+
+with its page tables kept on the device, and in 8 bits:
+
+    rows   = focus_paged_extend(table, length, page_rows, add, free_pages, free_count, n)
+    focus_paged_append8(k, v, cache8, rows.start, rows.cu_rows)  # rows stored in 8 bits
+    o, lse = focus_paged_attend8(q, cache8, rows.cu_rows, max_rows=4)  # the newest tokens
 """
 
 from __future__ import annotations
@@ -31,8 +37,8 @@ import numpy as np
 import torch
 
 from ._abi import (AdapterDesc, AdapterLayerDesc, AttnDesc, CompactDesc, DecodeDesc, DecodeSched, FidelityDesc, FocusError, GemmDesc, LayoutDesc, LayoutTotals,
-                   PagedDecodeDesc, PagedEvictDesc, PagedKv, QkvDesc, RopeDesc, RopeScaling,
-                   FOCUS_BF16, FOCUS_F32, FOCUS_MASK_CT, FOCUS_MASK_KMER_LOCAL,
+                   PagedAppend8Desc, PagedAttend8Desc, PagedDecodeDesc, PagedEvictDesc, PagedExtendDesc, PagedKv, PagedKv8, QkvDesc,
+                   RopeDesc, RopeScaling, FOCUS_BF16, FOCUS_F32, FOCUS_E4M3, FOCUS_MASK_CT, FOCUS_MASK_KMER_LOCAL,
                    FOCUS_TOK_BASE, FOCUS_TOK_SUMMARY, FOCUS_STEP_SUMMARY, FOCUS_STEP_WINDOW_END,
                    FOCUS_ERR_CAPACITY, FOCUS_ERR_BOUNDS, FOCUS_ERR_PLAN,
                    FOCUS_FID_LOGITS, FOCUS_FID_PROBS, FOCUS_FID_N,
@@ -45,11 +51,12 @@ __all__ = ["focus_layout_plan", "focus_layout", "focus_compact_kv", "focus_windo
            "focus_fidelity", "focus_gemm", "focus_adapter_attn", "focus_adapter_layer",
            "focus_adapter_layer_workspace", "focus_qkv_project", "focus_abi_version", "Layout", "LayoutTotals", "FocusError",
            "FOCUS_FID_LOGITS", "FOCUS_FID_PROBS", "FOCUS_FID_N",
-           "FOCUS_BF16", "FOCUS_F32", "FOCUS_MASK_CT", "FOCUS_MASK_KMER_LOCAL",
+           "FOCUS_BF16", "FOCUS_F32", "FOCUS_E4M3", "FOCUS_MASK_CT", "FOCUS_MASK_KMER_LOCAL",
            "FOCUS_TOK_BASE", "FOCUS_TOK_SUMMARY", "FOCUS_STEP_SUMMARY", "FOCUS_STEP_WINDOW_END",
            "FOCUS_ERR_CAPACITY", "FOCUS_ERR_BOUNDS", "FOCUS_ERR_PLAN",
            "PagedCache", "focus_rope_turns", "focus_rope", "focus_paged_decode", "focus_paged_decode_workspace",
-           "focus_paged_evict", "focus_paged_evict_workspace",
+           "focus_paged_evict", "focus_paged_evict_workspace", "PagedRows", "focus_paged_extend", "PagedCache8",
+           "focus_paged_append8", "focus_paged_attend8", "focus_paged_attend8_workspace",
            "FOCUS_ROPE_NONE", "FOCUS_ROPE_LINEAR", "FOCUS_ROPE_BASE", "FOCUS_ROPE_BANDS",
            "FOCUS_ROPE_INTERLEAVED", "FOCUS_ROPE_HALF"]
 
@@ -869,3 +876,155 @@ def focus_paged_evict(cache: PagedCache, out: PagedCache, budget, recent: int = 
             d.workspace, d.workspace_bytes = workspace.data_ptr(), n
     _launch("focus_paged_evict", d, cache.k.get_device(), stream)
     return keep
+
+
+@dataclass
+class PagedRows:
+    """The rows that focus_paged_extend found slots for: int32 tensors.
+
+    start    [batch] rows of each sequence before the new ones; -1: not served
+    cu_rows  [batch + 1] offsets of the sequences' rows
+    row_seq, row_slot, row_pos  [n_rows] sequence, row of the cache and position of each
+             row, as focus_rope takes them; slot -1: not stored
+    """
+    start: torch.Tensor
+    cu_rows: torch.Tensor
+    row_seq: torch.Tensor
+    row_slot: torch.Tensor
+    row_pos: torch.Tensor
+
+
+def focus_paged_extend(table, length, page_rows: int, add, free_pages, free_count, n_rows: int, first_pos=None,
+                       out: Optional[PagedRows] = None, err=None, stream=None) -> PagedRows:
+    """Slots of a paged cache for the rows that come and back from those that go, without
+    the host: sequence b takes add[b] rows behind its length[b], or gives back its last
+    -add[b].  table [batch, max_pages] and length [batch] (a PagedCache's or PagedCache8's)
+    are changed; pages are popped off and pushed on the end of free_pages[0 : free_count]
+    (int32; free_count one element).  n_rows: how many rows come at most, the size of the
+    three maps; a sequence whose rows do not all fit (maps, table or free pages) is not
+    served: start -1, slots -1.  first_pos [batch]: position of the first new row (default:
+    its slot).  out: a PagedRows of these sizes to be written again.  All arrays int32."""
+    dev = length.get_device()
+    if table.dim() != 2:
+        raise ValueError("table must be [batch, max_pages]")
+    batch, max_pages = table.shape
+    n_rows, page_rows = _i32(n_rows, "n_rows"), _i32(page_rows, "page_rows")
+    if out is None:
+        n = max(n_rows, 0)
+        # one allocation for all five
+        buf = _empty((2 * batch + 1 + 3 * n,), torch.int32, length.device, stream)
+        out = PagedRows(*buf.split([batch, batch + 1, n, n, n]))
+    i32 = torch.int32
+    d = PagedExtendDesc(page_rows, batch, max_pages, free_pages.numel(), _need(table, i32, None, dev, "table"),
+                        _need(length, i32, (batch,), dev, "length"), _need(add, i32, (batch,), dev, "add"),
+                        _need(free_pages, i32, None, dev, "free_pages"), _need(free_count, i32, (1,), dev, "free_count"),
+                        None if first_pos is None else _need(first_pos, i32, (batch,), dev, "first_pos"),
+                        _need(out.start, i32, (batch,), dev, "out.start"),
+                        _need(out.cu_rows, i32, (batch + 1,), dev, "out.cu_rows"), n_rows,
+                        _need(out.row_seq, i32, (n_rows,), dev, "out.row_seq"),
+                        _need(out.row_slot, i32, (n_rows,), dev, "out.row_slot"),
+                        _need(out.row_pos, i32, (n_rows,), dev, "out.row_pos"),
+                        None if err is None else _err_ptr(err, dev))
+    _launch("focus_paged_extend", d, dev, stream)
+    return out
+
+
+@dataclass
+class PagedCache8:
+    """A paged K/V cache in 8 bits (focus_paged_kv8), each block of rows and KV head with a
+    scale of its own.
+
+    k, v              float8_e4m3fn [n_pages, page_rows, H_kv, D], strides as PagedCache's
+    k_scale, v_scale  float32 [n_pages, H_kv, page_rows / scale_rows], contiguous; their last
+                      dimension sets scale_rows, a power of two, 8 to page_rows
+    table, length     as PagedCache's
+    """
+    k: torch.Tensor
+    v: torch.Tensor
+    k_scale: torch.Tensor
+    v_scale: torch.Tensor
+    table: torch.Tensor
+    length: torch.Tensor
+
+    def desc(self) -> PagedKv8:
+        k, v, table, scale = self.k, self.v, self.table, self.k_scale
+        shape, strides, dev = k.shape, k.stride(), k.get_device()
+        if (len(shape) != 4 or v.shape != shape or k.dtype is not torch.float8_e4m3fn or v.dtype is not k.dtype
+                or v.get_device() != dev or v.stride() != strides or strides[3] != 1):
+            raise ValueError("k and v must be float8_e4m3fn [n_pages, page_rows, H_kv, D] of one device and strides, "
+                             "with unit stride in D")
+        n_pages, rows, heads, dim = shape
+        batch_pages, blocks = table.shape, scale.shape[-1]
+        if len(batch_pages) != 2:
+            raise ValueError("table must be [batch, max_pages]")
+        batch, max_pages = batch_pages
+        if blocks < 1 or rows % blocks:
+            raise ValueError("scales must be [n_pages, H_kv, page_rows / scale_rows]")
+        if n_pages <= 1 or heads <= 1:
+            # the stride of a dimension of one element says nothing: replaced by one that passes
+            strides = [dim if n <= 1 else st for n, st in zip(shape, strides)]
+        ss = (n_pages, heads, blocks)
+        return PagedKv8(PagedKv(FOCUS_E4M3, heads, dim, rows, n_pages, k.data_ptr(), v.data_ptr(), strides[0], strides[1],
+                                strides[2], batch, max_pages, _need(table, torch.int32, None, dev, "table"),
+                                _need(self.length, torch.int32, (batch,), dev, "length"), None, 0), rows // blocks, 0,
+                        _need(scale, torch.float32, ss, dev, "k_scale"),
+                        _need(self.v_scale, torch.float32, ss, dev, "v_scale"))
+
+
+def focus_paged_append8(k, v, cache: PagedCache8, start, cu_rows=None, err=None, stream=None):
+    """New rows of k and v [rows, H_kv, D] (bfloat16 or float32, any row and head strides)
+    stored in an 8-bit paged cache: rows cu_rows[b] : cu_rows[b + 1] behind the first start[b]
+    of sequence b (cu_rows None: one row of every sequence), cache.length raised past them.
+    start (negative: not stored) and cu_rows int32, as focus_paged_extend gives them; start may
+    not be cache.length itself.  A block's scale is the least power of two that its new
+    rows fit, or its old one if that is greater and rows are left in it."""
+    c = cache.desc()
+    dev, dtype, kv = cache.k.get_device(), k.dtype, c.kv
+    if k.dim() != 3 or dtype not in _DTYPES:
+        raise ValueError("k must be [rows, heads, D], bfloat16 or float32")
+    shape = (k.shape[0], kv.n_kv_heads, kv.head_dim)
+    d = PagedAppend8Desc(c, _DTYPES[dtype], 0, shape[0],
+                         None if cu_rows is None else _need(cu_rows, torch.int32, (kv.batch + 1,), dev, "cu_rows"),
+                         _need(start, torch.int32, (kv.batch,), dev, "start"), *_rows(k, shape, dtype, dev, "k"),
+                         *_rows(v, shape, dtype, dev, "v"), None if err is None else _err_ptr(err, dev))
+    _launch("focus_paged_append8", d, dev, stream)
+
+
+def _paged_attend8_desc(q, cache, cu_rows, max_rows, o, lse, workspace, split_keys, softmax_scale, err):
+    c = cache.desc()
+    kv, dev, dtype, shape = c.kv, q.get_device(), q.dtype, q.shape
+    if len(shape) != 3 or shape[2] != kv.head_dim or dev != cache.k.get_device() or dtype not in _DTYPES:
+        raise ValueError("q must be [rows, heads, D], bfloat16 or float32, of the cache's head_dim and device")
+    return PagedAttend8Desc(c, _DTYPES[dtype], shape[1], _i32(max_rows, "max_rows"), _i32(split_keys, "split_keys"),
+                            float(softmax_scale), 0, shape[0],
+                            None if cu_rows is None else _need(cu_rows, torch.int32, (kv.batch + 1,), dev, "cu_rows"),
+                            *_rows(q, shape, dtype, dev, "q"), None if o is None else _need(o, dtype, shape, dev, "o"),
+                            None if lse is None else _need(lse, torch.float32, shape[:2], dev, "lse"),
+                            *_workspace(workspace, dev), None if err is None else _err_ptr(err, dev))
+
+
+def focus_paged_attend8_workspace(q, cache: PagedCache8, cu_rows=None, max_rows: int = 1, split_keys: int = 0) -> int:
+    d = _paged_attend8_desc(q, cache, cu_rows, max_rows, None, None, None, split_keys, 0.0, None)
+    return _query("focus_paged_attend8_workspace", d, q.get_device())
+
+
+def focus_paged_attend8(q, cache: PagedCache8, cu_rows=None, max_rows: int = 1, o=None, lse=None, workspace=None,
+                        split_keys: int = 0, softmax_scale: float = 0.0, want_lse: bool = True, err=None, stream=None):
+    """Attention of the newest tokens of every sequence over an 8-bit paged cache that holds
+    their rows already: q [rows, H, D] (turned; bfloat16 or float32; D 64 or 128), rows
+    cu_rows[b] : cu_rows[b + 1] (int32 [batch + 1], at most max_rows of them) the last ones of
+    sequence b in order, each seeing the rows up to its own (cu_rows None: one token of every
+    sequence).  Returns (o, lse); rows past cu_rows[batch] are left as they were."""
+    if o is None:
+        o = _empty_like(q, stream)
+    if lse is None and want_lse:
+        lse = q.new_empty(*q.shape[:2], dtype=torch.float32) if stream is None else \
+            _empty(q.shape[:2], torch.float32, q.device, stream)
+    d = _paged_attend8_desc(q, cache, cu_rows, max_rows, o, lse, workspace, split_keys, softmax_scale, err)
+    if workspace is None:
+        n = _query("focus_paged_attend8_workspace", d, q.get_device())
+        if n > 0:
+            workspace = _scratch(n, q.device, stream)
+            d.workspace, d.workspace_bytes = workspace.data_ptr(), n
+    _launch("focus_paged_attend8", d, q.get_device(), stream)
+    return o, lse

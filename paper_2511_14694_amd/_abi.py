@@ -11,7 +11,7 @@ FOCUS_OK = 0
 STATUS_NAMES = {0: "FOCUS_OK", 1: "FOCUS_E_NULL", 2: "FOCUS_E_ARG", 3: "FOCUS_E_SHAPE",
                 4: "FOCUS_E_DTYPE", 5: "FOCUS_E_UNSUPPORTED", 6: "FOCUS_E_WORKSPACE",
                 7: "FOCUS_E_CAPACITY", 8: "FOCUS_E_HIP"}
-FOCUS_BF16, FOCUS_F32 = 0, 1
+FOCUS_BF16, FOCUS_F32, FOCUS_E4M3 = 0, 1, 2
 FOCUS_MASK_CT, FOCUS_MASK_KMER_LOCAL = 0, 1
 FOCUS_TOK_BASE, FOCUS_TOK_SUMMARY = 0, 1
 FOCUS_STEP_SUMMARY, FOCUS_STEP_WINDOW_END = 1, 2
@@ -153,8 +153,30 @@ class PagedEvictDesc(C.Structure):
                 ("keep_rows", i64), ("workspace", p), ("workspace_bytes", sz), ("err", p)]
 
 
+class PagedExtendDesc(C.Structure):
+    _fields_ = [("page_rows", i32), ("batch", i32), ("max_pages", i32), ("free_cap", i32), ("table", p), ("length", p),
+                ("add", p), ("free_pages", p), ("free_count", p), ("first_pos", p), ("start", p), ("cu_rows", p),
+                ("n_rows", i64), ("row_seq", p), ("row_slot", p), ("row_pos", p), ("err", p)]
+
+
+class PagedKv8(C.Structure):
+    _fields_ = [("kv", PagedKv), ("scale_rows", i32), ("reserved", i32), ("k_scale", p), ("v_scale", p)]
+
+
+class PagedAppend8Desc(C.Structure):
+    _fields_ = [("cache", PagedKv8), ("dtype", i32), ("reserved", i32), ("n_rows", i64), ("cu_rows", p), ("start", p),
+                ("k", p), ("k_row", i64), ("k_head", i64), ("v", p), ("v_row", i64), ("v_head", i64), ("err", p)]
+
+
+class PagedAttend8Desc(C.Structure):
+    _fields_ = [("cache", PagedKv8), ("dtype", i32), ("n_heads", i32), ("max_rows", i32), ("split_keys", i32),
+                ("softmax_scale", f32), ("reserved", i32), ("n_rows", i64), ("cu_rows", p), ("q", p), ("q_row", i64),
+                ("q_head", i64), ("o", p), ("lse", p), ("workspace", p), ("workspace_bytes", sz), ("err", p)]
+
+
 STRUCTS = [LayoutTotals, LayoutDesc, CompactDesc, AttnDesc, DecodeDesc, FidelityDesc, GemmDesc, AdapterDesc,
-           AdapterLayerDesc, QkvDesc, DecodeSched, RopeScaling, PagedKv, RopeDesc, PagedDecodeDesc, PagedEvictDesc]
+           AdapterLayerDesc, QkvDesc, DecodeSched, RopeScaling, PagedKv, RopeDesc, PagedDecodeDesc, PagedEvictDesc,
+           PagedExtendDesc, PagedKv8, PagedAppend8Desc, PagedAttend8Desc]
 
 # name -> (restype, argtypes): every symbol include/focus.h declares
 SYMBOLS = {
@@ -185,6 +207,10 @@ SYMBOLS = {
     "focus_paged_decode": (i32, [C.POINTER(PagedDecodeDesc), p]),
     "focus_paged_evict_workspace": (sz, [C.POINTER(PagedEvictDesc)]),
     "focus_paged_evict": (i32, [C.POINTER(PagedEvictDesc), p]),
+    "focus_paged_extend": (i32, [C.POINTER(PagedExtendDesc), p]),
+    "focus_paged_append8": (i32, [C.POINTER(PagedAppend8Desc), p]),
+    "focus_paged_attend8_workspace": (sz, [C.POINTER(PagedAttend8Desc)]),
+    "focus_paged_attend8": (i32, [C.POINTER(PagedAttend8Desc), p]),
 }
 
 

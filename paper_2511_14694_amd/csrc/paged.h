@@ -27,9 +27,9 @@ inline bool disjoint_rows(int64_t row, const int64_t (&strides)[N], const int64_
   return true;
 }
 
-// Checks of a cache's description; E_OK for batch 0 whatever the pointers.
-inline focus_status check_paged(const focus_paged_kv& c) {
-  const int64_t es = elt_bytes(c.dtype);
+// Checks of a cache's description, elements of es bytes; E_OK for batch 0 whatever the
+// pointers.
+inline focus_status check_paged(const focus_paged_kv& c, int64_t es) {
   if (es == 0) return FOCUS_E_DTYPE;
   if (c.n_kv_heads <= 0 || c.head_dim <= 0 || c.n_pages < 0 || c.batch < 0 || c.max_pages < 0) return FOCUS_E_ARG;
   if (c.head_dim > 256 || !pieces16(c.head_dim, es)) return FOCUS_E_UNSUPPORTED;
@@ -46,6 +46,21 @@ inline focus_status check_paged(const focus_paged_kv& c) {
   if (!aligned16(c.k) || !aligned16(c.v) || (reinterpret_cast<uintptr_t>(c.table) & 3u) ||
       (reinterpret_cast<uintptr_t>(c.length) & 3u) || (reinterpret_cast<uintptr_t>(c.weight) & 3u))
     return FOCUS_E_ARG;
+  return FOCUS_OK;
+}
+
+inline focus_status check_paged(const focus_paged_kv& c) { return check_paged(c, elt_bytes(c.dtype)); }
+
+// The same of a cache of 8 bits.
+inline focus_status check_paged8(const focus_paged_kv8& c) {
+  const focus_status st = check_paged(c.kv, c.kv.dtype == FOCUS_E4M3 ? 1 : 0);
+  if (st != FOCUS_OK) return st;
+  if (c.kv.weight || c.scale_rows < 8 || c.scale_rows > c.kv.page_rows || (c.scale_rows & (c.scale_rows - 1)))
+    return FOCUS_E_UNSUPPORTED;
+  // (indexes of scales within a page in 32 bits)
+  if ((int64_t)c.kv.n_kv_heads * (c.kv.page_rows / c.scale_rows) > INT32_MAX) return FOCUS_E_SHAPE;
+  if (c.kv.batch > 0 && c.kv.n_pages > 0 && (!c.k_scale || !c.v_scale)) return FOCUS_E_NULL;
+  if ((reinterpret_cast<uintptr_t>(c.k_scale) & 3u) || (reinterpret_cast<uintptr_t>(c.v_scale) & 3u)) return FOCUS_E_ARG;
   return FOCUS_OK;
 }
 

@@ -1,0 +1,240 @@
+"""focus_paged_attend8 on the GPU against the float64 oracle (tolerances:
+oracle.paged8.attend_tolerances)."""
+
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2511_14694_amd as F
+from gpu_util import DEV, announce, to64
+from oracle import paged8 as O
+from paged8_util import NAN, Cache8, i32
+from paged_util import values, within
+
+pytestmark = pytest.mark.gpu
+
+
+def _check(c, q64, counts, got, dtype, scale=None, visible=None, tol=1.0):
+    o, lse = to64(got[0]), to64(got[1])
+    D = q64.shape[2]
+    sc = D ** -0.5 if scale is None else scale
+    at = 0
+    for b, (n, m) in enumerate(zip(c.lens, counts)):
+        k, v = c.rows(b, n, "k"), c.rows(b, n, "v")
+        q = q64[at:at + m]
+        seen = np.ones(n, bool) if visible is None else visible[b]
+        with np.errstate(invalid="ignore"):
+            ro, rl = O.attend(q, k, v, sc, seen)
+        to, tl = O.attend_tolerances(q, np.nan_to_num(k[seen]), np.nan_to_num(v[seen]), sc, dtype, np.nan_to_num(ro))
+        within(o[at:at + m], ro, to * tol, f"o[{b}]")
+        within(lse[at:at + m], rl, tl * tol, f"lse[{b}]")
+        at += m
+
+
+def _offsets(counts):
+    return i32(np.concatenate([[0], np.cumsum(counts)]))
+
+
+CASES = [
+    # lens, tokens, H, K, D, page, block, dtype, by_head
+    ([1], [1], 1, 1, 64, 8, 8, "f32", False),
+    ([1], [1], 32, 8, 128, 64, 16, "bf16", False),
+    ([137], [1], 32, 8, 128, 64, 32, "bf16", False),
+    ([0, 5, 0], [1, 1, 1], 4, 2, 64, 16, 8, "bf16", False),
+    ([31, 32, 33, 7, 8, 9], [1, 2, 3, 1, 0, 2], 6, 2, 128, 8, 8, "bf16", False),
+    ([15, 16, 17, 63, 65], [4, 4, 4, 4, 4], 6, 6, 64, 16, 16, "f32", True),
+    ([300, 1, 2021], [3, 1, 2], 6, 2, 64, 32, 8, "f32", True),
+    ([1000, 129, 127, 128], [5, 5, 5, 5], 8, 8, 128, 128, 64, "bf16", True),
+    ([513, 90], [1, 1], 16, 1, 128, 16, 16, "bf16", False),
+    ([257, 40], [7, 3], 40, 2, 64, 16, 8, "bf16", False),          # 20 heads of a KV head, 7 tokens: nine tiles
+    ([257, 70], [2, 1], 34, 2, 128, 16, 16, "f32", False),
+    ([3000], [16], 3, 3, 128, 1024, 256, "bf16", False),
+    ([5000, 10, 2500], [1, 4, 2], 8, 2, 128, 64, 16, "bf16", False),
+    ([5000, 10, 2500], [2, 2, 2], 4, 4, 128, 16, 8, "f32", False),
+    ([3, 2, 9], [3, 5, 12], 2, 1, 64, 8, 8, "bf16", False),         # tokens that see nothing
+]
+
+
+@pytest.mark.parametrize("lens,counts,H,K,D,page,block,dtype,by_head", CASES)
+@pytest.mark.parametrize("split", [0, 128, 640])
+def test_attend_matches_oracle(lens, counts, H, K, D, page, block, dtype, by_head, split):
+    announce(f"attend8 {lens} {counts} {H}/{K} x {D} page {page} block {block} {dtype} by_head {by_head} split {split}")
+    rng = np.random.default_rng(sum(lens) + H + D)
+    c = Cache8(rng, lens, K, D, page, block, by_head=by_head, padded=not by_head and D == 64, odd_scales=split == 640)
+    q, q64 = values(rng, (sum(counts), H, D), dtype, 1.5)
+    err = torch.zeros(1, dtype=torch.int32, device=DEV)
+    cu = None if counts == [1] * len(lens) and split else _offsets(counts)
+    got = F.focus_paged_attend8(q, c.dev, cu, max_rows=max(counts), split_keys=split, err=err)
+    _check(c, q64, counts, got, dtype)
+    assert err.item() == 0
+    again = F.focus_paged_attend8(q, c.dev, cu, max_rows=max(counts), split_keys=split)
+    assert torch.equal(again[0], got[0]) and torch.equal(again[1], got[1]), "not deterministic"
+    # a greater bound of the tokens changes nothing but the split
+    if split and (max(counts) + 3) * H // K <= 512:
+        more = F.focus_paged_attend8(q, c.dev, cu, max_rows=max(counts) + 3, split_keys=split)
+        _check(c, q64, counts, more, dtype)
+
+
+@pytest.mark.parametrize("batch,top,H,K,dim,dtype,new", [
+    (130, 700, 4, 4, 64, "bf16", 2),         # more sequences than a wave has lanes
+    (70, 1500, 2, 1, 128, "f32", 1),
+    (40, 1100, 8, 8, 128, "bf16", 3),
+    (5, 4000, 34, 2, 64, "bf16", 1),         # groups of 17, two KV heads together
+    (300, 90, 2, 1, 64, "bf16", 4),
+    (3, 9000, 4, 4, 128, "bf16", 8),
+])
+def test_attend_chunks_chosen(batch, top, H, K, dim, dtype, new):
+    """Lengths from 0 to top in tables long enough to be split, 0 to `new` tokens."""
+    announce(f"attend8 {batch} x {top} {H}/{K} x {dim} {dtype} new {new}")
+    rng = np.random.default_rng(batch)
+    lens = [top, 0, 1] + [int(x) for x in np.exp(rng.uniform(0, np.log(top), batch - 3))]
+    counts = [new] + [int(x) for x in rng.integers(0, new + 1, batch - 1)]
+    c = Cache8(rng, lens, K, dim, 64, 16)
+    q, q64 = values(rng, (sum(counts), H, dim), dtype)
+    got = F.focus_paged_attend8(q, c.dev, _offsets(counts), max_rows=new)
+    _check(c, q64, counts, got, dtype)
+
+
+def test_attend_table_far_larger_than_the_lengths():
+    rng = np.random.default_rng(31)
+    lens = [0, 1, 700, 33]
+    c = Cache8(rng, lens, 2, 128, 64, 32, max_pages=1024)
+    q, q64 = values(rng, (4, 8, 128), "bf16")
+    announce("attend8 wide table")
+    _check(c, q64, [1] * 4, F.focus_paged_attend8(q, c.dev), "bf16")
+
+
+def test_attend_chunk_of_more_pages_than_held():
+    """Chunks over more pages than a workgroup holds at a time."""
+    rng = np.random.default_rng(32)
+    c = Cache8(rng, [20_003], 1, 64, 8, 8)
+    q, q64 = values(rng, (3, 2, 64), "bf16")
+    announce("attend8 many pages")
+    _check(c, q64, [3], F.focus_paged_attend8(q, c.dev, _offsets([3]), max_rows=3, split_keys=128 * 80), "bf16")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_attend_strided_queries_scale_and_outputs(dtype):
+    rng = np.random.default_rng(33)
+    H, K, D = 6, 3, 64
+    c = Cache8(rng, [90, 300], K, D, 16, 8)
+    qkv, qkv64 = values(rng, (5, H + 2 * K, D), dtype)
+    t = torch.bfloat16 if dtype == "bf16" else torch.float32
+    o = torch.full((5, H, D), 7.0, dtype=t, device=DEV)
+    lse = torch.full((5, H), 7.0, device=DEV)
+    announce(f"attend8 strided {dtype}")
+    # 2 + 2 rows: the fifth belongs to nobody and is left as it was
+    F.focus_paged_attend8(qkv[:, :H], c.dev, _offsets([2, 2]), max_rows=2, o=o, lse=lse, softmax_scale=0.3)
+    _check(c, qkv64[:, :H], [2, 2], (o, lse), dtype, scale=0.3)
+    assert (o[4] == 7).all() and (lse[4] == 7).all()
+    # rows before the first offset too, and heads before rows
+    o.fill_(7.0)
+    q2 = qkv[:, :H].transpose(0, 1).contiguous().transpose(0, 1)
+    F.focus_paged_attend8(q2, c.dev, i32([1, 3, 5]), max_rows=2, o=o, want_lse=False, softmax_scale=0.3)
+    _check(c, qkv64[1:, :H], [2, 2], (o[1:], F.focus_paged_attend8(q2, c.dev, i32([1, 3, 5]), 2, softmax_scale=0.3)[1][1:]),
+           dtype, scale=0.3)
+    assert (o[0] == 7).all()
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("split", [0, 128])
+def test_attend_nan_only_where_it_is_seen(D, split):
+    """A NaN in a row's k, v or scales reaches the tokens that see it, not those before."""
+    rng = np.random.default_rng(34)
+    announce(f"attend8 NaN {D} {split}")
+    for n in (40, 300, 1027):
+        for which in ("k", "v", "k_scale", "v_scale"):
+            c = Cache8(rng, [n], 2, D, 16, 8)
+            row = n - 2                                   # seen by the last two tokens of four
+            p, r = c.table[0][row // 16], row % 16
+            if "scale" in which:
+                row = n - 1 - (n - 1) % 8
+                if row <= n - 4:
+                    continue                              # every token sees the block
+                p, r = c.table[0][row // 16], row % 16
+                getattr(c.dev, which)[p, 0, r // 8] = float("nan")
+            else:
+                getattr(c.dev, which).view(torch.uint8)[p, r, 0, 5] = NAN
+            q, q64 = values(rng, (4, 4, D), "bf16")
+            c.refresh()
+            o, lse = F.focus_paged_attend8(q, c.dev, i32([0, 4]), max_rows=4, split_keys=split)
+            first = next(i for i in range(4) if n - 3 + i > row)
+            k, v = c.rows(0, n, "k"), c.rows(0, n, "v")
+            for i in range(4):
+                upto = n - 3 + i
+                o_i, lse_i = to64(o[i]), to64(lse[i])
+                if i < first:
+                    ro, rl = O.attend(q64[i:i + 1], k[:upto], v[:upto])
+                    to, tl = O.attend_tolerances(q64[i:i + 1], k[:upto], v[:upto], D ** -0.5, "bf16", ro)
+                    within(o_i, ro[0], to[0], f"{which} token {i}")
+                    within(lse_i, rl[0], tl[0], f"{which} token {i}")
+                else:
+                    spoiled = o_i[:2] if "k" in which or "scale" in which else o_i[:2, 5]
+                    assert np.isnan(spoiled).all(), (which, i)
+                    fine = o_i[2:] if "k" in which or "scale" in which else np.delete(o_i, 5, 1)
+                    assert np.isfinite(fine).all() and np.isfinite(o_i[2:]).all(), (which, i)
+
+
+def test_attend_scales_of_all_sizes():
+    """Scales from the least to great ones: scores of some thousands, weights that leave one
+    row, values near the end of float32."""
+    rng = np.random.default_rng(35)
+    c = Cache8(rng, [200], 2, 128, 16, 8)
+    c.dev.k_scale.copy_(torch.as_tensor(2.0 ** rng.integers(-126, 0, tuple(c.dev.k_scale.shape))))
+    c.dev.v_scale.copy_(torch.as_tensor(2.0 ** rng.integers(-100, 110, tuple(c.dev.v_scale.shape))))
+    c.refresh()
+    q, q64 = values(rng, (1, 4, 128), "f32")
+    announce("attend8 scales")
+    _check(c, q64, [1], F.focus_paged_attend8(q, c.dev), "f32")
+    c.dev.k_scale.zero_()
+    c.dev.v_scale.zero_()
+    o, lse = F.focus_paged_attend8(q, c.dev)
+    assert (o == 0).all() and (lse - math.log(200)).abs().max() < 1e-6
+
+
+def test_attend_pages_outside_the_pool_and_bad_offsets():
+    rng = np.random.default_rng(36)
+    err = torch.zeros(1, dtype=torch.int32, device=DEV)
+    announce("attend8 pages outside the pool")
+    for split in (0, 128):
+        c = Cache8(rng, [600, 40, 20], 2, 64, 16, 8)
+        for j, bad in ((2, -1), (3, -2 ** 31), (20, 10 ** 6), (37, 2 ** 31 - 1)):
+            c.dev.table[0, j] = bad
+        c.dev.table[2, :2] = -1
+        seen = [np.ones(600, bool), np.ones(40, bool), np.zeros(20, bool)]
+        for j in (2, 3, 20, 37):
+            seen[0][16 * j:16 * j + 16] = False
+        q, q64 = values(rng, (5, 2, 64), "bf16")
+        err.zero_()
+        got = F.focus_paged_attend8(q, c.dev, i32([0, 2, 4, 5]), max_rows=2, split_keys=split, err=err)
+        _check(c, q64, [2, 2, 1], got, "bf16", visible=seen)
+        assert err.item() == F.FOCUS_ERR_BOUNDS
+    announce("attend8 lengths outside the table")
+    c = Cache8(rng, [32, 16], 2, 64, 16, 8)
+    q, q64 = values(rng, (2, 2, 64), "bf16")
+    c.dev.length.copy_(i32([99, -4]))
+    err.zero_()
+    got = F.focus_paged_attend8(q, c.dev, err=err)
+    c.lens = [32, 0]
+    _check(c, q64, [1, 1], got, "bf16")
+    assert err.item() == F.FOCUS_ERR_CAPACITY
+    announce("attend8 bad offsets")
+    c = Cache8(rng, [32, 300, 40], 2, 64, 16, 8)
+    q, q64 = values(rng, (6, 2, 64), "bf16")
+    for cu, bit, fine in (([0, 3, 4, 6], F.FOCUS_ERR_CAPACITY, [(1, 3, 4), (2, 4, 6)]),
+                          ([4, 2, 3, 5], F.FOCUS_ERR_BOUNDS, [(1, 2, 3), (2, 3, 5)]),
+                          ([-1, 1, 2, 9], F.FOCUS_ERR_BOUNDS, [(1, 1, 2)])):
+        o, lse = torch.full_like(q, 7.0), torch.full((6, 2), 7.0, device=DEV)
+        err.zero_()
+        F.focus_paged_attend8(q, c.dev, i32(cu), max_rows=2, o=o, lse=lse, err=err)
+        assert err.item() == bit
+        mine = set()
+        for b, r0, r1 in fine:
+            one = Cache8.__new__(Cache8)
+            one.__dict__.update(c.__dict__, lens=[c.lens[b]], table=c.table[b:b + 1])
+            _check(one, q64[r0:r1], [r1 - r0], (o[r0:r1], lse[r0:r1]), "bf16")
+            mine |= set(range(r0, r1))
+        for t in set(range(6)) - mine:
+            assert (o[t] == 7).all() and (lse[t] == 7).all()
