@@ -913,14 +913,15 @@ typedef struct {
   const int32_t* first_pos;     /* [device][batch] or NULL                   */
   int32_t* start;               /* [device][batch]                           */
   int32_t* cu_rows;             /* [device][batch + 1]                       */
-  int64_t n_rows;               /* of the three maps, below 2^31             */
+  int64_t n_rows;               /* of the three maps, below 2^31 - 1         */
   int32_t* row_seq;             /* [device][n_rows], each or NULL            */
   int32_t* row_slot;
   int32_t* row_pos;
   int32_t* err;                 /* optional error word                       */
 } focus_paged_extend_desc;
 
-/* Errors: E_NULL, E_ARG, E_SHAPE, E_UNSUPPORTED (page_rows), E_HIP.  A length outside [0,
+/* Errors: E_NULL, E_ARG, E_SHAPE (batch * max_pages of 2^31 - 1, among others),
+ * E_UNSUPPORTED (page_rows), E_HIP.  A length outside [0,
  * max_pages * page_rows] or a free_count outside [0, free_cap] is clipped to it
  * (FOCUS_ERR_BOUNDS); pages given back past free_cap are lost (FOCUS_ERR_CAPACITY).  With
  * batch 0 only cu_rows[0] and the maps are written. */

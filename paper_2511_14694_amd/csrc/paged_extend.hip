@@ -2,46 +2,55 @@
 //
 //   extend_tables   one workgroup: pages of dropped rows onto the free list, then pages for
 //                   new rows off it, both in the order of sequences by prefix sums; lengths,
-//                   starts, offsets
-//   extend_rows     the maps of the new rows
+//                   starts, offsets, and the maps of the new rows where these are few
+//   extend_rows     the maps of many rows
 //
-// Pages move one at a time through a list whose length every step needs, so all of them are
-// moved by one workgroup; what there is to do is a few words a sequence, a page and a row.
+// Pages move through one list in an order that is fixed, so all of them are moved by one
+// workgroup; what there is to do is a few words a sequence, a page and a row, and what it takes
+// is a chain of latencies: the lengths, the sums over the sequences, the pages, their entries.
 #include "paged.h"
 
 namespace {
 
-constexpr int kThreads = 1024, kWaves = kThreads / 64;
+constexpr int kFew = 256, kMany = 1024;  // threads of extend_tables for up to so many sequences, and for more
+constexpr int kMapRounds = 8;            // rows that a thread of it maps at most
 constexpr int kRowThreads = 256;
 
 struct Args {
   focus_paged_extend_desc d;
   int shift;            // log2 page_rows
+  bool maps;            // extend_tables writes the rows' maps
 };
 
-// Inclusive sum over the workgroup in 64 bits; `total` the sum of all.
-__device__ int64_t group_scan(int64_t x, int64_t* s_part, int64_t& total) {
+// Sum of two numbers from 0 up, at most 2^31 - 1.
+__device__ inline int add_up(int a, int b) { return (int)min((uint32_t)a + (uint32_t)b, (uint32_t)INT32_MAX); }
+
+// Inclusive sums over the workgroup of three values from 0 up; the third may pass 2^31 - 1
+// and stays there.  The caller's barriers keep s_part until all have read it.
+template <int THREADS>
+__device__ void group_scan(int (&x)[3], int (*s_part)[3], int (&total)[3]) {
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+  x[0] = focus::wave_scan(x[0]);
+  x[1] = focus::wave_scan(x[1]);
+  x[2] = focus::wave_prefix(x[2], add_up);
 #pragma unroll
-  for (int k = 1; k < 64; k <<= 1) {
-    const int64_t y = __shfl_up(x, k);
-    if (lane >= k) x += y;
+  for (int i = 0; i < 3; ++i) {
+    if (lane == 63) s_part[wave][i] = x[i];
+    total[i] = 0;
   }
-  __syncthreads();  // the last scan's sums are read
-  if (lane == 63) s_part[wave] = x;
   __syncthreads();
-  total = 0;
 #pragma unroll
-  for (int w = 0; w < kWaves; ++w) {
-    const int64_t y = s_part[w];
-    if (w < wave) x += y;
-    total += y;
-  }
-  return x;
+  for (int w = 0; w < THREADS / 64; ++w)
+#pragma unroll
+    for (int i = 0; i < 3; ++i) {
+      const int y = s_part[w][i];
+      if (w < wave) x[i] = add_up(x[i], y);
+      total[i] = add_up(total[i], y);
+    }
 }
 
 // Index of the first of n ascending values greater than x (n if none is).
-template <typename T> __device__ inline int first_above(const T* v, int n, int64_t x) {
+__device__ inline int first_above(const int* v, int n, int x) {
   int lo = 0;
   while (n > 0) {
     const int half = n / 2;
@@ -51,87 +60,110 @@ template <typename T> __device__ inline int first_above(const T* v, int n, int64
   return lo;
 }
 
-// A sequence of this call.
-struct Seq {
-  int64_t add, n;       // add 0 past the batch
-};
-__device__ inline Seq sequence(const Args& a, int b, int64_t cap, int32_t& bits) {
-  if (b >= a.d.batch) return {0, 0};
-  const int64_t n = a.d.length[b];
-  const int64_t clipped = n < 0 ? 0 : n > cap ? cap : n;
-  if (clipped != n) bits |= FOCUS_ERR_BOUNDS;
-  return {a.d.add[b], clipped};
+__device__ inline void write_row(const focus_paged_extend_desc& d, int t, int seq, int start, int i) {
+  const int slot = start < 0 ? -1 : start + i;
+  if (d.row_seq) d.row_seq[t] = seq;
+  if (d.row_slot) d.row_slot[t] = slot;
+  if (d.row_pos) d.row_pos[t] = seq < 0 ? -1 : d.first_pos ? (int)((uint32_t)d.first_pos[seq] + (uint32_t)i) : slot;
 }
 
-__global__ __launch_bounds__(kThreads) void extend_tables(Args a) {
-  __shared__ int64_t s_part[kWaves], s_upto[kThreads];
-  __shared__ int s_first[kThreads];
+// A thread a sequence; more sequences than threads take rounds, all of which give back before
+// any takes.  All sums over pages are below 2^31, as the tables' entries are.
+template <int THREADS>
+__global__ __launch_bounds__(THREADS) void extend_tables(Args a) {
+  __shared__ int s_part[THREADS / 64][3], s_upto[2][THREADS], s_first[2][THREADS], s_end[THREADS], s_start[THREADS], s_taken;
   const focus_paged_extend_desc& d = a.d;
-  const int tid = threadIdx.x, P = d.page_rows;
-  const int64_t cap = (int64_t)d.max_pages * P;
-  auto pages = [&](int64_t rows) { return (rows + P - 1) >> a.shift; };
+  const int tid = threadIdx.x, P = d.page_rows, cap = d.max_pages * P;
+  const bool once = d.batch <= THREADS;
+  auto pages = [&](int rows) { return (rows + P - 1) >> a.shift; };
   int32_t bits = 0;
-  int64_t count = d.free_count[0];
-  if (count < 0 || count > d.free_cap) count = count < 0 ? 0 : d.free_cap, bits |= FOCUS_ERR_BOUNDS;
 
-  // rows that go
-  for (int b0 = 0; b0 < d.batch; b0 += kThreads) {
+  // what sequence b asks for
+  int n, left, come;  // rows; of these, when the dropped ones have gone; new ones
+  bool room;          // the new ones fit the table
+  int x[3], total[3];
+  auto ask = [&](int b) {
+    const int length = b < d.batch ? d.length[b] : 0, add = b < d.batch ? d.add[b] : 0;
+    n = min(max(length, 0), cap);
+    if (n != length) bits |= FOCUS_ERR_BOUNDS;
+    left = add < 0 ? max(n + max(add, -n), 0) : n;
+    come = max(add, 0);
+    room = come <= cap - n;
+    x[0] = pages(n) - pages(left), x[1] = come > 0 && room ? pages(n + come) - pages(n) : 0, x[2] = come;
+  };
+
+  ask(tid);
+  const int free_count = d.free_count[0];
+  int count = min(max(free_count, 0), d.free_cap);
+  if (count != free_count) bits |= FOCUS_ERR_BOUNDS;
+  for (int b0 = 0; b0 < d.batch; b0 += THREADS) {
     const int b = b0 + tid;
-    const Seq q = sequence(a, b, cap, bits);
-    const int64_t left = q.add < 0 ? max(q.n + q.add, (int64_t)0) : q.n;
-    const int64_t back = pages(q.n) - pages(left);
-    int64_t total;
-    const int64_t upto = group_scan(back, s_part, total);
-    s_upto[tid] = upto;
-    s_first[tid] = (int)pages(left);
-    __syncthreads();
-    for (int64_t i = tid; i < total; i += kThreads) {
-      const int k = first_above(s_upto, kThreads, i);
-      const int64_t before = k > 0 ? s_upto[k - 1] : 0;
-      int32_t* entry = d.table + (int64_t)(b0 + k) * d.max_pages + s_first[k] + (i - before);
-      if (count + i < d.free_cap) d.free_pages[count + i] = *entry;
-      else bits |= FOCUS_ERR_CAPACITY;
-      *entry = -1;
+    if (b0 > 0) ask(b);
+    group_scan<THREADS>(x, s_part, total);
+    if (total[0] > 0) {
+      s_upto[0][tid] = x[0], s_first[0][tid] = pages(left);
+      __syncthreads();
+      for (int i = tid; i < total[0]; i += THREADS) {
+        const int k = first_above(s_upto[0], THREADS, i), before = k > 0 ? s_upto[0][k - 1] : 0;
+        int32_t* entry = d.table + (int64_t)(b0 + k) * d.max_pages + s_first[0][k] + (i - before);
+        const int64_t to = (int64_t)count + i;
+        if (to < d.free_cap) d.free_pages[to] = *entry;
+        else bits |= FOCUS_ERR_CAPACITY;
+        *entry = -1;
+      }
+      count = (int)min((int64_t)count + total[0], (int64_t)d.free_cap);
     }
-    count = min(count + total, (int64_t)d.free_cap);
-    if (b < d.batch && q.add <= 0) d.length[b] = (int)left, d.start[b] = (int)left;
+    if (b < d.batch && come == 0) d.length[b] = left, d.start[b] = left;
+    if (!once || total[0] > 0) __syncthreads();
   }
-  __syncthreads();
 
-  // rows that come
-  int64_t rows = 0, needs = 0, taken = 0;  // of the sequences before; pages handed out
-  for (int b0 = 0; b0 < d.batch; b0 += kThreads) {
+  int rows = 0, needs = 0, taken = 0;  // of the sequences before; pages handed out
+  for (int b0 = 0; b0 < d.batch; b0 += THREADS) {
     const int b = b0 + tid;
-    int32_t unused = 0;
-    Seq q = sequence(a, b, cap, unused);
-    q.add = max(q.add, (int64_t)0);
-    int64_t all_rows, all_needs;
-    const int64_t end = rows + group_scan(q.add, s_part, all_rows);
-    const bool fits = q.add > 0 && q.n + q.add <= cap && end <= d.n_rows;
-    const int64_t need = fits ? pages(q.n + q.add) - pages(q.n) : 0;
-    const int64_t upto = group_scan(need, s_part, all_needs);
-    const bool served = fits && (need == 0 || needs + upto <= count);
-    // (those that get pages are the first ones that need any)
-    s_upto[tid] = upto;
-    s_first[tid] = (int)pages(q.n);
-    int64_t here;  // pages handed out by this round
-    group_scan(served ? need : 0, s_part, here);
-    for (int64_t i = tid; i < here; i += kThreads) {
-      const int k = first_above(s_upto, kThreads, i);
-      const int64_t before = k > 0 ? s_upto[k - 1] : 0;
-      d.table[(int64_t)(b0 + k) * d.max_pages + s_first[k] + (i - before)] = d.free_pages[count - 1 - needs - i];
+    if (!once) {
+      int32_t told = bits;
+      ask(b);
+      bits = told;
+      group_scan<THREADS>(x, s_part, total);
     }
+    // Served while pages and maps last; both sums ascend, so those that get pages are the first
+    // ones that need any.
+    const int end = add_up(rows, x[2]), upto = needs + x[1];
+    const bool lasts = end <= d.n_rows && upto <= count;
+    const int need = pages(n + (room ? come : 0)) - pages(n);
+    const bool served = come > 0 && room && end <= d.n_rows && (need == 0 || lasts);
+    if (tid == 0) s_taken = needs;
+    s_upto[1][tid] = upto, s_first[1][tid] = pages(n);
+    s_end[tid] = end, s_start[tid] = come == 0 ? left : served ? n : -1;
+    __syncthreads();
+    const int last = focus::wave_max(lasts ? upto : 0);
+    if (tid % 64 == 0) atomicMax(&s_taken, last);
     if (b < d.batch) {
-      d.cu_rows[b + 1] = (int)min(end, (int64_t)INT32_MAX);
-      if (q.add > 0) {
-        d.start[b] = served ? (int)q.n : -1;
-        d.length[b] = (int)(served ? q.n + q.add : q.n);
+      d.cu_rows[b + 1] = end;
+      if (come > 0) {
+        d.start[b] = served ? n : -1;
+        d.length[b] = served ? n + come : n;
         if (!served) bits |= FOCUS_ERR_CAPACITY;
       }
     }
-    rows += all_rows, needs += all_needs, taken += here;
+    __syncthreads();
+    const int stop = s_taken;
+    for (int i = needs + tid; i < stop; i += THREADS) {
+      const int k = first_above(s_upto[1], THREADS, i), before = k > 0 ? s_upto[1][k - 1] : needs;
+      d.table[(int64_t)(b0 + k) * d.max_pages + s_first[1][k] + (i - before)] = d.free_pages[count - 1 - i];
+    }
+    taken += stop - needs;
+    rows = add_up(rows, total[2]), needs += total[1];
+    if (!once) __syncthreads();
   }
-  if (tid == 0) d.cu_rows[0] = 0, d.free_count[0] = (int)(count - taken);
+  if (tid == 0) d.cu_rows[0] = 0, d.free_count[0] = count - taken;
+  if (a.maps) {
+    for (int t = tid; t < d.n_rows; t += THREADS) {
+      const int b = first_above(s_end, d.batch, t);
+      if (b < d.batch) write_row(d, t, b, s_start[b], t - (b > 0 ? s_end[b - 1] : 0));
+      else write_row(d, t, -1, -1, 0);
+    }
+  }
   if (bits) focus::raise_err(d.err, bits);
 }
 
@@ -139,17 +171,9 @@ __global__ __launch_bounds__(kRowThreads) void extend_rows(Args a) {
   const focus_paged_extend_desc& d = a.d;
   const int64_t t = (int64_t)blockIdx.x * kRowThreads + threadIdx.x;
   if (t >= d.n_rows) return;
-  int seq = -1, slot = -1, pos = -1;
-  const int b = first_above(d.cu_rows + 1, d.batch, t);
-  if (b < d.batch) {
-    const int i = (int)(t - d.cu_rows[b]), start = d.start[b];
-    seq = b;
-    slot = start < 0 ? -1 : start + i;
-    pos = d.first_pos ? (int)((uint32_t)d.first_pos[b] + (uint32_t)i) : slot;
-  }
-  if (d.row_seq) d.row_seq[t] = seq;
-  if (d.row_slot) d.row_slot[t] = slot;
-  if (d.row_pos) d.row_pos[t] = pos;
+  const int b = first_above(d.cu_rows + 1, d.batch, (int)t);
+  if (b < d.batch) write_row(d, (int)t, b, d.start[b], (int)t - d.cu_rows[b]);
+  else write_row(d, (int)t, -1, -1, 0);
 }
 
 bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
@@ -160,7 +184,9 @@ extern "C" focus_status focus_paged_extend(const focus_paged_extend_desc* d, foc
   if (!d) return FOCUS_E_NULL;
   if (d->batch < 0 || d->max_pages < 0 || d->free_cap < 0 || d->n_rows < 0) return FOCUS_E_ARG;
   if (d->page_rows < 8 || d->page_rows > 1024 || (d->page_rows & (d->page_rows - 1))) return FOCUS_E_UNSUPPORTED;
-  if ((int64_t)d->max_pages * d->page_rows > INT32_MAX / 2 || d->n_rows > INT32_MAX) return FOCUS_E_SHAPE;
+  if ((int64_t)d->max_pages * d->page_rows > INT32_MAX / 2 || (int64_t)d->batch * d->max_pages >= INT32_MAX ||
+      d->batch == INT32_MAX || d->n_rows >= INT32_MAX)
+    return FOCUS_E_SHAPE;
   if (!d->cu_rows || !d->free_count || (d->free_cap > 0 && !d->free_pages)) return FOCUS_E_NULL;
   if (d->batch > 0 && (!d->length || !d->add || !d->start || (d->max_pages > 0 && !d->table))) return FOCUS_E_NULL;
   for (const void* p : {(const void*)d->table, (const void*)d->length, (const void*)d->add, (const void*)d->free_pages,
@@ -168,11 +194,14 @@ extern "C" focus_status focus_paged_extend(const focus_paged_extend_desc* d, foc
                         (const void*)d->cu_rows, (const void*)d->row_seq, (const void*)d->row_slot,
                         (const void*)d->row_pos, (const void*)d->err})
     if (!aligned4(p)) return FOCUS_E_ARG;
-  Args a = {*d, __builtin_ctz((unsigned)d->page_rows)};
+  const int threads = d->batch <= kFew ? kFew : kMany;
+  const bool any = d->n_rows > 0 && (d->row_seq || d->row_slot || d->row_pos);
+  Args a = {*d, __builtin_ctz((unsigned)d->page_rows), any && d->batch <= threads && d->n_rows <= kMapRounds * threads};
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
-  hipLaunchKernelGGL(extend_tables, dim3(1), dim3(kThreads), 0, s, a);
+  if (threads == kFew) hipLaunchKernelGGL(extend_tables<kFew>, dim3(1), dim3(kFew), 0, s, a);
+  else hipLaunchKernelGGL(extend_tables<kMany>, dim3(1), dim3(kMany), 0, s, a);
   const focus_status st = focus::launch_status();
-  if (st != FOCUS_OK || d->n_rows == 0 || (!d->row_seq && !d->row_slot && !d->row_pos)) return st;
+  if (st != FOCUS_OK || !any || a.maps) return st;
   hipLaunchKernelGGL(extend_rows, dim3((uint32_t)focus::ceil_div(d->n_rows, kRowThreads)), dim3(kRowThreads), 0, s, a);
   return focus::launch_status();
 }
