@@ -38,7 +38,7 @@ import torch
 
 from ._abi import (AdapterDesc, AdapterLayerDesc, AttnDesc, CompactDesc, DecodeDesc, DecodeSched, FidelityDesc, FocusError, GemmDesc, LayoutDesc, LayoutTotals,
                    PagedAppend8Desc, PagedAttend8Desc, PagedDecodeDesc, PagedEvictDesc, PagedExtendDesc, PagedKv, PagedKv8, QkvDesc,
-                   RopeDesc, RopeScaling, FOCUS_BF16, FOCUS_F32, FOCUS_E4M3, FOCUS_MASK_CT, FOCUS_MASK_KMER_LOCAL,
+                   RopeDesc, RopeScaling, FOCUS_BF16, FOCUS_F32, FOCUS_E4M3, FOCUS_E_WORKSPACE, FOCUS_MASK_CT, FOCUS_MASK_KMER_LOCAL,
                    FOCUS_TOK_BASE, FOCUS_TOK_SUMMARY, FOCUS_STEP_SUMMARY, FOCUS_STEP_WINDOW_END,
                    FOCUS_ERR_CAPACITY, FOCUS_ERR_BOUNDS, FOCUS_ERR_PLAN,
                    FOCUS_FID_LOGITS, FOCUS_FID_PROBS, FOCUS_FID_N,
@@ -635,8 +635,9 @@ def _workspace(t, dev: int):
     return t.data_ptr(), t.numel() * t.element_size()
 
 
-def _launch(call: str, d, dev: int, stream):
-    """Enqueue a call on device dev, whichever one is current."""
+def _launch(call: str, d, dev: int, stream, accept: int = 0):
+    """Enqueue a call on device dev, whichever one is current; returns its status, which
+    may be `accept` (else an error is raised)."""
     if dev < 0:
         raise ValueError(f"{call} needs tensors on a GPU")
     fn = getattr(lib(), call)
@@ -649,8 +650,9 @@ def _launch(call: str, d, dev: int, stream):
     else:
         with torch.cuda.device(dev):
             st = fn(C.byref(d), handle)
-    if st:
+    if st and st != accept:
         check(call, st)
+    return st
 
 
 def _query(call: str, d, dev: int) -> int:
@@ -904,27 +906,30 @@ def focus_paged_extend(table, length, page_rows: int, add, free_pages, free_coun
     three maps; a sequence whose rows do not all fit (maps, table or free pages) is not
     served: start -1, slots -1.  first_pos [batch]: position of the first new row (default:
     its slot).  out: a PagedRows of these sizes to be written again.  All arrays int32."""
-    dev = length.get_device()
-    if table.dim() != 2:
+    dev, i32 = length.get_device(), torch.int32
+    batch_pages = table.shape
+    if len(batch_pages) != 2:
         raise ValueError("table must be [batch, max_pages]")
-    batch, max_pages = table.shape
+    batch, max_pages = batch_pages
     n_rows, page_rows = _i32(n_rows, "n_rows"), _i32(page_rows, "page_rows")
+    one = (batch,)
     if out is None:
-        n = max(n_rows, 0)
-        # one allocation for all five
-        buf = _empty((2 * batch + 1 + 3 * n,), torch.int32, length.device, stream)
-        out = PagedRows(*buf.split([batch, batch + 1, n, n, n]))
-    i32 = torch.int32
+        # one allocation for all five (each by itself costs more than the views)
+        n = n_rows if n_rows > 0 else 0
+        buf = _empty((2 * batch + 1 + 3 * n,), i32, length.device, stream)
+        out = PagedRows(*buf.unsafe_split_with_sizes((batch, batch + 1, n, n, n)))
+        at = buf.data_ptr()
+        cu = at + 4 * batch
+        seq = cu + 4 * batch + 4
+        slot, pos = seq + 4 * n, seq + 8 * n
+    else:
+        at, cu = _need(out.start, i32, one, dev, "out.start"), _need(out.cu_rows, i32, (batch + 1,), dev, "out.cu_rows")
+        seq, slot, pos = (_need(x, i32, (n_rows,), dev, "out's maps") for x in (out.row_seq, out.row_slot, out.row_pos))
     d = PagedExtendDesc(page_rows, batch, max_pages, free_pages.numel(), _need(table, i32, None, dev, "table"),
-                        _need(length, i32, (batch,), dev, "length"), _need(add, i32, (batch,), dev, "add"),
+                        _need(length, i32, one, dev, "length"), _need(add, i32, one, dev, "add"),
                         _need(free_pages, i32, None, dev, "free_pages"), _need(free_count, i32, (1,), dev, "free_count"),
-                        None if first_pos is None else _need(first_pos, i32, (batch,), dev, "first_pos"),
-                        _need(out.start, i32, (batch,), dev, "out.start"),
-                        _need(out.cu_rows, i32, (batch + 1,), dev, "out.cu_rows"), n_rows,
-                        _need(out.row_seq, i32, (n_rows,), dev, "out.row_seq"),
-                        _need(out.row_slot, i32, (n_rows,), dev, "out.row_slot"),
-                        _need(out.row_pos, i32, (n_rows,), dev, "out.row_pos"),
-                        None if err is None else _err_ptr(err, dev))
+                        None if first_pos is None else _need(first_pos, i32, one, dev, "first_pos"), at, cu, n_rows, seq,
+                        slot, pos, None if err is None else _err_ptr(err, dev))
     _launch("focus_paged_extend", d, dev, stream)
     return out
 
@@ -948,27 +953,27 @@ class PagedCache8:
 
     def desc(self) -> PagedKv8:
         k, v, table, scale = self.k, self.v, self.table, self.k_scale
-        shape, strides, dev = k.shape, k.stride(), k.get_device()
-        if (len(shape) != 4 or v.shape != shape or k.dtype is not torch.float8_e4m3fn or v.dtype is not k.dtype
+        shape, strides, dev, e4m3 = k.shape, k.stride(), k.get_device(), torch.float8_e4m3fn
+        if (len(shape) != 4 or v.shape != shape or k.dtype is not e4m3 or v.dtype is not e4m3
                 or v.get_device() != dev or v.stride() != strides or strides[3] != 1):
             raise ValueError("k and v must be float8_e4m3fn [n_pages, page_rows, H_kv, D] of one device and strides, "
                              "with unit stride in D")
         n_pages, rows, heads, dim = shape
-        batch_pages, blocks = table.shape, scale.shape[-1]
+        batch_pages, scales = table.shape, scale.shape
         if len(batch_pages) != 2:
             raise ValueError("table must be [batch, max_pages]")
         batch, max_pages = batch_pages
-        if blocks < 1 or rows % blocks:
+        blocks = scales[-1] if scales else 0
+        if blocks < 1 or rows % blocks or scales != (n_pages, heads, blocks):
             raise ValueError("scales must be [n_pages, H_kv, page_rows / scale_rows]")
         if n_pages <= 1 or heads <= 1:
             # the stride of a dimension of one element says nothing: replaced by one that passes
             strides = [dim if n <= 1 else st for n, st in zip(shape, strides)]
-        ss = (n_pages, heads, blocks)
+        i32, f32 = torch.int32, torch.float32
         return PagedKv8(PagedKv(FOCUS_E4M3, heads, dim, rows, n_pages, k.data_ptr(), v.data_ptr(), strides[0], strides[1],
-                                strides[2], batch, max_pages, _need(table, torch.int32, None, dev, "table"),
-                                _need(self.length, torch.int32, (batch,), dev, "length"), None, 0), rows // blocks, 0,
-                        _need(scale, torch.float32, ss, dev, "k_scale"),
-                        _need(self.v_scale, torch.float32, ss, dev, "v_scale"))
+                                strides[2], batch, max_pages, _need(table, i32, None, dev, "table"),
+                                _need(self.length, i32, (batch,), dev, "length"), None, 0), rows // blocks, 0,
+                        _need(scale, f32, None, dev, "k_scale"), _need(self.v_scale, f32, scales, dev, "v_scale"))
 
 
 def focus_paged_append8(k, v, cache: PagedCache8, start, cu_rows=None, err=None, stream=None):
@@ -990,7 +995,8 @@ def focus_paged_append8(k, v, cache: PagedCache8, start, cu_rows=None, err=None,
     _launch("focus_paged_append8", d, dev, stream)
 
 
-def _paged_attend8_desc(q, cache, cu_rows, max_rows, o, lse, workspace, split_keys, softmax_scale, err):
+def _paged_attend8_desc(q, cache, cu_rows, max_rows, o, lse, split_keys, softmax_scale, err):
+    """The descriptor without a workspace; o and lse addresses."""
     c = cache.desc()
     kv, dev, dtype, shape = c.kv, q.get_device(), q.dtype, q.shape
     if len(shape) != 3 or shape[2] != kv.head_dim or dev != cache.k.get_device() or dtype not in _DTYPES:
@@ -998,13 +1004,11 @@ def _paged_attend8_desc(q, cache, cu_rows, max_rows, o, lse, workspace, split_ke
     return PagedAttend8Desc(c, _DTYPES[dtype], shape[1], _i32(max_rows, "max_rows"), _i32(split_keys, "split_keys"),
                             float(softmax_scale), 0, shape[0],
                             None if cu_rows is None else _need(cu_rows, torch.int32, (kv.batch + 1,), dev, "cu_rows"),
-                            *_rows(q, shape, dtype, dev, "q"), None if o is None else _need(o, dtype, shape, dev, "o"),
-                            None if lse is None else _need(lse, torch.float32, shape[:2], dev, "lse"),
-                            *_workspace(workspace, dev), None if err is None else _err_ptr(err, dev))
+                            *_rows(q, shape, dtype, dev, "q"), o, lse, None, 0, None if err is None else _err_ptr(err, dev))
 
 
 def focus_paged_attend8_workspace(q, cache: PagedCache8, cu_rows=None, max_rows: int = 1, split_keys: int = 0) -> int:
-    d = _paged_attend8_desc(q, cache, cu_rows, max_rows, None, None, None, split_keys, 0.0, None)
+    d = _paged_attend8_desc(q, cache, cu_rows, max_rows, None, None, split_keys, 0.0, None)
     return _query("focus_paged_attend8_workspace", d, q.get_device())
 
 
@@ -1015,16 +1019,29 @@ def focus_paged_attend8(q, cache: PagedCache8, cu_rows=None, max_rows: int = 1, 
     cu_rows[b] : cu_rows[b + 1] (int32 [batch + 1], at most max_rows of them) the last ones of
     sequence b in order, each seeing the rows up to its own (cu_rows None: one token of every
     sequence).  Returns (o, lse); rows past cu_rows[batch] are left as they were."""
+    dev = q.get_device()
+    # (what is allocated here need not be looked at again)
     if o is None:
         o = _empty_like(q, stream)
-    if lse is None and want_lse:
-        lse = q.new_empty(*q.shape[:2], dtype=torch.float32) if stream is None else \
-            _empty(q.shape[:2], torch.float32, q.device, stream)
-    d = _paged_attend8_desc(q, cache, cu_rows, max_rows, o, lse, workspace, split_keys, softmax_scale, err)
-    if workspace is None:
-        n = _query("focus_paged_attend8_workspace", d, q.get_device())
-        if n > 0:
-            workspace = _scratch(n, q.device, stream)
-            d.workspace, d.workspace_bytes = workspace.data_ptr(), n
-    _launch("focus_paged_attend8", d, q.get_device(), stream)
+        o_at = o.data_ptr()
+    else:
+        o_at = _need(o, q.dtype, q.shape, dev, "o")
+    lse_at = None
+    if lse is not None:
+        lse_at = _need(lse, torch.float32, q.shape[:2], dev, "lse")
+    elif want_lse:
+        lse = _empty(tuple(q.shape[:2]), torch.float32, q.device, stream)
+        lse_at = lse.data_ptr()
+    d = _paged_attend8_desc(q, cache, cu_rows, max_rows, o_at, lse_at, split_keys, softmax_scale, err)
+    if workspace is not None:
+        d.workspace, d.workspace_bytes = _workspace(workspace, dev)
+    # a call that needs a workspace says so before anything is enqueued; those that need none,
+    # the shortest, are spared the question
+    elif _launch("focus_paged_attend8", d, dev, stream, FOCUS_E_WORKSPACE) == 0:
+        return o, lse
+    else:
+        n = _query("focus_paged_attend8_workspace", d, dev)
+        workspace = _scratch(n, q.device, stream)
+        d.workspace, d.workspace_bytes = workspace.data_ptr(), n
+    _launch("focus_paged_attend8", d, dev, stream)
     return o, lse

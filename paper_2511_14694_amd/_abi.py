@@ -7,7 +7,7 @@ import os
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libfocus.so")
 
-FOCUS_OK = 0
+FOCUS_OK, FOCUS_E_WORKSPACE = 0, 6
 STATUS_NAMES = {0: "FOCUS_OK", 1: "FOCUS_E_NULL", 2: "FOCUS_E_ARG", 3: "FOCUS_E_SHAPE",
                 4: "FOCUS_E_DTYPE", 5: "FOCUS_E_UNSUPPORTED", 6: "FOCUS_E_WORKSPACE",
                 7: "FOCUS_E_CAPACITY", 8: "FOCUS_E_HIP"}
