@@ -49,15 +49,32 @@ __device__ void group_scan(int (&x)[3], int (*s_part)[3], int (&total)[3]) {
     }
 }
 
-// Index of the first of n ascending values greater than x (n if none is).
-__device__ inline int first_above(const int* v, int n, int x) {
+// Index of the first of THREADS ascending values in LDS greater than x, where one is.
+template <int THREADS> __device__ inline int first_above(const int* v, int x) {
   int lo = 0;
-  while (n > 0) {
-    const int half = n / 2;
-    if (v[lo + half] <= x) lo += half + 1, n -= half + 1;
-    else n = half;
-  }
+#pragma unroll
+  for (int half = THREADS / 2; half > 0; half /= 2) lo += v[lo + half - 1] <= x ? half : 0;
   return lo;
+}
+
+// f(k, i) of items i = from .. to - 1, k the first sequence whose sum `upto` is greater than i;
+// kTogether of a thread's at once, so that their searches and loads overlap.
+constexpr int kTogether = 4;
+template <int THREADS, typename Load, typename Store>
+__device__ inline void each_page(const int* upto, int from, int to, Load load, Store store) {
+  for (int i0 = from + (int)threadIdx.x; i0 < to; i0 += kTogether * THREADS) {
+    int k[kTogether], page[kTogether];
+#pragma unroll
+    for (int j = 0; j < kTogether; ++j) {
+      if (i0 - (int)threadIdx.x + j * THREADS >= to) break;  // for all threads
+      const int i = min(i0 + j * THREADS, to - 1);
+      k[j] = first_above<THREADS>(upto, i);
+      page[j] = load(k[j], i);
+    }
+#pragma unroll
+    for (int j = 0; j < kTogether; ++j)
+      if (to - i0 > j * THREADS) store(k[j], i0 + j * THREADS, page[j]);
+  }
 }
 
 __device__ inline void write_row(const focus_paged_extend_desc& d, int t, int seq, int start, int i) {
@@ -103,14 +120,17 @@ __global__ __launch_bounds__(THREADS) void extend_tables(Args a) {
     if (total[0] > 0) {
       s_upto[0][tid] = x[0], s_first[0][tid] = pages(left);
       __syncthreads();
-      for (int i = tid; i < total[0]; i += THREADS) {
-        const int k = first_above(s_upto[0], THREADS, i), before = k > 0 ? s_upto[0][k - 1] : 0;
-        int32_t* entry = d.table + (int64_t)(b0 + k) * d.max_pages + s_first[0][k] + (i - before);
-        const int64_t to = (int64_t)count + i;
-        if (to < d.free_cap) d.free_pages[to] = *entry;
-        else bits |= FOCUS_ERR_CAPACITY;
-        *entry = -1;
-      }
+      auto entry = [&](int k, int i) {
+        const int before = k > 0 ? s_upto[0][k - 1] : 0;
+        return d.table + (int64_t)(b0 + k) * d.max_pages + s_first[0][k] + (i - before);
+      };
+      each_page<THREADS>(s_upto[0], 0, total[0], [&](int k, int i) { return *entry(k, i); },
+                         [&](int k, int i, int page) {
+                           const int64_t to = (int64_t)count + i;
+                           if (to < d.free_cap) d.free_pages[to] = page;
+                           else bits |= FOCUS_ERR_CAPACITY;
+                           *entry(k, i) = -1;
+                         });
       count = (int)min((int64_t)count + total[0], (int64_t)d.free_cap);
     }
     if (b < d.batch && come == 0) d.length[b] = left, d.start[b] = left;
@@ -148,10 +168,11 @@ __global__ __launch_bounds__(THREADS) void extend_tables(Args a) {
     }
     __syncthreads();
     const int stop = s_taken;
-    for (int i = needs + tid; i < stop; i += THREADS) {
-      const int k = first_above(s_upto[1], THREADS, i), before = k > 0 ? s_upto[1][k - 1] : needs;
-      d.table[(int64_t)(b0 + k) * d.max_pages + s_first[1][k] + (i - before)] = d.free_pages[count - 1 - i];
-    }
+    each_page<THREADS>(s_upto[1], needs, stop, [&](int, int i) { return d.free_pages[count - 1 - i]; },
+                       [&](int k, int i, int page) {
+                         const int before = k > 0 ? s_upto[1][k - 1] : needs;
+                         d.table[(int64_t)(b0 + k) * d.max_pages + s_first[1][k] + (i - before)] = page;
+                       });
     taken += stop - needs;
     rows = add_up(rows, total[2]), needs += total[1];
     if (!once) __syncthreads();
@@ -159,21 +180,48 @@ __global__ __launch_bounds__(THREADS) void extend_tables(Args a) {
   if (tid == 0) d.cu_rows[0] = 0, d.free_count[0] = count - taken;
   if (a.maps) {
     for (int t = tid; t < d.n_rows; t += THREADS) {
-      const int b = first_above(s_end, d.batch, t);
-      if (b < d.batch) write_row(d, t, b, s_start[b], t - (b > 0 ? s_end[b - 1] : 0));
-      else write_row(d, t, -1, -1, 0);
+      if (t < rows) {
+        const int b = first_above<THREADS>(s_end, t);
+        write_row(d, t, b, s_start[b], t - (b > 0 ? s_end[b - 1] : 0));
+      } else {
+        write_row(d, t, -1, -1, 0);
+      }
     }
   }
   if (bits) focus::raise_err(d.err, bits);
 }
 
+// A wave takes 64 rows: the first one's sequence by a search of 64 offsets at a time, the
+// others' among the 64 sequences from there on, one a lane.
 __global__ __launch_bounds__(kRowThreads) void extend_rows(Args a) {
   const focus_paged_extend_desc& d = a.d;
-  const int64_t t = (int64_t)blockIdx.x * kRowThreads + threadIdx.x;
-  if (t >= d.n_rows) return;
-  const int b = first_above(d.cu_rows + 1, d.batch, (int)t);
-  if (b < d.batch) write_row(d, (int)t, b, d.start[b], (int)t - d.cu_rows[b]);
-  else write_row(d, (int)t, -1, -1, 0);
+  const int64_t t64 = (int64_t)blockIdx.x * kRowThreads + threadIdx.x;
+  const int lane = threadIdx.x % 64, t = (int)min(t64, d.n_rows - 1), t0 = (int)(t64 - lane);
+  const int* ends = d.cu_rows + 1;
+  int lo = 0, len = d.batch;
+  while (len > 0) {
+    const int step = (len + 63) / 64, last = lo + (lane + 1) * step - 1;  // of the lane's part
+    const int parts = __popcll(__ballot(last < lo + len && ends[last] <= t0));
+    lo += parts * step;
+    len = min(step - 1, len - parts * step);
+  }
+  for (int b = lo;; b += 64) {
+    const bool in = b + lane < d.batch;
+    const int end = in ? ends[b + lane] : INT32_MAX, begin = d.cu_rows[min(b + lane, d.batch)];
+    const int start = in ? d.start[b + lane] : -1;
+    // this lane's sequence among them: those that end at its row or before come first
+    int k = 0;
+#pragma unroll
+    for (int half = 32; half > 0; half /= 2) k += __shfl(end, k + half - 1) <= t ? half : 0;
+    const bool here = __shfl(end, k) > t;
+    const int from = __shfl(begin, k), to = __shfl(start, k);
+    if (here && t >= from && t64 < d.n_rows) {
+      if (b + k < d.batch) write_row(d, t, b + k, to, t - from);
+      else write_row(d, t, -1, -1, 0);
+    }
+    // (a row before these sequences was written with the ones before)
+    if (!__ballot(!here)) break;
+  }
 }
 
 bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }

@@ -74,6 +74,18 @@ def test_extend_long_prompts():
     assert p.length == [4, 0, 70_041]
 
 
+@pytest.mark.parametrize("batch,rows,more", [(64, 41, 0), (64, 41, 700), (128, 67, 3), (300, 30, 9000), (1100, 5, 100), (2, 9000, 1)])
+def test_extend_maps_of_many_rows(batch, rows, more):
+    """More rows than the first launch maps: sequences without rows between, rows past the last."""
+    rng = np.random.default_rng(batch)
+    announce(f"extend maps {batch} x {rows} + {more}")
+    add = [int(x) if y else 0 for x, y in zip(rng.integers(rows // 2, rows * 2, batch), rng.random(batch) < 0.8)]
+    add[-1] = 0
+    n = max(sum(add) + more, 9000 if batch > 256 else 2100)
+    p = Pool(rng, [int(x) for x in rng.integers(0, 9, batch)], 16, (2 * rows + 32) // 16 + 1, batch * (rows // 8 + 3))
+    assert p.step(add, n, first_pos=[int(x) for x in rng.integers(-50, 50, batch)])
+
+
 def test_extend_out_of_pages_and_slots():
     rng = np.random.default_rng(4)
     announce("extend out of pages")
