@@ -36,7 +36,6 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kThreads = 256, kWaves = 4;
-constexpr int kMaxGrid = focus::kSplitGrid;
 constexpr int kPages = 1024;    // pages held in LDS at a time
 constexpr int kWhole = 256;     // rows of a table that is not split
 constexpr int kUnit = 128;      // rows of a share's units times KV heads of a workgroup
@@ -119,7 +118,6 @@ struct Args {
   int per_head, columns;   // columns of a KV head at most, of all heads
   int unit, shares, over;  // rows of a unit; shares; units that a sequence costs besides
   bool single, fixed;   // a share is a sequence; a unit
-  int parts, lanes;     // attend8_join: workgroups of a KV head, threads of a column's output
   int2* info;
   int* ends;            // null unless planned
   float2* ml;
@@ -636,79 +634,86 @@ __global__ __launch_bounds__(kThreads, resident(D)) void attend8_attend(Args a) 
   }
 }
 
-constexpr int kJoin = 256;  // threads of attend8_join
-
-// One of `parts` workgroups of a (sequence, KV head) and of a part of the outputs' elements:
-// merges the partials of every parts-th of its columns (`lanes` threads over the elements, the
-// other groups of them over the shares).  The first partials are in flight while the maxima and
-// sums are merged, by every wave for itself.
-template <typename T, int D>
+// Merges a column's partials: by a wave, or, where a sequence has many shares (WIDE), by a
+// workgroup for every 32 elements of it.  Lanes lie over the elements, four each, and groups of
+// them over the shares; the first partials are in flight while the maxima and sums are merged,
+// by every wave for itself.
+constexpr int kJoin = 256, kManyShares = 32;
+template <typename T, int D, bool WIDE>
 __global__ __launch_bounds__(kJoin) void attend8_join(Args a) {
-  constexpr int kFlight = 8;
-  __shared__ float4 s_o[kJoin];
+  constexpr int kFlight = 8, kThreadsOf = WIDE ? kJoin : 64, kSlices = WIDE ? D / 32 : 1;
+  constexpr int kLanes = D / 4 / kSlices, kGroups = kThreadsOf / kLanes;
+  __shared__ float4 s_o[WIDE ? kJoin : 1];
   const focus_paged_kv& c = a.d.cache.kv;
-  const int H = a.d.n_heads, G = a.group, tid = threadIdx.x, parts = a.parts, lanes = a.lanes;
-  const int slices = D / 4 / lanes, g = blockIdx.x / slices, groups = kJoin / lanes;
-  const int part = c.batch <= kMaxGrid ? blockIdx.z : blockIdx.z % parts;
-  const int b = blockIdx.y + (c.batch <= kMaxGrid ? 0 : blockIdx.z / parts * kMaxGrid);
+  const int G = a.group, tid = threadIdx.x % kThreadsOf, lane = threadIdx.x % 64;
+  const int64_t id = WIDE ? blockIdx.x / kSlices : (int64_t)blockIdx.x * (kJoin / 64) + scalar(threadIdx.x / 64);
+  const int b = (int)(id / a.columns), column = (int)(id % a.columns), g = column / a.per_head, cc = column % a.per_head;
   if (b >= c.batch) return;
   const int2 info = a.info[b];
-  if (info.y <= 1) return;
   int32_t bits = 0;
   const Tokens tok = a.d.cu_rows ? tokens_of(a, a.d.cu_rows[b], a.d.cu_rows[b + 1], bits) : Tokens{b, 1};
-  const int e = blockIdx.x % slices * lanes + tid % lanes, grp = tid / lanes;
+  if (info.y <= 1 || cc >= tok.count * G) return;
+  const int e = (WIDE ? blockIdx.x % kSlices * kLanes : 0) + tid % kLanes, grp = tid / kLanes;
   const float4* o = reinterpret_cast<const float4*>(a.o);
-  for (int cc = part; cc < tok.count * G; cc += parts) {
-    const int column = g * a.per_head + cc;
-    float4 y[kFlight], sum = make_float4(0.f, 0.f, 0.f, 0.f);
-    float m[kFlight];
-    auto load = [&](int i0) {
+  float4 y[kFlight], sum = make_float4(0.f, 0.f, 0.f, 0.f);
+  float m[kFlight];
+  auto load = [&](int i0) {
 #pragma unroll
-      for (int k = 0; k < kFlight; ++k) {
-        const int64_t slot = slot_of(info.x, min(i0 + k * groups, info.y - 1)) * a.columns + column;
-        y[k] = o[slot * (D / 4) + e];
-        m[k] = a.ml[slot].x;
-      }
-    };
-    load(grp);
-    // maximum and sum over the shares
-    float M = kMinit, S = 0.f;
-    for (int i = tid % 64; i < info.y; i += 64) {
-      const float2 z = a.ml[slot_of(info.x, i) * a.columns + column];
-      const float top = fmaxf(M, z.x);
-      S = S * __builtin_amdgcn_exp2f((M - top) * a.sc) + z.y * __builtin_amdgcn_exp2f((z.x - top) * a.sc);
-      M = top;
+    for (int k = 0; k < kFlight; ++k) {
+      const int64_t slot = slot_of(info.x, min(i0 + k * kGroups, info.y - 1)) * a.columns + column;
+      y[k] = o[slot * (D / 4) + e];
+      m[k] = a.ml[slot].x;
     }
+  };
+  load(grp);
+  // maximum and sum over the shares
+  float M = kMinit, S = 0.f;
+  for (int i = lane; i < info.y; i += 64) {
+    const float2 z = a.ml[slot_of(info.x, i) * a.columns + column];
+    const float top = fmaxf(M, z.x);
+    S = S * __builtin_amdgcn_exp2f((M - top) * a.sc) + z.y * __builtin_amdgcn_exp2f((z.x - top) * a.sc);
+    M = top;
+  }
 #pragma unroll
-    for (int k = 32; k >= 1; k >>= 1) {
-      const float m2 = __shfl_xor(M, k), l2 = __shfl_xor(S, k), top = fmaxf(M, m2);
-      S = S * __builtin_amdgcn_exp2f((M - top) * a.sc) + l2 * __builtin_amdgcn_exp2f((m2 - top) * a.sc);
-      M = top;
-    }
-    for (int i0 = grp; i0 < info.y; i0 += groups * kFlight) {
-      if (i0 > grp) load(i0);
+  for (int k = 32; k >= 1; k >>= 1) {
+    const float m2 = __shfl_xor(M, k), l2 = __shfl_xor(S, k), top = fmaxf(M, m2);
+    S = S * __builtin_amdgcn_exp2f((M - top) * a.sc) + l2 * __builtin_amdgcn_exp2f((m2 - top) * a.sc);
+    M = top;
+  }
+  for (int i0 = grp; i0 < info.y; i0 += kGroups * kFlight) {
+    if (i0 > grp) load(i0);
 #pragma unroll
-      for (int k = 0; k < kFlight; ++k) {
-        if (i0 + k * groups < info.y) {
-          const float f = __builtin_amdgcn_exp2f((m[k] - M) * a.sc);
-          sum.x = fmaf(y[k].x, f, sum.x), sum.y = fmaf(y[k].y, f, sum.y);
-          sum.z = fmaf(y[k].z, f, sum.z), sum.w = fmaf(y[k].w, f, sum.w);
-        }
+    for (int k = 0; k < kFlight; ++k) {
+      if (i0 + k * kGroups < info.y) {
+        const float f = __builtin_amdgcn_exp2f((m[k] - M) * a.sc);
+        sum.x = fmaf(y[k].x, f, sum.x), sum.y = fmaf(y[k].y, f, sum.y);
+        sum.z = fmaf(y[k].z, f, sum.z), sum.w = fmaf(y[k].w, f, sum.w);
       }
     }
+  }
+  if constexpr (WIDE) {
     s_o[tid] = sum;
     __syncthreads();
-    if (tid < 4 * lanes) {
-      float z = 0.f;
-      for (int k = 0; k < groups; ++k) z += reinterpret_cast<const float*>(s_o + k * lanes)[tid];
-      const int i = cc / G;
-      const int64_t at = (tok.first + i) * H + g * G + (cc - i * G);
-      const int element = blockIdx.x % slices * lanes * 4 + tid;
-      reinterpret_cast<T*>(a.d.o)[at * D + element] = (T)(S == 0.f ? 0.f : z / S);
-      if (element == 0 && a.d.lse) a.d.lse[at] = focus::lse_of(a.sc, make_float2(M, S));
+    if (tid >= kLanes) return;
+    sum = s_o[tid];
+    for (int k = 1; k < kGroups; ++k) {
+      const float4 z = s_o[k * kLanes + tid];
+      sum.x += z.x, sum.y += z.y, sum.z += z.z, sum.w += z.w;
     }
-    __syncthreads();
+  } else {
+#pragma unroll
+    for (int k = kLanes; k < 64; k <<= 1)
+      sum.x += __shfl_xor(sum.x, k), sum.y += __shfl_xor(sum.y, k), sum.z += __shfl_xor(sum.z, k), sum.w += __shfl_xor(sum.w, k);
+    if (tid >= kLanes) return;
   }
+  const float inv = S == 0.f ? 0.f : 1.f / S;  // (the sum is zero too)
+  const int i = cc / G;
+  const int64_t at = (tok.first + i) * a.d.n_heads + g * G + (cc - i * G);
+  T* to = reinterpret_cast<T*>(a.d.o) + at * D + 4 * e;
+  if constexpr (sizeof(T) == 2)
+    *reinterpret_cast<u32x2*>(to) = u32x2{focus::pack_bf16x2(sum.x * inv, sum.y * inv), focus::pack_bf16x2(sum.z * inv, sum.w * inv)};
+  else *reinterpret_cast<float4*>(to) = make_float4(sum.x * inv, sum.y * inv, sum.z * inv, sum.w * inv);
+  if (e == 0 && a.d.lse) a.d.lse[at] = focus::lse_of(a.sc, make_float2(M, S));
 }
 
 focus_status validate(const focus_paged_attend8_desc* d) {
@@ -725,7 +730,7 @@ focus_status validate(const focus_paged_attend8_desc* d) {
   if ((int64_t)(d->n_heads / c.n_kv_heads) * d->max_rows > kMost || d->n_rows > INT32_MAX ||
       (!d->cu_rows && d->n_rows != c.batch))
     return FOCUS_E_SHAPE;
-  if ((int64_t)c.batch * d->n_heads * d->max_rows > INT32_MAX / kThreads) return FOCUS_E_SHAPE;
+  if ((int64_t)c.batch * d->n_heads * d->max_rows > INT32_MAX / 4 / kThreads) return FOCUS_E_SHAPE;
   // (units, of 32 rows at least, are counted in 32 bits)
   if ((int64_t)c.batch * (focus::ceil_div((int64_t)c.max_pages * c.page_rows, 32) + 1 + kEnds) > INT32_MAX / 2)
     return FOCUS_E_SHAPE;
@@ -737,15 +742,8 @@ focus_status validate(const focus_paged_attend8_desc* d) {
 template <typename T, int D>
 focus_status launch(Args a, const Plan& p, hipStream_t s) {
   const focus_paged_kv& c = a.d.cache.kv;
-  // workgroups of a (sequence, KV head) in the second launch: one per column, but not many
-  // more than the device holds; where they are few, four for the elements of each
-  const int64_t heads = (int64_t)c.batch * c.n_kv_heads, cus = focus::device_cus();
-  a.parts = (int)std::min<int64_t>(focus::ceil_div(8 * cus, heads), a.per_head);
-  a.lanes = heads * a.parts <= 2 * cus ? 8 : D / 4;
-  const int64_t batches = focus::ceil_div(c.batch, kMaxGrid), slices = D / 4 / a.lanes;
-  if (p.groups * p.shares > INT32_MAX / kThreads - focus::kXcds * kMost || heads * a.parts * slices > INT32_MAX / kThreads ||
-      batches * a.parts > kMaxGrid || c.n_kv_heads * slices > INT32_MAX / kThreads)
-    return FOCUS_E_SHAPE;
+  const int64_t columns = (int64_t)c.batch * p.columns;
+  if (p.groups * p.shares > INT32_MAX / kThreads - focus::kXcds * kMost) return FOCUS_E_SHAPE;
   if (p.planned) {
     hipLaunchKernelGGL(attend8_plan, dim3(1), dim3(kPlan), 0, s, a);
     const focus_status st = focus::launch_status();
@@ -763,9 +761,11 @@ focus_status launch(Args a, const Plan& p, hipStream_t s) {
   }
   const focus_status st = focus::launch_status();
   if (st != FOCUS_OK || p.single) return st;
-  hipLaunchKernelGGL((attend8_join<T, D>),
-                     dim3((uint32_t)(c.n_kv_heads * slices), (uint32_t)std::min(c.batch, kMaxGrid), (uint32_t)(batches * a.parts)),
-                     dim3(kJoin), 0, s, a);
+  // (a wave has 16 shares of 128 elements in flight)
+  if (p.shares >= kManyShares * c.batch)
+    hipLaunchKernelGGL((attend8_join<T, D, true>), dim3((uint32_t)(columns * (D / 32))), dim3(kJoin), 0, s, a);
+  else
+    hipLaunchKernelGGL((attend8_join<T, D, false>), dim3((uint32_t)focus::ceil_div(columns, kJoin / 64)), dim3(kJoin), 0, s, a);
   return focus::launch_status();
 }
 
