@@ -38,15 +38,12 @@ typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 constexpr int kThreads = 256, kWaves = 4;
 constexpr int kPages = 1024;    // pages held in LDS at a time
 constexpr int kWhole = 256;     // rows of a table that is not split
-constexpr int kUnit = 128;      // rows of a share's units times KV heads of a workgroup
+constexpr int kUnit = 128;      // rows of a share's units times sets of KV heads of a workgroup
 constexpr int kRows = 32;       // rows of a wave at a time
 constexpr int kMost = 512;      // columns of a KV head
 // Units that a sequence's beginning and end in a share cost: its queries, pages and first rows
 // arrive one after another, some 5 us in which a workgroup streams two units.
-#ifndef V_ENDS
-#define V_ENDS 4
-#endif
-constexpr int kEnds = V_ENDS;
+constexpr int kEnds = 4;
 
 // What a lane reads in the place of eight rows that begin past their sequence's end or
 // lie in a page outside the pool.
@@ -61,17 +58,15 @@ struct Plan {
   int64_t ends, ml, o;  // byte offsets
   size_t bytes;
   int cols, tiles;      // columns of a workgroup; workgroups a KV head's columns take
-  int wide, unit;       // KV heads of a workgroup; rows of a unit
+  int heads;            // KV heads of a wave
+  int wide, unit;       // sets of these of a workgroup; rows of a unit
   int64_t groups;       // workgroups of a share
   int columns;          // of all heads
   bool single, planned; // a share is a sequence; attend8_plan runs
 };
 
 // Workgroups of attend8_attend that a compute unit holds (by their registers).
-#ifndef V_R64
-#define V_R64 3
-#endif
-constexpr int resident(int head_dim) { return head_dim == 64 ? V_R64 : 2; }
+constexpr int resident(int head_dim, int tiles, int heads) { return head_dim == 64 && tiles * heads == 1 ? 3 : 2; }
 
 Plan make_plan(const focus_paged_attend8_desc* d) {
   const focus_paged_kv& c = d->cache.kv;
@@ -82,13 +77,19 @@ Plan make_plan(const focus_paged_attend8_desc* d) {
   // (float32 queries take three times the registers)
   p.cols = per_head > 16 && d->dtype == FOCUS_BF16 ? 32 : 16;
   p.tiles = (int)focus::ceil_div(per_head, p.cols);
-  // neighbouring heads' rows read together, where they lie side by side
-  p.wide = c.head_stride > c.row_stride ? 1 : c.n_kv_heads % 4 == 0 ? 4 : c.n_kv_heads % 2 == 0 ? 2 : 1;
+  // Neighbouring heads' rows read together, where they lie side by side; two heads of 64
+  // bytes, which share a cache line, by the same wave.  (By waves of their own half of the lines
+  // came twice: 16 x 10 000 rows of 32 such heads 165 us, now 138.  With two tiles of columns
+  // besides, the registers do not suffice.)
+  const bool beside = c.head_stride < c.row_stride;
+  p.heads = c.head_dim == 64 && p.cols == 16 && beside && c.n_kv_heads % 2 == 0 ? 2 : 1;
+  const int sets = c.n_kv_heads / p.heads;
+  p.wide = !beside ? 1 : sets % 4 == 0 ? 4 : sets % 2 == 0 ? 2 : 1;
   const int64_t heads = (int64_t)c.batch * c.n_kv_heads * p.tiles;
   p.single = d->split_keys == 0 && (p.cap <= kWhole || (p.cap <= 2 * kWhole && heads >= 128));
   if (p.single && heads <= 1024) p.wide = 1;
   p.planned = !p.single && c.batch > focus::kWave;
-  p.groups = (int64_t)c.n_kv_heads / p.wide * p.tiles;
+  p.groups = (int64_t)sets / p.wide * p.tiles;
   if (p.single) {
     p.unit = (int)std::max<int64_t>(p.cap, 1), p.shares = c.batch;
   } else if (d->split_keys > 0) {
@@ -96,7 +97,7 @@ Plan make_plan(const focus_paged_attend8_desc* d) {
   } else {
     p.unit = kUnit / p.wide;
     // as many as run together, but no more than there may be units
-    p.shares = std::min(std::max<int64_t>(1, resident(c.head_dim) * focus::device_cus() / p.groups),
+    p.shares = std::min(std::max<int64_t>(1, resident(c.head_dim, p.cols / 16, p.heads) * focus::device_cus() / p.groups),
                         c.batch * (std::max<int64_t>(1, focus::ceil_div(p.cap, p.unit)) + kEnds));
   }
   const int64_t partials = 2 * p.shares * p.columns;
@@ -264,24 +265,21 @@ __device__ inline bf16x8 widen8(uint32_t w0, uint32_t w1) {
 template <typename V, bool SHARED>
 __device__ __forceinline__ V load_row(const void* p) {
   const auto* from = reinterpret_cast<const __attribute__((address_space(1))) V*>(reinterpret_cast<uintptr_t>(p));
-#ifdef V_TEMP
-  return *from;
-#endif
   if constexpr (SHARED) return *from;
   else return __builtin_nontemporal_load(from);
 }
 
-template <int D> struct Tile {
+template <int D, int HEADS> struct Tile {
   static constexpr int kPer = D / 16;               // elements of a V row a lane holds
   static constexpr int kWords = kPer / 4;
   static constexpr int kPieces = D / 64;            // 16-byte pieces of a K row a lane holds
   using V = typename std::conditional<kWords == 2, u32x2, uint32_t>::type;
-  u32x4 k[2][kPieces];
-  V v[8];
-  float ks, vs;         // the scales of the rows of the lane's scores
-  __device__ uint32_t word(int j, int i) const {
-    if constexpr (kWords == 2) return v[j][i];
-    else return v[j];
+  u32x4 k[HEADS][2][kPieces];
+  V v[HEADS][8];
+  float ks[HEADS], vs[HEADS];  // the scales of the rows of the lane's scores
+  __device__ uint32_t word(int h, int j, int i) const {
+    if constexpr (kWords == 2) return v[h][j][i];
+    else return v[h][j];
   }
 };
 
@@ -289,17 +287,18 @@ template <int D> struct Tile {
 __device__ inline uint32_t nan_bytes(uint32_t w) { return (((w & 0x7f7f7f7fu) + 0x01010101u) >> 7) & 0x01010101u; }
 
 // SHARED: a KV head has more columns than a workgroup takes, whose workgroups read the same
-// rows.  TILES: 16 columns each, all of which use a wave's rows as they are loaded.
+// rows.  TILES: 16 columns each, all of which use a wave's rows as they are loaded.  HEADS: KV
+// heads of a wave, whose rows lie side by side.
 // T: of q and o.  float32 queries enter in three bf16 parts, weights in two (17 bits; their
 // rounding is far below that of a bf16 output) or, for float32 outputs, three.
-template <typename T, int D, int TILES, bool SHARED>
-__global__ __launch_bounds__(kThreads, resident(D)) void attend8_attend(Args a) {
-  using L = Tile<D>;
-  constexpr int kPitch = D + 4, kSteps = D / 32, kCols = 16 * TILES;
+template <typename T, int D, int TILES, int HEADS, bool SHARED>
+__global__ __launch_bounds__(kThreads, resident(D, TILES, HEADS)) void attend8_attend(Args a) {
+  using L = Tile<D, HEADS>;
+  constexpr int kPitch = D + 4, kSteps = D / 32, kCols = 16 * TILES, kStates = TILES * HEADS;
   constexpr int kParts = sizeof(T) == 2 ? 1 : 3, kWeightParts = sizeof(T) == 2 ? 2 : 3;
   __shared__ int s_page[kPages + 1];  // (rows may begin inside a page)
-  __shared__ float s_o[kWaves][kCols][kPitch];
-  __shared__ float2 s_ml[kWaves][kCols];
+  __shared__ float s_o[kWaves][HEADS * kCols][kPitch];
+  __shared__ float2 s_ml[kWaves][HEADS * kCols];
   const focus_paged_kv& c = a.d.cache.kv;
   const int H = a.d.n_heads, G = a.group;
   // (a wave's number in a scalar register: its loops are branches then, not masks)
@@ -320,9 +319,9 @@ __global__ __launch_bounds__(kThreads, resident(D)) void attend8_attend(Args a) 
     // of 512 bytes.
     share = blockIdx.x / a.units, g0 = (blockIdx.x + share / a.around) % a.units;
   }
-  g0 <<= a.wide_shift;
-  // waves of a KV head; this wave's head, and which of its waves it is
-  const int by = kWaves >> a.wide_shift, at_head = wave >> (2 - a.wide_shift), g = g0 + at_head, among = wave & (by - 1);
+  g0 *= HEADS << a.wide_shift;
+  // waves of a set of KV heads; this wave's first head, and which of the set's waves it is
+  const int by = kWaves >> a.wide_shift, at_set = wave >> (2 - a.wide_shift), g = g0 + HEADS * at_set, among = wave & (by - 1);
   const uint8_t* kbase = reinterpret_cast<const uint8_t*>(c.k) + (int64_t)g * c.head_stride;
   const uint8_t* vbase = reinterpret_cast<const uint8_t*>(c.v) + (int64_t)g * c.head_stride;
   const uint8_t* zeros = reinterpret_cast<const uint8_t*>(kZeros);
@@ -358,38 +357,39 @@ __global__ __launch_bounds__(kThreads, resident(D)) void attend8_attend(Args a) 
     if (cols <= 0) continue;
     const int sees_all = max(0, n - (tok.count - 1));
     int sees[TILES];
-    bf16x8 q[TILES][kParts][kSteps];  // column col, elements as the K rows' pieces
+    bf16x8 q[kStates][kParts][kSteps];  // column col, elements as the K rows' pieces
 #pragma unroll
-    for (int tile = 0; tile < TILES; ++tile) {
-      const int cc = tile_id * kCols + min(16 * tile + col, cols - 1), token = cc / G, head = cc - token * G;
+    for (int state = 0; state < kStates; ++state) {
+      const int tile = state % TILES, cc = tile_id * kCols + min(16 * tile + col, cols - 1), token = cc / G;
+      const int head = (g + state / TILES) * G + cc - token * G;
       sees[tile] = max(0, n - (tok.count - 1 - token));
-      const T* src = reinterpret_cast<const T*>(a.d.q) + (tok.first + token) * a.d.q_row + (int64_t)(g * G + head) * a.d.q_head;
+      const T* src = reinterpret_cast<const T*>(a.d.q) + (tok.first + token) * a.d.q_row + (int64_t)head * a.d.q_head;
 #pragma unroll
       for (int i = 0; i < kSteps; ++i) {
         const int e = (i / 2 * 4 + x) * 16 + i % 2 * 8;
         if constexpr (sizeof(T) == 2) {
-          q[tile][0][i] = *reinterpret_cast<const bf16x8*>(src + e);
+          q[state][0][i] = *reinterpret_cast<const bf16x8*>(src + e);
         } else {
 #pragma unroll
           for (int k = 0; k < 8; ++k) {
             float f = src[e + k];
 #pragma unroll
             for (int part = 0; part < kParts; ++part) {
-              q[tile][part][i][k] = (__bf16)f;
-              f -= (float)q[tile][part][i][k];
+              q[state][part][i][k] = (__bf16)f;
+              f -= (float)q[state][part][i][k];
             }
           }
         }
       }
     }
 
-    float m[TILES], l[TILES];
-    f32x4 o[TILES][L::kPer];
+    float m[kStates], l[kStates];
+    f32x4 o[kStates][L::kPer];
 #pragma unroll
-    for (int tile = 0; tile < TILES; ++tile) {
-      m[tile] = kMinit, l[tile] = 0.f;
+    for (int state = 0; state < kStates; ++state) {
+      m[state] = kMinit, l[state] = 0.f;
 #pragma unroll
-      for (int t = 0; t < L::kPer; ++t) o[tile][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+      for (int t = 0; t < L::kPer; ++t) o[state][t] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
     for (int seg = r0; seg < r1; seg += kPages << a.shift) {
       const int seg_end = min(r1, seg + (kPages << a.shift)), page0 = seg >> a.shift;
@@ -406,6 +406,7 @@ __global__ __launch_bounds__(kThreads, resident(D)) void attend8_attend(Args a) 
       // the page that holds the eight rows at r (negative: none, or past end)
       auto page = [&](int r, int end) { return r < end ? s_page[(r >> a.shift) - page0] : -1; };
       // Rows of eight lie in one page, so all of them can be read where the first is cached.
+      // Heads that share a cache line are read in turn, so that it comes once.
       auto load = [&](L& w, int r, int end) {
         const int pk = page(r + k8, end), pv = page(r + v8, end);
         const uint32_t step = (uint32_t)c.row_stride, far = (uint32_t)c.page_stride;
@@ -415,134 +416,147 @@ __global__ __launch_bounds__(kThreads, resident(D)) void attend8_attend(Args a) 
         };
         const uint8_t* kp = (pk >= 0 ? at(kbase, pk, r + k8) : zeros) + (uint64_t)(uint32_t)k_in * ks + x * 16;
         const uint8_t* vp = (pv >= 0 ? at(vbase, pv, r + v8) : zeros) + col * L::kPer;
+        const uint64_t k_next = pk >= 0 ? c.head_stride : 0, v_next = pv >= 0 ? c.head_stride : 0;
 #pragma unroll
         for (int t = 0; t < 2; ++t)
 #pragma unroll
-          for (int i = 0; i < L::kPieces; ++i) w.k[t][i] = load_row<u32x4, SHARED>(kp + 4 * t * (uint64_t)ks + i * 64);
+          for (int i = 0; i < L::kPieces; ++i)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) w.v[j] = load_row<typename L::V, SHARED>(vp + j * (uint64_t)vs);
+            for (int h = 0; h < HEADS; ++h)
+              w.k[h][t][i] = load_row<u32x4, SHARED>(kp + 4 * t * (uint64_t)ks + i * 64 + h * k_next);
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+#pragma unroll
+          for (int h = 0; h < HEADS; ++h) w.v[h][j] = load_row<typename L::V, SHARED>(vp + j * (uint64_t)vs + h * v_next);
         const uint64_t sc = (uint64_t)(uint32_t)pv * page_scales + (uint32_t)(((r + v8) & mask) >> a.scale_shift);
         const float* none = reinterpret_cast<const float*>(kZeros);
-        w.ks = load_row<float, true>(pv >= 0 ? ks_base + sc : none);
-        w.vs = load_row<float, true>(pv >= 0 ? vs_base + sc : none);
+#pragma unroll
+        for (int h = 0; h < HEADS; ++h) {
+          w.ks[h] = load_row<float, true>(pv >= 0 ? ks_base + h * per_page + sc : none);
+          w.vs[h] = load_row<float, true>(pv >= 0 ? vs_base + h * per_page + sc : none);
+        }
       };
       auto compute = [&](L& w, int r, auto whole) {
         constexpr bool kWholeTile = decltype(whole)::value;
         const int row = r + v8;  // of the lane's first score
         // of the lane's rows, those that count: the first `live`
         const int live = page(row, seg_end) >= 0 ? 8 : 0;
-        uint32_t bad = 0;
-        if constexpr (!kWholeTile) {
-          // Rows past the end may hold anything, and those that only later tokens see a NaN,
-          // and zero times a NaN is a NaN: the first are cleared, the NaN of the others
-          // taken out and put into the sums of the columns that see them.
-          const int in = min(live, seg_end - row);
 #pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            if (j >= in) w.v[j] = typename L::V{};
-#pragma unroll
-            for (int i = 0; i < L::kWords; ++i) bad |= nan_bytes(w.word(j, i));
-          }
-        }
-        float y[TILES][8];
-#pragma unroll
-        for (int tile = 0; tile < TILES; ++tile) {
-          f32x4 s[2];
-#pragma unroll
-          for (int t = 0; t < 2; ++t) {
-            s[t] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int i = 0; i < kSteps; ++i) {
-              const bf16x8 k = widen8(w.k[t][i / 2][i % 2 * 2], w.k[t][i / 2][i % 2 * 2 + 1]);
-#pragma unroll
-              for (int part = kParts - 1; part >= 0; --part)
-                s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, q[tile][part][i], s[t], 0, 0, 0);
-            }
-          }
-          const int lives = kWholeTile ? live : min(live, min(seg_end, sees[tile]) - row);
-          float mx = m[tile];
-#pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            y[tile][j] = j < lives ? s[j / 4][j % 4] * w.ks : -INFINITY;
-            mx = fmaxf(mx, y[tile][j]);
-          }
-          mx = focus::max_column(mx);
-          // (scaled after the difference: scaled before, a score of 4096 would be rounded to
-          // 2^-12, and so would the weight)
-          if (__ballot(mx > m[tile])) {  // rare once a few rows are seen
-            const float alpha = __builtin_amdgcn_exp2f((m[tile] - mx) * a.sc);
-            m[tile] = mx;
-            l[tile] *= alpha;
-#pragma unroll
-            for (int t = 0; t < L::kPer; ++t) o[tile][t] *= alpha;
-          }
-#pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            y[tile][j] = __builtin_amdgcn_exp2f((y[tile][j] - m[tile]) * a.sc);
-            l[tile] += y[tile][j];
-            y[tile][j] = kWholeTile || j < lives ? y[tile][j] * w.vs : 0.f;
-          }
-        }
-        if constexpr (!kWholeTile) {
-          if (__ballot(bad != 0)) {
-#pragma unroll
-            for (int t = 0; t < L::kPer; ++t) {
-              bf16x8 mark;
-#pragma unroll
-              for (int j = 0; j < 8; ++j)
-                mark[j] = (__bf16)(nan_bytes(w.word(j, t / 4)) >> (t % 4 * 8) & 1 ? 1.f : 0.f);
-#pragma unroll
-              for (int tile = 0; tile < TILES; ++tile) {
-                const int lives = min(live, min(seg_end, sees[tile]) - row);
-                bf16x8 seen;
-#pragma unroll
-                for (int j = 0; j < 8; ++j) seen[j] = (__bf16)(j < lives ? 1.f : 0.f);
-                const f32x4 k = __builtin_amdgcn_mfma_f32_16x16x32_bf16(mark, seen, f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                  if (k[e] != 0.f) o[tile][t][e] = NAN;
-              }
-            }
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-#pragma unroll
-              for (int i = 0; i < L::kWords; ++i) {
-                const uint32_t keep = ~(nan_bytes(w.word(j, i)) * 0xffu);
-                if constexpr (L::kWords == 2) w.v[j][i] &= keep;
-                else w.v[j] &= keep;
-              }
-          }
-        }
-        // product t's rows of V^T: pairs of rows by a byte permutation, then widened; half of
-        // them at a time
-        bf16x8 p[TILES][kWeightParts];
-#pragma unroll
-        for (int tile = 0; tile < TILES; ++tile)
-#pragma unroll
-          for (int part = 0; part < kWeightParts; ++part)
+        for (int h = 0; h < HEADS; ++h) {
+          const int at0 = h * TILES;  // the head's first state
+          uint32_t bad = 0;
+          if constexpr (!kWholeTile) {
+            // Rows past the end may hold anything, and those that only later tokens see a NaN,
+            // and zero times a NaN is a NaN: the first are cleared, the NaN of the others
+            // taken out and put into the sums of the columns that see them.
+            const int in = min(live, seg_end - row);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-              p[tile][part][j] = (__bf16)y[tile][j];
-              y[tile][j] -= (float)p[tile][part][j];
+              if (j >= in) w.v[h][j] = typename L::V{};
+#pragma unroll
+              for (int i = 0; i < L::kWords; ++i) bad |= nan_bytes(w.word(h, j, i));
+            }
+          }
+          float y[TILES][8];
+#pragma unroll
+          for (int tile = 0; tile < TILES; ++tile) {
+            f32x4 s[2];
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+              s[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+              for (int i = 0; i < kSteps; ++i) {
+                const bf16x8 k = widen8(w.k[h][t][i / 2][i % 2 * 2], w.k[h][t][i / 2][i % 2 * 2 + 1]);
+#pragma unroll
+                for (int part = kParts - 1; part >= 0; --part)
+                  s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, q[at0 + tile][part][i], s[t], 0, 0, 0);
+              }
+            }
+            const int lives = kWholeTile ? live : min(live, min(seg_end, sees[tile]) - row);
+            float mx = m[at0 + tile];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+              y[tile][j] = j < lives ? s[j / 4][j % 4] * w.ks[h] : -INFINITY;
+              mx = fmaxf(mx, y[tile][j]);
+            }
+            mx = focus::max_column(mx);
+            // (scaled after the difference: scaled before, a score of 4096 would be rounded to
+            // 2^-12, and so would the weight)
+            if (__ballot(mx > m[at0 + tile])) {  // rare once a few rows are seen
+              const float alpha = __builtin_amdgcn_exp2f((m[at0 + tile] - mx) * a.sc);
+              m[at0 + tile] = mx;
+              l[at0 + tile] *= alpha;
+#pragma unroll
+              for (int t = 0; t < L::kPer; ++t) o[at0 + tile][t] *= alpha;
             }
 #pragma unroll
-        for (int i = 0; i < L::kWords; ++i) {
-          u32x4 z[4];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const uint32_t lo = __builtin_amdgcn_perm(w.word(2 * e + 1, i), w.word(2 * e, i), 0x05010400);
-            const uint32_t hi = __builtin_amdgcn_perm(w.word(2 * e + 1, i), w.word(2 * e, i), 0x07030602);
-            z[0][e] = widen(lo, false), z[1][e] = widen(lo, true);
-            z[2][e] = widen(hi, false), z[3][e] = widen(hi, true);
+            for (int j = 0; j < 8; ++j) {
+              y[tile][j] = __builtin_amdgcn_exp2f((y[tile][j] - m[at0 + tile]) * a.sc);
+              l[at0 + tile] += y[tile][j];
+              y[tile][j] = kWholeTile || j < lives ? y[tile][j] * w.vs[h] : 0.f;
+            }
           }
+          if constexpr (!kWholeTile) {
+            if (__ballot(bad != 0)) {
+#pragma unroll
+              for (int t = 0; t < L::kPer; ++t) {
+                bf16x8 mark;
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                  mark[j] = (__bf16)(nan_bytes(w.word(h, j, t / 4)) >> (t % 4 * 8) & 1 ? 1.f : 0.f);
+#pragma unroll
+                for (int tile = 0; tile < TILES; ++tile) {
+                  const int lives = min(live, min(seg_end, sees[tile]) - row);
+                  bf16x8 seen;
+#pragma unroll
+                  for (int j = 0; j < 8; ++j) seen[j] = (__bf16)(j < lives ? 1.f : 0.f);
+                  const f32x4 k = __builtin_amdgcn_mfma_f32_16x16x32_bf16(mark, seen, f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+#pragma unroll
+                  for (int e = 0; e < 4; ++e)
+                    if (k[e] != 0.f) o[at0 + tile][t][e] = NAN;
+                }
+              }
+#pragma unroll
+              for (int j = 0; j < 8; ++j)
+#pragma unroll
+                for (int i = 0; i < L::kWords; ++i) {
+                  const uint32_t keep = ~(nan_bytes(w.word(h, j, i)) * 0xffu);
+                  if constexpr (L::kWords == 2) w.v[h][j][i] &= keep;
+                  else w.v[h][j] &= keep;
+                }
+            }
+          }
+          // product t's rows of V^T: pairs of rows by a byte permutation, then widened; half of
+          // them at a time
+          bf16x8 p[TILES][kWeightParts];
 #pragma unroll
           for (int tile = 0; tile < TILES; ++tile)
 #pragma unroll
             for (int part = 0; part < kWeightParts; ++part)
 #pragma unroll
-              for (int t = 0; t < 4; ++t)
-                o[tile][4 * i + t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, z[t]), p[tile][part],
-                                                                             o[tile][4 * i + t], 0, 0, 0);
+              for (int j = 0; j < 8; ++j) {
+                p[tile][part][j] = (__bf16)y[tile][j];
+                y[tile][j] -= (float)p[tile][part][j];
+              }
+#pragma unroll
+          for (int i = 0; i < L::kWords; ++i) {
+            u32x4 z[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const uint32_t lo = __builtin_amdgcn_perm(w.word(h, 2 * e + 1, i), w.word(h, 2 * e, i), 0x05010400);
+              const uint32_t hi = __builtin_amdgcn_perm(w.word(h, 2 * e + 1, i), w.word(h, 2 * e, i), 0x07030602);
+              z[0][e] = widen(lo, false), z[1][e] = widen(lo, true);
+              z[2][e] = widen(hi, false), z[3][e] = widen(hi, true);
+            }
+#pragma unroll
+            for (int tile = 0; tile < TILES; ++tile)
+#pragma unroll
+              for (int part = 0; part < kWeightParts; ++part)
+#pragma unroll
+                for (int t = 0; t < 4; ++t)
+                  o[at0 + tile][4 * i + t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, z[t]), p[tile][part],
+                                                                               o[at0 + tile][4 * i + t], 0, 0, 0);
+          }
         }
       };
       // A wave's whole tiles, two a round, the next one's loads in flight while one is
@@ -555,20 +569,7 @@ __global__ __launch_bounds__(kThreads, resident(D)) void attend8_attend(Args a) 
       if (r < full_end) {
         L w0, w1;
         load(w0, r, full_end);
-#ifdef V_PRIO
-        const int quarter = (r1 - r0) / 4;
-        int lower = r0 + quarter, prio = 3;
-        __builtin_amdgcn_s_setprio(3);
-#endif
         for (; r + stride < full_end; r += 2 * stride) {
-#ifdef V_PRIO
-        if (r >= lower) {
-          lower += quarter, --prio;
-          if (prio == 2) __builtin_amdgcn_s_setprio(2);
-          else if (prio == 1) __builtin_amdgcn_s_setprio(1);
-          else __builtin_amdgcn_s_setprio(0);
-        }
-#endif
           load(w1, r + stride, full_end);
           compute(w0, r, std::true_type{});
           load(w0, r + 2 * stride, full_end);
@@ -588,34 +589,39 @@ __global__ __launch_bounds__(kThreads, resident(D)) void attend8_attend(Args a) 
     }
     __syncthreads();  // the last sequence's outputs are read
 #pragma unroll
-    for (int tile = 0; tile < TILES; ++tile) {
+    for (int state = 0; state < kStates; ++state) {
 #pragma unroll
       for (int e = 0; e < 4; ++e)
 #pragma unroll
         for (int t = 0; t < L::kPer; t += 4)
-          *reinterpret_cast<float4*>(&s_o[wave][16 * tile + col][(x * 4 + e) * L::kPer + t]) =
-              make_float4(o[tile][t][e], o[tile][t + 1][e], o[tile][t + 2][e], o[tile][t + 3][e]);
+          *reinterpret_cast<float4*>(&s_o[wave][16 * state + col][(x * 4 + e) * L::kPer + t]) =
+              make_float4(o[state][t][e], o[state][t + 1][e], o[state][t + 2][e], o[state][t + 3][e]);
       // the waves' parts of each column, joined
-      l[tile] += __shfl_xor(l[tile], 16);
-      l[tile] += __shfl_xor(l[tile], 32);
-      if (x == 0) s_ml[wave][16 * tile + col] = make_float2(m[tile], l[tile]);
+      l[state] += __shfl_xor(l[state], 16);
+      l[state] += __shfl_xor(l[state], 32);
+      if (x == 0) s_ml[wave][16 * state + col] = make_float2(m[state], l[state]);
     }
     __syncthreads();
     constexpr int kLanes = D / 4;  // threads of a column, four elements each
     const int e = tid % kLanes * 4;
-    for (int h = tid / kLanes, w0 = 0; w0 < kWaves; h += kThreads / kLanes) {
-      while (h >= cols && w0 < kWaves) h -= cols, w0 += by;
+    // over the columns `h` of each head of the sets, which begin at waves w0
+    for (int h = tid / kLanes, w0 = 0, second = 0; w0 < kWaves; h += kThreads / kLanes) {
+      while (h >= cols && w0 < kWaves) {
+        h -= cols, ++second;
+        if (second == HEADS) second = 0, w0 += by;
+      }
       if (w0 >= kWaves) break;
-      float2 ml = s_ml[w0][h];
-      f32x4 y = *reinterpret_cast<const f32x4*>(&s_o[w0][h][e]);
+      const int at_lds = second * kCols + h;
+      float2 ml = s_ml[w0][at_lds];
+      f32x4 y = *reinterpret_cast<const f32x4*>(&s_o[w0][at_lds][e]);
       for (int w = w0 + 1; w < w0 + by; ++w) {
-        const float2 other = s_ml[w][h];
+        const float2 other = s_ml[w][at_lds];
         const float M = fmaxf(ml.x, other.x);
         const float f = __builtin_amdgcn_exp2f((ml.x - M) * a.sc), f2 = __builtin_amdgcn_exp2f((other.x - M) * a.sc);
         ml = make_float2(M, fmaf(ml.y, f, other.y * f2));
-        y = y * f + *reinterpret_cast<const f32x4*>(&s_o[w][h][e]) * f2;
+        y = y * f + *reinterpret_cast<const f32x4*>(&s_o[w][at_lds][e]) * f2;
       }
-      const int kv = g0 + (w0 >> (2 - a.wide_shift)), at_col = tile_id * kCols + h;
+      const int kv = g0 + HEADS * (w0 >> (2 - a.wide_shift)) + second, at_col = tile_id * kCols + h;
       if (chunks == 1) {
         const int i = at_col / G;
         const int64_t at = (tok.first + i) * H + kv * G + (at_col - i * G);
@@ -751,14 +757,22 @@ focus_status launch(Args a, const Plan& p, hipStream_t s) {
   }
   const dim3 grid((uint32_t)(p.tiles > 1 ? focus::ceil_div(a.units * p.shares, focus::kXcds) * focus::kXcds * p.tiles
                                          : p.groups * p.shares));
-  if constexpr (sizeof(T) == 2) {
-    if (p.cols == 32 && p.tiles > 1) hipLaunchKernelGGL((attend8_attend<T, D, 2, true>), grid, dim3(kThreads), 0, s, a);
-    else if (p.cols == 32) hipLaunchKernelGGL((attend8_attend<T, D, 2, false>), grid, dim3(kThreads), 0, s, a);
-    else hipLaunchKernelGGL((attend8_attend<T, D, 1, false>), grid, dim3(kThreads), 0, s, a);
-  } else {
-    if (p.tiles > 1) hipLaunchKernelGGL((attend8_attend<T, D, 1, true>), grid, dim3(kThreads), 0, s, a);
-    else hipLaunchKernelGGL((attend8_attend<T, D, 1, false>), grid, dim3(kThreads), 0, s, a);
-  }
+  auto attend = [&](auto tiles, auto heads, auto shared) {
+    constexpr int kTiles = decltype(tiles)::value, kHeads = decltype(heads)::value;
+    constexpr bool kShared = decltype(shared)::value;
+    hipLaunchKernelGGL((attend8_attend<T, D, kTiles, kHeads, kShared>), grid, dim3(kThreads), 0, s, a);
+  };
+  auto of_heads = [&](auto tiles, auto shared) {
+    if constexpr (D == 64 && decltype(tiles)::value == 1) {
+      if (p.heads == 2) return attend(tiles, std::integral_constant<int, 2>{}, shared);
+    }
+    attend(tiles, std::integral_constant<int, 1>{}, shared);
+  };
+  constexpr std::integral_constant<int, sizeof(T) == 2 ? 2 : 1> kMore;  // tiles of more than 16 columns
+  constexpr std::integral_constant<int, 1> kOne;
+  if (p.tiles > 1) of_heads(kMore, std::true_type{});
+  else if (p.cols == 32) of_heads(kMore, std::false_type{});
+  else of_heads(kOne, std::false_type{});
   const focus_status st = focus::launch_status();
   if (st != FOCUS_OK || p.single) return st;
   // (a wave has 16 shares of 128 elements in flight)
