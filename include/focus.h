@@ -14,8 +14,8 @@
  *   focus_paged_decode                 one-token attention over a paged cache
  *   focus_paged_evict                  a paged cache cut down to a budget
  *   focus_paged_extend                 page tables and slot maps from the rows to come
- *   focus_paged_append8                rows stored in a paged cache of 8 bits
- *   focus_paged_attend8                attention of the newest tokens over one
+ *   focus_paged_append                rows stored in a paged cache of 8 bits
+ *   focus_paged_attend                attention of the newest tokens over one
  *
  * Conventions shared by every call
  * --------------------------------
@@ -879,7 +879,7 @@ focus_status focus_paged_evict(const focus_paged_evict_desc* d, focus_stream_t s
 
 /* Slots for the rows to come and back from the rows that go, for every sequence of a
  * paged cache (of any type), without the host: page tables, lengths and the maps that
- * focus_rope, focus_paged_append8 and focus_paged_attend8 take.  With n = length[b],
+ * focus_rope, focus_paged_append and focus_paged_attend take.  With n = length[b],
  * a = add[b] and P = page_rows:
  *   a < 0   the last -a rows go (all of them if there are fewer): length[b] = n' =
  *           max(n + a, 0), table entries ceil(n' / P) .. ceil(n / P) - 1 are pushed on the
@@ -934,7 +934,7 @@ focus_status focus_paged_extend(const focus_paged_extend_desc* d, focus_stream_t
 /* A paged K/V cache in FOCUS_E4M3, with a scale for each block of scale_rows rows and KV
  * head: row r of sequence b in page p stands for its 8-bit elements times
  * k_scale[(p * n_kv_heads + g) * (page_rows / scale_rows) + r % page_rows / scale_rows].
- * Scales may be any float32 (focus_paged_append8 makes powers of two). */
+ * Scales may be any float32 (focus_paged_append makes powers of two). */
 typedef struct {
   focus_paged_kv kv;            /* dtype FOCUS_E4M3; strides in elements, whole
                                    16-byte pieces; weight NULL               */
@@ -970,13 +970,13 @@ typedef struct {
   const void* v;
   int64_t v_row, v_head;
   int32_t* err;                 /* optional error word                       */
-} focus_paged_append8_desc;
+} focus_paged_append_desc;
 
 /* Errors: E_NULL, E_ARG, E_DTYPE, E_SHAPE (n_rows of 2^31, or not batch without cu_rows,
  * among others), E_UNSUPPORTED, E_HIP.  A block in a page outside the pool
  * (FOCUS_ERR_BOUNDS) and rows past max_pages * page_rows (FOCUS_ERR_CAPACITY) are not
  * stored; offsets outside [0, n_rows] are clipped to it (FOCUS_ERR_BOUNDS). */
-focus_status focus_paged_append8(const focus_paged_append8_desc* d, focus_stream_t stream);
+focus_status focus_paged_append(const focus_paged_append_desc* d, focus_stream_t stream);
 
 /* Attention of the newest tokens of every sequence over its cached rows: of sequence b the
  * rows cu_rows[b] .. cu_rows[b + 1] - 1 of q, m of them, are its last m tokens (whose own
@@ -1008,19 +1008,19 @@ typedef struct {
   void* workspace;
   size_t workspace_bytes;
   int32_t* err;
-} focus_paged_attend8_desc;
+} focus_paged_attend_desc;
 
 /* Workspace bytes of this descriptor on the current device (0 where none is needed, or the
  * call refuses it).  The workspace is in use until the call's kernels end; calls that share
  * one on overlapping streams race. */
-size_t focus_paged_attend8_workspace(const focus_paged_attend8_desc* d);
+size_t focus_paged_attend_workspace(const focus_paged_attend_desc* d);
 /* Errors: E_NULL, E_ARG, E_DTYPE, E_SHAPE (as focus_paged_decode; n_rows not batch without
  * cu_rows), E_UNSUPPORTED, E_WORKSPACE, E_HIP.  Rows of a page outside the pool are left
  * out of the softmax (FOCUS_ERR_BOUNDS); a length outside [0, max_pages * page_rows] is
  * clipped to it (FOCUS_ERR_CAPACITY); the rows of a sequence that has more than max_rows
  * (FOCUS_ERR_CAPACITY) or whose offsets do not ascend within [0, n_rows]
  * (FOCUS_ERR_BOUNDS) are left as they were. */
-focus_status focus_paged_attend8(const focus_paged_attend8_desc* d, focus_stream_t stream);
+focus_status focus_paged_attend(const focus_paged_attend_desc* d, focus_stream_t stream);
 
 #ifdef __cplusplus
 }

@@ -23,8 +23,8 @@ Serving over a paged cache:
 with its page tables kept on the device, and in 8 bits:
 
     rows   = focus_paged_extend(table, length, page_rows, add, free_pages, free_count, n)
-    focus_paged_append8(k, v, cache8, rows.start, rows.cu_rows)  # rows stored in 8 bits
-    o, lse = focus_paged_attend8(q, cache8, rows.cu_rows, max_rows=4)  # the newest tokens
+    focus_paged_append(k, v, cache8, rows.start, rows.cu_rows)  # rows stored in 8 bits
+    o, lse = focus_paged_attend(q, cache8, rows.cu_rows, max_rows=4)  # the newest tokens
 """
 
 from __future__ import annotations
@@ -37,7 +37,7 @@ import numpy as np
 import torch
 
 from ._abi import (AdapterDesc, AdapterLayerDesc, AttnDesc, CompactDesc, DecodeDesc, DecodeSched, FidelityDesc, FocusError, GemmDesc, LayoutDesc, LayoutTotals,
-                   PagedAppend8Desc, PagedAttend8Desc, PagedDecodeDesc, PagedEvictDesc, PagedExtendDesc, PagedKv, PagedKv8, QkvDesc,
+                   PagedAppendDesc, PagedAttendDesc, PagedDecodeDesc, PagedEvictDesc, PagedExtendDesc, PagedKv, PagedKv8, QkvDesc,
                    RopeDesc, RopeScaling, FOCUS_BF16, FOCUS_F32, FOCUS_E4M3, FOCUS_E_WORKSPACE, FOCUS_MASK_CT, FOCUS_MASK_KMER_LOCAL,
                    FOCUS_TOK_BASE, FOCUS_TOK_SUMMARY, FOCUS_STEP_SUMMARY, FOCUS_STEP_WINDOW_END,
                    FOCUS_ERR_CAPACITY, FOCUS_ERR_BOUNDS, FOCUS_ERR_PLAN,
@@ -56,7 +56,7 @@ __all__ = ["focus_layout_plan", "focus_layout", "focus_compact_kv", "focus_windo
            "FOCUS_ERR_CAPACITY", "FOCUS_ERR_BOUNDS", "FOCUS_ERR_PLAN",
            "PagedCache", "focus_rope_turns", "focus_rope", "focus_paged_decode", "focus_paged_decode_workspace",
            "focus_paged_evict", "focus_paged_evict_workspace", "PagedRows", "focus_paged_extend", "PagedCache8",
-           "focus_paged_append8", "focus_paged_attend8", "focus_paged_attend8_workspace",
+           "focus_paged_append", "focus_paged_attend", "focus_paged_attend_workspace",
            "FOCUS_ROPE_NONE", "FOCUS_ROPE_LINEAR", "FOCUS_ROPE_BASE", "FOCUS_ROPE_BANDS",
            "FOCUS_ROPE_INTERLEAVED", "FOCUS_ROPE_HALF"]
 
@@ -976,7 +976,7 @@ class PagedCache8:
                         _need(scale, f32, None, dev, "k_scale"), _need(self.v_scale, f32, scales, dev, "v_scale"))
 
 
-def focus_paged_append8(k, v, cache: PagedCache8, start, cu_rows=None, err=None, stream=None):
+def focus_paged_append(k, v, cache: PagedCache8, start, cu_rows=None, err=None, stream=None):
     """New rows of k and v [rows, H_kv, D] (bfloat16 or float32, any row and head strides)
     stored in an 8-bit paged cache: rows cu_rows[b] : cu_rows[b + 1] behind the first start[b]
     of sequence b (cu_rows None: one row of every sequence), cache.length raised past them.
@@ -988,31 +988,31 @@ def focus_paged_append8(k, v, cache: PagedCache8, start, cu_rows=None, err=None,
     if k.dim() != 3 or dtype not in _DTYPES:
         raise ValueError("k must be [rows, heads, D], bfloat16 or float32")
     shape = (k.shape[0], kv.n_kv_heads, kv.head_dim)
-    d = PagedAppend8Desc(c, _DTYPES[dtype], 0, shape[0],
+    d = PagedAppendDesc(c, _DTYPES[dtype], 0, shape[0],
                          None if cu_rows is None else _need(cu_rows, torch.int32, (kv.batch + 1,), dev, "cu_rows"),
                          _need(start, torch.int32, (kv.batch,), dev, "start"), *_rows(k, shape, dtype, dev, "k"),
                          *_rows(v, shape, dtype, dev, "v"), None if err is None else _err_ptr(err, dev))
-    _launch("focus_paged_append8", d, dev, stream)
+    _launch("focus_paged_append", d, dev, stream)
 
 
-def _paged_attend8_desc(q, cache, cu_rows, max_rows, o, lse, split_keys, softmax_scale, err):
+def _paged_attend_desc(q, cache, cu_rows, max_rows, o, lse, split_keys, softmax_scale, err):
     """The descriptor without a workspace; o and lse addresses."""
     c = cache.desc()
     kv, dev, dtype, shape = c.kv, q.get_device(), q.dtype, q.shape
     if len(shape) != 3 or shape[2] != kv.head_dim or dev != cache.k.get_device() or dtype not in _DTYPES:
         raise ValueError("q must be [rows, heads, D], bfloat16 or float32, of the cache's head_dim and device")
-    return PagedAttend8Desc(c, _DTYPES[dtype], shape[1], _i32(max_rows, "max_rows"), _i32(split_keys, "split_keys"),
+    return PagedAttendDesc(c, _DTYPES[dtype], shape[1], _i32(max_rows, "max_rows"), _i32(split_keys, "split_keys"),
                             float(softmax_scale), 0, shape[0],
                             None if cu_rows is None else _need(cu_rows, torch.int32, (kv.batch + 1,), dev, "cu_rows"),
                             *_rows(q, shape, dtype, dev, "q"), o, lse, None, 0, None if err is None else _err_ptr(err, dev))
 
 
-def focus_paged_attend8_workspace(q, cache: PagedCache8, cu_rows=None, max_rows: int = 1, split_keys: int = 0) -> int:
-    d = _paged_attend8_desc(q, cache, cu_rows, max_rows, None, None, split_keys, 0.0, None)
-    return _query("focus_paged_attend8_workspace", d, q.get_device())
+def focus_paged_attend_workspace(q, cache: PagedCache8, cu_rows=None, max_rows: int = 1, split_keys: int = 0) -> int:
+    d = _paged_attend_desc(q, cache, cu_rows, max_rows, None, None, split_keys, 0.0, None)
+    return _query("focus_paged_attend_workspace", d, q.get_device())
 
 
-def focus_paged_attend8(q, cache: PagedCache8, cu_rows=None, max_rows: int = 1, o=None, lse=None, workspace=None,
+def focus_paged_attend(q, cache: PagedCache8, cu_rows=None, max_rows: int = 1, o=None, lse=None, workspace=None,
                         split_keys: int = 0, softmax_scale: float = 0.0, want_lse: bool = True, err=None, stream=None):
     """Attention of the newest tokens of every sequence over an 8-bit paged cache that holds
     their rows already: q [rows, H, D] (turned; bfloat16 or float32; D 64 or 128), rows
@@ -1032,16 +1032,16 @@ def focus_paged_attend8(q, cache: PagedCache8, cu_rows=None, max_rows: int = 1, 
     elif want_lse:
         lse = _empty(tuple(q.shape[:2]), torch.float32, q.device, stream)
         lse_at = lse.data_ptr()
-    d = _paged_attend8_desc(q, cache, cu_rows, max_rows, o_at, lse_at, split_keys, softmax_scale, err)
+    d = _paged_attend_desc(q, cache, cu_rows, max_rows, o_at, lse_at, split_keys, softmax_scale, err)
     if workspace is not None:
         d.workspace, d.workspace_bytes = _workspace(workspace, dev)
     # a call that needs a workspace says so before anything is enqueued; those that need none,
     # the shortest, are spared the question
-    elif _launch("focus_paged_attend8", d, dev, stream, FOCUS_E_WORKSPACE) == 0:
+    elif _launch("focus_paged_attend", d, dev, stream, FOCUS_E_WORKSPACE) == 0:
         return o, lse
     else:
-        n = _query("focus_paged_attend8_workspace", d, dev)
+        n = _query("focus_paged_attend_workspace", d, dev)
         workspace = _scratch(n, q.device, stream)
         d.workspace, d.workspace_bytes = workspace.data_ptr(), n
-    _launch("focus_paged_attend8", d, dev, stream)
+    _launch("focus_paged_attend", d, dev, stream)
     return o, lse

@@ -163,12 +163,12 @@ class PagedKv8(C.Structure):
     _fields_ = [("kv", PagedKv), ("scale_rows", i32), ("reserved", i32), ("k_scale", p), ("v_scale", p)]
 
 
-class PagedAppend8Desc(C.Structure):
+class PagedAppendDesc(C.Structure):
     _fields_ = [("cache", PagedKv8), ("dtype", i32), ("reserved", i32), ("n_rows", i64), ("cu_rows", p), ("start", p),
                 ("k", p), ("k_row", i64), ("k_head", i64), ("v", p), ("v_row", i64), ("v_head", i64), ("err", p)]
 
 
-class PagedAttend8Desc(C.Structure):
+class PagedAttendDesc(C.Structure):
     _fields_ = [("cache", PagedKv8), ("dtype", i32), ("n_heads", i32), ("max_rows", i32), ("split_keys", i32),
                 ("softmax_scale", f32), ("reserved", i32), ("n_rows", i64), ("cu_rows", p), ("q", p), ("q_row", i64),
                 ("q_head", i64), ("o", p), ("lse", p), ("workspace", p), ("workspace_bytes", sz), ("err", p)]
@@ -176,7 +176,7 @@ class PagedAttend8Desc(C.Structure):
 
 STRUCTS = [LayoutTotals, LayoutDesc, CompactDesc, AttnDesc, DecodeDesc, FidelityDesc, GemmDesc, AdapterDesc,
            AdapterLayerDesc, QkvDesc, DecodeSched, RopeScaling, PagedKv, RopeDesc, PagedDecodeDesc, PagedEvictDesc,
-           PagedExtendDesc, PagedKv8, PagedAppend8Desc, PagedAttend8Desc]
+           PagedExtendDesc, PagedKv8, PagedAppendDesc, PagedAttendDesc]
 
 # name -> (restype, argtypes): every symbol include/focus.h declares
 SYMBOLS = {
@@ -208,9 +208,9 @@ SYMBOLS = {
     "focus_paged_evict_workspace": (sz, [C.POINTER(PagedEvictDesc)]),
     "focus_paged_evict": (i32, [C.POINTER(PagedEvictDesc), p]),
     "focus_paged_extend": (i32, [C.POINTER(PagedExtendDesc), p]),
-    "focus_paged_append8": (i32, [C.POINTER(PagedAppend8Desc), p]),
-    "focus_paged_attend8_workspace": (sz, [C.POINTER(PagedAttend8Desc)]),
-    "focus_paged_attend8": (i32, [C.POINTER(PagedAttend8Desc), p]),
+    "focus_paged_append": (i32, [C.POINTER(PagedAppendDesc), p]),
+    "focus_paged_attend_workspace": (sz, [C.POINTER(PagedAttendDesc)]),
+    "focus_paged_attend": (i32, [C.POINTER(PagedAttendDesc), p]),
 }
 
 

@@ -22,8 +22,8 @@ INCLUDE = os.path.join(ROOT, "include")
 BUILD = os.path.join(ROOT, "_build")
 LIB = os.path.join(PKG, "libfocus.so")
 SOURCES = ["api.hip", "layout.hip", "compact.hip", "window_attn.hip", "decode.hip", "fidelity.hip", "gemm.hip", "adapter.hip",
-           "rope.hip", "paged_decode.hip", "paged_evict.hip", "paged_extend.hip", "paged_append8.hip",
-           "paged_attend8.hip"]
+           "rope.hip", "paged_decode.hip", "paged_evict.hip", "paged_extend.hip", "paged_append.hip",
+           "paged_attend.hip"]
 
 ARCH = "gfx950"
 # Packed fp32 VALU ops are kept out of all device code (-packed-fp32-ops); the

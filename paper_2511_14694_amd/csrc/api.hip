@@ -39,8 +39,8 @@ extern "C" int64_t focus_struct_size(int32_t which) {
     case 15: return sizeof(focus_paged_evict_desc);
     case 16: return sizeof(focus_paged_extend_desc);
     case 17: return sizeof(focus_paged_kv8);
-    case 18: return sizeof(focus_paged_append8_desc);
-    case 19: return sizeof(focus_paged_attend8_desc);
+    case 18: return sizeof(focus_paged_append_desc);
+    case 19: return sizeof(focus_paged_attend_desc);
     default: return -1;
   }
 }

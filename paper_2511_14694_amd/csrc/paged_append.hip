@@ -1,5 +1,5 @@
 // Rows stored in a paged cache of 8 bits, a power of two as scale for each block of rows and
-// KV head (focus_paged_append8).
+// KV head (focus_paged_append).
 //
 // One wave takes a block of a sequence and a KV head, of k and of v: the largest magnitude of the
 // new rows gives the scale, the elements times its inverse are exact and rounded once.  Lanes
@@ -19,7 +19,7 @@ constexpr float kLargest = 448.f;  // of e4m3
 constexpr uint32_t kInf = 0x7f800000u;
 
 struct Args {
-  focus_paged_append8_desc d;
+  focus_paged_append_desc d;
   int shift, scale_shift;  // log2 page_rows, scale_rows
   int span_shift;          // log2 of the rows a wave covers
   int pieces;              // of 16 elements, in a row of a head
@@ -113,7 +113,7 @@ struct Owner {
   int b;
   int64_t r0, r1, start;
 };
-__device__ Owner owner_of(const focus_paged_append8_desc& d, int64_t t) {
+__device__ Owner owner_of(const focus_paged_append_desc& d, int64_t t) {
   const int batch = d.cache.kv.batch, lane = threadIdx.x % 64;
   if (!d.cu_rows) return {(int)t, t, t + 1, d.start[t]};
   int lo = 0, len = batch;
@@ -144,7 +144,7 @@ template <typename T> struct Side {
   float was;
 
   __device__ Side(const Args& a, bool is_v, int64_t t0, int64_t page, int in_page, int g) {
-    const focus_paged_append8_desc& d = a.d;
+    const focus_paged_append_desc& d = a.d;
     const focus_paged_kv& c = d.cache.kv;
     step = is_v ? d.v_row : d.k_row, to_step = c.row_stride;
     src = reinterpret_cast<const T*>(is_v ? d.v : d.k) + t0 * step + (int64_t)g * (is_v ? d.v_head : d.k_head);
@@ -232,7 +232,7 @@ template <typename T> struct Side {
 
 template <typename T>
 __device__ void store_block(const Args& a, int64_t t0, int rows, int b, int64_t slot, int g) {
-  const focus_paged_append8_desc& d = a.d;
+  const focus_paged_append_desc& d = a.d;
   const focus_paged_kv& c = d.cache.kv;
   const int64_t page = focus::page_of(c, b, (int)slot, a.shift);
   if (page < 0) {
@@ -250,7 +250,7 @@ __device__ void store_block(const Args& a, int64_t t0, int rows, int b, int64_t 
 
 template <typename T>
 __global__ __launch_bounds__(kThreads) void append_rows(Args a) {
-  const focus_paged_append8_desc& d = a.d;
+  const focus_paged_append_desc& d = a.d;
   const focus_paged_kv& c = d.cache.kv;
   const int g = blockIdx.y * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   if (g >= c.n_kv_heads) return;
@@ -282,7 +282,7 @@ __global__ __launch_bounds__(kThreads) void append_rows(Args a) {
   }
 }
 
-focus_status validate(const focus_paged_append8_desc* d) {
+focus_status validate(const focus_paged_append_desc* d) {
   const focus_paged_kv& c = d->cache.kv;
   const focus_status st = focus::check_paged8(d->cache);
   if (st != FOCUS_OK) return st;
@@ -304,7 +304,7 @@ focus_status validate(const focus_paged_append8_desc* d) {
 
 }  // namespace
 
-extern "C" focus_status focus_paged_append8(const focus_paged_append8_desc* d, focus_stream_t stream) {
+extern "C" focus_status focus_paged_append(const focus_paged_append_desc* d, focus_stream_t stream) {
   if (!d) return FOCUS_E_NULL;
   const focus_status st = validate(d);
   const focus_paged_kv& c = d->cache.kv;

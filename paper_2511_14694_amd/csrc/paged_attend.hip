@@ -1,13 +1,13 @@
 // Attention of the newest tokens of every sequence over a paged cache of 8 bits
-// (focus_paged_attend8).
+// (focus_paged_attend).
 //
-//   attend8_attend  the rows of the whole batch, laid end to end, are dealt in equal shares:
+//   attend_rows  the rows of the whole batch, laid end to end, are dealt in equal shares:
 //                   one workgroup takes a share (parts of one sequence or of several) for one
 //                   to four KV heads and up to 16 or 32 columns of each (a column is a new token
 //                   and a query head); it writes o and lse where a sequence lies in its
 //                   share, else an unnormalised partial (running max, sum, output)
-//   attend8_join    merges the partials of a sequence by log-sum-exp
-//   attend8_plan    before both for more than 128 sequences: where each begins
+//   attend_join    merges the partials of a sequence by log-sum-exp
+//   attend_plan    before both for more than 128 sequences: where each begins
 //
 // Every cached byte is read once for up to 32 columns.  A wave takes 32 rows at a time; each
 // lane's loads become operands of bf16 matrix products as they arrive, without LDS (e4m3
@@ -62,13 +62,13 @@ struct Plan {
   int wide, unit;       // sets of these of a workgroup; rows of a unit
   int64_t groups;       // workgroups of a share
   int columns;          // of all heads
-  bool single, planned; // a share is a sequence; attend8_plan runs
+  bool single, planned; // a share is a sequence; attend_plan runs
 };
 
-// Workgroups of attend8_attend that a compute unit holds (by their registers).
+// Workgroups of attend_rows that a compute unit holds (by their registers).
 constexpr int resident(int head_dim, int tiles, int heads) { return head_dim == 64 && tiles * heads == 1 ? 3 : 2; }
 
-Plan make_plan(const focus_paged_attend8_desc* d) {
+Plan make_plan(const focus_paged_attend_desc* d) {
   const focus_paged_kv& c = d->cache.kv;
   Plan p = {};
   p.cap = (int64_t)c.max_pages * c.page_rows;
@@ -109,7 +109,7 @@ Plan make_plan(const focus_paged_attend8_desc* d) {
 }
 
 struct Args {
-  focus_paged_attend8_desc d;
+  focus_paged_attend_desc d;
   float sc;             // softmax scale in log2 units
   int shift, scale_shift;  // log2 page_rows, scale_rows
   int tiles, wide_shift;
@@ -148,7 +148,7 @@ __device__ inline int units_of_share(const Args& a, int total) { return a.fixed 
 
 constexpr int kPlan = 1024;
 
-__global__ __launch_bounds__(kPlan) void attend8_plan(Args a) {
+__global__ __launch_bounds__(kPlan) void attend_plan(Args a) {
   __shared__ int s_part[kPlan / 64];
   const focus_paged_kv& c = a.d.cache.kv;
   const int tid = threadIdx.x;
@@ -292,7 +292,7 @@ __device__ inline uint32_t nan_bytes(uint32_t w) { return (((w & 0x7f7f7f7fu) + 
 // T: of q and o.  float32 queries enter in three bf16 parts, weights in two (17 bits; their
 // rounding is far below that of a bf16 output) or, for float32 outputs, three.
 template <typename T, int D, int TILES, int HEADS, bool SHARED>
-__global__ __launch_bounds__(kThreads, resident(D, TILES, HEADS)) void attend8_attend(Args a) {
+__global__ __launch_bounds__(kThreads, resident(D, TILES, HEADS)) void attend_rows(Args a) {
   using L = Tile<D, HEADS>;
   constexpr int kPitch = D + 4, kSteps = D / 32, kCols = 16 * TILES, kStates = TILES * HEADS;
   constexpr int kParts = sizeof(T) == 2 ? 1 : 3, kWeightParts = sizeof(T) == 2 ? 2 : 3;
@@ -646,7 +646,7 @@ __global__ __launch_bounds__(kThreads, resident(D, TILES, HEADS)) void attend8_a
 // by every wave for itself.
 constexpr int kJoin = 256, kManyShares = 32;
 template <typename T, int D, bool WIDE>
-__global__ __launch_bounds__(kJoin) void attend8_join(Args a) {
+__global__ __launch_bounds__(kJoin) void attend_join(Args a) {
   constexpr int kFlight = 8, kThreadsOf = WIDE ? kJoin : 64, kSlices = WIDE ? D / 32 : 1;
   constexpr int kLanes = D / 4 / kSlices, kGroups = kThreadsOf / kLanes;
   __shared__ float4 s_o[WIDE ? kJoin : 1];
@@ -722,7 +722,7 @@ __global__ __launch_bounds__(kJoin) void attend8_join(Args a) {
   if (e == 0 && a.d.lse) a.d.lse[at] = focus::lse_of(a.sc, make_float2(M, S));
 }
 
-focus_status validate(const focus_paged_attend8_desc* d) {
+focus_status validate(const focus_paged_attend_desc* d) {
   const focus_paged_kv& c = d->cache.kv;
   const focus_status st = focus::check_paged8(d->cache);
   if (st != FOCUS_OK) return st;
@@ -751,7 +751,7 @@ focus_status launch(Args a, const Plan& p, hipStream_t s) {
   const int64_t columns = (int64_t)c.batch * p.columns;
   if (p.groups * p.shares > INT32_MAX / kThreads - focus::kXcds * kMost) return FOCUS_E_SHAPE;
   if (p.planned) {
-    hipLaunchKernelGGL(attend8_plan, dim3(1), dim3(kPlan), 0, s, a);
+    hipLaunchKernelGGL(attend_plan, dim3(1), dim3(kPlan), 0, s, a);
     const focus_status st = focus::launch_status();
     if (st != FOCUS_OK) return st;
   }
@@ -760,7 +760,7 @@ focus_status launch(Args a, const Plan& p, hipStream_t s) {
   auto attend = [&](auto tiles, auto heads, auto shared) {
     constexpr int kTiles = decltype(tiles)::value, kHeads = decltype(heads)::value;
     constexpr bool kShared = decltype(shared)::value;
-    hipLaunchKernelGGL((attend8_attend<T, D, kTiles, kHeads, kShared>), grid, dim3(kThreads), 0, s, a);
+    hipLaunchKernelGGL((attend_rows<T, D, kTiles, kHeads, kShared>), grid, dim3(kThreads), 0, s, a);
   };
   auto of_heads = [&](auto tiles, auto shared) {
     if constexpr (D == 64 && decltype(tiles)::value == 1) {
@@ -777,20 +777,20 @@ focus_status launch(Args a, const Plan& p, hipStream_t s) {
   if (st != FOCUS_OK || p.single) return st;
   // (a wave has 16 shares of 128 elements in flight)
   if (p.shares >= kManyShares * c.batch)
-    hipLaunchKernelGGL((attend8_join<T, D, true>), dim3((uint32_t)(columns * (D / 32))), dim3(kJoin), 0, s, a);
+    hipLaunchKernelGGL((attend_join<T, D, true>), dim3((uint32_t)(columns * (D / 32))), dim3(kJoin), 0, s, a);
   else
-    hipLaunchKernelGGL((attend8_join<T, D, false>), dim3((uint32_t)focus::ceil_div(columns, kJoin / 64)), dim3(kJoin), 0, s, a);
+    hipLaunchKernelGGL((attend_join<T, D, false>), dim3((uint32_t)focus::ceil_div(columns, kJoin / 64)), dim3(kJoin), 0, s, a);
   return focus::launch_status();
 }
 
 }  // namespace
 
-extern "C" size_t focus_paged_attend8_workspace(const focus_paged_attend8_desc* d) {
+extern "C" size_t focus_paged_attend_workspace(const focus_paged_attend_desc* d) {
   if (!d || validate(d) != FOCUS_OK) return 0;
   return make_plan(d).bytes;
 }
 
-extern "C" focus_status focus_paged_attend8(const focus_paged_attend8_desc* d, focus_stream_t stream) {
+extern "C" focus_status focus_paged_attend(const focus_paged_attend_desc* d, focus_stream_t stream) {
   if (!d) return FOCUS_E_NULL;
   const focus_status st = validate(d);
   if (st != FOCUS_OK) return st;

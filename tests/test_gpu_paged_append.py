@@ -1,4 +1,4 @@
-"""focus_paged_append8 on the GPU against the oracle, element for element: e4m3 numbers and
+"""focus_paged_append on the GPU against the oracle, element for element: e4m3 numbers and
 scales are exact, so nothing is allowed to differ."""
 
 import numpy as np
@@ -50,7 +50,7 @@ def _new(rng, counts, K, D, dtype, spread=6):
 ])
 @pytest.mark.parametrize("fused", [False, True])
 def test_append_matches_oracle(lens, add, K, D, page, block, dtype, by_head, fused):
-    announce(f"append8 {lens} + {add} {K} x {D} page {page} block {block} {dtype} by_head {by_head} fused {fused}")
+    announce(f"append {lens} + {add} {K} x {D} page {page} block {block} {dtype} by_head {by_head} fused {fused}")
     rng = np.random.default_rng(sum(lens) + sum(add) + D)
     ends = [n + a for n, a in zip(lens, add)]
     c = Cache8(rng, ends, K, D, page, block, by_head=by_head, padded=not by_head and fused)
@@ -61,12 +61,12 @@ def test_append_matches_oracle(lens, add, K, D, page, block, dtype, by_head, fus
         k, v = both[:, :K], both[:, K:]
     cu = _offsets(add)
     err = torch.zeros(1, dtype=torch.int32, device=DEV)
-    F.focus_paged_append8(k, v, c.dev, i32(lens), i32(cu), err=err)
+    F.focus_paged_append(k, v, c.dev, i32(lens), i32(cu), err=err)
     _check(c, k64, v64, lens, cu, "first")
     assert c.dev.length.tolist() == [e if a else n for n, a, e in zip(lens, add, ends)] and err.item() == 0
     # the same rows again, from an earlier row on: those behind it are overwritten
     start = [max(0, n - 3) for n in lens]
-    F.focus_paged_append8(k, v, c.dev, i32(start), i32(cu), err=err)
+    F.focus_paged_append(k, v, c.dev, i32(start), i32(cu), err=err)
     _check(c, k64, v64, start, cu, "again")
     assert err.item() == 0
 
@@ -76,8 +76,8 @@ def test_append_one_row_a_sequence_without_offsets():
     lens = [int(x) for x in rng.integers(0, 70, 300)]
     c = Cache8(rng, [n + 1 for n in lens], 2, 64, 16, 16)
     (k, k64), (v, v64) = _new(rng, [1] * 300, 2, 64, "bf16")
-    announce("append8 300 sequences")
-    F.focus_paged_append8(k, v, c.dev, i32(lens))
+    announce("append 300 sequences")
+    F.focus_paged_append(k, v, c.dev, i32(lens))
     _check(c, k64, v64, lens, list(range(301)))
 
 
@@ -90,8 +90,8 @@ def test_append_finds_its_sequences(batch, most):
     add[-1] = 0
     c = Cache8(rng, [n + a for n, a in zip(lens, add)], 1, 16, 8, 8)
     (k, k64), (v, v64) = _new(rng, add, 1, 16, "f32")
-    announce(f"append8 {batch} ragged sequences")
-    F.focus_paged_append8(k, v, c.dev, i32(lens), i32(_offsets(add)))
+    announce(f"append {batch} ragged sequences")
+    F.focus_paged_append(k, v, c.dev, i32(lens), i32(_offsets(add)))
     _check(c, k64, v64, lens, _offsets(add))
 
 
@@ -107,13 +107,13 @@ def test_append_row_by_row_grows_scales(dtype):
     c.dev.v_scale.fill_(float("nan"))
     c.refresh()
     e = np.linspace(-149 if dtype == "f32" else -133, 127, 24)
-    announce(f"append8 growing {dtype}")
+    announce(f"append growing {dtype}")
     for r in range(24):
         x = (rng.uniform(-1, 1, (1, 1, D)) * 2.0 ** e[r]).astype(np.float32)
         x[0, 0, 0] = np.float32(2.0 ** np.floor(e[r]))
         t = torch.as_tensor(x).to(torch.bfloat16 if dtype == "bf16" else torch.float32).to(DEV)
         t64 = t.double().cpu().numpy()
-        F.focus_paged_append8(t, -t, c.dev, i32([r]))
+        F.focus_paged_append(t, -t, c.dev, i32([r]))
         _check(c, t64, -t64, [r], [0, 1], f"row {r}")
     assert c.dev.length.tolist() == [24]
 
@@ -139,8 +139,8 @@ def test_append_special_values(dtype):
     full = full[torch.as_tensor(rng.permutation(len(full)))].repeat(1, K, 1).numpy()
     t = torch.as_tensor(np.concatenate([x, full])).to(torch.bfloat16 if dtype == "bf16" else torch.float32).to(DEV)
     t64 = t.cpu().double().numpy()
-    announce(f"append8 special values {dtype}")
-    F.focus_paged_append8(t, -t, c.dev, i32([0, 0]), i32([0, 48, 560]))
+    announce(f"append special values {dtype}")
+    F.focus_paged_append(t, -t, c.dev, i32([0, 0]), i32([0, 48, 560]))
     _check(c, t64, -t64, [0, 0], [0, 48, 560])
 
 
@@ -156,17 +156,17 @@ def test_append_skips_what_it_cannot_store():
         if change:
             change(c)
         err.zero_()
-        F.focus_paged_append8(k, v, c.dev, i32(start), i32(_offsets(add) if cu is None else cu), err=err)
+        F.focus_paged_append(k, v, c.dev, i32(start), i32(_offsets(add) if cu is None else cu), err=err)
         return c, k64, v64
 
     # not served: nothing stored, nothing reported; the others are
-    announce("append8 not served, rows past the last")
+    announce("append not served, rows past the last")
     c, k, v = call([5, 6, 7], [4, 30, 9], [5, -1, 7], extra=11)
     _check(c, k, v, [5, -1, 7], [0, 4, 34, 43])
     assert err.item() == 0 and c.dev.length.tolist() == [9, 6, 16]
 
     # a page outside the pool: its blocks are left out
-    announce("append8 page outside the pool")
+    announce("append page outside the pool")
     for bad in (-1, 1 << 30):
         def spoil(c):
             c.dev.table[0, 1] = bad
@@ -182,21 +182,21 @@ def test_append_skips_what_it_cannot_store():
         assert err.item() == F.FOCUS_ERR_BOUNDS
 
     # rows past the table
-    announce("append8 past the table")
+    announce("append past the table")
     c, k, v = call([30, 2], [2, 3], [30, 2])
     err.zero_()
     (x, x64), (y, y64) = _new(rng, [8, 1], K, D, "bf16")
-    F.focus_paged_append8(x, y, c.dev, i32([28, 2 ** 31 - 1]), i32([0, 8, 9]), err=err)
+    F.focus_paged_append(x, y, c.dev, i32([28, 2 ** 31 - 1]), i32([0, 8, 9]), err=err)
     c.refresh()
     ref = appended(c, x64[:4], y64[:4], [28, -1], [0, 4, 4])
-    F.focus_paged_append8(x, y, c.dev, i32([28, 2 ** 31 - 1]), i32([0, 8, 9]), err=err)
+    F.focus_paged_append(x, y, c.dev, i32([28, 2 ** 31 - 1]), i32([0, 8, 9]), err=err)
     c.refresh()
     for got, want in zip((c.pk, c.pv, c.ks, c.vs), ref):
         same(got, want, "inside")
     assert err.item() == F.FOCUS_ERR_CAPACITY and c.dev.length.tolist() == [32, 5]
 
     # offsets past the rows are clipped; rows before the first belong to nobody
-    announce("append8 offsets outside the rows")
+    announce("append offsets outside the rows")
     c, k, v = call([0, 0], [12, 9], [0, 0], cu=[3, 12, 40])
     _check(c, k, v, [0, 0], [3, 12, 21])
     assert err.item() == F.FOCUS_ERR_BOUNDS
@@ -213,9 +213,9 @@ def test_append_nothing():
     c = Cache8(rng, [5, 9], 2, 64, 16, 8)
     before = [to_codes(x) for x in (c.dev.k, c.dev.v)]
     k = torch.zeros(0, 2, 64, dtype=torch.bfloat16, device=DEV)
-    F.focus_paged_append8(k, k, c.dev, i32([5, 9]), i32([0, 0, 0]))
+    F.focus_paged_append(k, k, c.dev, i32([5, 9]), i32([0, 0, 0]))
     k = torch.ones(7, 2, 64, dtype=torch.bfloat16, device=DEV)
-    F.focus_paged_append8(k, k, c.dev, i32([5, 9]), i32([0, 0, 0]))
+    F.focus_paged_append(k, k, c.dev, i32([5, 9]), i32([0, 0, 0]))
     same(to_codes(c.dev.k), before[0], "k")
     same(to_codes(c.dev.v), before[1], "v")
     assert c.dev.length.tolist() == [5, 9]

@@ -1,4 +1,4 @@
-"""focus_paged_attend8 on the GPU against the float64 oracle (tolerances:
+"""focus_paged_attend on the GPU against the float64 oracle (tolerances:
 oracle.paged8.attend_tolerances)."""
 
 import math
@@ -60,20 +60,20 @@ CASES = [
 @pytest.mark.parametrize("lens,counts,H,K,D,page,block,dtype,by_head", CASES)
 @pytest.mark.parametrize("split", [0, 128, 640])
 def test_attend_matches_oracle(lens, counts, H, K, D, page, block, dtype, by_head, split):
-    announce(f"attend8 {lens} {counts} {H}/{K} x {D} page {page} block {block} {dtype} by_head {by_head} split {split}")
+    announce(f"attend {lens} {counts} {H}/{K} x {D} page {page} block {block} {dtype} by_head {by_head} split {split}")
     rng = np.random.default_rng(sum(lens) + H + D)
     c = Cache8(rng, lens, K, D, page, block, by_head=by_head, padded=not by_head and D == 64, odd_scales=split == 640)
     q, q64 = values(rng, (sum(counts), H, D), dtype, 1.5)
     err = torch.zeros(1, dtype=torch.int32, device=DEV)
     cu = None if counts == [1] * len(lens) and split else _offsets(counts)
-    got = F.focus_paged_attend8(q, c.dev, cu, max_rows=max(counts), split_keys=split, err=err)
+    got = F.focus_paged_attend(q, c.dev, cu, max_rows=max(counts), split_keys=split, err=err)
     _check(c, q64, counts, got, dtype)
     assert err.item() == 0
-    again = F.focus_paged_attend8(q, c.dev, cu, max_rows=max(counts), split_keys=split)
+    again = F.focus_paged_attend(q, c.dev, cu, max_rows=max(counts), split_keys=split)
     assert torch.equal(again[0], got[0]) and torch.equal(again[1], got[1]), "not deterministic"
     # a greater bound of the tokens changes nothing but the split
     if split and (max(counts) + 3) * H // K <= 512:
-        more = F.focus_paged_attend8(q, c.dev, cu, max_rows=max(counts) + 3, split_keys=split)
+        more = F.focus_paged_attend(q, c.dev, cu, max_rows=max(counts) + 3, split_keys=split)
         _check(c, q64, counts, more, dtype)
 
 
@@ -87,13 +87,13 @@ def test_attend_matches_oracle(lens, counts, H, K, D, page, block, dtype, by_hea
 ])
 def test_attend_chunks_chosen(batch, top, H, K, dim, dtype, new):
     """Lengths from 0 to top in tables long enough to be split, 0 to `new` tokens."""
-    announce(f"attend8 {batch} x {top} {H}/{K} x {dim} {dtype} new {new}")
+    announce(f"attend {batch} x {top} {H}/{K} x {dim} {dtype} new {new}")
     rng = np.random.default_rng(batch)
     lens = [top, 0, 1] + [int(x) for x in np.exp(rng.uniform(0, np.log(top), batch - 3))]
     counts = [new] + [int(x) for x in rng.integers(0, new + 1, batch - 1)]
     c = Cache8(rng, lens, K, dim, 64, 16)
     q, q64 = values(rng, (sum(counts), H, dim), dtype)
-    got = F.focus_paged_attend8(q, c.dev, _offsets(counts), max_rows=new)
+    got = F.focus_paged_attend(q, c.dev, _offsets(counts), max_rows=new)
     _check(c, q64, counts, got, dtype)
 
 
@@ -102,8 +102,8 @@ def test_attend_table_far_larger_than_the_lengths():
     lens = [0, 1, 700, 33]
     c = Cache8(rng, lens, 2, 128, 64, 32, max_pages=1024)
     q, q64 = values(rng, (4, 8, 128), "bf16")
-    announce("attend8 wide table")
-    _check(c, q64, [1] * 4, F.focus_paged_attend8(q, c.dev), "bf16")
+    announce("attend wide table")
+    _check(c, q64, [1] * 4, F.focus_paged_attend(q, c.dev), "bf16")
 
 
 def test_attend_chunk_of_more_pages_than_held():
@@ -111,8 +111,8 @@ def test_attend_chunk_of_more_pages_than_held():
     rng = np.random.default_rng(32)
     c = Cache8(rng, [20_003], 1, 64, 8, 8)
     q, q64 = values(rng, (3, 2, 64), "bf16")
-    announce("attend8 many pages")
-    _check(c, q64, [3], F.focus_paged_attend8(q, c.dev, _offsets([3]), max_rows=3, split_keys=128 * 80), "bf16")
+    announce("attend many pages")
+    _check(c, q64, [3], F.focus_paged_attend(q, c.dev, _offsets([3]), max_rows=3, split_keys=128 * 80), "bf16")
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
@@ -124,16 +124,16 @@ def test_attend_strided_queries_scale_and_outputs(dtype):
     t = torch.bfloat16 if dtype == "bf16" else torch.float32
     o = torch.full((5, H, D), 7.0, dtype=t, device=DEV)
     lse = torch.full((5, H), 7.0, device=DEV)
-    announce(f"attend8 strided {dtype}")
+    announce(f"attend strided {dtype}")
     # 2 + 2 rows: the fifth belongs to nobody and is left as it was
-    F.focus_paged_attend8(qkv[:, :H], c.dev, _offsets([2, 2]), max_rows=2, o=o, lse=lse, softmax_scale=0.3)
+    F.focus_paged_attend(qkv[:, :H], c.dev, _offsets([2, 2]), max_rows=2, o=o, lse=lse, softmax_scale=0.3)
     _check(c, qkv64[:, :H], [2, 2], (o, lse), dtype, scale=0.3)
     assert (o[4] == 7).all() and (lse[4] == 7).all()
     # rows before the first offset too, and heads before rows
     o.fill_(7.0)
     q2 = qkv[:, :H].transpose(0, 1).contiguous().transpose(0, 1)
-    F.focus_paged_attend8(q2, c.dev, i32([1, 3, 5]), max_rows=2, o=o, want_lse=False, softmax_scale=0.3)
-    _check(c, qkv64[1:, :H], [2, 2], (o[1:], F.focus_paged_attend8(q2, c.dev, i32([1, 3, 5]), 2, softmax_scale=0.3)[1][1:]),
+    F.focus_paged_attend(q2, c.dev, i32([1, 3, 5]), max_rows=2, o=o, want_lse=False, softmax_scale=0.3)
+    _check(c, qkv64[1:, :H], [2, 2], (o[1:], F.focus_paged_attend(q2, c.dev, i32([1, 3, 5]), 2, softmax_scale=0.3)[1][1:]),
            dtype, scale=0.3)
     assert (o[0] == 7).all()
 
@@ -143,7 +143,7 @@ def test_attend_strided_queries_scale_and_outputs(dtype):
 def test_attend_nan_only_where_it_is_seen(D, split):
     """A NaN in a row's k, v or scales reaches the tokens that see it, not those before."""
     rng = np.random.default_rng(34)
-    announce(f"attend8 NaN {D} {split}")
+    announce(f"attend NaN {D} {split}")
     for n in (40, 300, 1027):
         for which in ("k", "v", "k_scale", "v_scale"):
             c = Cache8(rng, [n], 2, D, 16, 8)
@@ -159,7 +159,7 @@ def test_attend_nan_only_where_it_is_seen(D, split):
                 getattr(c.dev, which).view(torch.uint8)[p, r, 0, 5] = NAN
             q, q64 = values(rng, (4, 4, D), "bf16")
             c.refresh()
-            o, lse = F.focus_paged_attend8(q, c.dev, i32([0, 4]), max_rows=4, split_keys=split)
+            o, lse = F.focus_paged_attend(q, c.dev, i32([0, 4]), max_rows=4, split_keys=split)
             first = next(i for i in range(4) if n - 3 + i > row)
             k, v = c.rows(0, n, "k"), c.rows(0, n, "v")
             for i in range(4):
@@ -186,18 +186,18 @@ def test_attend_scales_of_all_sizes():
     c.dev.v_scale.copy_(torch.as_tensor(2.0 ** rng.integers(-100, 110, tuple(c.dev.v_scale.shape))))
     c.refresh()
     q, q64 = values(rng, (1, 4, 128), "f32")
-    announce("attend8 scales")
-    _check(c, q64, [1], F.focus_paged_attend8(q, c.dev), "f32")
+    announce("attend scales")
+    _check(c, q64, [1], F.focus_paged_attend(q, c.dev), "f32")
     c.dev.k_scale.zero_()
     c.dev.v_scale.zero_()
-    o, lse = F.focus_paged_attend8(q, c.dev)
+    o, lse = F.focus_paged_attend(q, c.dev)
     assert (o == 0).all() and (lse - math.log(200)).abs().max() < 1e-6
 
 
 def test_attend_pages_outside_the_pool_and_bad_offsets():
     rng = np.random.default_rng(36)
     err = torch.zeros(1, dtype=torch.int32, device=DEV)
-    announce("attend8 pages outside the pool")
+    announce("attend pages outside the pool")
     for split in (0, 128):
         c = Cache8(rng, [600, 40, 20], 2, 64, 16, 8)
         for j, bad in ((2, -1), (3, -2 ** 31), (20, 10 ** 6), (37, 2 ** 31 - 1)):
@@ -208,19 +208,19 @@ def test_attend_pages_outside_the_pool_and_bad_offsets():
             seen[0][16 * j:16 * j + 16] = False
         q, q64 = values(rng, (5, 2, 64), "bf16")
         err.zero_()
-        got = F.focus_paged_attend8(q, c.dev, i32([0, 2, 4, 5]), max_rows=2, split_keys=split, err=err)
+        got = F.focus_paged_attend(q, c.dev, i32([0, 2, 4, 5]), max_rows=2, split_keys=split, err=err)
         _check(c, q64, [2, 2, 1], got, "bf16", visible=seen)
         assert err.item() == F.FOCUS_ERR_BOUNDS
-    announce("attend8 lengths outside the table")
+    announce("attend lengths outside the table")
     c = Cache8(rng, [32, 16], 2, 64, 16, 8)
     q, q64 = values(rng, (2, 2, 64), "bf16")
     c.dev.length.copy_(i32([99, -4]))
     err.zero_()
-    got = F.focus_paged_attend8(q, c.dev, err=err)
+    got = F.focus_paged_attend(q, c.dev, err=err)
     c.lens = [32, 0]
     _check(c, q64, [1, 1], got, "bf16")
     assert err.item() == F.FOCUS_ERR_CAPACITY
-    announce("attend8 bad offsets")
+    announce("attend bad offsets")
     c = Cache8(rng, [32, 300, 40], 2, 64, 16, 8)
     q, q64 = values(rng, (6, 2, 64), "bf16")
     for cu, bit, fine in (([0, 3, 4, 6], F.FOCUS_ERR_CAPACITY, [(1, 3, 4), (2, 4, 6)]),
@@ -228,7 +228,7 @@ def test_attend_pages_outside_the_pool_and_bad_offsets():
                           ([-1, 1, 2, 9], F.FOCUS_ERR_BOUNDS, [(1, 1, 2)])):
         o, lse = torch.full_like(q, 7.0), torch.full((6, 2), 7.0, device=DEV)
         err.zero_()
-        F.focus_paged_attend8(q, c.dev, i32(cu), max_rows=2, o=o, lse=lse, err=err)
+        F.focus_paged_attend(q, c.dev, i32(cu), max_rows=2, o=o, lse=lse, err=err)
         assert err.item() == bit
         mine = set()
         for b, r0, r1 in fine:
