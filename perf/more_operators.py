@@ -241,9 +241,9 @@ def _own_run(s):
                 "table": s["table"], "length": s["length"], "free_pages": s["free_pages"], "free_count": s["free_count"]}
     cache = F.PagedCache8(s["pk"], s["pv"], s["k_scale"], s["v_scale"], s["table"], s["length"])
     if c["kind"] == "append":
-        F.focus_paged_append8(s["k"], s["v"], cache, s["start"], cu_rows=s["cu_rows"])
+        F.focus_paged_append(s["k"], s["v"], cache, s["start"], cu_rows=s["cu_rows"])
         return {"pages_k": s["pk"], "pages_v": s["pv"], "k_scale": s["k_scale"], "v_scale": s["v_scale"]}
-    o, lse = F.focus_paged_attend8(s["q"], cache, cu_rows=s["cu_rows"], max_rows=c["new"])
+    o, lse = F.focus_paged_attend(s["q"], cache, cu_rows=s["cu_rows"], max_rows=c["new"])
     return {"o": o, "lse": lse}
 
 
