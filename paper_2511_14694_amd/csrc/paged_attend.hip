@@ -299,6 +299,7 @@ __global__ __launch_bounds__(kThreads, resident(D, TILES, HEADS)) void attend_ro
   __shared__ int s_page[kPages + 1];  // (rows may begin inside a page)
   __shared__ float s_o[kWaves][HEADS * kCols][kPitch];
   __shared__ float2 s_ml[kWaves][HEADS * kCols];
+  __shared__ __align__(16) uint8_t s_nan[kWaves][kRows][16];  // NaN among a row's elements, a bit each
   const focus_paged_kv& c = a.d.cache.kv;
   const int H = a.d.n_heads, G = a.group;
   // (a wave's number in a scalar register: its loops are branches then, not masks)
@@ -400,9 +401,7 @@ __global__ __launch_bounds__(kThreads, resident(D, TILES, HEADS)) void attend_ro
         s_page[i] = (int)p;
       }
       __syncthreads();
-      // tiles that are whole and seen by all columns end here
-      const int clean = max(seg, min(seg_end, sees_all));
-      const int full_end = clean - (clean - seg) % kRows;
+      const int clean = min(seg_end, sees_all);  // tiles up to here are whole and seen by all columns
       // the page that holds the eight rows at r (negative: none, or past end)
       auto page = [&](int r, int end) { return r < end ? s_page[(r >> a.shift) - page0] : -1; };
       // Rows of eight lie in one page, so all of them can be read where the first is cached.
@@ -436,16 +435,16 @@ __global__ __launch_bounds__(kThreads, resident(D, TILES, HEADS)) void attend_ro
           w.vs[h] = load_row<float, true>(pv >= 0 ? vs_base + h * per_page + sc : none);
         }
       };
-      auto compute = [&](L& w, int r, auto whole) {
-        constexpr bool kWholeTile = decltype(whole)::value;
+      auto compute = [&](L& w, int r) {
         const int row = r + v8;  // of the lane's first score
         // of the lane's rows, those that count: the first `live`
         const int live = page(row, seg_end) >= 0 ? 8 : 0;
+        const bool tail = r + kRows > clean;
 #pragma unroll
         for (int h = 0; h < HEADS; ++h) {
           const int at0 = h * TILES;  // the head's first state
           uint32_t bad = 0;
-          if constexpr (!kWholeTile) {
+          if (tail) {
             // Rows past the end may hold anything, and those that only later tokens see a NaN,
             // and zero times a NaN is a NaN: the first are cleared, the NaN of the others
             // taken out and put into the sums of the columns that see them.
@@ -472,7 +471,7 @@ __global__ __launch_bounds__(kThreads, resident(D, TILES, HEADS)) void attend_ro
                   s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, q[at0 + tile][part][i], s[t], 0, 0, 0);
               }
             }
-            const int lives = kWholeTile ? live : min(live, min(seg_end, sees[tile]) - row);
+            const int lives = tail ? min(live, min(seg_end, sees[tile]) - row) : live;
             float mx = m[at0 + tile];
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
@@ -493,38 +492,43 @@ __global__ __launch_bounds__(kThreads, resident(D, TILES, HEADS)) void attend_ro
             for (int j = 0; j < 8; ++j) {
               y[tile][j] = __builtin_amdgcn_exp2f((y[tile][j] - m[at0 + tile]) * a.sc);
               l[at0 + tile] += y[tile][j];
-              y[tile][j] = kWholeTile || j < lives ? y[tile][j] * w.vs[h] : 0.f;
+              y[tile][j] *= w.vs[h];
+            }
+            if (tail) {  // (of rows that do not count the scale may be anything)
+#pragma unroll
+              for (int j = 0; j < 8; ++j) y[tile][j] = j < lives ? y[tile][j] : 0.f;
             }
           }
-          if constexpr (!kWholeTile) {
-            if (__ballot(bad != 0)) {
+          if (tail && __ballot(bad != 0)) {
 #pragma unroll
-              for (int t = 0; t < L::kPer; ++t) {
-                bf16x8 mark;
+            for (int j = 0; j < 8; ++j) {
+              uint32_t bits = 0;
 #pragma unroll
-                for (int j = 0; j < 8; ++j)
-                  mark[j] = (__bf16)(nan_bytes(w.word(h, j, t / 4)) >> (t % 4 * 8) & 1 ? 1.f : 0.f);
+              for (int i = 0; i < L::kWords; ++i) {
+                const uint32_t is = nan_bytes(w.word(h, j, i)), keep = ~(is * 0xffu);
+                bits |= (is * 0x10204080u >> 28) << 4 * i;  // the bytes' bits side by side
+                if constexpr (L::kWords == 2) w.v[h][j][i] &= keep;
+                else w.v[h][j] &= keep;
+              }
+              s_nan[wave][v8 + j][col] = (uint8_t)bits;
+            }
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll
-                for (int tile = 0; tile < TILES; ++tile) {
-                  const int lives = min(live, min(seg_end, sees[tile]) - row);
-                  bf16x8 seen;
-#pragma unroll
-                  for (int j = 0; j < 8; ++j) seen[j] = (__bf16)(j < lives ? 1.f : 0.f);
-                  const f32x4 k = __builtin_amdgcn_mfma_f32_16x16x32_bf16(mark, seen, f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
-#pragma unroll
-                  for (int e = 0; e < 4; ++e)
-                    if (k[e] != 0.f) o[at0 + tile][t][e] = NAN;
-                }
+            for (int tile = 0; tile < TILES; ++tile) {
+              uint32_t any = 0;  // byte e: elements (4 x + e) kPer + t
+              const int end = min(seg_end, sees[tile]) - r;
+#pragma unroll 1
+              for (int i = 0; i < kRows; ++i) {
+                const uint32_t of_row = *reinterpret_cast<const uint32_t*>(&s_nan[wave][i][4 * x]);
+                any |= i < end ? of_row : 0u;
               }
 #pragma unroll
-              for (int j = 0; j < 8; ++j)
+              for (int t = 0; t < L::kPer; ++t)
 #pragma unroll
-                for (int i = 0; i < L::kWords; ++i) {
-                  const uint32_t keep = ~(nan_bytes(w.word(h, j, i)) * 0xffu);
-                  if constexpr (L::kWords == 2) w.v[h][j][i] &= keep;
-                  else w.v[h][j] &= keep;
-                }
+                for (int e = 0; e < 4; ++e)
+                  if (any >> (8 * e + t) & 1) o[at0 + tile][t][e] = NAN;
             }
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
           }
           // product t's rows of V^T: pairs of rows by a byte permutation, then widened; half of
           // them at a time
@@ -559,32 +563,23 @@ __global__ __launch_bounds__(kThreads, resident(D, TILES, HEADS)) void attend_ro
           }
         }
       };
-      // A wave's whole tiles, two a round, the next one's loads in flight while one is
-      // computed; then the tiles that the rows end in or that not all columns see.  One way
-      // out of the loop, loads past the end taken from kZeros and the last of them waited
-      // for behind it: otherwise the compiler cannot tell which loads are in flight at a
-      // round's start and waits for half of them.
+      // A wave's tiles, two a round, the next one's loads in flight while one is computed.
+      // One way out of the loop, loads past the end taken from kZeros and the last of them
+      // waited for behind it: otherwise the compiler cannot tell which loads are in flight
+      // at a round's start and waits for half of them.
       const int stride = by * kRows;
       int r = seg + among * kRows;
-      if (r < full_end) {
+      if (r < seg_end) {
         L w0, w1;
-        load(w0, r, full_end);
-        for (; r + stride < full_end; r += 2 * stride) {
-          load(w1, r + stride, full_end);
-          compute(w0, r, std::true_type{});
-          load(w0, r + 2 * stride, full_end);
-          compute(w1, r + stride, std::true_type{});
+        load(w0, r, seg_end);
+        for (; r + stride < seg_end; r += 2 * stride) {
+          load(w1, r + stride, seg_end);
+          compute(w0, r);
+          load(w0, r + 2 * stride, seg_end);
+          compute(w1, r + stride);
         }
-        if (r < full_end) {
-          compute(w0, r, std::true_type{});
-          r += stride;
-        }
+        if (r < seg_end) compute(w0, r);
         __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0)
-      }
-      for (; r < seg_end; r += stride) {
-        L w;
-        load(w, r, seg_end);
-        compute(w, r, std::false_type{});
       }
     }
     __syncthreads();  // the last sequence's outputs are read
