@@ -969,11 +969,19 @@ class PagedCache8:
         if n_pages <= 1 or heads <= 1:
             # the stride of a dimension of one element says nothing: replaced by one that passes
             strides = [dim if n <= 1 else st for n, st in zip(shape, strides)]
-        i32, f32 = torch.int32, torch.float32
+        i32, f32, length, v_scale = torch.int32, torch.float32, self.length, self.v_scale
+        # (all of them looked at together; one by one, with its name, where one does not fit)
+        if not (table.dtype is i32 and length.dtype is i32 and scale.dtype is f32 and v_scale.dtype is f32
+                and table.get_device() == dev == length.get_device() and scale.get_device() == dev == v_scale.get_device()
+                and table.is_contiguous() and length.is_contiguous() and scale.is_contiguous() and v_scale.is_contiguous()
+                and length.shape == (batch,) and v_scale.shape == scales):
+            _need(table, i32, None, dev, "table")
+            _need(length, i32, (batch,), dev, "length")
+            _need(scale, f32, scales, dev, "k_scale")
+            _need(v_scale, f32, scales, dev, "v_scale")
         return PagedKv8(PagedKv(FOCUS_E4M3, heads, dim, rows, n_pages, k.data_ptr(), v.data_ptr(), strides[0], strides[1],
-                                strides[2], batch, max_pages, _need(table, i32, None, dev, "table"),
-                                _need(self.length, i32, (batch,), dev, "length"), None, 0), rows // blocks, 0,
-                        _need(scale, f32, None, dev, "k_scale"), _need(self.v_scale, f32, scales, dev, "v_scale"))
+                                strides[2], batch, max_pages, table.data_ptr(), length.data_ptr(), None, 0), rows // blocks,
+                        0, scale.data_ptr(), v_scale.data_ptr())
 
 
 def focus_paged_append(k, v, cache: PagedCache8, start, cu_rows=None, err=None, stream=None):
@@ -1030,18 +1038,21 @@ def focus_paged_attend(q, cache: PagedCache8, cu_rows=None, max_rows: int = 1, o
     if lse is not None:
         lse_at = _need(lse, torch.float32, q.shape[:2], dev, "lse")
     elif want_lse:
-        lse = _empty(tuple(q.shape[:2]), torch.float32, q.device, stream)
+        lse = q.new_empty(q.shape[:2], dtype=torch.float32) if stream is None else \
+            _empty(q.shape[:2], torch.float32, q.device, stream)
         lse_at = lse.data_ptr()
     d = _paged_attend_desc(q, cache, cu_rows, max_rows, o_at, lse_at, split_keys, softmax_scale, err)
     if workspace is not None:
         d.workspace, d.workspace_bytes = _workspace(workspace, dev)
-    # a call that needs a workspace says so before anything is enqueued; those that need none,
-    # the shortest, are spared the question
-    elif _launch("focus_paged_attend", d, dev, stream, FOCUS_E_WORKSPACE) == 0:
+    # a call that needs a workspace says so before anything is enqueued: those of short tables,
+    # which need none, are spared the question
+    elif (d.cache.kv.max_pages * d.cache.kv.page_rows <= 512
+          and _launch("focus_paged_attend", d, dev, stream, FOCUS_E_WORKSPACE) == 0):
         return o, lse
     else:
         n = _query("focus_paged_attend_workspace", d, dev)
-        workspace = _scratch(n, q.device, stream)
-        d.workspace, d.workspace_bytes = workspace.data_ptr(), n
+        if n > 0:
+            workspace = _scratch(n, q.device, stream)
+            d.workspace, d.workspace_bytes = workspace.data_ptr(), n
     _launch("focus_paged_attend", d, dev, stream)
     return o, lse
