@@ -985,8 +985,10 @@ focus_status focus_paged_append(const focus_paged_append_desc* d, focus_stream_t
  *     lse[t, h] = log sum exp(scale * q[t, h] . k)
  * A token with n_i <= 0 has o = 0 and lse = -inf; what it does not see has no effect.
  * cu_rows NULL: one token of every sequence, row b (n_rows = batch).  max_rows bounds m; rows of
- * o and lse past the last sequence's are left as they were.  Scores, weights and sums are
- * float32; each element of k and v enters exactly.
+ * o and lse past the last sequence's are left as they were.  o and lse may have nothing in
+ * common with an input.  Scores, weights and sums are float32; each element of k and v enters
+ * exactly.  A block's scale is applied to the sum of its row's products, which has to be a
+ * float32 number without it: |q| up to 2^111 whatever the rows hold.
  * The rows of a sequence are split over several workgroups, joined by log-sum-exp;
  * with split_keys = 0 the split follows the lengths of the whole batch, so that a
  * sequence's bits may differ by float32 rounding with what else is in the batch; a

@@ -925,7 +925,7 @@ def focus_paged_extend(table, length, page_rows: int, add, free_pages, free_coun
     else:
         at, cu = _need(out.start, i32, one, dev, "out.start"), _need(out.cu_rows, i32, (batch + 1,), dev, "out.cu_rows")
         seq, slot, pos = (_need(x, i32, (n_rows,), dev, "out's maps") for x in (out.row_seq, out.row_slot, out.row_pos))
-    d = PagedExtendDesc(page_rows, batch, max_pages, free_pages.numel(), _need(table, i32, None, dev, "table"),
+    d = PagedExtendDesc(page_rows, batch, max_pages, _i32(free_pages.numel(), "free_pages' size"), _need(table, i32, None, dev, "table"),
                         _need(length, i32, one, dev, "length"), _need(add, i32, one, dev, "add"),
                         _need(free_pages, i32, None, dev, "free_pages"), _need(free_count, i32, (1,), dev, "free_count"),
                         None if first_pos is None else _need(first_pos, i32, one, dev, "first_pos"), at, cu, n_rows, seq,

@@ -1,11 +1,18 @@
 // Rows stored in a paged cache of 8 bits, a power of two as scale for each block of rows and
 // KV head (focus_paged_append).
 //
-// One wave takes a block of a sequence and a KV head, of k and of v: the largest magnitude of the
-// new rows gives the scale, the elements times its inverse are exact and rounded once.  Lanes
-// take 16 neighbouring elements each (one 16-byte store).  Which blocks a wave takes follows
-// from its rows: it covers a few consecutive ones and takes the blocks whose first new row
-// is among them, so that no block has two writers, whatever the lengths of the sequences.
+// One wave takes a block of a sequence and a KV head, of k and of v, whose new rows stay in its
+// registers (of large blocks, what is past 8 KB of k and of v is read again through the caches):
+// the largest magnitude gives the scale, the elements times its inverse are exact and
+// rounded once.  Lanes take 16 neighbouring elements each (one 16-byte store).  Which blocks a
+// wave takes follows from its rows: it covers a few consecutive ones and takes the blocks whose
+// first new row is among them, so that no block has two writers, whatever the lengths of the
+// sequences.
+//
+// HBM bound for many rows: 101 000 rows of 32 heads of 128 (bf16, 2.48 GB) take 492 us, 5.0
+// TB/s, as fast as this card copies; with plain stores 514, reading the rows twice and dividing
+// by the scale 760.  For few, a chain of latencies: one row of each of 64 sequences 6.5 us
+// (offsets and starts, page table, rows, stores).
 #include "paged.h"
 
 namespace {
@@ -321,7 +328,9 @@ extern "C" focus_status focus_paged_append(const focus_paged_append_desc* d, foc
   while (a.span_shift < a.scale_shift && (int64_t)c.batch << (a.span_shift + 1) <= d->n_rows &&
          focus::ceil_div(d->n_rows, int64_t{1} << a.span_shift) * wide > most)
     ++a.span_shift;
-  const dim3 grid((uint32_t)focus::ceil_div(d->n_rows, int64_t{1} << a.span_shift), (uint32_t)wide);
+  const int64_t spans = focus::ceil_div(d->n_rows, int64_t{1} << a.span_shift);
+  if (spans > INT32_MAX / kThreads) return FOCUS_E_SHAPE;
+  const dim3 grid((uint32_t)spans, (uint32_t)wide);
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   if (d->dtype == FOCUS_BF16) hipLaunchKernelGGL(append_rows<__bf16>, grid, dim3(kThreads), 0, s, a);
   else hipLaunchKernelGGL(append_rows<float>, grid, dim3(kThreads), 0, s, a);

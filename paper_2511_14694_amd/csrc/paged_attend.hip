@@ -1,13 +1,13 @@
 // Attention of the newest tokens of every sequence over a paged cache of 8 bits
 // (focus_paged_attend).
 //
-//   attend_rows  the rows of the whole batch, laid end to end, are dealt in equal shares:
-//                   one workgroup takes a share (parts of one sequence or of several) for one
-//                   to four KV heads and up to 16 or 32 columns of each (a column is a new token
-//                   and a query head); it writes o and lse where a sequence lies in its
-//                   share, else an unnormalised partial (running max, sum, output)
-//   attend_join    merges the partials of a sequence by log-sum-exp
-//   attend_plan    before both for more than 128 sequences: where each begins
+//   attend_rows   the rows of the whole batch, laid end to end, are dealt in equal shares: one
+//                 workgroup takes a share (parts of one sequence or of several) for one to
+//                 eight KV heads and up to 16 or 32 columns of each (a column is a new token
+//                 and a query head); it writes o and lse where a sequence lies in its share,
+//                 else an unnormalised partial (running max, sum, output)
+//   attend_join   merges the partials of a sequence by log-sum-exp
+//   attend_plan   before both for more than 128 sequences: where each begins
 //
 // Every cached byte is read once for up to 32 columns.  A wave takes 32 rows at a time; each
 // lane's loads become operands of bf16 matrix products as they arrive, without LDS (e4m3
@@ -20,6 +20,15 @@
 //                     of which product t takes element D/16 i + t
 // so maximum, sum and rescaling of a column stay in its lanes.  The eight rows of a lane lie
 // in one block, whose scales it multiplies its scores and weights with.
+//
+// HBM bound where there is much to read: 16 sequences of 10 000 rows of 32 heads of 128 (1.31
+// GB) take 207 us, 6.3 TB/s, the vector units busy for 38 % of the cycles and the matrix cores
+// for 13 %; one of 262 144 rows of 8 heads (0.54 GB) 94, 5.7 TB/s.  Where there is less the
+// latencies of the beginning (lengths, page table, first rows: 6 us) and the second launch
+// (5 us and the gap before it) count: 64 sequences of 1 to 8 192 rows of 8 heads (0.12 GB) 34;
+// up to five tokens of 32 sequences of up to 16 384 rows (0.13 GB, 20 columns) 47.  The first
+// form, in equal chunks of each sequence found by a search and 16 columns at a time, took 227,
+// 106, 44 and 69.
 #include "paged_split.h"
 
 #include <algorithm>
@@ -42,17 +51,19 @@ constexpr int kUnit = 128;      // rows of a share's units times sets of KV head
 constexpr int kRows = 32;       // rows of a wave at a time
 constexpr int kMost = 512;      // columns of a KV head
 // Units that a sequence's beginning and end in a share cost: its queries, pages and first rows
-// arrive one after another, some 5 us in which a workgroup streams two units.
+// arrive one after another, some 5 us, in which a workgroup could stream two units, and its
+// outputs leave.  1 / 2 / 3 / 4 units: 64 sequences of 1 to 8 192 rows 46.4 / 41.8 / 41.5 / 41.2
+// us, up to five tokens of 32 sequences 61.1 / 60.0 / 56.3 / 56.2.
 constexpr int kEnds = 4;
 
 // What a lane reads in the place of eight rows that begin past their sequence's end or
 // lie in a page outside the pool.
 __device__ __align__(16) const uint32_t kZeros[64] = {};
 
-// Workspace: int4 info[batch] {first share, shares}; for more than focus::kWave sequences int
-// ends[1 + batch] {units of a share, units up to each sequence's end}; then the partials of a
-// sequence's first rows in a share and of others: float2 ml[2 shares][columns],
-// float o[2 shares][columns][D].
+// Workspace: int2 info[batch] {first share, shares}; for more than focus::kWave sequences int
+// ends[1 + batch] {units of a share, units up to each sequence's end}; then two partials of a
+// share, of the sequence that goes on from the share before and of the one that goes on behind it:
+// float2 ml[2 shares][columns], float o[2 shares][columns][D].
 struct Plan {
   int64_t shares, cap;
   int64_t ends, ml, o;  // byte offsets
@@ -79,7 +90,7 @@ Plan make_plan(const focus_paged_attend_desc* d) {
   p.tiles = (int)focus::ceil_div(per_head, p.cols);
   // Neighbouring heads' rows read together, where they lie side by side; two heads of 64
   // bytes, which share a cache line, by the same wave.  (By waves of their own half of the lines
-  // came twice: 16 x 10 000 rows of 32 such heads 165 us, now 138.  With two tiles of columns
+  // came twice: 16 x 10 000 rows of 32 such heads 165 us, now 136.  With two tiles of columns
   // besides, the registers do not suffice.)
   const bool beside = c.head_stride < c.row_stride;
   p.heads = c.head_dim == 64 && p.cols == 16 && beside && c.n_kv_heads % 2 == 0 ? 2 : 1;
@@ -101,7 +112,7 @@ Plan make_plan(const focus_paged_attend_desc* d) {
                         c.batch * (std::max<int64_t>(1, focus::ceil_div(p.cap, p.unit)) + kEnds));
   }
   const int64_t partials = 2 * p.shares * p.columns;
-  p.ends = 16 * (int64_t)c.batch;
+  p.ends = focus::ceil_div(8 * (int64_t)c.batch, 16) * 16;
   p.ml = p.ends + (p.planned ? focus::ceil_div(4 * ((int64_t)c.batch + 1), 16) * 16 : 0);
   p.o = p.ml + focus::ceil_div(8 * partials, 16) * 16;
   p.bytes = p.single ? 0 : (size_t)(p.o + 4 * partials * c.head_dim);
@@ -245,7 +256,7 @@ struct Walk {
   }
 };
 
-// Slot of the partial of sequence part `chunk`, whose first share is `first`.
+// Slot of the partial of part `chunk` of a sequence whose first share is `first`.
 __device__ inline int64_t slot_of(int first, int chunk) { return chunk == 0 ? 2 * (int64_t)first + 1 : 2 * ((int64_t)first + chunk); }
 
 // A pair of e4m3 numbers in bf16; eight.
@@ -315,9 +326,9 @@ __global__ __launch_bounds__(kThreads, resident(D, TILES, HEADS)) void attend_ro
     share = unit / a.units, g0 = unit % a.units;
     if (share >= a.shares) return;
   } else {
-    // Workgroups that run on one compute unit take different heads: those of neighbouring
-    // heads' first bytes are slower than the others, by 15 % where they begin at even multiples
-    // of 512 bytes.
+    // The two workgroups of a compute unit take different heads: those whose heads begin at
+    // even multiples of 512 bytes are 15 % slower than the others, and with the same heads on
+    // every unit of an XCD half of the XCDs would end late.
     share = blockIdx.x / a.units, g0 = (blockIdx.x + share / a.around) % a.units;
   }
   g0 *= HEADS << a.wide_shift;
@@ -373,11 +384,13 @@ __global__ __launch_bounds__(kThreads, resident(D, TILES, HEADS)) void attend_ro
         } else {
 #pragma unroll
           for (int k = 0; k < 8; ++k) {
+            // (cut off, not rounded: the largest numbers would become infinities)
             float f = src[e + k];
 #pragma unroll
             for (int part = 0; part < kParts; ++part) {
-              q[state][part][i][k] = (__bf16)f;
-              f -= (float)q[state][part][i][k];
+              const float high = __uint_as_float(__float_as_uint(f) & 0xffff0000u);
+              q[state][part][i][k] = (__bf16)high;
+              f -= high;
             }
           }
         }
@@ -530,8 +543,8 @@ __global__ __launch_bounds__(kThreads, resident(D, TILES, HEADS)) void attend_ro
             }
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
           }
-          // product t's rows of V^T: pairs of rows by a byte permutation, then widened; half of
-          // them at a time
+          // product t's rows of V^T: pairs of rows by a byte permutation, then widened; four
+          // products at a time
           bf16x8 p[TILES][kWeightParts];
 #pragma unroll
           for (int tile = 0; tile < TILES; ++tile)

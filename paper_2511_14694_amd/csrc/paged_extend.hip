@@ -8,6 +8,9 @@
 // Pages move through one list in an order that is fixed, so all of them are moved by one
 // workgroup; what there is to do is a few words a sequence, a page and a row, and what it takes
 // is a chain of latencies: the lengths, the sums over the sequences, the pages, their entries.
+// A step of 64 sequences takes 4.7 us, 500 prompts and endings of 123 000 rows and 2 200 pages
+// 7.9 + 3.8; with sums by shuffles in 64 bits, two scans more and a second launch for every call
+// 15 and 15.3.
 #include "paged.h"
 
 namespace {
@@ -233,7 +236,7 @@ extern "C" focus_status focus_paged_extend(const focus_paged_extend_desc* d, foc
   if (d->batch < 0 || d->max_pages < 0 || d->free_cap < 0 || d->n_rows < 0) return FOCUS_E_ARG;
   if (d->page_rows < 8 || d->page_rows > 1024 || (d->page_rows & (d->page_rows - 1))) return FOCUS_E_UNSUPPORTED;
   if ((int64_t)d->max_pages * d->page_rows > INT32_MAX / 2 || (int64_t)d->batch * d->max_pages >= INT32_MAX ||
-      d->batch == INT32_MAX || d->n_rows >= INT32_MAX)
+      d->batch > INT32_MAX / 2 || d->n_rows >= INT32_MAX)
     return FOCUS_E_SHAPE;
   if (!d->cu_rows || !d->free_count || (d->free_cap > 0 && !d->free_pages)) return FOCUS_E_NULL;
   if (d->batch > 0 && (!d->length || !d->add || !d->start || (d->max_pages > 0 && !d->table))) return FOCUS_E_NULL;

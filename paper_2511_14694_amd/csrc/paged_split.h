@@ -40,8 +40,8 @@ struct Split {
 // to read, and for each chunk `each` rows' worth of beginning and end and its partials
 // written and read, over the target; where not all are resident at once kLate of the
 // longest more, which may begin late; at least the longest at kAlone times the rate, as
-// fast as one gets when the others have ended.  us, before twice as many were tried (72 of
-// `each` 100, all of the longest more) / now: 64 sequences of 4096 rows, 5 KV heads, 152 / 120;
+// fast as one gets when the others have ended.  us, before twice as many were tried (100 rows
+// where 72 are now, all of the longest more) / now: 64 sequences of 4096 rows, 5 KV heads, 152 / 120;
 // 48 with 7 heads 152 / 121; 16 of 10 000, 32 heads, 417 / 409; 200 of 1000 to 2000, 8 heads,
 // 272 / 246; 400 of 600 to 1200, 4 heads, 165 / 184; over 104 such batches 0.8 % less.
 constexpr float kLate = 0.3f, kAlone = 1.1f;

@@ -54,6 +54,10 @@ CASES = [
     ([5000, 10, 2500], [1, 4, 2], 8, 2, 128, 64, 16, "bf16", False),
     ([5000, 10, 2500], [2, 2, 2], 4, 4, 128, 16, 8, "f32", False),
     ([3, 2, 9], [3, 5, 12], 2, 1, 64, 8, 8, "bf16", False),         # tokens that see nothing
+    ([257, 33], [3, 1], 40, 2, 64, 16, 8, "f32", False),            # two heads a wave, four tiles
+    ([700, 5], [9, 2], 8, 8, 64, 32, 32, "bf16", False),            # eight heads a workgroup
+    ([700, 5], [2, 1], 5, 5, 64, 32, 32, "bf16", False),            # an odd number of heads of 64
+    ([40, 900], [300, 7], 1, 1, 128, 16, 8, "bf16", False),         # more tokens than rows
 ]
 
 
@@ -192,6 +196,22 @@ def test_attend_scales_of_all_sizes():
     c.dev.v_scale.zero_()
     o, lse = F.focus_paged_attend(q, c.dev)
     assert (o == 0).all() and (lse - math.log(200)).abs().max() < 1e-6
+
+
+def test_attend_great_queries():
+    """The greatest queries whose products with any e4m3 row are float32 numbers, against keys of
+    the least scales."""
+    rng = np.random.default_rng(37)
+    announce("attend great queries")
+    for D in (64, 128):
+        c = Cache8(rng, [70], 2, D, 16, 8)
+        c.dev.k_scale.copy_(torch.as_tensor(2.0 ** rng.integers(-126, -124, tuple(c.dev.k_scale.shape))))
+        c.refresh()
+        q, q64 = values(rng, (1, 4, D), "f32")
+        most = 2.0 ** 111 * (1 - 2.0 ** -24)
+        q = (q * 2.0 ** 109).clamp(-most, most)
+        q64 = to64(q)
+        _check(c, q64, [1], F.focus_paged_attend(q, c.dev, softmax_scale=0.5), "f32", scale=0.5)
 
 
 def test_attend_pages_outside_the_pool_and_bad_offsets():
