@@ -30,6 +30,7 @@ struct Args {
   int shift, scale_shift;  // log2 page_rows, scale_rows
   int span_shift;          // log2 of the rows a wave covers
   int pieces;              // of 16 elements, in a row of a head
+  uint32_t wide;           // workgroups for the heads of a row
   uint32_t inv;            // 2^20 / pieces, rounded up (exact quotients of less than 2^16)
 };
 
@@ -259,11 +260,13 @@ template <typename T>
 __global__ __launch_bounds__(kThreads) void append_rows(Args a) {
   const focus_paged_append_desc& d = a.d;
   const focus_paged_kv& c = d.cache.kv;
-  const int g = blockIdx.y * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  // (neighbouring workgroups take the heads of the same rows)
+  const uint32_t span = blockIdx.x / a.wide;
+  const int g = (int)(blockIdx.x - span * a.wide) * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   if (g >= c.n_kv_heads) return;
   const bool reports = g == 0 && threadIdx.x == 0;
   const int64_t cap = (int64_t)c.max_pages * c.page_rows, in_block = d.cache.scale_rows - 1;
-  int64_t t = (int64_t)blockIdx.x << a.span_shift;
+  int64_t t = (int64_t)span << a.span_shift;
   const int64_t end = min(t + (1 << a.span_shift), d.n_rows), first = t;
   if (d.cu_rows && t == 0 && reports && (d.cu_rows[0] < 0 || d.cu_rows[c.batch] > d.n_rows))
     focus::raise_err(d.err, FOCUS_ERR_BOUNDS);
@@ -329,8 +332,9 @@ extern "C" focus_status focus_paged_append(const focus_paged_append_desc* d, foc
          focus::ceil_div(d->n_rows, int64_t{1} << a.span_shift) * wide > most)
     ++a.span_shift;
   const int64_t spans = focus::ceil_div(d->n_rows, int64_t{1} << a.span_shift);
-  if (spans > INT32_MAX / kThreads) return FOCUS_E_SHAPE;
-  const dim3 grid((uint32_t)spans, (uint32_t)wide);
+  if (spans > INT32_MAX / kThreads / wide) return FOCUS_E_SHAPE;
+  a.wide = (uint32_t)wide;
+  const dim3 grid((uint32_t)(spans * wide));
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   if (d->dtype == FOCUS_BF16) hipLaunchKernelGGL(append_rows<__bf16>, grid, dim3(kThreads), 0, s, a);
   else hipLaunchKernelGGL(append_rows<float>, grid, dim3(kThreads), 0, s, a);
