@@ -15,22 +15,24 @@
 // (offsets and starts, page table, rows, stores).
 #include "paged.h"
 
+#include <algorithm>
+
 namespace {
 
 using focus::u32x4;
 typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kThreads = 256, kWaves = 4;
-constexpr int kResident = 5;         // workgroups of a compute unit that waves of fewer rows may make
+constexpr int kResident = 20;        // workgroups of a compute unit that spans of fewer rows may make
 constexpr float kLargest = 448.f;  // of e4m3
 constexpr uint32_t kInf = 0x7f800000u;
 
 struct Args {
   focus_paged_append_desc d;
   int shift, scale_shift;  // log2 page_rows, scale_rows
-  int span_shift;          // log2 of the rows a wave covers
+  int span_shift;          // log2 of the rows of a span
   int pieces;              // of 16 elements, in a row of a head
-  uint32_t wide;           // workgroups for the heads of a row
+  uint32_t wide;           // waves or workgroups for the heads of a row
   uint32_t inv;            // 2^20 / pieces, rounded up (exact quotients of less than 2^16)
 };
 
@@ -141,130 +143,150 @@ __device__ Owner owner_of(const focus_paged_append_desc& d, int64_t t) {
           __builtin_amdgcn_readlane(start, k)};
 }
 
-// A block's new rows of one KV head, of k or v: rows [t0, t0 + rows) at page + in_page on.
-template <typename T> struct Side {
-  static constexpr int kHeld = sizeof(T) == 2 ? 4 : 2;  // pieces that a lane keeps
+// A block's new rows of one KV head, [t0, t0 + rows) at page + in_page on, of k or v, by GROUP
+// threads, which keep HELD pieces each.
+template <typename T, int HELD, int GROUP> struct Side {
+  const Args& a;
   const T* src;
   int64_t step, to_step;
   uint8_t* dst;
   float* scale;
-  Piece<T> held[kHeld];
+  int n;                // pieces
+  Piece<T> piece[HELD];
   float was;
 
-  __device__ Side(const Args& a, bool is_v, int64_t t0, int64_t page, int in_page, int g) {
+  __device__ Side(const Args& a, bool is_v, int64_t t0, int rows, int64_t page, int in_page, int g) : a(a) {
     const focus_paged_append_desc& d = a.d;
     const focus_paged_kv& c = d.cache.kv;
     step = is_v ? d.v_row : d.k_row, to_step = c.row_stride;
-    src = reinterpret_cast<const T*>(is_v ? d.v : d.k) + t0 * step + (int64_t)g * (is_v ? d.v_head : d.k_head);
-    dst = reinterpret_cast<uint8_t*>(is_v ? c.v : c.k) + page * c.page_stride + (int64_t)g * c.head_stride +
-          in_page * to_step;
+    src = reinterpret_cast<const T*>(is_v ? d.v : d.k) + t0 * step + g * (is_v ? d.v_head : d.k_head);
+    dst = reinterpret_cast<uint8_t*>(is_v ? c.v : c.k) + page * c.page_stride + g * c.head_stride + in_page * to_step;
     scale = (is_v ? d.cache.v_scale : d.cache.k_scale) +
             (page * c.n_kv_heads + g) * (c.page_rows >> a.scale_shift) + (in_page >> a.scale_shift);
+    n = rows * a.pieces;
   }
+  __device__ static int thread() { return threadIdx.x % GROUP; }
   // Row and first element of piece i.
-  __device__ static int2 place(const Args& a, int i) {
+  __device__ int2 place(int i) const {
     const int r = (int)((uint32_t)i * a.inv >> 20);
     return make_int2(r, (i - r * a.pieces) * 16);
   }
-  __device__ void load(const Args& a, int n, bool partly) {
+  __device__ const T* from(int i) const {
+    const int2 at = place(i);
+    return src + at.x * step + at.y;
+  }
+  __device__ u32x4* to(int i) const {
+    const int2 at = place(i);
+    return reinterpret_cast<u32x4*>(dst + at.x * to_step + at.y);
+  }
+  __device__ void load(bool partly) {
 #pragma unroll
-    for (int j = 0; j < kHeld; ++j) {
-      const int i = threadIdx.x % 64 + 64 * j;
-      if (i < n) {
-        const int2 at = place(a, i);
-        held[j].load(src + at.x * step + at.y);
-      } else {
+    for (int j = 0; j < HELD; ++j) {
+      const int i = thread() + GROUP * j;
 #pragma unroll
-        for (int k = 0; k < Piece<T>::kLoads; ++k) held[j].w[k] = u32x4{0, 0, 0, 0};
-      }
+      for (int k = 0; k < Piece<T>::kLoads; ++k) piece[j].w[k] = u32x4{0, 0, 0, 0};
+      if (i < n) piece[j].load(from(i));
     }
     was = partly ? *scale : 0.f;
   }
-  template <bool FINITE> __device__ uint32_t most(const Args& a, int n) const {
+  template <bool FINITE> __device__ uint32_t most(uint32_t* s_max) const {
     uint32_t m = 0;
 #pragma unroll
-    for (int j = 0; j < kHeld; ++j) m = max(m, held[j].template most<FINITE>());
-    for (int i = threadIdx.x % 64 + 64 * kHeld; i < n; i += 64) {
-      const int2 at = place(a, i);
+    for (int j = 0; j < HELD; ++j) m = max(m, piece[j].template most<FINITE>());
+    for (int i = thread() + GROUP * HELD; i < n; i += GROUP) {
       Piece<T> p;
-      p.load(src + at.x * step + at.y);
+      p.load(from(i));
       m = max(m, p.template most<FINITE>());
     }
-    return (uint32_t)focus::wave_max((int)m);
+    m = (uint32_t)focus::wave_max((int)m);
+    if (GROUP > 64) {
+      if (threadIdx.x % 64 == 0) s_max[threadIdx.x / 64] = m;
+      __syncthreads();
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) m = max(m, s_max[w]);
+    }
+    return m;
   }
-  __device__ void store(const Args& a, int n, int in_block) {
-    const int lane = threadIdx.x % 64;
-    uint32_t m = most<false>(a, n);
+  // s_max: two sets of a value of each wave, used by nothing else until the next barrier but one.
+  __device__ void store(int in_block, uint32_t* s_max) {
+    uint32_t m = most<false>(s_max);
     const bool finite = m < kInf;
-    if (!finite) m = most<true>(a, n);
-    float to = __uint_as_float(scale_bits(m));
+    if (!finite) m = most<true>(s_max + kWaves);
+    float by = __uint_as_float(scale_bits(m));
     if (in_block > 0) {
-      if (was >= to) {
-        to = was;
+      if (was >= by) {
+        by = was;
       } else {
-        // (of powers of two, as it is but for the first append to a user's own scales)
-        const float f = was / to;
-        uint8_t* old = dst - in_block * to_step;
-        for (int i = lane; i < in_block * a.pieces; i += 64) {
-          const int2 at = place(a, i);
-          u32x4* p = reinterpret_cast<u32x4*>(old + at.x * to_step + at.y);
+        // the rows before the new ones, from their scale to the greater one
+        const float f = was / by;
+        for (int i = thread(); i < in_block * a.pieces; i += GROUP) {
+          const int2 at = place(i);
+          u32x4* p = reinterpret_cast<u32x4*>(dst + (at.x - in_block) * to_step + at.y);
           const u32x4 w = *p;
           float x[16];
 #pragma unroll
           for (int k = 0; k < 4; ++k) {
-            const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[k], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[k], true);
+            const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[k], false);
+            const auto hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[k], true);
             x[4 * k] = lo[0] * f, x[4 * k + 1] = lo[1] * f, x[4 * k + 2] = hi[0] * f, x[4 * k + 3] = hi[1] * f;
           }
           *p = round16(x);
         }
       }
     }
-    const Scaler by = scaler(to, finite);
+    const Scaler scaled = scaler(by, finite);
 #pragma unroll
-    for (int j = 0; j < kHeld; ++j) {
-      const int i = lane + 64 * j;
-      if (i < n) {
-        const int2 at = place(a, i);
-        __builtin_nontemporal_store(round_piece(held[j], by), reinterpret_cast<u32x4*>(dst + at.x * to_step + at.y));
-      }
+    for (int j = 0; j < HELD; ++j) {
+      const int i = thread() + GROUP * j;
+      if (i < n) __builtin_nontemporal_store(round_piece(piece[j], scaled), to(i));
     }
-    for (int i = lane + 64 * kHeld; i < n; i += 64) {
-      const int2 at = place(a, i);
+    for (int i = thread() + GROUP * HELD; i < n; i += GROUP) {
       Piece<T> p;
-      p.load(src + at.x * step + at.y);
-      __builtin_nontemporal_store(round_piece(p, by), reinterpret_cast<u32x4*>(dst + at.x * to_step + at.y));
+      p.load(from(i));
+      __builtin_nontemporal_store(round_piece(p, scaled), to(i));
     }
-    if (lane == 0) *scale = to;
+    if (thread() == 0) *scale = by;
   }
 };
 
-template <typename T>
-__device__ void store_block(const Args& a, int64_t t0, int rows, int b, int64_t slot, int g) {
+// more: the sequence has further rows behind these.
+template <typename T, int HELD, int GROUP>
+__device__ void store_block(const Args& a, int64_t t0, int rows, int b, int64_t slot, int g, bool more, uint32_t* s_max) {
   const focus_paged_append_desc& d = a.d;
   const focus_paged_kv& c = d.cache.kv;
   const int64_t page = focus::page_of(c, b, (int)slot, a.shift);
+  const bool reports = g == 0 && threadIdx.x % GROUP == 0;
   if (page < 0) {
-    if (g == 0 && threadIdx.x % 64 == 0) focus::raise_err(d.err, FOCUS_ERR_BOUNDS);
+    if (reports) focus::raise_err(d.err, FOCUS_ERR_BOUNDS);
     return;
   }
   const int in_block = (int)(slot & (d.cache.scale_rows - 1)), in_page = (int)(slot & (c.page_rows - 1));
-  const int n = rows * a.pieces;
   // (both in flight before either is looked at)
-  Side<T> k(a, false, t0, page, in_page, g), v(a, true, t0, page, in_page, g);
-  k.load(a, n, in_block > 0), v.load(a, n, in_block > 0);
-  k.store(a, n, in_block), v.store(a, n, in_block);
-  if (g == 0 && threadIdx.x % 64 == 0) atomicMax(&c.length[b], (int)slot + rows);
+  Side<T, HELD, GROUP> k(a, false, t0, rows, page, in_page, g), v(a, true, t0, rows, page, in_page, g);
+  k.load(in_block > 0), v.load(in_block > 0);
+  k.store(in_block, s_max), v.store(in_block, s_max + 2 * kWaves);
+  // The length is raised by the last block, or the last before one that is not stored.  (By all
+  // of them: 81 600 rows of one head in 10 200 blocks 128 us, now 21.)
+  if (reports) {
+    const int64_t next = slot + rows;
+    if (!more || next >= (int64_t)c.max_pages * c.page_rows ||
+        ((next & (c.page_rows - 1)) == 0 && focus::page_of(c, b, (int)next, a.shift) < 0))
+      atomicMax(&c.length[b], (int)next);
+  }
 }
 
-template <typename T>
+// GROUP: threads of a block, those of a wave or of the workgroup.  HELD: pieces that a thread
+// keeps of k, and of v.
+template <typename T, int HELD, int GROUP>
 __global__ __launch_bounds__(kThreads) void append_rows(Args a) {
+  __shared__ uint32_t s_max[4 * kWaves];
   const focus_paged_append_desc& d = a.d;
   const focus_paged_kv& c = d.cache.kv;
-  // (neighbouring workgroups take the heads of the same rows)
-  const uint32_t span = blockIdx.x / a.wide;
-  const int g = (int)(blockIdx.x - span * a.wide) * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-  if (g >= c.n_kv_heads) return;
-  const bool reports = g == 0 && threadIdx.x == 0;
+  // (neighbours take the heads of the same rows)
+  const uint32_t id = GROUP == 64 ? blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x / 64) : blockIdx.x;
+  const uint32_t span = id / a.wide;
+  const int g = (int)(id - span * a.wide);
+  const bool reports = g == 0 && threadIdx.x % GROUP == 0;
   const int64_t cap = (int64_t)c.max_pages * c.page_rows, in_block = d.cache.scale_rows - 1;
   int64_t t = (int64_t)span << a.span_shift;
   const int64_t end = min(t + (1 << a.span_shift), d.n_rows), first = t;
@@ -277,19 +299,48 @@ __global__ __launch_bounds__(kThreads) void append_rows(Args a) {
       t = t < o.r0 ? o.r0 : o.r1;
       continue;
     }
-    // from the first block whose first new row is not before this wave's rows
+    // from the first block whose first new row is not before this span
     const int64_t to_slot = o.start - o.r0;
     if (t == first && t > o.r0) t = ((t + to_slot + in_block) & ~(int64_t)in_block) - to_slot;
     for (; t < end && t < o.r1; t = ((t + to_slot + in_block + 1) & ~(int64_t)in_block) - to_slot) {
       const int64_t slot = t + to_slot, stop = min(o.r1, ((slot + in_block + 1) & ~(int64_t)in_block) - to_slot);
       if (slot < cap) {
-        store_block<T>(a, t, (int)(stop - t), o.b, slot, g);
+        store_block<T, HELD, GROUP>(a, t, (int)(stop - t), o.b, slot, g, stop < o.r1, s_max);
       } else if (reports) {
         focus::raise_err(d.err, FOCUS_ERR_CAPACITY);
       }
     }
     t = min(t, o.r1);
   }
+}
+
+template <typename T> focus_status launch(Args a, hipStream_t s) {
+  const focus_paged_append_desc& d = a.d;
+  const focus_paged_kv& c = d.cache.kv;
+  // A wave takes a block that fits its registers, of as many rows as sequences have on average;
+  // the fewer it has to keep, the more waves run together.  A larger block takes a workgroup.
+  constexpr int kMost = sizeof(T) == 2 ? 4 : 2;
+  const int64_t rows = std::min<int64_t>(d.cache.scale_rows, focus::ceil_div(d.n_rows, c.batch));
+  const int held = (int)focus::ceil_div(rows * a.pieces, 64);
+  const int group = held <= kMost ? kWaves : 1;  // blocks of a workgroup
+  const int64_t wide = c.n_kv_heads, most = (int64_t)group * kResident * focus::device_cus();
+  // Rows of a span: one (most then find that their block is another's) as long as that makes
+  // few of them, else up to as many as a block or a sequence has, on average: short sequences
+  // in a span follow one another.  24 calls of 1 to 80 000 rows, workgroups of a compute unit up
+  // to which spans are made shorter, geometric mean: 2 16.3 us, 5 16.1, 10 15.6, 20 15.6, 40
+  // 15.7, 80 16.1.
+  while (a.span_shift < a.scale_shift && (int64_t)c.batch << (a.span_shift + 1) <= d.n_rows &&
+         focus::ceil_div(d.n_rows, int64_t{1} << a.span_shift) * wide > most)
+    ++a.span_shift;
+  const int64_t spans = focus::ceil_div(d.n_rows, int64_t{1} << a.span_shift);
+  if (spans > INT32_MAX / kThreads / wide) return FOCUS_E_SHAPE;
+  a.wide = (uint32_t)wide;
+  const dim3 grid((uint32_t)focus::ceil_div(spans * wide, group));
+  if (held == 1) hipLaunchKernelGGL((append_rows<T, 1, 64>), grid, dim3(kThreads), 0, s, a);
+  else if (held == 2) hipLaunchKernelGGL((append_rows<T, 2, 64>), grid, dim3(kThreads), 0, s, a);
+  else if (held <= kMost) hipLaunchKernelGGL((append_rows<T, kMost, 64>), grid, dim3(kThreads), 0, s, a);
+  else hipLaunchKernelGGL((append_rows<T, kMost, kThreads>), grid, dim3(kThreads), 0, s, a);
+  return focus::launch_status();
 }
 
 focus_status validate(const focus_paged_append_desc* d) {
@@ -323,20 +374,6 @@ extern "C" focus_status focus_paged_append(const focus_paged_append_desc* d, foc
   a.d = *d;
   a.shift = focus::page_shift(c), a.scale_shift = __builtin_ctz((unsigned)d->cache.scale_rows);
   a.pieces = c.head_dim / 16, a.inv = ((1 << 20) + a.pieces - 1) / a.pieces;
-  // Rows of a wave: one (most then find that their block is another wave's) as long as that
-  // makes few workgroups, else up to as many as a block or a sequence has, on average.  1627
-  // rows of 3 heads of 96 in 7 sequences, blocks of 8 (float32): one row 18.7 us, two 12.2,
-  // four 13.4, eight 13.6.
-  const int64_t wide = focus::ceil_div(c.n_kv_heads, kWaves), most = kResident * focus::device_cus();
-  while (a.span_shift < a.scale_shift && (int64_t)c.batch << (a.span_shift + 1) <= d->n_rows &&
-         focus::ceil_div(d->n_rows, int64_t{1} << a.span_shift) * wide > most)
-    ++a.span_shift;
-  const int64_t spans = focus::ceil_div(d->n_rows, int64_t{1} << a.span_shift);
-  if (spans > INT32_MAX / kThreads / wide) return FOCUS_E_SHAPE;
-  a.wide = (uint32_t)wide;
-  const dim3 grid((uint32_t)(spans * wide));
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
-  if (d->dtype == FOCUS_BF16) hipLaunchKernelGGL(append_rows<__bf16>, grid, dim3(kThreads), 0, s, a);
-  else hipLaunchKernelGGL(append_rows<float>, grid, dim3(kThreads), 0, s, a);
-  return focus::launch_status();
+  return d->dtype == FOCUS_BF16 ? launch<__bf16>(a, s) : launch<float>(a, s);
 }

@@ -95,10 +95,13 @@ Plan make_plan(const focus_paged_attend_desc* d) {
   const bool beside = c.head_stride < c.row_stride;
   p.heads = c.head_dim == 64 && p.cols == 16 && beside && c.n_kv_heads % 2 == 0 ? 2 : 1;
   const int sets = c.n_kv_heads / p.heads;
-  p.wide = !beside ? 1 : sets % 4 == 0 ? 4 : sets % 2 == 0 ? 2 : 1;
+  auto wide = [&](int most) { return most >= 4 && sets % 4 == 0 ? 4 : most >= 2 && sets % 2 == 0 ? 2 : 1; };
+  p.wide = wide(beside ? 4 : 1);
   const int64_t heads = (int64_t)c.batch * c.n_kv_heads * p.tiles;
   p.single = d->split_keys == 0 && (p.cap <= kWhole || (p.cap <= 2 * kWhole && heads >= 128));
-  if (p.single && heads <= 1024) p.wide = 1;
+  // (short tables: no more waves for a head than there are tiles; 108 sequences of 32 float32
+  // heads in tables of 16 rows 51 us with four, now 22)
+  if (p.single) p.wide = std::max(heads <= 1024 ? 1 : p.wide, wide(p.cap <= kRows ? 4 : p.cap <= 2 * kRows ? 2 : 1));
   p.planned = !p.single && c.batch > focus::kWave;
   p.groups = (int64_t)sets / p.wide * p.tiles;
   if (p.single) {

@@ -179,7 +179,14 @@ def test_append_skips_what_it_cannot_store():
         c.refresh()
         for got, want in zip((c.pk, c.pv, c.ks, c.vs), ref):
             same(got, want, "others")
-        assert err.item() == F.FOCUS_ERR_BOUNDS
+        assert err.item() == F.FOCUS_ERR_BOUNDS and c.dev.length.tolist() == [45, 3]
+        # the last page: the length ends before it
+        err.zero_()
+        c.dev.length.zero_()
+        c.dev.table[0, 1], c.dev.table[0, 2] = int(p), bad
+        (x, _), (y, _) = _new(rng, [43], K, D, "bf16")
+        F.focus_paged_append(x, y, c.dev, i32([5, 0]), i32([0, 40, 43]), err=err)
+        assert err.item() == F.FOCUS_ERR_BOUNDS and c.dev.length.tolist() == [32, 3]
 
     # rows past the table
     announce("append past the table")
