@@ -14,8 +14,8 @@
  *   focus_paged_decode                 one-token attention over a paged cache
  *   focus_paged_evict                  a paged cache cut down to a budget
  *   focus_paged_extend                 page tables and slot maps from the rows to come
- *   focus_paged_append                rows stored in a paged cache of 8 bits
- *   focus_paged_attend                attention of the newest tokens over one
+ *   focus_paged_append                 rows stored in a paged cache of 8 bits
+ *   focus_paged_attend                 attention of the newest tokens over one
  *
  * Conventions shared by every call
  * --------------------------------
@@ -934,7 +934,8 @@ focus_status focus_paged_extend(const focus_paged_extend_desc* d, focus_stream_t
 /* A paged K/V cache in FOCUS_E4M3, with a scale for each block of scale_rows rows and KV
  * head: row r of sequence b in page p stands for its 8-bit elements times
  * k_scale[(p * n_kv_heads + g) * (page_rows / scale_rows) + r % page_rows / scale_rows].
- * Scales may be any float32 (focus_paged_append makes powers of two). */
+ * Scales may be any float32 below 2^127 in magnitude (focus_paged_append makes powers of
+ * two). */
 typedef struct {
   focus_paged_kv kv;            /* dtype FOCUS_E4M3; strides in elements, whole
                                    16-byte pieces; weight NULL               */

@@ -997,9 +997,9 @@ def focus_paged_append(k, v, cache: PagedCache8, start, cu_rows=None, err=None, 
         raise ValueError("k must be [rows, heads, D], bfloat16 or float32")
     shape = (k.shape[0], kv.n_kv_heads, kv.head_dim)
     d = PagedAppendDesc(c, _DTYPES[dtype], 0, shape[0],
-                         None if cu_rows is None else _need(cu_rows, torch.int32, (kv.batch + 1,), dev, "cu_rows"),
-                         _need(start, torch.int32, (kv.batch,), dev, "start"), *_rows(k, shape, dtype, dev, "k"),
-                         *_rows(v, shape, dtype, dev, "v"), None if err is None else _err_ptr(err, dev))
+                        None if cu_rows is None else _need(cu_rows, torch.int32, (kv.batch + 1,), dev, "cu_rows"),
+                        _need(start, torch.int32, (kv.batch,), dev, "start"), *_rows(k, shape, dtype, dev, "k"),
+                        *_rows(v, shape, dtype, dev, "v"), None if err is None else _err_ptr(err, dev))
     _launch("focus_paged_append", d, dev, stream)
 
 
@@ -1010,9 +1010,9 @@ def _paged_attend_desc(q, cache, cu_rows, max_rows, o, lse, split_keys, softmax_
     if len(shape) != 3 or shape[2] != kv.head_dim or dev != cache.k.get_device() or dtype not in _DTYPES:
         raise ValueError("q must be [rows, heads, D], bfloat16 or float32, of the cache's head_dim and device")
     return PagedAttendDesc(c, _DTYPES[dtype], shape[1], _i32(max_rows, "max_rows"), _i32(split_keys, "split_keys"),
-                            float(softmax_scale), 0, shape[0],
-                            None if cu_rows is None else _need(cu_rows, torch.int32, (kv.batch + 1,), dev, "cu_rows"),
-                            *_rows(q, shape, dtype, dev, "q"), o, lse, None, 0, None if err is None else _err_ptr(err, dev))
+                           float(softmax_scale), 0, shape[0],
+                           None if cu_rows is None else _need(cu_rows, torch.int32, (kv.batch + 1,), dev, "cu_rows"),
+                           *_rows(q, shape, dtype, dev, "q"), o, lse, None, 0, None if err is None else _err_ptr(err, dev))
 
 
 def focus_paged_attend_workspace(q, cache: PagedCache8, cu_rows=None, max_rows: int = 1, split_keys: int = 0) -> int:
@@ -1021,7 +1021,7 @@ def focus_paged_attend_workspace(q, cache: PagedCache8, cu_rows=None, max_rows: 
 
 
 def focus_paged_attend(q, cache: PagedCache8, cu_rows=None, max_rows: int = 1, o=None, lse=None, workspace=None,
-                        split_keys: int = 0, softmax_scale: float = 0.0, want_lse: bool = True, err=None, stream=None):
+                       split_keys: int = 0, softmax_scale: float = 0.0, want_lse: bool = True, err=None, stream=None):
     """Attention of the newest tokens of every sequence over an 8-bit paged cache that holds
     their rows already: q [rows, H, D] (turned; bfloat16 or float32; D 64 or 128), rows
     cu_rows[b] : cu_rows[b + 1] (int32 [batch + 1], at most max_rows of them) the last ones of

@@ -9,10 +9,11 @@
 // first new row is among them, so that no block has two writers, whatever the lengths of the
 // sequences.
 //
-// HBM bound for many rows: 101 000 rows of 32 heads of 128 (bf16, 2.48 GB) take 492 us, 5.0
-// TB/s, as fast as this card copies; with plain stores 514, reading the rows twice and dividing
-// by the scale 760.  For few, a chain of latencies: one row of each of 64 sequences 6.5 us
-// (offsets and starts, page table, rows, stores).
+// HBM bound for many rows: 101 000 rows of 32 heads of 128 (bf16, 2.48 GB) take 445 us, 5.6
+// TB/s (two bytes read for each written; this card copies at 5.0, one for one).  With the heads of
+// a row far apart among the workgroups 492; with plain stores besides 514; reading the rows twice
+// and dividing by the scale 760.  For few, a chain of latencies: one row of each of 64
+// sequences 6.1 us (offsets and starts, page table, rows, stores).
 #include "paged.h"
 
 #include <algorithm>
@@ -289,7 +290,7 @@ __global__ __launch_bounds__(kThreads) void append_rows(Args a) {
   const bool reports = g == 0 && threadIdx.x % GROUP == 0;
   const int64_t cap = (int64_t)c.max_pages * c.page_rows, in_block = d.cache.scale_rows - 1;
   int64_t t = (int64_t)span << a.span_shift;
-  const int64_t end = min(t + (1 << a.span_shift), d.n_rows), first = t;
+  const int64_t end = min(t + (int64_t{1} << a.span_shift), d.n_rows), first = t;
   if (d.cu_rows && t == 0 && reports && (d.cu_rows[0] < 0 || d.cu_rows[c.batch] > d.n_rows))
     focus::raise_err(d.err, FOCUS_ERR_BOUNDS);
   while (t < end) {
@@ -332,10 +333,11 @@ template <typename T> focus_status launch(Args a, hipStream_t s) {
   while (a.span_shift < a.scale_shift && (int64_t)c.batch << (a.span_shift + 1) <= d.n_rows &&
          focus::ceil_div(d.n_rows, int64_t{1} << a.span_shift) * wide > most)
     ++a.span_shift;
-  const int64_t spans = focus::ceil_div(d.n_rows, int64_t{1} << a.span_shift);
-  if (spans > INT32_MAX / kThreads / wide) return FOCUS_E_SHAPE;
+  // (more than a launch holds: a span of several blocks)
+  auto workgroups = [&] { return focus::ceil_div(focus::ceil_div(d.n_rows, int64_t{1} << a.span_shift) * wide, group); };
+  while (workgroups() > INT32_MAX / kThreads) ++a.span_shift;
   a.wide = (uint32_t)wide;
-  const dim3 grid((uint32_t)focus::ceil_div(spans * wide, group));
+  const dim3 grid((uint32_t)workgroups());
   if (held == 1) hipLaunchKernelGGL((append_rows<T, 1, 64>), grid, dim3(kThreads), 0, s, a);
   else if (held == 2) hipLaunchKernelGGL((append_rows<T, 2, 64>), grid, dim3(kThreads), 0, s, a);
   else if (held <= kMost) hipLaunchKernelGGL((append_rows<T, kMost, 64>), grid, dim3(kThreads), 0, s, a);

@@ -7,6 +7,7 @@ import torch
 
 import paper_2511_14694_amd as F
 from gpu_util import DEV, announce
+from oracle import paged8 as O
 from paged8_util import Cache8, appended, i32, same, to_codes
 from paged_util import values
 
@@ -226,3 +227,36 @@ def test_append_nothing():
     same(to_codes(c.dev.k), before[0], "k")
     same(to_codes(c.dev.v), before[1], "v")
     assert c.dev.length.tolist() == [5, 9]
+
+
+def test_append_more_blocks_than_a_launch_has_waves():
+    """262 144 rows of 1 024 heads of 16 in blocks of 8: 2^25 of them, one wave each would be more
+    threads than a launch may have.  Every head gets the same rows."""
+    announce("append 2^25 blocks")
+    rows, K, D, page, block = 262_144, 1024, 16, 1024, 8
+    pages = rows // page
+    rng = np.random.default_rng(11)
+    k64 = rng.standard_normal((rows, D)).astype(np.float32)
+    k64[:, 0] *= 2.0 ** rng.integers(-8, 9, rows)     # (blocks of different scales)
+    k = torch.as_tensor(k64).to(DEV).bfloat16()
+    wide = k[:, None, :].expand(rows, K, D)
+    pools = [torch.zeros(pages, page, K, D, dtype=torch.float8_e4m3fn, device=DEV) for _ in range(2)]
+    scales = [torch.zeros(pages, K, page // block, device=DEV) for _ in range(2)]
+    c = F.PagedCache8(*pools, *scales, torch.arange(pages, dtype=torch.int32, device=DEV)[None].flip(1).contiguous(), i32([0]))
+    F.focus_paged_append(wide, wide, c, i32([0]), i32([0, rows]))
+    # one head by itself, held to the definition elsewhere
+    one = F.PagedCache8(*(torch.zeros(pages, page, 1, D, dtype=torch.float8_e4m3fn, device=DEV) for _ in range(2)),
+                        *(torch.zeros(pages, 1, page // block, device=DEV) for _ in range(2)), c.table, i32([0]))
+    F.focus_paged_append(k[:, None], k[:, None], one, i32([0]), i32([0, rows]))
+    assert c.length.item() == one.length.item() == rows
+    assert one.k_scale.unique().numel() > 4
+    for x, y in ((c.k, one.k), (c.v, one.v)):
+        for i in range(0, pages, 32):
+            a, b = x.view(torch.uint8)[i:i + 32], y.view(torch.uint8)[i:i + 32]
+            assert bool((a == b).all())
+    for x, y in ((c.k_scale, one.k_scale), (c.v_scale, one.v_scale)):
+        assert bool((x == y).all())
+    block0 = k64[:block].astype(np.float64)
+    block0 = torch.as_tensor(block0).bfloat16().double().numpy()
+    want, scale = O.append(np.zeros((block, D)), np.zeros(1), block, 0, block0)
+    assert np.array_equal(to_codes(one.k)[pages - 1, :block, 0], want) and one.k_scale[pages - 1, 0, 0].item() == scale[0]
