@@ -21,6 +21,9 @@ Modules
   paged      rotary positions, one token's attention over a paged cache and the
              cache's eviction by accumulated weight (operators of serving that the
              paper does not define; their definitions are the module's own)
+  paged8     the same cache in 8 bits: numbers of e4m3, a scale for each block of rows,
+             slots taken and given back, attention of the newest tokens (operators of
+             serving, too)
 
 Parity pins (each function is checked against facts the paper or mathematics
 fix, never against itself) live in tests/test_oracle_*.py.  No function here is

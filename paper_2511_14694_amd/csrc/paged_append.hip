@@ -1,13 +1,13 @@
 // Rows stored in a paged cache of 8 bits, a power of two as scale for each block of rows and
 // KV head (focus_paged_append).
 //
-// One wave takes a block of a sequence and a KV head, of k and of v, whose new rows stay in its
-// registers (of large blocks, what is past 8 KB of k and of v is read again through the caches):
-// the largest magnitude gives the scale, the elements times its inverse are exact and
-// rounded once.  Lanes take 16 neighbouring elements each (one 16-byte store).  Which blocks a
-// wave takes follows from its rows: it covers a few consecutive ones and takes the blocks whose
-// first new row is among them, so that no block has two writers, whatever the lengths of the
-// sequences.
+// One wave takes a block of a sequence and a KV head, of k and of v (of larger blocks one of
+// them, or a workgroup does), whose new rows stay in its registers: the largest magnitude gives
+// the scale, the elements times its inverse are exact and rounded once.  Lanes take 32
+// neighbouring bytes each: two loads, one store.  (100 000 float32 rows of 8 heads by 64 / 32 / 16
+// bytes 270 / 198 / 195 us; 101 000 bf16 rows of 32 by 32 / 16 448 / 464.)  Which blocks a wave takes
+// follows from its rows: it covers a few consecutive ones and takes the blocks whose first new
+// row is among them, so that no block has two writers, whatever the lengths of the sequences.
 //
 // HBM bound for many rows: 101 000 rows of 32 heads of 128 (bf16, 2.48 GB) take 445 us, 5.6
 // TB/s (two bytes read for each written; this card copies at 5.0, one for one).  With the heads of
@@ -17,6 +17,7 @@
 #include "paged.h"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace {
 
@@ -32,9 +33,9 @@ struct Args {
   focus_paged_append_desc d;
   int shift, scale_shift;  // log2 page_rows, scale_rows
   int span_shift;          // log2 of the rows of a span
-  int pieces;              // of 16 elements, in a row of a head
+  int pieces;              // in a row of a head
   uint32_t wide;           // waves or workgroups for the heads of a row
-  uint32_t inv;            // 2^20 / pieces, rounded up (exact quotients of less than 2^16)
+  uint32_t inv;            // 2^20 / pieces, rounded up (exact quotients of less than 1 024 pieces)
 };
 
 // The least e >= -126 with most <= 448 2^e, as the bits of 2^e; most finite.
@@ -44,14 +45,18 @@ __device__ inline uint32_t scale_bits(uint32_t most) {
   return (uint32_t)(max(e, -126) + 127) << 23;
 }
 
-// 16 elements of T: as loaded, and as float32.
+// Neighbouring elements that a lane takes together, 32 bytes of T: as loaded, and as float32.
 template <typename T> struct Piece {
-  static constexpr int kLoads = sizeof(T);  // of 16 bytes
+  static constexpr int kElts = 32 / sizeof(T), kLoads = 2;
   u32x4 w[kLoads];
   __device__ void load(const T* p) {
 #pragma unroll
     for (int i = 0; i < kLoads; ++i)
-      w[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p + i * (16 / kLoads)));
+      w[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p + i * (kElts / kLoads)));
+  }
+  __device__ void clear() {
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) w[i] = u32x4{0, 0, 0, 0};
   }
   __device__ float at(int k) const {
     if constexpr (sizeof(T) == 2) return k % 2 ? focus::bf16_hi(w[k / 8][k / 2 % 4]) : focus::bf16_lo(w[k / 8][k / 2 % 4]);
@@ -63,12 +68,12 @@ template <typename T> struct Piece {
     if constexpr (sizeof(T) == 2 && !FINITE) {
       u16x2 x = {0, 0};
 #pragma unroll
-      for (int k = 0; k < 8; ++k)
+      for (int k = 0; k < kElts / 2; ++k)
         x = __builtin_elementwise_max(x, __builtin_bit_cast(u16x2, w[k / 4][k % 4] & 0x7fff7fffu));
       m = (uint32_t)max(x[0], x[1]) << 16;
     } else {
 #pragma unroll
-      for (int k = 0; k < 16; ++k) {
+      for (int k = 0; k < kElts; ++k) {
         const uint32_t x = __float_as_uint(at(k)) & 0x7fffffffu;
         m = max(m, FINITE && x >= kInf ? 0u : x);
       }
@@ -94,28 +99,36 @@ __device__ inline Scaler scaler(float to, bool finite) {
   return {to, __uint_as_float(0x7f000000u - u), exact, finite};
 }
 
-__device__ inline u32x4 round16(const float (&x)[16]) {
-  u32x4 r;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    int w = 0;
-    w = __builtin_amdgcn_cvt_pk_fp8_f32(x[4 * i], x[4 * i + 1], w, false);
-    w = __builtin_amdgcn_cvt_pk_fp8_f32(x[4 * i + 2], x[4 * i + 3], w, true);
-    r[i] = (uint32_t)w;
-  }
-  return r;
+__device__ inline uint32_t round4(float x0, float x1, float x2, float x3) {
+  const int w = __builtin_amdgcn_cvt_pk_fp8_f32(x0, x1, 0, false);
+  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(x2, x3, w, true);
 }
-template <typename T> __device__ inline u32x4 round_piece(const Piece<T>& p, const Scaler& by) {
-  float x[16];
-  if (by.exact && by.finite) {
+// A piece's elements in 8 bits, as they are stored.
+template <typename T> struct Narrow {
+  static constexpr int kWords = Piece<T>::kElts / 4;
+  typedef uint32_t W __attribute__((ext_vector_type(kWords)));
+  W w;
+  __device__ Narrow(const Piece<T>& p, const Scaler& by) {
+    float x[4 * kWords];
+    if (by.exact && by.finite) {
 #pragma unroll
-    for (int k = 0; k < 16; ++k) x[k] = p.at(k) * by.inv;
-  } else {
+      for (int k = 0; k < 4 * kWords; ++k) x[k] = p.at(k) * by.inv;
+    } else {
 #pragma unroll
-    for (int k = 0; k < 16; ++k) x[k] = by(p.at(k));
+      for (int k = 0; k < 4 * kWords; ++k) x[k] = by(p.at(k));
+    }
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) w[i] = round4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
   }
-  return round16(x);
-}
+  // Numbers that are stored, times f.
+  __device__ Narrow(W old, float f) {
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) {
+      const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)old[i], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)old[i], true);
+      w[i] = round4(lo[0] * f, lo[1] * f, hi[0] * f, hi[1] * f);
+    }
+  }
+};
 
 // The sequence of row t, the first whose rows end behind it (b = batch if none does), its
 // rows [r0, r1) and where they begin in it, by a wave: 64 offsets are looked at together.  (The
@@ -170,22 +183,21 @@ template <typename T, int HELD, int GROUP> struct Side {
   // Row and first element of piece i.
   __device__ int2 place(int i) const {
     const int r = (int)((uint32_t)i * a.inv >> 20);
-    return make_int2(r, (i - r * a.pieces) * 16);
+    return make_int2(r, (i - r * a.pieces) * Piece<T>::kElts);
   }
   __device__ const T* from(int i) const {
     const int2 at = place(i);
     return src + at.x * step + at.y;
   }
-  __device__ u32x4* to(int i) const {
+  __device__ typename Narrow<T>::W* to(int i) const {
     const int2 at = place(i);
-    return reinterpret_cast<u32x4*>(dst + at.x * to_step + at.y);
+    return reinterpret_cast<typename Narrow<T>::W*>(dst + at.x * to_step + at.y);
   }
   __device__ void load(bool partly) {
 #pragma unroll
     for (int j = 0; j < HELD; ++j) {
       const int i = thread() + GROUP * j;
-#pragma unroll
-      for (int k = 0; k < Piece<T>::kLoads; ++k) piece[j].w[k] = u32x4{0, 0, 0, 0};
+      piece[j].clear();
       if (i < n) piece[j].load(from(i));
     }
     was = partly ? *scale : 0.f;
@@ -208,7 +220,7 @@ template <typename T, int HELD, int GROUP> struct Side {
     }
     return m;
   }
-  // s_max: two sets of a value of each wave, used by nothing else until the next barrier but one.
+  // s_max: two sets of a value of each wave, used by nothing else until the caller's barrier.
   __device__ void store(int in_block, uint32_t* s_max) {
     uint32_t m = most<false>(s_max);
     const bool finite = m < kInf;
@@ -222,16 +234,8 @@ template <typename T, int HELD, int GROUP> struct Side {
         const float f = was / by;
         for (int i = thread(); i < in_block * a.pieces; i += GROUP) {
           const int2 at = place(i);
-          u32x4* p = reinterpret_cast<u32x4*>(dst + (at.x - in_block) * to_step + at.y);
-          const u32x4 w = *p;
-          float x[16];
-#pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[k], false);
-            const auto hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[k], true);
-            x[4 * k] = lo[0] * f, x[4 * k + 1] = lo[1] * f, x[4 * k + 2] = hi[0] * f, x[4 * k + 3] = hi[1] * f;
-          }
-          *p = round16(x);
+          auto* p = reinterpret_cast<typename Narrow<T>::W*>(dst + (at.x - in_block) * to_step + at.y);
+          *p = Narrow<T>(*p, f).w;
         }
       }
     }
@@ -239,33 +243,41 @@ template <typename T, int HELD, int GROUP> struct Side {
 #pragma unroll
     for (int j = 0; j < HELD; ++j) {
       const int i = thread() + GROUP * j;
-      if (i < n) __builtin_nontemporal_store(round_piece(piece[j], scaled), to(i));
+      if (i < n) __builtin_nontemporal_store(Narrow<T>(piece[j], scaled).w, to(i));
     }
     for (int i = thread() + GROUP * HELD; i < n; i += GROUP) {
       Piece<T> p;
       p.load(from(i));
-      __builtin_nontemporal_store(round_piece(p, scaled), to(i));
+      __builtin_nontemporal_store(Narrow<T>(p, scaled).w, to(i));
     }
     if (thread() == 0) *scale = by;
   }
 };
 
 // more: the sequence has further rows behind these.
-template <typename T, int HELD, int GROUP>
-__device__ void store_block(const Args& a, int64_t t0, int rows, int b, int64_t slot, int g, bool more, uint32_t* s_max) {
+template <typename T, int HELD, int GROUP, int SIDES>
+__device__ void store_block(const Args& a, int64_t t0, int rows, int b, int64_t slot, int g, int side, bool more, uint32_t* s_max) {
   const focus_paged_append_desc& d = a.d;
   const focus_paged_kv& c = d.cache.kv;
   const int64_t page = focus::page_of(c, b, (int)slot, a.shift);
-  const bool reports = g == 0 && threadIdx.x % GROUP == 0;
+  const bool reports = g == 0 && side == 0 && threadIdx.x % GROUP == 0;
   if (page < 0) {
     if (reports) focus::raise_err(d.err, FOCUS_ERR_BOUNDS);
     return;
   }
   const int in_block = (int)(slot & (d.cache.scale_rows - 1)), in_page = (int)(slot & (c.page_rows - 1));
-  // (both in flight before either is looked at)
-  Side<T, HELD, GROUP> k(a, false, t0, rows, page, in_page, g), v(a, true, t0, rows, page, in_page, g);
-  k.load(in_block > 0), v.load(in_block > 0);
-  k.store(in_block, s_max), v.store(in_block, s_max + 2 * kWaves);
+  if constexpr (SIDES == 2) {
+    static_assert(GROUP == 64, "waves share s_max");
+    // (both in flight before either is looked at)
+    Side<T, HELD, GROUP> k(a, false, t0, rows, page, in_page, g), v(a, true, t0, rows, page, in_page, g);
+    k.load(in_block > 0), v.load(in_block > 0);
+    k.store(in_block, s_max), v.store(in_block, s_max);
+  } else {
+    Side<T, HELD, GROUP> x(a, side, t0, rows, page, in_page, g);
+    x.load(in_block > 0);
+    x.store(in_block, s_max);
+    if (GROUP > 64) __syncthreads();
+  }
   // The length is raised by the last block, or the last before one that is not stored.  (By all
   // of them: 81 600 rows of one head in 10 200 blocks 128 us, now 21.)
   if (reports) {
@@ -276,18 +288,19 @@ __device__ void store_block(const Args& a, int64_t t0, int rows, int b, int64_t 
   }
 }
 
-// GROUP: threads of a block, those of a wave or of the workgroup.  HELD: pieces that a thread
-// keeps of k, and of v.
-template <typename T, int HELD, int GROUP>
+// GROUP: threads of a block, those of a wave or of the workgroup, which take SIDES of k and v.
+// HELD: pieces that a thread keeps of k, and of v.
+template <typename T, int HELD, int GROUP, int SIDES>
 __global__ __launch_bounds__(kThreads) void append_rows(Args a) {
-  __shared__ uint32_t s_max[4 * kWaves];
+  __shared__ uint32_t s_max[2 * kWaves];
   const focus_paged_append_desc& d = a.d;
   const focus_paged_kv& c = d.cache.kv;
   // (neighbours take the heads of the same rows)
   const uint32_t id = GROUP == 64 ? blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x / 64) : blockIdx.x;
   const uint32_t span = id / a.wide;
-  const int g = (int)(id - span * a.wide);
-  const bool reports = g == 0 && threadIdx.x % GROUP == 0;
+  const int among = (int)(id - span * a.wide), side = SIDES == 1 && among >= c.n_kv_heads;
+  const int g = side ? among - c.n_kv_heads : among;
+  const bool reports = g == 0 && side == 0 && threadIdx.x % GROUP == 0;
   const int64_t cap = (int64_t)c.max_pages * c.page_rows, in_block = d.cache.scale_rows - 1;
   int64_t t = (int64_t)span << a.span_shift;
   const int64_t end = min(t + (int64_t{1} << a.span_shift), d.n_rows), first = t;
@@ -306,7 +319,7 @@ __global__ __launch_bounds__(kThreads) void append_rows(Args a) {
     for (; t < end && t < o.r1; t = ((t + to_slot + in_block + 1) & ~(int64_t)in_block) - to_slot) {
       const int64_t slot = t + to_slot, stop = min(o.r1, ((slot + in_block + 1) & ~(int64_t)in_block) - to_slot);
       if (slot < cap) {
-        store_block<T, HELD, GROUP>(a, t, (int)(stop - t), o.b, slot, g, stop < o.r1, s_max);
+        store_block<T, HELD, GROUP, SIDES>(a, t, (int)(stop - t), o.b, slot, g, side, stop < o.r1, s_max);
       } else if (reports) {
         focus::raise_err(d.err, FOCUS_ERR_CAPACITY);
       }
@@ -318,13 +331,17 @@ __global__ __launch_bounds__(kThreads) void append_rows(Args a) {
 template <typename T> focus_status launch(Args a, hipStream_t s) {
   const focus_paged_append_desc& d = a.d;
   const focus_paged_kv& c = d.cache.kv;
-  // A wave takes a block that fits its registers, of as many rows as sequences have on average;
-  // the fewer it has to keep, the more waves run together.  A larger block takes a workgroup.
-  constexpr int kMost = sizeof(T) == 2 ? 4 : 2;
+  // The fewer pieces a lane has to keep, the more waves run together; blocks have as many rows as
+  // sequences have on average, at most.  A wave takes k and v of a block together up to 4 pieces (8
+  // KB of each), one of them up to 8; larger blocks take a workgroup for each, which keeps 128 KB
+  // (what is past that is read again).  100 000 rows of 8 heads of 128 so, and in brackets k and
+  // v together by a workgroup of 4 pieces: blocks of 64 119 us (143), of 256 134 (184); of float32
+  // 213 (289) and 274 (500).
+  constexpr int kBoth = 4, kMost = 8;
   const int64_t rows = std::min<int64_t>(d.cache.scale_rows, focus::ceil_div(d.n_rows, c.batch));
   const int held = (int)focus::ceil_div(rows * a.pieces, 64);
-  const int group = held <= kMost ? kWaves : 1;  // blocks of a workgroup
-  const int64_t wide = c.n_kv_heads, most = (int64_t)group * kResident * focus::device_cus();
+  const int group = held <= kMost ? kWaves : 1;  // waves of a workgroup that take blocks of their own
+  const int64_t wide = c.n_kv_heads * (held <= kBoth ? 1 : 2), most = (int64_t)group * kResident * focus::device_cus();
   // Rows of a span: one (most then find that their block is another's) as long as that makes
   // few of them, else up to as many as a block or a sequence has, on average: short sequences
   // in a span follow one another.  24 calls of 1 to 80 000 rows, workgroups of a compute unit up
@@ -338,10 +355,24 @@ template <typename T> focus_status launch(Args a, hipStream_t s) {
   while (workgroups() > INT32_MAX / kThreads) ++a.span_shift;
   a.wide = (uint32_t)wide;
   const dim3 grid((uint32_t)workgroups());
-  if (held == 1) hipLaunchKernelGGL((append_rows<T, 1, 64>), grid, dim3(kThreads), 0, s, a);
-  else if (held == 2) hipLaunchKernelGGL((append_rows<T, 2, 64>), grid, dim3(kThreads), 0, s, a);
-  else if (held <= kMost) hipLaunchKernelGGL((append_rows<T, kMost, 64>), grid, dim3(kThreads), 0, s, a);
-  else hipLaunchKernelGGL((append_rows<T, kMost, kThreads>), grid, dim3(kThreads), 0, s, a);
+  auto append = [&](auto held, auto group, auto sides) {
+    hipLaunchKernelGGL((append_rows<T, decltype(held)::value, decltype(group)::value, decltype(sides)::value>), grid,
+                       dim3(kThreads), 0, s, a);
+  };
+  using std::integral_constant;
+  constexpr integral_constant<int, 64> wave;
+  constexpr integral_constant<int, kThreads> workgroup;
+  constexpr integral_constant<int, 1> one;
+  constexpr integral_constant<int, 2> two;
+  constexpr integral_constant<int, 4> four;
+  constexpr integral_constant<int, 8> eight;
+  if (held == 1) append(one, wave, two);
+  else if (held == 2) append(two, wave, two);
+  else if (held <= kBoth) append(four, wave, two);
+  else if (held <= kMost) append(eight, wave, one);
+  else if (held <= kWaves * 4) append(four, workgroup, one);
+  else if (held <= kWaves * 8) append(eight, workgroup, one);
+  else append(integral_constant<int, 16>(), workgroup, one);
   return focus::launch_status();
 }
 
@@ -375,7 +406,8 @@ extern "C" focus_status focus_paged_append(const focus_paged_append_desc* d, foc
   Args a = {};
   a.d = *d;
   a.shift = focus::page_shift(c), a.scale_shift = __builtin_ctz((unsigned)d->cache.scale_rows);
-  a.pieces = c.head_dim / 16, a.inv = ((1 << 20) + a.pieces - 1) / a.pieces;
+  a.pieces = c.head_dim / (d->dtype == FOCUS_BF16 ? Piece<__bf16>::kElts : Piece<float>::kElts);
+  a.inv = ((1 << 20) + a.pieces - 1) / a.pieces;
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   return d->dtype == FOCUS_BF16 ? launch<__bf16>(a, s) : launch<float>(a, s);
 }

@@ -48,6 +48,10 @@ def _new(rng, counts, K, D, dtype, spread=6):
     ([10, 20, 30], [40, 50, 60], 5, 192, 32, 8, "f32", False),
     ([12], [1030], 4, 128, 128, 128, "bf16", False),
     ([1000], [1], 2, 256, 1024, 512, "f32", False),
+    ([3, 70], [130, 200], 3, 128, 64, 64, "bf16", False),
+    ([50, 0], [90, 300], 2, 64, 64, 64, "f32", True),
+    ([100, 300], [257, 400], 2, 256, 128, 128, "bf16", True),
+    ([120], [513], 3, 128, 128, 128, "f32", False),
 ])
 @pytest.mark.parametrize("fused", [False, True])
 def test_append_matches_oracle(lens, add, K, D, page, block, dtype, by_head, fused):
@@ -214,6 +218,30 @@ def test_append_skips_what_it_cannot_store():
     # offsets that do not ascend: nothing outside the pages, an end
     c, k, v = call([0, 0, 0], [12, 9, 4], [0, 0, 0], cu=[0, 20, 7, 25])
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("dtype,D,block", [("bf16", 128, 64), ("bf16", 128, 128), ("f32", 128, 128), ("bf16", 256, 256)])
+def test_append_large_blocks_of_ragged_sequences(dtype, D, block):
+    """Parts of several sequences and their blocks follow one another in a workgroup, some with
+    infinities and NaN; stored twice, the second time larger, so that first parts are turned."""
+    rng = np.random.default_rng(12)
+    lens = [int(x) for x in rng.integers(0, 300, 40)]
+    announce(f"append large blocks {dtype} {D} {block}")
+    parts = [[int(x) if y else 1 for x, y in zip(rng.integers(0, 450, 40), rng.random(40) < 0.5)] for _ in range(2)]
+    c = Cache8(rng, [n + a + b for n, a, b in zip(lens, *parts)], 3, D, block, block)
+    for i, add in enumerate(parts):
+        (k, k64), (v, v64) = _new(rng, add, 3, D, dtype)
+        for t, x in ((k, k64), (v, v64)):
+            t *= 2.0 ** (8 * i)
+            x *= 2.0 ** (8 * i)
+            at = tuple(rng.integers(0, n, 30) for n in x.shape)
+            bad = rng.choice([np.inf, -np.inf, np.nan], 30)
+            x[at] = bad
+            t[tuple(torch.as_tensor(j).to(DEV) for j in at)] = torch.as_tensor(x[at], dtype=t.dtype).to(DEV)
+        F.focus_paged_append(k, v, c.dev, i32(lens), i32(_offsets(add)))
+        _check(c, k64, v64, lens, _offsets(add), f"part {i}")
+        lens = [n + a for n, a in zip(lens, add)]
+    assert c.dev.length.tolist() == lens
 
 
 def test_append_nothing():
