@@ -119,6 +119,39 @@ def test_attend_chunk_of_more_pages_than_held():
     _check(c, q64, [3], F.focus_paged_attend(q, c.dev, _offsets([3]), max_rows=3, split_keys=128 * 80), "bf16")
 
 
+def test_attend_a_long_sequence_beside_a_short_one():
+    rng = np.random.default_rng(38)
+    c = Cache8(rng, [262_144, 3], 1, 64, 128, 64)
+    q, q64 = values(rng, (5, 4, 64), "bf16")
+    announce("attend 262144 rows")
+    _check(c, q64, [3, 2], F.focus_paged_attend(q, c.dev, _offsets([3, 2]), max_rows=3), "bf16")
+
+
+def test_attend_and_append_in_a_pool_past_32_bits():
+    """Pages at the end of pools of 4.6 GB give the bits that they give in a small one."""
+    page, K, D, block, pages = 64, 8, 128, 16, 70_000
+    rng = np.random.default_rng(39)
+    lens = [500, 64, 1]
+    (k, _), (v, _), (q, _) = (values(rng, (sum(lens), n, D), "bf16") for n in (K, K, 4 * K))
+    cu = _offsets(lens)
+    got = []
+    announce("attend and append past 32 bits")
+    for total in (16, pages):
+        pools = [torch.empty(total, page, K, D, dtype=torch.uint8, device=DEV) for _ in range(2)]
+        for x in pools:
+            x[-16:] = 0x7f
+        scales = [torch.full((total, K, page // block), float("nan"), device=DEV) for _ in range(2)]
+        table = torch.full((3, 8), -1, dtype=torch.int32, device=DEV)
+        table[0], table[1, 0], table[2, 0] = torch.arange(total - 8, total, device=DEV), total - 9, total - 16
+        c = F.PagedCache8(*(x.view(torch.float8_e4m3fn) for x in pools), *scales, table, i32([0, 0, 0]))
+        F.focus_paged_append(k, v, c, i32([0, 0, 0]), cu)
+        o, lse = F.focus_paged_attend(q[:5], c, _offsets([2, 2, 1]), max_rows=2)
+        got.append([o, lse, c.length] + [x[-16:].clone() for x in (*pools, *(y.view(torch.int32) for y in scales))])
+    assert pools[0].numel() > 2 ** 32 and torch.isfinite(got[0][0].float()).all()
+    for x, y in zip(*got):
+        assert torch.equal(x, y)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_attend_strided_queries_scale_and_outputs(dtype):
     rng = np.random.default_rng(33)
