@@ -101,6 +101,29 @@ def test_attend_chunks_chosen(batch, top, H, K, dim, dtype, new):
     _check(c, q64, counts, got, dtype)
 
 
+@pytest.mark.parametrize("batch,top,H,K,dim,dtype,new,split", [
+    (140, 600, 4, 4, 64, "bf16", 2, 128),
+    (140, 700, 2, 1, 128, "f32", 1, 256),
+    (150, 600, 40, 1, 128, "bf16", 2, 0),    # 80 columns
+    (150, 600, 40, 1, 64, "f32", 1, 128),
+    (129, 250, 66, 2, 64, "bf16", 1, 0),     # 33 columns, tables that are not split
+    (400, 60, 24, 1, 128, "f32", 1, 0),
+    (128, 900, 6, 2, 64, "bf16", 3, 0),      # as many sequences as a wave holds
+])
+def test_attend_many_sequences(batch, top, H, K, dim, dtype, new, split):
+    announce(f"attend {batch} x {top} {H}/{K} x {dim} {dtype} new {new} split {split}")
+    rng = np.random.default_rng(batch + H)
+    lens = [0, top, 1, 0] + [int(x) for x in rng.integers(0, top + 1, batch - 5)] + [0]
+    counts = [int(x) for x in rng.integers(0, new + 1, batch)]
+    counts[1] = counts[-1] = new
+    c = Cache8(rng, lens, K, dim, 32, 8)
+    q, q64 = values(rng, (sum(counts), H, dim), dtype)
+    err = torch.zeros(1, dtype=torch.int32, device=DEV)
+    got = F.focus_paged_attend(q, c.dev, _offsets(counts), max_rows=new, split_keys=split, err=err)
+    _check(c, q64, counts, got, dtype)
+    assert err.item() == 0
+
+
 def test_attend_table_far_larger_than_the_lengths():
     rng = np.random.default_rng(31)
     lens = [0, 1, 700, 33]
