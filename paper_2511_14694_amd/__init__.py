@@ -43,7 +43,7 @@ from ._abi import (AdapterDesc, AdapterLayerDesc, AttnDesc, CompactDesc, DecodeD
                    FOCUS_ERR_CAPACITY, FOCUS_ERR_BOUNDS, FOCUS_ERR_PLAN,
                    FOCUS_FID_LOGITS, FOCUS_FID_PROBS, FOCUS_FID_N,
                    FOCUS_ROPE_NONE, FOCUS_ROPE_LINEAR, FOCUS_ROPE_BASE, FOCUS_ROPE_BANDS,
-                   FOCUS_ROPE_INTERLEAVED, FOCUS_ROPE_HALF, check, lib)
+                   FOCUS_ROPE_INTERLEAVED, FOCUS_ROPE_HALF, check, filler, lib)
 
 __all__ = ["focus_layout_plan", "focus_layout", "focus_compact_kv", "focus_window_attn",
            "focus_window_attn_workspace", "focus_decode_step", "focus_decode_workspace",
@@ -880,6 +880,9 @@ def focus_paged_evict(cache: PagedCache, out: PagedCache, budget, recent: int = 
     return keep
 
 
+_paged_extend, _paged_kv8, _paged_append, _paged_attend = map(filler, (PagedExtendDesc, PagedKv8, PagedAppendDesc, PagedAttendDesc))
+
+
 @dataclass
 class PagedRows:
     """The rows that focus_paged_extend found slots for: int32 tensors.
@@ -916,7 +919,8 @@ def focus_paged_extend(table, length, page_rows: int, add, free_pages, free_coun
     if out is None:
         # one allocation for all five (each by itself costs more than the views)
         n = n_rows if n_rows > 0 else 0
-        buf = _empty((2 * batch + 1 + 3 * n,), i32, length.device, stream)
+        size = 2 * batch + 1 + 3 * n
+        buf = length.new_empty(size, dtype=i32) if stream is None else _empty((size,), i32, length.device, stream)
         out = PagedRows(*buf.unsafe_split_with_sizes((batch, batch + 1, n, n, n)))
         at = buf.data_ptr()
         cu = at + 4 * batch
@@ -925,11 +929,11 @@ def focus_paged_extend(table, length, page_rows: int, add, free_pages, free_coun
     else:
         at, cu = _need(out.start, i32, one, dev, "out.start"), _need(out.cu_rows, i32, (batch + 1,), dev, "out.cu_rows")
         seq, slot, pos = (_need(x, i32, (n_rows,), dev, "out's maps") for x in (out.row_seq, out.row_slot, out.row_pos))
-    d = PagedExtendDesc(page_rows, batch, max_pages, _i32(free_pages.numel(), "free_pages' size"), _need(table, i32, None, dev, "table"),
-                        _need(length, i32, one, dev, "length"), _need(add, i32, one, dev, "add"),
-                        _need(free_pages, i32, None, dev, "free_pages"), _need(free_count, i32, (1,), dev, "free_count"),
-                        None if first_pos is None else _need(first_pos, i32, one, dev, "first_pos"), at, cu, n_rows, seq,
-                        slot, pos, None if err is None else _err_ptr(err, dev))
+    d = _paged_extend(page_rows, batch, max_pages, _i32(free_pages.numel(), "free_pages' size"), _need(table, i32, None, dev, "table"),
+                      _need(length, i32, one, dev, "length"), _need(add, i32, one, dev, "add"),
+                      _need(free_pages, i32, None, dev, "free_pages"), _need(free_count, i32, (1,), dev, "free_count"),
+                      0 if first_pos is None else _need(first_pos, i32, one, dev, "first_pos"), at, cu, n_rows, seq,
+                      slot, pos, 0 if err is None else _err_ptr(err, dev))
     _launch("focus_paged_extend", d, dev, stream)
     return out
 
@@ -952,6 +956,10 @@ class PagedCache8:
     length: torch.Tensor
 
     def desc(self) -> PagedKv8:
+        return _paged_kv8(*self.fields())
+
+    def fields(self):
+        """The description's values in their order, checked."""
         k, v, table, scale = self.k, self.v, self.table, self.k_scale
         shape, strides, dev, e4m3 = k.shape, k.stride(), k.get_device(), torch.float8_e4m3fn
         if (len(shape) != 4 or v.shape != shape or k.dtype is not e4m3 or v.dtype is not e4m3
@@ -979,9 +987,8 @@ class PagedCache8:
             _need(length, i32, (batch,), dev, "length")
             _need(scale, f32, scales, dev, "k_scale")
             _need(v_scale, f32, scales, dev, "v_scale")
-        return PagedKv8(PagedKv(FOCUS_E4M3, heads, dim, rows, n_pages, k.data_ptr(), v.data_ptr(), strides[0], strides[1],
-                                strides[2], batch, max_pages, table.data_ptr(), length.data_ptr(), None, 0), rows // blocks,
-                        0, scale.data_ptr(), v_scale.data_ptr())
+        return (FOCUS_E4M3, heads, dim, rows, n_pages, k.data_ptr(), v.data_ptr(), strides[0], strides[1], strides[2], batch,
+                max_pages, table.data_ptr(), length.data_ptr(), 0, 0, rows // blocks, 0, scale.data_ptr(), v_scale.data_ptr())
 
 
 def focus_paged_append(k, v, cache: PagedCache8, start, cu_rows=None, err=None, stream=None):
@@ -991,32 +998,32 @@ def focus_paged_append(k, v, cache: PagedCache8, start, cu_rows=None, err=None, 
     start (negative: not stored) and cu_rows int32, as focus_paged_extend gives them; start may
     not be cache.length itself.  A block's scale is the least power of two that its new
     rows fit, or its old one if that is greater and rows are left in it."""
-    c = cache.desc()
-    dev, dtype, kv = cache.k.get_device(), k.dtype, c.kv
+    c = cache.fields()
+    dev, dtype, batch = cache.k.get_device(), k.dtype, c[10]
     if k.dim() != 3 or dtype not in _DTYPES:
         raise ValueError("k must be [rows, heads, D], bfloat16 or float32")
-    shape = (k.shape[0], kv.n_kv_heads, kv.head_dim)
-    d = PagedAppendDesc(c, _DTYPES[dtype], 0, shape[0],
-                        None if cu_rows is None else _need(cu_rows, torch.int32, (kv.batch + 1,), dev, "cu_rows"),
-                        _need(start, torch.int32, (kv.batch,), dev, "start"), *_rows(k, shape, dtype, dev, "k"),
-                        *_rows(v, shape, dtype, dev, "v"), None if err is None else _err_ptr(err, dev))
+    shape = (k.shape[0], c[1], c[2])
+    d = _paged_append(*c, _DTYPES[dtype], 0, shape[0],
+                      0 if cu_rows is None else _need(cu_rows, torch.int32, (batch + 1,), dev, "cu_rows"),
+                      _need(start, torch.int32, (batch,), dev, "start"), *_rows(k, shape, dtype, dev, "k"),
+                      *_rows(v, shape, dtype, dev, "v"), 0 if err is None else _err_ptr(err, dev))
     _launch("focus_paged_append", d, dev, stream)
 
 
 def _paged_attend_desc(q, cache, cu_rows, max_rows, o, lse, split_keys, softmax_scale, err):
     """The descriptor without a workspace; o and lse addresses."""
-    c = cache.desc()
-    kv, dev, dtype, shape = c.kv, q.get_device(), q.dtype, q.shape
-    if len(shape) != 3 or shape[2] != kv.head_dim or dev != cache.k.get_device() or dtype not in _DTYPES:
+    c = cache.fields()
+    dev, dtype, shape = q.get_device(), q.dtype, q.shape
+    if len(shape) != 3 or shape[2] != c[2] or dev != cache.k.get_device() or dtype not in _DTYPES:
         raise ValueError("q must be [rows, heads, D], bfloat16 or float32, of the cache's head_dim and device")
-    return PagedAttendDesc(c, _DTYPES[dtype], shape[1], _i32(max_rows, "max_rows"), _i32(split_keys, "split_keys"),
-                           float(softmax_scale), 0, shape[0],
-                           None if cu_rows is None else _need(cu_rows, torch.int32, (kv.batch + 1,), dev, "cu_rows"),
-                           *_rows(q, shape, dtype, dev, "q"), o, lse, None, 0, None if err is None else _err_ptr(err, dev))
+    return _paged_attend(*c, _DTYPES[dtype], shape[1], _i32(max_rows, "max_rows"), _i32(split_keys, "split_keys"),
+                         float(softmax_scale), 0, shape[0],
+                         0 if cu_rows is None else _need(cu_rows, torch.int32, (c[10] + 1,), dev, "cu_rows"),
+                         *_rows(q, shape, dtype, dev, "q"), o, lse, 0, 0, 0 if err is None else _err_ptr(err, dev))
 
 
 def focus_paged_attend_workspace(q, cache: PagedCache8, cu_rows=None, max_rows: int = 1, split_keys: int = 0) -> int:
-    d = _paged_attend_desc(q, cache, cu_rows, max_rows, None, None, split_keys, 0.0, None)
+    d = _paged_attend_desc(q, cache, cu_rows, max_rows, 0, 0, split_keys, 0.0, None)
     return _query("focus_paged_attend_workspace", d, q.get_device())
 
 
@@ -1034,12 +1041,12 @@ def focus_paged_attend(q, cache: PagedCache8, cu_rows=None, max_rows: int = 1, o
         o_at = o.data_ptr()
     else:
         o_at = _need(o, q.dtype, q.shape, dev, "o")
-    lse_at = None
+    lse_at = 0
     if lse is not None:
         lse_at = _need(lse, torch.float32, q.shape[:2], dev, "lse")
     elif want_lse:
-        lse = q.new_empty(q.shape[:2], dtype=torch.float32) if stream is None else \
-            _empty(q.shape[:2], torch.float32, q.device, stream)
+        rows, heads = q.shape[:2]
+        lse = q.new_empty(rows, heads, dtype=torch.float32) if stream is None else _empty((rows, heads), torch.float32, q.device, stream)
         lse_at = lse.data_ptr()
     d = _paged_attend_desc(q, cache, cu_rows, max_rows, o_at, lse_at, split_keys, softmax_scale, err)
     if workspace is not None:

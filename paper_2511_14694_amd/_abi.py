@@ -4,6 +4,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libfocus.so")
 
@@ -177,6 +178,24 @@ class PagedAttendDesc(C.Structure):
 STRUCTS = [LayoutTotals, LayoutDesc, CompactDesc, AttnDesc, DecodeDesc, FidelityDesc, GemmDesc, AdapterDesc,
            AdapterLayerDesc, QkvDesc, DecodeSched, RopeScaling, PagedKv, RopeDesc, PagedDecodeDesc, PagedEvictDesc,
            PagedExtendDesc, PagedKv8, PagedAppendDesc, PagedAttendDesc]
+
+_CODES = {i32: "i", i64: "q", f32: "f", p: "P", sz: "N"}
+
+
+def _codes(t):
+    return "".join(_codes(f) if issubclass(f, C.Structure) else _CODES[f] for _, f in t._fields_)
+
+
+def filler(desc):
+    """A function that makes a desc of its fields' values by position, those of a nested
+    structure in its place, 0 for a null pointer.  (A third of the time that constructors
+    take, field by field: 0.8 us for the 38 of PagedAttendDesc.)"""
+    fields = struct.Struct("@" + _codes(desc))
+    if fields.size != C.sizeof(desc):
+        raise ImportError(f"{desc.__name__} is not laid out as its fields in turn")
+    pack, make = fields.pack, desc.from_buffer_copy
+    return lambda *values: make(pack(*values))
+
 
 # name -> (restype, argtypes): every symbol include/focus.h declares
 SYMBOLS = {
