@@ -1011,7 +1011,7 @@ def focus_paged_append(k, v, cache: PagedCache8, start, cu_rows=None, err=None, 
 
 
 def _paged_attend_desc(q, cache, cu_rows, max_rows, o, lse, split_keys, softmax_scale, err):
-    """The descriptor without a workspace; o and lse addresses."""
+    """The descriptor without a workspace, and the rows of a table; o and lse addresses."""
     c = cache.fields()
     dev, dtype, shape = q.get_device(), q.dtype, q.shape
     if len(shape) != 3 or shape[2] != c[2] or dev != cache.k.get_device() or dtype not in _DTYPES:
@@ -1019,11 +1019,11 @@ def _paged_attend_desc(q, cache, cu_rows, max_rows, o, lse, split_keys, softmax_
     return _paged_attend(*c, _DTYPES[dtype], shape[1], _i32(max_rows, "max_rows"), _i32(split_keys, "split_keys"),
                          float(softmax_scale), 0, shape[0],
                          0 if cu_rows is None else _need(cu_rows, torch.int32, (c[10] + 1,), dev, "cu_rows"),
-                         *_rows(q, shape, dtype, dev, "q"), o, lse, 0, 0, 0 if err is None else _err_ptr(err, dev))
+                         *_rows(q, shape, dtype, dev, "q"), o, lse, 0, 0, 0 if err is None else _err_ptr(err, dev)), c[3] * c[11]
 
 
 def focus_paged_attend_workspace(q, cache: PagedCache8, cu_rows=None, max_rows: int = 1, split_keys: int = 0) -> int:
-    d = _paged_attend_desc(q, cache, cu_rows, max_rows, 0, 0, split_keys, 0.0, None)
+    d, _ = _paged_attend_desc(q, cache, cu_rows, max_rows, 0, 0, split_keys, 0.0, None)
     return _query("focus_paged_attend_workspace", d, q.get_device())
 
 
@@ -1048,13 +1048,12 @@ def focus_paged_attend(q, cache: PagedCache8, cu_rows=None, max_rows: int = 1, o
         rows, heads = q.shape[:2]
         lse = q.new_empty(rows, heads, dtype=torch.float32) if stream is None else _empty((rows, heads), torch.float32, q.device, stream)
         lse_at = lse.data_ptr()
-    d = _paged_attend_desc(q, cache, cu_rows, max_rows, o_at, lse_at, split_keys, softmax_scale, err)
+    d, table_rows = _paged_attend_desc(q, cache, cu_rows, max_rows, o_at, lse_at, split_keys, softmax_scale, err)
     if workspace is not None:
         d.workspace, d.workspace_bytes = _workspace(workspace, dev)
     # a call that needs a workspace says so before anything is enqueued: those of short tables,
     # which need none, are spared the question
-    elif (d.cache.kv.max_pages * d.cache.kv.page_rows <= 512
-          and _launch("focus_paged_attend", d, dev, stream, FOCUS_E_WORKSPACE) == 0):
+    elif table_rows <= 512 and _launch("focus_paged_attend", d, dev, stream, FOCUS_E_WORKSPACE) == 0:
         return o, lse
     else:
         n = _query("focus_paged_attend_workspace", d, dev)
