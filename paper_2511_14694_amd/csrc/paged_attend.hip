@@ -656,12 +656,12 @@ __global__ __launch_bounds__(kThreads, resident(D, TILES, HEADS)) void attend_ro
 // them over the shares; the first partials are in flight while the maxima and sums are merged,
 // by every wave for itself.
 //
-// (A wave has 16 shares of 128 elements in flight.  WIDE from 8 / 16 / 32 times as many shares as
-// sequences: 17 sequences of up to 242 695 rows of one KV head 37.7 / 37.9 / 53.5 us, up to five
-// tokens of 32 sequences 66.4 / 52.1 / 52.6; 16 also costs, seven sequences of up to 12 398 rows
-// of 16 float32 heads of 64 49.6 and by waves 44.6.  Few shares are not worth the workgroups: three
-// sequences of up to 2 021 rows 15.6 so, 14.7 by waves.)
-constexpr int kJoin = 256, kManyShares = 16, kWideFrom = 128;
+// (A wave has 16 shares of 128 elements in flight.  WIDE for few columns, two to a compute unit,
+// of many shares each: by waves and so one sequence of 100 000 rows, four columns of 512 shares, 47
+// and 22 us; 16 of up to 7 629 rows, 512 of 16 or fewer, 25.5 and 23.8, but 32 of up to 30 517, 2 048
+// of 8, 34.3 and 37.5; eight tokens of 16 of 8 000 rows, 4 096 of 16, 9.3 and 33.6 in the join alone.  Few shares are not
+// worth the workgroups: three sequences of up to 2 021 rows, 60 shares, 14.7 and 15.6.)
+constexpr int kJoin = 256, kManyShares = 16, kWideFrom = 128, kFewColumns = 512;
 template <typename T, int D, bool WIDE>
 __global__ __launch_bounds__(kJoin) void attend_join(Args a) {
   constexpr int kFlight = 8, kThreadsOf = WIDE ? kJoin : 64, kSlices = WIDE ? D / 32 : 1;
@@ -792,7 +792,7 @@ focus_status launch(Args a, const Plan& p, hipStream_t s) {
   else of_heads(kOne, std::false_type{});
   const focus_status st = focus::launch_status();
   if (st != FOCUS_OK || p.single) return st;
-  if (p.shares >= std::max<int64_t>((int64_t)kManyShares * c.batch, kWideFrom))
+  if (columns <= kFewColumns && p.shares >= std::max<int64_t>((int64_t)kManyShares * c.batch, kWideFrom))
     hipLaunchKernelGGL((attend_join<T, D, true>), dim3((uint32_t)(columns * (D / 32))), dim3(kJoin), 0, s, a);
   else
     hipLaunchKernelGGL((attend_join<T, D, false>), dim3((uint32_t)focus::ceil_div(columns, kJoin / 64)), dim3(kJoin), 0, s, a);

@@ -88,6 +88,7 @@ def test_attend_matches_oracle(lens, counts, H, K, D, page, block, dtype, by_hea
     (5, 4000, 34, 2, 64, "bf16", 1),         # groups of 17, two KV heads together
     (300, 90, 2, 1, 64, "bf16", 4),
     (3, 9000, 4, 4, 128, "bf16", 8),
+    (3, 9000, 32, 8, 128, "bf16", 8),        # 768 columns of many shares
 ])
 def test_attend_chunks_chosen(batch, top, H, K, dim, dtype, new):
     """Lengths from 0 to top in tables long enough to be split, 0 to `new` tokens."""
