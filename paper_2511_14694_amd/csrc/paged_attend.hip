@@ -103,16 +103,25 @@ Plan make_plan(const focus_paged_attend_desc* d) {
   // heads in tables of 16 rows 51 us with four, now 22)
   if (p.single) p.wide = std::max(heads <= 1024 ? 1 : p.wide, wide(p.cap <= kRows ? 4 : p.cap <= 2 * kRows ? 2 : 1));
   p.planned = !p.single && c.batch > focus::kWave;
+  // as many shares as run together, but no more than there may be units
+  auto shares = [&](int wide) {
+    return std::min(std::max<int64_t>(1, resident(c.head_dim, p.cols / 16, p.heads) * focus::device_cus() / (sets / wide * p.tiles)),
+                    c.batch * (std::max<int64_t>(1, focus::ceil_div(p.cap, kUnit / wide)) + kEnds));
+  };
+  // Neighbouring heads by one workgroup are read faster, but leave each head as many times more
+  // partials, of all columns: not where a share has few rows for its columns (the tables' rows:
+  // the lengths are not known here).  By 4 / 2 / 1 heads a workgroup: 16 sequences of 10 000 rows of 32
+  // heads 215 / 224 / 244 us, 20 columns of 32 of up to 16 384 rows 52.8 / 52.5 / 55.2, of two of up
+  // to 10 064 38.5 / 32.8 / 30.8; 240 shapes 32.9 / 31.9 / 32.4 in the geometric mean, by this rule 31.7.
+  if (!p.single && d->split_keys == 0)
+    while (p.wide > 1 && c.batch * p.cap < (p.wide == 4 ? 128 : 32) * per_head * shares(p.wide)) p.wide /= 2;
   p.groups = (int64_t)sets / p.wide * p.tiles;
   if (p.single) {
     p.unit = (int)std::max<int64_t>(p.cap, 1), p.shares = c.batch;
   } else if (d->split_keys > 0) {
     p.unit = d->split_keys, p.shares = c.batch * std::max<int64_t>(1, focus::ceil_div(p.cap, p.unit));
   } else {
-    p.unit = kUnit / p.wide;
-    // as many as run together, but no more than there may be units
-    p.shares = std::min(std::max<int64_t>(1, resident(c.head_dim, p.cols / 16, p.heads) * focus::device_cus() / p.groups),
-                        c.batch * (std::max<int64_t>(1, focus::ceil_div(p.cap, p.unit)) + kEnds));
+    p.unit = kUnit / p.wide, p.shares = shares(p.wide);
   }
   const int64_t partials = 2 * p.shares * p.columns;
   p.ends = focus::ceil_div(8 * (int64_t)c.batch, 16) * 16;

@@ -89,6 +89,10 @@ def test_attend_matches_oracle(lens, counts, H, K, D, page, block, dtype, by_hea
     (300, 90, 2, 1, 64, "bf16", 4),
     (3, 9000, 4, 4, 128, "bf16", 8),
     (3, 9000, 32, 8, 128, "bf16", 8),        # 768 columns of many shares
+    (16, 4096, 4, 4, 128, "bf16", 1),        # tables long enough for four heads a workgroup
+    (17, 4300, 8, 8, 64, "bf16", 1),
+    (20, 7000, 8, 4, 128, "f32", 1),
+    (17, 3000, 8, 8, 128, "bf16", 2),        # for two
 ])
 def test_attend_chunks_chosen(batch, top, H, K, dim, dtype, new):
     """Lengths from 0 to top in tables long enough to be split, 0 to `new` tokens."""
