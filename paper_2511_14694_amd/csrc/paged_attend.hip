@@ -26,7 +26,7 @@
 // for 13 %; one of 262 144 rows of 8 heads (0.54 GB) 94, 5.7 TB/s.  Where there is less the
 // latencies of the beginning (lengths, page table, first rows: 6 us) and the second launch
 // (5 us and the gap before it) count: 64 sequences of 1 to 8 192 rows of 8 heads (0.13 GB) 35;
-// up to five tokens of 32 sequences of up to 16 384 rows (0.15 GB, 20 columns) 48.  The first
+// up to five tokens of 32 sequences of up to 16 384 rows (0.15 GB, 20 columns) 45.  The first
 // form, in equal chunks of each sequence found by a search and 16 columns at a time, took 227,
 // 106, 44 and 69.
 #include "paged_split.h"
