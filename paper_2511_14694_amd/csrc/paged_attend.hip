@@ -670,6 +670,9 @@ __global__ __launch_bounds__(kThreads, resident(D, TILES, HEADS)) void attend_ro
 // and 22 us; 16 of up to 7 629 rows, 512 of 16 or fewer, 25.5 and 23.8, but 32 of up to 30 517, 2 048
 // of 8, 34.3 and 37.5; eight tokens of 16 of 8 000 rows, 4 096 of 16, 9.3 and 33.6 in the join alone.  Few shares are not
 // worth the workgroups: three sequences of up to 2 021 rows, 60 shares, 14.7 and 15.6.)
+//
+// The two add the partials in different orders, and which is taken follows from the batch and the
+// tables: a given split_keys, which fixes a sequence's bits, always takes the waves.
 constexpr int kJoin = 256, kManyShares = 16, kWideFrom = 128, kFewColumns = 512;
 template <typename T, int D, bool WIDE>
 __global__ __launch_bounds__(kJoin) void attend_join(Args a) {
@@ -801,7 +804,7 @@ focus_status launch(Args a, const Plan& p, hipStream_t s) {
   else of_heads(kOne, std::false_type{});
   const focus_status st = focus::launch_status();
   if (st != FOCUS_OK || p.single) return st;
-  if (columns <= kFewColumns && p.shares >= std::max<int64_t>((int64_t)kManyShares * c.batch, kWideFrom))
+  if (a.d.split_keys == 0 && columns <= kFewColumns && p.shares >= std::max<int64_t>((int64_t)kManyShares * c.batch, kWideFrom))
     hipLaunchKernelGGL((attend_join<T, D, true>), dim3((uint32_t)(columns * (D / 32))), dim3(kJoin), 0, s, a);
   else
     hipLaunchKernelGGL((attend_join<T, D, false>), dim3((uint32_t)focus::ceil_div(columns, kJoin / 64)), dim3(kJoin), 0, s, a);

@@ -319,3 +319,22 @@ def test_attend_pages_outside_the_pool_and_bad_offsets():
             mine |= set(range(r0, r1))
         for t in set(range(6)) - mine:
             assert (o[t] == 7).all() and (lse[t] == 7).all()
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_attend_split_keys_fix_a_sequences_bits(D, dtype):
+    """With a given split a sequence's result depends neither on the rest of the batch nor on
+    how wide its table is: 127 shares, in tables of 127 and 128 and with sixteen others."""
+    rng = np.random.default_rng(40)
+    c = Cache8(rng, [127 * 128] + [900, 40, 0, 128] * 4, 2, D, 64, 16, max_pages=256)
+    q, q64 = values(rng, (17, 32, D), dtype)
+    announce(f"attend given split {D} {dtype}")
+    o, lse = F.focus_paged_attend(q, c.dev, split_keys=128)
+    _check(c, q64, [1] * 17, (o, lse), dtype)
+    for n in (1, 2, 5, 17):
+        for width in (254, 256):
+            part = F.PagedCache8(c.dev.k, c.dev.v, c.dev.k_scale, c.dev.v_scale, c.dev.table[:n, :width].contiguous(),
+                                 c.dev.length[:n])
+            o1, l1 = F.focus_paged_attend(q[:n], part, split_keys=128)
+            assert torch.equal(o1, o[:n]) and torch.equal(l1, lse[:n]), (n, width)
