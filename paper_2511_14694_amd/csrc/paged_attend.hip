@@ -93,9 +93,12 @@ Plan make_plan(const focus_paged_attend_desc* d) {
   // came twice: 16 x 10 000 rows of 32 such heads 165 us, now 136.  With two tiles of columns
   // besides, the registers do not suffice.)
   const bool beside = c.head_stride < c.row_stride;
-  p.heads = c.head_dim == 64 && p.cols == 16 && beside && c.n_kv_heads % 2 == 0 ? 2 : 1;
+  const bool pairs = c.head_dim == 64 && beside && c.n_kv_heads % 2 == 0;
+  p.heads = pairs && p.cols == 16 ? 2 : 1;
   const int sets = c.n_kv_heads / p.heads;
-  auto wide = [&](int most) { return most >= 4 && sets % 4 == 0 ? 4 : most >= 2 && sets % 2 == 0 ? 2 : 1; };
+  // (a given split fixes which waves share a head's rows too, however many columns there are)
+  const int alike = d->split_keys > 0 && pairs ? c.n_kv_heads / 2 : sets;
+  auto wide = [&](int most) { return most >= 4 && alike % 4 == 0 ? 4 : most >= 2 && alike % 2 == 0 ? 2 : 1; };
   p.wide = wide(beside ? 4 : 1);
   const int64_t heads = (int64_t)c.batch * c.n_kv_heads * p.tiles;
   p.single = d->split_keys == 0 && (p.cap <= kWhole || (p.cap <= 2 * kWhole && heads >= 128));

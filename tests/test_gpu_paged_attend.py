@@ -338,3 +338,19 @@ def test_attend_split_keys_fix_a_sequences_bits(D, dtype):
                                  c.dev.length[:n])
             o1, l1 = F.focus_paged_attend(q[:n], part, split_keys=128)
             assert torch.equal(o1, o[:n]) and torch.equal(l1, lse[:n]), (n, width)
+
+
+@pytest.mark.parametrize("K", [1, 2, 4, 6, 8])
+@pytest.mark.parametrize("D,dtype,by_head", [(64, "bf16", False), (64, "bf16", True), (128, "bf16", False), (64, "f32", False),
+                                             (128, "f32", False)])
+def test_attend_split_keys_fix_bits_whatever_max_rows(K, D, dtype, by_head):
+    """Nor on how many tokens another sequence of the batch may have."""
+    rng = np.random.default_rng(42)
+    c = Cache8(rng, [1000, 300, 50], K, D, 32, 16, by_head=by_head)
+    q, q64 = values(rng, (3, 8 * K, D), dtype)
+    announce(f"attend given split, max_rows {K} x {D} {dtype} by_head {by_head}")
+    o, lse = F.focus_paged_attend(q, c.dev, split_keys=256)
+    _check(c, q64, [1] * 3, (o, lse), dtype)
+    for most in (2, 3, 5, 9, 33):
+        o1, l1 = F.focus_paged_attend(q, c.dev, i32([0, 1, 2, 3]), max_rows=most, split_keys=256)
+        assert torch.equal(o1, o) and torch.equal(l1, lse), most
