@@ -976,7 +976,8 @@ typedef struct {
 /* Errors: E_NULL, E_ARG, E_DTYPE, E_SHAPE (n_rows of 2^31, or not batch without cu_rows,
  * among others), E_UNSUPPORTED, E_HIP.  A block in a page outside the pool
  * (FOCUS_ERR_BOUNDS) and rows past max_pages * page_rows (FOCUS_ERR_CAPACITY) are not
- * stored; offsets outside [0, n_rows] are clipped to it (FOCUS_ERR_BOUNDS). */
+ * stored; offsets outside [0, n_rows] are clipped to it, and rows between offsets that
+ * descend may be left out (FOCUS_ERR_BOUNDS for both, wherever they are). */
 focus_status focus_paged_append(const focus_paged_append_desc* d, focus_stream_t stream);
 
 /* Attention of the newest tokens of every sequence over its cached rows: of sequence b the

@@ -288,3 +288,39 @@ def test_append_more_blocks_than_a_launch_has_waves():
     block0 = torch.as_tensor(block0).bfloat16().double().numpy()
     want, scale = O.append(np.zeros((block, D)), np.zeros(1), block, 0, block0)
     assert np.array_equal(to_codes(one.k)[pages - 1, :block, 0], want) and one.k_scale[pages - 1, 0, 0].item() == scale[0]
+
+
+@pytest.mark.parametrize("batch", [2, 40, 90, 300])
+@pytest.mark.parametrize("dtype,D,block", [("bf16", 64, 8), ("f32", 256, 128)])
+def test_append_reports_bad_offsets_wherever_they_are(batch, dtype, D, block):
+    """Offsets that leave the rows or descend, among others that do neither: reported, and
+    nothing written but the pages of the sequences' tables."""
+    rng = np.random.default_rng(batch)
+    K, page = 2, 128
+    add = [int(x) for x in rng.integers(1, 4, batch)]
+    n = sum(add)
+    fine = _offsets(add)
+    err = torch.zeros(1, dtype=torch.int32, device=DEV)
+    announce(f"append bad offsets {batch} {dtype} {D}")
+    cases = [(fine, False), (fine[:-1] + [n - 1], False)]
+    for at in sorted({1, batch // 2, batch - 1}):
+        for value in (n + 1, 2 ** 31 - 1, -1, -2 ** 31, fine[at + 1] + 1, fine[at - 1] - 1):
+            cases.append((fine[:at] + [value] + fine[at + 1:], True))
+    cases += [(fine[:-1] + [n + 1], True), ([-1] + fine[1:], True), ([fine[1] + 1] + fine[1:], True),
+              ([n] + [0] * (batch - 1) + [n], True), ([0] * batch + [-3], True)]
+    (k, _), (v, _) = _new(rng, add, K, D, dtype)
+    c = Cache8(rng, [page] * batch, K, D, page, block, spare=5)
+    outside = torch.as_tensor([p for p in range(c.dev.k.shape[0]) if p not in c.table]).to(DEV)
+    keep = [x.view(torch.uint8)[outside].clone() for x in (c.dev.k, c.dev.v, c.dev.k_scale, c.dev.v_scale)]
+    for cu, bad in cases:
+        err.zero_()
+        c.dev.length.zero_()
+        F.focus_paged_append(k, v, c.dev, i32([0] * batch), i32(cu), err=err)
+        # (a sequence may get more rows by them than its table's one page holds, which is said too)
+        most = max(min(y, n) - max(x, 0) for x, y in zip(cu, cu[1:]))
+        said = err.item() & ~(F.FOCUS_ERR_CAPACITY if most > page else 0)
+        assert said == (F.FOCUS_ERR_BOUNDS if bad else 0), cu[:8]
+        for x, y in zip((c.dev.k, c.dev.v, c.dev.k_scale, c.dev.v_scale), keep):
+            assert torch.equal(x.view(torch.uint8)[outside], y)
+        if not bad:
+            assert c.dev.length.tolist() == [y - x for x, y in zip(cu, cu[1:])]
