@@ -817,7 +817,8 @@ focus_status launch(Args a, const Plan& p, hipStream_t s) {
 }  // namespace
 
 extern "C" size_t focus_paged_attend_workspace(const focus_paged_attend_desc* d) {
-  if (!d || validate(d) != FOCUS_OK) return 0;
+  // (nothing to do, nothing to plan: with no sequences there may be any number of heads)
+  if (!d || validate(d) != FOCUS_OK || d->cache.kv.batch == 0 || d->n_rows == 0) return 0;
   return make_plan(d).bytes;
 }
 

@@ -149,6 +149,21 @@ def test_attend_workspace():
     assert query(None) == 0 and _abi.lib().focus_paged_attend(None, None) == E_NULL
 
 
+def test_attend_workspace_of_nothing():
+    """No sequences or no rows: none, for any sizes, as many workgroups as they would be."""
+    query = _abi.lib().focus_paged_attend_workspace
+    d = _attend_ok()
+    kv = d.cache.kv
+    kv.max_pages, d.n_rows = 5000, 0
+    assert query(C.byref(d)) == 0 and _call("focus_paged_attend", d) == 0
+    # as many tiles of columns times sets of heads as 32 bits count
+    kv.batch, kv.n_pages, kv.head_dim, kv.page_rows, kv.max_pages = 0, 1, 64, 16, 100
+    kv.page_stride, kv.row_stride, kv.head_stride, d.cache.scale_rows = 64, 64, 1024, 16
+    kv.n_kv_heads = d.n_heads = 1 << 29
+    d.dtype, d.max_rows, d.q_row, d.q_head = 1, 512, 64, 64
+    assert _call("focus_paged_attend", d) == 0 and query(C.byref(d)) == 0
+
+
 # ------------------------------------------------------------------- the binding
 
 def _cache(B=2, K=2, D=64, page=16, block=8, pages=4, width=3):
