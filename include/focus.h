@@ -1019,11 +1019,11 @@ typedef struct {
  * one on overlapping streams race. */
 size_t focus_paged_attend_workspace(const focus_paged_attend_desc* d);
 /* Errors: E_NULL, E_ARG, E_DTYPE, E_SHAPE (as focus_paged_decode; n_rows not batch without
- * cu_rows), E_UNSUPPORTED, E_WORKSPACE, E_HIP.  Rows of a page outside the pool are left
- * out of the softmax (FOCUS_ERR_BOUNDS); a length outside [0, max_pages * page_rows] is
- * clipped to it (FOCUS_ERR_CAPACITY); the rows of a sequence that has more than max_rows
- * (FOCUS_ERR_CAPACITY) or whose offsets do not ascend within [0, n_rows]
- * (FOCUS_ERR_BOUNDS) are left as they were. */
+ * cu_rows, or more workgroups than a launch holds), E_UNSUPPORTED, E_WORKSPACE, E_HIP.  Rows
+ * of a page outside the pool are left out of the softmax (FOCUS_ERR_BOUNDS); a length outside
+ * [0, max_pages * page_rows] is clipped to it (FOCUS_ERR_CAPACITY); the rows of a sequence
+ * that has more than max_rows (FOCUS_ERR_CAPACITY) or whose offsets do not ascend within
+ * [0, n_rows] (FOCUS_ERR_BOUNDS) are left as they were. */
 focus_status focus_paged_attend(const focus_paged_attend_desc* d, focus_stream_t stream);
 
 #ifdef __cplusplus

@@ -777,11 +777,20 @@ focus_status validate(const focus_paged_attend_desc* d) {
   return FOCUS_OK;
 }
 
+// The plan of a call that has something to do, if a launch holds its workgroups; of one that has
+// not, an empty one (with no sequences there may be any number of heads).
+focus_status checked_plan(const focus_paged_attend_desc* d, Plan& p) {
+  p = {};
+  const focus_status st = validate(d);
+  if (st != FOCUS_OK || d->cache.kv.batch == 0 || d->n_rows == 0) return st;
+  p = make_plan(d);
+  return p.groups * p.shares > INT32_MAX / kThreads - focus::kXcds * kMost ? FOCUS_E_SHAPE : FOCUS_OK;
+}
+
 template <typename T, int D>
 focus_status launch(Args a, const Plan& p, hipStream_t s) {
   const focus_paged_kv& c = a.d.cache.kv;
   const int64_t columns = (int64_t)c.batch * p.columns;
-  if (p.groups * p.shares > INT32_MAX / kThreads - focus::kXcds * kMost) return FOCUS_E_SHAPE;
   if (p.planned) {
     hipLaunchKernelGGL(attend_plan, dim3(1), dim3(kPlan), 0, s, a);
     const focus_status st = focus::launch_status();
@@ -817,22 +826,20 @@ focus_status launch(Args a, const Plan& p, hipStream_t s) {
 }  // namespace
 
 extern "C" size_t focus_paged_attend_workspace(const focus_paged_attend_desc* d) {
-  // (nothing to do, nothing to plan: with no sequences there may be any number of heads)
-  if (!d || validate(d) != FOCUS_OK || d->cache.kv.batch == 0 || d->n_rows == 0) return 0;
-  return make_plan(d).bytes;
+  Plan p;
+  return d && checked_plan(d, p) == FOCUS_OK ? p.bytes : 0;
 }
 
 extern "C" focus_status focus_paged_attend(const focus_paged_attend_desc* d, focus_stream_t stream) {
   if (!d) return FOCUS_E_NULL;
-  const focus_status st = validate(d);
-  if (st != FOCUS_OK) return st;
+  Plan p;
+  const focus_status st = checked_plan(d, p);
   const focus_paged_kv& c = d->cache.kv;
-  if (c.batch == 0 || d->n_rows == 0) return FOCUS_OK;
+  if (st != FOCUS_OK || c.batch == 0 || d->n_rows == 0) return st;
   if (!d->q || !d->o) return FOCUS_E_NULL;
   if (!focus::aligned16(d->q) || !focus::aligned16(d->o)) return FOCUS_E_ARG;
   for (const void* p : {(const void*)d->lse, (const void*)d->cu_rows, (const void*)d->err})
     if (reinterpret_cast<uintptr_t>(p) & 3u) return FOCUS_E_ARG;
-  const Plan p = make_plan(d);
   if (p.bytes > 0 && (!d->workspace || d->workspace_bytes < p.bytes)) return FOCUS_E_WORKSPACE;
   if (!focus::aligned16(d->workspace)) return FOCUS_E_ARG;
   char* ws = reinterpret_cast<char*>(d->workspace);

@@ -164,6 +164,32 @@ def test_attend_workspace_of_nothing():
     assert _call("focus_paged_attend", d) == 0 and query(C.byref(d)) == 0
 
 
+@pytest.mark.parametrize("dtype,dim,heads,by_head", [(0, 128, 8, True), (0, 64, 8, True), (1, 128, 8, True), (0, 128, 9, False),
+                                                      (0, 128, 40, False)])
+def test_attend_call_and_query_agree_on_the_most_workgroups(dtype, dim, heads, by_head):
+    """More workgroups than a launch holds: refused before a workspace is asked for, and the
+    query, which a caller allocates by, says 0."""
+    query = _abi.lib().focus_paged_attend_workspace
+    d = _attend_ok()
+    kv, page = d.cache.kv, 1024
+    d.dtype, d.max_rows, d.split_keys, d.n_rows = dtype, 4, 128, 1
+    kv.head_dim, kv.page_rows, kv.n_kv_heads, d.n_heads = dim, page, heads, heads
+    kv.row_stride, kv.head_stride = (dim, page * dim) if by_head else (heads * dim, dim)
+    kv.page_stride, d.q_row, d.q_head = page * heads * dim, heads * dim, dim
+    kv.max_pages = 256
+    seen = set()
+    for batch in range(100, 4000, 50):
+        kv.batch = batch
+        st, need = _call("focus_paged_attend", d), query(C.byref(d))
+        assert (st, need > 0) in ((E_WORKSPACE, True), (E_SHAPE, False)), batch
+        seen.add(st)
+        if st == E_SHAPE:
+            d.workspace, d.workspace_bytes = FAKE, 1 << 60
+            assert _call("focus_paged_attend", d) == E_SHAPE
+            d.workspace, d.workspace_bytes = None, 0
+    assert seen == {E_WORKSPACE, E_SHAPE}
+
+
 # ------------------------------------------------------------------- the binding
 
 def _cache(B=2, K=2, D=64, page=16, block=8, pages=4, width=3):
