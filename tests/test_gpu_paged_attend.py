@@ -354,3 +354,37 @@ def test_attend_split_keys_fix_bits_whatever_max_rows(K, D, dtype, by_head):
     for most in (2, 3, 5, 9, 33):
         o1, l1 = F.focus_paged_attend(q, c.dev, i32([0, 1, 2, 3]), max_rows=most, split_keys=256)
         assert torch.equal(o1, o) and torch.equal(l1, lse), most
+
+
+@pytest.mark.parametrize("H,K,D,dtype,by_head", [
+    (12, 2, 128, "bf16", False),     # two tiles of columns
+    (10, 2, 64, "bf16", False),
+    (12, 2, 64, "bf16", True),
+    (80, 4, 128, "bf16", False),     # tiles of several workgroups
+    (34, 2, 64, "bf16", False),
+    (4, 2, 64, "bf16", False),       # two heads a wave
+    (4, 2, 64, "f32", False),        # queries in three parts
+    (3, 3, 128, "f32", False),
+    (40, 2, 128, "f32", False),
+    (40, 2, 64, "f32", False),
+])
+@pytest.mark.parametrize("split", [0, 128])
+def test_attend_nan_only_where_it_is_seen_by_every_form(H, K, D, dtype, by_head, split):
+    """NaN in the last rows' k and v: which elements of which tokens and heads become NaN is
+    the oracle's, all others hold their tolerances."""
+    rng = np.random.default_rng(H + K + D)
+    announce(f"attend NaN {H}/{K} x {D} {dtype} by_head {by_head} split {split}")
+    for lens in ([40, 31, 4], [300, 7, 1027]):
+        c = Cache8(rng, lens, K, D, 16, 8, by_head=by_head)
+        for b, n in enumerate(lens):
+            for row, which, g, e in ((n - 1, "v", 0, [3, D - 1]), (n - 2, "v", K - 1, [D // 2, D // 2 + 7, 0]),
+                                     (n - 3, "v", 0, [17]), (n - 1, "k", K - 1, [5])):
+                p, r = c.table[b][row // 16], row % 16
+                for x in e:
+                    getattr(c.dev, which).view(torch.uint8)[p, r, g, x] = NAN if x % 2 else 0xff
+        c.refresh()
+        q, q64 = values(rng, (12, H, D), dtype)
+        got = F.focus_paged_attend(q, c.dev, i32([0, 4, 8, 12]), max_rows=4, split_keys=split)
+        bad = np.isnan(to64(got[0]))
+        assert bad.any() and not bad[::4].any() and not bad.all(2).all()
+        _check(c, q64, [4, 4, 4], got, dtype)
