@@ -990,7 +990,9 @@ focus_status focus_paged_append(const focus_paged_append_desc* d, focus_stream_t
  * o and lse past the last sequence's are left as they were.  o and lse may have nothing in
  * common with an input.  Scores, weights and sums are float32; each element of k and v enters
  * exactly.  A block's scale is applied to the sum of its row's products, which has to be a
- * float32 number without it: |q| up to 2^111 whatever the rows hold.
+ * float32 number without it: |q| up to 2^111 whatever the rows hold.  Values may be any that
+ * float32 has; a weight times v's scale is held to 2^-132 times the rows of a table or to its
+ * 17 bits (float32 q: 24), whichever is coarser.
  * The rows of a sequence are split over several workgroups, joined by log-sum-exp;
  * with split_keys = 0 the split follows the lengths of the whole batch, so that a
  * sequence's bits may differ by float32 rounding with what else is in the batch; a

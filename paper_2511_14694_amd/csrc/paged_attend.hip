@@ -137,6 +137,7 @@ Plan make_plan(const focus_paged_attend_desc* d) {
 struct Args {
   focus_paged_attend_desc d;
   float sc;             // softmax scale in log2 units
+  float less, more;     // what weights are multiplied by; its inverse, what sums are
   int shift, scale_shift;  // log2 page_rows, scale_rows
   int tiles, wide_shift;
   int units;            // workgroups of a share, tiles aside
@@ -361,6 +362,11 @@ __global__ __launch_bounds__(kThreads, resident(D, TILES, HEADS)) void attend_ro
   const int k8 = col / 4 * 8, k_in = col % 4, v8 = x * 8;
   const bool reports = g0 == 0 && tile_id == 0;
 
+  // (a vector register: the scalar ones are all taken, and with this one more in a lane of a spilled
+  // one two tiles of columns were 1.5 to 2 % slower)
+  float less = a.less;
+  asm("" : "+v"(less));
+
   Walk walk(a, share);
   const int from = share * walk.share, upto = from + walk.share;
   for (; walk.b < c.batch && walk.begin < upto; walk.next(a)) {
@@ -484,6 +490,7 @@ __global__ __launch_bounds__(kThreads, resident(D, TILES, HEADS)) void attend_ro
               for (int i = 0; i < L::kWords; ++i) bad |= nan_bytes(w.word(h, j, i));
             }
           }
+          const float vs = w.vs[h] * less;
           float y[TILES][8];
 #pragma unroll
           for (int tile = 0; tile < TILES; ++tile) {
@@ -520,7 +527,7 @@ __global__ __launch_bounds__(kThreads, resident(D, TILES, HEADS)) void attend_ro
             for (int j = 0; j < 8; ++j) {
               y[tile][j] = __builtin_amdgcn_exp2f((y[tile][j] - m[at0 + tile]) * a.sc);
               l[at0 + tile] += y[tile][j];
-              y[tile][j] *= w.vs[h];
+              y[tile][j] *= vs;
             }
             if (tail) {  // (of rows that do not count the scale may be anything)
 #pragma unroll
@@ -648,7 +655,7 @@ __global__ __launch_bounds__(kThreads, resident(D, TILES, HEADS)) void attend_ro
       if (chunks == 1) {
         const int i = at_col / G;
         const int64_t at = (tok.first + i) * H + kv * G + (at_col - i * G);
-        y = ml.y == 0.f ? f32x4{0.f, 0.f, 0.f, 0.f} : y * (1.f / ml.y);
+        y = ml.y == 0.f ? f32x4{0.f, 0.f, 0.f, 0.f} : y * (a.more / ml.y);
         T* to = reinterpret_cast<T*>(a.d.o) + at * D + e;
         if constexpr (sizeof(T) == 2)
           *reinterpret_cast<u32x2*>(to) = u32x2{focus::pack_bf16x2(y[0], y[1]), focus::pack_bf16x2(y[2], y[3])};
@@ -744,7 +751,7 @@ __global__ __launch_bounds__(kJoin) void attend_join(Args a) {
       sum.x += __shfl_xor(sum.x, k), sum.y += __shfl_xor(sum.y, k), sum.z += __shfl_xor(sum.z, k), sum.w += __shfl_xor(sum.w, k);
     if (tid >= kLanes) return;
   }
-  const float inv = S == 0.f ? 0.f : 1.f / S;  // (the sum is zero too)
+  const float inv = S == 0.f ? 0.f : a.more / S;  // (the sum is zero too)
   const int i = cc / G;
   const int64_t at = (tok.first + i) * a.d.n_heads + g * G + (cc - i * G);
   T* to = reinterpret_cast<T*>(a.d.o) + at * D + 4 * e;
@@ -858,6 +865,12 @@ extern "C" focus_status focus_paged_attend(const focus_paged_attend_desc* d, foc
   if (p.planned) a.ends = reinterpret_cast<int*>(ws + p.ends);
   const float scale = d->softmax_scale > 0.f ? d->softmax_scale : 1.0f / sqrtf((float)c.head_dim);
   a.sc = scale * focus::kLog2e;
+  // Where the mean of values is a float32 number, their sum need not be one: weights are multiplied
+  // by a power of two below half of one over a table's rows, which is exact, and the mean by its inverse.
+  // (What it costs is at the other end: a weight times its scale has the least step of bf16, 2^-133,
+  // times that inverse.)
+  const int bits = 33 - __builtin_clz((unsigned)std::max<int64_t>(p.cap, 1));
+  a.less = ldexpf(1.f, -bits), a.more = ldexpf(1.f, bits);
   hipStream_t on = reinterpret_cast<hipStream_t>(stream);
   if (d->dtype == FOCUS_BF16) return c.head_dim == 128 ? launch<__bf16, 128>(a, p, on) : launch<__bf16, 64>(a, p, on);
   return c.head_dim == 128 ? launch<float, 128>(a, p, on) : launch<float, 64>(a, p, on);

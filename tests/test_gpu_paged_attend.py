@@ -388,3 +388,89 @@ def test_attend_nan_only_where_it_is_seen_by_every_form(H, K, D, dtype, by_head,
         bad = np.isnan(to64(got[0]))
         assert bad.any() and not bad[::4].any() and not bad.all(2).all()
         _check(c, q64, [4, 4, 4], got, dtype)
+
+
+@pytest.mark.parametrize("H,K,D,dtype", [(4, 2, 64, "bf16"), (12, 2, 128, "bf16"), (4, 2, 64, "f32"), (3, 3, 128, "f32")])
+@pytest.mark.parametrize("split", [0, 128])
+def test_attend_values_over_the_whole_of_float32(H, K, D, dtype, split):
+    """Values from the greatest numbers to the smallest: their weighted mean is a number that
+    float32 has, whatever the sums of the weights are.  Compared with the scale taken off.
+
+    For the least scales: a weight times the scale and a power of two, more than a quarter of one
+    over the table's rows, enters in bf16 parts, whose least step is 2^-133: off by 2^-134, so o by
+    that times 4 rows, 448 n and one over the weights' sum; an output below 2^-126 is rounded
+    by half of 2^-133, or 2^-149, more."""
+    announce(f"attend values {H}/{K} x {D} {dtype} split {split}")
+    for p in (119, 118, 100, 64, 33, 32, 31, -31, -32, -33, -64, -90, -100, -110, -117, -126):
+        rng = np.random.default_rng(41)
+        c = Cache8(rng, [1500, 40, 3], K, D, 16, 8)
+        c.dev.v_scale.fill_(2.0 ** p)
+        if p == 119:
+            c.dev.v.view(torch.uint8)[:] = c.dev.v.view(torch.uint8) & 0x7f       # all of one sign
+        c.refresh()
+        c.vs = np.ones_like(c.vs)
+        q, q64 = values(rng, (5, H, D), dtype, 0.1)
+        o, lse = F.focus_paged_attend(q, c.dev, i32([0, 2, 4, 5]), max_rows=2, split_keys=split)
+        sc, at = D ** -0.5, 0
+        for b, (n, m) in enumerate(zip(c.lens, (2, 2, 1))):
+            k, v = c.rows(b, n, "k"), c.rows(b, n, "v")
+            ro, rl = O.attend(q64[at:at + m], k, v, sc)
+            to, tl = O.attend_tolerances(q64[at:at + m], k, v, sc, dtype, ro)
+            least = 0.0
+            if p < -80:
+                group = H // K
+                top = sc * np.stack([(q64[at:at + m, h] @ k[:, h // group].T).max(1) for h in range(H)], 1)
+                least = 2.0 ** ((-134 if dtype == "bf16" else -150) - p)
+                least = least + 2.0 ** (-134 - p) * 4 * c.max_pages * 16 * 448 * n / np.exp(rl - top)[..., None]
+            within(to64(o)[at:at + m] * 2.0 ** -p, ro, to + least, f"2^{p} o[{b}]")
+            within(to64(lse)[at:at + m], rl, tl, f"2^{p} lse[{b}]")
+            at += m
+
+
+@pytest.mark.parametrize("D,dtype", [(64, "bf16"), (128, "bf16"), (64, "f32"), (128, "f32")])
+@pytest.mark.parametrize("split", [0, 128])
+def test_attend_values_that_grow_along_a_sequence(D, dtype, split):
+    """Blocks of ever greater scales, over all that there are and over parts; of the greatest
+    several, whose sum float32 does not have; and the same from the end on."""
+    announce(f"attend growing values {D} {dtype} split {split}")
+    for n, lo, hi in ((1500, -126, 119), (1500, -40, -20), (1500, 20, 40), (1500, -10, 10), (250, -126, 119), (30, -70, 70)):
+        for back in (False, True):
+            rng = np.random.default_rng(abs(n + lo))
+            c = Cache8(rng, [n], 2, D, 16, 8)
+            e = np.sort(rng.integers(lo, hi + 1, -(-n // 8)))
+            e[-8:] = hi
+            e = e[::-1] if back else e
+            s = c.dev.v_scale
+            for j, x in enumerate(e):
+                s[int(c.table[0][j // 2]), :, j % 2] = 2.0 ** float(x)
+            c.dev.v.view(torch.uint8)[:] = c.dev.v.view(torch.uint8) & 0x7f
+            c.refresh()
+            q, q64 = values(rng, (2, 4, D), dtype, 0.1)
+            _check(c, q64, [2], F.focus_paged_attend(q, c.dev, i32([0, 2]), max_rows=2, split_keys=split), dtype)
+
+
+@pytest.mark.parametrize("H,K,D,dtype", [(4, 2, 64, "bf16"), (12, 2, 128, "bf16"), (34, 2, 64, "bf16"), (4, 2, 64, "f32"),
+                                         (3, 3, 128, "f32")])
+@pytest.mark.parametrize("split", [0, 128])
+def test_attend_great_values_reach_only_who_sees_them(H, K, D, dtype, split):
+    """A last block of the greatest values, in one KV head and one sequence of three: tokens and
+    heads that do not see it keep their bits, the others' outputs are theirs; NaN stay NaN."""
+    rng = np.random.default_rng(43)
+    announce(f"attend great values seen {H}/{K} x {D} {dtype} split {split}")
+    for lens in ([41, 5, 16], [1025, 700, 9]):
+        c = Cache8(rng, lens, K, D, 16, 8)
+        q, q64 = values(rng, (6, H, D), dtype, 0.1)
+        cu = i32([0, 2, 4, 6])
+        before = F.focus_paged_attend(q, c.dev, cu, max_rows=2, split_keys=split)
+        n = lens[0]
+        p = int(c.table[0][(n - 1) // 16])
+        c.dev.v_scale[p, K - 1, (n - 1) % 16 // 8] = 2.0 ** 119
+        c.refresh()
+        o, lse = F.focus_paged_attend(q, c.dev, cu, max_rows=2, split_keys=split)
+        _check(c, q64, [2, 2, 2], (o, lse), dtype)
+        same = torch.ones(6, H, dtype=torch.bool, device=DEV)
+        same[1, H - H // K:] = False
+        assert torch.equal(o[same], before[0][same]) and torch.equal(lse[same], before[1][same])
+        c.dev.v.view(torch.uint8)[p, (n - 1) % 16, K - 1, 7] = NAN
+        c.refresh()
+        _check(c, q64, [2, 2, 2], F.focus_paged_attend(q, c.dev, cu, max_rows=2, split_keys=split), dtype)
