@@ -29,7 +29,7 @@
 // up to five tokens of 32 sequences of up to 16 384 rows (0.15 GB, 20 columns) 45.  The first
 // form, in equal chunks of each sequence found by a search and 16 columns at a time, took 227,
 // 106, 44 and 69.
-#include "paged_split.h"
+#include "paged_softmax.h"
 
 #include <algorithm>
 #include <type_traits>

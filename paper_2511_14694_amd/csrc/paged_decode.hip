@@ -30,7 +30,7 @@
 // and the second launch count: 64 sequences of 1 to 8 192 rows of 8 heads (0.26 GB), with
 // weights, 71 us, of which 61 in paged_attend and 10 in paged_join.  The first form, one
 // workgroup a (sequence, head) on the vector units, took 2754, 62 241 and 2061.
-#include "paged_split.h"
+#include "paged_softmax.h"
 
 #include <algorithm>
 #include <type_traits>
@@ -39,21 +39,23 @@ namespace {
 
 using focus::bf16x8;
 using focus::f32x4;
-using focus::u32x4;
-using focus::Chunk;
-using focus::joined;
 using focus::kLog2e;
 using focus::kMinit;
 using focus::kWave;
 using focus::lse_of;
 using focus::max_column;
+using focus::scalar;
+using focus::u32x4;
+using focus::wave_max;
+using focus::wave_scan;
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kThreads = 256, kWaves = 4;
-constexpr int kMaxGrid = focus::kSplitGrid;
+constexpr int kMaxGrid = 32768; // workgroups in a grid's second and third dimension
 constexpr int kCols = 16;       // query heads of a workgroup: columns of a product
 constexpr int kPages = 1024;    // page offsets held in LDS at a time
 constexpr int kWhole = 256;     // rows of a table that is not split
+constexpr int kPlan = 1024;     // threads of paged_plan
 constexpr int kUnit = 128;      // rows of a chunk times KV heads of a workgroup: a multiple of this
 
 // What a lane reads in the place of eight rows that begin past their sequence's end or
@@ -126,22 +128,180 @@ Plan make_plan(const focus_paged_decode_desc* d) {
 
 struct Args {
   focus_paged_decode_desc d;
-  focus::Split split;
   float sc;             // softmax scale in log2 units
   int shift;            // log2 page_rows
-  int tiles, wide_shift;  // KV heads of a workgroup: 1 << wide_shift
+  int tiles, wide_shift, unit_shift, target;   // wide and unit are powers of two
   int units;            // workgroups of a chunk and 16 query heads each
   int group, parts;     // query heads of a KV head; workgroups of one in the second launch
+  int64_t cap;
+  bool single;
+  int64_t slots;
+  int4* info;
+  int* owner;           // sequence of each slot (-1: none); null unless planned
   float2* ml;
   float* o;
   float* score;
 };
 
-// Rows that a chunk's beginning and end cost (focus::Split::each); each query head's
-// partials more.
+// Rows of a chunk when they are to be chosen, for `target` chunks resident at a time: the
+// least estimate of the time among
+//   the rows of the whole batch spread over `target` chunks, rounded up to units, or over
+//   half or twice as many;
+//   the least size at which the chunks of all sequences are resident at once (up to kWave
+//   sequences; it needs 16 steps of a search);
+//   no split at all.
+// The estimate, in rows a resident workgroup streams while all of them do: what there is
+// to read, and for each chunk kStart rows' worth of beginning and end and its partials
+// written and read, over the target; where not all are resident at once kLate of the
+// longest more, which may begin late; at least the longest at kAlone times the rate, as
+// fast as one gets when the others have ended.  us, before twice as many were tried (kStart
+// 100, all of the longest more) / now: 64 sequences of 4096 rows, 5 KV heads, 152 / 120; 48
+// with 7 heads 152 / 121; 16 of 10 000, 32 heads, 417 / 409; 200 of 1000 to 2000, 8 heads,
+// 272 / 246; 400 of 600 to 1200, 4 heads, 165 / 184; over 104 such batches 0.8 % less.
 constexpr int kStart = 72;
+constexpr float kLate = 0.3f, kAlone = 1.1f;
 
-__global__ __launch_bounds__(focus::kPlan) void paged_plan(Args a) { focus::plan_chunks(a.split, a.d.cache); }
+__device__ inline float estimate(const Args& a, uint32_t units, int chunks, int rows, int longest) {
+  const float each = (float)(kStart >> a.wide_shift) + (a.d.cache.dtype == FOCUS_BF16 ? 4.f : 2.f) * a.group;
+  const float even = ((float)units * (1 << a.unit_shift) + each * (float)chunks) / (float)a.target;
+  const float last = (float)min(rows, longest);
+  return fmaxf(chunks > a.target ? even + kLate * last : even, last / kAlone);
+}
+
+// Sum and maximum of f(rows) over the sequences: of a wave, two sequences a lane, or of
+// paged_plan's workgroup.  The results are the same in all threads.
+struct OverWave {
+  int n0, n1;  // rows of the lane's sequences; -1 for none
+  template <typename F> __device__ uint32_t total(F f) const {
+    return (uint32_t)__builtin_amdgcn_readlane(wave_scan((int)(f(n0) + f(n1))), 63);
+  }
+  template <typename F> __device__ uint32_t most(F f) const { return (uint32_t)wave_max((int)max(f(n0), f(n1))); }
+};
+struct OverGroup {
+  const focus_paged_kv& c;
+  int* s_part;  // one per wave
+  template <typename F> __device__ uint32_t total(F f) const {
+    uint32_t x = 0;
+    for (int b = threadIdx.x; b < c.batch; b += kPlan) x += f(focus::paged_length(c, b));
+    return join(wave_scan((int)x), [](int x, int y) { return x + y; });
+  }
+  template <typename F> __device__ uint32_t most(F f) const {
+    uint32_t x = 0;
+    for (int b = threadIdx.x; b < c.batch; b += kPlan) x = max(x, f(focus::paged_length(c, b)));
+    return join(wave_max((int)x), [](int x, int y) { return max(x, y); });
+  }
+  template <typename Op> __device__ uint32_t join(int x, Op op) const {
+    __syncthreads();
+    if (threadIdx.x % 64 == 63) s_part[threadIdx.x / 64] = x;
+    __syncthreads();
+    x = 0;
+#pragma unroll
+    for (int w = 0; w < kPlan / 64; ++w) x = op(x, s_part[w]);
+    return (uint32_t)x;
+  }
+};
+
+// (Counted in units: the host has checked that all tables together hold fewer than 2^31.)
+template <typename Over> __device__ int chunk_rows(const Args& a, const Over& over) {
+  const int batch = a.d.cache.batch, shift = a.unit_shift, unit = 1 << shift;
+  const uint32_t target = (uint32_t)a.target;
+  // units of a sequence; its chunks of so many units
+  auto units_of = [&](int n) { return (uint32_t)(max(n, 0) + unit - 1) >> shift; };
+  auto chunks = [&](uint32_t units) {
+    return over.total([&](int n) { return n < 0 ? 0u : max(1u, (units_of(n) + units - 1) / units); });
+  };
+  const uint32_t total = over.total(units_of);
+  if (total + batch <= target) return unit;
+  const uint32_t one = (total + target - 1) / target, two = min(2 * one, 1u << 30 >> shift);
+  const uint32_t whole = max(1u, over.most(units_of));
+  if (one >= whole) return (int)(whole << shift);
+  const int longest = (int)(whole << shift);
+  const uint32_t count1 = chunks(one), count2 = chunks(two);
+  uint32_t units = one;
+  float best = estimate(a, total, count1, one << shift, longest);
+  auto better = [&](uint32_t count, uint32_t with) {
+    const float e = estimate(a, total, count, with << shift, longest);
+    if (e < best) best = e, units = with;
+  };
+  better(count2, two);
+  const uint32_t half = (one + 1) / 2;
+  better(chunks(half), half);
+  if (count1 > target && batch <= kWave && (uint32_t)batch <= target) {
+    uint32_t lo = one, hi = whole;  // too many chunks at lo, few enough at hi
+    for (int k = 0; k < 16 && hi - lo > 1; ++k) {
+      const uint32_t mid = (lo + hi) / 2;
+      const bool many = chunks(mid) > target;
+      lo = many ? mid : lo, hi = many ? hi : mid;
+    }
+    better(chunks(hi), hi);
+  }
+  better(batch, whole);
+  return (int)(units << shift);
+}
+
+// The chunk of slot i (chunks 0: none), in scalar registers: all of a wave's lanes ask for
+// the same.
+struct Chunk {
+  int b, c, n, slot0, chunks, rows;
+};
+__device__ __forceinline__ Chunk find_chunk(const Args& a, int i) {
+  const focus_paged_kv& c = a.d.cache;
+  int b = 0, n = 0, slot0 = i, chunks = 0, rows = (int)a.cap;
+  if (a.single) {
+    if (i < c.batch) b = i, n = focus::paged_length(c, i), chunks = 1;
+  } else if (a.owner) {
+    const int own = i < a.slots ? scalar(a.owner[i]) : -1;
+    if (own >= 0) {
+      const int4 info = a.info[own];
+      b = own, slot0 = info.x, chunks = info.y, n = info.z, rows = info.w;
+    }
+  } else {
+    const int two = threadIdx.x % 64 * 2;
+    const int n0 = two < c.batch ? focus::paged_length(c, two) : -1;
+    const int n1 = two + 1 < c.batch ? focus::paged_length(c, two + 1) : -1;
+    rows = scalar(a.d.split_keys ? a.d.split_keys : chunk_rows(a, OverWave{n0, n1}));
+    auto chunks_of = [&](int n) { return n < 0 ? 0 : max(1, (n - 1) / rows + 1); };
+    const int own0 = chunks_of(n0), own1 = chunks_of(n1), upto = wave_scan(own0 + own1);
+    if (i < __builtin_amdgcn_readlane(upto, 63)) {
+      const int lane = __ffsll((unsigned long long)__ballot(i < upto)) - 1;
+      const int end = __builtin_amdgcn_readlane(upto, lane), last = __builtin_amdgcn_readlane(own1, lane);
+      const bool second = i >= end - last;
+      b = 2 * lane + second;
+      n = __builtin_amdgcn_readlane(second ? n1 : n0, lane);
+      chunks = __builtin_amdgcn_readlane(second ? own1 : own0, lane);
+      slot0 = end - last - (second ? 0 : chunks);
+    }
+  }
+  slot0 = scalar(slot0);
+  return {scalar(b), i - slot0, scalar(n), slot0, scalar(chunks), scalar(rows)};
+}
+
+// The chunks of more than kWave sequences, by one workgroup.  (With every wave going through
+// all lengths by itself 4096 sequences of 200 to 400 rows, 8 KV heads of 128, took 1570 us,
+// now 900; of 128 sequences the launch would cost as much as it saves.)
+__global__ __launch_bounds__(kPlan) void paged_plan(Args a) {
+  __shared__ int s_part[kPlan / 64];
+  const focus_paged_kv& c = a.d.cache;
+  const int tid = threadIdx.x;
+  const int rows = a.d.split_keys ? a.d.split_keys : chunk_rows(a, OverGroup{c, s_part});
+  int before = 0;
+  for (int b0 = 0; b0 < c.batch; b0 += kPlan) {
+    const int b = b0 + tid, n = b < c.batch ? focus::paged_length(c, b) : 0;
+    const int own = b < c.batch ? max(1, (n - 1) / rows + 1) : 0, upto = wave_scan(own);
+    __syncthreads();  // the last round's sums are read
+    if (tid % 64 == 63) s_part[tid / 64] = upto;
+    __syncthreads();
+    int slot = before + upto - own;
+#pragma unroll
+    for (int w = 0; w < kPlan / 64; ++w) {
+      if (w < tid / 64) slot += s_part[w];
+      before += s_part[w];
+    }
+    if (b < c.batch) a.info[b] = make_int4(slot, own, n, rows);
+    for (int k = 0; k < own && slot + k < a.slots; ++k) a.owner[slot + k] = b;
+  }
+  for (int64_t i = before + tid; i < a.slots; i += kPlan) a.owner[i] = -1;
+}
 
 template <typename T, int D> struct Tile {
   static constexpr bool kBf16 = sizeof(T) == 2;
@@ -201,7 +361,7 @@ __global__ __launch_bounds__(kThreads, resident(D)) void paged_attend(Args a) {
   g0 <<= a.wide_shift;
   // waves of a KV head; this wave's head, and which of its waves it is
   const int by = kWaves >> a.wide_shift, at_head = wave >> (2 - a.wide_shift), g = g0 + at_head, among = wave & (by - 1);
-  const Chunk ch = focus::find_chunk(a.split, c, slot_id);
+  const Chunk ch = find_chunk(a, slot_id);
   if (ch.chunks == 0) return;
   const int b = ch.b, r0 = ch.c * ch.rows, r1 = min(ch.n, r0 + ch.rows);
   const bool first = g0 == 0 && tile_id == 0;
@@ -223,7 +383,7 @@ __global__ __launch_bounds__(kThreads, resident(D)) void paged_attend(Args a) {
   // rows of eight from which this lane reads K and V; the offsets of its rows in them
   const int k8 = L::kBf16 ? col / 4 * 8 : col / 8 * 8, k_in = L::kBf16 ? col % 4 : col % 8;
   const int v8 = L::kBf16 ? x * 8 : x / 2 * 8, v_in = L::kBf16 ? 0 : x % 2 * 4;
-  float* score = a.d.accumulate && col < heads ? a.score + ((int64_t)b * H + h0 + col) * a.split.cap : nullptr;
+  float* score = a.d.accumulate && col < heads ? a.score + ((int64_t)b * H + h0 + col) * a.cap : nullptr;
 
   float m, l;
   f32x4 o[L::kPer];
@@ -403,7 +563,7 @@ __global__ __launch_bounds__(kThreads, resident(D)) void paged_attend(Args a) {
 
   // (not at the start, where it would leave b in vector registers during the loops)
   if (first && ch.c == 0 && tid == 0) {
-    if (a.split.info && !a.split.owner) a.split.info[b] = make_int4(ch.slot0, ch.chunks, ch.n, ch.rows);
+    if (a.info && !a.owner) a.info[b] = make_int4(ch.slot0, ch.chunks, ch.n, ch.rows);
     if (ch.n != c.length[b]) focus::raise_err(a.d.err, FOCUS_ERR_CAPACITY);
   }
   // the waves' parts of each query head, joined
@@ -441,6 +601,25 @@ __global__ __launch_bounds__(kThreads, resident(D)) void paged_attend(Args a) {
   }
 }
 
+// Maximum and sum over a sequence's chunks of head h, by one wave.
+__device__ float2 joined(const Args& a, const int4& info, int h) {
+  const int H = a.d.n_heads, lane = threadIdx.x % 64;
+  float M = kMinit, L = 0.f;
+  for (int i = lane; i < info.y; i += 64) {
+    const float2 y = a.ml[(int64_t)(info.x + i) * H + h];
+    const float m = fmaxf(M, y.x);
+    L = L * __builtin_amdgcn_exp2f((M - m) * a.sc) + y.y * __builtin_amdgcn_exp2f((y.x - m) * a.sc);
+    M = m;
+  }
+#pragma unroll
+  for (int k = 32; k >= 1; k >>= 1) {
+    const float m2 = __shfl_xor(M, k), l2 = __shfl_xor(L, k), m = fmaxf(M, m2);
+    L = L * __builtin_amdgcn_exp2f((M - m) * a.sc) + l2 * __builtin_amdgcn_exp2f((m2 - m) * a.sc);
+    M = m;
+  }
+  return make_float2(M, L);
+}
+
 constexpr int kWeightRows = 4 * kThreads;   // rows whose weights a workgroup writes at a time
 constexpr int kMaxGroup = 512;              // query heads of a KV head
 
@@ -462,7 +641,7 @@ __global__ __launch_bounds__(kThreads) void paged_join(Args a) {
   const int part = c.batch <= kMaxGrid ? blockIdx.z : blockIdx.z % parts, g = blockIdx.x;
   const int b = blockIdx.y + (c.batch <= kMaxGrid ? 0 : blockIdx.z / parts * kMaxGrid);
   if (b >= c.batch) return;
-  const int4 info = a.split.info[b];
+  const int4 info = a.info[b];
   const int n = info.z;
   const bool merges = info.y > 1 && part < G, weighs = a.d.accumulate && part * kWeightRows < n;
   if (!merges && !weighs) return;
@@ -481,11 +660,11 @@ __global__ __launch_bounds__(kThreads) void paged_join(Args a) {
   float* w = c.weight + ((int64_t)b * K + g) * c.weight_rows;
   float4 sc[kHeads];
   float old[4];
-  const float* score = a.score + ((int64_t)b * H + g * G) * a.split.cap;
+  const float* score = a.score + ((int64_t)b * H + g * G) * a.cap;
   auto load_scores = [&](int r, int h0) {
 #pragma unroll
     for (int k = 0; k < kHeads; ++k)
-      if (r < n && h0 + k < G) sc[k] = *reinterpret_cast<const float4*>(score + (h0 + k) * a.split.cap + r);
+      if (r < n && h0 + k < G) sc[k] = *reinterpret_cast<const float4*>(score + (h0 + k) * a.cap + r);
   };
   auto load_weights = [&](int r) {
 #pragma unroll
@@ -496,7 +675,7 @@ __global__ __launch_bounds__(kThreads) void paged_join(Args a) {
   // of all heads for the weights, else of those to be merged
   const int first = weighs ? 0 : part, step = weighs ? 1 : parts;
   for (int h = first + tid / 64 * step; h < G; h += kWaves * step) {
-    const float2 ml = joined(a.ml, a.sc, info, H, g * G + h);
+    const float2 ml = joined(a, info, g * G + h);
     if (tid % 64 == 0) s_ml[h] = ml, s_inv[h] = ml.y == 0.f ? 0.f : 1.f / ml.y;
   }
   __syncthreads();
@@ -583,7 +762,7 @@ focus_status launch(Args a, const Plan& p, hipStream_t s) {
       heads * a.parts > INT32_MAX / kThreads || slots > kMaxGrid || batches * a.parts > kMaxGrid)
     return FOCUS_E_SHAPE;
   if (p.planned) {
-    hipLaunchKernelGGL(paged_plan, dim3(1), dim3(focus::kPlan), 0, s, a);
+    hipLaunchKernelGGL(paged_plan, dim3(1), dim3(kPlan), 0, s, a);
     const focus_status st = focus::launch_status();
     if (st != FOCUS_OK) return st;
   }
@@ -621,20 +800,18 @@ extern "C" focus_status focus_paged_decode(const focus_paged_decode_desc* d, foc
   Args a = {};
   a.d = *d;
   a.shift = focus::page_shift(c);
-  a.tiles = p.tiles, a.wide_shift = __builtin_ctz((unsigned)p.wide), a.units = (int)(p.groups / p.tiles);
+  a.tiles = p.tiles, a.wide_shift = __builtin_ctz((unsigned)p.wide), a.unit_shift = __builtin_ctz((unsigned)p.unit);
+  a.target = (int)p.target, a.units = (int)(p.groups / p.tiles);
   a.group = d->n_heads / c.n_kv_heads;
-  focus::Split& s = a.split;
-  s.split_keys = d->split_keys, s.unit_shift = __builtin_ctz((unsigned)p.unit), s.target = (int)p.target;
-  s.each = (float)(kStart >> a.wide_shift) + (c.dtype == FOCUS_BF16 ? 4.f : 2.f) * a.group;
-  s.cap = p.cap, s.single = p.single, s.slots = p.slots;
+  a.cap = p.cap, a.single = p.single, a.slots = p.slots;
   if (p.bytes > 0) {
-    s.info = reinterpret_cast<int4*>(ws), a.ml = reinterpret_cast<float2*>(ws + p.ml);
+    a.info = reinterpret_cast<int4*>(ws), a.ml = reinterpret_cast<float2*>(ws + p.ml);
     a.o = reinterpret_cast<float*>(ws + p.o), a.score = reinterpret_cast<float*>(ws + p.score);
   }
-  if (p.planned) s.owner = reinterpret_cast<int*>(ws + p.owner);
+  if (p.planned) a.owner = reinterpret_cast<int*>(ws + p.owner);
   const float scale = d->softmax_scale > 0.f ? d->softmax_scale : 1.0f / sqrtf((float)c.head_dim);
   a.sc = scale * kLog2e;
-  hipStream_t on = reinterpret_cast<hipStream_t>(stream);
-  if (c.dtype == FOCUS_BF16) return c.head_dim == 128 ? launch<__bf16, 128>(a, p, on) : launch<__bf16, 64>(a, p, on);
-  return c.head_dim == 128 ? launch<float, 128>(a, p, on) : launch<float, 64>(a, p, on);
+  hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+  if (c.dtype == FOCUS_BF16) return c.head_dim == 128 ? launch<__bf16, 128>(a, p, s) : launch<__bf16, 64>(a, p, s);
+  return c.head_dim == 128 ? launch<float, 128>(a, p, s) : launch<float, 64>(a, p, s);
 }
