@@ -146,6 +146,7 @@ struct Args {
   int per_head, columns;   // columns of a KV head at most, of all heads
   int unit, shares, over;  // rows of a unit; shares; units that a sequence costs besides
   bool single, fixed;   // a share is a sequence; a unit
+  int wide_from;        // shares of a sequence from which on a workgroup joins its columns
   int2* info;
   int* ends;            // null unless planned
   float2* ml;
@@ -681,8 +682,10 @@ __global__ __launch_bounds__(kThreads, resident(D, TILES, HEADS)) void attend_ro
 // of 8, 34.3 and 37.5; eight tokens of 16 of 8 000 rows, 4 096 of 16, 9.3 and 33.6 in the join alone.  Few shares are not
 // worth the workgroups: three sequences of up to 2 021 rows, 60 shares, 14.7 and 15.6.)
 //
-// The two add the partials in different orders, and which is taken follows from the batch and the
-// tables: a given split_keys, which fixes a sequence's bits, always takes the waves.
+// The two add the partials in different orders, and the rule follows from the batch and the
+// tables: with a given split_keys, which fixes a sequence's bits, its own shares alone say which,
+// 128 or more a workgroup, and both are launched where tables hold so many.  (One sequence of 262 144
+// rows in 512 shares 144 us by waves, by workgroups 113.)
 constexpr int kJoin = 256, kManyShares = 16, kWideFrom = 128, kFewColumns = 512;
 template <typename T, int D, bool WIDE>
 __global__ __launch_bounds__(kJoin) void attend_join(Args a) {
@@ -697,7 +700,7 @@ __global__ __launch_bounds__(kJoin) void attend_join(Args a) {
   const int2 info = a.info[b];
   int32_t bits = 0;
   const Tokens tok = a.d.cu_rows ? tokens_of(a, a.d.cu_rows[b], a.d.cu_rows[b + 1], bits) : Tokens{b, 1};
-  if (info.y <= 1 || cc >= tok.count * G) return;
+  if (info.y <= 1 || (info.y >= a.wide_from) != WIDE || cc >= tok.count * G) return;
   const int e = (WIDE ? blockIdx.x % kSlices * kLanes : 0) + tid % kLanes, grp = tid / kLanes;
   const float4* o = reinterpret_cast<const float4*>(a.o);
   float4 y[kFlight], sum = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -823,9 +826,13 @@ focus_status launch(Args a, const Plan& p, hipStream_t s) {
   else of_heads(kOne, std::false_type{});
   const focus_status st = focus::launch_status();
   if (st != FOCUS_OK || p.single) return st;
-  if (a.d.split_keys == 0 && columns <= kFewColumns && p.shares >= std::max<int64_t>((int64_t)kManyShares * c.batch, kWideFrom))
+  const bool given = a.d.split_keys > 0;
+  const bool wide = given ? focus::ceil_div(p.cap, p.unit) >= kWideFrom
+                          : columns <= kFewColumns && p.shares >= std::max<int64_t>((int64_t)kManyShares * c.batch, kWideFrom);
+  a.wide_from = given ? kWideFrom : wide ? 0 : INT32_MAX;
+  if (wide)
     hipLaunchKernelGGL((attend_join<T, D, true>), dim3((uint32_t)(columns * (D / 32))), dim3(kJoin), 0, s, a);
-  else
+  if (given || !wide)
     hipLaunchKernelGGL((attend_join<T, D, false>), dim3((uint32_t)focus::ceil_div(columns, kJoin / 64)), dim3(kJoin), 0, s, a);
   return focus::launch_status();
 }

@@ -340,6 +340,24 @@ def test_attend_split_keys_fix_a_sequences_bits(D, dtype):
             assert torch.equal(o1, o[:n]) and torch.equal(l1, lse[:n]), (n, width)
 
 
+@pytest.mark.parametrize("D,dtype", [(64, "bf16"), (128, "f32"), (64, "f32")])
+def test_attend_split_keys_fix_bits_of_many_shares(D, dtype):
+    """The same of sequences of 127, 128 and 150 shares, which are joined in two ways, and of
+    shorter ones beside them."""
+    rng = np.random.default_rng(44)
+    c = Cache8(rng, [127 * 128, 128 * 128, 150 * 128 - 77, 127 * 128 + 1, 300, 1, 0] + [200] * 10, 1, D, 64, 16, max_pages=400)
+    q, q64 = values(rng, (17, 32, D), dtype)
+    announce(f"attend given split, many shares {D} {dtype}")
+    o, lse = F.focus_paged_attend(q, c.dev, split_keys=128)
+    _check(c, q64, [1] * 17, (o, lse), dtype)
+    for part, width in ((slice(0, 1), 254), (slice(1, 2), 256), (slice(2, 3), 300), (slice(3, 4), 255), (slice(0, 4), 400),
+                        (slice(2, 7), 300)):
+        one = F.PagedCache8(c.dev.k, c.dev.v, c.dev.k_scale, c.dev.v_scale, c.dev.table[part, :width].contiguous(),
+                            c.dev.length[part])
+        o1, l1 = F.focus_paged_attend(q[part], one, split_keys=128)
+        assert torch.equal(o1, o[part]) and torch.equal(l1, lse[part]), (part, width)
+
+
 @pytest.mark.parametrize("K", [1, 2, 4, 6, 8])
 @pytest.mark.parametrize("D,dtype,by_head", [(64, "bf16", False), (64, "bf16", True), (128, "bf16", False), (64, "f32", False),
                                              (128, "f32", False)])
