@@ -986,6 +986,9 @@ focus_status focus_paged_append(const focus_paged_append_desc* d, focus_stream_t
  *     o[t, h]   = softmax(scale * q[t, h] . k[b, 0:n_i, g]^T) . v,  g = h / (H / H_kv)
  *     lse[t, h] = log sum exp(scale * q[t, h] . k)
  * A token with n_i <= 0 has o = 0 and lse = -inf; what it does not see has no effect.
+ * The rows of a sequence that focus_paged_extend did not serve (start[b] = -1, row_slot -1)
+ * are in no cache: they are taken for its last cached tokens, and what comes out for them is
+ * to be left aside.
  * cu_rows NULL: one token of every sequence, row b (n_rows = batch).  max_rows bounds m; rows of
  * o and lse past the last sequence's are left as they were.  o and lse may have nothing in
  * common with an input.  Scores, weights and sums are float32; each element of k and v enters

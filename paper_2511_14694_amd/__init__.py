@@ -1033,7 +1033,8 @@ def focus_paged_attend(q, cache: PagedCache8, cu_rows=None, max_rows: int = 1, o
     their rows already: q [rows, H, D] (turned; bfloat16 or float32; D 64 or 128), rows
     cu_rows[b] : cu_rows[b + 1] (int32 [batch + 1], at most max_rows of them) the last ones of
     sequence b in order, each seeing the rows up to its own (cu_rows None: one token of every
-    sequence).  Returns (o, lse); rows past cu_rows[batch] are left as they were."""
+    sequence).  Returns (o, lse); rows past cu_rows[batch] are left as they were, and those of
+    sequences that focus_paged_extend did not serve (start -1) mean nothing."""
     dev = q.get_device()
     # (what is allocated here need not be looked at again)
     if o is None:
